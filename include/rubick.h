@@ -433,6 +433,137 @@ int rubick_greedy_round_spread(rubick_ctx *ctx, const rubick_job *d_jobs, int J,
                                rubick_node *d_node_out, int32_t *d_step_log, int32_t *d_pieces, int32_t *d_class,
                                int32_t *h_steps);
 
+/* ---- operators of a training step --------------------------------------------------------------
+ * The scheduler plans with what a profile of a job measured (tau, the forward seconds of a sample, and k_bwd, the
+ * ratio of the backward to the forward pass; Section 4.3's profiling step).  These calls are the part of such a
+ * step that does not follow from the FLOPs of its matrix products: the norms around a block with the gate and the
+ * residual sum, the router of a mixture of experts with its balance loss, and a distillation loss at the head, each
+ * forward and backward.  They need no plan space; rubick_create's stream and device apply, and so do the
+ * conventions at the top of this file.
+ *
+ * Element types: RUBICK_BF16, RUBICK_F16, RUBICK_F32.  Whatever the type, sums, norms and softmax statistics are
+ * held in single precision and every output is rounded to its type once.  Distances between rows (ld_*) are in
+ * elements; rows of any alignment are taken, rows on 16-byte boundaries are the fast case.  An output may be the
+ * input that a call names as its equal (same address and distance) and must not overlap any other input.
+ * rows = 0 is allowed: reductions over no rows are written as zeros.  Results do not depend on the order in which
+ * blocks run: there are no floating-point atomics. */
+
+#define RUBICK_BF16 0
+#define RUBICK_F16  1
+#define RUBICK_F32  2
+
+#define RUBICK_MAX_NORM_COLS       16384
+#define RUBICK_MAX_EXPERTS         1024
+#define RUBICK_MAX_CHOSEN          32      /* experts per token */
+#define RUBICK_MAX_TEACHER_LOGITS  1024    /* teacher entries per row */
+
+/* flags of rubick_block_norm_desc */
+#define RUBICK_NORM_AFTER        1u   /* normalise the block's output y                        */
+#define RUBICK_NORM_BEFORE       2u   /* normalise the new stream for the next block           */
+#define RUBICK_NORM_UNIT_OFFSET  4u   /* weights are stored as their distance from one         */
+#define RUBICK_NORM_TANH_GATE    8u   /* the gate passes through tanh                          */
+
+typedef struct {
+    int64_t rows;                /* tokens, below 2^31                                                       */
+    int64_t group_rows;          /* consecutive rows that share one row of the gate (1 .. ; the last group may be
+                                    shorter): rows = one vector, a sequence's length, or 1                   */
+    int64_t ld_x, ld_y, ld_h;    /* distance between rows of x, x_out, dx_out, dx / y, dy / h, dh; >= cols     */
+    int64_t ld_gate;             /* ... of gate and dgate                                                     */
+    int32_t cols;                /* 1 .. RUBICK_MAX_NORM_COLS                                                 */
+    int32_t dtype;               /* type of every tensor but the weights, rstd and the weights' gradients     */
+    int32_t wtype;               /* type of the two weight vectors: dtype or RUBICK_F32                       */
+    uint32_t flags;
+    float   eps, alpha;          /* eps > 0; alpha = scale of the branch that joins the residual stream        */
+} rubick_block_norm_desc;
+
+/* The edge between two blocks, with rstd(v) = 1 / sqrt(mean(v^2) + eps) and o = 1 under NORM_UNIT_OFFSET, else 0:
+ *     u  = y rstd(y) (w_after + o)      (u = y without NORM_AFTER)
+ *     x_out = x + alpha g u             (g = gate, tanh(gate) or, with d_gate NULL, 1)
+ *     h  = x_out rstd(x_out) (w_before + o)          (with NORM_BEFORE; from x_out before it is rounded)
+ * d_y NULL (then d_x_out and d_gate too, no NORM_AFTER): the stream is x itself, only h is written.  A weight of
+ * NULL is a norm without weights.  d_x_out may equal d_x, d_h may equal d_y.
+ * d_rstd (optional, [rows][2] float): the two factors, for the backward pass; 0 for a norm that is not taken.
+ * Errors: EINVAL, ECUDA. */
+int rubick_block_norm_forward(rubick_ctx *ctx, const rubick_block_norm_desc *h_desc, const void *d_x, const void *d_y,
+                              const void *d_w_after, const void *d_gate, const void *d_w_before, void *d_x_out,
+                              void *d_h, float *d_rstd);
+
+/* Gradients of the same edge.  d_x_out (read with NORM_BEFORE): the stream that forward wrote (x itself when there
+ * is no y); d_dx_out: gradient that reaches x_out from behind the edge (NULL = 0), d_dh: gradient of h.  Writes d_dx
+ * and d_dy, and where not NULL d_dw_after, d_dw_before (float [cols]) and d_dgate (dtype, laid out as the gate).
+ * d_dx may equal d_dx_out, d_dy may equal d_dh or d_y.  The context keeps scratch of a few rows per SM (grown on demand).
+ * Errors: EINVAL, ENOMEM, ECUDA. */
+int rubick_block_norm_backward(rubick_ctx *ctx, const rubick_block_norm_desc *h_desc, const void *d_x_out, const void *d_y,
+                               const void *d_w_after, const void *d_gate, const void *d_w_before, const float *d_rstd,
+                               const void *d_dx_out, const void *d_dh, void *d_dx, void *d_dy, float *d_dw_after,
+                               void *d_dgate, float *d_dw_before);
+
+/* flags of rubick_router_desc */
+#define RUBICK_ROUTER_RENORM  1u      /* weights sum to one over the chosen experts                       */
+
+typedef struct {
+    int64_t rows;                /* tokens, below 2^31                                                       */
+    int64_t group_rows;          /* rows balanced together: a sequence's length, or rows for the whole batch  */
+    int64_t ld;                  /* distance between rows of logits and dlogits, >= experts                   */
+    int32_t experts;             /* 1 .. RUBICK_MAX_EXPERTS                                                   */
+    int32_t k;                   /* experts per token, 1 .. min(experts, RUBICK_MAX_CHOSEN)                    */
+    int32_t dtype;               /* type of logits and dlogits                                                */
+    uint32_t flags;
+    float   coef;                /* coefficient of the balance loss                                           */
+    int32_t reserved;            /* 0                                                                         */
+} rubick_router_desc;
+
+/* Router of a mixture of experts: p = softmax(logits) of every row, the k largest logits in descending order (ties:
+ * lowest index), their weights p (divided by their sum under ROUTER_RENORM), per group g the assignments per expert,
+ * the sums of p and the number of valid rows n_g, and
+ *     loss = coef * mean over groups with n_g > 0 of  E * sum_e (counts_e / (k n_g)) (prob_sum_e / n_g)
+ * (0 if no row is valid).  A row is valid when its mask byte is not 0 (d_mask NULL: all rows) and one of its logits is
+ * above -inf.  What a masked row holds is not looked at.  Experts whose logit is -inf are never chosen: places that
+ * cannot be filled, and those of rows that are not valid, get index -1 and weight 0.  NaN logits are not chosen either
+ * (they make the row's probabilities and the loss NaN).
+ * d_index [rows][k] int32, d_weight [rows][k] float, d_counts [G][experts] int32, d_prob_sum [G][experts] float, d_valid
+ * [G] int32, d_loss one float; G = ceil(rows / group_rows).  Errors: EINVAL, ENOMEM, ECUDA. */
+int rubick_router_forward(rubick_ctx *ctx, const rubick_router_desc *h_desc, const void *d_logits, const uint8_t *d_mask,
+                          int32_t *d_index, float *d_weight, int32_t *d_counts, float *d_prob_sum, int32_t *d_valid,
+                          float *d_loss);
+
+/* Gradient of  d_dloss[0] * loss + sum(d_dweight * weight)  with respect to the logits (the choice and the counts are
+ * held fixed).  d_index, d_weight, d_counts and d_valid are what forward wrote; d_dloss NULL = 1, d_dweight NULL = 0.  Rows
+ * whose first index is negative get zeros.  d_dlogits may equal d_logits.  Errors: EINVAL, ECUDA. */
+int rubick_router_backward(rubick_ctx *ctx, const rubick_router_desc *h_desc, const void *d_logits, const int32_t *d_index,
+                           const float *d_weight, const int32_t *d_counts, const int32_t *d_valid, const float *d_dloss,
+                           const float *d_dweight, void *d_dlogits);
+
+typedef struct {
+    int64_t rows;                /* tokens, below 2^31                                                       */
+    int64_t ld;                  /* distance between rows of z and dz, >= vocab                               */
+    int32_t vocab;               /* student logits per row, >= 1                                              */
+    int32_t k;                   /* teacher entries per row, 1 .. RUBICK_MAX_TEACHER_LOGITS                    */
+    int32_t dtype;               /* type of z and dz                                                          */
+    int32_t ttype;               /* type of the teacher's logits                                              */
+    float   temperature;         /* T > 0                                                                     */
+    int32_t reserved;            /* 0                                                                         */
+} rubick_distill_desc;
+
+/* Distillation from a teacher's largest logits.  d_index / d_teacher [rows][k]: vocabulary index (int32) and logit of
+ * the teacher's entries; an entry with an index outside 0 .. vocab - 1 or a logit of -inf does not take part.  With
+ * q = softmax(teacher / T) over a row's entries and p = softmax(z / T) over the vocabulary,
+ *     d_loss[n] = T^2 sum_j q_j (log q_j - log p_{index j})          d_lse[n] = log sum_v exp(z_v / T)
+ * Both are 0 for a row without entries (padding), whatever its z holds.  d_lse is optional.  Errors: EINVAL, ECUDA. */
+int rubick_distill_forward(rubick_ctx *ctx, const rubick_distill_desc *h_desc, const void *d_z, const int32_t *d_index,
+                           const void *d_teacher, float *d_loss, float *d_lse);
+
+/* dz = d_dloss[n] T (p - q) from forward's d_lse; 0 in rows without entries.  d_dloss NULL = 1.  An index that a row
+ * lists twice counts with the sum of its entries.  d_dz may equal d_z.  Errors: EINVAL, ECUDA. */
+int rubick_distill_backward(rubick_ctx *ctx, const rubick_distill_desc *h_desc, const void *d_z, const int32_t *d_index,
+                            const void *d_teacher, const float *d_lse, const float *d_dloss, void *d_dz);
+
+/* Both at once, for a loss whose weight per row is known beforehand: reads z once and writes dz once, where forward
+ * and backward read z twice (a row longer than a cluster's registers, 131,072 single-precision or 262,144 16-bit
+ * logits, is read twice all the same).  Outputs as theirs; d_lse is not optional here. */
+int rubick_distill_step(rubick_ctx *ctx, const rubick_distill_desc *h_desc, const void *d_z, const int32_t *d_index,
+                        const void *d_teacher, const float *d_dloss, float *d_loss, float *d_lse, void *d_dz);
+
 /* ---- measurement aids (the paper has no counterpart) ------------------------------------------- */
 
 #define RUBICK_PROBE_WRITE 0   /* float4 streaming stores over d_buf:            work = bytes written        */

@@ -58,6 +58,63 @@ class SpreadClass(C.Structure):
 
 MAX_PIECES = 32
 
+# element types and flags of the training-step operators
+BF16, F16, F32 = 0, 1, 2
+NORM_AFTER, NORM_BEFORE, NORM_UNIT_OFFSET, NORM_TANH_GATE = 1, 2, 4, 8
+ROUTER_RENORM = 1
+MAX_NORM_COLS, MAX_EXPERTS, MAX_CHOSEN, MAX_TEACHER_LOGITS = 16384, 1024, 32, 1024
+
+
+class BlockNormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("group_rows", C.c_int64), ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("ld_h", C.c_int64),
+                ("ld_gate", C.c_int64), ("cols", C.c_int32), ("dtype", C.c_int32), ("wtype", C.c_int32), ("flags", C.c_uint32),
+                ("eps", C.c_float), ("alpha", C.c_float)]
+
+
+class RouterDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("group_rows", C.c_int64), ("ld", C.c_int64), ("experts", C.c_int32), ("k", C.c_int32),
+                ("dtype", C.c_int32), ("flags", C.c_uint32), ("coef", C.c_float), ("reserved", C.c_int32)]
+
+
+class DistillDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("ld", C.c_int64), ("vocab", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32),
+                ("ttype", C.c_int32), ("temperature", C.c_float), ("reserved", C.c_int32)]
+
+
+def _type_code(dtype):
+    """RUBICK_BF16 / F16 / F32 of a torch dtype (or a code itself)."""
+    if isinstance(dtype, int):
+        return dtype
+    name = str(dtype).replace("torch.", "")
+    codes = {"bfloat16": BF16, "float16": F16, "float32": F32}
+    if name not in codes:
+        raise ValueError(f"the training-step operators take bfloat16, float16 and float32, not {name}")
+    return codes[name]
+
+
+def block_norm(rows, cols, dtype, wtype=None, *, eps=1e-5, alpha=1.0, group_rows=None, norm_after=True, norm_before=True,
+               unit_offset=False, tanh_gate=False, ld=None, ld_x=None, ld_y=None, ld_h=None, ld_gate=None):
+    """rubick_block_norm_desc.  group_rows: rows that share a gate row (None: all); ld: distance between rows of every
+    row tensor (None: cols), ld_x / ld_y / ld_h where they differ."""
+    ld = int(cols) if ld is None else int(ld)
+    flags = (NORM_AFTER * bool(norm_after) | NORM_BEFORE * bool(norm_before) | NORM_UNIT_OFFSET * bool(unit_offset)
+             | NORM_TANH_GATE * bool(tanh_gate))
+    return BlockNormDesc(int(rows), max(int(rows), 1) if group_rows is None else int(group_rows), ld if ld_x is None else int(ld_x),
+                         ld if ld_y is None else int(ld_y), ld if ld_h is None else int(ld_h), int(cols) if ld_gate is None else int(ld_gate),
+                         int(cols), _type_code(dtype), _type_code(dtype if wtype is None else wtype), flags, float(eps), float(alpha))
+
+
+def router(rows, experts, k, dtype, *, group_rows=None, coef=0.01, renorm=False, ld=None):
+    """rubick_router_desc.  group_rows: rows balanced together (None: all)."""
+    return RouterDesc(int(rows), max(int(rows), 1) if group_rows is None else int(group_rows), int(experts) if ld is None else int(ld),
+                      int(experts), int(k), _type_code(dtype), ROUTER_RENORM * bool(renorm), float(coef), 0)
+
+
+def distill(rows, vocab, k, dtype, ttype=None, *, temperature=1.0, ld=None):
+    """rubick_distill_desc.  ttype: type of the teacher's logits (None: as dtype)."""
+    return DistillDesc(int(rows), int(vocab) if ld is None else int(ld), int(vocab), int(k), _type_code(dtype),
+                       _type_code(dtype if ttype is None else ttype), float(temperature), 0)
+
 
 class Cluster(C.Structure):
     _fields_ = [("n_nodes", C.c_int32), ("n_tenants", C.c_int32), ("quota_gpus", C.POINTER(C.c_int32)),
@@ -79,7 +136,9 @@ EXPORTS = ["rubick_create", "rubick_destroy", "rubick_sync", "rubick_last_error"
            "rubick_min_resources", "rubick_fit_models",
            "rubick_greedy_round", "rubick_incremental_round", "rubick_greedy_round_noalloc", "rubick_schedule_round",
            "rubick_schedule_round_host", "rubick_incremental_event_host", "rubick_probe", "rubick_kernel_launches",
-           "rubick_set_placement", "rubick_greedy_round_spread"]
+           "rubick_set_placement", "rubick_greedy_round_spread",
+           "rubick_block_norm_forward", "rubick_block_norm_backward", "rubick_router_forward", "rubick_router_backward",
+           "rubick_distill_forward", "rubick_distill_backward", "rubick_distill_step"]
 
 _lib = None
 
@@ -127,6 +186,13 @@ def lib():
         L.rubick_greedy_round_spread.argtypes = [vp, vp, ip, vp, vp, vp, vp, C.POINTER(SpreadClass), ip, C.POINTER(Cluster), ip, vp, vp, vp,
                                                  vp, vp, C.POINTER(C.c_int32)]
         L.rubick_probe.argtypes = [vp, ip, vp, C.c_size_t, ip, C.POINTER(C.c_double)]
+        L.rubick_block_norm_forward.argtypes = [vp, C.POINTER(BlockNormDesc)] + [vp] * 8
+        L.rubick_block_norm_backward.argtypes = [vp, C.POINTER(BlockNormDesc)] + [vp] * 13
+        L.rubick_router_forward.argtypes = [vp, C.POINTER(RouterDesc)] + [vp] * 8
+        L.rubick_router_backward.argtypes = [vp, C.POINTER(RouterDesc)] + [vp] * 8
+        L.rubick_distill_forward.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 5
+        L.rubick_distill_backward.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 6
+        L.rubick_distill_step.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 7
         L.rubick_kernel_launches.argtypes = []
         L.rubick_kernel_launches.restype = C.c_ulonglong
         for name in EXPORTS:
@@ -143,6 +209,11 @@ def _ptr(x):
     if hasattr(x, "data_ptr"):
         return C.c_void_p(x.data_ptr())
     return C.c_void_p(x.ctypes.data)
+
+
+def _addr(x):
+    """Address of a torch tensor or None, as a plain integer (what an entry point with many pointers takes fastest)."""
+    return None if x is None else x.data_ptr()
 
 
 def enumerate_plans(g_levels):
@@ -376,3 +447,43 @@ class Context:
                                                              int(min(max_steps, 0x7fffffff)), _ptr(h_out), _ptr(h_node_out),
                                                              C.byref(steps)), allow=(ESTEPS,))
         return steps.value, rc == ESTEPS
+
+    # ---- operators of a training step.  Descriptors: block_norm(), router(), distill().  Tensors are the caller's, on
+    # ---- this context's device; None where the header allows NULL.  The work goes to the context's stream.
+
+    def block_norm_forward(self, desc, d_x, d_y, d_w_after, d_gate, d_w_before, d_x_out, d_h, d_rstd=None):
+        """rubick_block_norm_forward"""
+        return self._check(lib().rubick_block_norm_forward(self._h, desc, _addr(d_x), _addr(d_y), _addr(d_w_after), _addr(d_gate),
+                                                           _addr(d_w_before), _addr(d_x_out), _addr(d_h), _addr(d_rstd)))
+
+    def block_norm_backward(self, desc, d_x_out, d_y, d_w_after, d_gate, d_w_before, d_rstd, d_dx_out, d_dh, d_dx, d_dy,
+                            d_dw_after=None, d_dgate=None, d_dw_before=None):
+        """rubick_block_norm_backward"""
+        return self._check(lib().rubick_block_norm_backward(
+            self._h, desc, _addr(d_x_out), _addr(d_y), _addr(d_w_after), _addr(d_gate), _addr(d_w_before), _addr(d_rstd),
+            _addr(d_dx_out), _addr(d_dh), _addr(d_dx), _addr(d_dy), _addr(d_dw_after), _addr(d_dgate), _addr(d_dw_before)))
+
+    def router_forward(self, desc, d_logits, d_mask, d_index, d_weight, d_counts, d_prob_sum, d_valid, d_loss):
+        """rubick_router_forward"""
+        return self._check(lib().rubick_router_forward(self._h, desc, _addr(d_logits), _addr(d_mask), _addr(d_index), _addr(d_weight),
+                                                       _addr(d_counts), _addr(d_prob_sum), _addr(d_valid), _addr(d_loss)))
+
+    def router_backward(self, desc, d_logits, d_index, d_weight, d_counts, d_valid, d_dloss, d_dweight, d_dlogits):
+        """rubick_router_backward"""
+        return self._check(lib().rubick_router_backward(self._h, desc, _addr(d_logits), _addr(d_index), _addr(d_weight), _addr(d_counts),
+                                                        _addr(d_valid), _addr(d_dloss), _addr(d_dweight), _addr(d_dlogits)))
+
+    def distill_forward(self, desc, d_z, d_index, d_teacher, d_loss, d_lse=None):
+        """rubick_distill_forward"""
+        return self._check(lib().rubick_distill_forward(self._h, desc, _addr(d_z), _addr(d_index), _addr(d_teacher), _addr(d_loss),
+                                                        _addr(d_lse)))
+
+    def distill_backward(self, desc, d_z, d_index, d_teacher, d_lse, d_dloss, d_dz):
+        """rubick_distill_backward"""
+        return self._check(lib().rubick_distill_backward(self._h, desc, _addr(d_z), _addr(d_index), _addr(d_teacher), _addr(d_lse),
+                                                         _addr(d_dloss), _addr(d_dz)))
+
+    def distill_step(self, desc, d_z, d_index, d_teacher, d_dloss, d_loss, d_lse, d_dz):
+        """rubick_distill_step"""
+        return self._check(lib().rubick_distill_step(self._h, desc, _addr(d_z), _addr(d_index), _addr(d_teacher), _addr(d_dloss),
+                                                     _addr(d_loss), _addr(d_lse), _addr(d_dz)))

@@ -106,6 +106,8 @@ struct rubick_ctx {
     int inc_cur;                        // which of the two state buffers holds the last result
     rubick_assignment *d_inc_state[2]; rubick_node *d_inc_nodes[2]; rubick_reconf *d_inc_reconf; rubick_job *d_inc_jobs;
     size_t cap_inc_state[2], cap_inc_nodes[2], cap_inc_reconf, cap_inc_jobs;
+    void *d_train; size_t cap_train;                // scratch of the training-step operators, in bytes
+    uint32_t *d_tickets; size_t cap_tickets;        // their arrival counters, zero between calls
     int tile_jobs;                      // job tile of rubick_schedule_round
     int num_sms;
     std::string err;

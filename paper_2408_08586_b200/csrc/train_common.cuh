@@ -1,0 +1,219 @@
+// What the training-step operators share: element types, 16-byte rows in registers, reductions.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "rubick_internal.cuh"
+
+namespace rubick {
+namespace train {
+
+using bf16 = __nv_bfloat16;
+using f16 = __half;
+
+__device__ __forceinline__ float to_f(float v) { return v; }
+__device__ __forceinline__ float to_f(bf16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_f(f16 v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ bf16 from_f<bf16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ f16 from_f<f16>(float v) { return __float2half_rn(v); }
+
+// elements of T in 16 bytes
+template <typename T> struct Lanes { static constexpr int N = 16 / int(sizeof(T)); };
+
+__device__ __forceinline__ void unpack(const uint4 &r, float (&v)[4])
+{
+    v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+}
+// a bf16 is the upper half of a float: two integer operations unpack a pair
+__device__ __forceinline__ void unpack_pair(uint32_t w, bf16, float &a, float &b)
+{
+    a = __uint_as_float(w << 16); b = __uint_as_float(w & 0xffff0000u);
+}
+__device__ __forceinline__ void unpack_pair(uint32_t w, f16, float &a, float &b)
+{
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+    a = f.x; b = f.y;
+}
+__device__ __forceinline__ uint32_t pack_pair(float a, float b, bf16)
+{
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+__device__ __forceinline__ uint32_t pack_pair(float a, float b, f16)
+{
+    const __half2 p = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&p);
+}
+template <typename T> __device__ __forceinline__ void unpack16(const uint4 &r, float (&v)[Lanes<T>::N])
+{
+    if constexpr (sizeof(T) == 4) {
+        unpack(r, v);
+    } else {
+        unpack_pair(r.x, T(), v[0], v[1]); unpack_pair(r.y, T(), v[2], v[3]);
+        unpack_pair(r.z, T(), v[4], v[5]); unpack_pair(r.w, T(), v[6], v[7]);
+    }
+}
+template <typename T> __device__ __forceinline__ uint4 pack16(const float (&v)[Lanes<T>::N])
+{
+    uint4 r;
+    if constexpr (sizeof(T) == 4) {
+        r.x = __float_as_uint(v[0]); r.y = __float_as_uint(v[1]); r.z = __float_as_uint(v[2]); r.w = __float_as_uint(v[3]);
+    } else {
+        r.x = pack_pair(v[0], v[1], T()); r.y = pack_pair(v[2], v[3], T());
+        r.z = pack_pair(v[4], v[5], T()); r.w = pack_pair(v[6], v[7], T());
+    }
+    return r;
+}
+
+// Streaming 16-byte accesses: each byte of a row tensor is used once, so it is kept out of L1.
+__device__ __forceinline__ uint4 ld_stream(const void *p)
+{
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+__device__ __forceinline__ void st_stream(void *p, const uint4 &r)
+{
+    asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w) : "memory");
+}
+
+// VE consecutive elements of a row from column c (VE = 1, or 16 bytes' worth on a 16-byte boundary); columns from
+// `cols` on are not touched and read as 0.
+template <typename T, int VE> __device__ __forceinline__ void load_cols(const T *row, int c, int cols, float (&v)[VE])
+{
+    if constexpr (VE == Lanes<T>::N) {
+        if (c + VE <= cols) { unpack16<T>(ld_stream(row + c), v); return; }
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) v[e] = c + e < cols ? to_f(row[c + e]) : 0.f;
+}
+template <typename T, int VE> __device__ __forceinline__ void store_cols(T *row, int c, int cols, const float (&v)[VE])
+{
+    if constexpr (VE == Lanes<T>::N) {
+        if (c + VE <= cols) { st_stream(row + c, pack16<T>(v)); return; }
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) if (c + e < cols) row[c + e] = from_f<T>(v[e]);
+}
+// VE elements of a row as they came from memory, so that a row waiting for its reduction takes half the registers
+template <typename T, int VE> struct Raw {
+    static_assert(VE == 1 || VE == Lanes<T>::N, "one element or 16 bytes");
+    uint4 r;
+    __device__ __forceinline__ void load(const T *row, int c, int cols)
+    {
+        if (c + VE <= cols) { r = ld_stream(row + c); return; }
+        float v[VE];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) v[e] = c + e < cols ? to_f(row[c + e]) : 0.f;
+        r = pack16<T>(v);
+    }
+    __device__ __forceinline__ void zero() { r = make_uint4(0u, 0u, 0u, 0u); }
+    __device__ __forceinline__ void get(float (&v)[VE]) const { unpack16<T>(r, v); }
+};
+template <typename T> struct Raw<T, 1> {
+    float r;
+    __device__ __forceinline__ void load(const T *row, int c, int cols) { r = c < cols ? to_f(row[c]) : 0.f; }
+    __device__ __forceinline__ void zero() { r = 0.f; }
+    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = r; }
+};
+__device__ __forceinline__ uint4 ld_cached(const void *p)
+{
+    uint4 r;
+    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+// the same for a small vector that many rows read (kept in L1 and read again for each row: holding it in registers
+// would cost the registers that rows in flight need), with a value for the columns past the end
+template <typename W, int VE> __device__ __forceinline__ void load_shared_cols(const W *w, int c, int cols, float (&v)[VE], float other)
+{
+    if constexpr (VE > 1) {
+        if (c + VE <= cols) {
+            constexpr int N = Lanes<W>::N;
+#pragma unroll
+            for (int i = 0; i < VE; i += N) {
+                float part[N];
+                unpack16<W>(ld_cached(w + c + i), part);
+#pragma unroll
+                for (int e = 0; e < N && i + e < VE; ++e) v[i + e] = part[e];
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) v[e] = c + e < cols ? to_f(w[c + e]) : other;
+}
+
+__device__ __forceinline__ float warp_sum(float v)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max(float v)
+{
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+
+inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+}  // namespace train
+
+// argument blocks of the kernels, filled by the entry points
+struct NormArgs {
+    rubick_block_norm_desc d;
+    const void *x, *y, *w_after, *gate, *w_before;
+    void *x_out, *h;
+    float *rstd;
+    // backward
+    const float *rstd_in;
+    const void *dx_out, *dh;
+    void *dx, *dy, *dgate;
+    float *dw_after, *dw_before;
+    float *part;                 // scratch: partial column sums of the row chunks
+    int64_t chunk_rows;
+    int n_chunks;
+};
+struct RouterArgs {
+    rubick_router_desc d;
+    const void *logits;
+    const uint8_t *mask;
+    int32_t *index; float *weight; int32_t *counts; float *prob_sum; int32_t *valid; float *loss;
+    // backward
+    const int32_t *index_in; const float *weight_in; const int32_t *counts_in; const int32_t *valid_in;
+    const float *dloss, *dweight;
+    void *dlogits;
+    // scratch
+    float *part;                 // [G][chunks][experts] probability sums
+    int32_t *part_counts;        // [G][chunks][experts + 1] assignments, valid rows
+    float *group_loss;           // [G] loss of a group (-1: no valid row)
+    uint32_t *tickets;           // [G + 1] arrivals, zero between calls
+    int64_t groups;
+    int chunks;                  // row chunks of a group
+};
+struct DistillArgs {
+    rubick_distill_desc d;
+    const void *z, *teacher;
+    const int32_t *index;
+    const float *lse_in, *dloss;
+    float *loss, *lse;
+    void *dz;
+};
+
+size_t norm_backward_scratch(const NormArgs &a, int num_sms, int64_t *chunk_rows, int *n_chunks);
+cudaError_t launch_norm_forward(const NormArgs &a, int num_sms, cudaStream_t st);
+cudaError_t launch_norm_backward(const NormArgs &a, int num_sms, cudaStream_t st);
+int router_chunks(const RouterArgs &a, int num_sms);
+cudaError_t launch_router_forward(const RouterArgs &a, int num_sms, cudaStream_t st);
+cudaError_t launch_router_backward(const RouterArgs &a, int num_sms, cudaStream_t st);
+cudaError_t launch_distill_forward(const DistillArgs &a, int num_sms, cudaStream_t st);
+cudaError_t launch_distill_backward(const DistillArgs &a, int num_sms, cudaStream_t st);
+cudaError_t launch_distill_step(const DistillArgs &a, int num_sms, cudaStream_t st);
+
+}  // namespace rubick
