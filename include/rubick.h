@@ -482,7 +482,7 @@ typedef struct {
  *     h  = x_out rstd(x_out) (w_before + o)          (with NORM_BEFORE; from x_out before it is rounded)
  * d_y NULL (then d_x_out and d_gate too, no NORM_AFTER): the stream is x itself, only h is written.  A weight of
  * NULL is a norm without weights.  d_x_out may equal d_x, d_h may equal d_y.
- * d_rstd (optional, [rows][2] float): the two factors, for the backward pass; 0 for a norm that is not taken.
+ * d_rstd (optional, [rows][2] float, 8-byte aligned): the two factors, for the backward pass; 0 for a norm that is not taken.
  * Errors: EINVAL, ECUDA. */
 int rubick_block_norm_forward(rubick_ctx *ctx, const rubick_block_norm_desc *h_desc, const void *d_x, const void *d_y,
                               const void *d_w_after, const void *d_gate, const void *d_w_before, void *d_x_out,

@@ -115,6 +115,10 @@ int rubick_sync(rubick_ctx *ctx)
     CUDA_TRY(ctx, cudaStreamSynchronize(ctx->stream), "cudaStreamSynchronize");
     uint32_t st = 0;
     CUDA_TRY(ctx, cudaMemcpy(&st, ctx->d_status, 4, cudaMemcpyDeviceToHost), "read status");
+    if (st & DS_COPY_LOST) {
+        cudaMemset(ctx->d_status, 0, 4);
+        return fail(ctx, RUBICK_ECUDA, "a copy into shared memory did not arrive: the results of the training-step operators are not valid");
+    }
     if (st & DS_FEAS_NOT_THRESHOLD) {
         cudaMemset(ctx->d_status, 0, 4);
         return fail(ctx, RUBICK_ESTATE, "a feasibility word is not a threshold in the memory-level index");

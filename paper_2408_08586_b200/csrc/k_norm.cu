@@ -23,6 +23,15 @@ using namespace train;
 
 namespace {
 
+// tanh(x) and its slope 4 e / (1 + e)^2, e = e^(-2|x|), which keeps its digits where tanh is close to one (1 - tanh^2
+// does not).
+__device__ __forceinline__ float tanh_slope(float x, float &slope)
+{
+    const float e = expf(-2.f * fabsf(x)), inv = __fdividef(1.f, 1.f + e);
+    slope = 4.f * e * inv * inv;
+    return tanhf(x);
+}
+
 // sum of v[0..N) over the TPR threads of a row; `red` has a slot per warp of the block, alternated by the caller
 template <int N> __device__ __forceinline__ void row_sum(float (&v)[N], float *red, int warps, int row_slot)
 {
@@ -132,15 +141,18 @@ __device__ __forceinline__ float *part_row(const NormArgs &a, int which, int chu
 // where the whole group is in the chunk, a partial sum otherwise.
 template <typename T, int VE, int NV>
 __device__ __forceinline__ void flush_gate(const NormArgs &a, int chunk, int64_t begin, int64_t end_row, int64_t group, int tpr,
-                                           float (&acc)[NV][VE], const float (&g)[NV][VE])
+                                           float (&acc)[NV][VE])
 {
     const int64_t g0 = group * a.d.group_rows;
     const int64_t g1 = g0 + a.d.group_rows < a.d.rows ? g0 + a.d.group_rows : a.d.rows;
-    if (a.d.flags & RUBICK_NORM_TANH_GATE) {      // g holds tanh(gate)
+    if (a.d.flags & RUBICK_NORM_TANH_GATE) {
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            float g[VE], slope;
+            load_shared_cols<T, VE>(static_cast<const T *>(a.gate) + group * a.d.ld_gate, (i * tpr + int(threadIdx.x)) * VE, a.d.cols, g, 0.f);
 #pragma unroll
-            for (int e = 0; e < VE; ++e) acc[i][e] *= 1.f - g[i][e] * g[i][e];
+            for (int e = 0; e < VE; ++e) { tanh_slope(g[e], slope); acc[i][e] *= slope; }
+        }
     }
     if (!a.dgate) {
         // nobody asked for it
@@ -207,7 +219,7 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
             if (need_y) yr[i].load(static_cast<const T *>(a.y) + row * a.d.ld_y, c, end);
         }
         if (a.gate && live && row >= group_end) {
-            if (group >= 0) flush_gate<T, VE, NV>(a, chunk, begin, stop, group, tpr, acc_g, g);
+            if (group >= 0) flush_gate<T, VE, NV>(a, chunk, begin, stop, group, tpr, acc_g);
             group = row / a.d.group_rows;
             group_end = (group + 1) * a.d.group_rows;
             const T *gate = static_cast<const T *>(a.gate) + group * a.d.ld_gate;
@@ -264,7 +276,7 @@ __global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constan
         }
     }
     if (chunk >= a.n_chunks) return;
-    if (group >= 0) flush_gate<T, VE, NV>(a, chunk, begin, stop, group, tpr, acc_g, g);
+    if (group >= 0) flush_gate<T, VE, NV>(a, chunk, begin, stop, group, tpr, acc_g);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -302,7 +314,7 @@ __global__ void __launch_bounds__(512) norm_backward_wide_kernel(const __grid_co
                 for (int c = int(threadIdx.x) * VE; c < cols; c += int(blockDim.x) * VE)
                     for (int e = 0; e < VE && c + e < cols; ++e) {
                         float v = sums[2 * cols + c + e];
-                        if (th) { const float t = tanhf(to_f(gate[c + e])); v *= 1.f - t * t; }
+                        if (th) { float slope; tanh_slope(to_f(gate[c + e]), slope); v *= slope; }
                         if (whole) static_cast<T *>(a.dgate)[group * a.d.ld_gate + c + e] = from_f<T>(v);
                         else part_row(a, g0 < begin ? 2 : 3, chunk)[c + e] = v;
                         sums[2 * cols + c + e] = 0.f;
@@ -367,6 +379,376 @@ __global__ void __launch_bounds__(512) norm_backward_wide_kernel(const __grid_co
         }
 }
 
+// ---- rows through a ring of shared-memory stages ---------------------------------------------------------------
+//
+// Where every row is a whole number of 16-byte units, a block takes a run of consecutive rows and one thread copies
+// them with the bulk-copy engine, several rows ahead: the copies in flight do not depend on how many warps are
+// waiting, and a row that waits for its sums holds no registers.  What is the same for all rows of a gate group,
+// k = alpha g W_after, is kept per column; a column's gradients of gate and weight are both
+// sum G yh times a factor of the group, so one running sum serves both:
+//   dgate = g' alpha W_after t,   dW_after += alpha g t,   t = sum over the group's rows of G yh.
+
+constexpr int RING_MOST = 8;      // stages
+
+struct Ring {
+    int stages, tensors;
+    int i_x, i_y, i_dxo, i_dh, i_gate;    // place of a tensor in a stage, -1: not copied
+    uint32_t row_bytes;
+};
+
+// One barrier for the threads of a block (a warp where it is one).
+__device__ __forceinline__ void row_barrier(int warps) { if (warps == 1) __syncwarp(); else __syncthreads(); }
+
+// Sums of N values over the block; red: N x 16 words, those of absent warps 0.  Every thread adds up the warps' sums
+// itself: a handful of 16-byte loads instead of a second chain of shuffles.
+template <int N> __device__ __forceinline__ void ring_sum(const f2 (&in)[N], float (&v)[N], float *red, int warps)
+{
+    static_assert(N == 1 || N == 3, "one sum or three");
+    const int lane = threadIdx.x & 31;
+    if constexpr (N == 1) {
+        v[0] = warp_sum(lo(in[0]) + hi(in[0]));
+        if (warps > 1 && lane == 0) red[threadIdx.x >> 5] = v[0];
+    } else {
+        // two exchanges leave a quarter of the warp with one sum each (the fourth is 0), three more steps finish it:
+        // 6 shuffles instead of 15
+        const float a0 = lo(in[0]) + hi(in[0]), a1 = lo(in[1]) + hi(in[1]), a2 = lo(in[2]) + hi(in[2]);
+        const bool up = lane & 16, odd = lane & 8;
+        const float x0 = (up ? a2 : a0) + __shfl_xor_sync(0xffffffffu, up ? a0 : a2, 16);
+        const float x1 = (up ? 0.f : a1) + __shfl_xor_sync(0xffffffffu, up ? a1 : 0.f, 16);
+        float z = (odd ? x1 : x0) + __shfl_xor_sync(0xffffffffu, odd ? x0 : x1, 8);
+#pragma unroll
+        for (int o = 4; o; o >>= 1) z += __shfl_xor_sync(0xffffffffu, z, o);
+        if (warps == 1) {
+            v[0] = __shfl_sync(0xffffffffu, z, 0); v[1] = __shfl_sync(0xffffffffu, z, 8); v[2] = __shfl_sync(0xffffffffu, z, 16);
+        } else if ((lane & 7) == 0 && lane < 24) {
+            red[(lane >> 3) * 16 + (threadIdx.x >> 5)] = z;
+        }
+    }
+    if (warps == 1) { __syncwarp(); return; }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = 0.f;
+    for (int w = 0; w < warps; w += 4)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float4 t = *reinterpret_cast<const float4 *>(red + i * 16 + w);
+            v[i] += (t.x + t.y) + (t.z + t.w);
+        }
+}
+
+// The copies of row `row` into stage `s`, by one thread.
+template <typename T> __device__ __forceinline__ void ring_issue(const NormArgs &a, const Ring &r, uint8_t *smem, uint64_t *bars, int s, int64_t row)
+{
+    uint8_t *stage = smem + size_t(s) * r.tensors * r.row_bytes;
+    bar_expect(bars + s, r.row_bytes * r.tensors);
+    if (r.i_x >= 0) bulk_load(stage + r.i_x * r.row_bytes, static_cast<const T *>(a.x) + row * a.d.ld_x, r.row_bytes, bars + s);
+    if (r.i_y >= 0) bulk_load(stage + r.i_y * r.row_bytes, static_cast<const T *>(a.y) + row * a.d.ld_y, r.row_bytes, bars + s);
+    if (r.i_dxo >= 0) bulk_load(stage + r.i_dxo * r.row_bytes, static_cast<const T *>(a.dx_out) + row * a.d.ld_x, r.row_bytes, bars + s);
+    if (r.i_dh >= 0) bulk_load(stage + r.i_dh * r.row_bytes, static_cast<const T *>(a.dh) + row * a.d.ld_h, r.row_bytes, bars + s);
+    if (r.i_gate >= 0) bulk_load(stage + r.i_gate * r.row_bytes, static_cast<const T *>(a.gate) + (row / a.d.group_rows) * a.d.ld_gate, r.row_bytes, bars + s);
+}
+
+template <typename T, int VP> __device__ __forceinline__ void stage_cols(const uint8_t *tensor, int c, f2 (&v)[VP])
+{
+    unpack16<T>(*reinterpret_cast<const uint4 *>(tensor + size_t(c) * sizeof(T)), v);
+}
+
+template <int VP> __device__ __forceinline__ void zero_cols(f2 (&v)[VP])
+{
+#pragma unroll
+    for (int e = 0; e < VP; ++e) v[e] = 0ull;
+}
+
+// k = alpha g W_after of this thread's columns for the gate row at `gate` (NULL: g = 1)
+template <typename T, typename W, int VE, int NV>
+__device__ __forceinline__ void group_factors(const NormArgs &a, const T *gate, int tpr, float o, f2 (&k)[NV][VE / 2])
+{
+    const bool th = a.d.flags & RUBICK_NORM_TANH_GATE;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * tpr + int(threadIdx.x)) * VE;
+        float w[VE], g[VE];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) { w[e] = 1.f - o; g[e] = 1.f; }
+        if (c < a.d.cols) {
+            if (a.w_after) load_shared_cols<W, VE>(static_cast<const W *>(a.w_after), c, a.d.cols, w, 0.f);
+            if (gate) unpack16<T>(*reinterpret_cast<const uint4 *>(gate + c), g);
+        }
+#pragma unroll
+        for (int e = 0; e < VE; e += 2)
+            k[i][e / 2] = pair(a.d.alpha * (th ? tanhf(g[e]) : g[e]) * (w[e] + o), a.d.alpha * (th ? tanhf(g[e + 1]) : g[e + 1]) * (w[e + 1] + o));
+    }
+}
+
+// W_before of this thread's columns
+template <typename W, int VE, int NV> __device__ __forceinline__ void before_factors(const NormArgs &a, int tpr, float o, f2 (&wb)[NV][VE / 2])
+{
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * tpr + int(threadIdx.x)) * VE;
+        float w[VE];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) w[e] = 1.f - o;
+        if (a.w_before && c < a.d.cols) load_shared_cols<W, VE>(static_cast<const W *>(a.w_before), c, a.d.cols, w, 0.f);
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) wb[i][e / 2] = pair(w[e] + o, w[e + 1] + o);
+    }
+}
+
+// FULL: both norms and a block between them, known when the kernel is compiled; 96 registers: 640 threads an SM
+template <typename T, typename W, int NV, bool FULL>
+__global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ Ring r)
+{
+    constexpr int VE = Lanes<T>::N, VP = VE / 2;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(16) float red[4][16];                  // one row's sums may still be read when the next row's are written
+    __shared__ __align__(8) uint64_t bars[RING_MOST];
+    const int tpr = blockDim.x, warps = tpr >> 5, cols = a.d.cols;
+    const int64_t begin = blockIdx.x * a.chunk_rows;
+    const int n = int(begin + a.chunk_rows < a.d.rows ? a.chunk_rows : a.d.rows - begin);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < r.stages; ++s) bar_init(bars + s);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T>(a, r, smem, bars, s, begin + s);
+    }
+    if (threadIdx.x < 32) {                       // the 64 words by one warp: the smallest block has no more
+        (&red[0][0])[threadIdx.x] = 0.f;
+        (&red[0][0])[threadIdx.x + 32] = 0.f;
+    }
+    const bool block = FULL || a.y, after = FULL || (a.d.flags & RUBICK_NORM_AFTER), before = FULL || (a.d.flags & RUBICK_NORM_BEFORE);
+    const float o = a.d.flags & RUBICK_NORM_UNIT_OFFSET ? 1.f : 0.f, inv_cols = 1.f / float(cols);
+    f2 wb[NV][VP], k[NV][VP];
+    before_factors<W, VE, NV>(a, tpr, o, wb);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VP; ++e) k[i][e] = 0ull;
+    __syncthreads();
+    T *x_out = static_cast<T *>(a.x_out) + begin * a.d.ld_x, *h = static_cast<T *>(a.h) + begin * a.d.ld_h;
+    int64_t group_end = begin;
+    bool lost = false;
+    int s = 0;
+    uint32_t parity = 0;
+    for (int i_row = 0; i_row < n; ++i_row) {
+        const int64_t row = begin + i_row;
+        const uint8_t *stage = smem + size_t(s) * r.tensors * r.row_bytes;
+        if (!lost && !bar_wait(bars + s, parity)) { lost = true; atomicOr(a.status, DS_COPY_LOST); }
+        if (block && row >= group_end) {
+            const int64_t group = row / a.d.group_rows;
+            group_end = (group + 1) * a.d.group_rows;
+            const T *gate = !a.gate ? nullptr : r.i_gate >= 0 ? reinterpret_cast<const T *>(stage + r.i_gate * r.row_bytes)
+                                                              : static_cast<const T *>(a.gate) + group * a.d.ld_gate;
+            group_factors<T, W, VE, NV>(a, gate, tpr, o, k);
+        }
+        f2 v[NV][VP], y[NV][VP], part[1] = {0ull};
+        float sum[1], ra = 0.f, rb = 0.f, scale = 1.f;
+        if (after) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * tpr + int(threadIdx.x)) * VE;
+                if (c < cols) {
+                    stage_cols<T, VP>(stage + r.i_y * r.row_bytes, c, y[i]);
+#pragma unroll
+                    for (int e = 0; e < VP; ++e) part[0] = fma2(y[i][e], y[i][e], part[0]);
+                }
+            }
+            ring_sum<1>(part, sum, red[i_row & 1], warps);
+            scale = ra = rsqrtf(sum[0] * inv_cols + a.d.eps);
+        } else row_barrier(warps);
+        // every thread has left the stage of the row before
+        if (threadIdx.x == 0 && i_row >= 1 && i_row - 1 + r.stages < n)
+            ring_issue<T>(a, r, smem, bars, s ? s - 1 : r.stages - 1, row - 1 + r.stages);
+        part[0] = 0ull;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * tpr + int(threadIdx.x)) * VE;
+            if (c < cols) {
+                stage_cols<T, VP>(stage + r.i_x * r.row_bytes, c, v[i]);
+                if (block) {
+                    if (!after) stage_cols<T, VP>(stage + r.i_y * r.row_bytes, c, y[i]);
+#pragma unroll
+                    for (int e = 0; e < VP; ++e) v[i][e] = fma2(mul2(k[i][e], both(scale)), y[i][e], v[i][e]);
+                    st_stream(x_out + c, pack16<T>(v[i]));
+                }
+#pragma unroll
+                for (int e = 0; e < VP; ++e) part[0] = fma2(v[i][e], v[i][e], part[0]);
+            }
+        }
+        if (before) {
+            ring_sum<1>(part, sum, red[2 + (i_row & 1)], warps);
+            rb = rsqrtf(sum[0] * inv_cols + a.d.eps);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = (i * tpr + int(threadIdx.x)) * VE;
+                if (c < cols) {
+#pragma unroll
+                    for (int e = 0; e < VP; ++e) v[i][e] = mul2(mul2(v[i][e], both(rb)), wb[i][e]);
+                    st_stream(h + c, pack16<T>(v[i]));
+                }
+            }
+        }
+        if (a.rstd && threadIdx.x == 0) *reinterpret_cast<float2 *>(a.rstd + 2 * row) = make_float2(ra, rb);
+        x_out += a.d.ld_x;
+        h += a.d.ld_h;
+        if (++s == r.stages) { s = 0; parity ^= 1u; }
+    }
+}
+
+// the gradients of a gate group whose rows this chunk has summed up in t
+template <typename T, typename W, int VE, int NV>
+__device__ __forceinline__ void ring_flush(const NormArgs &a, int chunk, int64_t begin, int64_t stop, int64_t group, const T *gate, int tpr, float o,
+                                           f2 (&t)[NV][VE / 2], f2 (&acc_a)[NV][VE / 2])
+{
+    const int64_t g0 = group * a.d.group_rows;
+    const int64_t g1 = g0 + a.d.group_rows < a.d.rows ? g0 + a.d.group_rows : a.d.rows;
+    const bool whole = g0 >= begin && g1 <= stop, th = a.d.flags & RUBICK_NORM_TANH_GATE;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * tpr + int(threadIdx.x)) * VE;
+        if (c >= a.d.cols) continue;
+        float w[VE], g[VE], d[VE];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) { w[e] = 1.f - o; g[e] = 1.f; }
+        if (a.w_after) load_shared_cols<W, VE>(static_cast<const W *>(a.w_after), c, a.d.cols, w, 0.f);
+        if (gate) unpack16<T>(*reinterpret_cast<const uint4 *>(gate + c), g);
+#pragma unroll
+        for (int e = 0; e < VE; e += 2) {
+            float slope0 = 1.f, slope1 = 1.f;
+            if (th) { g[e] = tanh_slope(g[e], slope0); g[e + 1] = tanh_slope(g[e + 1], slope1); }
+            const f2 at = mul2(both(a.d.alpha), t[i][e / 2]);
+            acc_a[i][e / 2] = fma2(pair(g[e], g[e + 1]), at, acc_a[i][e / 2]);
+            d[e] = lo(at) * (w[e] + o) * slope0;
+            d[e + 1] = hi(at) * (w[e + 1] + o) * slope1;
+            t[i][e / 2] = 0ull;
+        }
+        if (!a.dgate) continue;
+        if (whole) {
+            st_stream(static_cast<T *>(a.dgate) + group * a.d.ld_gate + c, pack16<T>(d));
+        } else {
+            float *p = part_row(a, g0 < begin ? 2 : 3, chunk) + c;
+#pragma unroll
+            for (int e = 0; e < VE; e += 4) *reinterpret_cast<float4 *>(p + e) = make_float4(d[e], d[e + 1], d[e + 2], d[e + 3]);
+        }
+    }
+}
+
+template <typename T, typename W, int NV, bool FULL>
+__global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ Ring r)
+{
+    constexpr int VE = Lanes<T>::N, VP = VE / 2;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(16) float red[2][3 * 16];
+    __shared__ __align__(8) uint64_t bars[RING_MOST];
+    const int tpr = blockDim.x, warps = tpr >> 5, cols = a.d.cols, chunk = blockIdx.x;
+    const int64_t begin = chunk * a.chunk_rows;
+    const int n = int(begin + a.chunk_rows < a.d.rows ? a.chunk_rows : a.d.rows - begin);
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < r.stages; ++s) bar_init(bars + s);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T>(a, r, smem, bars, s, begin + s);
+    }
+    if (threadIdx.x < 32) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) (&red[0][0])[threadIdx.x + 32 * i] = 0.f;
+    }
+    const bool block = FULL || a.y, after = FULL || (a.d.flags & RUBICK_NORM_AFTER), before = FULL || (a.d.flags & RUBICK_NORM_BEFORE);
+    const bool stream = FULL || a.dx_out, need_y = FULL || r.i_y >= 0;
+    const float o = a.d.flags & RUBICK_NORM_UNIT_OFFSET ? 1.f : 0.f, inv_cols = 1.f / float(cols);
+    f2 wb[NV][VP], k[NV][VP], t[NV][VP], acc_a[NV][VP], acc_b[NV][VP];
+    before_factors<W, VE, NV>(a, tpr, o, wb);
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < VP; ++e) k[i][e] = t[i][e] = acc_a[i][e] = acc_b[i][e] = 0ull;
+    float2 next = make_float2(1.f, 0.f);
+    if (a.rstd_in) next = *reinterpret_cast<const float2 *>(a.rstd_in + 2 * begin);
+    __syncthreads();
+    T *dx = static_cast<T *>(a.dx) + begin * a.d.ld_x, *dy = static_cast<T *>(a.dy) + begin * a.d.ld_y;
+    int64_t group = -1, group_end = begin;
+    const T *gate = nullptr;                      // of the current group
+    bool lost = false;
+    int s = 0;
+    uint32_t parity = 0;
+    for (int i_row = 0; i_row < n; ++i_row) {
+        const int64_t row = begin + i_row;
+        const uint8_t *stage = smem + size_t(s) * r.tensors * r.row_bytes;
+        const float ra = after ? next.x : 1.f, rb = before ? next.y : 0.f;
+        if (a.rstd_in && i_row + 1 < n) next = *reinterpret_cast<const float2 *>(a.rstd_in + 2 * row + 2);
+        if (!lost && !bar_wait(bars + s, parity)) { lost = true; atomicOr(a.status, DS_COPY_LOST); }
+        if (block && row >= group_end) {
+            // the stage of the row before, where its gate row may lie, is still untouched
+            if (group >= 0) ring_flush<T, W, VE, NV>(a, chunk, begin, begin + n, group, gate, tpr, o, t, acc_a);
+            group = row / a.d.group_rows;
+            group_end = (group + 1) * a.d.group_rows;
+            gate = a.gate ? static_cast<const T *>(a.gate) + group * a.d.ld_gate : nullptr;
+            group_factors<T, W, VE, NV>(a, r.i_gate >= 0 ? reinterpret_cast<const T *>(stage + r.i_gate * r.row_bytes) : gate, tpr, o, k);
+        }
+        if (r.i_gate >= 0) gate = reinterpret_cast<const T *>(stage + r.i_gate * r.row_bytes);
+        f2 part[3] = {0ull, 0ull, 0ull};
+        const f2 rb2 = both(rb);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * tpr + int(threadIdx.x)) * VE;
+            if (c < cols) {
+                f2 d[VP], x[VP], h[VP], y[VP];
+                if (stream) stage_cols<T, VP>(stage + r.i_dxo * r.row_bytes, c, d); else zero_cols(d);
+                if (before) stage_cols<T, VP>(stage + r.i_x * r.row_bytes, c, x); else zero_cols(x);
+                if (before) stage_cols<T, VP>(stage + r.i_dh * r.row_bytes, c, h); else zero_cols(h);
+                if (need_y) stage_cols<T, VP>(stage + r.i_y * r.row_bytes, c, y); else zero_cols(y);
+#pragma unroll
+                for (int e = 0; e < VP; ++e) {
+                    // the sums without the row's factors ra and rb, which come in behind the reduction
+                    const f2 hw = mul2(h[e], wb[i][e]), q = mul2(k[i][e], y[e]);
+                    acc_b[i][e] = fma2(mul2(h[e], rb2), x[e], acc_b[i][e]);
+                    part[0] = fma2(hw, x[e], part[0]);
+                    part[1] = fma2(q, fma2(rb2, hw, d[e]), part[1]);
+                    part[2] = fma2(q, x[e], part[2]);
+                }
+            }
+        }
+        float sum[3];
+        ring_sum<3>(part, sum, red[i_row & 1], warps);
+        if (threadIdx.x == 0 && i_row >= 1 && i_row - 1 + r.stages < n)
+            ring_issue<T>(a, r, smem, bars, s ? s - 1 : r.stages - 1, row - 1 + r.stages);
+        const float m1 = rb * sum[0] * inv_cols, m2 = after ? ra * (sum[1] - rb * rb * m1 * sum[2]) * inv_cols : 0.f;
+        const f2 f1 = both(-rb * rb * m1), f2y = both(-ra * ra * m2), ra2 = both(ra);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (i * tpr + int(threadIdx.x)) * VE;
+            if (c < cols) {
+                f2 d[VP], x[VP], h[VP], y[VP];
+                if (stream) stage_cols<T, VP>(stage + r.i_dxo * r.row_bytes, c, d); else zero_cols(d);
+                if (before) stage_cols<T, VP>(stage + r.i_x * r.row_bytes, c, x); else zero_cols(x);
+                if (before) stage_cols<T, VP>(stage + r.i_dh * r.row_bytes, c, h); else zero_cols(h);
+                if (need_y) stage_cols<T, VP>(stage + r.i_y * r.row_bytes, c, y); else zero_cols(y);
+#pragma unroll
+                for (int e = 0; e < VP; ++e) {
+                    d[e] = fma2(f1, x[e], fma2(rb2, mul2(h[e], wb[i][e]), d[e]));           // G
+                    const f2 rg = mul2(ra2, d[e]);
+                    t[i][e] = fma2(rg, y[e], t[i][e]);
+                    y[e] = fma2(f2y, y[e], mul2(k[i][e], rg));
+                }
+                st_stream(dx + c, pack16<T>(d));
+                if (block) st_stream(dy + c, pack16<T>(y));
+            }
+        }
+        dx += a.d.ld_x;
+        dy += a.d.ld_y;
+        if (++s == r.stages) { s = 0; parity ^= 1u; }
+    }
+    if (group >= 0) ring_flush<T, W, VE, NV>(a, chunk, begin, begin + n, group, gate, tpr, o, t, acc_a);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = (i * tpr + int(threadIdx.x)) * VE;
+        if (c >= cols) continue;
+#pragma unroll
+        for (int e = 0; e < VP; e += 2) {
+            if (a.dw_after) *reinterpret_cast<ulonglong2 *>(part_row(a, 0, chunk) + c + 2 * e) = make_ulonglong2(acc_a[i][e], acc_a[i][e + 1]);
+            if (a.dw_before) *reinterpret_cast<ulonglong2 *>(part_row(a, 1, chunk) + c + 2 * e) = make_ulonglong2(acc_b[i][e], acc_b[i][e + 1]);
+        }
+    }
+}
+
 // Adds up the chunks' partial sums, in chunk order: blockIdx.y = 0 dW_after, 1 dW_before, from 2 on the gate groups that
 // lie in more than one chunk.  32 columns a block, one chunk a warp at a time.
 template <typename T>
@@ -408,28 +790,73 @@ __global__ void __launch_bounds__(512) norm_backward_join_kernel(const __grid_co
     }
 }
 
-// Threads and vectors of a row: VE elements a vector, NV vectors a thread.
-struct Shape { int ve, nv, tpr, slots; bool wide; };
+// Threads and vectors of a row: VE elements a vector, NV vectors a thread; for the ring its stages and blocks per SM.
+struct Shape { int ve, nv, tpr, slots; bool wide, ring; int blocks, smem; Ring r; };
+
+int esize_of(int dtype) { return dtype == RUBICK_F32 ? 4 : 2; }
 
 // 16-byte accesses where every row of every tensor starts on a 16-byte boundary
-bool vectors_fit(const NormArgs &a, int esize, int wsize)
+bool vectors_fit(const NormArgs &a, int esize)
 {
     const void *rows[] = {a.x, a.y, a.x_out, a.h, a.dx_out, a.dh, a.dx, a.dy, a.gate, a.dgate, a.w_after, a.w_before};
     for (const void *p : rows) if (!aligned16(p)) return false;
-    (void)wsize;
     const bool blk = a.y != nullptr, bef = (a.d.flags & RUBICK_NORM_BEFORE) != 0;
     return a.d.ld_x * esize % 16 == 0 && (!blk || a.d.ld_y * esize % 16 == 0) && (!bef || a.d.ld_h * esize % 16 == 0)
         && (!a.gate || a.d.ld_gate * esize % 16 == 0);
 }
 
-int esize_of(int dtype) { return dtype == RUBICK_F32 ? 4 : 2; }
+// dynamic shared memory of one of n blocks on an SM: 228 KB, less what the system and the static part take of each
+int ring_budget(int n) { return 228 * 1024 / n - 1792; }
+
+// The ring's shape; false where a row does not fit: fewer than two stages, or more columns than 16 a thread cover.
+bool ring_shape(const NormArgs &a, bool back, Shape &s)
+{
+    const int es = esize_of(a.d.dtype);
+    if (s.ve == 1 || a.d.cols % s.ve) return false;
+    const int nvec = a.d.cols / s.ve, most = 16 / s.ve, warps = (nvec + most * 32 - 1) / (most * 32);
+    if (warps > 16) return false;
+    Ring &r = s.r;
+    const bool before = a.d.flags & RUBICK_NORM_BEFORE, after = a.d.flags & RUBICK_NORM_AFTER;
+    int n = 0;
+    r.i_x = !back || before ? n++ : -1;
+    r.i_y = a.y && (!back || after || a.gate) ? n++ : -1;
+    r.i_dxo = back && a.dx_out ? n++ : -1;
+    r.i_dh = back && before ? n++ : -1;
+    // a gate row that serves few rows travels with them; one that serves many is read when its group begins
+    r.i_gate = a.gate && a.d.group_rows < 8 ? n++ : -1;
+    if (n == 0) return false;
+    r.tensors = n;
+    r.row_bytes = uint32_t(a.d.cols * es);
+    s.tpr = warps * 32;
+    s.nv = (nvec + s.tpr - 1) / s.tpr;
+    s.slots = 1;
+    // 128 registers a thread backward, up to 102 forward (40 to 64 with one vector a thread)
+    s.blocks = (back ? 512 : s.nv == 1 ? 1024 : 640) / s.tpr;
+    if (s.blocks > 16) s.blocks = 16;
+    for (;; --s.blocks) {
+        if (s.blocks == 0) return false;
+        r.stages = ring_budget(s.blocks) / (n * int(r.row_bytes));
+        if (r.stages >= 3 || (s.blocks == 1 && r.stages == 2)) break;
+    }
+    if (r.stages > RING_MOST) r.stages = RING_MOST;
+    s.smem = r.stages * n * int(r.row_bytes);
+    return true;
+}
+
+void cut_rows(const NormArgs &a, int64_t want, int64_t *chunk_rows, int *n_chunks)
+{
+    *chunk_rows = a.d.rows > want ? (a.d.rows + want - 1) / want : 1;
+    *n_chunks = int((a.d.rows + *chunk_rows - 1) / *chunk_rows);
+}
 
 Shape forward_shape(const NormArgs &a, int num_sms)
 {
     Shape s;
     const int es = esize_of(a.d.dtype);
     s.wide = false;
-    s.ve = vectors_fit(a, es, 0) ? 16 / es : 1;
+    s.ve = vectors_fit(a, es) ? 16 / es : 1;
+    s.ring = ring_shape(a, false, s) && a.d.rows >= int64_t(num_sms) * s.blocks * 4;
+    if (s.ring) return s;
     const int most = 32 / s.ve, nvec = (a.d.cols + s.ve - 1) / s.ve;
     int warps = (nvec + most * 32 - 1) / (most * 32);
     // few rows: more warps a row while the rows do not fill the SMs' 64 warps
@@ -445,18 +872,48 @@ Shape backward_shape(const NormArgs &a)
 {
     Shape s;
     const int es = esize_of(a.d.dtype);
-    s.ve = vectors_fit(a, es, 0) ? 16 / es : 1;
+    s.ve = vectors_fit(a, es) ? 16 / es : 1;
+    s.wide = false;
+    s.ring = ring_shape(a, true, s);
+    if (s.ring) return s;
     const int most = 16 / s.ve, nvec = (a.d.cols + s.ve - 1) / s.ve;   // 16 columns a thread
     const int warps = (nvec + most * 32 - 1) / (most * 32);
     s.wide = warps > 16;
     s.tpr = s.wide ? 512 : warps * 32;
     s.nv = (nvec + s.tpr - 1) / s.tpr;
     s.slots = s.wide || s.tpr >= 128 ? 1 : 128 / s.tpr;
+    s.blocks = s.wide ? 1 : 512 / (s.tpr * s.slots) > 0 ? 512 / (s.tpr * s.slots) : 1;
     return s;
+}
+
+template <typename K> cudaError_t launch_ring(K kernel, const NormArgs &a, const Shape &s, cudaStream_t st)
+{
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, s.smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<unsigned(a.n_chunks), s.tpr, s.smem, st>>>(a, s.r);
+    count_launch();
+    return cudaGetLastError();
+}
+
+template <typename T, typename W, int VE, bool FULL> cudaError_t forward_ring(const NormArgs &a, const Shape &s, cudaStream_t st)
+{
+    if (s.nv <= 1) return launch_ring(norm_forward_ring_kernel<T, W, 1, FULL>, a, s, st);
+    if (VE == 8 || s.nv <= 2) return launch_ring(norm_forward_ring_kernel<T, W, 2, FULL>, a, s, st);
+    return launch_ring(norm_forward_ring_kernel<T, W, VE == 4 ? 4 : 2, FULL>, a, s, st);
+}
+template <typename T, typename W, int VE, bool FULL> cudaError_t backward_ring(const NormArgs &a, const Shape &s, cudaStream_t st)
+{
+    if (s.nv <= 1) return launch_ring(norm_backward_ring_kernel<T, W, 1, FULL>, a, s, st);
+    if (VE == 8 || s.nv <= 2) return launch_ring(norm_backward_ring_kernel<T, W, 2, FULL>, a, s, st);
+    return launch_ring(norm_backward_ring_kernel<T, W, VE == 4 ? 4 : 2, FULL>, a, s, st);
 }
 
 template <typename T, typename W, int VE> cudaError_t forward_nv(const NormArgs &a, const Shape &s, cudaStream_t st)
 {
+    if constexpr (VE > 1) {
+        const bool full = a.y && (a.d.flags & RUBICK_NORM_AFTER) && (a.d.flags & RUBICK_NORM_BEFORE);
+        if (s.ring) return full ? forward_ring<T, W, VE, true>(a, s, st) : forward_ring<T, W, VE, false>(a, s, st);
+    }
     const dim3 block(s.tpr, s.slots);
     const unsigned grid = unsigned((a.d.rows + s.slots - 1) / s.slots);
     if constexpr (VE > 1) {
@@ -478,7 +935,17 @@ template <typename T, typename W, int VE> cudaError_t backward_nv(const NormArgs
 {
     const dim3 block(s.tpr, s.slots);
     const unsigned grid = unsigned((a.n_chunks + s.slots - 1) / s.slots);
-    if (s.wide) {
+    bool ring = false;
+    if constexpr (VE > 1) {
+        if (s.ring) {
+            ring = true;
+            const bool full = a.y && (a.d.flags & RUBICK_NORM_AFTER) && (a.d.flags & RUBICK_NORM_BEFORE) && a.dx_out;
+            const cudaError_t e = full ? backward_ring<T, W, VE, true>(a, s, st) : backward_ring<T, W, VE, false>(a, s, st);
+            if (e != cudaSuccess) return e;
+        }
+    }
+    if (ring) {
+    } else if (s.wide) {
         const int smem = 3 * a.d.cols * int(sizeof(float));
         const cudaError_t e = cudaFuncSetAttribute(norm_backward_wide_kernel<T, W, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
         if (e != cudaSuccess) return e;
@@ -493,7 +960,7 @@ template <typename T, typename W, int VE> cudaError_t backward_nv(const NormArgs
         if (s.nv <= 4) norm_backward_kernel<T, W, VE, 4><<<grid, block, 0, st>>>(a);
         else norm_backward_kernel<T, W, VE, 16><<<grid, block, 0, st>>>(a);
     }
-    count_launch();
+    if (!ring) count_launch();
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
     const int64_t groups = (a.d.rows + a.d.group_rows - 1) / a.d.group_rows;
@@ -532,21 +999,20 @@ struct Backward {
 
 }  // namespace
 
-cudaError_t launch_norm_forward(const NormArgs &a, int num_sms, cudaStream_t st)
+cudaError_t launch_norm_forward(const NormArgs &args, int num_sms, cudaStream_t st)
 {
+    NormArgs a = args;
     const Shape s = forward_shape(a, num_sms);
+    if (s.ring) cut_rows(a, int64_t(num_sms) * s.blocks, &a.chunk_rows, &a.n_chunks);
     return by_type(a, s.ve, Forward{a, s, st});
 }
 
 // floats of scratch; also fixes how the rows are cut into chunks: one chunk per row slot, as many blocks as the SMs
-// hold at once (16 warps an SM at the kernel's registers)
+// hold at once
 size_t norm_backward_scratch(const NormArgs &a, int num_sms, int64_t *chunk_rows, int *n_chunks)
 {
     const Shape s = backward_shape(a);
-    const int blocks = s.wide ? 1 : 512 / (s.tpr * s.slots) > 0 ? 512 / (s.tpr * s.slots) : 1;
-    const int64_t want = int64_t(num_sms) * blocks * s.slots;
-    *chunk_rows = a.d.rows > want ? (a.d.rows + want - 1) / want : 1;
-    *n_chunks = int((a.d.rows + *chunk_rows - 1) / *chunk_rows);
+    cut_rows(a, int64_t(num_sms) * s.blocks * s.slots, chunk_rows, n_chunks);
     return size_t(4) * size_t(*n_chunks) * size_t(a.d.cols);
 }
 

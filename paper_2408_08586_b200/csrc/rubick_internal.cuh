@@ -55,6 +55,7 @@ struct Space {
 enum : uint32_t {
     DS_FEAS_NOT_THRESHOLD = 1u,
     DS_STEP_CAP = 2u,
+    DS_COPY_LOST = 8u,            // training-step operators: a copy into shared memory did not arrive
     DS_BAD_PREV = 4u,             // incremental round: the previous state does not fit the grid or the cluster
 };
 

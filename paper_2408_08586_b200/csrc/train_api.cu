@@ -104,12 +104,13 @@ int rubick_block_norm_forward(rubick_ctx *ctx, const rubick_block_norm_desc *h_d
     const bool before = h_desc->flags & RUBICK_NORM_BEFORE;
     if (!d_x || !d_y != !d_x_out || before != (d_h != nullptr)) return fail(ctx, RUBICK_EINVAL, "block norm: x is null, x_out does not go with y, or h with the norm before the block");
     const int es = esize(h_desc->dtype);
-    if (!on(d_x, es) || !on(d_y, es) || !on(d_gate, es) || !on(d_x_out, es) || !on(d_h, es) || !on(d_rstd, 4)) return fail(ctx, RUBICK_EINVAL, "block norm: a tensor is not aligned to its type");
+    if (!on(d_x, es) || !on(d_y, es) || !on(d_gate, es) || !on(d_x_out, es) || !on(d_h, es) || !on(d_rstd, 8)) return fail(ctx, RUBICK_EINVAL, "block norm: a tensor is not aligned to its type");
     if ((rc = set_device(ctx))) return rc;
     NormArgs a = {};
     a.d = *h_desc;
     a.x = d_x; a.y = d_y; a.w_after = d_w_after; a.gate = d_gate; a.w_before = d_w_before;
-    a.x_out = d_x_out; a.h = d_h; a.rstd = d_rstd;
+    a.x_out = d_x_out; a.h = d_h; a.rstd = d_rstd; a.status = ctx->d_status;
+    if (!d_gate) a.d.group_rows = a.d.rows;
     CUDA_TRY(ctx, launch_norm_forward(a, ctx->num_sms, ctx->stream), "launch block_norm_forward");
     return RUBICK_OK;
 }
@@ -134,13 +135,14 @@ int rubick_block_norm_backward(rubick_ctx *ctx, const rubick_block_norm_desc *h_
     }
     if (!d_dx || !d_y != !d_dy || (before && (!d_x_out || !d_dh)) || (!before && d_dh)) return fail(ctx, RUBICK_EINVAL, "block norm: dx is null, dy does not go with y, or x_out and dh with the norm before the block");
     if ((after || before) && !d_rstd) return fail(ctx, RUBICK_EINVAL, "block norm: rstd is null");
-    if (!on(d_x_out, es) || !on(d_y, es) || !on(d_gate, es) || !on(d_dx_out, es) || !on(d_dh, es) || !on(d_dx, es) || !on(d_dy, es) || !on(d_dgate, es) || !on(d_rstd, 4))
+    if (!on(d_x_out, es) || !on(d_y, es) || !on(d_gate, es) || !on(d_dx_out, es) || !on(d_dh, es) || !on(d_dx, es) || !on(d_dy, es) || !on(d_dgate, es) || !on(d_rstd, 8))
         return fail(ctx, RUBICK_EINVAL, "block norm: a tensor is not aligned to its type");
     if ((rc = set_device(ctx))) return rc;
     NormArgs a = {};
     a.d = *h_desc;
     if (!d_gate) a.d.group_rows = a.d.rows;
     a.x = before ? d_x_out : nullptr; a.y = d_y; a.w_after = d_w_after; a.gate = d_gate; a.w_before = d_w_before;
+    a.status = ctx->d_status;
     a.rstd_in = d_rstd; a.dx_out = d_dx_out; a.dh = d_dh;
     a.dx = d_dx; a.dy = d_dy; a.dw_after = d_dw_after; a.dgate = d_dgate; a.dw_before = d_dw_before;
     const size_t need = norm_backward_scratch(a, ctx->num_sms, &a.chunk_rows, &a.n_chunks);

@@ -161,6 +161,67 @@ __device__ __forceinline__ float warp_max(float v)
     return v;
 }
 
+// ---- pairs of single-precision numbers: one instruction adds, multiplies or fuses both halves --------------------
+using f2 = unsigned long long;
+__device__ __forceinline__ f2 pair(float lo, float hi) { f2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi)); return r; }
+__device__ __forceinline__ f2 both(float v) { return pair(v, v); }
+__device__ __forceinline__ float lo(f2 v) { return __uint_as_float(uint32_t(v)); }
+__device__ __forceinline__ float hi(f2 v) { return __uint_as_float(uint32_t(v >> 32)); }
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+template <typename T> __device__ __forceinline__ void unpack16(const uint4 &r, f2 (&v)[Lanes<T>::N / 2])
+{
+    if constexpr (sizeof(T) == 4) {
+        v[0] = pair(__uint_as_float(r.x), __uint_as_float(r.y)); v[1] = pair(__uint_as_float(r.z), __uint_as_float(r.w));
+    } else {
+        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { float a, b; unpack_pair(w[i], T(), a, b); v[i] = pair(a, b); }
+    }
+}
+template <typename T> __device__ __forceinline__ uint4 pack16(const f2 (&v)[Lanes<T>::N / 2])
+{
+    uint4 r;
+    if constexpr (sizeof(T) == 4) {
+        r.x = __float_as_uint(lo(v[0])); r.y = __float_as_uint(hi(v[0])); r.z = __float_as_uint(lo(v[1])); r.w = __float_as_uint(hi(v[1]));
+    } else {
+        r.x = pack_pair(lo(v[0]), hi(v[0]), T()); r.y = pack_pair(lo(v[1]), hi(v[1]), T());
+        r.z = pack_pair(lo(v[2]), hi(v[2]), T()); r.w = pack_pair(lo(v[3]), hi(v[3]), T());
+    }
+    return r;
+}
+
+// ---- rows copied into shared memory by the bulk-copy engine, with a barrier that counts the bytes that have arrived
+__device__ __forceinline__ uint32_t smem_addr(const void *p) { return uint32_t(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ void bar_init(uint64_t *bar)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_addr(bar)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_addr(bar)), "r"(bytes) : "memory");
+}
+// dst, src and bytes: multiples of 16
+__device__ __forceinline__ void bulk_load(void *dst, const void *src, uint32_t bytes, uint64_t *bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_addr(dst)), "l"(src), "r"(bytes), "r"(smem_addr(bar)) : "memory");
+}
+// Waits for the phase to end, a bounded number of times; false: it did not (the kernel then reports it and goes on with
+// what is there -- no address depends on the data).
+__device__ __forceinline__ bool bar_wait(uint64_t *bar, uint32_t parity)
+{
+    const uint32_t at = smem_addr(bar);
+    for (int i = 0; i < (1 << 18); ++i) {
+        uint32_t done;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done) : "r"(at), "r"(parity) : "memory");
+        if (done) return true;
+    }
+    return false;
+}
+
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 }  // namespace train
@@ -179,6 +240,7 @@ struct NormArgs {
     float *part;                 // scratch: partial column sums of the row chunks
     int64_t chunk_rows;
     int n_chunks;
+    uint32_t *status;            // the context's status word
 };
 struct RouterArgs {
     rubick_router_desc d;

@@ -104,6 +104,18 @@ NORM_CASES = [
     (50, 640, "bf16", "bf16", "none", dict(block=False)),
     (700, 1024, "bf16", "bf16", "one", dict(after=False, before=False)),
     (20, 384, "bf16", "bf16", "one", dict(weights=False)),
+    # enough rows for the ring of stages in the forward pass too
+    (9700, 64, "bf16", "bf16", "group", dict(group=1000)),
+    (9700, 72, "fp32", "fp32", "token", dict(tanh=True)),
+    (9700, 128, "fp16", "fp32", "group", dict(group=3, offset=True)),
+    (5000, 768, "bf16", "bf16", "one", dict(after=False)),
+    (5000, 520, "bf16", "bf16", "group", dict(group=7, before=False)),
+    (5000, 512, "bf16", "bf16", "none", dict(after=False, before=False)),
+    (5000, 640, "fp32", "fp32", "none", dict(block=False, pad=4)),
+    (2400, 2048, "bf16", "fp32", "group", dict(group=512, tanh=True, pad=8)),
+    (1300, 4096, "bf16", "bf16", "token", {}),
+    (700, 8192, "fp16", "fp16", "one", {}),
+    (620, 8192, "fp32", "fp32", "one", {}),
 ]
 
 
@@ -161,11 +173,11 @@ def test_block_norm_forward_and_backward(ctx, case):
             guarded(out)
 
 
-@pytest.mark.parametrize("cols", [768, 1537])
-def test_block_norm_in_place_equals_out_of_place(ctx, cols):
+@pytest.mark.parametrize("rows,cols", [(40, 768), (40, 1537), (5000, 768)])
+def test_block_norm_in_place_equals_out_of_place(ctx, rows, cols):
     import torch
-    s, opt, desc = norm_case(40, cols, "bf16", "bf16", "group", group=9)
-    x_out, h, rstd = torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty(40, 2, device="cuda")
+    s, opt, desc = norm_case(rows, cols, "bf16", "bf16", "group", group=9)
+    x_out, h, rstd = torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty(rows, 2, device="cuda")
     args = (s["w_after"], s["gate"], s["w_before"])
     ctx.block_norm_forward(desc, s["x"], s["y"], *args, x_out, h, rstd)
     x, y = s["x"].clone(), s["y"].clone()
