@@ -22,10 +22,11 @@ namespace cg = cooperative_groups;
 
 namespace {
 
-constexpr int THREADS = 512;
-constexpr int WARPS = THREADS / 32;
-constexpr float LOG2E = 1.4426950408889634f;
+constexpr int ROW_WARPS = 16, ROW_THREADS = ROW_WARPS * 32;      // a block of a row's cluster
+constexpr int BACK_THREADS = 256;                                 // a block of the separate gradient
+constexpr int MAX_RANKS = 8;                                      // the portable cluster size
 constexpr double LOG2E_D = 1.4426950408889634;
+constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float ex2(float x)
@@ -58,13 +59,24 @@ template <typename T> struct RowView {
         for (int e = 0; e < VE; ++e) f[e] = c + e >= 0 && c + e < vocab ? to_f(row[c + e]) : -INFINITY;
         return pack16<T>(f);
     }
+    // vector v of a gradient row that may start elsewhere in its 16 bytes than z's (`same`: it does not)
+    __device__ __forceinline__ void store(T *out, bool same, int v, const uint4 &r) const
+    {
+        const int c = first(v);
+        if (same && whole(v)) { st_stream(out + c, r); return; }
+        float f[VE];
+        unpack16<T>(r, f);
+#pragma unroll
+        for (int e = 0; e < VE; ++e) if (c + e >= 0 && c + e < vocab) out[c + e] = from_f<T>(f[e]);
+    }
 };
 
 // A row's teacher entries in shared memory.
 struct Teacher {
     int32_t index[RUBICK_MAX_TEACHER_LOGITS];     // -1: does not take part
-    float q[RUBICK_MAX_TEACHER_LOGITS];
-    float red[WARPS];
+    float log_q[RUBICK_MAX_TEACHER_LOGITS];       // log2 q
+    float z[RUBICK_MAX_TEACHER_LOGITS];           // the student's logit there
+    int32_t live;                                 // whether the row has entries
 };
 
 __device__ __forceinline__ float teacher_logit(const DistillArgs &a, int64_t at)
@@ -74,237 +86,215 @@ __device__ __forceinline__ float teacher_logit(const DistillArgs &a, int64_t at)
     return static_cast<const float *>(a.teacher)[at];
 }
 
-__device__ __forceinline__ float block_sum(float v, float *red)
+// Softmax over the entries of a row and the student's logits at the entries in elements c0 .. c1, by one warp; the
+// others meet it at the next barrier.
+template <typename T> __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, const RowView<T> &z, int c0, int c1, Teacher &t)
 {
-    v = warp_sum(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = (threadIdx.x & 31) < WARPS ? red[threadIdx.x & 31] : 0.f;
-    return warp_sum(v);
-}
-__device__ __forceinline__ float block_max(float v, float *red)
-{
-    v = warp_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = (threadIdx.x & 31) < WARPS ? red[threadIdx.x & 31] : -INFINITY;
-    return warp_max(v);
-}
-
-// Softmax over the entries of a row, by the whole block; log_q and z are handed back for the entry of this thread's
-// turn through f(j, q, log q).  Returns whether the row has entries.
-__device__ __forceinline__ bool teacher_softmax(const DistillArgs &a, int64_t row, Teacher &t)
-{
-    const int k = a.d.k;
-    float top = -INFINITY;
-    for (int j = threadIdx.x; j < k; j += THREADS) {
+    const int k = a.d.k, lane = threadIdx.x & 31;
+    const float c = LOG2E / a.d.temperature;
+    float top = -INFINITY, total = 0.f;
+    bool any = false;
+#pragma unroll 4
+    for (int j = lane; j < k; j += 32) {
         const int i = a.index[row * k + j];
         const float l = teacher_logit(a, row * k + j);
         const bool in = i >= 0 && i < a.d.vocab && !(l == -INFINITY);
         t.index[j] = in ? i : -1;
-        t.q[j] = l;
-        // a NaN must reach the sum: it does not win a maximum, but exp(NaN - top) is NaN
-        if (in) top = fmaxf(top, l != l ? -3e38f : l);
+        t.log_q[j] = l;
+        if (in) { top = fmaxf(top, l); any = true; }
     }
-    top = block_max(top, t.red);
-    if (top == -INFINITY) return false;
-    const float c = LOG2E / a.d.temperature;
-    float total = 0.f;
-    for (int j = threadIdx.x; j < k; j += THREADS) total += t.index[j] >= 0 ? ex2((t.q[j] - top) * c) : 0.f;
-    total = block_sum(total, t.red);
-    // q in place of the logit; log q is taken again from it where the loss needs it
-    const float log2_total = log2f(total);
-    for (int j = threadIdx.x; j < k; j += THREADS) t.q[j] = t.index[j] >= 0 ? (t.q[j] - top) * c - log2_total : -INFINITY;   // log2 q
-    return true;
+    any = __any_sync(0xffffffffu, any);
+    top = warp_max(top);
+    if (top == -INFINITY) top = 0.f;              // only NaN entries: they reach the sum
+#pragma unroll 4
+    for (int j = lane; j < k; j += 32) total += t.index[j] >= 0 ? ex2((t.log_q[j] - top) * c) : 0.f;
+    total = warp_sum(total);
+    const float log_total = log2f(total);
+#pragma unroll 4
+    for (int j = lane; j < k; j += 32) {
+        const int i = t.index[j];
+        t.log_q[j] = i >= 0 ? (t.log_q[j] - top) * c - log_total : -INFINITY;
+        t.z[j] = i >= c0 && i < c1 ? to_f(z.row[i]) : -INFINITY;
+    }
+    if (lane == 0) t.live = any;
+    __syncwarp();
 }
 
 // q of vocabulary entry i: an index listed twice counts with the sum of its entries
 __device__ __forceinline__ float teacher_mass(const Teacher &t, int k, int i)
 {
     float s = 0.f;
-    for (int j = 0; j < k; ++j) if (t.index[j] == i) s += ex2(t.q[j]);
+    for (int j = 0; j < k; ++j) if (t.index[j] == i) s += ex2(t.log_q[j]);
     return s;
 }
 
 struct Pair { float m, s; };      // maximum of z, sum of 2^((z - m) c)
 
-__device__ __forceinline__ Pair merge(Pair a, Pair b, float c)
-{
-    const float m = fmaxf(a.m, b.m);
-    const float shift = m == -INFINITY ? 0.f : m;
-    Pair r;
-    r.m = m;
-    r.s = a.s * ex2((a.m - shift) * c) + b.s * ex2((b.m - shift) * c);
-    return r;
-}
-__device__ __forceinline__ Pair warp_merge(Pair p, float c)
-{
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        Pair q;
-        q.m = __shfl_xor_sync(0xffffffffu, p.m, o);
-        q.s = __shfl_xor_sync(0xffffffffu, p.s, o);
-        // both sides of a pair must get the same bits: the lower lane's pair first
-        p = (threadIdx.x & o) ? merge(q, p, c) : merge(p, q, c);
+// maxima in the storage type: exact, and two at a time in 16 bits; NaN loses, and reaches the sum instead
+template <typename T> struct Top;
+template <> struct Top<float> {
+    float m = -INFINITY;
+    __device__ __forceinline__ void take(const uint4 &r)
+    {
+        m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(r.x), __uint_as_float(r.y)), fmaxf(__uint_as_float(r.z), __uint_as_float(r.w))));
     }
-    return p;
-}
+    __device__ __forceinline__ float get() const { return m; }
+};
+template <> struct Top<bf16> {
+    __nv_bfloat162 m = __nv_bfloat162(__float2bfloat16_rn(-INFINITY), __float2bfloat16_rn(-INFINITY));
+    static __device__ __forceinline__ __nv_bfloat162 as(const uint32_t &w) { return *reinterpret_cast<const __nv_bfloat162 *>(&w); }
+    __device__ __forceinline__ void take(const uint4 &r) { m = __hmax2(m, __hmax2(__hmax2(as(r.x), as(r.y)), __hmax2(as(r.z), as(r.w)))); }
+    __device__ __forceinline__ float get() const { return fmaxf(__low2float(m), __high2float(m)); }
+};
+template <> struct Top<f16> {
+    __half2 m = __half2(__float2half_rn(-INFINITY), __float2half_rn(-INFINITY));
+    static __device__ __forceinline__ __half2 as(const uint32_t &w) { return *reinterpret_cast<const __half2 *>(&w); }
+    __device__ __forceinline__ void take(const uint4 &r) { m = __hmax2(m, __hmax2(__hmax2(as(r.x), as(r.y)), __hmax2(as(r.z), as(r.w)))); }
+    __device__ __forceinline__ float get() const { return fmaxf(__low2float(m), __high2float(m)); }
+};
 
-template <typename T> __device__ __forceinline__ float vector_max(const uint4 &r, float m)
+// s + sum of 2^(v c + off), pairwise
+template <typename T> __device__ __forceinline__ f2 add_exps(const uint4 &r, f2 c, f2 off, f2 s)
 {
-    float v[Lanes<T>::N];
+    f2 v[Lanes<T>::N / 2];
     unpack16<T>(r, v);
 #pragma unroll
-    for (int e = 0; e < Lanes<T>::N; ++e) m = fmaxf(m, v[e]);
-    return m;
-}
-// sum of 2^(v c - mc)
-template <typename T> __device__ __forceinline__ float vector_sum(const uint4 &r, float c, float mc)
-{
-    float v[Lanes<T>::N], s = 0.f;
-    unpack16<T>(r, v);
-#pragma unroll
-    for (int e = 0; e < Lanes<T>::N; ++e) s += ex2(fmaf(v[e], c, -mc));
+    for (int e = 0; e < Lanes<T>::N / 2; ++e) {
+        const f2 x = fma2(v[e], c, off);
+        s = add2(s, pair(ex2(lo(x)), ex2(hi(x))));
+    }
     return s;
 }
+// scale 2^(v c + off)
+template <typename T> __device__ __forceinline__ uint4 scaled_exps(const uint4 &r, f2 c, f2 off, f2 scale)
+{
+    f2 v[Lanes<T>::N / 2];
+    unpack16<T>(r, v);
+#pragma unroll
+    for (int e = 0; e < Lanes<T>::N / 2; ++e) {
+        const f2 x = fma2(v[e], c, off);
+        v[e] = mul2(scale, pair(ex2(lo(x)), ex2(hi(x))));
+    }
+    return pack16<T>(v);
+}
+
+// the cluster's barrier in its two halves; what was read and written before the arrival is done with by then
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 // One row per cluster.  STEP: the row's vectors stay in registers (NV a thread) and the gradient is written; otherwise
-// any number of vectors is read in batches of NV.
+// any number of vectors is read in batches of NV.  Per warp a maximum, then a sum against it: the block's threads meet
+// once, at the cluster's barrier, behind which every warp puts all warps' pairs together for itself.
 template <typename T, int NV, bool STEP>
-__global__ void __launch_bounds__(THREADS, 2) distill_row_kernel(const __grid_constant__ DistillArgs a)
+__global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __grid_constant__ DistillArgs a)
 {
     __shared__ Teacher teacher;
-    __shared__ Pair parts[WARPS];
-    __shared__ Pair mine;
+    __shared__ Pair pairs[ROW_WARPS];
     constexpr int VE = Lanes<T>::N;
     cg::cluster_group cluster = cg::this_cluster();
     const int ranks = int(cluster.num_blocks()), rank = int(cluster.block_rank());
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = a.d.k;
     const int64_t row = blockIdx.x / ranks;
-    const int k = a.d.k;
     const RowView<T> z(a.z, row, a.d.ld, a.d.vocab);
     const int per = (z.vectors + ranks - 1) / ranks;
-    const int v0 = rank * per, v1 = v0 + per < z.vectors ? v0 + per : z.vectors;
+    const int v0 = rank * per, v1 = v0 + per < z.vectors ? v0 + per : z.vectors, mine = v0 + int(threadIdx.x);
     const float c = LOG2E / a.d.temperature;
+    const f2 c2 = both(c);
 
     uint4 r[NV];
-    if constexpr (STEP) {
-        // the loads go out before anything else is waited for
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = v0 + i * THREADS + int(threadIdx.x);
-            if (v < v1) r[i] = z.load(v);
-        }
-    }
-    const bool live = teacher_softmax(a, row, teacher);      // the same in every block of the cluster
+    for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) r[i] = z.load(mine + i * ROW_THREADS);
+    // the last warp, which has the fewest vectors, reads the teacher while the row is on its way; the first block
+    // takes the loss and so every entry's logit, the others those that they will write
+    if (warp == ROW_WARPS - 1) read_teacher<T>(a, row, z, rank ? z.first(v0) : 0, rank ? z.first(v1) : z.vocab, teacher);
     Pair p{-INFINITY, 0.f};
-    if constexpr (STEP) {
+    {
+        Top<T> top;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) if (v0 + i * THREADS + int(threadIdx.x) < v1) p.m = vector_max<T>(r[i], p.m);
-        p.m = block_max(p.m, teacher.red);                   // one maximum for the block: no rescaling between its threads
-        const float mc = p.m == -INFINITY ? 0.f : p.m * c;
+        for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) top.take(r[i]);
+        p.m = warp_max(top.get());
+        f2 off = both(p.m == -INFINITY ? 0.f : -p.m * c), s = 0ull;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) if (v0 + i * THREADS + int(threadIdx.x) < v1) p.s += vector_sum<T>(r[i], c, mc);
-        p.s = block_sum(p.s, teacher.red);
-        if (threadIdx.x == 0) mine = p;
-    } else if (live) {
-        for (int v = v0 + int(threadIdx.x); v < v1; v += NV * THREADS) {
-            uint4 b[NV];
+        for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) s = add_exps<T>(r[i], c2, off, s);
+        if constexpr (!STEP) {
+            __syncthreads();
+            // a row without entries is not read on
+            for (int v = mine + NV * ROW_THREADS; teacher.live && v - int(threadIdx.x) < v1; v += NV * ROW_THREADS) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) if (v + i * THREADS < v1) b[i] = z.load(v + i * THREADS);
-            float m = p.m;
+                for (int i = 0; i < NV; ++i) if (v + i * ROW_THREADS < v1) r[i] = z.load(v + i * ROW_THREADS);
+                Top<T> more;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) if (v + i * THREADS < v1) m = vector_max<T>(b[i], m);
-            const float mc = m == -INFINITY ? 0.f : m * c;
-            p.s *= ex2(fmaf(p.m, c, -mc));
-            p.m = m;
+                for (int i = 0; i < NV; ++i) if (v + i * ROW_THREADS < v1) more.take(r[i]);
+                const float m = fmaxf(p.m, warp_max(more.get()));
+                const float shift = m == -INFINITY ? 0.f : m;
+                off = both(-shift * c);
+                s = mul2(s, both(ex2((p.m - shift) * c)));
+                p.m = m;
 #pragma unroll
-            for (int i = 0; i < NV; ++i) if (v + i * THREADS < v1) p.s += vector_sum<T>(b[i], c, mc);
-        }
-        p = warp_merge(p, c);
-        if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = p;
-        __syncthreads();
-        if (threadIdx.x < 32) {
-            p = threadIdx.x < WARPS ? parts[threadIdx.x] : Pair{-INFINITY, 0.f};
-            p = warp_merge(p, c);
-            if (threadIdx.x == 0) mine = p;
-        }
-    }
-    // the student's logits at the teacher's entries, before any block of the cluster writes a gradient over them
-    constexpr int PER = RUBICK_MAX_TEACHER_LOGITS / THREADS;
-    float zk[PER];
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-        const int j = threadIdx.x + u * THREADS;
-        zk[u] = live && j < k && teacher.index[j] >= 0 ? to_f(z.row[teacher.index[j]]) : -INFINITY;
-    }
-    cluster.sync();
-    p = Pair{-INFINITY, 0.f};
-    if (ranks == 1) p = mine;
-    else for (int q = 0; q < ranks; ++q) p = merge(p, *cluster.map_shared_rank(&mine, q), c);
-    cluster.sync();                                          // no block leaves while others read its pair
-    const float shift = p.m == -INFINITY ? 0.f : p.m;
-    const float log2_s = log2f(p.s);
-    if (rank == 0) {
-        float loss = 0.f;
-#pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int j = threadIdx.x + u * THREADS;
-            if (live && j < k && teacher.index[j] >= 0) {
-                const float lq = teacher.q[j];
-                const float lp = zk[u] == -INFINITY ? -INFINITY : (zk[u] - shift) * c - log2_s;
-                const float q = ex2(lq);
-                if (q > 0.f || q != q) loss = fmaf(q, lq - lp, loss);
+                for (int i = 0; i < NV; ++i) if (v + i * ROW_THREADS < v1) s = add_exps<T>(r[i], c2, off, s);
             }
         }
-        loss = block_sum(loss, teacher.red);
-        if (threadIdx.x == 0) {
+        p.s = warp_sum(lo(s) + hi(s));
+    }
+    if (lane == 0) pairs[warp] = p;
+    cluster_arrive();
+    cluster_wait();
+    // all warps' pairs of all blocks, lane by lane
+    Pair got[MAX_RANKS / 2];
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < MAX_RANKS / 2; ++u) {
+        const int q = 2 * u + (lane >> 4);        // half a warp per block
+        got[u] = q < ranks ? *cluster.map_shared_rank(&pairs[lane & 15], q) : Pair{-INFINITY, 0.f};
+        m = fmaxf(m, got[u].m);
+    }
+    m = warp_max(m);
+    const float shift = m == -INFINITY ? 0.f : m;
+    float total = 0.f;
+#pragma unroll
+    for (int u = 0; u < MAX_RANKS / 2; ++u) total = fmaf(got[u].s, ex2((got[u].m - shift) * c), total);
+    cluster_arrive();                             // read: the others may go (awaited before this block goes itself)
+    total = warp_sum(total);
+    const bool live = teacher.live;
+    if (rank == 0 && warp == ROW_WARPS - 1) {
+        const float log_s = log2f(total);
+        float loss = 0.f;
+        for (int j = lane; live && j < k; j += 32) {
+            const float lq = teacher.log_q[j], zj = teacher.z[j], q = ex2(lq);
+            const float lp = zj == -INFINITY ? -INFINITY : (zj - shift) * c - log_s;
+            if (teacher.index[j] >= 0 && !(q == 0.f)) loss = fmaf(q, lq - lp, loss);
+        }
+        loss = warp_sum(loss);
+        if (lane == 0) {
             a.loss[row] = live ? a.d.temperature * a.d.temperature * LN2 * loss : 0.f;
-            if (a.lse) a.lse[row] = live ? fmaf(shift, 1.f / a.d.temperature, LN2 * log2_s) : 0.f;
+            if (a.lse) a.lse[row] = live ? fmaf(shift, 1.f / a.d.temperature, LN2 * log_s) : 0.f;
         }
     }
     if constexpr (STEP) {
-        const float up = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature;
+        const float up = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature, inv = total > 0.f || total != total ? 1.f / total : 0.f;
         T *dz = static_cast<T *>(a.dz) + row * a.d.ld;
         const bool same = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z.row) & 15);
-        const float mc = shift * c, scale = live ? up * (1.f / p.s) : 0.f;
+        const f2 off = both(-shift * c), scale = both(up * inv);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int v = v0 + i * THREADS + int(threadIdx.x);
-            if (v < v1) {
-                float f[VE];
-                unpack16<T>(r[i], f);
-#pragma unroll
-                for (int e = 0; e < VE; ++e) f[e] = live ? (f[e] == -INFINITY ? 0.f : scale * ex2(fmaf(f[e], c, -mc))) : 0.f;
-                const int c0 = z.first(v);
-                if (same && z.whole(v)) st_stream(dz + c0, pack16<T>(f));
-                else {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) if (c0 + e >= 0 && c0 + e < z.vocab) dz[c0 + e] = from_f<T>(f[e]);
-                }
-            }
+            const int v = mine + i * ROW_THREADS;
+            if (v < v1) z.store(dz, same, v, live ? scaled_exps<T>(r[i], c2, off, scale) : make_uint4(0u, 0u, 0u, 0u));
         }
-        if (live) {
-            __syncthreads();
-#pragma unroll
-            for (int u = 0; u < PER; ++u) {
-                const int j = threadIdx.x + u * THREADS;
-                if (j < k && teacher.index[j] >= 0) {
-                    const int i = teacher.index[j], v = (i + z.shift) / VE;
-                    if (v >= v0 && v < v1) {
-                        const float pj = zk[u] == -INFINITY ? 0.f : ex2(fmaf(zk[u], c, -mc)) / p.s;
-                        dz[i] = from_f<T>(up * (pj - teacher_mass(teacher, k, i)));
-                    }
-                }
+        __syncthreads();
+        for (int j = threadIdx.x; live && j < k; j += ROW_THREADS) {
+            const int i = teacher.index[j], v = (i + z.shift) / VE;
+            if (i >= 0 && v >= v0 && v < v1) {
+                const float pj = ex2(fmaf(teacher.z[j], c, -shift * c)) * inv;
+                dz[i] = from_f<T>(up * (pj - teacher_mass(teacher, k, i)));
             }
         }
     }
+    cluster_wait();
 }
 
-// Gradient from a saved log-sum: element-wise, so a row is cut into blockIdx.x parts that need nothing of each other.
+// Gradient from a saved log-sum: element-wise, so a row is cut into parts that need nothing of each other.
 template <typename T>
-__global__ void __launch_bounds__(THREADS, 2) distill_backward_kernel(const __grid_constant__ DistillArgs a, int parts)
+__global__ void __launch_bounds__(BACK_THREADS, 4) distill_backward_kernel(const __grid_constant__ DistillArgs a, int parts)
 {
     __shared__ Teacher teacher;
     constexpr int VE = Lanes<T>::N, NV = 4;
@@ -313,52 +303,54 @@ __global__ void __launch_bounds__(THREADS, 2) distill_backward_kernel(const __gr
     const RowView<T> z(a.z, row, a.d.ld, a.d.vocab);
     const int per = (z.vectors + parts - 1) / parts;
     const int v0 = part * per, v1 = v0 + per < z.vectors ? v0 + per : z.vectors;
-    const bool live = teacher_softmax(a, row, teacher);
-    constexpr int PER = RUBICK_MAX_TEACHER_LOGITS / THREADS;
-    float zk[PER];
+    int v = v0 + int(threadIdx.x);
+    uint4 r[NV];
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-        const int j = threadIdx.x + u * THREADS;
-        const int i = live && j < k ? teacher.index[j] : -1, v = (i + z.shift) / VE;
-        zk[u] = i >= 0 && v >= v0 && v < v1 ? to_f(z.row[i]) : -INFINITY;
-    }
-    __syncthreads();                                         // read before anything is written over them
+    for (int i = 0; i < NV; ++i) if (v + i * BACK_THREADS < v1) r[i] = z.load(v + i * BACK_THREADS);
+    if (threadIdx.x >= BACK_THREADS - 32) read_teacher<T>(a, row, z, z.first(v0), z.first(v1), teacher);
+    __syncthreads();                                         // the entries' logits are read before they are written over
+    const bool live = teacher.live;
     const float c = LOG2E / a.d.temperature, lse = a.lse_in[row] * LOG2E;
     // single-precision gradients: what the two factors lose by rounding shows in p, so it is added back
-    const float c_low = float(double(LOG2E_D) / double(a.d.temperature) - double(c)), lse_low = float(double(a.lse_in[row]) * LOG2E_D - double(lse));
-    const auto prob = [&](float v) { return ex2(sizeof(T) == 4 ? fmaf(v, c, -lse) + fmaf(v, c_low, -lse_low) : fmaf(v, c, -lse)); };
+    const float c_low = float(LOG2E_D / double(a.d.temperature) - double(c)), lse_low = float(double(a.lse_in[row]) * LOG2E_D - double(lse));
+    const auto prob = [&](float x) { return ex2(sizeof(T) == 4 ? fmaf(x, c, -lse) + fmaf(x, c_low, -lse_low) : fmaf(x, c, -lse)); };
+    // a row whose logits are all -inf has a log-sum of -inf and no probabilities
     const float up = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature;
+    const bool none = a.lse_in[row] == -INFINITY;
     T *dz = static_cast<T *>(a.dz) + row * a.d.ld;
     const bool same = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z.row) & 15);
-    for (int v = v0 + int(threadIdx.x); v < v1; v += NV * THREADS) {
-        uint4 b[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) if (live && v + i * THREADS < v1) b[i] = z.load(v + i * THREADS);
+    while (v - int(threadIdx.x) < v1) {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int w = v + i * THREADS;
+            const int w = v + i * BACK_THREADS;
             if (w < v1) {
-                float f[VE];
-                unpack16<T>(b[i], f);
+                uint4 g = make_uint4(0u, 0u, 0u, 0u);
+                if (live && !none) {
+                    if constexpr (sizeof(T) == 4) {
+                        float f[VE];
+                        unpack16<T>(r[i], f);
 #pragma unroll
-                for (int e = 0; e < VE; ++e) f[e] = live ? (f[e] == -INFINITY ? 0.f : up * prob(f[e])) : 0.f;
-                const int c0 = z.first(w);
-                if (same && z.whole(w)) st_stream(dz + c0, pack16<T>(f));
-                else {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) if (c0 + e >= 0 && c0 + e < z.vocab) dz[c0 + e] = from_f<T>(f[e]);
+                        for (int e = 0; e < VE; ++e) f[e] = f[e] == -INFINITY ? 0.f : up * prob(f[e]);
+                        g = pack16<T>(f);
+                    } else {
+                        g = scaled_exps<T>(r[i], both(c), both(-lse), both(up));
+                    }
                 }
+                z.store(dz, same, w, g);
             }
+        }
+        v += NV * BACK_THREADS;
+        if (live) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) if (v + i * BACK_THREADS < v1) r[i] = z.load(v + i * BACK_THREADS);
         }
     }
     if (!live) return;
     __syncthreads();
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-        const int j = threadIdx.x + u * THREADS;
-        const int i = j < k ? teacher.index[j] : -1, v = (i + z.shift) / VE;
-        if (i >= 0 && v >= v0 && v < v1) {
-            const float pj = zk[u] == -INFINITY ? 0.f : prob(zk[u]);
+    for (int j = threadIdx.x; j < k; j += BACK_THREADS) {
+        const int i = teacher.index[j], w = (i + z.shift) / VE;
+        if (i >= 0 && w >= v0 && w < v1) {
+            const float pj = none || teacher.z[j] == -INFINITY ? 0.f : prob(teacher.z[j]);
             dz[i] = from_f<T>(up * (pj - teacher_mass(teacher, k, i)));
         }
     }
@@ -368,7 +360,7 @@ template <typename T, int NV, bool STEP> cudaError_t launch_rows(const DistillAr
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(unsigned(a.d.rows * ranks));
-    cfg.blockDim = dim3(THREADS);
+    cfg.blockDim = dim3(ROW_THREADS);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
@@ -380,23 +372,23 @@ template <typename T, int NV, bool STEP> cudaError_t launch_rows(const DistillAr
     return e;
 }
 
-// blocks of a row: a power of two up to 8 (the portable cluster size)
+// blocks of a row: a power of two up to 8
 template <typename T> cudaError_t forward_of(const DistillArgs &a, int num_sms, cudaStream_t st)
 {
     const int vectors = a.d.vocab / Lanes<T>::N + 2;
     int ranks = 1;
-    while (ranks < 8 && a.d.rows * ranks < 2 * int64_t(num_sms) && vectors > ranks * THREADS) ranks *= 2;
+    while (ranks < MAX_RANKS && a.d.rows * ranks < 2 * int64_t(num_sms) && vectors > ranks * ROW_THREADS) ranks *= 2;
     return launch_rows<T, 4, false>(a, ranks, st);
 }
 
 template <typename T> cudaError_t backward_of(const DistillArgs &a, int num_sms, cudaStream_t st)
 {
     const int64_t vectors = a.d.vocab / Lanes<T>::N + 2;
-    // 16 KB or more of z a block; fewer where the rows do not fill the SMs
-    int64_t parts = (vectors + 4 * THREADS - 1) / (4 * THREADS);
-    while (parts * a.d.rows < 2 * int64_t(num_sms) && parts * THREADS < vectors) parts *= 2;
+    // up to 32 KB of z a block; less where that does not fill the SMs twice over
+    int64_t parts = (vectors + 8 * BACK_THREADS - 1) / (8 * BACK_THREADS);
+    while (parts * a.d.rows < 8 * int64_t(num_sms) && parts * BACK_THREADS < vectors) parts *= 2;
     if (parts * a.d.rows > 0x7fffffff) parts = 0x7fffffff / a.d.rows;
-    distill_backward_kernel<T><<<unsigned(a.d.rows * parts), THREADS, 0, st>>>(a, int(parts));
+    distill_backward_kernel<T><<<unsigned(a.d.rows * parts), BACK_THREADS, 0, st>>>(a, int(parts));
     count_launch();
     return cudaGetLastError();
 }
@@ -406,9 +398,9 @@ template <typename T> cudaError_t step_of(const DistillArgs &a, int num_sms, cud
     constexpr int NV = 8;
     const int vectors = (a.d.vocab + 2 * Lanes<T>::N - 2) / Lanes<T>::N;       // of a row at the worst shift
     int ranks = 1;
-    while (ranks < 8 && ranks * NV * THREADS < vectors) ranks *= 2;
-    while (ranks < 8 && a.d.rows * ranks < 2 * int64_t(num_sms) && vectors > ranks * THREADS) ranks *= 2;
-    if (ranks * NV * THREADS >= vectors) return launch_rows<T, NV, true>(a, ranks, st);
+    while (ranks < MAX_RANKS && ranks * NV * ROW_THREADS < vectors) ranks *= 2;
+    while (ranks < MAX_RANKS && a.d.rows * ranks < 2 * int64_t(num_sms) && vectors > ranks * ROW_THREADS) ranks *= 2;
+    if (ranks * NV * ROW_THREADS >= vectors) return launch_rows<T, NV, true>(a, ranks, st);
     // longer than a cluster's registers: two passes
     DistillArgs b = a;
     const cudaError_t e = forward_of<T>(a, num_sms, st);
