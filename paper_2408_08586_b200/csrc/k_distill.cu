@@ -13,6 +13,8 @@
 
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "train_common.cuh"
 
 namespace rubick {
@@ -37,46 +39,77 @@ __device__ __forceinline__ float ex2(float x)
 }
 
 // The vectors of one row: vector v holds the elements v * VE - shift + e; those outside 0 .. vocab - 1 are other rows'.
+// Only the first and the last vector can hold such elements (`head`, `tail`: their places, -1 if they do not); what is
+// done element by element for those two is kept out of line, so that the loops stay short.
 template <typename T> struct RowView {
     static constexpr int VE = Lanes<T>::N;
     const T *row;
-    int shift, vocab, vectors;
+    int shift, vocab, vectors, head, tail;
     __device__ RowView(const void *base, int64_t row_index, int64_t ld, int vocab_)
     {
         row = static_cast<const T *>(base) + row_index * ld;
         shift = int((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
         vocab = vocab_;
         vectors = (vocab + shift + VE - 1) / VE;
+        head = shift ? 0 : -1;
+        tail = vectors * VE - shift > vocab ? vectors - 1 : -1;
     }
     __device__ __forceinline__ int first(int v) const { return v * VE - shift; }
-    __device__ __forceinline__ bool whole(int v) const { return first(v) >= 0 && first(v) + VE <= vocab; }
-    __device__ __forceinline__ uint4 load(int v) const
+    __device__ __forceinline__ bool whole(int v) const { return v != head && v != tail; }
+    __device__ __forceinline__ uint4 load(int v) const { return whole(v) ? ld_stream(row + first(v)) : edge_load(row, first(v), vocab); }
+    // vector v of a gradient row that may start elsewhere in its 16 bytes than z's (`same`: it does not)
+    __device__ __forceinline__ void store(T *out, bool same, int v, const uint4 &r) const
     {
-        const int c = first(v);
-        if (c >= 0 && c + VE <= vocab) return ld_stream(row + c);
+        if (same && whole(v)) st_stream(out + first(v), r);
+        else edge_store(out, first(v), vocab, r);
+    }
+    // -inf in place of other rows' elements of vector v in shared memory
+    __device__ __forceinline__ void mask(int v, T *at) const
+    {
+#pragma unroll 1
+        for (int e = 0; e < VE; ++e) if (first(v) + e < 0 || first(v) + e >= vocab) at[e] = from_f<T>(-INFINITY);
+    }
+    // the elements of vector v that are this row's, from shared memory
+    __device__ __forceinline__ void put(T *out, int v, const T *at) const
+    {
+#pragma unroll 1
+        for (int e = 0; e < VE; ++e) if (first(v) + e >= 0 && first(v) + e < vocab) out[first(v) + e] = at[e];
+    }
+
+    static __device__ __noinline__ uint4 edge_load(const T *row, int c, int vocab)
+    {
         float f[VE];
 #pragma unroll
         for (int e = 0; e < VE; ++e) f[e] = c + e >= 0 && c + e < vocab ? to_f(row[c + e]) : -INFINITY;
         return pack16<T>(f);
     }
-    // vector v of a gradient row that may start elsewhere in its 16 bytes than z's (`same`: it does not)
-    __device__ __forceinline__ void store(T *out, bool same, int v, const uint4 &r) const
+    static __device__ __noinline__ void edge_store(T *out, int c, int vocab, uint4 r)
     {
-        const int c = first(v);
-        if (same && whole(v)) { st_stream(out + c, r); return; }
         float f[VE];
         unpack16<T>(r, f);
 #pragma unroll
         for (int e = 0; e < VE; ++e) if (c + e >= 0 && c + e < vocab) out[c + e] = from_f<T>(f[e]);
     }
 };
+// a vector of -inf: it changes neither a maximum nor a sum
+template <typename T> __device__ __forceinline__ uint4 no_logits()
+{
+    const uint32_t w = sizeof(T) == 4 ? 0xff800000u : std::is_same<T, bf16>::value ? 0xff80ff80u : 0xfc00fc00u;
+    return make_uint4(w, w, w, w);
+}
 
 // A row's teacher entries in shared memory.
 struct Teacher {
-    int32_t index[RUBICK_MAX_TEACHER_LOGITS];     // -1: does not take part
-    float log_q[RUBICK_MAX_TEACHER_LOGITS];       // log2 q
-    float z[RUBICK_MAX_TEACHER_LOGITS];           // the student's logit there
-    int32_t live;                                 // whether the row has entries
+    int32_t *index;               // -1: does not take part
+    float *log_q;                 // log2 q
+    float *z;                     // the student's logit there
+    int32_t *live;                // whether the row has entries
+};
+struct TeacherSpace {
+    int32_t index[RUBICK_MAX_TEACHER_LOGITS];
+    float log_q[RUBICK_MAX_TEACHER_LOGITS], z[RUBICK_MAX_TEACHER_LOGITS];
+    int32_t live;
+    __device__ __forceinline__ Teacher view() { return Teacher{index, log_q, z, &live}; }
 };
 
 __device__ __forceinline__ float teacher_logit(const DistillArgs &a, int64_t at)
@@ -88,7 +121,7 @@ __device__ __forceinline__ float teacher_logit(const DistillArgs &a, int64_t at)
 
 // Softmax over the entries of a row and the student's logits at the entries in elements c0 .. c1, by one warp; the
 // others meet it at the next barrier.
-template <typename T> __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, const RowView<T> &z, int c0, int c1, Teacher &t)
+template <typename T> __device__ __forceinline__ void read_teacher(const DistillArgs &a, int64_t row, const RowView<T> &z, int c0, int c1, const Teacher &t)
 {
     const int k = a.d.k, lane = threadIdx.x & 31;
     const float c = LOG2E / a.d.temperature;
@@ -116,7 +149,7 @@ template <typename T> __device__ __forceinline__ void read_teacher(const Distill
         t.log_q[j] = i >= 0 ? (t.log_q[j] - top) * c - log_total : -INFINITY;
         t.z[j] = i >= c0 && i < c1 ? to_f(z.row[i]) : -INFINITY;
     }
-    if (lane == 0) t.live = any;
+    if (lane == 0) *t.live = any;
     __syncwarp();
 }
 
@@ -182,13 +215,32 @@ template <typename T> __device__ __forceinline__ uint4 scaled_exps(const uint4 &
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
+// loss and log-sum of a row, by one warp
+__device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, const Teacher &t, float shift, float total, bool live)
+{
+    const float c = LOG2E / a.d.temperature, log_s = log2f(total);
+    const int lane = threadIdx.x & 31;
+    float loss = 0.f;
+    for (int j = lane; live && j < a.d.k; j += 32) {
+        const float lq = t.log_q[j], zj = t.z[j], q = ex2(lq);
+        const float lp = zj == -INFINITY ? -INFINITY : (zj - shift) * c - log_s;
+        if (t.index[j] >= 0 && !(q == 0.f)) loss = fmaf(q, lq - lp, loss);
+    }
+    loss = warp_sum(loss);
+    if (lane == 0) {
+        a.loss[row] = live ? a.d.temperature * a.d.temperature * LN2 * loss : 0.f;
+        if (a.lse) a.lse[row] = live ? fmaf(shift, 1.f / a.d.temperature, LN2 * log_s) : 0.f;
+    }
+}
+
 // One row per cluster.  STEP: the row's vectors stay in registers (NV a thread) and the gradient is written; otherwise
 // any number of vectors is read in batches of NV.  Per warp a maximum, then a sum against it: the block's threads meet
 // once, at the cluster's barrier, behind which every warp puts all warps' pairs together for itself.
 template <typename T, int NV, bool STEP>
 __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __grid_constant__ DistillArgs a)
 {
-    __shared__ Teacher teacher;
+    __shared__ TeacherSpace space;
+    const Teacher teacher = space.view();
     __shared__ Pair pairs[ROW_WARPS];
     constexpr int VE = Lanes<T>::N;
     cg::cluster_group cluster = cg::this_cluster();
@@ -219,7 +271,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
         if constexpr (!STEP) {
             __syncthreads();
             // a row without entries is not read on
-            for (int v = mine + NV * ROW_THREADS; teacher.live && v - int(threadIdx.x) < v1; v += NV * ROW_THREADS) {
+            for (int v = mine + NV * ROW_THREADS; *teacher.live && v - int(threadIdx.x) < v1; v += NV * ROW_THREADS) {
 #pragma unroll
                 for (int i = 0; i < NV; ++i) if (v + i * ROW_THREADS < v1) r[i] = z.load(v + i * ROW_THREADS);
                 Top<T> more;
@@ -255,20 +307,9 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
     for (int u = 0; u < MAX_RANKS / 2; ++u) total = fmaf(got[u].s, ex2((got[u].m - shift) * c), total);
     cluster_arrive();                             // read: the others may go (awaited before this block goes itself)
     total = warp_sum(total);
-    const bool live = teacher.live;
+    const bool live = *teacher.live;
     if (rank == 0 && warp == ROW_WARPS - 1) {
-        const float log_s = log2f(total);
-        float loss = 0.f;
-        for (int j = lane; live && j < k; j += 32) {
-            const float lq = teacher.log_q[j], zj = teacher.z[j], q = ex2(lq);
-            const float lp = zj == -INFINITY ? -INFINITY : (zj - shift) * c - log_s;
-            if (teacher.index[j] >= 0 && !(q == 0.f)) loss = fmaf(q, lq - lp, loss);
-        }
-        loss = warp_sum(loss);
-        if (lane == 0) {
-            a.loss[row] = live ? a.d.temperature * a.d.temperature * LN2 * loss : 0.f;
-            if (a.lse) a.lse[row] = live ? fmaf(shift, 1.f / a.d.temperature, LN2 * log_s) : 0.f;
-        }
+        write_loss(a, row, teacher, shift, total, live);
     }
     if constexpr (STEP) {
         const float up = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature, inv = total > 0.f || total != total ? 1.f / total : 0.f;
@@ -296,7 +337,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
 template <typename T>
 __global__ void __launch_bounds__(BACK_THREADS, 4) distill_backward_kernel(const __grid_constant__ DistillArgs a, int parts)
 {
-    __shared__ Teacher teacher;
+    __shared__ TeacherSpace space;
+    const Teacher teacher = space.view();
     constexpr int VE = Lanes<T>::N, NV = 4;
     const int64_t row = blockIdx.x / parts;
     const int part = blockIdx.x % parts, k = a.d.k;
@@ -309,7 +351,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 4) distill_backward_kernel(const
     for (int i = 0; i < NV; ++i) if (v + i * BACK_THREADS < v1) r[i] = z.load(v + i * BACK_THREADS);
     if (threadIdx.x >= BACK_THREADS - 32) read_teacher<T>(a, row, z, z.first(v0), z.first(v1), teacher);
     __syncthreads();                                         // the entries' logits are read before they are written over
-    const bool live = teacher.live;
+    const bool live = *teacher.live;
     const float c = LOG2E / a.d.temperature, lse = a.lse_in[row] * LOG2E;
     // single-precision gradients: what the two factors lose by rounding shows in p, so it is added back
     const float c_low = float(LOG2E_D / double(a.d.temperature) - double(c)), lse_low = float(double(a.lse_in[row]) * LOG2E_D - double(lse));
@@ -356,6 +398,224 @@ __global__ void __launch_bounds__(BACK_THREADS, 4) distill_backward_kernel(const
     }
 }
 
+// ---- many rows: clusters that stay, fed by the bulk-copy engine --------------------------------------------------
+//
+// A cluster takes every n-th row; a block holds its part of the row in registers and meanwhile the parts of the next
+// rows are on their way into shared memory.  One more warp per block issues those copies and reads the next row's
+// teacher entries, whose two dependent reads (index, then logit) would otherwise stand before every row.  The blocks of
+// a cluster send each other their warps' pairs with asynchronous stores that count towards the receiver's barrier:
+// nobody waits for anything but the 8 bytes a warp that it needs.
+
+enum { RING_STEP, RING_FORWARD, RING_BACKWARD };
+constexpr int RING_NV = 8;        // vectors a thread holds
+constexpr int RING_STAGES = 2;
+
+struct RingSync {
+    uint64_t full[RING_STAGES], empty[RING_STAGES], t_full[2], t_empty[2], x_full[2];
+};
+
+__device__ __forceinline__ void bar_init_n(uint64_t *bar, uint32_t n)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_addr(bar)), "r"(n) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint64_t *bar)
+{
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+}
+// 8 bytes into block `to`'s copy of `at`, counted by its copy of `bar`
+__device__ __forceinline__ void send_pair(Pair *at, uint64_t *bar, Pair p, uint32_t to)
+{
+    uint32_t ra, rb;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(ra) : "r"(smem_addr(at)), "r"(to));
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(rb) : "r"(smem_addr(bar)), "r"(to));
+    asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.b32 [%0], {%1, %2}, [%3];"
+                 ::"r"(ra), "r"(__float_as_uint(p.m)), "r"(__float_as_uint(p.s)), "r"(rb) : "memory");
+}
+
+template <typename T, int M, int MODE>
+__global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(const __grid_constant__ DistillArgs a, int ranks, int stage_bytes)
+{
+    constexpr int VE = Lanes<T>::N, NV = RING_NV, WARPS = M / 32;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) RingSync sync;
+    __shared__ __align__(16) Pair pairs[2][MAX_RANKS * WARPS];
+    __shared__ int32_t live_of[2];
+    __shared__ uint4 edge[2];                     // gradients of the row's first and last vector where it shares them
+    __shared__ float lse_of[2], up_of[2];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = a.d.k;
+    const int rank = blockIdx.x % ranks, clusters = gridDim.x / ranks, first_row = blockIdx.x / ranks;
+    const float c = LOG2E / a.d.temperature;
+    uint8_t *entries = smem + RING_STAGES * stage_bytes;
+    const auto teacher_at = [&](int b) {
+        int32_t *base = reinterpret_cast<int32_t *>(entries) + b * 3 * k;
+        return Teacher{base, reinterpret_cast<float *>(base + k), reinterpret_cast<float *>(base + 2 * k), live_of + b};
+    };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < RING_STAGES; ++i) { bar_init_n(sync.full + i, 1); bar_init_n(sync.empty + i, WARPS); }
+        for (int i = 0; i < 2; ++i) { bar_init_n(sync.t_full + i, 1); bar_init_n(sync.t_empty + i, WARPS); bar_init_n(sync.x_full + i, 1); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (MODE == RING_BACKWARD) __syncthreads();
+    else { cluster_arrive(); cluster_wait(); }               // no pair is sent to a barrier that is not there yet
+    bool lost = false;
+    const auto wait = [&](uint64_t *bar, uint32_t parity) {
+        if (!lost && !bar_wait(bar, parity)) { lost = true; atomicOr(a.status, DS_COPY_LOST); }
+    };
+
+    if (warp == WARPS) {
+        // the part of row n, rounded out to 16-byte units; the units that reach out of the tensor itself (before its
+        // first row, behind its last) are put together element by element
+        const auto issue = [&](int n) {
+            const int64_t row = first_row + int64_t(n) * clusters;
+            if (row >= a.d.rows) return;
+            const RowView<T> z(a.z, row, a.d.ld, a.d.vocab);
+            const int per = (z.vectors + ranks - 1) / ranks, v0 = rank * per, v1 = v0 + per < z.vectors ? v0 + per : z.vectors;
+            uint8_t *stage = smem + (n % RING_STAGES) * stage_bytes;
+            int b0 = v0, b1 = v1 > v0 ? v1 : v0;
+            if (row == 0 && b0 == 0 && b1 > 0 && !z.whole(0)) {
+                if (lane == 0) *reinterpret_cast<uint4 *>(stage) = z.load(0);
+                b0 = 1;
+            }
+            if (row == a.d.rows - 1 && b1 == z.vectors && b1 > b0 && !z.whole(b1 - 1)) {
+                if (lane == 0) *reinterpret_cast<uint4 *>(stage + size_t(b1 - 1 - v0) * 16) = z.load(b1 - 1);
+                --b1;
+            }
+            if (lane == 0) {
+                const uint32_t bytes = b1 > b0 ? uint32_t(b1 - b0) * 16 : 0;
+                bar_expect(sync.full + n % RING_STAGES, bytes);
+                if (bytes) bulk_load(stage + size_t(b0 - v0) * 16, z.row + z.first(b0), bytes, sync.full + n % RING_STAGES);
+            }
+            __syncwarp();
+        };
+        for (int n = 0; n < RING_STAGES; ++n) issue(n);
+        int n = 0;
+        for (int64_t row = first_row; row < a.d.rows; row += clusters, ++n) {
+            const int b = n & 1;
+            if (n >= 2) wait(sync.t_empty + b, ((n >> 1) - 1) & 1);
+            const RowView<T> z(a.z, row, a.d.ld, a.d.vocab);
+            const int per = (z.vectors + ranks - 1) / ranks, v0 = rank * per, v1 = v0 + per < z.vectors ? v0 + per : z.vectors;
+            const bool all = MODE != RING_BACKWARD && rank == 0;         // the loss is this block's
+            if (lane == 0) {
+                if (MODE == RING_BACKWARD) lse_of[b] = a.lse_in[row];
+                if (MODE != RING_FORWARD) up_of[b] = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature;
+            }
+            read_teacher<T>(a, row, z, all ? 0 : z.first(v0), all ? z.vocab : z.first(v1), teacher_at(b));
+            __syncwarp();
+            if (lane == 0) bar_arrive(sync.t_full + b);
+            wait(sync.empty + n % RING_STAGES, (n / RING_STAGES) & 1);   // the row is in the other warps' registers
+            issue(n + RING_STAGES);
+        }
+    } else {
+        const f2 c2 = both(c);
+        int n = 0;
+        for (int64_t row = first_row; row < a.d.rows; row += clusters, ++n) {
+            const int b = n & 1, st = n % RING_STAGES;
+            const RowView<T> z(a.z, row, a.d.ld, a.d.vocab);
+            const int per = (z.vectors + ranks - 1) / ranks, v0 = rank * per, v1 = v0 + per < z.vectors ? v0 + per : z.vectors;
+            const int mine = v0 + int(threadIdx.x);
+            if (MODE != RING_BACKWARD && threadIdx.x == 0) bar_expect(sync.x_full + b, uint32_t(ranks * WARPS * sizeof(Pair)));
+            wait(sync.full + st, (n / RING_STAGES) & 1);
+            uint4 r[NV];
+            uint8_t *from = smem + st * stage_bytes + threadIdx.x * 16;
+            // the thread that holds the row's first or last vector clears what is not the row's
+            const bool has_head = v0 <= z.head && z.head < v1 && threadIdx.x == 0;
+            const bool has_tail = v0 <= z.tail && z.tail < v1 && int(threadIdx.x) == (z.tail - v0) % M;
+            if (has_head) z.mask(z.head, reinterpret_cast<T *>(from));
+            if (has_tail) z.mask(z.tail, reinterpret_cast<T *>(smem + st * stage_bytes + size_t(z.tail - v0) * 16));
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                r[i] = no_logits<T>();                       // so that the arithmetic below need not ask
+                if (mine + i * M < v1) r[i] = *reinterpret_cast<const uint4 *>(from + i * M * 16);
+            }
+            __syncwarp();
+            if (lane == 0) bar_arrive(sync.empty + st);
+            float shift = 0.f, total = 0.f;
+            if constexpr (MODE != RING_BACKWARD) {
+                Top<T> top;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) top.take(r[i]);
+                Pair p;
+                p.m = warp_max(top.get());
+                const f2 off = both(p.m == -INFINITY ? 0.f : -p.m * c);
+                f2 s = 0ull;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) s = add_exps<T>(r[i], c2, off, s);
+                p.s = warp_sum(lo(s) + hi(s));
+                // the first block has read every logit that it needs before another block may write over it
+                wait(sync.t_full + b, (n >> 1) & 1);
+                if (lane < ranks) send_pair(&pairs[b][rank * WARPS + warp], sync.x_full + b, p, uint32_t(lane));
+                wait(sync.x_full + b, (n >> 1) & 1);
+                Pair got[MAX_RANKS * WARPS / 32];
+                float m = -INFINITY;
+#pragma unroll
+                for (int u = 0; u < MAX_RANKS * WARPS / 32; ++u) {
+                    const int q = u * 32 + lane;
+                    got[u] = q < ranks * WARPS ? pairs[b][q] : Pair{-INFINITY, 0.f};
+                    m = fmaxf(m, got[u].m);
+                }
+                m = warp_max(m);
+                shift = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int u = 0; u < MAX_RANKS * WARPS / 32; ++u) total = fmaf(got[u].s, ex2((got[u].m - shift) * c), total);
+                total = warp_sum(total);
+            } else {
+                wait(sync.t_full + b, (n >> 1) & 1);
+            }
+            const Teacher teacher = teacher_at(b);
+            const bool live = *teacher.live;
+            if (MODE != RING_BACKWARD && rank == 0 && warp == 0) write_loss(a, row, teacher, shift, total, live);
+            if constexpr (MODE != RING_FORWARD) {
+                const float up = up_of[b];
+                float inv = 1.f, sub = -shift * c;           // p = inv 2^(z c + sub)
+                bool none = false;
+                if (MODE == RING_STEP) inv = total > 0.f || total != total ? 1.f / total : 0.f;
+                else { sub = -lse_of[b] * LOG2E; none = lse_of[b] == -INFINITY; }
+                // single-precision gradients from a saved log-sum: what the factors lose by rounding is added back
+                const bool fine = MODE == RING_BACKWARD && sizeof(T) == 4;
+                const float c_low = fine ? float(LOG2E_D / double(a.d.temperature) - double(c)) : 0.f;
+                const float sub_low = fine ? float(-double(lse_of[b]) * LOG2E_D - double(sub)) : 0.f;
+                const auto prob = [&](float x) {
+                    return x == -INFINITY || none ? 0.f : inv * ex2(fine ? fmaf(x, c, sub) + fmaf(x, c_low, sub_low) : fmaf(x, c, sub));
+                };
+                T *dz = static_cast<T *>(a.dz) + row * a.d.ld;
+                // unpacked anew: kept since the sum they would fill the registers
+#pragma unroll
+                for (int i = 0; i < NV; ++i) asm volatile("" : "+r"(r[i].x), "+r"(r[i].y), "+r"(r[i].z), "+r"(r[i].w));
+                T *to = dz + z.first(mine);
+                const bool some = live && !none;
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    if (mine + i * M >= v1) continue;
+                    uint4 g = make_uint4(0u, 0u, 0u, 0u);
+                    if (some) {
+                        if (fine) {
+                            float f[VE];
+                            unpack16<T>(r[i], f);
+#pragma unroll
+                            for (int e = 0; e < VE; ++e) f[e] = up * prob(f[e]);
+                            g = pack16<T>(f);
+                        } else {
+                            g = scaled_exps<T>(r[i], c2, both(sub), both(up * inv));
+                        }
+                    }
+                    if (z.whole(mine + i * M)) st_stream(to + i * M * VE, g);
+                    else edge[mine + i * M == z.tail] = g;
+                }
+                if (has_head) z.put(dz, z.head, reinterpret_cast<const T *>(edge + (z.head == z.tail)));
+                if (has_tail && z.tail != z.head) z.put(dz, z.tail, reinterpret_cast<const T *>(edge + 1));
+                asm volatile("bar.sync 1, %0;" ::"n"(M) : "memory");     // the warps that hold the row, not the one that reads ahead
+                for (int j = threadIdx.x; live && j < k; j += M) {
+                    const int i = teacher.index[j], v = (i + z.shift) / VE;
+                    if (i >= 0 && v >= v0 && v < v1) dz[i] = from_f<T>(up * (prob(teacher.z[j]) - teacher_mass(teacher, k, i)));
+                }
+            }
+            __syncwarp();
+            if (lane == 0) bar_arrive(sync.t_empty + b);
+        }
+    }
+    if (MODE != RING_BACKWARD) { cluster_arrive(); cluster_wait(); }
+}
+
 template <typename T, int NV, bool STEP> cudaError_t launch_rows(const DistillArgs &a, int ranks, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg = {};
@@ -372,9 +632,78 @@ template <typename T, int NV, bool STEP> cudaError_t launch_rows(const DistillAr
     return e;
 }
 
+// How many clusters of `ranks` blocks the GPU holds at once, asked once per kernel and shape.
+template <typename K> int resident_clusters(K kernel, int threads, int smem, int ranks, int num_sms)
+{
+    struct Known { const void *kernel; int smem, ranks, n; };
+    static thread_local Known known[16];
+    static thread_local unsigned turn = 0;
+    for (const Known &e : known) if (e.kernel == reinterpret_cast<const void *>(kernel) && e.smem == smem && e.ranks == ranks) return e.n;
+    int n = 0;
+    if (ranks > 1) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(unsigned(num_sms / ranks * ranks));
+        cfg.blockDim = dim3(threads);
+        cfg.dynamicSmemBytes = smem;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) { (void)cudaGetLastError(); n = 0; }
+    } else {
+        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess) { (void)cudaGetLastError(); n = 0; }
+        n *= num_sms;
+    }
+    known[turn++ % 16] = Known{reinterpret_cast<const void *>(kernel), smem, ranks, n};
+    return n;
+}
+
+// The ring, where a row fits the registers of up to eight blocks and every resident cluster gets three rows or more;
+// otherwise *done stays false and nothing is launched.
+template <typename T, int M, int MODE> cudaError_t launch_ring(const DistillArgs &a, int vectors, int num_sms, cudaStream_t st, bool *done)
+{
+    const int ranks = (vectors + M * RING_NV - 1) / (M * RING_NV), per = (vectors + ranks - 1) / ranks;
+    const int stage = (per * 16 + 127) / 128 * 128, smem = RING_STAGES * stage + 2 * 3 * a.d.k * 4;
+    auto kernel = distill_ring_kernel<T, M, MODE>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    // the separate gradient needs no cluster: its parts are blocks that know nothing of each other
+    int n = resident_clusters(kernel, M + 32, smem, MODE == RING_BACKWARD ? 1 : ranks, num_sms);
+    if (MODE == RING_BACKWARD) n /= ranks;
+    if (n < 1 || a.d.rows < 3 * int64_t(n)) return cudaSuccess;
+    // the gradient's vectors are stored as z's are read: its rows have to lie in their 16 bytes as z's do
+    if (MODE != RING_FORWARD && ((reinterpret_cast<uintptr_t>(a.dz) ^ reinterpret_cast<uintptr_t>(a.z)) & 15)) return cudaSuccess;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned(n * ranks));
+    cfg.blockDim = dim3(M + 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = MODE == RING_BACKWARD ? 1 : ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, a, ranks, stage);
+    count_launch();
+    *done = true;
+    return e;
+}
+template <typename T, int MODE> cudaError_t try_ring(const DistillArgs &a, int num_sms, cudaStream_t st, bool *done)
+{
+    const int vectors = (a.d.vocab + 2 * Lanes<T>::N - 2) / Lanes<T>::N;       // of a row at the worst shift
+    *done = false;
+    if (vectors <= 256 * RING_NV * MAX_RANKS) return launch_ring<T, 256, MODE>(a, vectors, num_sms, st, done);
+    if (vectors <= 512 * RING_NV * MAX_RANKS) return launch_ring<T, 512, MODE>(a, vectors, num_sms, st, done);
+    return cudaSuccess;
+}
+
 // blocks of a row: a power of two up to 8
 template <typename T> cudaError_t forward_of(const DistillArgs &a, int num_sms, cudaStream_t st)
 {
+    bool done;
+    const cudaError_t e = try_ring<T, RING_FORWARD>(a, num_sms, st, &done);
+    if (done || e != cudaSuccess) return e;
     const int vectors = a.d.vocab / Lanes<T>::N + 2;
     int ranks = 1;
     while (ranks < MAX_RANKS && a.d.rows * ranks < 2 * int64_t(num_sms) && vectors > ranks * ROW_THREADS) ranks *= 2;
@@ -383,6 +712,9 @@ template <typename T> cudaError_t forward_of(const DistillArgs &a, int num_sms, 
 
 template <typename T> cudaError_t backward_of(const DistillArgs &a, int num_sms, cudaStream_t st)
 {
+    bool done;
+    const cudaError_t e = try_ring<T, RING_BACKWARD>(a, num_sms, st, &done);
+    if (done || e != cudaSuccess) return e;
     const int64_t vectors = a.d.vocab / Lanes<T>::N + 2;
     // up to 32 KB of z a block; less where that does not fill the SMs twice over
     int64_t parts = (vectors + 8 * BACK_THREADS - 1) / (8 * BACK_THREADS);
@@ -395,6 +727,9 @@ template <typename T> cudaError_t backward_of(const DistillArgs &a, int num_sms,
 
 template <typename T> cudaError_t step_of(const DistillArgs &a, int num_sms, cudaStream_t st)
 {
+    bool done;
+    cudaError_t e = try_ring<T, RING_STEP>(a, num_sms, st, &done);
+    if (done || e != cudaSuccess) return e;
     constexpr int NV = 8;
     const int vectors = (a.d.vocab + 2 * Lanes<T>::N - 2) / Lanes<T>::N;       // of a row at the worst shift
     int ranks = 1;
@@ -402,9 +737,9 @@ template <typename T> cudaError_t step_of(const DistillArgs &a, int num_sms, cud
     while (ranks < MAX_RANKS && a.d.rows * ranks < 2 * int64_t(num_sms) && vectors > ranks * ROW_THREADS) ranks *= 2;
     if (ranks * NV * ROW_THREADS >= vectors) return launch_rows<T, NV, true>(a, ranks, st);
     // longer than a cluster's registers: two passes
-    DistillArgs b = a;
-    const cudaError_t e = forward_of<T>(a, num_sms, st);
+    e = forward_of<T>(a, num_sms, st);
     if (e != cudaSuccess) return e;
+    DistillArgs b = a;
     b.lse_in = a.lse;
     return backward_of<T>(b, num_sms, st);
 }

@@ -223,6 +223,7 @@ int rubick_distill_forward(rubick_ctx *ctx, const rubick_distill_desc *h_desc, c
     if ((rc = set_device(ctx))) return rc;
     DistillArgs a = {};
     a.d = *h_desc;
+    a.status = ctx->d_status;
     a.z = d_z; a.index = d_index; a.teacher = d_teacher; a.loss = d_loss; a.lse = d_lse;
     CUDA_TRY(ctx, launch_distill_forward(a, ctx->num_sms, ctx->stream), "launch distill_forward");
     return RUBICK_OK;
@@ -242,6 +243,7 @@ int rubick_distill_backward(rubick_ctx *ctx, const rubick_distill_desc *h_desc, 
     if ((rc = set_device(ctx))) return rc;
     DistillArgs a = {};
     a.d = *h_desc;
+    a.status = ctx->d_status;
     a.z = d_z; a.index = d_index; a.teacher = d_teacher; a.lse_in = d_lse; a.dloss = d_dloss; a.dz = d_dz;
     CUDA_TRY(ctx, launch_distill_backward(a, ctx->num_sms, ctx->stream), "launch distill_backward");
     return RUBICK_OK;
@@ -261,6 +263,7 @@ int rubick_distill_step(rubick_ctx *ctx, const rubick_distill_desc *h_desc, cons
     if ((rc = set_device(ctx))) return rc;
     DistillArgs a = {};
     a.d = *h_desc;
+    a.status = ctx->d_status;
     a.z = d_z; a.index = d_index; a.teacher = d_teacher; a.dloss = d_dloss; a.loss = d_loss; a.lse = d_lse; a.dz = d_dz;
     CUDA_TRY(ctx, launch_distill_step(a, ctx->num_sms, ctx->stream), "launch distill_step");
     return RUBICK_OK;

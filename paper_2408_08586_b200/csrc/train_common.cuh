@@ -266,6 +266,7 @@ struct DistillArgs {
     const float *lse_in, *dloss;
     float *loss, *lse;
     void *dz;
+    uint32_t *status;            // the context's status word
 };
 
 size_t norm_backward_scratch(const NormArgs &a, int num_sms, int64_t *chunk_rows, int *n_chunks);

@@ -396,6 +396,14 @@ DISTILL_CASES = [
     (1, 270001, 100, "bf16", "fp32", dict(temperature=1.5)),
     (600, 200, 16, "bf16", "fp32", dict(padded=300)),
     (350, 4100, 8, "fp32", "fp32", {}),
+    # rows enough for the clusters that stay: one, two, five and eight blocks a row
+    (1500, 203, 7, "fp32", "fp32", dict(padded=4)),
+    (2100, 1003, 20, "bf16", "fp32", dict(padded=100, shift=5)),
+    (1400, 16384, 9, "bf16", "bf16", {}),
+    (720, 20011, 33, "fp16", "fp32", dict(temperature=2.0)),
+    (110, 140001, 64, "bf16", "fp32", dict(padded=3)),
+    (170, 128000, 64, "bf16", "fp32", dict(temperature=0.5)),
+    (100, 70001, 1024, "fp32", "fp16", dict(pad=3)),
 ]
 
 
@@ -442,11 +450,11 @@ def test_distill_forward_backward_and_step(ctx, case):
     assert torch.equal(alone, loss)
 
 
-@pytest.mark.parametrize("vocab", [4096, 5001, 140001])
-def test_distill_writes_the_gradient_over_the_logits(ctx, vocab):
+@pytest.mark.parametrize("rows,vocab", [(6, 4096), (6, 5001), (6, 140001), (700, 20011)])
+def test_distill_writes_the_gradient_over_the_logits(ctx, rows, vocab):
     import torch
-    z, index, teacher, desc = distill_case(6, vocab, 16, "bf16" if vocab < 9000 else "fp32", "fp32", padded=1)
-    f = lambda: torch.empty(6, device="cuda")  # noqa: E731
+    z, index, teacher, desc = distill_case(rows, vocab, 16, "bf16" if vocab < 90000 else "fp32", "fp32", padded=1)
+    f = lambda: torch.empty(rows, device="cuda")  # noqa: E731
     loss, lse, out = f(), f(), torch.empty_like(z)
     ctx.distill_step(desc, z, index, teacher, None, loss, lse, out)
     z1, z2 = z.clone(), z.clone()
