@@ -147,7 +147,7 @@ template <typename T> __device__ __forceinline__ void read_teacher(const Distill
     for (int j = lane; j < k; j += 32) {
         const int i = t.index[j];
         t.log_q[j] = i >= 0 ? (t.log_q[j] - top) * c - log_total : -INFINITY;
-        t.z[j] = i >= c0 && i < c1 ? to_f(z.row[i]) : -INFINITY;
+        t.z[j] = i >= 0 && i >= c0 && i < c1 ? to_f(z.row[i]) : -INFINITY;
     }
     if (lane == 0) *t.live = any;
     __syncwarp();
@@ -404,14 +404,23 @@ __global__ void __launch_bounds__(BACK_THREADS, 4) distill_backward_kernel(const
 // rows are on their way into shared memory.  One more warp per block issues those copies and reads the next row's
 // teacher entries, whose two dependent reads (index, then logit) would otherwise stand before every row.  The blocks of
 // a cluster send each other their warps' pairs with asynchronous stores that count towards the receiver's barrier:
-// nobody waits for anything but the 8 bytes a warp that it needs.
+// nobody waits for anything but the 8 bytes a warp that it needs.  The teacher's places are corrected by the warp that
+// wrote them, so that the block's warps never meet.
 
 enum { RING_STEP, RING_FORWARD, RING_BACKWARD };
 constexpr int RING_NV = 8;        // vectors a thread holds
 constexpr int RING_STAGES = 2;
+constexpr int RING_CLAIMS = 1024; // slots in which the entries of a row find their doubles
 
 struct RingSync {
     uint64_t full[RING_STAGES], empty[RING_STAGES], t_full[2], t_empty[2], x_full[2];
+};
+
+// the entries that lie in a block's own part, each place once, with all of its q
+struct Own {
+    int32_t *index;
+    float *z, *mass;
+    int32_t *count;
 };
 
 __device__ __forceinline__ void bar_init_n(uint64_t *bar, uint32_t n)
@@ -432,23 +441,64 @@ __device__ __forceinline__ void send_pair(Pair *at, uint64_t *bar, Pair p, uint3
                  ::"r"(ra), "r"(__float_as_uint(p.m)), "r"(__float_as_uint(p.s)), "r"(rb) : "memory");
 }
 
-template <typename T, int M, int MODE>
-__global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(const __grid_constant__ DistillArgs a, int ranks, int stage_bytes)
+// Lists the entries in elements c0 .. c1, by one warp.  Doubles are found by claiming: every entry writes its number into
+// the slot of its index and looks who stayed; only one that lost its slot compares itself with all the others.  Where
+// there are doubles, the first of a place takes the q of all of them.
+__device__ __forceinline__ void list_own(const Teacher &t, int k, int c0, int c1, uint16_t *claims, const Own &own)
+{
+    const int lane = threadIdx.x & 31;
+    for (int j = lane; j < k; j += 32) if (t.index[j] >= 0) claims[t.index[j] % RING_CLAIMS] = uint16_t(j);
+    __syncwarp();
+    bool doubles = false;
+    for (int j = lane; j < k; j += 32) {
+        const int i = t.index[j];
+        if (i >= 0 && i >= c0 && i < c1 && claims[i % RING_CLAIMS] != j)
+            for (int q = 0; q < k; ++q) doubles |= q != j && t.index[q] == i;
+    }
+    doubles = __any_sync(0xffffffffu, doubles);
+    int n = 0;
+    for (int j0 = 0; j0 < k; j0 += 32) {
+        const int j = j0 + lane, i = j < k ? t.index[j] : -1;
+        bool mine = i >= 0 && i >= c0 && i < c1;    // (a part may begin before its row does: c0 < 0)
+        float mass = mine ? ex2(t.log_q[j]) : 0.f;
+        if (mine && doubles)
+            for (int q = 0; q < k; ++q)
+                if (q != j && t.index[q] == i) { mass += ex2(t.log_q[q]); if (q < j) mine = false; }
+        const uint32_t set = __ballot_sync(0xffffffffu, mine);
+        if (mine) {
+            const int at = n + __popc(set & ((1u << lane) - 1u));
+            own.index[at] = i; own.z[at] = t.z[j]; own.mass[at] = mass;
+        }
+        n += __popc(set);
+    }
+    if (lane == 0) *own.count = n;
+    __syncwarp();
+}
+
+// RAGGED: rows that do not begin and end on 16-byte boundaries
+template <typename T, int M, int MODE, bool RAGGED>
+__global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(const __grid_constant__ DistillArgs a, int ranks, int per)
 {
     constexpr int VE = Lanes<T>::N, NV = RING_NV, WARPS = M / 32;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) RingSync sync;
     __shared__ __align__(16) Pair pairs[2][MAX_RANKS * WARPS];
-    __shared__ int32_t live_of[2];
-    __shared__ uint4 edge[2];                     // gradients of the row's first and last vector where it shares them
+    __shared__ int32_t live_of[2], count_of[2];
     __shared__ float lse_of[2], up_of[2];
+    __shared__ uint16_t claims[RING_CLAIMS];
+    __shared__ uint4 edge[2];                     // gradients of the row's first and last vector where it shares them
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, k = a.d.k;
     const int rank = blockIdx.x % ranks, clusters = gridDim.x / ranks, first_row = blockIdx.x / ranks;
+    const int v0 = rank * per, iters = (per + M - 1) / M, stage_bytes = per * 16;
     const float c = LOG2E / a.d.temperature;
-    uint8_t *entries = smem + RING_STAGES * stage_bytes;
+    const auto entries = [&](int b) { return reinterpret_cast<int32_t *>(smem + RING_STAGES * stage_bytes) + b * 6 * k; };
     const auto teacher_at = [&](int b) {
-        int32_t *base = reinterpret_cast<int32_t *>(entries) + b * 3 * k;
+        int32_t *base = entries(b);
         return Teacher{base, reinterpret_cast<float *>(base + k), reinterpret_cast<float *>(base + 2 * k), live_of + b};
+    };
+    const auto own_at = [&](int b) {
+        int32_t *base = entries(b) + 3 * k;
+        return Own{base, reinterpret_cast<float *>(base + k), reinterpret_cast<float *>(base + 2 * k), count_of + b};
     };
     if (threadIdx.x == 0) {
         for (int i = 0; i < RING_STAGES; ++i) { bar_init_n(sync.full + i, 1); bar_init_n(sync.empty + i, WARPS); }
@@ -469,16 +519,18 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
             const int64_t row = first_row + int64_t(n) * clusters;
             if (row >= a.d.rows) return;
             const RowView<T> z(a.z, row, a.d.ld, a.d.vocab);
-            const int per = (z.vectors + ranks - 1) / ranks, v0 = rank * per, v1 = v0 + per < z.vectors ? v0 + per : z.vectors;
+            const int v1 = v0 + per < z.vectors ? v0 + per : z.vectors;
             uint8_t *stage = smem + (n % RING_STAGES) * stage_bytes;
             int b0 = v0, b1 = v1 > v0 ? v1 : v0;
-            if (row == 0 && b0 == 0 && b1 > 0 && !z.whole(0)) {
-                if (lane == 0) *reinterpret_cast<uint4 *>(stage) = z.load(0);
-                b0 = 1;
-            }
-            if (row == a.d.rows - 1 && b1 == z.vectors && b1 > b0 && !z.whole(b1 - 1)) {
-                if (lane == 0) *reinterpret_cast<uint4 *>(stage + size_t(b1 - 1 - v0) * 16) = z.load(b1 - 1);
-                --b1;
+            if (RAGGED) {
+                if (row == 0 && b0 == 0 && b1 > 0 && !z.whole(0)) {
+                    if (lane == 0) *reinterpret_cast<uint4 *>(stage) = z.load(0);
+                    b0 = 1;
+                }
+                if (row == a.d.rows - 1 && b1 == z.vectors && b1 > b0 && !z.whole(b1 - 1)) {
+                    if (lane == 0) *reinterpret_cast<uint4 *>(stage + size_t(b1 - 1 - v0) * 16) = z.load(b1 - 1);
+                    --b1;
+                }
             }
             if (lane == 0) {
                 const uint32_t bytes = b1 > b0 ? uint32_t(b1 - b0) * 16 : 0;
@@ -493,14 +545,14 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
             const int b = n & 1;
             if (n >= 2) wait(sync.t_empty + b, ((n >> 1) - 1) & 1);
             const RowView<T> z(a.z, row, a.d.ld, a.d.vocab);
-            const int per = (z.vectors + ranks - 1) / ranks, v0 = rank * per, v1 = v0 + per < z.vectors ? v0 + per : z.vectors;
+            const int v1 = v0 + per < z.vectors ? v0 + per : z.vectors, c0 = z.first(v0), c1 = z.first(v1);
             const bool all = MODE != RING_BACKWARD && rank == 0;         // the loss is this block's
             if (lane == 0) {
                 if (MODE == RING_BACKWARD) lse_of[b] = a.lse_in[row];
                 if (MODE != RING_FORWARD) up_of[b] = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature;
             }
-            read_teacher<T>(a, row, z, all ? 0 : z.first(v0), all ? z.vocab : z.first(v1), teacher_at(b));
-            __syncwarp();
+            read_teacher<T>(a, row, z, all ? 0 : c0, all ? z.vocab : c1, teacher_at(b));
+            if (MODE != RING_FORWARD) list_own(teacher_at(b), k, c0, c1, claims, own_at(b));
             if (lane == 0) bar_arrive(sync.t_full + b);
             wait(sync.empty + n % RING_STAGES, (n / RING_STAGES) & 1);   // the row is in the other warps' registers
             issue(n + RING_STAGES);
@@ -508,24 +560,27 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
     } else {
         const f2 c2 = both(c);
         int n = 0;
+        RowView<T> z(a.z, first_row, a.d.ld, a.d.vocab);
         for (int64_t row = first_row; row < a.d.rows; row += clusters, ++n) {
             const int b = n & 1, st = n % RING_STAGES;
-            const RowView<T> z(a.z, row, a.d.ld, a.d.vocab);
-            const int per = (z.vectors + ranks - 1) / ranks, v0 = rank * per, v1 = v0 + per < z.vectors ? v0 + per : z.vectors;
-            const int mine = v0 + int(threadIdx.x);
+            if (RAGGED) z = RowView<T>(a.z, row, a.d.ld, a.d.vocab);
+            const int v1 = v0 + per < z.vectors ? v0 + per : z.vectors, mine = v0 + int(threadIdx.x);
             if (MODE != RING_BACKWARD && threadIdx.x == 0) bar_expect(sync.x_full + b, uint32_t(ranks * WARPS * sizeof(Pair)));
             wait(sync.full + st, (n / RING_STAGES) & 1);
             uint4 r[NV];
-            uint8_t *from = smem + st * stage_bytes + threadIdx.x * 16;
+            uint8_t *stage = smem + st * stage_bytes;
             // the thread that holds the row's first or last vector clears what is not the row's
-            const bool has_head = v0 <= z.head && z.head < v1 && threadIdx.x == 0;
-            const bool has_tail = v0 <= z.tail && z.tail < v1 && int(threadIdx.x) == (z.tail - v0) % M;
-            if (has_head) z.mask(z.head, reinterpret_cast<T *>(from));
-            if (has_tail) z.mask(z.tail, reinterpret_cast<T *>(smem + st * stage_bytes + size_t(z.tail - v0) * 16));
+            const bool has_head = RAGGED && v0 <= z.head && z.head < v1 && threadIdx.x == 0;
+            const bool has_tail = RAGGED && v0 <= z.tail && z.tail < v1 && int(threadIdx.x) == (z.tail - v0) % M;
+            if (has_head) z.mask(z.head, reinterpret_cast<T *>(stage));
+            if (has_tail) z.mask(z.tail, reinterpret_cast<T *>(stage + size_t(z.tail - v0) * 16));
+            // the next copy into this stage comes behind these stores
+            if (has_head || has_tail) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
+                if (i >= iters) continue;                    // (the same for all threads)
                 r[i] = no_logits<T>();                       // so that the arithmetic below need not ask
-                if (mine + i * M < v1) r[i] = *reinterpret_cast<const uint4 *>(from + i * M * 16);
+                if (mine + i * M < v1) r[i] = *reinterpret_cast<const uint4 *>(stage + (i * M + int(threadIdx.x)) * 16);
             }
             __syncwarp();
             if (lane == 0) bar_arrive(sync.empty + st);
@@ -533,13 +588,13 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
             if constexpr (MODE != RING_BACKWARD) {
                 Top<T> top;
 #pragma unroll
-                for (int i = 0; i < NV; ++i) top.take(r[i]);
+                for (int i = 0; i < NV; ++i) if (i < iters) top.take(r[i]);
                 Pair p;
                 p.m = warp_max(top.get());
                 const f2 off = both(p.m == -INFINITY ? 0.f : -p.m * c);
                 f2 s = 0ull;
 #pragma unroll
-                for (int i = 0; i < NV; ++i) s = add_exps<T>(r[i], c2, off, s);
+                for (int i = 0; i < NV; ++i) if (i < iters) s = add_exps<T>(r[i], c2, off, s);
                 p.s = warp_sum(lo(s) + hi(s));
                 // the first block has read every logit that it needs before another block may write over it
                 wait(sync.t_full + b, (n >> 1) & 1);
@@ -561,34 +616,32 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
             } else {
                 wait(sync.t_full + b, (n >> 1) & 1);
             }
-            const Teacher teacher = teacher_at(b);
-            const bool live = *teacher.live;
-            if (MODE != RING_BACKWARD && rank == 0 && warp == 0) write_loss(a, row, teacher, shift, total, live);
+            const bool live = live_of[b];
+            if (MODE != RING_BACKWARD && rank == 0 && warp == 0) write_loss(a, row, teacher_at(b), shift, total, live);
             if constexpr (MODE != RING_FORWARD) {
                 const float up = up_of[b];
                 float inv = 1.f, sub = -shift * c;           // p = inv 2^(z c + sub)
                 bool none = false;
-                if (MODE == RING_STEP) inv = total > 0.f || total != total ? 1.f / total : 0.f;
+                if (MODE == RING_STEP) inv = total > 0.f || total != total ? __fdividef(1.f, total) : 0.f;
                 else { sub = -lse_of[b] * LOG2E; none = lse_of[b] == -INFINITY; }
                 // single-precision gradients from a saved log-sum: what the factors lose by rounding is added back
-                const bool fine = MODE == RING_BACKWARD && sizeof(T) == 4;
-                const float c_low = fine ? float(LOG2E_D / double(a.d.temperature) - double(c)) : 0.f;
-                const float sub_low = fine ? float(-double(lse_of[b]) * LOG2E_D - double(sub)) : 0.f;
+                constexpr bool FINE = MODE == RING_BACKWARD && sizeof(T) == 4;
+                const float c_low = FINE ? float(LOG2E_D / double(a.d.temperature) - double(c)) : 0.f;
+                const float sub_low = FINE ? float(-double(lse_of[b]) * LOG2E_D - double(sub)) : 0.f;
                 const auto prob = [&](float x) {
-                    return x == -INFINITY || none ? 0.f : inv * ex2(fine ? fmaf(x, c, sub) + fmaf(x, c_low, sub_low) : fmaf(x, c, sub));
+                    return x == -INFINITY || none ? 0.f : inv * ex2(FINE ? fmaf(x, c, sub) + fmaf(x, c_low, sub_low) : fmaf(x, c, sub));
                 };
-                T *dz = static_cast<T *>(a.dz) + row * a.d.ld;
+                T *dz = static_cast<T *>(a.dz) + row * a.d.ld, *to = dz + z.first(mine);
+                const bool some = live && !none;
                 // unpacked anew: kept since the sum they would fill the registers
 #pragma unroll
                 for (int i = 0; i < NV; ++i) asm volatile("" : "+r"(r[i].x), "+r"(r[i].y), "+r"(r[i].z), "+r"(r[i].w));
-                T *to = dz + z.first(mine);
-                const bool some = live && !none;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) {
-                    if (mine + i * M >= v1) continue;
+                    if (i >= iters) continue;
                     uint4 g = make_uint4(0u, 0u, 0u, 0u);
                     if (some) {
-                        if (fine) {
+                        if constexpr (FINE) {
                             float f[VE];
                             unpack16<T>(r[i], f);
 #pragma unroll
@@ -598,15 +651,19 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
                             g = scaled_exps<T>(r[i], c2, both(sub), both(up * inv));
                         }
                     }
-                    if (z.whole(mine + i * M)) st_stream(to + i * M * VE, g);
-                    else edge[mine + i * M == z.tail] = g;
+                    if (mine + i * M < v1) {
+                        if (!RAGGED || z.whole(mine + i * M)) st_stream(to + i * M * VE, g);
+                        else edge[mine + i * M == z.tail] = g;
+                    }
                 }
                 if (has_head) z.put(dz, z.head, reinterpret_cast<const T *>(edge + (z.head == z.tail)));
                 if (has_tail && z.tail != z.head) z.put(dz, z.tail, reinterpret_cast<const T *>(edge + 1));
-                asm volatile("bar.sync 1, %0;" ::"n"(M) : "memory");     // the warps that hold the row, not the one that reads ahead
-                for (int j = threadIdx.x; live && j < k; j += M) {
-                    const int i = teacher.index[j], v = (i + z.shift) / VE;
-                    if (i >= 0 && v >= v0 && v < v1) dz[i] = from_f<T>(up * (prob(teacher.z[j]) - teacher_mass(teacher, k, i)));
+                __syncwarp();                                // this warp's vectors are written
+                const Own own = own_at(b);
+                const int count = live && !lost ? count_of[b] : 0;
+                for (int j = lane; j < count; j += 32) {
+                    const int i = own.index[j], u = (i + z.shift) / VE - v0;
+                    if (u % M / 32 == warp) dz[i] = from_f<T>(up * (prob(own.z[j]) - own.mass[j]));
                 }
             }
             __syncwarp();
@@ -661,11 +718,11 @@ template <typename K> int resident_clusters(K kernel, int threads, int smem, int
 
 // The ring, where a row fits the registers of up to eight blocks and every resident cluster gets three rows or more;
 // otherwise *done stays false and nothing is launched.
-template <typename T, int M, int MODE> cudaError_t launch_ring(const DistillArgs &a, int vectors, int num_sms, cudaStream_t st, bool *done)
+template <typename T, int M, int MODE, bool RAGGED> cudaError_t launch_ring(const DistillArgs &a, int vectors, int num_sms, cudaStream_t st, bool *done)
 {
     const int ranks = (vectors + M * RING_NV - 1) / (M * RING_NV), per = (vectors + ranks - 1) / ranks;
-    const int stage = (per * 16 + 127) / 128 * 128, smem = RING_STAGES * stage + 2 * 3 * a.d.k * 4;
-    auto kernel = distill_ring_kernel<T, M, MODE>;
+    const int smem = RING_STAGES * per * 16 + 2 * 6 * a.d.k * 4;
+    auto kernel = distill_ring_kernel<T, M, MODE, RAGGED>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != cudaSuccess) return e;
     // the separate gradient needs no cluster: its parts are blocks that know nothing of each other
@@ -684,7 +741,7 @@ template <typename T, int M, int MODE> cudaError_t launch_ring(const DistillArgs
     at[0].val.clusterDim.x = MODE == RING_BACKWARD ? 1 : ranks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, a, ranks, stage);
+    e = cudaLaunchKernelEx(&cfg, kernel, a, ranks, per);
     count_launch();
     *done = true;
     return e;
@@ -693,8 +750,9 @@ template <typename T, int MODE> cudaError_t try_ring(const DistillArgs &a, int n
 {
     const int vectors = (a.d.vocab + 2 * Lanes<T>::N - 2) / Lanes<T>::N;       // of a row at the worst shift
     *done = false;
-    if (vectors <= 256 * RING_NV * MAX_RANKS) return launch_ring<T, 256, MODE>(a, vectors, num_sms, st, done);
-    if (vectors <= 512 * RING_NV * MAX_RANKS) return launch_ring<T, 512, MODE>(a, vectors, num_sms, st, done);
+    const bool ragged = a.d.ld * int64_t(sizeof(T)) % 16 || reinterpret_cast<uintptr_t>(a.z) % 16 || a.d.vocab % Lanes<T>::N;
+    if (vectors <= 256 * RING_NV * MAX_RANKS) return ragged ? launch_ring<T, 256, MODE, true>(a, vectors, num_sms, st, done) : launch_ring<T, 256, MODE, false>(a, vectors, num_sms, st, done);
+    if (vectors <= 512 * RING_NV * MAX_RANKS) return ragged ? launch_ring<T, 512, MODE, true>(a, vectors, num_sms, st, done) : launch_ring<T, 512, MODE, false>(a, vectors, num_sms, st, done);
     return cudaSuccess;
 }
 
