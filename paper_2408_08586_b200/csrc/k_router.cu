@@ -7,10 +7,20 @@
 //   + w_j d_j at the chosen and - p_e sum_i w_i d_i everywhere (raw weights).
 //
 // A row is spread over a power of two of lanes, EPL elements a lane, so that a warp works on 32 / lanes rows at once
-// and nothing of a row leaves the registers.  The choice compares 32-bit keys whose unsigned order is that of the
-// logits; the lowest index wins among equal ones.  Probability sums stay in the lane that owns the column until
-// its chunk of rows ends, then go chunk by chunk, in order, into the group's sum: the last block of a group to arrive
-// adds them up, the last group to arrive adds up the loss.
+// and nothing of a row leaves the registers.
+//
+// The choice works on 32-bit keys: the upper bits of the logit, in unsigned order, and in the lower ones the expert's
+// number from the top, so that no two keys are equal and the lowest index wins among equal logits.  Sixteen-bit
+// logits fit the upper bits whole.  Of single-precision ones some bits are cut off: where two neighbours among the
+// first k + 1 keys differ in nothing but these, the row is chosen again with whole keys.  Every lane sorts its own keys
+// once; after that one of the k is a maximum over the lanes' first keys (one instruction for a whole warp) and a
+// shift of one lane's list.
+//
+// Bound by instruction issue, not by memory: a row of 128 experts is 512 bytes, and its choice some 200 instructions.
+//
+// Probability sums stay in the lane that owns the column until its chunk of rows ends, then go chunk by chunk, in order,
+// into the group's sum: the last block of a group to arrive adds them up, the last of all the loss.  Where groups are
+// many, each belongs to one warp alone.
 
 #include "train_common.cuh"
 
@@ -64,17 +74,171 @@ __device__ __forceinline__ void load_logits(const T *row, int sub, int lanes, in
     }
 }
 
-__device__ __forceinline__ float lanes_sum(float v, int lanes)
+template <bool WARP> __device__ __forceinline__ float lanes_sum(float v, int lanes)
 {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) { const float t = __shfl_xor_sync(0xffffffffu, v, o); if (o < lanes) v += t; }
+    for (int o = 16; o; o >>= 1) {
+        const float t = __shfl_xor_sync(0xffffffffu, v, o);
+        if (WARP || o < lanes) v += t;
+    }
     return v;
 }
-__device__ __forceinline__ float lanes_max(float v, int lanes)
+template <bool WARP> __device__ __forceinline__ float lanes_max(float v, int lanes)
 {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) { const float t = __shfl_xor_sync(0xffffffffu, v, o); if (o < lanes) v = fmaxf(v, t); }
+    for (int o = 16; o; o >>= 1) { const float t = __shfl_xor_sync(0xffffffffu, v, o); if (WARP || o < lanes) v = fmaxf(v, t); }
     return v;
+}
+template <bool WARP> __device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes)
+{
+    if constexpr (WARP) {
+        return __reduce_max_sync(0xffffffffu, v);
+    } else {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) { const uint32_t t = __shfl_xor_sync(0xffffffffu, v, o); if (o < lanes) v = max(v, t); }
+        return v;
+    }
+}
+
+// Descending sort of a lane's keys by Batcher's odd-even merge network (K. E. Batcher, 1968)
+template <int N> __device__ __forceinline__ void sort_keys(uint32_t (&s)[N])
+{
+#pragma unroll
+    for (int p = 1; p < N; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int j = k % p; j + k < N; j += 2 * k)
+#pragma unroll
+                for (int i = 0; i < k; ++i)
+                    if (i + j + k < N && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                        const uint32_t x = s[i + j], y = s[i + j + k];
+                        s[i + j] = max(x, y); s[i + j + k] = min(x, y);
+                    }
+}
+
+// The state of a warp's rows while it goes through a chunk
+template <int EPL> struct Tally { float acc[EPL]; int valid; };
+
+// One row per group of lanes: index, weight and histogram are written, probabilities added to the tally.
+template <typename T, int EPL, bool VEC, bool WARP>
+__device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, bool here, const float (&z)[EPL], int lanes, int sub, int bits,
+                                           uint32_t *list, float *kept, int32_t *hist, Tally<EPL> &tally)
+{
+    constexpr int VE = Lanes<T>::N;
+    const int k = a.d.k;
+    const uint32_t low = (1u << bits) - 1u;
+    // keys: NaN counts as -inf, -0 as 0; a row that is masked reads as -inf
+    uint32_t key[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        const uint32_t b = __float_as_uint(fmaxf(z[i], -INFINITY) + 0.f);
+        const uint32_t ordered = b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
+        key[i] = (ordered & ~low) | (low - uint32_t(column<VEC, VE>(i, sub, lanes)));
+    }
+    if constexpr (sizeof(T) == 4) {
+        // the chosen logits are looked up whole
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) kept[column<VEC, VE>(i, sub, lanes)] = z[i];
+    }
+    sort_keys<EPL>(key);
+    uint32_t first = 0u, mine = 0u;
+#pragma unroll 1
+    for (int j = 0; j < k; ++j) {
+        const uint32_t m = lanes_max<WARP>(key[0], lanes);
+        if (j == 0) first = m;
+        if (WARP) mine = sub == j ? m : mine;
+        else if (sub == (j & (lanes - 1))) list[j] = m;
+        const bool won = key[0] == m;
+#pragma unroll
+        for (int i = 0; i + 1 < EPL; ++i) key[i] = won ? key[i + 1] : key[i];
+        key[EPL - 1] = won ? 0u : key[EPL - 1];
+    }
+    const uint32_t none = KEY_NINF | low;         // up to here: closed, or not a column
+    const bool some = first > none;
+    // what the keys leave of the largest logit: the exponentials need its neighbourhood, not its last bits
+    const uint32_t top = first & ~low;
+    const float shift = some ? __uint_as_float(top & 0x80000000u ? top & 0x7fffffffu : ~(top | low)) : 0.f;
+    const float off = -shift * 1.4426950408889634f;
+    float e[EPL], total = 0.f;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[i]) : "f"(fmaf(z[i], 1.4426950408889634f, off)));
+        total += e[i];
+    }
+    total = lanes_sum<WARP>(total, lanes);
+    const float inv = some ? __fdividef(1.f, total) : 0.f;
+    if (some) {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) tally.acc[i] = fmaf(e[i], inv, tally.acc[i]);
+    }
+    tally.valid += some && sub == 0 ? 1 : 0;
+    if (!WARP || sizeof(T) == 4) __syncwarp();
+    if constexpr (sizeof(T) == 4) {
+        // neighbours that only the cut-off bits tell apart: once more, with whole keys
+        const uint32_t next = lanes_max<WARP>(key[0], lanes);
+        bool unsure = false;
+        for (int j = sub; j < k; j += lanes) {
+            const uint32_t x = WARP ? mine : list[j], y = j + 1 == k ? next : WARP ? 0u : list[j + 1];
+            if (WARP && j + 1 < k) continue;      // (compared below, with the next lane's)
+            unsure |= (x & ~low) == (y & ~low) && x > none && kept[low - (x & low)] != kept[low - (y & low)];
+        }
+        if constexpr (WARP) {
+            const uint32_t y = __shfl_down_sync(0xffffffffu, mine, 1);
+            if (sub + 1 < k) unsure |= (mine & ~low) == (y & ~low) && mine > none && kept[low - (mine & low)] != kept[low - (y & low)];
+        }
+        if (__any_sync(0xffffffffu, unsure)) {
+            uint32_t whole[EPL];
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) whole[i] = order_key(z[i]);
+#pragma unroll 1
+            for (int j = 0; j < k; ++j) {
+                uint32_t best = 0u;
+                int col = 0x7fffffff;
+#pragma unroll
+                for (int i = 0; i < EPL; ++i)
+                    if (whole[i] > best) { best = whole[i]; col = column<VEC, VE>(i, sub, lanes); }
+#pragma unroll
+                for (int o = 16; o; o >>= 1) {
+                    const uint32_t kb = __shfl_xor_sync(0xffffffffu, best, o);
+                    const int cb = __shfl_xor_sync(0xffffffffu, col, o);
+                    if (o < lanes && (kb > best || (kb == best && cb < col))) { best = kb; col = cb; }
+                }
+                const uint32_t m = best > KEY_NINF ? 0x80000000u | (low - uint32_t(col)) : 0u;      // any key of that column that is open
+                if (WARP) mine = sub == j ? m : mine;
+                else if (sub == (j & (lanes - 1))) list[j] = m;
+#pragma unroll
+                for (int i = 0; i < EPL; ++i) if (column<VEC, VE>(i, sub, lanes) == col) whole[i] = 0u;
+            }
+            __syncwarp();
+        }
+    }
+    // places: lane j of the row has the j-th (and the j + lanes-th ...)
+    float sum = 0.f;
+    for (int j = sub; j < k; j += lanes) {
+        const uint32_t m = WARP ? mine : list[j];
+        const int col = int(low - (m & low));
+        const bool ok = m > none;
+        const uint32_t b = m & ~low;
+        const float logit = sizeof(T) == 4 ? (ok ? kept[col] : 0.f) : __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~(b | low));
+        float w;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(fmaf(logit, 1.4426950408889634f, off)));
+        w = ok ? w * inv : 0.f;
+        sum += w;
+        if (here) {
+            a.index[row * k + j] = ok ? col : -1;
+            if (!(a.d.flags & RUBICK_ROUTER_RENORM)) a.weight[row * k + j] = w;
+            else if (!WARP) list[j] = __float_as_uint(w);     // (this lane's own place)
+            else mine = __float_as_uint(w);
+            if (ok) atomicAdd(hist + col, 1);
+        }
+    }
+    if (a.d.flags & RUBICK_ROUTER_RENORM) {
+        sum = lanes_sum<WARP>(sum, lanes);
+        const float share = sum > 0.f || sum != sum ? __fdividef(1.f, sum) : 0.f;
+        for (int j = sub; here && j < k; j += lanes) a.weight[row * k + j] = __uint_as_float(WARP ? mine : list[j]) * share;
+    }
+    if (!WARP || sizeof(T) == 4) __syncwarp();    // list and kept are free again
 }
 
 // What is left of a group once every row is counted: dot = sum_e counts_e S_e of this thread's experts
@@ -132,88 +296,122 @@ __device__ void join_loss(const RouterArgs &a)
     }
 }
 
-// blockIdx.x = chunk of rows within the group, blockIdx.y (and z) = group
-template <typename T, int EPL, bool VEC>
-__global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __grid_constant__ RouterArgs a, int lanes)
+// Goes through rows first, first + stride, ... below end, per_warp at a time, with the next ones on their way.
+template <typename T, int EPL, bool VEC, bool WARP>
+__device__ __forceinline__ void route_chunk(const RouterArgs &a, int64_t first, int64_t end, int64_t stride, int lanes, int sub, int slot, int bits,
+                                            uint32_t *list, float *kept, int32_t *hist, Tally<EPL> &tally)
+{
+    const int E = a.d.experts;
+    float z[EPL], next[EPL];
+    bool here = false;
+    const auto fetch = [&](int64_t row, float (&v)[EPL]) {
+        here = row < end;
+        const bool keep = here && (!a.mask || a.mask[row]);
+        load_logits<T, EPL, VEC>(static_cast<const T *>(a.logits) + (keep ? row : 0) * a.d.ld, sub, lanes, keep ? E : 0, v);
+    };
+    if (first < end) fetch(first + slot, next);
+    for (int64_t row = first; row < end; row += stride) {
+        const bool h = here;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) z[i] = next[i];
+        if (row + stride < end) fetch(row + stride + slot, next);
+        route_rows<T, EPL, VEC, WARP>(a, row + slot, h, z, lanes, sub, bits, list, kept, hist, tally);
+    }
+}
+
+// the sums of a warp's rows, at the lanes of its first row
+template <int EPL> __device__ __forceinline__ void fold_rows(Tally<EPL> &t, int lanes)
+{
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+#pragma unroll
+        for (int o = 16; o; o >>= 1) { const float x = __shfl_xor_sync(0xffffffffu, t.acc[i], o); if (o >= lanes) t.acc[i] += x; }
+    t.valid = __reduce_add_sync(0xffffffffu, t.valid);
+}
+
+// shared memory of the forward kernel, in words: [1 or warps][E] assignments, [warps][E] probability sums, per warp
+// 32 EPL logits (single precision) and a list of k keys per row
+template <typename T, int EPL> __host__ __device__ __forceinline__ int kept_words() { return sizeof(T) == 4 ? 32 * EPL : 0; }
+
+// blockIdx.x = chunk of rows within the group, blockIdx.y = group; by_warp: a warp takes whole groups
+template <typename T, int EPL, bool VEC, bool WARP>
+__global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __grid_constant__ RouterArgs a, int lanes, int bits, bool by_warp)
 {
     constexpr int VE = Lanes<T>::N;
-    extern __shared__ int32_t smem[];             // [E] assignments, then [warps][E] probability sums
+    extern __shared__ int32_t smem[];
     __shared__ int32_t valid_rows;
     __shared__ bool last;
-    const int E = a.d.experts, k = a.d.k, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int sub = lane & (lanes - 1), per_warp = 32 / lanes;
-    int32_t *hist = smem;
+    const int E = a.d.experts, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (WARP) lanes = 32;
+    const int sub = lane & (lanes - 1), per_warp = 32 / lanes, slot = lane / lanes;
+    int32_t *hist = smem + (by_warp ? warp * E : 0);
     float *psum = reinterpret_cast<float *>(smem + E);
-    for (int e = threadIdx.x; e < E; e += ROUTER_THREADS) hist[e] = 0;
+    int32_t *own = smem + (by_warp ? ROUTER_WARPS : ROUTER_WARPS + 1) * E + warp * (kept_words<T, EPL>() + (WARP ? 0 : per_warp * a.d.k));
+    float *kept = reinterpret_cast<float *>(own) + slot * lanes * EPL;
+    uint32_t *list = reinterpret_cast<uint32_t *>(own + kept_words<T, EPL>()) + slot * a.d.k;
+    for (int e = threadIdx.x; e < E * (by_warp ? ROUTER_WARPS : 1); e += ROUTER_THREADS) smem[e] = 0;
     if (threadIdx.x == 0) valid_rows = 0;
     __syncthreads();
+    if (by_warp) {
+        for (int64_t g = int64_t(blockIdx.x) * ROUTER_WARPS + warp; g < a.groups; g += int64_t(gridDim.x) * ROUTER_WARPS) {
+            const int64_t g0 = g * a.d.group_rows, g1 = g0 + a.d.group_rows < a.d.rows ? g0 + a.d.group_rows : a.d.rows;
+            Tally<EPL> t;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) t.acc[i] = 0.f;
+            t.valid = 0;
+            route_chunk<T, EPL, VEC, WARP>(a, g0, g1, per_warp, lanes, sub, slot, bits, list, kept, hist, t);
+            fold_rows(t, lanes);
+            __syncwarp();
+            float dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                const int c = column<VEC, VE>(i, sub, lanes);
+                if (lane < lanes && c < E) {
+                    const int n = hist[c];
+                    hist[c] = 0;
+                    a.counts[g * E + c] = n;
+                    a.prob_sum[g * E + c] = t.acc[i];
+                    dot = fmaf(float(n), t.acc[i], dot);
+                }
+            }
+            dot = warp_sum(dot);
+            __syncwarp();
+            if (lane == 0) {
+                const float n = float(t.valid);
+                a.valid[g] = t.valid;
+                a.group_loss[g] = t.valid > 0 ? dot * float(E) / (float(a.d.k) * n * n) : 0.f;
+            }
+        }
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) last = atomicAdd(a.tickets + a.groups, 1u) == gridDim.x - 1;
+        __syncthreads();
+        if (last) {
+            __threadfence();
+            join_loss(a);
+            if (threadIdx.x == 0) a.tickets[a.groups] = 0u;
+        }
+        return;
+    }
     for (int64_t g = blockIdx.y; g < a.groups; g += gridDim.y) {
         const int64_t g0 = g * a.d.group_rows;
         const int64_t g1 = g0 + a.d.group_rows < a.d.rows ? g0 + a.d.group_rows : a.d.rows;
-        float acc[EPL];
+        Tally<EPL> t;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) acc[i] = 0.f;
-        int n_valid = 0;
-        const int64_t stride = int64_t(a.chunks) * ROUTER_WARPS * per_warp;
-        for (int64_t first = g0 + (int64_t(blockIdx.x) * ROUTER_WARPS + warp) * per_warp; first < g1; first += stride) {
-            const int64_t row = first + lane / lanes;
-            const bool here = row < g1, keep = here && (!a.mask || a.mask[row]);
-            float v[EPL];
-            load_logits<T, EPL, VEC>(static_cast<const T *>(a.logits) + (keep ? row : g0) * a.d.ld, sub, lanes, keep ? E : 0, v);
-            uint32_t key[EPL];
-            float top = -INFINITY, total = 0.f;
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) { key[i] = order_key(v[i]); top = fmaxf(top, v[i]); }
-            top = lanes_max(top, lanes);
-            const bool some = top > -INFINITY;
-            const float shift = some ? top : 0.f;
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) { v[i] = some ? __expf(v[i] - shift) : 0.f; total += v[i]; }
-            total = lanes_sum(total, lanes);
-            const float inv = some ? 1.f / total : 0.f;
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) acc[i] = fmaf(v[i], inv, acc[i]);
-            n_valid += some && sub == 0 ? 1 : 0;
-            // the k largest, one after the other: best of the lane, best of the row, out of the race
-            float chosen_sum = 0.f;
-            for (int j = 0; j < k; ++j) {
-                uint32_t best = 0u;
-                int col = 0x7fffffff;
-#pragma unroll
-                for (int i = 0; i < EPL; ++i)
-                    if (key[i] > best) { best = key[i]; col = column<VEC, VE>(i, sub, lanes); }
-#pragma unroll
-                for (int o = 16; o; o >>= 1) {
-                    const uint32_t kb = __shfl_xor_sync(0xffffffffu, best, o);
-                    const int cb = __shfl_xor_sync(0xffffffffu, col, o);
-                    if (o < lanes && (kb > best || (kb == best && cb < col))) { best = kb; col = cb; }
-                }
-                const bool ok = best > KEY_NINF;
-                const float w = ok ? __expf(__uint_as_float(best & 0x80000000u ? best & 0x7fffffffu : ~best) - shift) * inv : 0.f;
-                chosen_sum += w;
-#pragma unroll
-                for (int i = 0; i < EPL; ++i) if (column<VEC, VE>(i, sub, lanes) == col) key[i] = 0u;
-                if (j % lanes == sub) {
-                    // lanes < k: a lane hands out several places; weights that are normalised are rewritten below
-                    if (here) { a.index[row * k + j] = ok ? col : -1; a.weight[row * k + j] = w; }
-                    if (here && ok) atomicAdd(&hist[col], 1);
-                }
-            }
-            if ((a.d.flags & RUBICK_ROUTER_RENORM) && here && chosen_sum > 0.f)
-                for (int j = sub; j < k; j += lanes) a.weight[row * k + j] = a.weight[row * k + j] / chosen_sum;
-        }
+        for (int i = 0; i < EPL; ++i) t.acc[i] = 0.f;
+        t.valid = 0;
+        route_chunk<T, EPL, VEC, WARP>(a, g0 + (int64_t(blockIdx.x) * ROUTER_WARPS + warp) * per_warp, g1, int64_t(a.chunks) * ROUTER_WARPS * per_warp,
+                                       lanes, sub, slot, bits, list, kept, hist, t);
         // rows of a warp, then warps of the block
+        fold_rows(t, lanes);
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
-#pragma unroll
-            for (int o = 16; o; o >>= 1) { const float t = __shfl_xor_sync(0xffffffffu, acc[i], o); if (o >= lanes) acc[i] += t; }
             const int c = column<VEC, VE>(i, sub, lanes);
-            if (lane < lanes && c < E) psum[warp * E + c] = acc[i];
+            if (lane < lanes && c < E) psum[warp * E + c] = t.acc[i];
         }
-        n_valid = __reduce_add_sync(0xffffffffu, n_valid);
-        if (lane == 0 && n_valid) atomicAdd(&valid_rows, n_valid);
+        if (lane == 0 && t.valid) atomicAdd(&valid_rows, t.valid);
         __syncthreads();
-        const int64_t slot = g * a.chunks + blockIdx.x;
+        const int64_t place = g * a.chunks + blockIdx.x;
         const bool alone = a.chunks == 1;
         float dot = 0.f;
         for (int e = threadIdx.x; e < E; e += ROUTER_THREADS) {
@@ -226,13 +424,13 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __
                 a.prob_sum[g * E + e] = s;
                 dot = fmaf(float(n), s, dot);
             } else {
-                __stcg(a.part + slot * E + e, s);
-                __stcg(a.part_counts + slot * (E + 1) + e, n);
+                __stcg(a.part + place * E + e, s);
+                __stcg(a.part_counts + place * (E + 1) + e, n);
             }
         }
         const int rows_here = valid_rows;
-        if (threadIdx.x == 0 && !alone) __stcg(a.part_counts + slot * (E + 1) + E, rows_here);
-        __threadfence();
+        if (threadIdx.x == 0 && !alone) __stcg(a.part_counts + place * (E + 1) + E, rows_here);
+        if (!alone) __threadfence();
         __syncthreads();
         if (threadIdx.x == 0) {
             valid_rows = 0;
@@ -240,14 +438,13 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __
         }
         __syncthreads();
         if (last) {                                // every chunk of the group has arrived
-            __threadfence();
             if (alone) finish_group(a, g, dot, rows_here);
-            else join_group(a, g);
+            else { __threadfence(); join_group(a, g); }
             __threadfence();
             __syncthreads();
             if (threadIdx.x == 0) {
                 if (!alone) a.tickets[g] = 0u;
-                last = atomicAdd(a.tickets + a.groups, 1u) == uint32_t(a.groups - 1);
+                last = a.groups == 1 || atomicAdd(a.tickets + a.groups, 1u) == uint32_t(a.groups - 1);
             }
             __syncthreads();
             if (last) {
@@ -260,19 +457,20 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __
     }
 }
 
-template <typename T, int EPL, bool VEC>
-__global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const __grid_constant__ RouterArgs a, int lanes, int smem_cols)
+// A warp takes a run of consecutive rows, so that a group's factors a_e stay in registers from row to row.
+template <typename T, int EPL, bool VEC, bool WARP>
+__global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const __grid_constant__ RouterArgs a, int lanes, int run)
 {
     constexpr int VE = Lanes<T>::N;
-    extern __shared__ float add[];                // [warps][rows of a warp][smem_cols]: what the weights' gradients add
+    extern __shared__ float add[];                // [warps][rows of a warp][lanes * EPL]: what the weights' gradients add
     const int E = a.d.experts, k = a.d.k, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int sub = lane & (lanes - 1), per_warp = 32 / lanes;
-    float *mine = add + (warp * per_warp + lane / lanes) * smem_cols;
-    for (int c = sub; c < smem_cols; c += lanes) mine[c] = 0.f;
-    __syncthreads();
-    // groups that take part in the loss
+    if (WARP) lanes = 32;
+    const int sub = lane & (lanes - 1), per_warp = 32 / lanes, slot = lane / lanes;
+    float *mine = add + (warp * 32 + slot * lanes) * EPL;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) mine[i * lanes + sub] = 0.f;
     __shared__ float red[ROUTER_WARPS];
-    float n = 0.f;
+    float n = 0.f;                                // groups that take part in the loss
     for (int64_t g = threadIdx.x; g < a.groups; g += ROUTER_THREADS) n += a.valid_in[g] > 0 ? 1.f : 0.f;
     n = warp_sum(n);
     if (lane == 0) red[warp] = n;
@@ -281,67 +479,104 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const _
     for (int w = 0; w < ROUTER_WARPS; ++w) n += red[w];
     const float pull = (a.dloss ? *a.dloss : 1.f) * a.d.coef * float(E) / (float(k) * fmaxf(n, 1.f));
     const bool renorm = a.d.flags & RUBICK_ROUTER_RENORM;
-    const int64_t stride = int64_t(gridDim.x) * ROUTER_WARPS * per_warp;
-    for (int64_t first = (int64_t(blockIdx.x) * ROUTER_WARPS + warp) * per_warp; first < a.d.rows; first += stride) {
-        const int64_t row = first + lane / lanes;
-        const bool here = row < a.d.rows, live = here && a.index_in[row * k] >= 0;
-        float v[EPL];
-        load_logits<T, EPL, VEC>(static_cast<const T *>(a.logits) + (live ? row : 0) * a.d.ld, sub, lanes, live ? E : 0, v);
-        // the chosen: d_j w_j, and their sum over the row
-        float wd = 0.f;
-        if (live && a.dweight)
-            for (int j = sub; j < k; j += lanes) wd = fmaf(a.weight_in[row * k + j], a.index_in[row * k + j] >= 0 ? a.dweight[row * k + j] : 0.f, wd);
-        wd = lanes_sum(wd, lanes);
-        if (live && a.dweight)
-            for (int j = sub; j < k; j += lanes) {
-                const int e = a.index_in[row * k + j];
-                if (e >= 0 && e < E) atomicAdd(mine + e, a.weight_in[row * k + j] * (a.dweight[row * k + j] - (renorm ? wd : 0.f)));
+    const int64_t begin = (int64_t(blockIdx.x) * ROUTER_WARPS + warp) * run * per_warp;
+    const int64_t end = begin + int64_t(run) * per_warp < a.d.rows ? begin + int64_t(run) * per_warp : a.d.rows;
+    float next[EPL];
+    bool here = false, live = false;
+    int col = -1;                                 // this lane's place of the row (the first of them if it has more)
+    float w = 0.f, d = 0.f;
+    const auto fetch = [&](int64_t row) {
+        here = row < end;
+        live = here && a.index_in[row * k] >= 0;
+        load_logits<T, EPL, VEC>(static_cast<const T *>(a.logits) + (here ? row : 0) * a.d.ld, sub, lanes, here ? E : 0, next);
+        const bool has = here && sub < k && a.dweight;
+        col = has ? a.index_in[row * k + sub] : -1;
+        w = has ? a.weight_in[row * k + sub] : 0.f;
+        d = has ? a.dweight[row * k + sub] : 0.f;
+    };
+    int64_t group = -1, group_end = -1;
+    float f[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) f[i] = 0.f;
+    if (begin < end) fetch(begin + slot);
+    for (int64_t first = begin; first < end; first += per_warp) {
+        const int64_t row = first + slot;
+        const bool h = here, l = live;
+        const int c0 = col;
+        const float w0 = w, d0 = d;
+        float z[EPL];
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) z[i] = next[i];
+        if (first + per_warp < end) fetch(row + per_warp);
+        if (h && row >= group_end) {
+            group = row / a.d.group_rows;
+            group_end = (group + 1) * a.d.group_rows;
+            const float m = fmaxf(float(a.valid_in[group]), 1.f), scale = pull / (m * m);
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                const int c = column<VEC, VE>(i, sub, lanes);
+                f[i] = c < E ? scale * float(__ldg(a.counts_in + group * E + c)) : 0.f;
             }
-        float top = -INFINITY, total = 0.f;
+        }
+        // the chosen: w_j d_j, their sum over the row, and what goes to their columns
+        float wd = 0.f;
+        const bool weights = a.dweight != nullptr;
+        if (weights) {
+            wd = l && c0 >= 0 ? w0 * d0 : 0.f;
+            for (int j = sub + lanes; j < k; j += lanes)
+                if (l && a.index_in[row * k + j] >= 0) wd = fmaf(a.weight_in[row * k + j], a.dweight[row * k + j], wd);
+            wd = lanes_sum<WARP>(wd, lanes);
+            const float mean = renorm ? wd : 0.f;
+            if (l && c0 >= 0 && c0 < E) atomicAdd(mine + c0, w0 * (d0 - mean));
+            for (int j = sub + lanes; j < k; j += lanes) {
+                const int e = l ? a.index_in[row * k + j] : -1;
+                if (e >= 0 && e < E) atomicAdd(mine + e, a.weight_in[row * k + j] * (a.dweight[row * k + j] - mean));
+            }
+        }
+        float top = z[0], total = 0.f, dot = 0.f;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) top = fmaxf(top, v[i]);
-        top = lanes_max(top, lanes);
-        const float shift = top > -INFINITY ? top : 0.f;
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) { v[i] = __expf(v[i] - shift); total += v[i]; }
-        total = lanes_sum(total, lanes);
-        const float inv = live ? 1.f / total : 0.f;
-        const int64_t g = live ? row / a.d.group_rows : 0;
-        const float m = fmaxf(float(a.valid_in[g]), 1.f), scale = pull / (m * m);
-        float f[EPL], dot = 0.f;
+        for (int i = 1; i < EPL; ++i) top = fmaxf(top, z[i]);
+        top = lanes_max<WARP>(top, lanes);
+        const float off = top > -INFINITY ? -top * 1.4426950408889634f : 0.f;
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
-            const int c = column<VEC, VE>(i, sub, lanes);
-            f[i] = c < E ? scale * float(__ldg(a.counts_in + g * E + c)) : 0.f;
-            v[i] *= inv;
-            dot = fmaf(f[i], v[i], dot);
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(z[i]) : "f"(fmaf(z[i], 1.4426950408889634f, off)));
+            total += z[i];
+            dot = fmaf(f[i], z[i], dot);
         }
-        dot = lanes_sum(dot, lanes) + (renorm ? 0.f : wd);
-        __syncwarp();
-        T *out = static_cast<T *>(a.dlogits) + (here ? row : 0) * a.d.ld;
-        const int end = here ? E : 0;
+        total = lanes_sum<WARP>(total, lanes);
+        dot = lanes_sum<WARP>(dot, lanes);
+        const float inv = __fdividef(1.f, total);
+        dot = fmaf(dot, inv, renorm ? 0.f : wd);
+        if (weights) __syncwarp();
+        T *out = static_cast<T *>(a.dlogits) + (h ? row : 0) * a.d.ld;
+        const int stop = h ? E : 0;
 #pragma unroll
         for (int i = 0; i < EPL; i += VEC ? VE : 1) {
             const int c = column<VEC, VE>(i, sub, lanes);
             if constexpr (VEC) {
-                float r[VE];
+                float r[VE], more[VE];
 #pragma unroll
-                for (int e = 0; e < VE; ++e) {
-                    const float more = c + e < E ? mine[c + e] : 0.f;
-                    r[e] = live ? fmaf(v[i + e], f[i + e] - dot, more) : 0.f;
+                for (int e = 0; e < VE; e += 4) {
+                    const float4 q = weights ? *reinterpret_cast<const float4 *>(mine + c + e) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    more[e] = q.x; more[e + 1] = q.y; more[e + 2] = q.z; more[e + 3] = q.w;
                 }
-                store_cols<T, VE>(out, c, end, r);
-            } else if (c < end) {
-                out[c] = from_f<T>(live ? fmaf(v[i], f[i] - dot, mine[c]) : 0.f);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) r[e] = l ? fmaf(z[i + e] * inv, f[i + e] - dot, more[e]) : 0.f;
+                store_cols<T, VE>(out, c, stop, r);
+            } else if (c < stop) {
+                out[c] = from_f<T>(l ? fmaf(z[i] * inv, f[i] - dot, weights ? mine[c] : 0.f) : 0.f);
             }
         }
-        __syncwarp();
-        if (live && a.dweight)
-            for (int j = sub; j < k; j += lanes) {
-                const int e = a.index_in[row * k + j];
+        if (weights) {
+            __syncwarp();
+            if (l && c0 >= 0 && c0 < E) mine[c0] = 0.f;
+            for (int j = sub + lanes; j < k; j += lanes) {
+                const int e = l ? a.index_in[row * k + j] : -1;
                 if (e >= 0 && e < E) mine[e] = 0.f;
             }
-        __syncwarp();
+            __syncwarp();
+        }
     }
 }
 
@@ -358,20 +593,41 @@ RouterShape router_shape(const RouterArgs &a)
     return s;
 }
 
-template <typename T, bool BACK, int EPL, bool VEC> cudaError_t launch_router(const RouterArgs &a, const RouterShape &s, int num_sms, cudaStream_t st)
+// groups so many that a warp each fills the SMs
+bool by_warp(const RouterArgs &a, int num_sms) { return a.groups >= int64_t(num_sms) * ROUTER_WARPS * 2; }
+
+template <typename T, bool BACK, int EPL, bool VEC, bool WARP> cudaError_t launch_shape(const RouterArgs &a, const RouterShape &s, int num_sms, cudaStream_t st)
 {
+    const int per_warp = 32 / s.lanes;
     if constexpr (BACK) {
-        const int per_warp = 32 / s.lanes, cols = s.lanes * s.epl + 1;        // one word more: rows start in different banks
-        const int smem = ROUTER_WARPS * per_warp * cols * int(sizeof(float));
-        const int64_t blocks = (a.d.rows + ROUTER_WARPS * per_warp - 1) / (ROUTER_WARPS * per_warp);
-        const int64_t most = int64_t(num_sms) * 8;
-        router_backward_kernel<T, EPL, VEC><<<unsigned(blocks < most ? blocks : most), ROUTER_THREADS, smem, st>>>(a, s.lanes, cols);
+        const int smem = ROUTER_THREADS * EPL * int(sizeof(float));
+        // a run of rows a warp: long enough to keep a group's factors, short enough for four blocks an SM
+        const int64_t slots = int64_t(num_sms) * 4 * ROUTER_WARPS * per_warp;
+        const int run = int((a.d.rows + slots - 1) / slots);
+        const int64_t per_block = int64_t(run) * ROUTER_WARPS * per_warp;
+        if (smem > 48 * 1024) {
+            const cudaError_t e = cudaFuncSetAttribute(router_backward_kernel<T, EPL, VEC, WARP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+            if (e != cudaSuccess) return e;
+        }
+        router_backward_kernel<T, EPL, VEC, WARP><<<unsigned((a.d.rows + per_block - 1) / per_block), ROUTER_THREADS, smem, st>>>(a, s.lanes, run);
     } else {
-        const int smem = a.d.experts * int(sizeof(float)) * (ROUTER_WARPS + 1);
-        router_forward_kernel<T, EPL, VEC><<<dim3(a.chunks, unsigned(a.groups < 32768 ? a.groups : 32768)), ROUTER_THREADS, smem, st>>>(a, s.lanes);
+        const bool one = by_warp(a, num_sms);
+        const int words = a.d.experts * (one ? ROUTER_WARPS : ROUTER_WARPS + 1) + ROUTER_WARPS * (kept_words<T, EPL>() + (WARP ? 0 : per_warp * a.d.k));
+        int bits = 0;
+        while ((1 << bits) < s.lanes * s.epl) ++bits;
+        if (words > 12 * 1024) {
+            const cudaError_t e = cudaFuncSetAttribute(router_forward_kernel<T, EPL, VEC, WARP>, cudaFuncAttributeMaxDynamicSharedMemorySize, words * 4);
+            if (e != cudaSuccess) return e;
+        }
+        const dim3 grid = one ? dim3(unsigned(num_sms) * 4) : dim3(a.chunks, unsigned(a.groups < 32768 ? a.groups : 32768));
+        router_forward_kernel<T, EPL, VEC, WARP><<<grid, ROUTER_THREADS, words * 4, st>>>(a, s.lanes, bits, one);
     }
     count_launch();
     return cudaGetLastError();
+}
+template <typename T, bool BACK, int EPL, bool VEC> cudaError_t launch_router(const RouterArgs &a, const RouterShape &s, int num_sms, cudaStream_t st)
+{
+    return s.lanes == 32 && a.d.k <= 32 ? launch_shape<T, BACK, EPL, VEC, true>(a, s, num_sms, st) : launch_shape<T, BACK, EPL, VEC, false>(a, s, num_sms, st);
 }
 
 template <typename T, bool BACK> cudaError_t router_epl(const RouterArgs &a, int num_sms, cudaStream_t st)
