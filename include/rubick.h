@@ -529,7 +529,7 @@ int rubick_router_forward(rubick_ctx *ctx, const rubick_router_desc *h_desc, con
 
 /* Gradient of  d_dloss[0] * loss + sum(d_dweight * weight)  with respect to the logits (the choice and the counts are
  * held fixed).  d_index, d_weight, d_counts and d_valid are what forward wrote; d_dloss NULL = 1, d_dweight NULL = 0.  Rows
- * whose first index is negative get zeros.  d_dlogits may equal d_logits.  Errors: EINVAL, ECUDA. */
+ * whose first index is negative get zeros.  d_dlogits may equal d_logits.  Errors: EINVAL, ENOMEM, ECUDA. */
 int rubick_router_backward(rubick_ctx *ctx, const rubick_router_desc *h_desc, const void *d_logits, const int32_t *d_index,
                            const float *d_weight, const int32_t *d_counts, const int32_t *d_valid, const float *d_dloss,
                            const float *d_dweight, void *d_dlogits);

@@ -13,10 +13,11 @@
 // number from the top, so that no two keys are equal and the lowest index wins among equal logits.  Sixteen-bit
 // logits fit the upper bits whole.  Of single-precision ones some bits are cut off: where two neighbours among the
 // first k + 1 keys differ in nothing but these, the row is chosen again with whole keys.  Every lane sorts its own keys
-// once; after that one of the k is a maximum over the lanes' first keys (one instruction for a whole warp) and a
-// shift of one lane's list.
+// once and puts the list into shared memory; after that one of the k is a maximum over the lanes' first keys and one
+// lane's step down its list, a dozen instructions for all rows of the warp together.  Sixteen elements a lane: fewer
+// leave the steps that a warp's rows share to fewer rows, more make the sort dear.
 //
-// Bound by instruction issue, not by memory: a row of 128 experts is 512 bytes, and its choice some 200 instructions.
+// Bound by instruction issue, not by memory: a row of 128 experts is 512 bytes, and its choice some 150 instructions.
 //
 // Probability sums stay in the lane that owns the column until its chunk of rows ends, then go chunk by chunk, in order,
 // into the group's sum: the last block of a group to arrive adds them up, the last of all the loss.  Where groups are
@@ -32,6 +33,7 @@ namespace {
 
 constexpr int ROUTER_THREADS = 256;
 constexpr int ROUTER_WARPS = ROUTER_THREADS / 32;
+constexpr int FORWARD_BLOCKS = 2, BACKWARD_BLOCKS = 3;      // blocks an SM holds, by their registers
 
 // unsigned keys in the order of the values: -inf gets 0x007fffff, NaN of either sign 0 (never chosen)
 __device__ __forceinline__ uint32_t order_key(float v)
@@ -43,59 +45,72 @@ __device__ __forceinline__ uint32_t order_key(float v)
 constexpr uint32_t KEY_NINF = 0x007fffffu;
 
 // column of element i of lane `sub` of a row
-template <bool VEC, int VE> __device__ __forceinline__ int column(int i, int sub, int lanes)
+template <bool VEC, int VE, int LANES> __device__ __forceinline__ int column(int i, int sub)
 {
-    return VEC ? ((i / VE) * lanes + sub) * VE + i % VE : i * lanes + sub;
+    return VEC ? ((i / VE) * LANES + sub) * VE + i % VE : i * LANES + sub;
 }
 
-template <typename T, int EPL, bool VEC>
-__device__ __forceinline__ void load_logits(const T *row, int sub, int lanes, int experts, float (&v)[EPL])
-{
-    constexpr int VE = Lanes<T>::N;
-    if constexpr (VEC) {
+// A row's elements of one lane as they come from memory: nothing looks at them before the row's turn, so that the load
+// is under way during the row before.
+template <typename T, int EPL, bool VEC, int LANES> struct RawRow {
+    static constexpr int VE = Lanes<T>::N;
+    uint4 v[VEC ? EPL / VE : 1];
+    T s[VEC ? 1 : EPL];
+    __device__ __forceinline__ void load(const T *row, int sub, int experts)
+    {
+        if constexpr (VEC) {
 #pragma unroll
-        for (int i = 0; i < EPL; i += VE) {
-            const int c = column<VEC, VE>(i, sub, lanes);
-            float part[VE];
-            if (c + VE <= experts) unpack16<T>(ld_stream(row + c), part);
-            else {
+            for (int i = 0; i < EPL / VE; ++i) {
+                const int c = (i * LANES + sub) * VE;
+                if (c + VE <= experts) v[i] = ld_stream(row + c);
+                else {
+                    float f[VE];
 #pragma unroll
-                for (int e = 0; e < VE; ++e) part[e] = c + e < experts ? to_f(row[c + e]) : -INFINITY;
+                    for (int e = 0; e < VE; ++e) f[e] = c + e < experts ? to_f(row[c + e]) : -INFINITY;
+                    v[i] = pack16<T>(f);
+                }
             }
+        } else {
 #pragma unroll
-            for (int e = 0; e < VE; ++e) v[i + e] = part[e];
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-            const int c = column<VEC, VE>(i, sub, lanes);
-            v[i] = c < experts ? to_f(row[c]) : -INFINITY;
+            for (int i = 0; i < EPL; ++i) s[i] = i * LANES + sub < experts ? row[i * LANES + sub] : from_f<T>(-INFINITY);
         }
     }
-}
+    __device__ __forceinline__ void get(float (&f)[EPL]) const
+    {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < EPL / VE; ++i) {
+                float part[VE];
+                unpack16<T>(v[i], part);
+#pragma unroll
+                for (int e = 0; e < VE; ++e) f[i * VE + e] = part[e];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) f[i] = to_f(s[i]);
+        }
+    }
+};
 
-template <bool WARP> __device__ __forceinline__ float lanes_sum(float v, int lanes)
+template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
 {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const float t = __shfl_xor_sync(0xffffffffu, v, o);
-        if (WARP || o < lanes) v += t;
-    }
+    for (int o = LANES / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-template <bool WARP> __device__ __forceinline__ float lanes_max(float v, int lanes)
+template <int LANES> __device__ __forceinline__ float lanes_max(float v)
 {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) { const float t = __shfl_xor_sync(0xffffffffu, v, o); if (WARP || o < lanes) v = fmaxf(v, t); }
+    for (int o = LANES / 2; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
     return v;
 }
-template <bool WARP> __device__ __forceinline__ uint32_t lanes_max(uint32_t v, int lanes)
+template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
 {
-    if constexpr (WARP) {
+    if constexpr (LANES == 32) {
         return __reduce_max_sync(0xffffffffu, v);
     } else {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) { const uint32_t t = __shfl_xor_sync(0xffffffffu, v, o); if (o < lanes) v = max(v, t); }
+        for (int o = LANES / 2; o; o >>= 1) v = max(v, __shfl_xor_sync(0xffffffffu, v, o));
         return v;
     }
 }
@@ -121,38 +136,43 @@ template <int N> __device__ __forceinline__ void sort_keys(uint32_t (&s)[N])
 template <int EPL> struct Tally { float acc[EPL]; int valid; };
 
 // One row per group of lanes: index, weight and histogram are written, probabilities added to the tally.
-template <typename T, int EPL, bool VEC, bool WARP>
-__device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, bool here, const float (&z)[EPL], int lanes, int sub, int bits,
-                                           uint32_t *list, float *kept, int32_t *hist, Tally<EPL> &tally)
+template <typename T, int EPL, bool VEC, int LANES>
+__device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, bool here, const float (&z)[EPL], int sub,
+                                           uint32_t *sorted, uint32_t *list, float *kept, int32_t *hist, Tally<EPL> &tally)
 {
-    constexpr int VE = Lanes<T>::N;
+    constexpr int VE = Lanes<T>::N, lanes = LANES;
+    constexpr bool WARP = LANES == 32;
+    constexpr uint32_t low = LANES * EPL - 1;     // a power of two less one
     const int k = a.d.k;
-    const uint32_t low = (1u << bits) - 1u;
     // keys: NaN counts as -inf, -0 as 0; a row that is masked reads as -inf
     uint32_t key[EPL];
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
         const uint32_t b = __float_as_uint(fmaxf(z[i], -INFINITY) + 0.f);
         const uint32_t ordered = b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
-        key[i] = (ordered & ~low) | (low - uint32_t(column<VEC, VE>(i, sub, lanes)));
+        key[i] = (ordered & ~low) | (low - uint32_t(column<VEC, VE, LANES>(i, sub)));
     }
     if constexpr (sizeof(T) == 4) {
         // the chosen logits are looked up whole
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) kept[column<VEC, VE>(i, sub, lanes)] = z[i];
+        for (int i = 0; i < EPL; i += VEC ? 4 : 1) {
+            if constexpr (VEC) *reinterpret_cast<float4 *>(kept + column<VEC, VE, LANES>(i, sub)) = make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]);
+            else kept[column<VEC, VE, LANES>(i, sub)] = z[i];
+        }
     }
     sort_keys<EPL>(key);
-    uint32_t first = 0u, mine = 0u;
+    // this lane's list, 32 words from one to the next; behind its last key a 0 (written once, at the start)
+#pragma unroll
+    for (int i = 1; i < EPL; ++i) sorted[i * 32] = key[i];
+    uint32_t first = 0u, mine = 0u, head = key[0];
+    const uint32_t *next_key = sorted + 32;
 #pragma unroll 1
     for (int j = 0; j < k; ++j) {
-        const uint32_t m = lanes_max<WARP>(key[0], lanes);
+        const uint32_t m = lanes_max<LANES>(head);
         if (j == 0) first = m;
         if (WARP) mine = sub == j ? m : mine;
         else if (sub == (j & (lanes - 1))) list[j] = m;
-        const bool won = key[0] == m;
-#pragma unroll
-        for (int i = 0; i + 1 < EPL; ++i) key[i] = won ? key[i + 1] : key[i];
-        key[EPL - 1] = won ? 0u : key[EPL - 1];
+        if (head == m && m) { head = *next_key; next_key += 32; }
     }
     const uint32_t none = KEY_NINF | low;         // up to here: closed, or not a column
     const bool some = first > none;
@@ -166,7 +186,7 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[i]) : "f"(fmaf(z[i], 1.4426950408889634f, off)));
         total += e[i];
     }
-    total = lanes_sum<WARP>(total, lanes);
+    total = lanes_sum<LANES>(total);
     const float inv = some ? __fdividef(1.f, total) : 0.f;
     if (some) {
 #pragma unroll
@@ -176,7 +196,7 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
     if (!WARP || sizeof(T) == 4) __syncwarp();
     if constexpr (sizeof(T) == 4) {
         // neighbours that only the cut-off bits tell apart: once more, with whole keys
-        const uint32_t next = lanes_max<WARP>(key[0], lanes);
+        const uint32_t next = lanes_max<LANES>(head);
         bool unsure = false;
         for (int j = sub; j < k; j += lanes) {
             const uint32_t x = WARP ? mine : list[j], y = j + 1 == k ? next : WARP ? 0u : list[j + 1];
@@ -197,7 +217,7 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
                 int col = 0x7fffffff;
 #pragma unroll
                 for (int i = 0; i < EPL; ++i)
-                    if (whole[i] > best) { best = whole[i]; col = column<VEC, VE>(i, sub, lanes); }
+                    if (whole[i] > best) { best = whole[i]; col = column<VEC, VE, LANES>(i, sub); }
 #pragma unroll
                 for (int o = 16; o; o >>= 1) {
                     const uint32_t kb = __shfl_xor_sync(0xffffffffu, best, o);
@@ -208,7 +228,7 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
                 if (WARP) mine = sub == j ? m : mine;
                 else if (sub == (j & (lanes - 1))) list[j] = m;
 #pragma unroll
-                for (int i = 0; i < EPL; ++i) if (column<VEC, VE>(i, sub, lanes) == col) whole[i] = 0u;
+                for (int i = 0; i < EPL; ++i) if (column<VEC, VE, LANES>(i, sub) == col) whole[i] = 0u;
             }
             __syncwarp();
         }
@@ -234,7 +254,7 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
         }
     }
     if (a.d.flags & RUBICK_ROUTER_RENORM) {
-        sum = lanes_sum<WARP>(sum, lanes);
+        sum = lanes_sum<LANES>(sum);
         const float share = sum > 0.f || sum != sum ? __fdividef(1.f, sum) : 0.f;
         for (int j = sub; here && j < k; j += lanes) a.weight[row * k + j] = __uint_as_float(WARP ? mine : list[j]) * share;
     }
@@ -252,8 +272,10 @@ __device__ void finish_group(const RouterArgs &a, int64_t g, float dot, int vali
         dot = 0.f;
         for (int w = 0; w < ROUTER_WARPS; ++w) dot += red[w];
         const float n = float(valid);
+        const float loss = valid > 0 ? dot * float(a.d.experts) / (float(a.d.k) * n * n) : 0.f;
         a.valid[g] = valid;
-        a.group_loss[g] = valid > 0 ? dot * float(a.d.experts) / (float(a.d.k) * n * n) : 0.f;
+        a.group_loss[g] = loss;
+        if (a.groups == 1) *a.loss = a.d.coef * loss;
     }
 }
 
@@ -296,60 +318,68 @@ __device__ void join_loss(const RouterArgs &a)
     }
 }
 
-// Goes through rows first, first + stride, ... below end, per_warp at a time, with the next ones on their way.
-template <typename T, int EPL, bool VEC, bool WARP>
-__device__ __forceinline__ void route_chunk(const RouterArgs &a, int64_t first, int64_t end, int64_t stride, int lanes, int sub, int slot, int bits,
-                                            uint32_t *list, float *kept, int32_t *hist, Tally<EPL> &tally)
+// Goes through rows first, first + stride, ... below end, 32 / LANES at a time, with the next ones on their way.
+template <typename T, int EPL, bool VEC, int LANES>
+__device__ __forceinline__ void route_chunk(const RouterArgs &a, int64_t first, int64_t end, int64_t stride, int sub, int slot,
+                                            uint32_t *sorted, uint32_t *list, float *kept, int32_t *hist, Tally<EPL> &tally)
 {
-    const int E = a.d.experts;
-    float z[EPL], next[EPL];
-    bool here = false;
-    const auto fetch = [&](int64_t row, float (&v)[EPL]) {
-        here = row < end;
-        const bool keep = here && (!a.mask || a.mask[row]);
-        load_logits<T, EPL, VEC>(static_cast<const T *>(a.logits) + (keep ? row : 0) * a.d.ld, sub, lanes, keep ? E : 0, v);
+    RawRow<T, EPL, VEC, LANES> next;
+    uint8_t mask = 1;
+    const auto fetch = [&](int64_t row) {
+        const bool here = row < end;
+        if (a.mask) mask = here ? a.mask[row] : uint8_t(0);
+        next.load(static_cast<const T *>(a.logits) + (here ? row : 0) * a.d.ld, sub, here ? a.d.experts : 0);
     };
-    if (first < end) fetch(first + slot, next);
+    if (first < end) fetch(first + slot);
     for (int64_t row = first; row < end; row += stride) {
-        const bool h = here;
+        float z[EPL];
+        next.get(z);
+        if (!mask) {                              // what stands in a masked row is not looked at
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) z[i] = next[i];
-        if (row + stride < end) fetch(row + stride + slot, next);
-        route_rows<T, EPL, VEC, WARP>(a, row + slot, h, z, lanes, sub, bits, list, kept, hist, tally);
+            for (int i = 0; i < EPL; ++i) z[i] = -INFINITY;
+        }
+        if (row + stride < end) fetch(row + stride + slot);
+        route_rows<T, EPL, VEC, LANES>(a, row + slot, row + slot < end, z, sub, sorted, list, kept, hist, tally);
     }
 }
 
 // the sums of a warp's rows, at the lanes of its first row
-template <int EPL> __device__ __forceinline__ void fold_rows(Tally<EPL> &t, int lanes)
+template <int EPL, int LANES> __device__ __forceinline__ void fold_rows(Tally<EPL> &t)
 {
 #pragma unroll
     for (int i = 0; i < EPL; ++i)
 #pragma unroll
-        for (int o = 16; o; o >>= 1) { const float x = __shfl_xor_sync(0xffffffffu, t.acc[i], o); if (o >= lanes) t.acc[i] += x; }
+        for (int o = 16; o >= LANES; o >>= 1) t.acc[i] += __shfl_xor_sync(0xffffffffu, t.acc[i], o);
     t.valid = __reduce_add_sync(0xffffffffu, t.valid);
 }
 
-// shared memory of the forward kernel, in words: [1 or warps][E] assignments, [warps][E] probability sums, per warp
-// 32 EPL logits (single precision) and a list of k keys per row
+// Shared memory of the forward kernel, in words: per warp its 32 EPL logits (single precision), the lanes' sorted lists
+// and a list of k keys per row; then [1 or warps][E] assignments and [warps][E] probability sums.
 template <typename T, int EPL> __host__ __device__ __forceinline__ int kept_words() { return sizeof(T) == 4 ? 32 * EPL : 0; }
+template <typename T, int EPL, int LANES> __host__ __device__ __forceinline__ int warp_words(int k)
+{
+    return kept_words<T, EPL>() + 32 * (EPL + 1) + (LANES == 32 ? 0 : (32 / LANES * k + 3) / 4 * 4);
+}
 
 // blockIdx.x = chunk of rows within the group, blockIdx.y = group; by_warp: a warp takes whole groups
-template <typename T, int EPL, bool VEC, bool WARP>
-__global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __grid_constant__ RouterArgs a, int lanes, int bits, bool by_warp)
+template <typename T, int EPL, bool VEC, int LANES>
+__global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : FORWARD_BLOCKS) router_forward_kernel(const __grid_constant__ RouterArgs a, bool by_warp)
 {
-    constexpr int VE = Lanes<T>::N;
-    extern __shared__ int32_t smem[];
+    constexpr int VE = Lanes<T>::N, lanes = LANES, per_warp = 32 / LANES;
+    extern __shared__ __align__(16) int32_t smem[];
     __shared__ int32_t valid_rows;
     __shared__ bool last;
     const int E = a.d.experts, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (WARP) lanes = 32;
-    const int sub = lane & (lanes - 1), per_warp = 32 / lanes, slot = lane / lanes;
-    int32_t *hist = smem + (by_warp ? warp * E : 0);
-    float *psum = reinterpret_cast<float *>(smem + E);
-    int32_t *own = smem + (by_warp ? ROUTER_WARPS : ROUTER_WARPS + 1) * E + warp * (kept_words<T, EPL>() + (WARP ? 0 : per_warp * a.d.k));
+    const int sub = lane & (lanes - 1), slot = lane / lanes;
+    const int own_words = warp_words<T, EPL, LANES>(a.d.k);
+    int32_t *own = smem + warp * own_words, *tables = smem + ROUTER_WARPS * own_words;
     float *kept = reinterpret_cast<float *>(own) + slot * lanes * EPL;
-    uint32_t *list = reinterpret_cast<uint32_t *>(own + kept_words<T, EPL>()) + slot * a.d.k;
-    for (int e = threadIdx.x; e < E * (by_warp ? ROUTER_WARPS : 1); e += ROUTER_THREADS) smem[e] = 0;
+    uint32_t *sorted = reinterpret_cast<uint32_t *>(own + kept_words<T, EPL>()) + lane;
+    uint32_t *list = reinterpret_cast<uint32_t *>(own + kept_words<T, EPL>() + 32 * (EPL + 1)) + slot * a.d.k;
+    int32_t *hist = tables + (by_warp ? warp * E : 0);
+    float *psum = reinterpret_cast<float *>(tables + E);
+    sorted[EPL * 32] = 0u;
+    for (int e = threadIdx.x; e < E * (by_warp ? ROUTER_WARPS : 1); e += ROUTER_THREADS) tables[e] = 0;
     if (threadIdx.x == 0) valid_rows = 0;
     __syncthreads();
     if (by_warp) {
@@ -359,13 +389,13 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __
 #pragma unroll
             for (int i = 0; i < EPL; ++i) t.acc[i] = 0.f;
             t.valid = 0;
-            route_chunk<T, EPL, VEC, WARP>(a, g0, g1, per_warp, lanes, sub, slot, bits, list, kept, hist, t);
-            fold_rows(t, lanes);
+            route_chunk<T, EPL, VEC, LANES>(a, g0, g1, per_warp, sub, slot, sorted, list, kept, hist, t);
+            fold_rows<EPL, LANES>(t);
             __syncwarp();
             float dot = 0.f;
 #pragma unroll
             for (int i = 0; i < EPL; ++i) {
-                const int c = column<VEC, VE>(i, sub, lanes);
+                const int c = column<VEC, VE, LANES>(i, sub);
                 if (lane < lanes && c < E) {
                     const int n = hist[c];
                     hist[c] = 0;
@@ -400,13 +430,13 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __
 #pragma unroll
         for (int i = 0; i < EPL; ++i) t.acc[i] = 0.f;
         t.valid = 0;
-        route_chunk<T, EPL, VEC, WARP>(a, g0 + (int64_t(blockIdx.x) * ROUTER_WARPS + warp) * per_warp, g1, int64_t(a.chunks) * ROUTER_WARPS * per_warp,
-                                       lanes, sub, slot, bits, list, kept, hist, t);
+        route_chunk<T, EPL, VEC, LANES>(a, g0 + (int64_t(blockIdx.x) * ROUTER_WARPS + warp) * per_warp, g1, int64_t(a.chunks) * ROUTER_WARPS * per_warp,
+                                          sub, slot, sorted, list, kept, hist, t);
         // rows of a warp, then warps of the block
-        fold_rows(t, lanes);
+        fold_rows<EPL, LANES>(t);
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
-            const int c = column<VEC, VE>(i, sub, lanes);
+            const int c = column<VEC, VE, LANES>(i, sub);
             if (lane < lanes && c < E) psum[warp * E + c] = t.acc[i];
         }
         if (lane == 0 && t.valid) atomicAdd(&valid_rows, t.valid);
@@ -440,12 +470,11 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __
         if (last) {                                // every chunk of the group has arrived
             if (alone) finish_group(a, g, dot, rows_here);
             else { __threadfence(); join_group(a, g); }
+            if (!alone && threadIdx.x == 0) a.tickets[g] = 0u;
+            if (a.groups == 1) return;             // finish_group has written the loss
             __threadfence();
             __syncthreads();
-            if (threadIdx.x == 0) {
-                if (!alone) a.tickets[g] = 0u;
-                last = a.groups == 1 || atomicAdd(a.tickets + a.groups, 1u) == uint32_t(a.groups - 1);
-            }
+            if (threadIdx.x == 0) last = atomicAdd(a.tickets + a.groups, 1u) == uint32_t(a.groups - 1);
             __syncthreads();
             if (last) {
                 __threadfence();
@@ -458,41 +487,45 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_forward_kernel(const __
 }
 
 // A warp takes a run of consecutive rows, so that a group's factors a_e stay in registers from row to row.
-template <typename T, int EPL, bool VEC, bool WARP>
-__global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const __grid_constant__ RouterArgs a, int lanes, int run)
+template <typename T, int EPL, bool VEC, int LANES>
+__global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : BACKWARD_BLOCKS) router_backward_kernel(const __grid_constant__ RouterArgs a, int run)
 {
-    constexpr int VE = Lanes<T>::N;
+    constexpr int VE = Lanes<T>::N, lanes = LANES, per_warp = 32 / LANES;
     extern __shared__ float add[];                // [warps][rows of a warp][lanes * EPL]: what the weights' gradients add
     const int E = a.d.experts, k = a.d.k, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (WARP) lanes = 32;
-    const int sub = lane & (lanes - 1), per_warp = 32 / lanes, slot = lane / lanes;
+    const int sub = lane & (lanes - 1), slot = lane / lanes;
     float *mine = add + (warp * 32 + slot * lanes) * EPL;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) mine[i * lanes + sub] = 0.f;
     __shared__ float red[ROUTER_WARPS];
     float n = 0.f;                                // groups that take part in the loss
-    for (int64_t g = threadIdx.x; g < a.groups; g += ROUTER_THREADS) n += a.valid_in[g] > 0 ? 1.f : 0.f;
-    n = warp_sum(n);
-    if (lane == 0) red[warp] = n;
-    __syncthreads();
-    n = 0.f;
-    for (int w = 0; w < ROUTER_WARPS; ++w) n += red[w];
+    if (a.some) n = *a.some;
+    else {
+        for (int64_t g = threadIdx.x; g < a.groups; g += ROUTER_THREADS) n += a.valid_in[g] > 0 ? 1.f : 0.f;
+        n = warp_sum(n);
+        if (lane == 0) red[warp] = n;
+        __syncthreads();
+        n = 0.f;
+        for (int w = 0; w < ROUTER_WARPS; ++w) n += red[w];
+    }
     const float pull = (a.dloss ? *a.dloss : 1.f) * a.d.coef * float(E) / (float(k) * fmaxf(n, 1.f));
     const bool renorm = a.d.flags & RUBICK_ROUTER_RENORM;
     const int64_t begin = (int64_t(blockIdx.x) * ROUTER_WARPS + warp) * run * per_warp;
     const int64_t end = begin + int64_t(run) * per_warp < a.d.rows ? begin + int64_t(run) * per_warp : a.d.rows;
-    float next[EPL];
-    bool here = false, live = false;
-    int col = -1;                                 // this lane's place of the row (the first of them if it has more)
+    RawRow<T, EPL, VEC, LANES> next;
+    int lead = -1, col = -1;                      // the row's first index; this lane's (the first of them if it has more)
     float w = 0.f, d = 0.f;
+    const bool weights = a.dweight != nullptr;
     const auto fetch = [&](int64_t row) {
-        here = row < end;
-        live = here && a.index_in[row * k] >= 0;
-        load_logits<T, EPL, VEC>(static_cast<const T *>(a.logits) + (here ? row : 0) * a.d.ld, sub, lanes, here ? E : 0, next);
-        const bool has = here && sub < k && a.dweight;
-        col = has ? a.index_in[row * k + sub] : -1;
-        w = has ? a.weight_in[row * k + sub] : 0.f;
-        d = has ? a.dweight[row * k + sub] : 0.f;
+        const bool here = row < end;
+        next.load(static_cast<const T *>(a.logits) + (here ? row : 0) * a.d.ld, sub, here ? E : 0);
+        lead = col = -1;
+        if (here) lead = a.index_in[row * k];
+        if (here && sub < k && weights) {
+            col = a.index_in[row * k + sub];
+            w = a.weight_in[row * k + sub];
+            d = a.dweight[row * k + sub];
+        }
     };
     int64_t group = -1, group_end = -1;
     float f[EPL];
@@ -501,12 +534,11 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const _
     if (begin < end) fetch(begin + slot);
     for (int64_t first = begin; first < end; first += per_warp) {
         const int64_t row = first + slot;
-        const bool h = here, l = live;
+        const bool h = row < end, l = lead >= 0;
         const int c0 = col;
         const float w0 = w, d0 = d;
         float z[EPL];
-#pragma unroll
-        for (int i = 0; i < EPL; ++i) z[i] = next[i];
+        next.get(z);
         if (first + per_warp < end) fetch(row + per_warp);
         if (h && row >= group_end) {
             group = row / a.d.group_rows;
@@ -514,18 +546,17 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const _
             const float m = fmaxf(float(a.valid_in[group]), 1.f), scale = pull / (m * m);
 #pragma unroll
             for (int i = 0; i < EPL; ++i) {
-                const int c = column<VEC, VE>(i, sub, lanes);
+                const int c = column<VEC, VE, LANES>(i, sub);
                 f[i] = c < E ? scale * float(__ldg(a.counts_in + group * E + c)) : 0.f;
             }
         }
         // the chosen: w_j d_j, their sum over the row, and what goes to their columns
         float wd = 0.f;
-        const bool weights = a.dweight != nullptr;
         if (weights) {
             wd = l && c0 >= 0 ? w0 * d0 : 0.f;
             for (int j = sub + lanes; j < k; j += lanes)
                 if (l && a.index_in[row * k + j] >= 0) wd = fmaf(a.weight_in[row * k + j], a.dweight[row * k + j], wd);
-            wd = lanes_sum<WARP>(wd, lanes);
+            wd = lanes_sum<LANES>(wd);
             const float mean = renorm ? wd : 0.f;
             if (l && c0 >= 0 && c0 < E) atomicAdd(mine + c0, w0 * (d0 - mean));
             for (int j = sub + lanes; j < k; j += lanes) {
@@ -536,7 +567,7 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const _
         float top = z[0], total = 0.f, dot = 0.f;
 #pragma unroll
         for (int i = 1; i < EPL; ++i) top = fmaxf(top, z[i]);
-        top = lanes_max<WARP>(top, lanes);
+        top = lanes_max<LANES>(top);
         const float off = top > -INFINITY ? -top * 1.4426950408889634f : 0.f;
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
@@ -544,8 +575,8 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const _
             total += z[i];
             dot = fmaf(f[i], z[i], dot);
         }
-        total = lanes_sum<WARP>(total, lanes);
-        dot = lanes_sum<WARP>(dot, lanes);
+        total = lanes_sum<LANES>(total);
+        dot = lanes_sum<LANES>(dot);
         const float inv = __fdividef(1.f, total);
         dot = fmaf(dot, inv, renorm ? 0.f : wd);
         if (weights) __syncwarp();
@@ -553,7 +584,7 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const _
         const int stop = h ? E : 0;
 #pragma unroll
         for (int i = 0; i < EPL; i += VEC ? VE : 1) {
-            const int c = column<VEC, VE>(i, sub, lanes);
+            const int c = column<VEC, VE, LANES>(i, sub);
             if constexpr (VEC) {
                 float r[VE], more[VE];
 #pragma unroll
@@ -580,14 +611,27 @@ __global__ void __launch_bounds__(ROUTER_THREADS) router_backward_kernel(const _
     }
 }
 
+// how many groups take part in the loss, where they are too many for every block to count them
+__global__ void __launch_bounds__(1024) count_groups_kernel(const int32_t *valid, int64_t groups, float *some)
+{
+    __shared__ float red[32];
+    float n = 0.f;
+    for (int64_t g = threadIdx.x; g < groups; g += 1024) n += valid[g] > 0 ? 1.f : 0.f;
+    n = warp_sum(n);
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = n;
+    __syncthreads();
+    n = warp_sum(red[threadIdx.x & 31]);
+    if (threadIdx.x == 0) *some = n;
+}
+
 struct RouterShape { int epl, lanes; bool vec; };
 
 RouterShape router_shape(const RouterArgs &a)
 {
     RouterShape s;
-    const int es = a.d.dtype == RUBICK_F32 ? 4 : 2, ve = 16 / es;
+    const int es = a.d.dtype == RUBICK_F32 ? 4 : 2;
     s.vec = aligned16(a.logits) && (!a.dlogits || aligned16(a.dlogits)) && a.d.ld * es % 16 == 0;
-    s.epl = a.d.experts > 512 ? 32 : a.d.experts > 256 ? 16 : s.vec && ve == 4 && a.d.experts <= 128 ? 4 : 8;
+    s.epl = a.d.experts > 512 ? 32 : a.d.experts > 8 ? 16 : 8;
     s.lanes = 1;
     while (s.lanes * s.epl < a.d.experts) s.lanes *= 2;
     return s;
@@ -596,48 +640,51 @@ RouterShape router_shape(const RouterArgs &a)
 // groups so many that a warp each fills the SMs
 bool by_warp(const RouterArgs &a, int num_sms) { return a.groups >= int64_t(num_sms) * ROUTER_WARPS * 2; }
 
-template <typename T, bool BACK, int EPL, bool VEC, bool WARP> cudaError_t launch_shape(const RouterArgs &a, const RouterShape &s, int num_sms, cudaStream_t st)
+template <typename T, bool BACK, int EPL, bool VEC, int LANES> cudaError_t launch_shape(const RouterArgs &a, int num_sms, cudaStream_t st)
 {
-    const int per_warp = 32 / s.lanes;
+    constexpr int per_warp = 32 / LANES;
     if constexpr (BACK) {
         const int smem = ROUTER_THREADS * EPL * int(sizeof(float));
-        // a run of rows a warp: long enough to keep a group's factors, short enough for four blocks an SM
-        const int64_t slots = int64_t(num_sms) * 4 * ROUTER_WARPS * per_warp;
+        // a run of rows a warp, so long that all blocks are resident at once
+        const int64_t slots = int64_t(num_sms) * BACKWARD_BLOCKS * ROUTER_WARPS * per_warp;
         const int run = int((a.d.rows + slots - 1) / slots);
         const int64_t per_block = int64_t(run) * ROUTER_WARPS * per_warp;
-        if (smem > 48 * 1024) {
-            const cudaError_t e = cudaFuncSetAttribute(router_backward_kernel<T, EPL, VEC, WARP>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-            if (e != cudaSuccess) return e;
+        if (a.some) {
+            count_groups_kernel<<<1, 1024, 0, st>>>(a.valid_in, a.groups, const_cast<float *>(a.some));
+            count_launch();
         }
-        router_backward_kernel<T, EPL, VEC, WARP><<<unsigned((a.d.rows + per_block - 1) / per_block), ROUTER_THREADS, smem, st>>>(a, s.lanes, run);
+        router_backward_kernel<T, EPL, VEC, LANES><<<unsigned((a.d.rows + per_block - 1) / per_block), ROUTER_THREADS, smem, st>>>(a, run);
     } else {
         const bool one = by_warp(a, num_sms);
-        const int words = a.d.experts * (one ? ROUTER_WARPS : ROUTER_WARPS + 1) + ROUTER_WARPS * (kept_words<T, EPL>() + (WARP ? 0 : per_warp * a.d.k));
-        int bits = 0;
-        while ((1 << bits) < s.lanes * s.epl) ++bits;
+        const int words = a.d.experts * (one ? ROUTER_WARPS : ROUTER_WARPS + 1) + ROUTER_WARPS * warp_words<T, EPL, LANES>(a.d.k);
         if (words > 12 * 1024) {
-            const cudaError_t e = cudaFuncSetAttribute(router_forward_kernel<T, EPL, VEC, WARP>, cudaFuncAttributeMaxDynamicSharedMemorySize, words * 4);
+            const cudaError_t e = cudaFuncSetAttribute(router_forward_kernel<T, EPL, VEC, LANES>, cudaFuncAttributeMaxDynamicSharedMemorySize, words * 4);
             if (e != cudaSuccess) return e;
         }
-        const dim3 grid = one ? dim3(unsigned(num_sms) * 4) : dim3(a.chunks, unsigned(a.groups < 32768 ? a.groups : 32768));
-        router_forward_kernel<T, EPL, VEC, WARP><<<grid, ROUTER_THREADS, words * 4, st>>>(a, s.lanes, bits, one);
+        const dim3 grid = one ? dim3(unsigned(num_sms) * FORWARD_BLOCKS) : dim3(a.chunks, unsigned(a.groups < 32768 ? a.groups : 32768));
+        router_forward_kernel<T, EPL, VEC, LANES><<<grid, ROUTER_THREADS, words * 4, st>>>(a, one);
     }
     count_launch();
     return cudaGetLastError();
 }
-template <typename T, bool BACK, int EPL, bool VEC> cudaError_t launch_router(const RouterArgs &a, const RouterShape &s, int num_sms, cudaStream_t st)
-{
-    return s.lanes == 32 && a.d.k <= 32 ? launch_shape<T, BACK, EPL, VEC, true>(a, s, num_sms, st) : launch_shape<T, BACK, EPL, VEC, false>(a, s, num_sms, st);
-}
 
+template <typename T, bool BACK, bool VEC> cudaError_t launch_vec(const RouterArgs &a, const RouterShape &s, int num_sms, cudaStream_t st)
+{
+    if (s.epl == 8) return launch_shape<T, BACK, 8, VEC, 1>(a, num_sms, st);
+    if (s.epl == 32) return launch_shape<T, BACK, 32, VEC, 32>(a, num_sms, st);
+    switch (s.lanes) {
+    case 1: return launch_shape<T, BACK, 16, VEC, 1>(a, num_sms, st);
+    case 2: return launch_shape<T, BACK, 16, VEC, 2>(a, num_sms, st);
+    case 4: return launch_shape<T, BACK, 16, VEC, 4>(a, num_sms, st);
+    case 8: return launch_shape<T, BACK, 16, VEC, 8>(a, num_sms, st);
+    case 16: return launch_shape<T, BACK, 16, VEC, 16>(a, num_sms, st);
+    default: return launch_shape<T, BACK, 16, VEC, 32>(a, num_sms, st);
+    }
+}
 template <typename T, bool BACK> cudaError_t router_epl(const RouterArgs &a, int num_sms, cudaStream_t st)
 {
     const RouterShape s = router_shape(a);
-    if constexpr (sizeof(T) == 4)
-        if (s.epl == 4) return launch_router<T, BACK, 4, true>(a, s, num_sms, st);
-    if (s.epl == 8) return s.vec ? launch_router<T, BACK, 8, true>(a, s, num_sms, st) : launch_router<T, BACK, 8, false>(a, s, num_sms, st);
-    if (s.epl == 16) return s.vec ? launch_router<T, BACK, 16, true>(a, s, num_sms, st) : launch_router<T, BACK, 16, false>(a, s, num_sms, st);
-    return s.vec ? launch_router<T, BACK, 32, true>(a, s, num_sms, st) : launch_router<T, BACK, 32, false>(a, s, num_sms, st);
+    return s.vec ? launch_vec<T, BACK, true>(a, s, num_sms, st) : launch_vec<T, BACK, false>(a, s, num_sms, st);
 }
 
 template <bool BACK> cudaError_t router_type(const RouterArgs &a, int num_sms, cudaStream_t st)
@@ -651,14 +698,15 @@ template <bool BACK> cudaError_t router_type(const RouterArgs &a, int num_sms, c
 
 }  // namespace
 
-// blocks per group: enough to fill the SMs, at least one pass of a block's warps each
+// blocks per group: as many as are resident at once, at least one pass of a block's warps each
 int router_chunks(const RouterArgs &a, int num_sms)
 {
     const RouterShape s = router_shape(a);
     const int64_t rows = a.d.group_rows < a.d.rows ? a.d.group_rows : a.d.rows;
     const int64_t most = (rows + ROUTER_WARPS * (32 / s.lanes) - 1) / (ROUTER_WARPS * (32 / s.lanes));
-    const int64_t want = (int64_t(num_sms) * 4 + a.groups - 1) / a.groups;
-    return int(most < want ? most : want);
+    const int64_t want = int64_t(num_sms) * FORWARD_BLOCKS / a.groups;
+    if (most <= 4) return 1;                      // one block and no join: the few passes cost less than the join
+    return int(most < want ? most : want > 1 ? want : 1);
 }
 
 cudaError_t launch_router_forward(const RouterArgs &a, int num_sms, cudaStream_t st) { return router_type<false>(a, num_sms, st); }

@@ -206,6 +206,10 @@ int rubick_router_backward(rubick_ctx *ctx, const rubick_router_desc *h_desc, co
     a.groups = (a.d.rows + a.d.group_rows - 1) / a.d.group_rows;
     a.logits = d_logits; a.index_in = d_index; a.weight_in = d_weight; a.counts_in = d_counts; a.valid_in = d_valid;
     a.dloss = d_dloss; a.dweight = d_dweight; a.dlogits = d_dlogits;
+    if (a.groups > 2048) {
+        if ((rc = scratch(ctx, sizeof(float)))) return rc;
+        a.some = static_cast<const float *>(ctx->d_train);
+    }
     CUDA_TRY(ctx, launch_router_backward(a, ctx->num_sms, ctx->stream), "launch router_backward");
     return RUBICK_OK;
 }

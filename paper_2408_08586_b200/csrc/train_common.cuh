@@ -254,7 +254,8 @@ struct RouterArgs {
     // scratch
     float *part;                 // [G][chunks][experts] probability sums
     int32_t *part_counts;        // [G][chunks][experts + 1] assignments, valid rows
-    float *group_loss;           // [G] loss of a group (-1: no valid row)
+    float *group_loss;           // [G] loss of a group
+    const float *some;           // backward: number of groups with valid rows, counted beforehand (NULL: by every block)
     uint32_t *tickets;           // [G + 1] arrivals, zero between calls
     int64_t groups;
     int chunks;                  // row chunks of a group
