@@ -518,7 +518,7 @@ typedef struct {
  * the sums of p and the number of valid rows n_g, and
  *     loss = coef * mean over groups with n_g > 0 of  E * sum_e (counts_e / (k n_g)) (prob_sum_e / n_g)
  * (0 if no row is valid).  A row is valid when its mask byte is not 0 (d_mask NULL: all rows) and one of its logits is
- * above -inf.  What a masked row holds is not looked at.  Experts whose logit is -inf are never chosen: places that
+ * above -inf (or NaN).  What a masked row holds is not looked at.  Experts whose logit is -inf are never chosen: places that
  * cannot be filled, and those of rows that are not valid, get index -1 and weight 0.  NaN logits are not chosen either
  * (they make the row's probabilities and the loss NaN).
  * d_index [rows][k] int32, d_weight [rows][k] float, d_counts [G][experts] int32, d_prob_sum [G][experts] float, d_valid

@@ -58,7 +58,10 @@ template <typename T, int EPL, bool VEC, int LANES> struct RawRow {
     T s[VEC ? 1 : EPL];
     __device__ __forceinline__ void load(const T *row, int sub, int experts)
     {
-        if constexpr (VEC) {
+        if (VEC && experts == LANES * EPL) {
+#pragma unroll
+            for (int i = 0; i < EPL / VE; ++i) v[i] = ld_stream(row + (i * LANES + sub) * VE);
+        } else if constexpr (VEC) {
 #pragma unroll
             for (int i = 0; i < EPL / VE; ++i) {
                 const int c = (i * LANES + sub) * VE;
@@ -73,6 +76,21 @@ template <typename T, int EPL, bool VEC, int LANES> struct RawRow {
         } else {
 #pragma unroll
             for (int i = 0; i < EPL; ++i) s[i] = i * LANES + sub < experts ? row[i * LANES + sub] : from_f<T>(-INFINITY);
+        }
+    }
+    __device__ __forceinline__ void get(f2 (&f)[EPL / 2]) const
+    {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < EPL / VE; ++i) {
+                f2 part[VE / 2];
+                unpack16<T>(v[i], part);
+#pragma unroll
+                for (int e = 0; e < VE / 2; ++e) f[i * VE / 2 + e] = part[e];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < EPL; i += 2) f[i / 2] = pair(to_f(s[i]), to_f(s[i + 1]));
         }
     }
     __device__ __forceinline__ void get(float (&f)[EPL]) const
@@ -133,46 +151,53 @@ template <int N> __device__ __forceinline__ void sort_keys(uint32_t (&s)[N])
 }
 
 // The state of a warp's rows while it goes through a chunk
-template <int EPL> struct Tally { float acc[EPL]; int valid; };
+template <int EPL> struct Tally { f2 acc[EPL / 2]; int valid; };
 
 // One row per group of lanes: index, weight and histogram are written, probabilities added to the tally.
 template <typename T, int EPL, bool VEC, int LANES>
-__device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, bool here, const float (&z)[EPL], int sub,
+__device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, bool here, const f2 (&z)[EPL / 2], int sub,
                                            uint32_t *sorted, uint32_t *list, float *kept, int32_t *hist, Tally<EPL> &tally)
 {
     constexpr int VE = Lanes<T>::N, lanes = LANES;
     constexpr bool WARP = LANES == 32;
     constexpr uint32_t low = LANES * EPL - 1;     // a power of two less one
     const int k = a.d.k;
-    // keys: NaN counts as -inf, -0 as 0; a row that is masked reads as -inf
+    // keys; -0 counts as 0 (a NaN may be anywhere: the row's sum shows it)
     uint32_t key[EPL];
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-        const uint32_t b = __float_as_uint(fmaxf(z[i], -INFINITY) + 0.f);
-        const uint32_t ordered = b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
-        key[i] = (ordered & ~low) | (low - uint32_t(column<VEC, VE, LANES>(i, sub)));
+    for (int i = 0; i < EPL; i += 2) {
+        const f2 v = add2(z[i / 2], 0ull);
+        const uint32_t b0 = uint32_t(v), b1 = uint32_t(v >> 32);
+        key[i] = ((b0 ^ (uint32_t(int32_t(b0) >> 31) | 0x80000000u)) & ~low) | (low - uint32_t(column<VEC, VE, LANES>(i, sub)));
+        key[i + 1] = ((b1 ^ (uint32_t(int32_t(b1) >> 31) | 0x80000000u)) & ~low) | (low - uint32_t(column<VEC, VE, LANES>(i + 1, sub)));
     }
     if constexpr (sizeof(T) == 4) {
         // the chosen logits are looked up whole
 #pragma unroll
-        for (int i = 0; i < EPL; i += VEC ? 4 : 1) {
-            if constexpr (VEC) *reinterpret_cast<float4 *>(kept + column<VEC, VE, LANES>(i, sub)) = make_float4(z[i], z[i + 1], z[i + 2], z[i + 3]);
-            else kept[column<VEC, VE, LANES>(i, sub)] = z[i];
+        for (int i = 0; i < EPL; i += VEC ? 4 : 2) {
+            if constexpr (VEC) {
+                *reinterpret_cast<float4 *>(kept + column<VEC, VE, LANES>(i, sub)) = make_float4(lo(z[i / 2]), hi(z[i / 2]), lo(z[i / 2 + 1]), hi(z[i / 2 + 1]));
+            } else {
+                kept[column<VEC, VE, LANES>(i, sub)] = lo(z[i / 2]);
+                kept[column<VEC, VE, LANES>(i + 1, sub)] = hi(z[i / 2]);
+            }
         }
     }
     sort_keys<EPL>(key);
     // this lane's list, 32 words from one to the next; behind its last key a 0 (written once, at the start)
 #pragma unroll
     for (int i = 1; i < EPL; ++i) sorted[i * 32] = key[i];
-    uint32_t first = 0u, mine = 0u, head = key[0];
+    uint32_t mine = 0u, head = key[0];
     const uint32_t *next_key = sorted + 32;
-#pragma unroll 1
+    uint32_t next = lanes_max<LANES>(head);
+    const uint32_t first = next;
+#pragma unroll 2
     for (int j = 0; j < k; ++j) {
-        const uint32_t m = lanes_max<LANES>(head);
-        if (j == 0) first = m;
-        if (WARP) mine = sub == j ? m : mine;
-        else if (sub == (j & (lanes - 1))) list[j] = m;
-        if (head == m && m) { head = *next_key; next_key += 32; }
+        // keys are never 0 before the lists end, and k places do not reach that end
+        if (LANES >= RUBICK_MAX_CHOSEN) mine = sub == j ? next : mine;
+        else if (sub == (j & (lanes - 1))) list[j] = next;
+        if (head == next) { head = *next_key; next_key += 32; }
+        next = lanes_max<LANES>(head);
     }
     const uint32_t none = KEY_NINF | low;         // up to here: closed, or not a column
     const bool some = first > none;
@@ -180,58 +205,66 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
     const uint32_t top = first & ~low;
     const float shift = some ? __uint_as_float(top & 0x80000000u ? top & 0x7fffffffu : ~(top | low)) : 0.f;
     const float off = -shift * 1.4426950408889634f;
-    float e[EPL], total = 0.f;
+    f2 e[EPL / 2], sums = 0ull;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e[i]) : "f"(fmaf(z[i], 1.4426950408889634f, off)));
-        total += e[i];
+    for (int i = 0; i < EPL / 2; ++i) {
+        const f2 x = fma2(z[i], both(1.4426950408889634f), both(off));
+        float e0, e1;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(lo(x)));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(hi(x)));
+        e[i] = pair(e0, e1);
+        sums = add2(sums, e[i]);
     }
-    total = lanes_sum<LANES>(total);
+    const float total = lanes_sum<LANES>(lo(sums) + hi(sums));
     const float inv = some ? __fdividef(1.f, total) : 0.f;
-    if (some) {
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) tally.acc[i] = fmaf(e[i], inv, tally.acc[i]);
-    }
-    tally.valid += some && sub == 0 ? 1 : 0;
+    for (int i = 0; i < EPL / 2; ++i) tally.acc[i] = fma2(e[i], both(inv), tally.acc[i]);
+    tally.valid += (some || total != total) && sub == 0 ? 1 : 0;      // (a NaN counts as above -inf)
     if (!WARP || sizeof(T) == 4) __syncwarp();
+    // A NaN, or neighbours that only the cut-off bits tell apart: once more, with whole keys.
+    bool unsure = total != total;
     if constexpr (sizeof(T) == 4) {
-        // neighbours that only the cut-off bits tell apart: once more, with whole keys
-        const uint32_t next = lanes_max<LANES>(head);
-        bool unsure = false;
+        bool near = false;
+        const uint32_t below = WARP ? __shfl_down_sync(0xffffffffu, mine, 1) : 0u;
         for (int j = sub; j < k; j += lanes) {
-            const uint32_t x = WARP ? mine : list[j], y = j + 1 == k ? next : WARP ? 0u : list[j + 1];
-            if (WARP && j + 1 < k) continue;      // (compared below, with the next lane's)
-            unsure |= (x & ~low) == (y & ~low) && x > none && kept[low - (x & low)] != kept[low - (y & low)];
+            const uint32_t x = WARP ? mine : list[j], y = j + 1 == k ? next : WARP ? below : list[j + 1];
+            near |= (x ^ y) <= low && x > none;
         }
-        if constexpr (WARP) {
-            const uint32_t y = __shfl_down_sync(0xffffffffu, mine, 1);
-            if (sub + 1 < k) unsure |= (mine & ~low) == (y & ~low) && mine > none && kept[low - (mine & low)] != kept[low - (y & low)];
-        }
-        if (__any_sync(0xffffffffu, unsure)) {
-            uint32_t whole[EPL];
-#pragma unroll
-            for (int i = 0; i < EPL; ++i) whole[i] = order_key(z[i]);
-#pragma unroll 1
-            for (int j = 0; j < k; ++j) {
-                uint32_t best = 0u;
-                int col = 0x7fffffff;
-#pragma unroll
-                for (int i = 0; i < EPL; ++i)
-                    if (whole[i] > best) { best = whole[i]; col = column<VEC, VE, LANES>(i, sub); }
-#pragma unroll
-                for (int o = 16; o; o >>= 1) {
-                    const uint32_t kb = __shfl_xor_sync(0xffffffffu, best, o);
-                    const int cb = __shfl_xor_sync(0xffffffffu, col, o);
-                    if (o < lanes && (kb > best || (kb == best && cb < col))) { best = kb; col = cb; }
-                }
-                const uint32_t m = best > KEY_NINF ? 0x80000000u | (low - uint32_t(col)) : 0u;      // any key of that column that is open
-                if (WARP) mine = sub == j ? m : mine;
-                else if (sub == (j & (lanes - 1))) list[j] = m;
-#pragma unroll
-                for (int i = 0; i < EPL; ++i) if (column<VEC, VE, LANES>(i, sub) == col) whole[i] = 0u;
+        if (__any_sync(0xffffffffu, near)) {
+            for (int j = sub; j < k; j += lanes) {
+                const uint32_t x = WARP ? mine : list[j], y = j + 1 == k ? next : WARP ? below : list[j + 1];
+                unsure |= (x ^ y) <= low && x > none && kept[low - (x & low)] != kept[low - (y & low)];
             }
-            __syncwarp();
         }
+    }
+    if (__any_sync(0xffffffffu, unsure)) {
+        uint32_t whole[EPL];
+#pragma unroll
+        for (int i = 0; i < EPL; i += 2) { whole[i] = order_key(lo(z[i / 2])); whole[i + 1] = order_key(hi(z[i / 2])); }
+        __syncwarp();
+#pragma unroll 1
+        for (int j = 0; j < k; ++j) {
+            uint32_t best = 0u;
+            int col = 0x7fffffff;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) {
+                const int c = column<VEC, VE, LANES>(i, sub);
+                if (whole[i] > best || (whole[i] == best && c < col && best)) { best = whole[i]; col = c; }
+            }
+#pragma unroll
+            for (int o = LANES / 2; o; o >>= 1) {
+                const uint32_t kb = __shfl_xor_sync(0xffffffffu, best, o);
+                const int cb = __shfl_xor_sync(0xffffffffu, col, o);
+                if (kb > best || (kb == best && cb < col)) { best = kb; col = cb; }
+            }
+            // the key of that column as above; 0 where nothing is open
+            const uint32_t m = best > KEY_NINF ? (best & ~low) | (low - uint32_t(col)) : 0u;
+            if (LANES >= RUBICK_MAX_CHOSEN) mine = sub == j ? m : mine;
+            else if (sub == (j & (lanes - 1))) list[j] = m;
+#pragma unroll
+            for (int i = 0; i < EPL; ++i) if (column<VEC, VE, LANES>(i, sub) == col) whole[i] = 0u;
+        }
+        __syncwarp();
     }
     // places: lane j of the row has the j-th (and the j + lanes-th ...)
     float sum = 0.f;
@@ -326,17 +359,18 @@ __device__ __forceinline__ void route_chunk(const RouterArgs &a, int64_t first, 
     RawRow<T, EPL, VEC, LANES> next;
     uint8_t mask = 1;
     const auto fetch = [&](int64_t row) {
-        const bool here = row < end;
-        if (a.mask) mask = here ? a.mask[row] : uint8_t(0);
-        next.load(static_cast<const T *>(a.logits) + (here ? row : 0) * a.d.ld, sub, here ? a.d.experts : 0);
+        const int64_t at = row < end ? row : first;      // (a row that is there)
+        if (a.mask) mask = a.mask[at];
+        next.load(static_cast<const T *>(a.logits) + at * a.d.ld, sub, a.d.experts);
     };
     if (first < end) fetch(first + slot);
     for (int64_t row = first; row < end; row += stride) {
-        float z[EPL];
+        f2 z[EPL / 2];
         next.get(z);
-        if (!mask) {                              // what stands in a masked row is not looked at
+        const bool out = !mask || row + slot >= end;
+        if (__any_sync(0xffffffffu, out)) {       // what stands in a masked row is not looked at
 #pragma unroll
-            for (int i = 0; i < EPL; ++i) z[i] = -INFINITY;
+            for (int i = 0; i < EPL / 2; ++i) z[i] = out ? both(-INFINITY) : z[i];
         }
         if (row + stride < end) fetch(row + stride + slot);
         route_rows<T, EPL, VEC, LANES>(a, row + slot, row + slot < end, z, sub, sorted, list, kept, hist, tally);
@@ -344,13 +378,15 @@ __device__ __forceinline__ void route_chunk(const RouterArgs &a, int64_t first, 
 }
 
 // the sums of a warp's rows, at the lanes of its first row
-template <int EPL, int LANES> __device__ __forceinline__ void fold_rows(Tally<EPL> &t)
+template <int EPL, int LANES> __device__ __forceinline__ void fold_rows(const Tally<EPL> &t, float (&acc)[EPL], int &valid)
 {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i)
+    for (int i = 0; i < EPL; ++i) {
+        acc[i] = i & 1 ? hi(t.acc[i / 2]) : lo(t.acc[i / 2]);
 #pragma unroll
-        for (int o = 16; o >= LANES; o >>= 1) t.acc[i] += __shfl_xor_sync(0xffffffffu, t.acc[i], o);
-    t.valid = __reduce_add_sync(0xffffffffu, t.valid);
+        for (int o = 16; o >= LANES; o >>= 1) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
+    }
+    valid = __reduce_add_sync(0xffffffffu, t.valid);
 }
 
 // Shared memory of the forward kernel, in words: per warp its 32 EPL logits (single precision), the lanes' sorted lists
@@ -387,10 +423,12 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : FORWARD_BLOCKS)
             const int64_t g0 = g * a.d.group_rows, g1 = g0 + a.d.group_rows < a.d.rows ? g0 + a.d.group_rows : a.d.rows;
             Tally<EPL> t;
 #pragma unroll
-            for (int i = 0; i < EPL; ++i) t.acc[i] = 0.f;
+            for (int i = 0; i < EPL / 2; ++i) t.acc[i] = 0ull;
             t.valid = 0;
             route_chunk<T, EPL, VEC, LANES>(a, g0, g1, per_warp, sub, slot, sorted, list, kept, hist, t);
-            fold_rows<EPL, LANES>(t);
+            float acc[EPL];
+            int valid;
+            fold_rows<EPL, LANES>(t, acc, valid);
             __syncwarp();
             float dot = 0.f;
 #pragma unroll
@@ -400,16 +438,16 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : FORWARD_BLOCKS)
                     const int n = hist[c];
                     hist[c] = 0;
                     a.counts[g * E + c] = n;
-                    a.prob_sum[g * E + c] = t.acc[i];
-                    dot = fmaf(float(n), t.acc[i], dot);
+                    a.prob_sum[g * E + c] = acc[i];
+                    dot = fmaf(float(n), acc[i], dot);
                 }
             }
             dot = warp_sum(dot);
             __syncwarp();
             if (lane == 0) {
-                const float n = float(t.valid);
-                a.valid[g] = t.valid;
-                a.group_loss[g] = t.valid > 0 ? dot * float(E) / (float(a.d.k) * n * n) : 0.f;
+                const float n = float(valid);
+                a.valid[g] = valid;
+                a.group_loss[g] = valid > 0 ? dot * float(E) / (float(a.d.k) * n * n) : 0.f;
             }
         }
         __threadfence();
@@ -428,18 +466,20 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : FORWARD_BLOCKS)
         const int64_t g1 = g0 + a.d.group_rows < a.d.rows ? g0 + a.d.group_rows : a.d.rows;
         Tally<EPL> t;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) t.acc[i] = 0.f;
+        for (int i = 0; i < EPL / 2; ++i) t.acc[i] = 0ull;
         t.valid = 0;
         route_chunk<T, EPL, VEC, LANES>(a, g0 + (int64_t(blockIdx.x) * ROUTER_WARPS + warp) * per_warp, g1, int64_t(a.chunks) * ROUTER_WARPS * per_warp,
                                           sub, slot, sorted, list, kept, hist, t);
         // rows of a warp, then warps of the block
-        fold_rows<EPL, LANES>(t);
+        float acc[EPL];
+        int valid;
+        fold_rows<EPL, LANES>(t, acc, valid);
 #pragma unroll
         for (int i = 0; i < EPL; ++i) {
             const int c = column<VEC, VE, LANES>(i, sub);
-            if (lane < lanes && c < E) psum[warp * E + c] = t.acc[i];
+            if (lane < lanes && c < E) psum[warp * E + c] = acc[i];
         }
-        if (lane == 0 && t.valid) atomicAdd(&valid_rows, t.valid);
+        if (lane == 0 && valid) atomicAdd(&valid_rows, valid);
         __syncthreads();
         const int64_t place = g * a.chunks + blockIdx.x;
         const bool alone = a.chunks == 1;
@@ -518,7 +558,7 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : BACKWARD_BLOCKS
     const bool weights = a.dweight != nullptr;
     const auto fetch = [&](int64_t row) {
         const bool here = row < end;
-        next.load(static_cast<const T *>(a.logits) + (here ? row : 0) * a.d.ld, sub, here ? E : 0);
+        next.load(static_cast<const T *>(a.logits) + (here ? row : begin) * a.d.ld, sub, E);
         lead = col = -1;
         if (here) lead = a.index_in[row * k];
         if (here && sub < k && weights) {
@@ -528,16 +568,16 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : BACKWARD_BLOCKS
         }
     };
     int64_t group = -1, group_end = -1;
-    float f[EPL];
+    f2 f[EPL / 2];
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) f[i] = 0.f;
+    for (int i = 0; i < EPL / 2; ++i) f[i] = 0ull;
     if (begin < end) fetch(begin + slot);
     for (int64_t first = begin; first < end; first += per_warp) {
         const int64_t row = first + slot;
         const bool h = row < end, l = lead >= 0;
         const int c0 = col;
         const float w0 = w, d0 = d;
-        float z[EPL];
+        f2 z[EPL / 2];
         next.get(z);
         if (first + per_warp < end) fetch(row + per_warp);
         if (h && row >= group_end) {
@@ -545,9 +585,9 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : BACKWARD_BLOCKS
             group_end = (group + 1) * a.d.group_rows;
             const float m = fmaxf(float(a.valid_in[group]), 1.f), scale = pull / (m * m);
 #pragma unroll
-            for (int i = 0; i < EPL; ++i) {
-                const int c = column<VEC, VE, LANES>(i, sub);
-                f[i] = c < E ? scale * float(__ldg(a.counts_in + group * E + c)) : 0.f;
+            for (int i = 0; i < EPL; i += 2) {
+                const int c = column<VEC, VE, LANES>(i, sub), c1 = column<VEC, VE, LANES>(i + 1, sub);
+                f[i / 2] = pair(c < E ? scale * float(__ldg(a.counts_in + group * E + c)) : 0.f, c1 < E ? scale * float(__ldg(a.counts_in + group * E + c1)) : 0.f);
             }
         }
         // the chosen: w_j d_j, their sum over the row, and what goes to their columns
@@ -564,39 +604,55 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : BACKWARD_BLOCKS
                 if (e >= 0 && e < E) atomicAdd(mine + e, a.weight_in[row * k + j] * (a.dweight[row * k + j] - mean));
             }
         }
-        float top = z[0], total = 0.f, dot = 0.f;
+        float top = -INFINITY;
 #pragma unroll
-        for (int i = 1; i < EPL; ++i) top = fmaxf(top, z[i]);
+        for (int i = 0; i < EPL / 2; ++i) top = fmaxf(top, fmaxf(lo(z[i]), hi(z[i])));
         top = lanes_max<LANES>(top);
-        const float off = top > -INFINITY ? -top * 1.4426950408889634f : 0.f;
+        const f2 off = both(top > -INFINITY ? -top * 1.4426950408889634f : 0.f);
+        f2 sums = 0ull, dots = 0ull;
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) {
-            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(z[i]) : "f"(fmaf(z[i], 1.4426950408889634f, off)));
-            total += z[i];
-            dot = fmaf(f[i], z[i], dot);
+        for (int i = 0; i < EPL / 2; ++i) {
+            const f2 x = fma2(z[i], both(1.4426950408889634f), off);
+            float e0, e1;
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(lo(x)));
+            asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(hi(x)));
+            z[i] = pair(e0, e1);
+            sums = add2(sums, z[i]);
+            dots = fma2(f[i], z[i], dots);
         }
-        total = lanes_sum<LANES>(total);
-        dot = lanes_sum<LANES>(dot);
+        const float total = lanes_sum<LANES>(lo(sums) + hi(sums));
+        float dot = lanes_sum<LANES>(lo(dots) + hi(dots));
         const float inv = __fdividef(1.f, total);
         dot = fmaf(dot, inv, renorm ? 0.f : wd);
         if (weights) __syncwarp();
-        T *out = static_cast<T *>(a.dlogits) + (h ? row : 0) * a.d.ld;
-        const int stop = h ? E : 0;
+        T *out = static_cast<T *>(a.dlogits) + (h ? row : begin) * a.d.ld;
+        const f2 inv2 = both(inv), less = both(-dot);
 #pragma unroll
-        for (int i = 0; i < EPL; i += VEC ? VE : 1) {
+        for (int i = 0; i < EPL; i += VEC ? VE : 2) {
             const int c = column<VEC, VE, LANES>(i, sub);
             if constexpr (VEC) {
-                float r[VE], more[VE];
+                f2 r[VE / 2];
 #pragma unroll
                 for (int e = 0; e < VE; e += 4) {
-                    const float4 q = weights ? *reinterpret_cast<const float4 *>(mine + c + e) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    more[e] = q.x; more[e + 1] = q.y; more[e + 2] = q.z; more[e + 3] = q.w;
+                    const ulonglong2 q = weights ? *reinterpret_cast<const ulonglong2 *>(mine + c + e) : make_ulonglong2(0ull, 0ull);
+                    r[e / 2] = fma2(mul2(z[(i + e) / 2], inv2), add2(f[(i + e) / 2], less), q.x);
+                    r[e / 2 + 1] = fma2(mul2(z[(i + e) / 2 + 1], inv2), add2(f[(i + e) / 2 + 1], less), q.y);
                 }
+                uint4 v = pack16<T>(r);
+                if (!l) v = make_uint4(0u, 0u, 0u, 0u);
+                if (h && c + VE <= E) st_stream(out + c, v);
+                else if (h && c < E) {
+                    float t[VE];
+                    unpack16<T>(v, t);
 #pragma unroll
-                for (int e = 0; e < VE; ++e) r[e] = l ? fmaf(z[i + e] * inv, f[i + e] - dot, more[e]) : 0.f;
-                store_cols<T, VE>(out, c, stop, r);
-            } else if (c < stop) {
-                out[c] = from_f<T>(l ? fmaf(z[i] * inv, f[i] - dot, weights ? mine[c] : 0.f) : 0.f);
+                    for (int e = 0; e < VE; ++e) if (c + e < E) out[c + e] = from_f<T>(t[e]);
+                }
+            } else {
+                const int c1 = column<VEC, VE, LANES>(i + 1, sub);
+                const f2 q = weights ? pair(mine[c], mine[c1]) : 0ull;
+                const f2 r = fma2(mul2(z[i / 2], inv2), add2(f[i / 2], less), q);
+                if (h && c < E) out[c] = from_f<T>(l ? lo(r) : 0.f);
+                if (h && c1 < E) out[c1] = from_f<T>(l ? hi(r) : 0.f);
             }
         }
         if (weights) {

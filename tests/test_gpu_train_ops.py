@@ -277,6 +277,9 @@ ROUTER_CASES = [
     (16, 1024, 32, "bf16", dict(group=5)),
     (5000, 16, 2, "bf16", dict(group=1250, masked=2000)),
     (64, 32, 4, "bf16", dict(masked=64)),
+    # groups so many that a warp takes each, and that they are counted beforehand in the backward pass
+    (9600, 24, 3, "fp32", dict(group=2, masked=50)),
+    (12000, 256, 2, "bf16", dict(group=3, renorm=True)),
 ]
 
 
@@ -348,6 +351,33 @@ def test_router_repeats_itself_and_takes_its_output_over_its_input(ctx):
     for name in a:
         assert torch.equal(a[name], b[name]), name
     assert torch.equal(z, out)
+
+
+@pytest.mark.parametrize("dtype,experts", [("bf16", 16), ("fp32", 128), ("fp32", 300), ("fp16", 7)])
+def test_router_never_chooses_nan_and_keeps_near_ties_in_order(ctx, dtype, experts):
+    """Logits that differ in their last bit only are chosen in their order, equal ones (0 and -0 among them) by index; a NaN
+    is never chosen and spoils its own row's weights, its group's sums and the loss, not the choice."""
+    import torch
+    z = torch.zeros(6, experts)
+    if dtype == "fp32":
+        z[0] = torch.nextafter(torch.tensor(1.0), torch.tensor(2.0))
+        z[0, 3:] = 1.0
+        z[0, 5] = 1.0 + 2.0 ** -21
+    z[1, ::2] = -0.0
+    z[2, 1] = float("nan")
+    z[2, 4] = 2.0
+    z[3, 0] = -float("nan")
+    z[4] = -torch.arange(experts) - 1.0
+    z = z.to(T(dtype)).cuda()
+    k = 5
+    o = router_outputs(6, experts, k, 2)
+    ctx.router_forward(rb.router(6, experts, k, T(dtype), group_rows=3), z, None, o["index"], o["weight"], o["counts"], o["prob_sum"], o["valid"], o["loss"])
+    ctx.sync()
+    clean = torch.where(torch.isnan(z), NINF, z.float())
+    want = ref.router_forward(clean, None, k, group_rows=3, coef=0.01, renorm=False)
+    assert torch.equal(o["index"].cpu().long(), want["index"]) and torch.equal(o["counts"].cpu().long(), want["counts"])
+    weight = o["weight"].cpu()
+    assert torch.isnan(weight[[2, 3]]).all() and torch.isfinite(weight[[0, 1, 4, 5]]).all() and torch.isnan(o["loss"]).all()
 
 
 def test_router_gradient_is_the_slope_of_the_loss(ctx):
