@@ -312,25 +312,46 @@ __device__ void finish_group(const RouterArgs &a, int64_t g, float dot, int vali
     }
 }
 
-// What the last block of a group does: the chunks' sums in chunk order
-__device__ void join_group(const RouterArgs &a, int64_t g)
+// What the last block of a group does: the chunks' sums, every warp a run of them, then the warps' sums in order (a block
+// that joins takes no further group: there are chunks only where groups are fewer than blocks).  `red`:
+// 2 x [warps][32] words.
+__device__ void join_group(const RouterArgs &a, int64_t g, float *red)
 {
-    const int E = a.d.experts, C = a.chunks;
+    __shared__ int32_t valid_rows;
+    const int E = a.d.experts, C = a.chunks, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t *pc = a.part_counts + g * C * (E + 1);
     const float *ps = a.part + g * C * E;
+    int32_t *red_n = reinterpret_cast<int32_t *>(red + ROUTER_THREADS);
+    if (threadIdx.x == 0) valid_rows = 0;
+    __syncthreads();
     int valid = 0;
-    for (int q = 0; q < C; ++q) valid += __ldcg(pc + int64_t(q) * (E + 1) + E);
+    for (int q = threadIdx.x; q < C; q += ROUTER_THREADS) valid += __ldcg(pc + int64_t(q) * (E + 1) + E);
+    valid = __reduce_add_sync(0xffffffffu, valid);
+    if (lane == 0 && valid) atomicAdd(&valid_rows, valid);
+    const int run = (C + ROUTER_WARPS - 1) / ROUTER_WARPS, q0 = warp * run, q1 = q0 + run < C ? q0 + run : C;
     float dot = 0.f;
-    for (int e = threadIdx.x; e < E; e += ROUTER_THREADS) {
+    for (int e0 = 0; e0 < E; e0 += 32) {
+        const int e = e0 + lane;
         int n = 0;
         float s = 0.f;
-#pragma unroll 4
-        for (int q = 0; q < C; ++q) { n += __ldcg(pc + int64_t(q) * (E + 1) + e); s += __ldcg(ps + int64_t(q) * E + e); }
-        a.counts[g * E + e] = n;
-        a.prob_sum[g * E + e] = s;
-        dot = fmaf(float(n), s, dot);
+        if (e < E)
+#pragma unroll 8
+            for (int q = q0; q < q1; ++q) { n += __ldcg(pc + int64_t(q) * (E + 1) + e); s += __ldcg(ps + int64_t(q) * E + e); }
+        __syncthreads();                          // the columns before are read
+        red[threadIdx.x] = s;
+        red_n[threadIdx.x] = n;
+        __syncthreads();
+        if (warp == (e0 >> 5) % ROUTER_WARPS && e < E) {
+            n = 0;
+            s = 0.f;
+#pragma unroll
+            for (int w = 0; w < ROUTER_WARPS; ++w) { n += red_n[w * 32 + lane]; s += red[w * 32 + lane]; }
+            a.counts[g * E + e] = n;
+            a.prob_sum[g * E + e] = s;
+            dot = fmaf(float(n), s, dot);
+        }
     }
-    finish_group(a, g, dot, valid);
+    finish_group(a, g, dot, valid_rows);
 }
 
 __device__ void join_loss(const RouterArgs &a)
@@ -509,7 +530,7 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : FORWARD_BLOCKS)
         __syncthreads();
         if (last) {                                // every chunk of the group has arrived
             if (alone) finish_group(a, g, dot, rows_here);
-            else { __threadfence(); join_group(a, g); }
+            else { __threadfence(); join_group(a, g, reinterpret_cast<float *>(smem)); }
             if (!alone && threadIdx.x == 0) a.tickets[g] = 0u;
             if (a.groups == 1) return;             // finish_group has written the loss
             __threadfence();
