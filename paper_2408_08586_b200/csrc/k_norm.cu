@@ -137,158 +137,8 @@ __device__ __forceinline__ float *part_row(const NormArgs &a, int which, int chu
     return a.part + (int64_t(which) * a.n_chunks + chunk) * a.d.cols;
 }
 
-// Writes the gate gradient of rows [first, last] of a chunk that starts at row `begin`, all in one gate group: final
-// where the whole group is in the chunk, a partial sum otherwise.
-template <typename T, int VE, int NV>
-__device__ __forceinline__ void flush_gate(const NormArgs &a, int chunk, int64_t begin, int64_t end_row, int64_t group, int tpr,
-                                           float (&acc)[NV][VE])
-{
-    const int64_t g0 = group * a.d.group_rows;
-    const int64_t g1 = g0 + a.d.group_rows < a.d.rows ? g0 + a.d.group_rows : a.d.rows;
-    if (a.d.flags & RUBICK_NORM_TANH_GATE) {
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float g[VE], slope;
-            load_shared_cols<T, VE>(static_cast<const T *>(a.gate) + group * a.d.ld_gate, (i * tpr + int(threadIdx.x)) * VE, a.d.cols, g, 0.f);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) { tanh_slope(g[e], slope); acc[i][e] *= slope; }
-        }
-    }
-    if (!a.dgate) {
-        // nobody asked for it
-    } else if (g0 >= begin && g1 <= end_row) {
-        T *dg = static_cast<T *>(a.dgate) + group * a.d.ld_gate;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            float r[VE];
-#pragma unroll
-            for (int e = 0; e < VE; ++e) r[e] = acc[i][e];
-            store_cols<T, VE>(dg, (i * tpr + int(threadIdx.x)) * VE, a.d.cols, r);
-        }
-    } else {
-        float *p = part_row(a, g0 < begin ? 2 : 3, chunk);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const int c = (i * tpr + int(threadIdx.x)) * VE + e;
-                if (c < a.d.cols) p[c] = acc[i][e];
-            }
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < VE; ++e) acc[i][e] = 0.f;
-}
-
-// One row slot (threadIdx.y) of a block works through one chunk of consecutive rows; the column sums stay in
-// registers until the chunk ends.
-template <typename T, typename W, int VE, int NV>
-__global__ void __launch_bounds__(512) norm_backward_kernel(const __grid_constant__ NormArgs a)
-{
-    __shared__ float red[2][3 * 32];
-    const int tpr = blockDim.x, warps = tpr >> 5, cols = a.d.cols;
-    const int chunk = blockIdx.x * blockDim.y + threadIdx.y;
-    const int64_t begin = chunk * a.chunk_rows;
-    const int64_t stop = begin + a.chunk_rows < a.d.rows ? begin + a.chunk_rows : a.d.rows;
-    const bool after = a.d.flags & RUBICK_NORM_AFTER, before = a.d.flags & RUBICK_NORM_BEFORE;
-    const bool th = a.d.flags & RUBICK_NORM_TANH_GATE, need_y = a.y && (after || a.gate);
-    const float o = a.d.flags & RUBICK_NORM_UNIT_OFFSET ? 1.f : 0.f;
-    const float inv_cols = 1.f / float(cols);
-    const int c0 = int(threadIdx.x) * VE;
-    float acc_a[NV][VE], acc_b[NV][VE], acc_g[NV][VE], g[NV][VE];
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < VE; ++e) { acc_a[i][e] = acc_b[i][e] = acc_g[i][e] = 0.f; g[i][e] = 1.f; }
-    int64_t group = -1, group_end = begin;        // the gate row in g[][]
-    for (int64_t step = 0; step < a.chunk_rows; ++step) {          // the same count for every row slot of the block
-        const int64_t row = begin + step;
-        const bool live = row < stop;
-        const int end = live ? cols : 0;
-        Raw<T, VE> dxo[NV], xr[NV], dh[NV], yr[NV];
-        const float ra = after && live ? a.rstd_in[2 * row] : 1.f;
-        const float rb = before && live ? a.rstd_in[2 * row + 1] : 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = i * tpr * VE + c0;
-            dxo[i].zero(); xr[i].zero(); dh[i].zero(); yr[i].zero();
-            if (a.dx_out) dxo[i].load(static_cast<const T *>(a.dx_out) + row * a.d.ld_x, c, end);
-            if (before) xr[i].load(static_cast<const T *>(a.x) + row * a.d.ld_x, c, end);
-            if (before) dh[i].load(static_cast<const T *>(a.dh) + row * a.d.ld_h, c, end);
-            if (need_y) yr[i].load(static_cast<const T *>(a.y) + row * a.d.ld_y, c, end);
-        }
-        if (a.gate && live && row >= group_end) {
-            if (group >= 0) flush_gate<T, VE, NV>(a, chunk, begin, stop, group, tpr, acc_g);
-            group = row / a.d.group_rows;
-            group_end = (group + 1) * a.d.group_rows;
-            const T *gate = static_cast<const T *>(a.gate) + group * a.d.ld_gate;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                load_shared_cols<T, VE>(gate, i * tpr * VE + c0, cols, g[i], 0.f);
-                if (th) {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) g[i][e] = tanhf(g[i][e]);
-                }
-            }
-        }
-        float s[3] = {0.f, 0.f, 0.f};
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = i * tpr * VE + c0;
-            float wa[VE], wb[VE], d[VE], x[VE], e1[VE], y[VE];
-#pragma unroll
-            for (int e = 0; e < VE; ++e) wa[e] = wb[e] = 1.f - o;
-            if (a.w_after) load_shared_cols<W, VE>(static_cast<const W *>(a.w_after), c, cols, wa, 0.f);
-            if (a.w_before) load_shared_cols<W, VE>(static_cast<const W *>(a.w_before), c, cols, wb, 0.f);
-            dxo[i].get(d); xr[i].get(x); dh[i].get(e1); yr[i].get(y);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const float xh = x[e] * rb, ew = e1[e] * (wb[e] + o);
-                acc_b[i][e] = fmaf(e1[e], xh, acc_b[i][e]);
-                s[0] = fmaf(ew, xh, s[0]);
-                const float q = a.d.alpha * g[i][e] * (wa[e] + o) * (y[e] * ra);
-                s[1] = fmaf(q, fmaf(rb, ew, d[e]), s[1]);
-                s[2] = fmaf(q, xh, s[2]);
-            }
-        }
-        row_sum<3>(s, red[step & 1], warps, threadIdx.y);
-        const float m1 = s[0] * inv_cols, m2 = after ? (s[1] - rb * m1 * s[2]) * inv_cols : 0.f;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = i * tpr * VE + c0;
-            float wa[VE], wb[VE], d[VE], x[VE], e1[VE], y[VE], dx[VE], dy[VE];
-#pragma unroll
-            for (int e = 0; e < VE; ++e) wa[e] = wb[e] = 1.f - o;
-            if (a.w_after) load_shared_cols<W, VE>(static_cast<const W *>(a.w_after), c, cols, wa, 0.f);
-            if (a.w_before) load_shared_cols<W, VE>(static_cast<const W *>(a.w_before), c, cols, wb, 0.f);
-            dxo[i].get(d); xr[i].get(x); dh[i].get(e1); yr[i].get(y);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                dx[e] = fmaf(rb, e1[e] * (wb[e] + o) - x[e] * rb * m1, d[e]);
-                const float f = a.d.alpha * dx[e], fg = f * g[i][e], yh = y[e] * ra, w = wa[e] + o;
-                acc_g[i][e] = fmaf(f * w, yh, acc_g[i][e]);
-                acc_a[i][e] = fmaf(fg, yh, acc_a[i][e]);
-                dy[e] = after ? ra * (fg * w - yh * m2) : fg;
-            }
-            store_cols<T, VE>(static_cast<T *>(a.dx) + row * a.d.ld_x, c, end, dx);
-            if (a.dy) store_cols<T, VE>(static_cast<T *>(a.dy) + row * a.d.ld_y, c, end, dy);
-        }
-    }
-    if (chunk >= a.n_chunks) return;
-    if (group >= 0) flush_gate<T, VE, NV>(a, chunk, begin, stop, group, tpr, acc_g);
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int e = 0; e < VE; ++e) {
-            const int c = i * tpr * VE + c0 + e;
-            if (c < cols && a.dw_after) part_row(a, 0, chunk)[c] = acc_a[i][e];
-            if (c < cols && a.dw_before) part_row(a, 1, chunk)[c] = acc_b[i][e];
-        }
-}
-
-// The same for rows that are too wide for registers: the column sums are in shared memory, and a row is read twice
-// (the second time from L2), once for its sums and once for its gradients.
+// Rows too wide for the ring below: the column sums are in shared memory, and a row is read twice (the second time from
+// L2), once for its sums and once for its gradients.
 template <typename T, typename W, int VE>
 __global__ void __launch_bounds__(512) norm_backward_wide_kernel(const __grid_constant__ NormArgs a)
 {
@@ -381,9 +231,11 @@ __global__ void __launch_bounds__(512) norm_backward_wide_kernel(const __grid_co
 
 // ---- rows through a ring of shared-memory stages ---------------------------------------------------------------
 //
-// Where every row is a whole number of 16-byte units, a block takes a run of consecutive rows and one thread copies
-// them with the bulk-copy engine, several rows ahead: the copies in flight do not depend on how many warps are
-// waiting, and a row that waits for its sums holds no registers.  What is the same for all rows of a gate group,
+// A block takes a run of consecutive rows and one thread copies them with the bulk-copy engine, several rows ahead: the
+// copies in flight do not depend on how many warps are waiting, and a row that waits for its sums holds no registers.
+// Rows that are a whole number of 16-byte units are read and written 16 bytes at a time.  Others are copied with the
+// units that they begin and end in and taken element by element, column c by thread c mod (threads), so that a column
+// stays with its thread whatever the row's place in its unit.  What is the same for all rows of a gate group,
 // k = alpha g W_after, is kept per column; a column's gradients of gate and weight are both
 // sum G yh times a factor of the group, so one running sum serves both:
 //   dgate = g' alpha W_after t,   dW_after += alpha g t,   t = sum over the group's rows of G yh.
@@ -393,7 +245,42 @@ constexpr int RING_MOST = 8;      // stages
 struct Ring {
     int stages, tensors;
     int i_x, i_y, i_dxo, i_dh, i_gate;    // place of a tensor in a stage, -1: not copied
-    uint32_t row_bytes;
+    uint32_t slot_bytes;                  // of a row in a stage
+};
+
+// A thread's i-th set of columns: VE neighbours, or (VEC = false) two that are a row of threads apart
+template <typename T, bool VEC> struct Cols {
+    static constexpr int VE = VEC ? Lanes<T>::N : 2, VP = VE / 2;
+    static __device__ __forceinline__ int first(int i, int tpr) { return VEC ? (i * tpr + int(threadIdx.x)) * VE : 2 * i * tpr + int(threadIdx.x); }
+    static __device__ __forceinline__ void load(const T *from, int c, int tpr, int cols, f2 (&v)[VP])
+    {
+        if constexpr (VEC) unpack16<T>(*reinterpret_cast<const uint4 *>(from + c), v);
+        else v[0] = pair(to_f(from[c]), c + tpr < cols ? to_f(from[c + tpr]) : 0.f);
+    }
+    static __device__ __forceinline__ void store(T *to, int c, int tpr, int cols, const f2 (&v)[VP])
+    {
+        if constexpr (VEC) {
+            st_stream(to + c, pack16<T>(v));
+        } else {
+            to[c] = from_f<T>(lo(v[0]));
+            if (c + tpr < cols) to[c + tpr] = from_f<T>(hi(v[0]));
+        }
+    }
+    template <typename W> static __device__ __forceinline__ void weights(const W *from, int c, int tpr, int cols, float (&v)[VE])
+    {
+        if constexpr (VEC) load_shared_cols<W, VE>(from, c, cols, v, 0.f);
+        else { v[0] = to_f(from[c]); v[1] = c + tpr < cols ? to_f(from[c + tpr]) : 0.f; }
+    }
+    static __device__ __forceinline__ void put(float *to, int c, int tpr, int cols, const f2 (&v)[VP])
+    {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int e = 0; e < VP; e += 2) *reinterpret_cast<ulonglong2 *>(to + c + 2 * e) = make_ulonglong2(v[e], v[e + 1]);
+        } else {
+            to[c] = lo(v[0]);
+            if (c + tpr < cols) to[c + tpr] = hi(v[0]);
+        }
+    }
 };
 
 // One barrier for the threads of a block (a warp where it is one).
@@ -436,21 +323,69 @@ template <int N> __device__ __forceinline__ void ring_sum(const f2 (&in)[N], flo
         }
 }
 
-// The copies of row `row` into stage `s`, by one thread.
-template <typename T> __device__ __forceinline__ void ring_issue(const NormArgs &a, const Ring &r, uint8_t *smem, uint64_t *bars, int s, int64_t row)
+// What is to be copied of `bytes` bytes at `from` in whole 16-byte units.  The units that reach out of the tensor (before
+// its first row, behind its last) are put together byte by byte.
+struct Units { uintptr_t b0, b1; };
+__device__ __forceinline__ Units row_units(uintptr_t from, uint32_t bytes, bool first, bool last, uint8_t *slot)
 {
-    uint8_t *stage = smem + size_t(s) * r.tensors * r.row_bytes;
-    bar_expect(bars + s, r.row_bytes * r.tensors);
-    if (r.i_x >= 0) bulk_load(stage + r.i_x * r.row_bytes, static_cast<const T *>(a.x) + row * a.d.ld_x, r.row_bytes, bars + s);
-    if (r.i_y >= 0) bulk_load(stage + r.i_y * r.row_bytes, static_cast<const T *>(a.y) + row * a.d.ld_y, r.row_bytes, bars + s);
-    if (r.i_dxo >= 0) bulk_load(stage + r.i_dxo * r.row_bytes, static_cast<const T *>(a.dx_out) + row * a.d.ld_x, r.row_bytes, bars + s);
-    if (r.i_dh >= 0) bulk_load(stage + r.i_dh * r.row_bytes, static_cast<const T *>(a.dh) + row * a.d.ld_h, r.row_bytes, bars + s);
-    if (r.i_gate >= 0) bulk_load(stage + r.i_gate * r.row_bytes, static_cast<const T *>(a.gate) + (row / a.d.group_rows) * a.d.ld_gate, r.row_bytes, bars + s);
+    const uintptr_t low = from & ~uintptr_t(15), end = from + bytes, high = (end + 15) & ~uintptr_t(15);
+    Units u{low, high};
+    if (first && low < from) {
+        for (uintptr_t p = from; p < end && p < low + 16; ++p) slot[p - low] = *reinterpret_cast<const uint8_t *>(p);
+        u.b0 = low + 16;
+    }
+    if (last && end < high && u.b1 > u.b0) {
+        for (uintptr_t p = high - 16 < from ? from : high - 16; p < end; ++p) slot[p - low] = *reinterpret_cast<const uint8_t *>(p);
+        u.b1 = high - 16;
+    }
+    return u;
 }
 
-template <typename T, int VP> __device__ __forceinline__ void stage_cols(const uint8_t *tensor, int c, f2 (&v)[VP])
+// The copies of row `row` into stage `s`, by one thread.
+template <typename T, bool VEC> __device__ __forceinline__ void ring_issue(const NormArgs &a, const Ring &r, uint8_t *smem, uint64_t *bars, int s, int64_t row)
 {
-    unpack16<T>(*reinterpret_cast<const uint4 *>(tensor + size_t(c) * sizeof(T)), v);
+    uint8_t *stage = smem + size_t(s) * r.tensors * r.slot_bytes;
+    const int64_t gate_row = r.i_gate >= 0 ? row / a.d.group_rows : 0;
+    const auto from = [&](int which) {
+        return which == 0 ? static_cast<const T *>(a.x) + row * a.d.ld_x : which == 1 ? static_cast<const T *>(a.y) + row * a.d.ld_y
+            : which == 2 ? static_cast<const T *>(a.dx_out) + row * a.d.ld_x : which == 3 ? static_cast<const T *>(a.dh) + row * a.d.ld_h
+            : static_cast<const T *>(a.gate) + gate_row * a.d.ld_gate;
+    };
+    const int place[5] = {r.i_x, r.i_y, r.i_dxo, r.i_dh, r.i_gate};
+    if constexpr (VEC) {
+        bar_expect(bars + s, r.slot_bytes * r.tensors);
+#pragma unroll
+        for (int t = 0; t < 5; ++t)
+            if (place[t] >= 0) bulk_load(stage + place[t] * r.slot_bytes, from(t), r.slot_bytes, bars + s);
+    } else {
+        const uint32_t bytes = a.d.cols * uint32_t(sizeof(T));
+        Units u[5];
+        uint32_t total = 0;
+        bool by_hand = false;
+#pragma unroll
+        for (int t = 0; t < 5; ++t) {
+            u[t] = Units{0, 0};
+            if (place[t] < 0) continue;
+            const bool first = t < 4 ? row == 0 : gate_row == 0, last = t < 4 ? row == a.d.rows - 1 : (gate_row + 1) * a.d.group_rows >= a.d.rows;
+            u[t] = row_units(reinterpret_cast<uintptr_t>(from(t)), bytes, first, last, stage + place[t] * r.slot_bytes);
+            total += uint32_t(u[t].b1 - u[t].b0);
+            by_hand |= first || last;
+        }
+        if (by_hand) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // a later copy comes behind these stores
+        bar_expect(bars + s, total);
+#pragma unroll
+        for (int t = 0; t < 5; ++t)
+            if (u[t].b1 > u[t].b0)
+                bulk_load(stage + place[t] * r.slot_bytes + (u[t].b0 - (reinterpret_cast<uintptr_t>(from(t)) & ~uintptr_t(15))), reinterpret_cast<const void *>(u[t].b0),
+                          uint32_t(u[t].b1 - u[t].b0), bars + s);
+    }
+}
+
+// the row of a tensor in a stage: where its unit begins, or its place in it
+template <typename T, bool VEC> __device__ __forceinline__ const T *stage_row(const uint8_t *stage, const Ring &r, int place, const void *base, int64_t row, int64_t ld)
+{
+    const uint32_t shift = VEC ? 0u : (uint32_t(reinterpret_cast<uintptr_t>(base)) + uint32_t(row) * uint32_t(ld) * uint32_t(sizeof(T))) & 15u;
+    return reinterpret_cast<const T *>(stage + place * r.slot_bytes + shift);
 }
 
 template <int VP> __device__ __forceinline__ void zero_cols(f2 (&v)[VP])
@@ -460,46 +395,52 @@ template <int VP> __device__ __forceinline__ void zero_cols(f2 (&v)[VP])
 }
 
 // k = alpha g W_after of this thread's columns for the gate row at `gate` (NULL: g = 1)
-template <typename T, typename W, int VE, int NV>
-__device__ __forceinline__ void group_factors(const NormArgs &a, const T *gate, int tpr, float o, f2 (&k)[NV][VE / 2])
+template <typename T, typename W, bool VEC, int NV>
+__device__ __forceinline__ void group_factors(const NormArgs &a, const T *gate, int tpr, float o, f2 (&k)[NV][Cols<T, VEC>::VP])
 {
+    using C = Cols<T, VEC>;
     const bool th = a.d.flags & RUBICK_NORM_TANH_GATE;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * tpr + int(threadIdx.x)) * VE;
-        float w[VE], g[VE];
+        const int c = C::first(i, tpr);
+        float w[C::VE];
+        f2 g[C::VP];
 #pragma unroll
-        for (int e = 0; e < VE; ++e) { w[e] = 1.f - o; g[e] = 1.f; }
+        for (int e = 0; e < C::VE; ++e) { w[e] = 1.f - o; g[e / 2] = both(1.f); }
         if (c < a.d.cols) {
-            if (a.w_after) load_shared_cols<W, VE>(static_cast<const W *>(a.w_after), c, a.d.cols, w, 0.f);
-            if (gate) unpack16<T>(*reinterpret_cast<const uint4 *>(gate + c), g);
+            if (a.w_after) C::weights(static_cast<const W *>(a.w_after), c, tpr, a.d.cols, w);
+            if (gate) C::load(gate, c, tpr, a.d.cols, g);
         }
 #pragma unroll
-        for (int e = 0; e < VE; e += 2)
-            k[i][e / 2] = pair(a.d.alpha * (th ? tanhf(g[e]) : g[e]) * (w[e] + o), a.d.alpha * (th ? tanhf(g[e + 1]) : g[e + 1]) * (w[e + 1] + o));
+        for (int e = 0; e < C::VP; ++e) {
+            const float g0 = th ? tanhf(lo(g[e])) : lo(g[e]), g1 = th ? tanhf(hi(g[e])) : hi(g[e]);
+            k[i][e] = pair(a.d.alpha * g0 * (w[2 * e] + o), a.d.alpha * g1 * (w[2 * e + 1] + o));
+        }
     }
 }
 
 // W_before of this thread's columns
-template <typename W, int VE, int NV> __device__ __forceinline__ void before_factors(const NormArgs &a, int tpr, float o, f2 (&wb)[NV][VE / 2])
+template <typename T, typename W, bool VEC, int NV> __device__ __forceinline__ void before_factors(const NormArgs &a, int tpr, float o, f2 (&wb)[NV][Cols<T, VEC>::VP])
 {
+    using C = Cols<T, VEC>;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * tpr + int(threadIdx.x)) * VE;
-        float w[VE];
+        const int c = C::first(i, tpr);
+        float w[C::VE];
 #pragma unroll
-        for (int e = 0; e < VE; ++e) w[e] = 1.f - o;
-        if (a.w_before && c < a.d.cols) load_shared_cols<W, VE>(static_cast<const W *>(a.w_before), c, a.d.cols, w, 0.f);
+        for (int e = 0; e < C::VE; ++e) w[e] = 1.f - o;
+        if (a.w_before && c < a.d.cols) C::weights(static_cast<const W *>(a.w_before), c, tpr, a.d.cols, w);
 #pragma unroll
-        for (int e = 0; e < VE; e += 2) wb[i][e / 2] = pair(w[e] + o, w[e + 1] + o);
+        for (int e = 0; e < C::VP; ++e) wb[i][e] = pair(w[2 * e] + o, w[2 * e + 1] + o);
     }
 }
 
 // FULL: both norms and a block between them, known when the kernel is compiled; 96 registers: 640 threads an SM
-template <typename T, typename W, int NV, bool FULL>
+template <typename T, typename W, int NV, bool FULL, bool VEC>
 __global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ Ring r)
 {
-    constexpr int VE = Lanes<T>::N, VP = VE / 2;
+    using C = Cols<T, VEC>;
+    constexpr int VP = C::VP;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(16) float red[4][16];                  // one row's sums may still be read when the next row's are written
     __shared__ __align__(8) uint64_t bars[RING_MOST];
@@ -509,7 +450,7 @@ __global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __
     if (threadIdx.x == 0) {
         for (int s = 0; s < r.stages; ++s) bar_init(bars + s);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T>(a, r, smem, bars, s, begin + s);
+        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T, VEC>(a, r, smem, bars, s, begin + s);
     }
     if (threadIdx.x < 32) {                       // the 64 words by one warp: the smallest block has no more
         (&red[0][0])[threadIdx.x] = 0.f;
@@ -518,7 +459,7 @@ __global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __
     const bool block = FULL || a.y, after = FULL || (a.d.flags & RUBICK_NORM_AFTER), before = FULL || (a.d.flags & RUBICK_NORM_BEFORE);
     const float o = a.d.flags & RUBICK_NORM_UNIT_OFFSET ? 1.f : 0.f, inv_cols = 1.f / float(cols);
     f2 wb[NV][VP], k[NV][VP];
-    before_factors<W, VE, NV>(a, tpr, o, wb);
+    before_factors<T, W, VEC, NV>(a, tpr, o, wb);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -531,23 +472,24 @@ __global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __
     uint32_t parity = 0;
     for (int i_row = 0; i_row < n; ++i_row) {
         const int64_t row = begin + i_row;
-        const uint8_t *stage = smem + size_t(s) * r.tensors * r.row_bytes;
+        const uint8_t *stage = smem + size_t(s) * r.tensors * r.slot_bytes;
         if (!lost && !bar_wait(bars + s, parity)) { lost = true; atomicOr(a.status, DS_COPY_LOST); }
+        const T *x_row = stage_row<T, VEC>(stage, r, r.i_x, a.x, row, a.d.ld_x), *y_row = stage_row<T, VEC>(stage, r, r.i_y, a.y, row, a.d.ld_y);
         if (block && row >= group_end) {
             const int64_t group = row / a.d.group_rows;
             group_end = (group + 1) * a.d.group_rows;
-            const T *gate = !a.gate ? nullptr : r.i_gate >= 0 ? reinterpret_cast<const T *>(stage + r.i_gate * r.row_bytes)
+            const T *gate = !a.gate ? nullptr : r.i_gate >= 0 ? stage_row<T, VEC>(stage, r, r.i_gate, a.gate, row / a.d.group_rows, a.d.ld_gate)
                                                               : static_cast<const T *>(a.gate) + group * a.d.ld_gate;
-            group_factors<T, W, VE, NV>(a, gate, tpr, o, k);
+            group_factors<T, W, VEC, NV>(a, gate, tpr, o, k);
         }
         f2 v[NV][VP], y[NV][VP], part[1] = {0ull};
         float sum[1], ra = 0.f, rb = 0.f, scale = 1.f;
         if (after) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (i * tpr + int(threadIdx.x)) * VE;
+                const int c = C::first(i, tpr);
                 if (c < cols) {
-                    stage_cols<T, VP>(stage + r.i_y * r.row_bytes, c, y[i]);
+                    C::load(y_row, c, tpr, cols, y[i]);
 #pragma unroll
                     for (int e = 0; e < VP; ++e) part[0] = fma2(y[i][e], y[i][e], part[0]);
                 }
@@ -557,18 +499,18 @@ __global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __
         } else row_barrier(warps);
         // every thread has left the stage of the row before
         if (threadIdx.x == 0 && i_row >= 1 && i_row - 1 + r.stages < n)
-            ring_issue<T>(a, r, smem, bars, s ? s - 1 : r.stages - 1, row - 1 + r.stages);
+            ring_issue<T, VEC>(a, r, smem, bars, s ? s - 1 : r.stages - 1, row - 1 + r.stages);
         part[0] = 0ull;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * tpr + int(threadIdx.x)) * VE;
+            const int c = C::first(i, tpr);
             if (c < cols) {
-                stage_cols<T, VP>(stage + r.i_x * r.row_bytes, c, v[i]);
+                C::load(x_row, c, tpr, cols, v[i]);
                 if (block) {
-                    if (!after) stage_cols<T, VP>(stage + r.i_y * r.row_bytes, c, y[i]);
+                    if (!after) C::load(y_row, c, tpr, cols, y[i]);
 #pragma unroll
                     for (int e = 0; e < VP; ++e) v[i][e] = fma2(mul2(k[i][e], both(scale)), y[i][e], v[i][e]);
-                    st_stream(x_out + c, pack16<T>(v[i]));
+                    C::store(x_out, c, tpr, cols, v[i]);
                 }
 #pragma unroll
                 for (int e = 0; e < VP; ++e) part[0] = fma2(v[i][e], v[i][e], part[0]);
@@ -579,11 +521,11 @@ __global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __
             rb = rsqrtf(sum[0] * inv_cols + a.d.eps);
 #pragma unroll
             for (int i = 0; i < NV; ++i) {
-                const int c = (i * tpr + int(threadIdx.x)) * VE;
+                const int c = C::first(i, tpr);
                 if (c < cols) {
 #pragma unroll
                     for (int e = 0; e < VP; ++e) v[i][e] = mul2(mul2(v[i][e], both(rb)), wb[i][e]);
-                    st_stream(h + c, pack16<T>(v[i]));
+                    C::store(h, c, tpr, cols, v[i]);
                 }
             }
         }
@@ -595,47 +537,44 @@ __global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __
 }
 
 // the gradients of a gate group whose rows this chunk has summed up in t
-template <typename T, typename W, int VE, int NV>
+template <typename T, typename W, bool VEC, int NV>
 __device__ __forceinline__ void ring_flush(const NormArgs &a, int chunk, int64_t begin, int64_t stop, int64_t group, const T *gate, int tpr, float o,
-                                           f2 (&t)[NV][VE / 2], f2 (&acc_a)[NV][VE / 2])
+                                           f2 (&t)[NV][Cols<T, VEC>::VP], f2 (&acc_a)[NV][Cols<T, VEC>::VP])
 {
+    using C = Cols<T, VEC>;
     const int64_t g0 = group * a.d.group_rows;
     const int64_t g1 = g0 + a.d.group_rows < a.d.rows ? g0 + a.d.group_rows : a.d.rows;
     const bool whole = g0 >= begin && g1 <= stop, th = a.d.flags & RUBICK_NORM_TANH_GATE;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * tpr + int(threadIdx.x)) * VE;
+        const int c = C::first(i, tpr);
         if (c >= a.d.cols) continue;
-        float w[VE], g[VE], d[VE];
+        float w[C::VE];
+        f2 g[C::VP], d[C::VP];
 #pragma unroll
-        for (int e = 0; e < VE; ++e) { w[e] = 1.f - o; g[e] = 1.f; }
-        if (a.w_after) load_shared_cols<W, VE>(static_cast<const W *>(a.w_after), c, a.d.cols, w, 0.f);
-        if (gate) unpack16<T>(*reinterpret_cast<const uint4 *>(gate + c), g);
+        for (int e = 0; e < C::VE; ++e) { w[e] = 1.f - o; g[e / 2] = both(1.f); }
+        if (a.w_after) C::weights(static_cast<const W *>(a.w_after), c, tpr, a.d.cols, w);
+        if (gate) C::load(gate, c, tpr, a.d.cols, g);
 #pragma unroll
-        for (int e = 0; e < VE; e += 2) {
-            float slope0 = 1.f, slope1 = 1.f;
-            if (th) { g[e] = tanh_slope(g[e], slope0); g[e + 1] = tanh_slope(g[e + 1], slope1); }
-            const f2 at = mul2(both(a.d.alpha), t[i][e / 2]);
-            acc_a[i][e / 2] = fma2(pair(g[e], g[e + 1]), at, acc_a[i][e / 2]);
-            d[e] = lo(at) * (w[e] + o) * slope0;
-            d[e + 1] = hi(at) * (w[e + 1] + o) * slope1;
-            t[i][e / 2] = 0ull;
+        for (int e = 0; e < C::VP; ++e) {
+            float s0 = 1.f, s1 = 1.f, g0f = lo(g[e]), g1f = hi(g[e]);
+            if (th) { g0f = tanh_slope(g0f, s0); g1f = tanh_slope(g1f, s1); }
+            const f2 at = mul2(both(a.d.alpha), t[i][e]);
+            acc_a[i][e] = fma2(pair(g0f, g1f), at, acc_a[i][e]);
+            d[e] = mul2(at, pair((w[2 * e] + o) * s0, (w[2 * e + 1] + o) * s1));
+            t[i][e] = 0ull;
         }
         if (!a.dgate) continue;
-        if (whole) {
-            st_stream(static_cast<T *>(a.dgate) + group * a.d.ld_gate + c, pack16<T>(d));
-        } else {
-            float *p = part_row(a, g0 < begin ? 2 : 3, chunk) + c;
-#pragma unroll
-            for (int e = 0; e < VE; e += 4) *reinterpret_cast<float4 *>(p + e) = make_float4(d[e], d[e + 1], d[e + 2], d[e + 3]);
-        }
+        if (whole) C::store(static_cast<T *>(a.dgate) + group * a.d.ld_gate, c, tpr, a.d.cols, d);
+        else C::put(part_row(a, g0 < begin ? 2 : 3, chunk), c, tpr, a.d.cols, d);
     }
 }
 
-template <typename T, typename W, int NV, bool FULL>
+template <typename T, typename W, int NV, bool FULL, bool VEC>
 __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_constant__ NormArgs a, const __grid_constant__ Ring r)
 {
-    constexpr int VE = Lanes<T>::N, VP = VE / 2;
+    using C = Cols<T, VEC>;
+    constexpr int VP = C::VP;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(16) float red[2][3 * 16];
     __shared__ __align__(8) uint64_t bars[RING_MOST];
@@ -645,7 +584,7 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
     if (threadIdx.x == 0) {
         for (int s = 0; s < r.stages; ++s) bar_init(bars + s);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T>(a, r, smem, bars, s, begin + s);
+        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T, VEC>(a, r, smem, bars, s, begin + s);
     }
     if (threadIdx.x < 32) {
 #pragma unroll
@@ -655,7 +594,7 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
     const bool stream = FULL || a.dx_out, need_y = FULL || r.i_y >= 0;
     const float o = a.d.flags & RUBICK_NORM_UNIT_OFFSET ? 1.f : 0.f, inv_cols = 1.f / float(cols);
     f2 wb[NV][VP], k[NV][VP], t[NV][VP], acc_a[NV][VP], acc_b[NV][VP];
-    before_factors<W, VE, NV>(a, tpr, o, wb);
+    before_factors<T, W, VEC, NV>(a, tpr, o, wb);
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
@@ -671,30 +610,32 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
     uint32_t parity = 0;
     for (int i_row = 0; i_row < n; ++i_row) {
         const int64_t row = begin + i_row;
-        const uint8_t *stage = smem + size_t(s) * r.tensors * r.row_bytes;
+        const uint8_t *stage = smem + size_t(s) * r.tensors * r.slot_bytes;
         const float ra = after ? next.x : 1.f, rb = before ? next.y : 0.f;
         if (a.rstd_in && i_row + 1 < n) next = *reinterpret_cast<const float2 *>(a.rstd_in + 2 * row + 2);
         if (!lost && !bar_wait(bars + s, parity)) { lost = true; atomicOr(a.status, DS_COPY_LOST); }
+        const T *x_row = stage_row<T, VEC>(stage, r, r.i_x, a.x, row, a.d.ld_x), *y_row = stage_row<T, VEC>(stage, r, r.i_y, a.y, row, a.d.ld_y);
+        const T *d_row = stage_row<T, VEC>(stage, r, r.i_dxo, a.dx_out, row, a.d.ld_x), *h_row = stage_row<T, VEC>(stage, r, r.i_dh, a.dh, row, a.d.ld_h);
         if (block && row >= group_end) {
             // the stage of the row before, where its gate row may lie, is still untouched
-            if (group >= 0) ring_flush<T, W, VE, NV>(a, chunk, begin, begin + n, group, gate, tpr, o, t, acc_a);
+            if (group >= 0) ring_flush<T, W, VEC, NV>(a, chunk, begin, begin + n, group, gate, tpr, o, t, acc_a);
             group = row / a.d.group_rows;
             group_end = (group + 1) * a.d.group_rows;
             gate = a.gate ? static_cast<const T *>(a.gate) + group * a.d.ld_gate : nullptr;
-            group_factors<T, W, VE, NV>(a, r.i_gate >= 0 ? reinterpret_cast<const T *>(stage + r.i_gate * r.row_bytes) : gate, tpr, o, k);
+            group_factors<T, W, VEC, NV>(a, r.i_gate >= 0 ? stage_row<T, VEC>(stage, r, r.i_gate, a.gate, row / a.d.group_rows, a.d.ld_gate) : gate, tpr, o, k);
         }
-        if (r.i_gate >= 0) gate = reinterpret_cast<const T *>(stage + r.i_gate * r.row_bytes);
+        if (r.i_gate >= 0) gate = stage_row<T, VEC>(stage, r, r.i_gate, a.gate, row / a.d.group_rows, a.d.ld_gate);
         f2 part[3] = {0ull, 0ull, 0ull};
         const f2 rb2 = both(rb);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * tpr + int(threadIdx.x)) * VE;
+            const int c = C::first(i, tpr);
             if (c < cols) {
                 f2 d[VP], x[VP], h[VP], y[VP];
-                if (stream) stage_cols<T, VP>(stage + r.i_dxo * r.row_bytes, c, d); else zero_cols(d);
-                if (before) stage_cols<T, VP>(stage + r.i_x * r.row_bytes, c, x); else zero_cols(x);
-                if (before) stage_cols<T, VP>(stage + r.i_dh * r.row_bytes, c, h); else zero_cols(h);
-                if (need_y) stage_cols<T, VP>(stage + r.i_y * r.row_bytes, c, y); else zero_cols(y);
+                if (stream) C::load(d_row, c, tpr, cols, d); else zero_cols(d);
+                if (before) C::load(x_row, c, tpr, cols, x); else zero_cols(x);
+                if (before) C::load(h_row, c, tpr, cols, h); else zero_cols(h);
+                if (need_y) C::load(y_row, c, tpr, cols, y); else zero_cols(y);
 #pragma unroll
                 for (int e = 0; e < VP; ++e) {
                     // the sums without the row's factors ra and rb, which come in behind the reduction
@@ -709,18 +650,18 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
         float sum[3];
         ring_sum<3>(part, sum, red[i_row & 1], warps);
         if (threadIdx.x == 0 && i_row >= 1 && i_row - 1 + r.stages < n)
-            ring_issue<T>(a, r, smem, bars, s ? s - 1 : r.stages - 1, row - 1 + r.stages);
+            ring_issue<T, VEC>(a, r, smem, bars, s ? s - 1 : r.stages - 1, row - 1 + r.stages);
         const float m1 = rb * sum[0] * inv_cols, m2 = after ? ra * (sum[1] - rb * rb * m1 * sum[2]) * inv_cols : 0.f;
         const f2 f1 = both(-rb * rb * m1), f2y = both(-ra * ra * m2), ra2 = both(ra);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = (i * tpr + int(threadIdx.x)) * VE;
+            const int c = C::first(i, tpr);
             if (c < cols) {
                 f2 d[VP], x[VP], h[VP], y[VP];
-                if (stream) stage_cols<T, VP>(stage + r.i_dxo * r.row_bytes, c, d); else zero_cols(d);
-                if (before) stage_cols<T, VP>(stage + r.i_x * r.row_bytes, c, x); else zero_cols(x);
-                if (before) stage_cols<T, VP>(stage + r.i_dh * r.row_bytes, c, h); else zero_cols(h);
-                if (need_y) stage_cols<T, VP>(stage + r.i_y * r.row_bytes, c, y); else zero_cols(y);
+                if (stream) C::load(d_row, c, tpr, cols, d); else zero_cols(d);
+                if (before) C::load(x_row, c, tpr, cols, x); else zero_cols(x);
+                if (before) C::load(h_row, c, tpr, cols, h); else zero_cols(h);
+                if (need_y) C::load(y_row, c, tpr, cols, y); else zero_cols(y);
 #pragma unroll
                 for (int e = 0; e < VP; ++e) {
                     d[e] = fma2(f1, x[e], fma2(rb2, mul2(h[e], wb[i][e]), d[e]));           // G
@@ -728,24 +669,21 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
                     t[i][e] = fma2(rg, y[e], t[i][e]);
                     y[e] = fma2(f2y, y[e], mul2(k[i][e], rg));
                 }
-                st_stream(dx + c, pack16<T>(d));
-                if (block) st_stream(dy + c, pack16<T>(y));
+                C::store(dx, c, tpr, cols, d);
+                if (block) C::store(dy, c, tpr, cols, y);
             }
         }
         dx += a.d.ld_x;
         dy += a.d.ld_y;
         if (++s == r.stages) { s = 0; parity ^= 1u; }
     }
-    if (group >= 0) ring_flush<T, W, VE, NV>(a, chunk, begin, begin + n, group, gate, tpr, o, t, acc_a);
+    if (group >= 0) ring_flush<T, W, VEC, NV>(a, chunk, begin, begin + n, group, gate, tpr, o, t, acc_a);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = (i * tpr + int(threadIdx.x)) * VE;
+        const int c = C::first(i, tpr);
         if (c >= cols) continue;
-#pragma unroll
-        for (int e = 0; e < VP; e += 2) {
-            if (a.dw_after) *reinterpret_cast<ulonglong2 *>(part_row(a, 0, chunk) + c + 2 * e) = make_ulonglong2(acc_a[i][e], acc_a[i][e + 1]);
-            if (a.dw_before) *reinterpret_cast<ulonglong2 *>(part_row(a, 1, chunk) + c + 2 * e) = make_ulonglong2(acc_b[i][e], acc_b[i][e + 1]);
-        }
+        if (a.dw_after) C::put(part_row(a, 0, chunk), c, tpr, cols, acc_a[i]);
+        if (a.dw_before) C::put(part_row(a, 1, chunk), c, tpr, cols, acc_b[i]);
     }
 }
 
@@ -791,7 +729,7 @@ __global__ void __launch_bounds__(512) norm_backward_join_kernel(const __grid_co
 }
 
 // Threads and vectors of a row: VE elements a vector, NV vectors a thread; for the ring its stages and blocks per SM.
-struct Shape { int ve, nv, tpr, slots; bool wide, ring; int blocks, smem; Ring r; };
+struct Shape { int ve, nv, tpr, slots; bool ring, ring_vec; int blocks, smem; Ring r; };
 
 int esize_of(int dtype) { return dtype == RUBICK_F32 ? 4 : 2; }
 
@@ -812,8 +750,8 @@ int ring_budget(int n) { return 228 * 1024 / n - 1792; }
 bool ring_shape(const NormArgs &a, bool back, Shape &s)
 {
     const int es = esize_of(a.d.dtype);
-    if (s.ve == 1 || a.d.cols % s.ve) return false;
-    const int nvec = a.d.cols / s.ve, most = 16 / s.ve, warps = (nvec + most * 32 - 1) / (most * 32);
+    const bool vec = s.ve > 1 && a.d.cols % s.ve == 0;
+    const int unit = vec ? s.ve : 2, units = (a.d.cols + unit - 1) / unit, most = 16 / unit, warps = (units + most * 32 - 1) / (most * 32);
     if (warps > 16) return false;
     Ring &r = s.r;
     const bool before = a.d.flags & RUBICK_NORM_BEFORE, after = a.d.flags & RUBICK_NORM_AFTER;
@@ -826,20 +764,21 @@ bool ring_shape(const NormArgs &a, bool back, Shape &s)
     r.i_gate = a.gate && a.d.group_rows < 8 ? n++ : -1;
     if (n == 0) return false;
     r.tensors = n;
-    r.row_bytes = uint32_t(a.d.cols * es);
+    r.slot_bytes = vec ? uint32_t(a.d.cols * es) : uint32_t((a.d.cols * es + 15) / 16 + 1) * 16;
     s.tpr = warps * 32;
-    s.nv = (nvec + s.tpr - 1) / s.tpr;
+    s.nv = vec ? (units + s.tpr - 1) / s.tpr : 8;
     s.slots = 1;
-    // 128 registers a thread backward, up to 102 forward (40 to 64 with one vector a thread)
+    // 128 registers a thread backward, 96 forward (64 with one vector a thread)
     s.blocks = (back ? 512 : s.nv == 1 ? 1024 : 640) / s.tpr;
     if (s.blocks > 16) s.blocks = 16;
     for (;; --s.blocks) {
         if (s.blocks == 0) return false;
-        r.stages = ring_budget(s.blocks) / (n * int(r.row_bytes));
+        r.stages = ring_budget(s.blocks) / (n * int(r.slot_bytes));
         if (r.stages >= 3 || (s.blocks == 1 && r.stages == 2)) break;
     }
     if (r.stages > RING_MOST) r.stages = RING_MOST;
-    s.smem = r.stages * n * int(r.row_bytes);
+    s.smem = r.stages * n * int(r.slot_bytes);
+    s.ring_vec = vec;
     return true;
 }
 
@@ -853,7 +792,6 @@ Shape forward_shape(const NormArgs &a, int num_sms)
 {
     Shape s;
     const int es = esize_of(a.d.dtype);
-    s.wide = false;
     s.ve = vectors_fit(a, es) ? 16 / es : 1;
     s.ring = ring_shape(a, false, s) && a.d.rows >= int64_t(num_sms) * s.blocks * 4;
     if (s.ring) return s;
@@ -873,16 +811,8 @@ Shape backward_shape(const NormArgs &a)
     Shape s;
     const int es = esize_of(a.d.dtype);
     s.ve = vectors_fit(a, es) ? 16 / es : 1;
-    s.wide = false;
     s.ring = ring_shape(a, true, s);
-    if (s.ring) return s;
-    const int most = 16 / s.ve, nvec = (a.d.cols + s.ve - 1) / s.ve;   // 16 columns a thread
-    const int warps = (nvec + most * 32 - 1) / (most * 32);
-    s.wide = warps > 16;
-    s.tpr = s.wide ? 512 : warps * 32;
-    s.nv = (nvec + s.tpr - 1) / s.tpr;
-    s.slots = s.wide || s.tpr >= 128 ? 1 : 128 / s.tpr;
-    s.blocks = s.wide ? 1 : 512 / (s.tpr * s.slots) > 0 ? 512 / (s.tpr * s.slots) : 1;
+    if (!s.ring) { s.tpr = 512; s.blocks = 1; }
     return s;
 }
 
@@ -895,25 +825,25 @@ template <typename K> cudaError_t launch_ring(K kernel, const NormArgs &a, const
     return cudaGetLastError();
 }
 
-template <typename T, typename W, int VE, bool FULL> cudaError_t forward_ring(const NormArgs &a, const Shape &s, cudaStream_t st)
+template <typename T, typename W, bool FULL> cudaError_t forward_ring(const NormArgs &a, const Shape &s, cudaStream_t st)
 {
-    if (s.nv <= 1) return launch_ring(norm_forward_ring_kernel<T, W, 1, FULL>, a, s, st);
-    if (VE == 8 || s.nv <= 2) return launch_ring(norm_forward_ring_kernel<T, W, 2, FULL>, a, s, st);
-    return launch_ring(norm_forward_ring_kernel<T, W, VE == 4 ? 4 : 2, FULL>, a, s, st);
+    constexpr int MOST = 16 / Lanes<T>::N;
+    if (!s.ring_vec) return launch_ring(norm_forward_ring_kernel<T, W, 8, FULL, false>, a, s, st);
+    if (s.nv <= 1) return launch_ring(norm_forward_ring_kernel<T, W, 1, FULL, true>, a, s, st);
+    if (s.nv <= 2) return launch_ring(norm_forward_ring_kernel<T, W, 2, FULL, true>, a, s, st);
+    return launch_ring(norm_forward_ring_kernel<T, W, MOST, FULL, true>, a, s, st);
 }
-template <typename T, typename W, int VE, bool FULL> cudaError_t backward_ring(const NormArgs &a, const Shape &s, cudaStream_t st)
+template <typename T, typename W, bool FULL> cudaError_t backward_ring(const NormArgs &a, const Shape &s, cudaStream_t st)
 {
-    if (s.nv <= 1) return launch_ring(norm_backward_ring_kernel<T, W, 1, FULL>, a, s, st);
-    if (VE == 8 || s.nv <= 2) return launch_ring(norm_backward_ring_kernel<T, W, 2, FULL>, a, s, st);
-    return launch_ring(norm_backward_ring_kernel<T, W, VE == 4 ? 4 : 2, FULL>, a, s, st);
+    constexpr int MOST = 16 / Lanes<T>::N;
+    if (!s.ring_vec) return launch_ring(norm_backward_ring_kernel<T, W, 8, FULL, false>, a, s, st);
+    if (s.nv <= 1) return launch_ring(norm_backward_ring_kernel<T, W, 1, FULL, true>, a, s, st);
+    if (s.nv <= 2) return launch_ring(norm_backward_ring_kernel<T, W, 2, FULL, true>, a, s, st);
+    return launch_ring(norm_backward_ring_kernel<T, W, MOST, FULL, true>, a, s, st);
 }
 
 template <typename T, typename W, int VE> cudaError_t forward_nv(const NormArgs &a, const Shape &s, cudaStream_t st)
 {
-    if constexpr (VE > 1) {
-        const bool full = a.y && (a.d.flags & RUBICK_NORM_AFTER) && (a.d.flags & RUBICK_NORM_BEFORE);
-        if (s.ring) return full ? forward_ring<T, W, VE, true>(a, s, st) : forward_ring<T, W, VE, false>(a, s, st);
-    }
     const dim3 block(s.tpr, s.slots);
     const unsigned grid = unsigned((a.d.rows + s.slots - 1) / s.slots);
     if constexpr (VE > 1) {
@@ -931,37 +861,30 @@ template <typename T, typename W, int VE> cudaError_t forward_nv(const NormArgs 
     return cudaGetLastError();
 }
 
-template <typename T, typename W, int VE> cudaError_t backward_nv(const NormArgs &a, const Shape &s, cudaStream_t st)
+template <typename T, typename W> cudaError_t forward_any(const NormArgs &a, const Shape &s, cudaStream_t st)
 {
-    const dim3 block(s.tpr, s.slots);
-    const unsigned grid = unsigned((a.n_chunks + s.slots - 1) / s.slots);
-    bool ring = false;
-    if constexpr (VE > 1) {
-        if (s.ring) {
-            ring = true;
-            const bool full = a.y && (a.d.flags & RUBICK_NORM_AFTER) && (a.d.flags & RUBICK_NORM_BEFORE) && a.dx_out;
-            const cudaError_t e = full ? backward_ring<T, W, VE, true>(a, s, st) : backward_ring<T, W, VE, false>(a, s, st);
-            if (e != cudaSuccess) return e;
-        }
+    if (s.ring) {
+        const bool full = a.y && (a.d.flags & RUBICK_NORM_AFTER) && (a.d.flags & RUBICK_NORM_BEFORE);
+        return full ? forward_ring<T, W, true>(a, s, st) : forward_ring<T, W, false>(a, s, st);
     }
-    if (ring) {
-    } else if (s.wide) {
-        const int smem = 3 * a.d.cols * int(sizeof(float));
-        const cudaError_t e = cudaFuncSetAttribute(norm_backward_wide_kernel<T, W, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
-        norm_backward_wide_kernel<T, W, VE><<<grid, block, smem, st>>>(a);
-    } else if constexpr (VE == 8) {
-        if (s.nv <= 1) norm_backward_kernel<T, W, VE, 1><<<grid, block, 0, st>>>(a);
-        else norm_backward_kernel<T, W, VE, 2><<<grid, block, 0, st>>>(a);
-    } else if constexpr (VE == 4) {
-        if (s.nv <= 2) norm_backward_kernel<T, W, VE, 2><<<grid, block, 0, st>>>(a);
-        else norm_backward_kernel<T, W, VE, 4><<<grid, block, 0, st>>>(a);
-    } else {
-        if (s.nv <= 4) norm_backward_kernel<T, W, VE, 4><<<grid, block, 0, st>>>(a);
-        else norm_backward_kernel<T, W, VE, 16><<<grid, block, 0, st>>>(a);
-    }
-    if (!ring) count_launch();
-    cudaError_t e = cudaGetLastError();
+    return s.ve > 1 ? forward_nv<T, W, Lanes<T>::N>(a, s, st) : forward_nv<T, W, 1>(a, s, st);
+}
+
+template <typename T, typename W, int VE> cudaError_t backward_wide(const NormArgs &a, const Shape &s, cudaStream_t st)
+{
+    const int smem = 3 * a.d.cols * int(sizeof(float));
+    const cudaError_t e = cudaFuncSetAttribute(norm_backward_wide_kernel<T, W, VE>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    norm_backward_wide_kernel<T, W, VE><<<unsigned(a.n_chunks), s.tpr, smem, st>>>(a);
+    count_launch();
+    return cudaGetLastError();
+}
+
+template <typename T, typename W> cudaError_t backward_any(const NormArgs &a, const Shape &s, cudaStream_t st)
+{
+    const bool full = a.y && (a.d.flags & RUBICK_NORM_AFTER) && (a.d.flags & RUBICK_NORM_BEFORE) && a.dx_out;
+    const cudaError_t e = s.ring ? (full ? backward_ring<T, W, true>(a, s, st) : backward_ring<T, W, false>(a, s, st))
+                                 : s.ve > 1 ? backward_wide<T, W, Lanes<T>::N>(a, s, st) : backward_wide<T, W, 1>(a, s, st);
     if (e != cudaSuccess) return e;
     const int64_t groups = (a.d.rows + a.d.group_rows - 1) / a.d.group_rows;
     const bool split = a.gate && a.dgate && a.chunk_rows % a.d.group_rows != 0;
@@ -972,30 +895,11 @@ template <typename T, typename W, int VE> cudaError_t backward_nv(const NormArgs
     return cudaGetLastError();
 }
 
-// calls f.template operator()<T, W, VE>() for the element type, the weights' type and the vector width at hand
-template <typename F> cudaError_t by_type(const NormArgs &a, int ve, F f)
-{
-    const bool wide_w = a.d.wtype == RUBICK_F32;
-    switch (a.d.dtype) {
-    case RUBICK_BF16:
-        if (wide_w) return ve > 1 ? f.template operator()<bf16, float, 8>() : f.template operator()<bf16, float, 1>();
-        return ve > 1 ? f.template operator()<bf16, bf16, 8>() : f.template operator()<bf16, bf16, 1>();
-    case RUBICK_F16:
-        if (wide_w) return ve > 1 ? f.template operator()<f16, float, 8>() : f.template operator()<f16, float, 1>();
-        return ve > 1 ? f.template operator()<f16, f16, 8>() : f.template operator()<f16, f16, 1>();
-    default:
-        return ve > 1 ? f.template operator()<float, float, 4>() : f.template operator()<float, float, 1>();
-    }
-}
-
-struct Forward {
-    const NormArgs &a; const Shape &s; cudaStream_t st;
-    template <typename T, typename W, int VE> cudaError_t operator()() const { return forward_nv<T, W, VE>(a, s, st); }
-};
-struct Backward {
-    const NormArgs &a; const Shape &s; cudaStream_t st;
-    template <typename T, typename W, int VE> cudaError_t operator()() const { return backward_nv<T, W, VE>(a, s, st); }
-};
+// by the element type and the weights' type
+#define BY_TYPE(call)                                                                                                     \
+    (a.d.dtype == RUBICK_BF16 ? (a.d.wtype == RUBICK_F32 ? call<bf16, float>(a, s, st) : call<bf16, bf16>(a, s, st))       \
+     : a.d.dtype == RUBICK_F16 ? (a.d.wtype == RUBICK_F32 ? call<f16, float>(a, s, st) : call<f16, f16>(a, s, st))         \
+                               : call<float, float>(a, s, st))
 
 }  // namespace
 
@@ -1004,7 +908,7 @@ cudaError_t launch_norm_forward(const NormArgs &args, int num_sms, cudaStream_t 
     NormArgs a = args;
     const Shape s = forward_shape(a, num_sms);
     if (s.ring) cut_rows(a, int64_t(num_sms) * s.blocks, &a.chunk_rows, &a.n_chunks);
-    return by_type(a, s.ve, Forward{a, s, st});
+    return BY_TYPE(forward_any);
 }
 
 // floats of scratch; also fixes how the rows are cut into chunks: one chunk per row slot, as many blocks as the SMs
@@ -1012,7 +916,7 @@ cudaError_t launch_norm_forward(const NormArgs &args, int num_sms, cudaStream_t 
 size_t norm_backward_scratch(const NormArgs &a, int num_sms, int64_t *chunk_rows, int *n_chunks)
 {
     const Shape s = backward_shape(a);
-    cut_rows(a, int64_t(num_sms) * s.blocks * s.slots, chunk_rows, n_chunks);
+    cut_rows(a, int64_t(num_sms) * s.blocks, chunk_rows, n_chunks);
     return size_t(4) * size_t(*n_chunks) * size_t(a.d.cols);
 }
 
@@ -1020,7 +924,7 @@ cudaError_t launch_norm_backward(const NormArgs &a, int num_sms, cudaStream_t st
 {
     (void)num_sms;
     const Shape s = backward_shape(a);
-    return by_type(a, s.ve, Backward{a, s, st});
+    return BY_TYPE(backward_any);
 }
 
 }  // namespace rubick

@@ -100,27 +100,6 @@ template <typename T, int VE> __device__ __forceinline__ void store_cols(T *row,
 #pragma unroll
     for (int e = 0; e < VE; ++e) if (c + e < cols) row[c + e] = from_f<T>(v[e]);
 }
-// VE elements of a row as they came from memory, so that a row waiting for its reduction takes half the registers
-template <typename T, int VE> struct Raw {
-    static_assert(VE == 1 || VE == Lanes<T>::N, "one element or 16 bytes");
-    uint4 r;
-    __device__ __forceinline__ void load(const T *row, int c, int cols)
-    {
-        if (c + VE <= cols) { r = ld_stream(row + c); return; }
-        float v[VE];
-#pragma unroll
-        for (int e = 0; e < VE; ++e) v[e] = c + e < cols ? to_f(row[c + e]) : 0.f;
-        r = pack16<T>(v);
-    }
-    __device__ __forceinline__ void zero() { r = make_uint4(0u, 0u, 0u, 0u); }
-    __device__ __forceinline__ void get(float (&v)[VE]) const { unpack16<T>(r, v); }
-};
-template <typename T> struct Raw<T, 1> {
-    float r;
-    __device__ __forceinline__ void load(const T *row, int c, int cols) { r = c < cols ? to_f(row[c]) : 0.f; }
-    __device__ __forceinline__ void zero() { r = 0.f; }
-    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = r; }
-};
 __device__ __forceinline__ uint4 ld_cached(const void *p)
 {
     uint4 r;

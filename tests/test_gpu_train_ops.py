@@ -116,6 +116,15 @@ NORM_CASES = [
     (1300, 4096, "bf16", "bf16", "token", {}),
     (700, 8192, "fp16", "fp16", "one", {}),
     (620, 8192, "fp32", "fp32", "one", {}),
+    # rows at odd addresses through the ring
+    (9700, 65, "bf16", "bf16", "token", dict(tanh=True)),
+    (4800, 301, "fp16", "fp32", "group", dict(group=700, shift=3)),
+    (2400, 1537, "bf16", "bf16", "one", {}),
+    (2400, 1030, "fp32", "fp32", "group", dict(group=5, pad=7)),
+    (1300, 4001, "bf16", "fp32", "none", dict(pad=2, after=False)),
+    (1300, 4095, "fp32", "fp32", "one", dict(before=False)),
+    (620, 8191, "fp16", "fp16", "group", dict(group=100)),
+    (5000, 77, "bf16", "bf16", "none", dict(block=False)),
 ]
 
 
@@ -173,7 +182,7 @@ def test_block_norm_forward_and_backward(ctx, case):
             guarded(out)
 
 
-@pytest.mark.parametrize("rows,cols", [(40, 768), (40, 1537), (5000, 768)])
+@pytest.mark.parametrize("rows,cols", [(40, 768), (40, 1537), (5000, 768), (5000, 777)])
 def test_block_norm_in_place_equals_out_of_place(ctx, rows, cols):
     import torch
     s, opt, desc = norm_case(rows, cols, "bf16", "bf16", "group", group=9)
