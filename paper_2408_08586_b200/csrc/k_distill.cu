@@ -127,6 +127,11 @@ template <typename T> __device__ __forceinline__ void read_teacher(const Distill
     const float c = LOG2E / a.d.temperature;
     float top = -INFINITY, total = 0.f;
     bool any = false;
+    // the first entries' student logits are asked for as soon as their places are known, and awaited last
+    constexpr int AHEAD = 4;
+    float ahead[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) ahead[u] = -INFINITY;
 #pragma unroll 4
     for (int j = lane; j < k; j += 32) {
         const int i = a.index[row * k + j];
@@ -136,6 +141,11 @@ template <typename T> __device__ __forceinline__ void read_teacher(const Distill
         t.log_q[j] = l;
         if (in) { top = fmaxf(top, l); any = true; }
     }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+        const int j = lane + 32 * u, i = j < k ? t.index[j] : -1;
+        if (i >= 0 && i >= c0 && i < c1) ahead[u] = to_f(z.row[i]);
+    }
     any = __any_sync(0xffffffffu, any);
     top = warp_max(top);
     if (top == -INFINITY) top = 0.f;              // only NaN entries: they reach the sum
@@ -144,9 +154,12 @@ template <typename T> __device__ __forceinline__ void read_teacher(const Distill
     total = warp_sum(total);
     const float log_total = log2f(total);
 #pragma unroll 4
-    for (int j = lane; j < k; j += 32) {
+    for (int j = lane; j < k; j += 32) t.log_q[j] = t.index[j] >= 0 ? (t.log_q[j] - top) * c - log_total : -INFINITY;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) if (lane + 32 * u < k) t.z[lane + 32 * u] = ahead[u];
+#pragma unroll 4
+    for (int j = lane + 32 * AHEAD; j < k; j += 32) {
         const int i = t.index[j];
-        t.log_q[j] = i >= 0 ? (t.log_q[j] - top) * c - log_total : -INFINITY;
         t.z[j] = i >= 0 && i >= c0 && i < c1 ? to_f(z.row[i]) : -INFINITY;
     }
     if (lane == 0) *t.live = any;

@@ -323,27 +323,12 @@ template <int N> __device__ __forceinline__ void ring_sum(const f2 (&in)[N], flo
         }
 }
 
-// What is to be copied of `bytes` bytes at `from` in whole 16-byte units.  The units that reach out of the tensor (before
-// its first row, behind its last) are put together byte by byte.
-struct Units { uintptr_t b0, b1; };
-__device__ __forceinline__ Units row_units(uintptr_t from, uint32_t bytes, bool first, bool last, uint8_t *slot)
-{
-    const uintptr_t low = from & ~uintptr_t(15), end = from + bytes, high = (end + 15) & ~uintptr_t(15);
-    Units u{low, high};
-    if (first && low < from) {
-        for (uintptr_t p = from; p < end && p < low + 16; ++p) slot[p - low] = *reinterpret_cast<const uint8_t *>(p);
-        u.b0 = low + 16;
-    }
-    if (last && end < high && u.b1 > u.b0) {
-        for (uintptr_t p = high - 16 < from ? from : high - 16; p < end; ++p) slot[p - low] = *reinterpret_cast<const uint8_t *>(p);
-        u.b1 = high - 16;
-    }
-    return u;
-}
-
-// The copies of row `row` into stage `s`, by one thread.
+// The copies of row `row` into stage `s`, by one warp.  Ragged rows come with the 16-byte units that they begin and end in;
+// units that reach out of the tensor itself (before its first row, behind its last) are put together by the lanes,
+// element by element, eight lanes a tensor.
 template <typename T, bool VEC> __device__ __forceinline__ void ring_issue(const NormArgs &a, const Ring &r, uint8_t *smem, uint64_t *bars, int s, int64_t row)
 {
+    const int lane = threadIdx.x & 31;
     uint8_t *stage = smem + size_t(s) * r.tensors * r.slot_bytes;
     const int64_t gate_row = r.i_gate >= 0 ? row / a.d.group_rows : 0;
     const auto from = [&](int which) {
@@ -351,33 +336,59 @@ template <typename T, bool VEC> __device__ __forceinline__ void ring_issue(const
             : which == 2 ? static_cast<const T *>(a.dx_out) + row * a.d.ld_x : which == 3 ? static_cast<const T *>(a.dh) + row * a.d.ld_h
             : static_cast<const T *>(a.gate) + gate_row * a.d.ld_gate;
     };
-    const int place[5] = {r.i_x, r.i_y, r.i_dxo, r.i_dh, r.i_gate};
+    const auto place = [&](int which) { return which == 0 ? r.i_x : which == 1 ? r.i_y : which == 2 ? r.i_dxo : which == 3 ? r.i_dh : r.i_gate; };
     if constexpr (VEC) {
+        if (lane) return;
         bar_expect(bars + s, r.slot_bytes * r.tensors);
 #pragma unroll
         for (int t = 0; t < 5; ++t)
-            if (place[t] >= 0) bulk_load(stage + place[t] * r.slot_bytes, from(t), r.slot_bytes, bars + s);
+            if (place(t) >= 0) bulk_load(stage + place(t) * r.slot_bytes, from(t), r.slot_bytes, bars + s);
     } else {
         const uint32_t bytes = a.d.cols * uint32_t(sizeof(T));
-        Units u[5];
-        uint32_t total = 0;
-        bool by_hand = false;
+        const bool gate_first = gate_row == 0, gate_last = (gate_row + 1) * a.d.group_rows >= a.d.rows;
+        const bool row_first = row == 0, row_last = row == a.d.rows - 1;
+        // first whole unit, and the end of the last one
+        const auto units = [&](int t, uintptr_t &b0, uintptr_t &b1) {
+            const uintptr_t p = reinterpret_cast<uintptr_t>(from(t)), end = p + bytes;
+            b0 = (t < 4 ? row_first : gate_first) ? (p + 15) & ~uintptr_t(15) : p & ~uintptr_t(15);
+            b1 = (t < 4 ? row_last : gate_last) ? end & ~uintptr_t(15) : (end + 15) & ~uintptr_t(15);
+            if (b1 < b0) b1 = b0;                 // (within one unit: all of it by hand)
+        };
+        if (row_first || row_last || (r.i_gate >= 0 && (gate_first || gate_last))) {
 #pragma unroll
-        for (int t = 0; t < 5; ++t) {
-            u[t] = Units{0, 0};
-            if (place[t] < 0) continue;
-            const bool first = t < 4 ? row == 0 : gate_row == 0, last = t < 4 ? row == a.d.rows - 1 : (gate_row + 1) * a.d.group_rows >= a.d.rows;
-            u[t] = row_units(reinterpret_cast<uintptr_t>(from(t)), bytes, first, last, stage + place[t] * r.slot_bytes);
-            total += uint32_t(u[t].b1 - u[t].b0);
-            by_hand |= first || last;
+            for (int t0 = 0; t0 < 5; t0 += 4) {
+                const int t = t0 + (lane >> 3);
+                if (t < 5 && place(t) >= 0) {
+                    uintptr_t b0, b1;
+                    units(t, b0, b1);
+                    const uintptr_t p = reinterpret_cast<uintptr_t>(from(t)), end = p + bytes, low = p & ~uintptr_t(15);
+                    uint8_t *slot = stage + place(t) * r.slot_bytes;
+                    const uintptr_t head = p + (lane & 7) * sizeof(T), tail = b1 + (lane & 7) * sizeof(T);
+                    const bool has_head = head < b0 && head < end, has_tail = tail < end && tail >= b0 && tail >= p;
+                    T h, e;
+                    if (has_head) h = *reinterpret_cast<const T *>(head);
+                    if (has_tail) e = *reinterpret_cast<const T *>(tail);
+                    if (has_head) *reinterpret_cast<T *>(slot + (head - low)) = h;
+                    if (has_tail) *reinterpret_cast<T *>(slot + (tail - low)) = e;
+                }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // a later copy comes behind these stores
+            __syncwarp();
         }
-        if (by_hand) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // a later copy comes behind these stores
+        if (lane) return;
+        uint32_t total = 0;
+#pragma unroll
+        for (int t = 0; t < 5; ++t)
+            if (place(t) >= 0) { uintptr_t b0, b1; units(t, b0, b1); total += uint32_t(b1 - b0); }
         bar_expect(bars + s, total);
 #pragma unroll
         for (int t = 0; t < 5; ++t)
-            if (u[t].b1 > u[t].b0)
-                bulk_load(stage + place[t] * r.slot_bytes + (u[t].b0 - (reinterpret_cast<uintptr_t>(from(t)) & ~uintptr_t(15))), reinterpret_cast<const void *>(u[t].b0),
-                          uint32_t(u[t].b1 - u[t].b0), bars + s);
+            if (place(t) >= 0) {
+                uintptr_t b0, b1;
+                units(t, b0, b1);
+                if (b1 > b0)
+                    bulk_load(stage + place(t) * r.slot_bytes + (b0 - (reinterpret_cast<uintptr_t>(from(t)) & ~uintptr_t(15))), reinterpret_cast<const void *>(b0), uint32_t(b1 - b0), bars + s);
+            }
     }
 }
 
@@ -450,8 +461,10 @@ __global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __
     if (threadIdx.x == 0) {
         for (int s = 0; s < r.stages; ++s) bar_init(bars + s);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T, VEC>(a, r, smem, bars, s, begin + s);
     }
+    __syncwarp();
+    if (threadIdx.x < 32)
+        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T, VEC>(a, r, smem, bars, s, begin + s);
     if (threadIdx.x < 32) {                       // the 64 words by one warp: the smallest block has no more
         (&red[0][0])[threadIdx.x] = 0.f;
         (&red[0][0])[threadIdx.x + 32] = 0.f;
@@ -498,7 +511,7 @@ __global__ void __maxnreg__(NV == 1 ? 64 : 96) norm_forward_ring_kernel(const __
             scale = ra = rsqrtf(sum[0] * inv_cols + a.d.eps);
         } else row_barrier(warps);
         // every thread has left the stage of the row before
-        if (threadIdx.x == 0 && i_row >= 1 && i_row - 1 + r.stages < n)
+        if (threadIdx.x < 32 && i_row >= 1 && i_row - 1 + r.stages < n)
             ring_issue<T, VEC>(a, r, smem, bars, s ? s - 1 : r.stages - 1, row - 1 + r.stages);
         part[0] = 0ull;
 #pragma unroll
@@ -584,12 +597,15 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
     if (threadIdx.x == 0) {
         for (int s = 0; s < r.stages; ++s) bar_init(bars + s);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T, VEC>(a, r, smem, bars, s, begin + s);
     }
+    __syncwarp();
+    if (threadIdx.x < 32)
+        for (int s = 0; s < r.stages && s < n; ++s) ring_issue<T, VEC>(a, r, smem, bars, s, begin + s);
     if (threadIdx.x < 32) {
 #pragma unroll
         for (int i = 0; i < 3; ++i) (&red[0][0])[threadIdx.x + 32 * i] = 0.f;
     }
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const bool block = FULL || a.y, after = FULL || (a.d.flags & RUBICK_NORM_AFTER), before = FULL || (a.d.flags & RUBICK_NORM_BEFORE);
     const bool stream = FULL || a.dx_out, need_y = FULL || r.i_y >= 0;
     const float o = a.d.flags & RUBICK_NORM_UNIT_OFFSET ? 1.f : 0.f, inv_cols = 1.f / float(cols);
@@ -649,7 +665,7 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
         }
         float sum[3];
         ring_sum<3>(part, sum, red[i_row & 1], warps);
-        if (threadIdx.x == 0 && i_row >= 1 && i_row - 1 + r.stages < n)
+        if (threadIdx.x < 32 && i_row >= 1 && i_row - 1 + r.stages < n)
             ring_issue<T, VEC>(a, r, smem, bars, s ? s - 1 : r.stages - 1, row - 1 + r.stages);
         const float m1 = rb * sum[0] * inv_cols, m2 = after ? ra * (sum[1] - rb * rb * m1 * sum[2]) * inv_cols : 0.f;
         const f2 f1 = both(-rb * rb * m1), f2y = both(-ra * ra * m2), ra2 = both(ra);
@@ -682,18 +698,21 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
     for (int i = 0; i < NV; ++i) {
         const int c = C::first(i, tpr);
         if (c >= cols) continue;
-        if (a.dw_after) C::put(part_row(a, 0, chunk), c, tpr, cols, acc_a[i]);
-        if (a.dw_before) C::put(part_row(a, 1, chunk), c, tpr, cols, acc_b[i]);
+        // one chunk has the sums whole
+        if (a.dw_after) C::put(a.n_chunks == 1 ? a.dw_after : part_row(a, 0, chunk), c, tpr, cols, acc_a[i]);
+        if (a.dw_before) C::put(a.n_chunks == 1 ? a.dw_before : part_row(a, 1, chunk), c, tpr, cols, acc_b[i]);
     }
 }
 
-// Adds up the chunks' partial sums, in chunk order: blockIdx.y = 0 dW_after, 1 dW_before, from 2 on the gate groups that
-// lie in more than one chunk.  32 columns a block, one chunk a warp at a time.
+// Adds up the chunks' partial sums, always in the same order: blockIdx.y = 0 dW_after, 1 dW_before, from 2 on the gate
+// groups that lie in more than one chunk.  Eight columns (a 32-byte sector) a block, 64 chunks at a time: the sums are few
+// and lie in L2, so it is loads in flight that count.
 template <typename T>
 __global__ void __launch_bounds__(512) norm_backward_join_kernel(const __grid_constant__ NormArgs a)
 {
-    __shared__ float tile[16][33];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    __shared__ float tile[16][8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 8 + (lane & 7), turn = threadIdx.x >> 3;
+    asm volatile("griddepcontrol.wait;" ::: "memory");       // launched while the chunks are still at work
     const int64_t groups = (a.d.rows + a.d.group_rows - 1) / a.d.group_rows;
     const bool weights = blockIdx.y < 2;
     if (weights && !(blockIdx.y ? a.dw_before : a.dw_after)) return;
@@ -714,10 +733,13 @@ __global__ void __launch_bounds__(512) norm_backward_join_kernel(const __grid_co
         }
         float v = 0.f;
         if (c < a.d.cols)
-            for (int q = first + warp; q <= last; q += 16) v += part_row(a, weights ? blockIdx.y : q == first ? 3 : 2, q)[c];
-        tile[warp][lane] = v;
+#pragma unroll 8
+            for (int q = first + turn; q <= last; q += 64) v += part_row(a, weights ? blockIdx.y : q == first ? 3 : 2, q)[c];
+        v += __shfl_xor_sync(0xffffffffu, v, 8);
+        v += __shfl_xor_sync(0xffffffffu, v, 16);
+        if (lane < 8) tile[warp][lane] = v;
         __syncthreads();
-        if (warp == 0 && c < a.d.cols) {
+        if (threadIdx.x < 8 && c < a.d.cols) {
             v = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) v += tile[i][lane];
@@ -747,12 +769,15 @@ bool vectors_fit(const NormArgs &a, int esize)
 int ring_budget(int n) { return 228 * 1024 / n - 1792; }
 
 // The ring's shape; false where a row does not fit: fewer than two stages, or more columns than 16 a thread cover.
-bool ring_shape(const NormArgs &a, bool back, Shape &s)
+bool ring_shape(const NormArgs &a, bool back, int num_sms, Shape &s)
 {
     const int es = esize_of(a.d.dtype);
     const bool vec = s.ve > 1 && a.d.cols % s.ve == 0;
-    const int unit = vec ? s.ve : 2, units = (a.d.cols + unit - 1) / unit, most = 16 / unit, warps = (units + most * 32 - 1) / (most * 32);
+    const int unit = vec ? s.ve : 2, units = (a.d.cols + unit - 1) / unit, most = 16 / unit;
+    int warps = (units + most * 32 - 1) / (most * 32);
     if (warps > 16) return false;
+    // few rows: more warps a row, down to one set of columns a thread
+    while (a.d.rows * warps < int64_t(num_sms) * 8 && warps * 2 <= 16 && warps * 32 < units) warps *= 2;
     Ring &r = s.r;
     const bool before = a.d.flags & RUBICK_NORM_BEFORE, after = a.d.flags & RUBICK_NORM_AFTER;
     int n = 0;
@@ -793,7 +818,7 @@ Shape forward_shape(const NormArgs &a, int num_sms)
     Shape s;
     const int es = esize_of(a.d.dtype);
     s.ve = vectors_fit(a, es) ? 16 / es : 1;
-    s.ring = ring_shape(a, false, s) && a.d.rows >= int64_t(num_sms) * s.blocks * 4;
+    s.ring = ring_shape(a, false, num_sms, s) && a.d.rows >= int64_t(num_sms) * s.blocks * 4;
     if (s.ring) return s;
     const int most = 32 / s.ve, nvec = (a.d.cols + s.ve - 1) / s.ve;
     int warps = (nvec + most * 32 - 1) / (most * 32);
@@ -806,12 +831,12 @@ Shape forward_shape(const NormArgs &a, int num_sms)
     return s;
 }
 
-Shape backward_shape(const NormArgs &a)
+Shape backward_shape(const NormArgs &a, int num_sms)
 {
     Shape s;
     const int es = esize_of(a.d.dtype);
     s.ve = vectors_fit(a, es) ? 16 / es : 1;
-    s.ring = ring_shape(a, true, s);
+    s.ring = ring_shape(a, true, num_sms, s);
     if (!s.ring) { s.tpr = 512; s.blocks = 1; }
     return s;
 }
@@ -886,13 +911,22 @@ template <typename T, typename W> cudaError_t backward_any(const NormArgs &a, co
     const cudaError_t e = s.ring ? (full ? backward_ring<T, W, true>(a, s, st) : backward_ring<T, W, false>(a, s, st))
                                  : s.ve > 1 ? backward_wide<T, W, Lanes<T>::N>(a, s, st) : backward_wide<T, W, 1>(a, s, st);
     if (e != cudaSuccess) return e;
+    if (a.n_chunks == 1 && s.ring) return cudaSuccess;         // nothing is left to be joined
     const int64_t groups = (a.d.rows + a.d.group_rows - 1) / a.d.group_rows;
     const bool split = a.gate && a.dgate && a.chunk_rows % a.d.group_rows != 0;
     const unsigned more = split ? unsigned(groups < 32 ? groups : 32) : 0u;
     if (!a.dw_after && !a.dw_before && !more) return cudaSuccess;
-    norm_backward_join_kernel<T><<<dim3((a.d.cols + 31) / 32, 2 + more), 512, 0, st>>>(a);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((a.d.cols + 7) / 8, 2 + more);
+    cfg.blockDim = dim3(512);
+    cfg.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
     count_launch();
-    return cudaGetLastError();
+    return cudaLaunchKernelEx(&cfg, norm_backward_join_kernel<T>, a);
 }
 
 // by the element type and the weights' type
@@ -915,15 +949,16 @@ cudaError_t launch_norm_forward(const NormArgs &args, int num_sms, cudaStream_t 
 // hold at once
 size_t norm_backward_scratch(const NormArgs &a, int num_sms, int64_t *chunk_rows, int *n_chunks)
 {
-    const Shape s = backward_shape(a);
+    const Shape s = backward_shape(a, num_sms);
     cut_rows(a, int64_t(num_sms) * s.blocks, chunk_rows, n_chunks);
+    // up to four rows one after the other cost less than a second kernel; the sums then go straight to their places
+    if (s.ring && a.d.rows <= 4 && aligned16(a.dw_after) && aligned16(a.dw_before)) { *chunk_rows = a.d.rows; *n_chunks = 1; }
     return size_t(4) * size_t(*n_chunks) * size_t(a.d.cols);
 }
 
 cudaError_t launch_norm_backward(const NormArgs &a, int num_sms, cudaStream_t st)
 {
-    (void)num_sms;
-    const Shape s = backward_shape(a);
+    const Shape s = backward_shape(a, num_sms);
     return BY_TYPE(backward_any);
 }
 
