@@ -323,72 +323,59 @@ template <int N> __device__ __forceinline__ void ring_sum(const f2 (&in)[N], flo
         }
 }
 
-// The copies of row `row` into stage `s`, by one warp.  Ragged rows come with the 16-byte units that they begin and end in;
-// units that reach out of the tensor itself (before its first row, behind its last) are put together by the lanes,
-// element by element, eight lanes a tensor.
+// The copies of row `row` into stage `s`, by one warp: by its first lane, or, where rows are ragged, lane t copies the
+// t-th tensor's (x, y, dx_out, dh, gate).  Ragged rows come with the 16-byte units that they begin and end in; units that
+// reach out of the tensor itself (before its first row, behind its last) are put together by the lanes, element by
+// element, eight lanes a tensor.
 template <typename T, bool VEC> __device__ __forceinline__ void ring_issue(const NormArgs &a, const Ring &r, uint8_t *smem, uint64_t *bars, int s, int64_t row)
 {
     const int lane = threadIdx.x & 31;
     uint8_t *stage = smem + size_t(s) * r.tensors * r.slot_bytes;
-    const int64_t gate_row = r.i_gate >= 0 ? row / a.d.group_rows : 0;
-    const auto from = [&](int which) {
-        return which == 0 ? static_cast<const T *>(a.x) + row * a.d.ld_x : which == 1 ? static_cast<const T *>(a.y) + row * a.d.ld_y
-            : which == 2 ? static_cast<const T *>(a.dx_out) + row * a.d.ld_x : which == 3 ? static_cast<const T *>(a.dh) + row * a.d.ld_h
-            : static_cast<const T *>(a.gate) + gate_row * a.d.ld_gate;
-    };
-    const auto place = [&](int which) { return which == 0 ? r.i_x : which == 1 ? r.i_y : which == 2 ? r.i_dxo : which == 3 ? r.i_dh : r.i_gate; };
     if constexpr (VEC) {
         if (lane) return;
         bar_expect(bars + s, r.slot_bytes * r.tensors);
-#pragma unroll
-        for (int t = 0; t < 5; ++t)
-            if (place(t) >= 0) bulk_load(stage + place(t) * r.slot_bytes, from(t), r.slot_bytes, bars + s);
+        if (r.i_x >= 0) bulk_load(stage + r.i_x * r.slot_bytes, static_cast<const T *>(a.x) + row * a.d.ld_x, r.slot_bytes, bars + s);
+        if (r.i_y >= 0) bulk_load(stage + r.i_y * r.slot_bytes, static_cast<const T *>(a.y) + row * a.d.ld_y, r.slot_bytes, bars + s);
+        if (r.i_dxo >= 0) bulk_load(stage + r.i_dxo * r.slot_bytes, static_cast<const T *>(a.dx_out) + row * a.d.ld_x, r.slot_bytes, bars + s);
+        if (r.i_dh >= 0) bulk_load(stage + r.i_dh * r.slot_bytes, static_cast<const T *>(a.dh) + row * a.d.ld_h, r.slot_bytes, bars + s);
+        if (r.i_gate >= 0) bulk_load(stage + r.i_gate * r.slot_bytes, static_cast<const T *>(a.gate) + (row / a.d.group_rows) * a.d.ld_gate, r.slot_bytes, bars + s);
     } else {
+        const int place = lane == 0 ? r.i_x : lane == 1 ? r.i_y : lane == 2 ? r.i_dxo : lane == 3 ? r.i_dh : lane == 4 ? r.i_gate : -1;
+        const bool gate = lane == 4, copied = place >= 0;
+        const void *base = lane == 0 ? a.x : lane == 1 ? a.y : lane == 2 ? a.dx_out : lane == 3 ? a.dh : a.gate;
+        const int64_t ld = lane == 0 || lane == 2 ? a.d.ld_x : lane == 1 ? a.d.ld_y : lane == 3 ? a.d.ld_h : a.d.ld_gate;
+        const int64_t at = gate && copied ? row / a.d.group_rows : row;
+        const uintptr_t p = copied ? reinterpret_cast<uintptr_t>(base) + uintptr_t(at * ld) * sizeof(T) : 0;
+        const uint32_t my_slot = copied ? place * r.slot_bytes : 0u;
         const uint32_t bytes = a.d.cols * uint32_t(sizeof(T));
-        const bool gate_first = gate_row == 0, gate_last = (gate_row + 1) * a.d.group_rows >= a.d.rows;
-        const bool row_first = row == 0, row_last = row == a.d.rows - 1;
+        const bool first = at == 0, last = gate ? (at + 1) * a.d.group_rows >= a.d.rows : at == a.d.rows - 1;
         // first whole unit, and the end of the last one
-        const auto units = [&](int t, uintptr_t &b0, uintptr_t &b1) {
-            const uintptr_t p = reinterpret_cast<uintptr_t>(from(t)), end = p + bytes;
-            b0 = (t < 4 ? row_first : gate_first) ? (p + 15) & ~uintptr_t(15) : p & ~uintptr_t(15);
-            b1 = (t < 4 ? row_last : gate_last) ? end & ~uintptr_t(15) : (end + 15) & ~uintptr_t(15);
-            if (b1 < b0) b1 = b0;                 // (within one unit: all of it by hand)
-        };
-        if (row_first || row_last || (r.i_gate >= 0 && (gate_first || gate_last))) {
+        const uintptr_t low = p & ~uintptr_t(15), end = p + bytes;
+        const uintptr_t b0 = first ? (p + 15) & ~uintptr_t(15) : low;
+        uintptr_t b1 = last ? end & ~uintptr_t(15) : (end + 15) & ~uintptr_t(15);
+        if (b1 < b0) b1 = b0;                     // (within one unit: all of it by hand)
+        if (__any_sync(0xffffffffu, copied && (first || last))) {
 #pragma unroll
-            for (int t0 = 0; t0 < 5; t0 += 4) {
+            for (int t0 = 0; t0 < 8; t0 += 4) {
                 const int t = t0 + (lane >> 3);
-                if (t < 5 && place(t) >= 0) {
-                    uintptr_t b0, b1;
-                    units(t, b0, b1);
-                    const uintptr_t p = reinterpret_cast<uintptr_t>(from(t)), end = p + bytes, low = p & ~uintptr_t(15);
-                    uint8_t *slot = stage + place(t) * r.slot_bytes;
-                    const uintptr_t head = p + (lane & 7) * sizeof(T), tail = b1 + (lane & 7) * sizeof(T);
-                    const bool has_head = head < b0 && head < end, has_tail = tail < end && tail >= b0 && tail >= p;
-                    T h, e;
-                    if (has_head) h = *reinterpret_cast<const T *>(head);
-                    if (has_tail) e = *reinterpret_cast<const T *>(tail);
-                    if (has_head) *reinterpret_cast<T *>(slot + (head - low)) = h;
-                    if (has_tail) *reinterpret_cast<T *>(slot + (tail - low)) = e;
-                }
+                const uintptr_t tp = __shfl_sync(0xffffffffu, (unsigned long long)p, t);
+                const uintptr_t tb0 = __shfl_sync(0xffffffffu, (unsigned long long)b0, t), tb1 = __shfl_sync(0xffffffffu, (unsigned long long)b1, t);
+                const uint32_t slot = __shfl_sync(0xffffffffu, my_slot, t);
+                const uintptr_t tend = tp + bytes, tlow = tp & ~uintptr_t(15);
+                const uintptr_t head = tp + (lane & 7) * sizeof(T), tail = tb1 + (lane & 7) * sizeof(T);
+                const bool has_head = tp && head < tb0 && head < tend, has_tail = tp && tail < tend && tail >= tb0 && tail >= tp;
+                T h, e;
+                if (has_head) h = *reinterpret_cast<const T *>(head);
+                if (has_tail) e = *reinterpret_cast<const T *>(tail);
+                if (has_head) *reinterpret_cast<T *>(stage + slot + (head - tlow)) = h;
+                if (has_tail) *reinterpret_cast<T *>(stage + slot + (tail - tlow)) = e;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // a later copy comes behind these stores
-            __syncwarp();
         }
-        if (lane) return;
-        uint32_t total = 0;
-#pragma unroll
-        for (int t = 0; t < 5; ++t)
-            if (place(t) >= 0) { uintptr_t b0, b1; units(t, b0, b1); total += uint32_t(b1 - b0); }
-        bar_expect(bars + s, total);
-#pragma unroll
-        for (int t = 0; t < 5; ++t)
-            if (place(t) >= 0) {
-                uintptr_t b0, b1;
-                units(t, b0, b1);
-                if (b1 > b0)
-                    bulk_load(stage + place(t) * r.slot_bytes + (b0 - (reinterpret_cast<uintptr_t>(from(t)) & ~uintptr_t(15))), reinterpret_cast<const void *>(b0), uint32_t(b1 - b0), bars + s);
-            }
+        const uint32_t mine = copied ? uint32_t(b1 - b0) : 0u, total = __reduce_add_sync(0xffffffffu, mine);
+        if (lane == 0) bar_expect(bars + s, total);
+        __syncwarp();
+        if (mine) bulk_load(stage + my_slot + (b0 - low), reinterpret_cast<const void *>(b0), mine, bars + s);
     }
 }
 
@@ -705,13 +692,13 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
 }
 
 // Adds up the chunks' partial sums, always in the same order: blockIdx.y = 0 dW_after, 1 dW_before, from 2 on the gate
-// groups that lie in more than one chunk.  Eight columns (a 32-byte sector) a block, 64 chunks at a time: the sums are few
-// and lie in L2, so it is loads in flight that count.
-template <typename T>
+// groups that lie in more than one chunk.  CB columns a block, 512 / CB chunks at a time: the sums lie in L2, so it is loads
+// in flight that count; few columns are taken eight (a 32-byte sector) a block, for more blocks.
+template <typename T, int CB>
 __global__ void __launch_bounds__(512) norm_backward_join_kernel(const __grid_constant__ NormArgs a)
 {
-    __shared__ float tile[16][8];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 8 + (lane & 7), turn = threadIdx.x >> 3;
+    __shared__ float tile[16][CB];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * CB + lane % CB, turn = threadIdx.x / CB;
     asm volatile("griddepcontrol.wait;" ::: "memory");       // launched while the chunks are still at work
     const int64_t groups = (a.d.rows + a.d.group_rows - 1) / a.d.group_rows;
     const bool weights = blockIdx.y < 2;
@@ -734,12 +721,12 @@ __global__ void __launch_bounds__(512) norm_backward_join_kernel(const __grid_co
         float v = 0.f;
         if (c < a.d.cols)
 #pragma unroll 8
-            for (int q = first + turn; q <= last; q += 64) v += part_row(a, weights ? blockIdx.y : q == first ? 3 : 2, q)[c];
-        v += __shfl_xor_sync(0xffffffffu, v, 8);
-        v += __shfl_xor_sync(0xffffffffu, v, 16);
-        if (lane < 8) tile[warp][lane] = v;
+            for (int q = first + turn; q <= last; q += 512 / CB) v += part_row(a, weights ? blockIdx.y : q == first ? 3 : 2, q)[c];
+#pragma unroll
+        for (int o = 16; o >= CB; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane < CB) tile[warp][lane] = v;
         __syncthreads();
-        if (threadIdx.x < 8 && c < a.d.cols) {
+        if (threadIdx.x < CB && c < a.d.cols) {
             v = 0.f;
 #pragma unroll
             for (int i = 0; i < 16; ++i) v += tile[i][lane];
@@ -917,7 +904,8 @@ template <typename T, typename W> cudaError_t backward_any(const NormArgs &a, co
     const unsigned more = split ? unsigned(groups < 32 ? groups : 32) : 0u;
     if (!a.dw_after && !a.dw_before && !more) return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((a.d.cols + 7) / 8, 2 + more);
+    const int cb = a.d.cols <= 2048 ? 8 : 32;
+    cfg.gridDim = dim3((a.d.cols + cb - 1) / cb, 2 + more);
     cfg.blockDim = dim3(512);
     cfg.stream = st;
     cudaLaunchAttribute at[1];
@@ -926,7 +914,7 @@ template <typename T, typename W> cudaError_t backward_any(const NormArgs &a, co
     cfg.attrs = at;
     cfg.numAttrs = 1;
     count_launch();
-    return cudaLaunchKernelEx(&cfg, norm_backward_join_kernel<T>, a);
+    return cb == 8 ? cudaLaunchKernelEx(&cfg, norm_backward_join_kernel<T, 8>, a) : cudaLaunchKernelEx(&cfg, norm_backward_join_kernel<T, 32>, a);
 }
 
 // by the element type and the weights' type
