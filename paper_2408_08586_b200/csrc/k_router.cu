@@ -13,9 +13,11 @@
 // number from the top, so that no two keys are equal and the lowest index wins among equal logits.  Sixteen-bit
 // logits fit the upper bits whole.  Of single-precision ones some bits are cut off: where two neighbours among the
 // first k + 1 keys differ in nothing but these, the row is chosen again with whole keys.  Every lane sorts its own keys
-// once and puts the list into shared memory; after that one of the k is a maximum over the lanes' first keys and one
-// lane's step down its list, a dozen instructions for all rows of the warp together.  Sixteen elements a lane: fewer
-// leave the steps that a warp's rows share to fewer rows, more make the sort dear.
+// once, in two halves, and puts the two lists into shared memory; after that one of the k is a maximum over the lanes'
+// first keys and one lane's step down one list, some fifteen instructions for all rows of the warp together.  (Two lists of
+// eight take 38 comparators, one of sixteen 63: 800 against 1,020 instructions for four rows of 128, 39 against 43 us for
+// 65,536 of them.)  Sixteen elements a lane: fewer leave the steps that a warp's rows share to fewer rows, more make the
+// sort dear.
 //
 // Bound by instruction issue, not by memory: a row of 128 experts is 512 bytes, and its choice some 150 instructions.
 //
@@ -134,7 +136,7 @@ template <int LANES> __device__ __forceinline__ uint32_t lanes_max(uint32_t v)
 }
 
 // Descending sort of a lane's keys by Batcher's odd-even merge network (K. E. Batcher, 1968)
-template <int N> __device__ __forceinline__ void sort_keys(uint32_t (&s)[N])
+template <int N> __device__ __forceinline__ void sort_keys(uint32_t *s)
 {
 #pragma unroll
     for (int p = 1; p < N; p *= 2)
@@ -183,21 +185,23 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
             }
         }
     }
-    sort_keys<EPL>(key);
-    // this lane's list, 32 words from one to the next; behind its last key a 0 (written once, at the start)
+    sort_keys<EPL / 2>(key);
+    sort_keys<EPL / 2>(key + EPL / 2);
+    // this lane's two lists, 32 words from one key to the next; behind each a 0 (written once, at the start)
 #pragma unroll
-    for (int i = 1; i < EPL; ++i) sorted[i * 32] = key[i];
-    uint32_t mine = 0u, head = key[0];
-    const uint32_t *next_key = sorted + 32;
-    uint32_t next = lanes_max<LANES>(head);
+    for (int i = 1; i < EPL / 2; ++i) { sorted[i * 32] = key[i]; sorted[(EPL / 2 + 1 + i) * 32] = key[EPL / 2 + i]; }
+    uint32_t mine = 0u, head0 = key[0], head1 = key[EPL / 2];
+    const uint32_t *next0 = sorted + 32, *next1 = sorted + (EPL / 2 + 2) * 32;
+    uint32_t next = lanes_max<LANES>(max(head0, head1));
     const uint32_t first = next;
 #pragma unroll 2
     for (int j = 0; j < k; ++j) {
         // keys are never 0 before the lists end, and k places do not reach that end
         if (LANES >= RUBICK_MAX_CHOSEN) mine = sub == j ? next : mine;
         else if (sub == (j & (lanes - 1))) list[j] = next;
-        if (head == next) { head = *next_key; next_key += 32; }
-        next = lanes_max<LANES>(head);
+        if (head0 == next) { head0 = *next0; next0 += 32; }
+        if (head1 == next) { head1 = *next1; next1 += 32; }
+        next = lanes_max<LANES>(max(head0, head1));
     }
     const uint32_t none = KEY_NINF | low;         // up to here: closed, or not a column
     const bool some = first > none;
@@ -313,42 +317,51 @@ __device__ void finish_group(const RouterArgs &a, int64_t g, float dot, int vali
 }
 
 // What the last block of a group does: the chunks' sums, every warp a run of them, then the warps' sums in order (a block
-// that joins takes no further group: there are chunks only where groups are fewer than blocks).  `red`:
-// 2 x [warps][32] words.
+// that joins takes no further group: there are chunks only where groups are fewer than blocks).  JOIN columns at a time,
+// all their loads under way together.  `red`: 2 x [warps][JOIN] words.
+constexpr int JOIN = 128;
 __device__ void join_group(const RouterArgs &a, int64_t g, float *red)
 {
     __shared__ int32_t valid_rows;
     const int E = a.d.experts, C = a.chunks, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int32_t *pc = a.part_counts + g * C * (E + 1);
     const float *ps = a.part + g * C * E;
-    int32_t *red_n = reinterpret_cast<int32_t *>(red + ROUTER_THREADS);
+    int32_t *red_n = reinterpret_cast<int32_t *>(red + ROUTER_WARPS * JOIN);
     if (threadIdx.x == 0) valid_rows = 0;
     __syncthreads();
     int valid = 0;
     for (int q = threadIdx.x; q < C; q += ROUTER_THREADS) valid += __ldcg(pc + int64_t(q) * (E + 1) + E);
-    valid = __reduce_add_sync(0xffffffffu, valid);
-    if (lane == 0 && valid) atomicAdd(&valid_rows, valid);
     const int run = (C + ROUTER_WARPS - 1) / ROUTER_WARPS, q0 = warp * run, q1 = q0 + run < C ? q0 + run : C;
     float dot = 0.f;
-    for (int e0 = 0; e0 < E; e0 += 32) {
-        const int e = e0 + lane;
-        int n = 0;
-        float s = 0.f;
-        if (e < E)
-#pragma unroll 8
-            for (int q = q0; q < q1; ++q) { n += __ldcg(pc + int64_t(q) * (E + 1) + e); s += __ldcg(ps + int64_t(q) * E + e); }
-        __syncthreads();                          // the columns before are read
-        red[threadIdx.x] = s;
-        red_n[threadIdx.x] = n;
-        __syncthreads();
-        if (warp == (e0 >> 5) % ROUTER_WARPS && e < E) {
-            n = 0;
-            s = 0.f;
+    for (int e0 = 0; e0 < E; e0 += JOIN) {
+        int n[JOIN / 32];
+        float s[JOIN / 32];
 #pragma unroll
-            for (int w = 0; w < ROUTER_WARPS; ++w) { n += red_n[w * 32 + lane]; s += red[w * 32 + lane]; }
-            a.counts[g * E + e] = n;
-            a.prob_sum[g * E + e] = s;
-            dot = fmaf(float(n), s, dot);
+        for (int u = 0; u < JOIN / 32; ++u) { n[u] = 0; s[u] = 0.f; }
+#pragma unroll 2
+        for (int q = q0; q < q1; ++q)
+#pragma unroll
+            for (int u = 0; u < JOIN / 32; ++u) {
+                const int e = e0 + u * 32 + lane;
+                if (e < E) { n[u] += __ldcg(pc + int64_t(q) * (E + 1) + e); s[u] += __ldcg(ps + int64_t(q) * E + e); }
+            }
+        if (e0) __syncthreads();                  // the columns before are read
+        else {
+            valid = __reduce_add_sync(0xffffffffu, valid);
+            if (lane == 0 && valid) atomicAdd(&valid_rows, valid);
+        }
+#pragma unroll
+        for (int u = 0; u < JOIN / 32; ++u) { red[warp * JOIN + u * 32 + lane] = s[u]; red_n[warp * JOIN + u * 32 + lane] = n[u]; }
+        __syncthreads();
+        const int e = e0 + int(threadIdx.x);
+        if (threadIdx.x < JOIN && e < E) {
+            int m = 0;
+            float t = 0.f;
+#pragma unroll
+            for (int w = 0; w < ROUTER_WARPS; ++w) { m += red_n[w * JOIN + threadIdx.x]; t += red[w * JOIN + threadIdx.x]; }
+            a.counts[g * E + e] = m;
+            a.prob_sum[g * E + e] = t;
+            dot = fmaf(float(m), t, dot);
         }
     }
     finish_group(a, g, dot, valid_rows);
@@ -415,7 +428,7 @@ template <int EPL, int LANES> __device__ __forceinline__ void fold_rows(const Ta
 template <typename T, int EPL> __host__ __device__ __forceinline__ int kept_words() { return sizeof(T) == 4 ? 32 * EPL : 0; }
 template <typename T, int EPL, int LANES> __host__ __device__ __forceinline__ int warp_words(int k)
 {
-    return kept_words<T, EPL>() + 32 * (EPL + 1) + (LANES == 32 ? 0 : (32 / LANES * k + 3) / 4 * 4);
+    return kept_words<T, EPL>() + 32 * (EPL + 2) + (LANES == 32 ? 0 : (32 / LANES * k + 3) / 4 * 4);
 }
 
 // blockIdx.x = chunk of rows within the group, blockIdx.y = group; by_warp: a warp takes whole groups
@@ -432,10 +445,10 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : FORWARD_BLOCKS)
     int32_t *own = smem + warp * own_words, *tables = smem + ROUTER_WARPS * own_words;
     float *kept = reinterpret_cast<float *>(own) + slot * lanes * EPL;
     uint32_t *sorted = reinterpret_cast<uint32_t *>(own + kept_words<T, EPL>()) + lane;
-    uint32_t *list = reinterpret_cast<uint32_t *>(own + kept_words<T, EPL>() + 32 * (EPL + 1)) + slot * a.d.k;
+    uint32_t *list = reinterpret_cast<uint32_t *>(own + kept_words<T, EPL>() + 32 * (EPL + 2)) + slot * a.d.k;
     int32_t *hist = tables + (by_warp ? warp * E : 0);
     float *psum = reinterpret_cast<float *>(tables + E);
-    sorted[EPL * 32] = 0u;
+    sorted[EPL / 2 * 32] = sorted[(EPL + 1) * 32] = 0u;
     for (int e = threadIdx.x; e < E * (by_warp ? ROUTER_WARPS : 1); e += ROUTER_THREADS) tables[e] = 0;
     if (threadIdx.x == 0) valid_rows = 0;
     __syncthreads();
