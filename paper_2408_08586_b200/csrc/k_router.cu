@@ -193,7 +193,8 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
     uint32_t mine = 0u, head0 = key[0], head1 = key[EPL / 2];
     const uint32_t *next0 = sorted + 32, *next1 = sorted + (EPL / 2 + 2) * 32;
     uint32_t next = lanes_max<LANES>(max(head0, head1));
-    const uint32_t first = next;
+    const uint32_t first = next, none = KEY_NINF | low;      // up to `none`: closed, or not a column
+    bool near = false;                            // two neighbours that only the cut-off bits may tell apart
 #pragma unroll 2
     for (int j = 0; j < k; ++j) {
         // keys are never 0 before the lists end, and k places do not reach that end
@@ -201,9 +202,10 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
         else if (sub == (j & (lanes - 1))) list[j] = next;
         if (head0 == next) { head0 = *next0; next0 += 32; }
         if (head1 == next) { head1 = *next1; next1 += 32; }
+        const uint32_t above = next;
         next = lanes_max<LANES>(max(head0, head1));
+        if (sizeof(T) == 4) near |= (above ^ next) <= low && next > none;
     }
-    const uint32_t none = KEY_NINF | low;         // up to here: closed, or not a column
     const bool some = first > none;
     // what the keys leave of the largest logit: the exponentials need its neighbourhood, not its last bits
     const uint32_t top = first & ~low;
@@ -228,13 +230,8 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
     // A NaN, or neighbours that only the cut-off bits tell apart: once more, with whole keys.
     bool unsure = total != total;
     if constexpr (sizeof(T) == 4) {
-        bool near = false;
-        const uint32_t below = WARP ? __shfl_down_sync(0xffffffffu, mine, 1) : 0u;
-        for (int j = sub; j < k; j += lanes) {
-            const uint32_t x = WARP ? mine : list[j], y = j + 1 == k ? next : WARP ? below : list[j + 1];
-            near |= (x ^ y) <= low && x > none;
-        }
         if (__any_sync(0xffffffffu, near)) {
+            const uint32_t below = WARP ? __shfl_down_sync(0xffffffffu, mine, 1) : 0u;
             for (int j = sub; j < k; j += lanes) {
                 const uint32_t x = WARP ? mine : list[j], y = j + 1 == k ? next : WARP ? below : list[j + 1];
                 unsure |= (x ^ y) <= low && x > none && kept[low - (x & low)] != kept[low - (y & low)];
