@@ -6,7 +6,8 @@
  * gains, and a greedy allocation round that runs entirely on the device; further the minimum
  * demand of guaranteed jobs and tenant quotas, the incremental round (shrink / exchange step,
  * preemption, reconfiguration gate), batched fitting of the model's coefficients, and a wider plan
- * space (degrees of any size, explicit gradient accumulation).
+ * space (degrees of any size, explicit gradient accumulation).  Besides, the bandwidth-bound operators of the
+ * training steps that it schedules: block norm, router and distillation, forward and backward.
  *
  * Conventions
  *  - Every call returns an int: RUBICK_OK (0) or a negative error code.  Nothing throws, aborts
