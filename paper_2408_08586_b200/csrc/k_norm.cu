@@ -141,6 +141,12 @@ __device__ __forceinline__ float *part_row(const NormArgs &a, int which, int chu
     return a.part + (int64_t(which) * a.n_chunks + chunk) * a.d.cols;
 }
 
+// One chunk has the weights' sums whole: the ring writes them to their places, sixteen bytes at a time, where these allow it.
+__host__ __device__ __forceinline__ bool sums_go_straight(const NormArgs &a)
+{
+    return a.n_chunks == 1 && ((reinterpret_cast<uintptr_t>(a.dw_after) | reinterpret_cast<uintptr_t>(a.dw_before)) & 15) == 0;
+}
+
 // Rows too wide for the ring below: the column sums are in shared memory, and a row is read twice (the second time from
 // L2), once for its sums and once for its gradients.
 template <typename T, typename W, int VE>
@@ -692,9 +698,9 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
     for (int i = 0; i < NV; ++i) {
         const int c = C::first(i, tpr);
         if (c >= cols) continue;
-        // one chunk has the sums whole
-        if (a.dw_after) C::put(a.n_chunks == 1 ? a.dw_after : part_row(a, 0, chunk), c, tpr, cols, acc_a[i]);
-        if (a.dw_before) C::put(a.n_chunks == 1 ? a.dw_before : part_row(a, 1, chunk), c, tpr, cols, acc_b[i]);
+        const bool straight = sums_go_straight(a);
+        if (a.dw_after) C::put(straight ? a.dw_after : part_row(a, 0, chunk), c, tpr, cols, acc_a[i]);
+        if (a.dw_before) C::put(straight ? a.dw_before : part_row(a, 1, chunk), c, tpr, cols, acc_b[i]);
     }
 }
 
@@ -930,7 +936,7 @@ template <typename T, typename W> cudaError_t backward_any(const NormArgs &a, co
     const cudaError_t e = s.ring ? (full ? backward_ring<T, W, true>(a, s, st) : backward_ring<T, W, false>(a, s, st))
                                  : s.ve > 1 ? backward_wide<T, W, Lanes<T>::N>(a, s, st) : backward_wide<T, W, 1>(a, s, st);
     if (e != cudaSuccess) return e;
-    if (a.n_chunks == 1 && s.ring) return cudaSuccess;         // nothing is left to be joined
+    if (s.ring && sums_go_straight(a)) return cudaSuccess;     // nothing is left to be joined
     const int64_t groups = (a.d.rows + a.d.group_rows - 1) / a.d.group_rows;
     const bool split = a.gate && a.dgate && a.chunk_rows % a.d.group_rows != 0;
     const int64_t blocks = few_chunks(a) ? (groups + 15) / 16 : groups;

@@ -1,0 +1,56 @@
+"""Block norm at addresses, widths and group lengths where a launch, a copy or an index can go wrong, against double
+precision.  Tolerances as in test_gpu_train_ops.py, fixed beforehand: 64 2^-24 of the terms' size."""
+import pytest
+
+from gpu_util import has_cuda
+from paper_2408_08586_b200 import binding as rb
+import test_gpu_train_ops as ops
+import train_ref as ref
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_cuda(), reason="needs a CUDA device")]
+ctx = ops.ctx
+
+
+def gradients(ctx, s, opt, desc, rows, cols, shift=0):
+    """The backward pass from what the reference's forward pass gives, weight gradients `shift` floats behind 16 bytes."""
+    import torch
+    x, _, rstd, _, _ = ref.norm_forward(s["x"], s["y"], s["w_after"], s["gate"], s["w_before"], eps=1e-5, **opt)
+    x_out = ops.like(s["x"])[0].copy_(x.to(s["x"].dtype))
+    rstd = rstd.float().cuda()
+    dx, dy = ops.like(s["x"]), ops.like(s["x"])
+    buf = torch.full((2 * cols + 32,), 77.0, device="cuda")
+    dwa = buf[shift:shift + cols] if opt["after"] else None
+    at = (cols + 8 + 3) // 4 * 4 + shift
+    dwb = buf[at:at + cols] if opt["before"] else None
+    dg = ops.like(s["gate"]) if s["gate"] is not None else None
+    ctx.block_norm_backward(desc, x_out, s["y"], s["w_after"], s["gate"], s["w_before"], rstd, s["dx_out"], s["dh"], dx[0], dy[0], dwa, dg and dg[0], dwb)
+    ctx.sync()
+    for out in (dx, dy, dg):
+        if out is not None:
+            ops.guarded(out)
+    keep = torch.ones(len(buf), dtype=torch.bool, device="cuda")
+    for w, b in ((dwa, shift), (dwb, at)):
+        if w is not None:
+            keep[b:b + cols] = False
+    assert (buf[keep] == 77.0).all()
+    got = dict(dx=dx[0], dy=dy[0], dw_after=dwa, dw_before=dwb, dgate=dg and dg[0])
+    want = ref.norm_backward(x_out, s["y"], s["w_after"], s["gate"], s["w_before"], rstd, s["dx_out"], s["dh"], **opt)
+    return {k: v for k, v in got.items() if v is not None}, want
+
+
+def check(got, want, dtype):
+    for name, v in got.items():
+        ops.close(v, *want[name], "fp32" if name.startswith("dw") else dtype, 64, name)
+
+
+@pytest.mark.parametrize("shift", [0, 1, 2, 3])
+@pytest.mark.parametrize("rows,gate,kw", [(1, "one", {}), (1, "none", {}), (1, "token", {}), (2, "group", dict(group=2)), (2, "one", {}), (2, "token", {}),
+                                          (3, "one", {}), (4, "group", dict(group=3)), (5, "group", dict(group=5)), (300, "one", {})])
+@pytest.mark.parametrize("cols,dtype", [(768, "bf16"), (64, "fp32"), (8192, "fp16"), (771, "bf16"), (16384, "bf16")])
+def test_block_norm_weight_gradients_at_any_address(ctx, rows, gate, kw, cols, dtype, shift):
+    """Weight gradients are slices of a flat buffer as often as not: any address that a float may have will do."""
+    if rows == 300 and cols > 8192:
+        rows = 20
+    s, opt, desc = ops.norm_case(rows, cols, dtype, dtype, gate, **kw)
+    got, want = gradients(ctx, s, opt, desc, rows, cols, shift)
+    check(got, want, dtype)
