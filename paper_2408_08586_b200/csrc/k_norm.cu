@@ -386,6 +386,7 @@ template <typename T, bool VEC> __device__ __forceinline__ void ring_issue(const
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");       // a later copy comes behind these stores
         }
         const uint32_t mine = copied ? uint32_t(b1 - b0) : 0u, total = __reduce_add_sync(0xffffffffu, mine);
+        __syncwarp();                             // the stores of all lanes come before the arrival that stands for them
         if (lane == 0) bar_expect(bars + s, total);
         __syncwarp();
         if (mine) bulk_load(stage + my_slot + (b0 - low), reinterpret_cast<const void *>(b0), mine, bars + s);

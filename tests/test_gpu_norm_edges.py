@@ -54,3 +54,15 @@ def test_block_norm_weight_gradients_at_any_address(ctx, rows, gate, kw, cols, d
     s, opt, desc = ops.norm_case(rows, cols, dtype, dtype, gate, **kw)
     got, want = gradients(ctx, s, opt, desc, rows, cols, shift)
     check(got, want, dtype)
+
+
+@pytest.mark.parametrize("rows,cols,dtype,pad", [(300, 5501, "fp32", 0), (300, 5500, "fp32", 1), (9, 5501, "fp32", 0), (700, 8191, "bf16", 2), (1200, 515, "fp16", 0)])
+def test_block_norm_first_and_last_ragged_rows(ctx, rows, cols, dtype, pad):
+    """The first and the last row of a tensor come to their stage partly by hand, with two stages and with more."""
+    import torch
+    s, opt, desc = ops.norm_case(rows, cols, dtype, dtype, "token", pad=pad, shift=1)
+    first, want = gradients(ctx, s, opt, desc, rows, cols)
+    check(first, want, dtype)
+    for _ in range(6):
+        got, _ = gradients(ctx, s, opt, desc, rows, cols)
+        assert all(torch.equal(got[k], first[k]) for k in first)
