@@ -571,6 +571,7 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : BACKWARD_BLOCKS
     float *mine = add + (warp * 32 + slot * lanes) * EPL;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) mine[i * lanes + sub] = 0.f;
+    __syncwarp();                                 // one lane clears what others add to
     __shared__ float red[ROUTER_WARPS];
     float n = 0.f;                                // groups that take part in the loss
     if (a.some) n = *a.some;
