@@ -539,8 +539,8 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
     };
 
     if (warp == WARPS) {
-        // the part of row n, rounded out to 16-byte units; the units that reach out of the tensor itself (before its
-        // first row, behind its last) are put together element by element
+        // the part of row n, rounded out to 16-byte units; units that may reach out of the tensor itself (of rows that begin or
+        // end less than 16 bytes from its own ends) are put together element by element
         const auto issue = [&](int n) {
             const int64_t row = first_row + int64_t(n) * clusters;
             if (row >= a.d.rows) return;
@@ -549,11 +549,11 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
             uint8_t *stage = smem + (n % RING_STAGES) * stage_bytes;
             int b0 = v0, b1 = v1 > v0 ? v1 : v0;
             if (RAGGED) {
-                if (row == 0 && b0 == 0 && b1 > 0 && !z.whole(0)) {
+                if (row * a.d.ld < VE && b0 == 0 && b1 > 0 && !z.whole(0)) {
                     if (lane == 0) *reinterpret_cast<uint4 *>(stage) = z.load(0);
                     b0 = 1;
                 }
-                if (row == a.d.rows - 1 && b1 == z.vectors && b1 > b0 && !z.whole(b1 - 1)) {
+                if ((a.d.rows - 1 - row) * a.d.ld < VE && b1 == z.vectors && b1 > b0 && !z.whole(b1 - 1)) {
                     if (lane == 0) *reinterpret_cast<uint4 *>(stage + size_t(b1 - 1 - v0) * 16) = z.load(b1 - 1);
                     --b1;
                 }

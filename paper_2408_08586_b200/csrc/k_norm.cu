@@ -338,8 +338,8 @@ template <int N> __device__ __forceinline__ void ring_sum(const f2 (&in)[N], flo
 
 // The copies of row `row` into stage `s`, by one warp: by its first lane, or, where rows are ragged, lane t copies the
 // t-th tensor's (x, y, dx_out, dh, gate).  Ragged rows come with the 16-byte units that they begin and end in; units that
-// reach out of the tensor itself (before its first row, behind its last) are put together by the lanes, element by
-// element, eight lanes a tensor.
+// may reach out of the tensor itself (of rows that begin or end less than 16 bytes from the tensor's own ends: the first and
+// the last, and more where rows are short) are put together by the lanes, element by element, eight lanes a tensor.
 template <typename T, bool VEC> __device__ __forceinline__ void ring_issue(const NormArgs &a, const Ring &r, uint8_t *smem, uint64_t *bars, int s, int64_t row)
 {
     const int lane = threadIdx.x & 31;
@@ -358,10 +358,12 @@ template <typename T, bool VEC> __device__ __forceinline__ void ring_issue(const
         const void *base = lane == 0 ? a.x : lane == 1 ? a.y : lane == 2 ? a.dx_out : lane == 3 ? a.dh : a.gate;
         const int64_t ld = lane == 0 || lane == 2 ? a.d.ld_x : lane == 1 ? a.d.ld_y : lane == 3 ? a.d.ld_h : a.d.ld_gate;
         const int64_t at = gate && copied ? row / a.d.group_rows : row;
+        const int64_t left = gate && copied ? int64_t(uint32_t(a.d.rows - 1) / uint32_t(a.d.group_rows)) - at : a.d.rows - 1 - at;      // rows behind it
         const uintptr_t p = copied ? reinterpret_cast<uintptr_t>(base) + uintptr_t(at * ld) * sizeof(T) : 0;
         const uint32_t my_slot = copied ? place * r.slot_bytes : 0u;
         const uint32_t bytes = a.d.cols * uint32_t(sizeof(T));
-        const bool first = at == 0, last = gate ? (at + 1) * a.d.group_rows >= a.d.rows : at == a.d.rows - 1;
+        constexpr int64_t near = 16 / int64_t(sizeof(T));
+        const bool first = at * ld < near, last = left * ld < near;
         // first whole unit, and the end of the last one
         const uintptr_t low = p & ~uintptr_t(15), end = p + bytes;
         const uintptr_t b0 = first ? (p + 15) & ~uintptr_t(15) : low;

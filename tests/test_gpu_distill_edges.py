@@ -1,0 +1,45 @@
+"""Distillation at logits where single precision can go wrong, against double precision: finite mask values over whole
+stretches of the vocabulary, rows far from zero, infinite losses.
+
+Tolerances as in test_gpu_train_ops.py, fixed beforehand: 96 2^-24 of the terms' size, with differences of logits exact in
+double precision and every exponent below 2^5 where it counts."""
+import pytest
+
+from gpu_util import has_cuda
+from paper_2408_08586_b200 import binding as rb
+import test_gpu_train_ops as ops
+import train_ref as ref
+
+pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_cuda(), reason="needs a CUDA device")]
+ctx = ops.ctx
+NINF = float("-inf")
+LOWEST = {"bf16": -3.3895313892515355e38, "fp32": -3.4028234663852886e38, "fp16": -65504.0}
+
+
+def run(ctx, z, index, teacher, desc, up, backward=True):
+    """(loss, lse) of forward, (loss, lse, dz) of the step, dz of backward"""
+    import torch
+    rows = len(z)
+    f = lambda: torch.full((rows,), 9.0, device="cuda")  # noqa: E731
+    loss, lse, loss2, lse2 = f(), f(), f(), f()
+    ctx.distill_forward(desc, z, index, teacher, loss, lse)
+    both, back = ops.like(z), ops.like(z)
+    ctx.distill_step(desc, z, index, teacher, up, loss2, lse2, both[0])
+    if backward:
+        ctx.distill_backward(desc, z, index, teacher, lse, up, back[0])
+    ctx.sync()
+    ops.guarded(both)
+    ops.guarded(back)
+    return loss, lse, loss2, lse2, both[0], back[0] if backward else None
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 3, 5, 7, 9])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,pad,shift", [(3000, 0, 0), (3000, 0, 5), (3000, 2, 3), (3, 0, 1)])
+def test_distill_rows_shorter_than_a_copy(ctx, rows, pad, shift, vocab, dtype):
+    """Rows of a few bytes lie several to a 16-byte unit: units that reach out of the tensor are not only the first and last row's."""
+    z, index, teacher, desc = ops.distill_case(rows, vocab, 2, dtype, "fp32", pad=pad, shift=shift)
+    want = ref.distill(z, index, teacher, 1.0)
+    loss, lse, loss2, lse2, both, back = run(ctx, z, index, teacher, desc, None)
+    for name, got, t in (("loss", loss, "fp32"), ("lse", lse, "fp32"), ("loss", loss2, "fp32"), ("lse", lse2, "fp32"), ("dz", both, dtype), ("dz", back, dtype)):
+        ops.close(got, want[name], want["s_" + name], t, 96, name)

@@ -66,3 +66,22 @@ def test_block_norm_first_and_last_ragged_rows(ctx, rows, cols, dtype, pad):
     for _ in range(6):
         got, _ = gradients(ctx, s, opt, desc, rows, cols)
         assert all(torch.equal(got[k], first[k]) for k in first)
+
+
+@pytest.mark.parametrize("cols", [1, 2, 3, 5, 7, 9])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("rows,pad,shift", [(9700, 0, 0), (9700, 0, 5), (9700, 2, 3), (3, 0, 1), (2, 0, 0)])
+def test_block_norm_of_rows_shorter_than_a_copy(ctx, rows, pad, shift, cols, dtype):
+    """Rows of a few bytes lie several to a 16-byte unit: units that reach out of the tensor are not only the first and last row's."""
+    import torch
+    s, opt, desc = ops.norm_case(rows, cols, dtype, dtype, "group", group=3, pad=pad, shift=shift)
+    x_out, h, rstd = ops.like(s["x"]), ops.like(s["x"]), torch.empty(rows, 2, device="cuda")
+    ctx.block_norm_forward(desc, s["x"], s["y"], s["w_after"], s["gate"], s["w_before"], x_out[0], h[0], rstd)
+    ctx.sync()
+    want_x, want_h, want_r, size_x, size_h = ref.norm_forward(s["x"], s["y"], s["w_after"], s["gate"], s["w_before"], eps=1e-5, **opt)
+    ops.close(x_out[0], want_x, size_x, dtype, 64, "x_out")
+    ops.close(h[0], want_h, size_h, dtype, 64, "h")
+    ops.guarded(x_out)
+    ops.guarded(h)
+    got, want = gradients(ctx, s, opt, desc, rows, cols)
+    check(got, want, dtype)
