@@ -748,7 +748,8 @@ template <typename T, bool BACK, int EPL, bool VEC, int LANES> cudaError_t launc
     } else {
         const bool one = by_warp(a, num_sms);
         const int words = a.d.experts * (one ? ROUTER_WARPS : ROUTER_WARPS + 1) + ROUTER_WARPS * warp_words<T, EPL, LANES>(a.d.k);
-        if (words > 12 * 1024) {
+        // 48 KB come without asking, the kernel's static variables (some hundred bytes) included
+        if (words * 4 > 47 * 1024) {
             const cudaError_t e = cudaFuncSetAttribute(router_forward_kernel<T, EPL, VEC, LANES>, cudaFuncAttributeMaxDynamicSharedMemorySize, words * 4);
             if (e != cudaSuccess) return e;
         }

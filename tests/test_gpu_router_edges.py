@@ -18,6 +18,36 @@ pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_cuda(), reason="needs 
 ctx = ops.ctx
 NINF = float("-inf")
 
+SIZES = """
+import os, sys
+sys.path[:0] = [{tests!r}, os.path.dirname({tests!r})]
+import torch
+import test_gpu_train_ops as ops
+import train_ref as ref
+from paper_2408_08586_b200 import binding as rb, workloads
+ctx = rb.Context(workloads.ENV, device=0)
+# smallest shared memory first: a larger shape's opt-in would serve the smaller ones behind it
+for rows, experts, k, group in [(50, 26, 26, 50), (50, 27, 26, 50), (50, 28, 26, 50), (3000, 29, 26, 1), (3000, 32, 26, 1),
+                                (40, 396, 2, 40), (40, 397, 2, 40), (40, 398, 2, 40), (3000, 445, 1, 1), (3000, 447, 1, 1), (3000, 448, 1, 1)]:
+    z = torch.randn(rows, experts, generator=ops.gen(rows, experts)).cuda()
+    o = ops.router_outputs(rows, experts, k, -(-rows // group))
+    ctx.router_forward(rb.router(rows, experts, k, torch.float32, group_rows=group), z, None, o["index"], o["weight"], o["counts"], o["prob_sum"],
+                       o["valid"], o["loss"])
+    ctx.sync()
+    want = ref.router_forward(z, None, k, group_rows=group, coef=0.01, renorm=False)
+    assert torch.equal(o["index"].cpu().long(), want["index"]), (rows, experts)
+    assert torch.equal(o["counts"].cpu().long(), want["counts"]), (rows, experts)
+print("all of them ran")
+"""
+
+
+def test_router_sizes_about_the_default_shared_memory():
+    """In a process of its own: what a call may use must not depend on the calls before it."""
+    import os
+    got = subprocess.run([sys.executable, "-c", SIZES.format(tests=os.path.dirname(os.path.abspath(__file__)))], capture_output=True, text=True, timeout=600)
+    assert got.returncode == 0 and "all of them ran" in got.stdout, got.stderr[-2000:]
+
+
 def test_router_gradient_of_many_groups_repeats_itself(ctx):
     """Weights' gradients go through accumulators that one lane of a warp clears and others add to."""
     import torch
