@@ -210,14 +210,24 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
         if (sizeof(T) == 4) near |= (above ^ next) <= low && next > none;
     }
     const bool some = first > none;
-    // what the keys leave of the largest logit: the exponentials need its neighbourhood, not its last bits
-    const uint32_t top = first & ~low;
-    const float shift = some ? __uint_as_float(top & 0x80000000u ? top & 0x7fffffffu : ~(top | low)) : 0.f;
-    const float off = -shift * 1.4426950408889634f;
+    // The row's largest logit, with all of its bits (the keys have those of 16-bit logits only), and the differences to it
+    // before they are multiplied: what a shortened or a rounded maximum is off by grows with the logits, and moves every
+    // exponent of a row of a few million by more than single precision has room for.
+    float top;
+    if constexpr (sizeof(T) == 4) {
+        top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < EPL / 2; ++i) top = fmaxf(top, fmaxf(lo(z[i]), hi(z[i])));
+        top = lanes_max<LANES>(top);
+    } else {
+        const uint32_t b = first & ~low;
+        top = __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~(b | low));
+    }
+    const float shift = some ? top : 0.f;
     f2 e[EPL / 2], sums = 0ull;
 #pragma unroll
     for (int i = 0; i < EPL / 2; ++i) {
-        const f2 x = fma2(z[i], both(1.4426950408889634f), both(off));
+        const f2 x = mul2(add2(z[i], both(-shift)), both(1.4426950408889634f));
         float e0, e1;
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(lo(x)));
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(hi(x)));
@@ -279,7 +289,7 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
         const uint32_t b = m & ~low;
         const float logit = sizeof(T) == 4 ? (ok ? kept[col] : 0.f) : __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~(b | low));
         float w;
-        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(fmaf(logit, 1.4426950408889634f, off)));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"((logit - shift) * 1.4426950408889634f));
         w = ok ? w * inv : 0.f;
         sum += w;
         if (here) {

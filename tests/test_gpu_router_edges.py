@@ -18,6 +18,45 @@ pytestmark = [pytest.mark.gpu, pytest.mark.skipif(not has_cuda(), reason="needs 
 ctx = ops.ctx
 NINF = float("-inf")
 
+LOWEST = {"bf16": -3.3895313892515355e38, "fp32": -3.4028234663852886e38, "fp16": -65504.0}
+
+
+def far_rows(experts, dtype, fill):
+    """Six rows about `fill`: all of it, one expert above it, half ordinary, all but one, spread by whole exponents, and ordinary."""
+    import torch
+    g = ops.gen(experts, dtype, fill)
+    z = torch.randn(6, experts, generator=g)
+    z[0] = fill
+    z[1] = fill
+    z[1, experts // 2] = fill / 2 if fill < 0 else fill * 1.5
+    z[2, : experts // 2] = fill
+    z[3, 1:] = fill
+    z[4] = fill * (1 - torch.randint(0, 3, (experts,), generator=g) * 2.0 ** -6)
+    return z.to(ops.T(dtype)).cuda()
+
+
+@pytest.mark.parametrize("experts", [7, 16, 64, 128, 256, 600])
+@pytest.mark.parametrize("dtype,fill", [("fp32", -1e9), ("fp32", 1e7), ("fp32", -1e4), ("fp32", 2e38), ("fp32", LOWEST["fp32"]),
+                                        ("bf16", -1e9), ("bf16", 1e7), ("bf16", LOWEST["bf16"]), ("fp16", LOWEST["fp16"])])
+def test_router_takes_logits_far_from_zero(ctx, dtype, fill, experts):
+    """Padding that was filled with a finite mask value instead of being masked: such a row is uniform, not NaN."""
+    import torch
+    z, k = far_rows(experts, dtype, fill), 3
+    opt = dict(group_rows=4, coef=0.3, renorm=False)
+    want = ref.router_forward(z, None, k, **opt)
+    desc = rb.router(6, experts, k, ops.T(dtype), **opt)
+    o = ops.router_outputs(6, experts, k, 2)
+    ctx.router_forward(desc, z, None, o["index"], o["weight"], o["counts"], o["prob_sum"], o["valid"], o["loss"])
+    ctx.sync()
+    for name in ("index", "counts", "valid"):
+        assert torch.equal(o[name].cpu().long(), want[name]), name
+    one = torch.ones(1, dtype=torch.float64)
+    ops.close(o["weight"], want["weight"], one, "fp32", 32, "weight")
+    ops.close(o["prob_sum"], want["prob_sum"], 4 * one, "fp32", 64, "prob_sum")
+    loss = torch.tensor([want["loss"]], dtype=torch.float64)
+    ops.close(o["loss"], loss, loss.abs(), "fp32", 64, "loss")
+
+
 SIZES = """
 import os, sys
 sys.path[:0] = [{tests!r}, os.path.dirname({tests!r})]
