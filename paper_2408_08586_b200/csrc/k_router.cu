@@ -653,11 +653,11 @@ __global__ void __launch_bounds__(ROUTER_THREADS, EPL > 16 ? 1 : BACKWARD_BLOCKS
 #pragma unroll
         for (int i = 0; i < EPL / 2; ++i) top = fmaxf(top, fmaxf(lo(z[i]), hi(z[i])));
         top = lanes_max<LANES>(top);
-        const f2 off = both(top > -INFINITY ? -top * 1.4426950408889634f : 0.f);
+        const f2 less_top = both(top > -INFINITY ? -top : 0.f);       // (a difference first, as in the forward pass)
         f2 sums = 0ull, dots = 0ull;
 #pragma unroll
         for (int i = 0; i < EPL / 2; ++i) {
-            const f2 x = fma2(z[i], both(1.4426950408889634f), off);
+            const f2 x = mul2(add2(z[i], less_top), both(1.4426950408889634f));
             float e0, e1;
             asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(lo(x)));
             asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(hi(x)));

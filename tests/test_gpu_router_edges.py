@@ -57,6 +57,27 @@ def test_router_takes_logits_far_from_zero(ctx, dtype, fill, experts):
     ops.close(o["loss"], loss, loss.abs(), "fp32", 64, "loss")
 
 
+@pytest.mark.parametrize("experts", [7, 16, 64, 128, 256, 600])
+@pytest.mark.parametrize("dtype,fill", [("fp32", -1e9), ("fp32", 1e11), ("fp32", 2e38), ("fp32", LOWEST["fp32"]),
+                                        ("bf16", -1e9), ("bf16", 1e11), ("bf16", LOWEST["bf16"]), ("fp16", LOWEST["fp16"])])
+def test_router_gradient_takes_logits_far_from_zero(ctx, dtype, fill, experts):
+    import torch
+    z, k = far_rows(experts, dtype, fill), 3
+    for renorm in (False, True):
+        opt = dict(group_rows=4, coef=0.3, renorm=renorm)
+        want = ref.router_forward(z, None, k, **opt)
+        desc = rb.router(6, experts, k, ops.T(dtype), **opt)
+        dweight = torch.randn(6, k, generator=ops.gen(3, experts)).cuda()
+        out = ops.like(z)
+        ctx.router_backward(desc, z, want["index"].int().cuda(), want["weight"].float().cuda(), want["counts"].int().cuda(), want["valid"].int().cuda(),
+                            None, dweight, out[0])
+        ctx.sync()
+        dz, size = ref.router_backward(want, k, 1.0, dweight, **opt)
+        most = dweight.abs().max().double().cpu() + 0.3 * experts * want["counts"].max() / (k * 2 * 2)
+        ops.close(out[0], dz, size + most, dtype, 64, "dlogits")
+        ops.guarded(out)
+
+
 SIZES = """
 import os, sys
 sys.path[:0] = [{tests!r}, os.path.dirname({tests!r})]
