@@ -78,6 +78,30 @@ def test_router_gradient_takes_logits_far_from_zero(ctx, dtype, fill, experts):
         ops.guarded(out)
 
 
+@pytest.mark.parametrize("experts", [16, 60, 128, 256, 300, 600, 1024])
+@pytest.mark.parametrize("k", [1, 2, 5, 8])
+def test_router_settles_ties_at_its_last_place(ctx, experts, k):
+    """Single-precision logits a few units in the last place apart, many of them equal: whatever lies behind the k-th place
+    in the same run of equal upper bits may still be larger."""
+    import torch
+    g = ops.gen(experts, k)
+    z = torch.ones(60, experts)
+    z[0, 2] = 1 + 2.0 ** -20                                # behind an exact tie of the first two
+    z[1, experts - 1] = 1 + 2.0 ** -20
+    z[2:20] += torch.randint(0, 2, (18, experts), generator=g) * 2.0 ** -23
+    z[20:40] += (torch.rand(20, experts, generator=g) < 0.05) * 2.0 ** -22
+    z[40:] = -z[40:] - torch.randint(0, 3, (20, experts), generator=g) * 2.0 ** -21
+    z[50:, : experts // 2] = 2.0                            # places are taken before the run of near ties begins
+    z[50:, k - 1: experts // 2] = 1.0
+    z = z.cuda()
+    want = ref.router_forward(z, None, k, group_rows=60, coef=0.01, renorm=False)
+    o = ops.router_outputs(60, experts, k, 1)
+    ctx.router_forward(rb.router(60, experts, k, torch.float32), z, None, o["index"], o["weight"], o["counts"], o["prob_sum"], o["valid"], o["loss"])
+    ctx.sync()
+    assert torch.equal(o["index"].cpu().long(), want["index"])
+    assert torch.equal(o["counts"].cpu().long(), want["counts"])
+
+
 SIZES = """
 import os, sys
 sys.path[:0] = [{tests!r}, os.path.dirname({tests!r})]
