@@ -554,14 +554,17 @@ typedef struct {
 int rubick_distill_forward(rubick_ctx *ctx, const rubick_distill_desc *h_desc, const void *d_z, const int32_t *d_index,
                            const void *d_teacher, float *d_loss, float *d_lse);
 
-/* dz = d_dloss[n] T (p - q) from forward's d_lse; 0 in rows without entries.  d_dloss NULL = 1.  An index that a row
- * lists twice counts with the sum of its entries.  d_dz may equal d_z.  Errors: EINVAL, ECUDA. */
+/* dz = d_dloss[n] T (p - q), p = exp(z / T - lse) from forward's d_lse; 0 in rows without entries.  d_lse is one float, so
+ * p is off by a share of |lse| 2^-24: rows whose logits are all far from zero (beyond 1,000 T, say) want the step below.
+ * d_dloss NULL = 1.  An index that a row lists twice counts with the sum of its entries.  d_dz may equal d_z.
+ * Errors: EINVAL, ECUDA. */
 int rubick_distill_backward(rubick_ctx *ctx, const rubick_distill_desc *h_desc, const void *d_z, const int32_t *d_index,
                             const void *d_teacher, const float *d_lse, const float *d_dloss, void *d_dz);
 
 /* Both at once, for a loss whose weight per row is known beforehand: reads z once and writes dz once, where forward
  * and backward read z twice (a row longer than a cluster's registers, 131,072 single-precision or 262,144 16-bit
- * logits, is read twice all the same).  Outputs as theirs; d_lse is not optional here. */
+ * logits, is read twice all the same, and the context keeps a float a row between the two).  Outputs as theirs; d_lse is
+ * not optional here.  Errors: EINVAL, ENOMEM (long rows), ECUDA. */
 int rubick_distill_step(rubick_ctx *ctx, const rubick_distill_desc *h_desc, const void *d_z, const int32_t *d_index,
                         const void *d_teacher, const float *d_dloss, float *d_loss, float *d_lse, void *d_dz);
 

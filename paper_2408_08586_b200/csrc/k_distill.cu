@@ -30,9 +30,11 @@ namespace {
 
 constexpr int ROW_WARPS = 16, ROW_THREADS = ROW_WARPS * 32;      // a block of a row's cluster
 constexpr int BACK_THREADS = 256;                                 // a block of the separate gradient
+constexpr int STEP_NV = 8;                                        // vectors a thread of the step holds
 constexpr int MAX_RANKS = 8;                                      // the portable cluster size
 constexpr double LOG2E_D = 1.4426950408889634;
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr double LN2_D = 0.6931471805599453;
 constexpr float LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float ex2(float x)
@@ -203,6 +205,18 @@ template <> struct Top<f16> {
     __device__ __forceinline__ float get() const { return fmaxf(__low2float(m), __high2float(m)); }
 };
 
+// 2^((v - m) c) is taken as 2^(v c + off) with off = -m c: one instruction for the exponents of two logits.  The product is
+// rounded, and every exponent is off by what that took (2^-20 of a row about 12, 2^-9 of one about 30,000); a fused
+// product gives it whole, and this factor puts it right once for a sum.
+__device__ __forceinline__ float give_back(float m, float c, float off) { return ex2(-fmaf(m, c, off)); }
+
+// Of a log-sum given in two parts: the factor that 2^(z c + sub), sub = -lse log2(e), lacks by the rounding of lse, of c and
+// of sub (near the row's largest logits; what is far below these has little of its own to lose).
+__device__ __forceinline__ float give_back_lse(float lse, float low, float temperature, float c, float sub)
+{
+    return ex2(-float((double(lse) + double(low)) * double(temperature) * double(c) + double(sub)));
+}
+
 // s + sum of 2^(v c + off), pairwise
 template <typename T> __device__ __forceinline__ f2 add_exps(const uint4 &r, f2 c, f2 off, f2 s)
 {
@@ -253,7 +267,13 @@ __device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, co
     loss = warp_sum(loss);
     if (lane == 0) {
         a.loss[row] = live ? a.d.temperature * a.d.temperature * LN2 * loss : 0.f;
-        if (a.lse) a.lse[row] = live ? fmaf(shift, 1.f / a.d.temperature, LN2 * (log_whole + log_rest)) : 0.f;
+        if (a.lse_low) {
+            const double lse = live ? double(shift) / double(a.d.temperature) + LN2_D * (double(log_whole) + double(log_rest)) : 0.0;
+            a.lse[row] = float(lse);
+            a.lse_low[row] = isfinite(float(lse)) ? float(lse - double(float(lse))) : 0.f;
+        } else if (a.lse) {
+            a.lse[row] = live ? fmaf(shift, 1.f / a.d.temperature, LN2 * (log_whole + log_rest)) : 0.f;
+        }
     }
 }
 
@@ -289,9 +309,11 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
 #pragma unroll
         for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) top.take(r[i]);
         p.m = warp_max(top.get());
-        f2 off = both(p.m == -INFINITY ? 0.f : -p.m * c), s = 0ull;
+        float base = p.m == -INFINITY ? 0.f : p.m;
+        f2 s = 0ull;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) s = add_exps<T>(r[i], c2, off, s);
+        for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) s = add_exps<T>(r[i], c2, both(-base * c), s);
+        s = mul2(s, both(give_back(base, c, -base * c)));
         if constexpr (!STEP) {
             __syncthreads();
             // a row without entries is not read on
@@ -302,12 +324,13 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
 #pragma unroll
                 for (int i = 0; i < NV; ++i) if (v + i * ROW_THREADS < v1) more.take(r[i]);
                 const float m = fmaxf(p.m, warp_max(more.get()));
-                const float shift = m == -INFINITY ? 0.f : m;
-                off = both(-shift * c);
-                s = mul2(s, both(ex2((p.m - shift) * c)));
+                base = m == -INFINITY ? 0.f : m;
+                s = mul2(s, both(ex2((p.m - base) * c)));
                 p.m = m;
+                f2 t = 0ull;
 #pragma unroll
-                for (int i = 0; i < NV; ++i) if (v + i * ROW_THREADS < v1) s = add_exps<T>(r[i], c2, off, s);
+                for (int i = 0; i < NV; ++i) if (v + i * ROW_THREADS < v1) t = add_exps<T>(r[i], c2, both(-base * c), t);
+                s = fma2(t, both(give_back(base, c, -base * c)), s);
             }
         }
         p.s = warp_sum(lo(s) + hi(s));
@@ -339,7 +362,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
         const float up = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature, inv = total > 0.f || total != total ? 1.f / total : 0.f;
         T *dz = static_cast<T *>(a.dz) + row * a.d.ld;
         const bool same = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z.row) & 15);
-        const f2 off = both(-shift * c), scale = both(up * inv);
+        const f2 off = both(-shift * c), scale = both(up * inv * give_back(shift, c, -shift * c));
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = mine + i * ROW_THREADS;
@@ -349,7 +372,7 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
         for (int j = threadIdx.x; live && j < k; j += ROW_THREADS) {
             const int i = teacher.index[j], v = (i + z.shift) / VE;
             if (i >= 0 && v >= v0 && v < v1) {
-                const float pj = ex2(fmaf(teacher.z[j], c, -shift * c)) * inv;
+                const float pj = ex2((teacher.z[j] - shift) * c) * inv;
                 dz[i] = from_f<T>(up * (pj - teacher_mass(teacher, k, i)));
             }
         }
@@ -378,8 +401,11 @@ __global__ void __launch_bounds__(BACK_THREADS, 4) distill_backward_kernel(const
     const bool live = *teacher.live;
     const float c = LOG2E / a.d.temperature, lse = a.lse_in[row] * LOG2E;
     // single-precision gradients: what the two factors lose by rounding shows in p, so it is added back
-    const float c_low = float(LOG2E_D / double(a.d.temperature) - double(c)), lse_low = float(double(a.lse_in[row]) * LOG2E_D - double(lse));
-    const auto prob = [&](float x) { return ex2(sizeof(T) == 4 ? fmaf(x, c, -lse) + fmaf(x, c_low, -lse_low) : fmaf(x, c, -lse)); };
+    const float given_low = a.lse_low ? a.lse_low[row] : 0.f;
+    const float c_low = float(LOG2E_D / double(a.d.temperature) - double(c));
+    const float lse_low = float((double(a.lse_in[row]) + double(given_low)) * LOG2E_D - double(lse));
+    const float back = sizeof(T) == 2 && a.lse_low ? give_back_lse(a.lse_in[row], given_low, a.d.temperature, c, -lse) : 1.f;
+    const auto prob = [&](float x) { return sizeof(T) == 4 ? ex2(fmaf(x, c, -lse) + fmaf(x, c_low, -lse_low)) : back * ex2(fmaf(x, c, -lse)); };
     // a row whose logits are all -inf has a log-sum of -inf and no probabilities
     const float up = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature;
     const bool none = a.lse_in[row] == -INFINITY;
@@ -399,7 +425,7 @@ __global__ void __launch_bounds__(BACK_THREADS, 4) distill_backward_kernel(const
                         for (int e = 0; e < VE; ++e) f[e] = f[e] == -INFINITY ? 0.f : up * prob(f[e]);
                         g = pack16<T>(f);
                     } else {
-                        g = scaled_exps<T>(r[i], both(c), both(-lse), both(up));
+                        g = scaled_exps<T>(r[i], both(c), both(-lse), both(up * back));
                     }
                 }
                 z.store(dz, same, w, g);
@@ -627,11 +653,12 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
                 for (int i = 0; i < NV; ++i) if (i < iters) top.take(r[i]);
                 Pair p;
                 p.m = warp_max(top.get());
-                const f2 off = both(p.m == -INFINITY ? 0.f : -p.m * c);
+                const float base = p.m == -INFINITY ? 0.f : p.m;
+                const f2 off = both(-base * c);
                 f2 s = 0ull;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) if (i < iters) s = add_exps<T>(r[i], c2, off, s);
-                p.s = warp_sum(lo(s) + hi(s));
+                p.s = warp_sum(lo(s) + hi(s)) * give_back(base, c, -base * c);
                 // the first block has read every logit that it needs before another block may write over it
                 wait(sync.t_full + b, (n >> 1) & 1);
                 if (lane < ranks) send_pair(&pairs[b][rank * WARPS + warp], sync.x_full + b, p, uint32_t(lane));
@@ -656,16 +683,19 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
             if (MODE != RING_BACKWARD && threadIdx.x == 0) sum_of[b] = Pair{shift, total};
             if constexpr (MODE != RING_FORWARD) {
                 const float up = up_of[b];
-                float inv = 1.f, sub = -shift * c;           // p = inv 2^(z c + sub)
+                float inv = 1.f, sub = -shift * c, back = 1.f;           // p = inv back 2^(z c + sub)
                 bool none = false;
-                if (MODE == RING_STEP) inv = total > 0.f || total != total ? __fdividef(1.f, total) : 0.f;
+                if (MODE == RING_STEP) { inv = total > 0.f || total != total ? __fdividef(1.f, total) : 0.f; back = give_back(shift, c, sub); }
                 else { sub = -lse_of[b] * LOG2E; none = lse_of[b] == -INFINITY; }
                 // single-precision gradients from a saved log-sum: what the factors lose by rounding is added back
                 constexpr bool FINE = MODE == RING_BACKWARD && sizeof(T) == 4;
                 const float c_low = FINE ? float(LOG2E_D / double(a.d.temperature) - double(c)) : 0.f;
-                const float sub_low = FINE ? float(-double(lse_of[b]) * LOG2E_D - double(sub)) : 0.f;
+                const float given_low = MODE == RING_BACKWARD && a.lse_low ? a.lse_low[row] : 0.f;
+                const float sub_low = FINE ? float(-(double(lse_of[b]) + double(given_low)) * LOG2E_D - double(sub)) : 0.f;
+                if (MODE == RING_BACKWARD && !FINE && a.lse_low) back = give_back_lse(lse_of[b], given_low, a.d.temperature, c, sub);
                 const auto prob = [&](float x) {
-                    return x == -INFINITY || none ? 0.f : inv * ex2(FINE ? fmaf(x, c, sub) + fmaf(x, c_low, sub_low) : fmaf(x, c, sub));
+                    if (MODE == RING_STEP) return inv * ex2((x - shift) * c);
+                    return x == -INFINITY || none ? 0.f : FINE ? ex2(fmaf(x, c, sub) + fmaf(x, c_low, sub_low)) : back * ex2(fmaf(x, c, sub));
                 };
                 T *dz = static_cast<T *>(a.dz) + row * a.d.ld, *to = dz + z.first(mine);
                 const bool some = live && !none;
@@ -684,7 +714,7 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
                             for (int e = 0; e < VE; ++e) f[e] = up * prob(f[e]);
                             g = pack16<T>(f);
                         } else {
-                            g = scaled_exps<T>(r[i], c2, both(sub), both(up * inv));
+                            g = scaled_exps<T>(r[i], c2, both(sub), both(up * inv * back));
                         }
                     }
                     if (mine + i * M < v1) {
@@ -824,13 +854,14 @@ template <typename T> cudaError_t step_of(const DistillArgs &a, int num_sms, cud
     bool done;
     cudaError_t e = try_ring<T, RING_STEP>(a, num_sms, st, &done);
     if (done || e != cudaSuccess) return e;
-    constexpr int NV = 8;
+    constexpr int NV = STEP_NV;
     const int vectors = (a.d.vocab + 2 * Lanes<T>::N - 2) / Lanes<T>::N;       // of a row at the worst shift
     int ranks = 1;
     while (ranks < MAX_RANKS && ranks * NV * ROW_THREADS < vectors) ranks *= 2;
     while (ranks < MAX_RANKS && a.d.rows * ranks < 2 * int64_t(num_sms) && vectors > ranks * ROW_THREADS) ranks *= 2;
     if (ranks * NV * ROW_THREADS >= vectors) return launch_rows<T, NV, true>(a, ranks, st);
-    // longer than a cluster's registers: two passes
+    // longer than a cluster's registers: two passes, with the log-sum between them in two parts (one float has ulps of 2^-9
+    // about 30,000, and every probability would be off by as much)
     e = forward_of<T>(a, num_sms, st);
     if (e != cudaSuccess) return e;
     DistillArgs b = a;
@@ -841,6 +872,11 @@ template <typename T> cudaError_t step_of(const DistillArgs &a, int num_sms, cud
 }  // namespace
 
 #define BY_TYPE(call) (a.d.dtype == RUBICK_BF16 ? call<bf16>(a, num_sms, st) : a.d.dtype == RUBICK_F16 ? call<f16>(a, num_sms, st) : call<float>(a, num_sms, st))
+size_t distill_step_scratch(const DistillArgs &a)
+{
+    const int lanes = a.d.dtype == RUBICK_F32 ? 4 : 8;
+    return (a.d.vocab + 2 * lanes - 2) / lanes > MAX_RANKS * STEP_NV * ROW_THREADS ? size_t(a.d.rows) : 0;
+}
 cudaError_t launch_distill_forward(const DistillArgs &a, int num_sms, cudaStream_t st) { return BY_TYPE(forward_of); }
 cudaError_t launch_distill_backward(const DistillArgs &a, int num_sms, cudaStream_t st) { return BY_TYPE(backward_of); }
 cudaError_t launch_distill_step(const DistillArgs &a, int num_sms, cudaStream_t st) { return BY_TYPE(step_of); }

@@ -269,6 +269,10 @@ int rubick_distill_step(rubick_ctx *ctx, const rubick_distill_desc *h_desc, cons
     a.d = *h_desc;
     a.status = ctx->d_status;
     a.z = d_z; a.index = d_index; a.teacher = d_teacher; a.dloss = d_dloss; a.loss = d_loss; a.lse = d_lse; a.dz = d_dz;
+    if (const size_t need = distill_step_scratch(a)) {
+        if ((rc = scratch(ctx, need * sizeof(float)))) return rc;
+        a.lse_low = static_cast<float *>(ctx->d_train);
+    }
     CUDA_TRY(ctx, launch_distill_step(a, ctx->num_sms, ctx->stream), "launch distill_step");
     return RUBICK_OK;
 }

@@ -245,6 +245,7 @@ struct DistillArgs {
     const int32_t *index;
     const float *lse_in, *dloss;
     float *loss, *lse;
+    float *lse_low;              // scratch of a step in two passes: what lse lacks by its rounding
     void *dz;
     uint32_t *status;            // the context's status word
 };
@@ -255,6 +256,7 @@ cudaError_t launch_norm_backward(const NormArgs &a, int num_sms, cudaStream_t st
 int router_chunks(const RouterArgs &a, int num_sms);
 cudaError_t launch_router_forward(const RouterArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_router_backward(const RouterArgs &a, int num_sms, cudaStream_t st);
+size_t distill_step_scratch(const DistillArgs &a);
 cudaError_t launch_distill_forward(const DistillArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_distill_backward(const DistillArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_distill_step(const DistillArgs &a, int num_sms, cudaStream_t st);

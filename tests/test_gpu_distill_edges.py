@@ -33,6 +33,21 @@ def run(ctx, z, index, teacher, desc, up, backward=True):
     return loss, lse, loss2, lse2, both[0], back[0] if backward else None
 
 
+@pytest.mark.parametrize("rows,vocab", [(5, 5000), (32, 50257), (3, 140001), (900, 3001), (170, 64000)])
+@pytest.mark.parametrize("dtype,middle,spread,temperature", [("fp32", 30000.0, 2.0, 1.0), ("fp32", -5000.0, 2.0, 0.5), ("fp16", 2100.0, 4.0, 1.0),
+                                                             ("bf16", 1000.0, 12.0, 1.5)])
+def test_distill_loss_of_rows_far_from_zero(ctx, rows, vocab, dtype, middle, spread, temperature):
+    """A softmax does not change when a row is shifted: neither does the loss's error, whatever the shift's own rounding."""
+    import torch
+    z, index, teacher, desc = ops.distill_case(rows, vocab, 12, dtype, "fp32", temperature=temperature)
+    g = ops.gen(7, rows, vocab)
+    z.copy_(torch.randn(rows, vocab, generator=g) * spread + middle)
+    want = ref.distill(z, index, teacher, temperature)
+    loss, lse, loss2, lse2, both, _ = run(ctx, z, index, teacher, desc, None)
+    for name, got, t in (("loss", loss, "fp32"), ("loss", loss2, "fp32"), ("dz", both, dtype)):
+        ops.close(got, want[name], want["s_" + name], t, 96, name)
+
+
 @pytest.mark.parametrize("vocab", [1, 2, 3, 5, 7, 9])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows,pad,shift", [(3000, 0, 0), (3000, 0, 5), (3000, 2, 3), (3, 0, 1)])
