@@ -210,6 +210,32 @@ template <> struct Top<f16> {
 // product gives it whole, and this factor puts it right once for a sum.
 __device__ __forceinline__ float give_back(float m, float c, float off) { return ex2(-fmaf(m, c, off)); }
 
+// From FAR on |m c| has a remainder that moves exponents out of their range (and is infinite for the lowest values, masks of a
+// whole stretch of the vocabulary): a warp then moves its part of the row to its maximum first, in the row's own type.
+// That is exact for what lies within a factor of two of the maximum; what lies farther has no probability either way.  (The
+// difference before the product for every row cost 1.5 % of the step, and out of line 9 %; this costs 0.3 to 1 %.)  Beyond
+// FARTHEST a remainder is no factor that single precision has.
+constexpr float FAR = 1048576.f, FARTHEST = 1073741824.f;
+// the same answer for the whole warp
+__device__ __forceinline__ bool far_away(float m, float c, float limit = FAR) { return __any_sync(0xffffffffu, !(fabsf(m) * c < limit)); }
+template <typename T> __device__ __forceinline__ uint4 less(const uint4 &r, float m)
+{
+    float v[Lanes<T>::N];
+    unpack16<T>(r, v);
+#pragma unroll
+    for (int e = 0; e < Lanes<T>::N; ++e) v[e] -= m;
+    return pack16<T>(v);
+}
+// A part's exponents towards the row's maximum, z c + sub: of a part that was moved to its own maximum (`far`), and of others,
+// which have no probability, nor a remainder, where the row is far (all -inf, or the row far above them).
+struct Toward { float sub, back; };
+__device__ __forceinline__ Toward toward(float shift, float c, bool far, float own)
+{
+    const float sub = fminf(-shift * c, FARTHEST);
+    const Toward t{sub, far_away(shift, c, FARTHEST) ? 1.f : give_back(shift, c, sub)};
+    return far ? Toward{(own - shift) * c, 1.f} : t;
+}
+
 // Of a log-sum given in two parts: the factor that 2^(z c + sub), sub = -lse log2(e), lacks by the rounding of lse, of c and
 // of sub (near the row's largest logits; what is far below these has little of its own to lose).
 __device__ __forceinline__ float give_back_lse(float lse, float low, float temperature, float c, float sub)
@@ -304,12 +330,19 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
     // takes the loss and so every entry's logit, the others those that they will write
     if (warp == ROW_WARPS - 1) read_teacher<T>(a, row, z, rank ? z.first(v0) : 0, rank ? z.first(v1) : z.vocab, teacher);
     Pair p{-INFINITY, 0.f};
+    bool far = false;             // this warp's part has been moved to its maximum
     {
         Top<T> top;
 #pragma unroll
         for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) top.take(r[i]);
         p.m = warp_max(top.get());
         float base = p.m == -INFINITY ? 0.f : p.m;
+        far = far_away(base, c);
+        if (far) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) r[i] = less<T>(r[i], base);
+            base = 0.f;
+        }
         f2 s = 0ull;
 #pragma unroll
         for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) s = add_exps<T>(r[i], c2, both(-base * c), s);
@@ -327,6 +360,11 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
                 base = m == -INFINITY ? 0.f : m;
                 s = mul2(s, both(ex2((p.m - base) * c)));
                 p.m = m;
+                if (far_away(base, c)) {
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) if (v + i * ROW_THREADS < v1) r[i] = less<T>(r[i], base);
+                    base = 0.f;
+                }
                 f2 t = 0ull;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) if (v + i * ROW_THREADS < v1) t = add_exps<T>(r[i], c2, both(-base * c), t);
@@ -362,7 +400,8 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
         const float up = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature, inv = total > 0.f || total != total ? 1.f / total : 0.f;
         T *dz = static_cast<T *>(a.dz) + row * a.d.ld;
         const bool same = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z.row) & 15);
-        const f2 off = both(-shift * c), scale = both(up * inv * give_back(shift, c, -shift * c));
+        const Toward t = toward(shift, c, far, p.m);
+        const f2 off = both(t.sub), scale = both(up * inv * t.back);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = mine + i * ROW_THREADS;
@@ -647,13 +686,20 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
             __syncwarp();
             if (lane == 0) bar_arrive(sync.empty + st);
             float shift = 0.f, total = 0.f;
+            bool far = false;                                // this warp's part has been moved to its maximum
             if constexpr (MODE != RING_BACKWARD) {
                 Top<T> top;
 #pragma unroll
                 for (int i = 0; i < NV; ++i) if (i < iters) top.take(r[i]);
                 Pair p;
                 p.m = warp_max(top.get());
-                const float base = p.m == -INFINITY ? 0.f : p.m;
+                float base = p.m == -INFINITY ? 0.f : p.m;
+                far = far_away(base, c);
+                if (far) {
+#pragma unroll
+                    for (int i = 0; i < NV; ++i) if (i < iters) r[i] = less<T>(r[i], base);
+                    base = 0.f;
+                }
                 const f2 off = both(-base * c);
                 f2 s = 0ull;
 #pragma unroll
@@ -685,8 +731,15 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
                 const float up = up_of[b];
                 float inv = 1.f, sub = -shift * c, back = 1.f;           // p = inv back 2^(z c + sub)
                 bool none = false;
-                if (MODE == RING_STEP) { inv = total > 0.f || total != total ? __fdividef(1.f, total) : 0.f; back = give_back(shift, c, sub); }
-                else { sub = -lse_of[b] * LOG2E; none = lse_of[b] == -INFINITY; }
+                if (MODE == RING_STEP) {
+                    inv = total > 0.f || total != total ? __fdividef(1.f, total) : 0.f;
+                    const Toward t = toward(shift, c, far, far ? pairs[b][rank * WARPS + warp].m : 0.f);
+                    sub = t.sub;
+                    back = t.back;
+                } else {
+                    sub = -lse_of[b] * LOG2E;
+                    none = lse_of[b] == -INFINITY;
+                }
                 // single-precision gradients from a saved log-sum: what the factors lose by rounding is added back
                 constexpr bool FINE = MODE == RING_BACKWARD && sizeof(T) == 4;
                 const float c_low = FINE ? float(LOG2E_D / double(a.d.temperature) - double(c)) : 0.f;

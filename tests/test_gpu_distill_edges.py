@@ -16,6 +16,17 @@ NINF = float("-inf")
 LOWEST = {"bf16": -3.3895313892515355e38, "fp32": -3.4028234663852886e38, "fp16": -65504.0}
 
 
+def definition(z, index, teacher, temperature, up=None):
+    """The reference on rows moved to their maximum (exactly, in double precision), which changes nothing but the log-sum: at
+    1e30 even a double has no room for the logarithm of a sum beside the logits."""
+    import torch
+    z = z.double().cpu()
+    top = z.max(1, keepdim=True)[0]
+    want = ref.distill(z - top, index, teacher, temperature, up)
+    live = (want["s_lse"] > 0).double()
+    return {**want, "lse": want["lse"] + live * torch.nan_to_num(top[:, 0]) / temperature, "s_lse": want["s_lse"] + live * torch.nan_to_num(top[:, 0]).abs() / temperature}
+
+
 def run(ctx, z, index, teacher, desc, up, backward=True):
     """(loss, lse) of forward, (loss, lse, dz) of the step, dz of backward"""
     import torch
@@ -31,6 +42,25 @@ def run(ctx, z, index, teacher, desc, up, backward=True):
     ops.guarded(both)
     ops.guarded(back)
     return loss, lse, loss2, lse2, both[0], back[0] if backward else None
+
+
+@pytest.mark.parametrize("rows,vocab", [(6, 5000), (4, 50257), (1200, 1003), (2, 270001)])
+@pytest.mark.parametrize("dtype,fill", [("bf16", LOWEST["bf16"]), ("fp32", LOWEST["fp32"]), ("fp32", -1e9), ("fp32", 1e30), ("bf16", -1e6), ("fp16", LOWEST["fp16"])])
+def test_distill_takes_rows_of_one_far_value(ctx, rows, vocab, dtype, fill):
+    """Rows that are all one value, however large, are uniform; so are those whose other half is far below."""
+    import torch
+    z, index, teacher, desc = ops.distill_case(rows, vocab, 12, dtype, "fp32", temperature=2.0)
+    z[0::2] = fill
+    z[1::2] = fill
+    z[1::2, ::2] = fill / 2 if fill < 0 else fill * 1.5
+    index = torch.where((index >= 0) & (index < vocab), index // 2 * 2, index).contiguous()
+    want = definition(z, index, teacher, 2.0)
+    loss, lse, loss2, lse2, both, _ = run(ctx, z, index, teacher, desc, None, backward=vocab > 262144)
+    names = (("loss", loss, "fp32"), ("loss", loss2, "fp32"), ("lse", lse, "fp32"), ("lse", lse2, "fp32"))
+    if vocab <= 262144:                                     # (longer rows have their gradient from the rounded log-sum)
+        names += (("dz", both, dtype),)
+    for name, got, t in names:
+        ops.close(got, want[name], want["s_" + name], t, 96, name)
 
 
 @pytest.mark.parametrize("rows,vocab", [(5, 5000), (32, 50257), (3, 140001), (900, 3001), (170, 64000)])
