@@ -277,7 +277,6 @@ __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.w
 __device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, const Teacher &t, float shift, float total, bool live)
 {
     const int lane = threadIdx.x & 31;
-    const float c = LOG2E / a.d.temperature;
     float log_whole = 0.f, log_rest = log2f(total);
     if (total > 1e-30f && total < 1e30f) {
         const uint32_t bits = __float_as_uint(total);
@@ -285,14 +284,16 @@ __device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, co
         log_rest = log2f(__uint_as_float((bits & 0x007fffffu) | 0x3f800000u));
     }
     float loss = 0.f;
+    // in the logits' own unit: the loss of an entry on the lowest value is a number, the same to the base of two at T = 1 is not
+    const double unit = LN2_D * double(a.d.temperature), log_total = double(log_whole) + double(log_rest);
     for (int j = lane; live && j < a.d.k; j += 32) {
         const float lq = t.log_q[j], zj = t.z[j], q = ex2(lq);
-        const double gap = double(lq) + double(log_whole) - (double(zj) - double(shift)) * double(c) + double(log_rest);
+        const double gap = unit * (double(lq) + log_total) + (double(shift) - double(zj));
         if (t.index[j] >= 0 && !(q == 0.f)) loss = fmaf(q, zj == -INFINITY ? INFINITY : float(gap), loss);
     }
     loss = warp_sum(loss);
     if (lane == 0) {
-        a.loss[row] = live ? a.d.temperature * a.d.temperature * LN2 * loss : 0.f;
+        a.loss[row] = live ? a.d.temperature * loss : 0.f;
         if (a.lse_low) {
             const double lse = live ? double(shift) / double(a.d.temperature) + LN2_D * (double(log_whole) + double(log_rest)) : 0.0;
             a.lse[row] = float(lse);

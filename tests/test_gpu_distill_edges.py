@@ -44,6 +44,37 @@ def run(ctx, z, index, teacher, desc, up, backward=True):
     return loss, lse, loss2, lse2, both[0], back[0] if backward else None
 
 
+# rows per call: a cluster a row, clusters that stay with one, two and eight blocks, rows longer than a cluster
+SHAPES = [(8, 5000, 1.0), (32, 50257, 1.0), (3, 270001, 2.0), (1500, 3000, 0.5), (700, 20011, 2.0), (170, 128000, 1.0), (110, 140001, 1.0)]
+
+
+@pytest.mark.parametrize("rows,vocab,temperature", SHAPES)
+@pytest.mark.parametrize("dtype,fill", [("bf16", LOWEST["bf16"]), ("fp32", LOWEST["fp32"]), ("fp16", LOWEST["fp16"]), ("bf16", -1e10), ("fp32", -1e30),
+                                        ("fp32", -1e7)])
+def test_distill_takes_vocabularies_masked_with_a_finite_value(ctx, rows, vocab, temperature, dtype, fill):
+    """A closed vocabulary: all but the first thousand or so, or a stretch in the middle, at the type's lowest value or a large
+    negative number.  Such places have no probability and no gradient, and the rest is as if they were not there."""
+    import torch
+    if dtype == "fp32" and rows * vocab > 15_000_000:
+        rows = 15_000_000 // vocab
+    z, index, teacher, desc = ops.distill_case(rows, vocab, 12, dtype, "fp32", temperature=temperature)
+    if rows > 2:
+        z[2, 4:7] = 0.5                                     # (no -inf here: losses stay finite)
+    z[0::3, 1100:] = fill
+    z[1::3, vocab // 4: vocab - vocab // 4] = fill
+    index[0::3] %= 1100
+    inner = (index[1::3] >= vocab // 4) & (index[1::3] < vocab - vocab // 4)
+    index[1::3] = torch.where(inner, index[1::3] - vocab // 4, index[1::3])
+    up = (torch.rand(rows, generator=ops.gen(2, rows)) + 0.5).cuda()
+    want = definition(z, index, teacher, temperature, up)
+    loss, lse, loss2, lse2, both, back = run(ctx, z, index, teacher, desc, up)
+    for name, got, t in (("loss", loss, "fp32"), ("lse", lse, "fp32"), ("loss", loss2, "fp32"), ("lse", lse2, "fp32"), ("dz", both, dtype), ("dz", back, dtype)):
+        # (q times the lowest value may lie beyond single precision where T^2 q > T)
+        fine = want[name].abs() <= torch.finfo(torch.float32).max
+        assert torch.equal(torch.isfinite(got.float()).cpu(), fine) and not torch.isnan(got.float()).any(), name
+        ops.close(torch.where(fine.cuda(), got, 0), torch.where(fine, want[name], 0.0), want["s_" + name], t, 96, name)
+
+
 @pytest.mark.parametrize("rows,vocab", [(6, 5000), (4, 50257), (1200, 1003), (2, 270001)])
 @pytest.mark.parametrize("dtype,fill", [("bf16", LOWEST["bf16"]), ("fp32", LOWEST["fp32"]), ("fp32", -1e9), ("fp32", 1e30), ("bf16", -1e6), ("fp16", LOWEST["fp16"])])
 def test_distill_takes_rows_of_one_far_value(ctx, rows, vocab, dtype, fill):
@@ -61,6 +92,22 @@ def test_distill_takes_rows_of_one_far_value(ctx, rows, vocab, dtype, fill):
         names += (("dz", both, dtype),)
     for name, got, t in names:
         ops.close(got, want[name], want["s_" + name], t, 96, name)
+
+
+def test_distill_loss_of_a_masked_entry_is_as_large_as_the_mask(ctx):
+    """A teacher's entry that the student masks with the lowest value costs q times that value, which has a place in
+    single precision where the value times log2(e) has not."""
+    import torch
+    z = torch.randn(2, 600, generator=ops.gen(9)).cuda()
+    z[:, 100:300] = LOWEST["fp32"]
+    index = torch.tensor([[5, 150], [6, 7]], dtype=torch.int32, device="cuda")
+    teacher = torch.tensor([[1.0, 0.5], [1.0, 0.5]], device="cuda")
+    desc = rb.distill(2, 600, 2, torch.float32)
+    want = ref.distill(z, index, teacher, 1.0)
+    loss, lse, loss2, lse2, both, _ = run(ctx, z, index, teacher, desc, None)
+    for got in (loss, loss2):
+        assert torch.isfinite(got).all()
+        ops.close(got, want["loss"], want["s_loss"], "fp32", 96, "loss")
 
 
 @pytest.mark.parametrize("rows,vocab", [(5, 5000), (32, 50257), (3, 140001), (900, 3001), (170, 64000)])
