@@ -125,6 +125,25 @@ def test_distill_loss_of_rows_far_from_zero(ctx, rows, vocab, dtype, middle, spr
         ops.close(got, want[name], want["s_" + name], t, 96, name)
 
 
+def test_distill_infinite_losses_are_infinite(ctx):
+    """Entries on logits of -inf: the loss is +inf, not any other number, in each of the kernels."""
+    import torch
+    for rows, vocab in ((6, 5000), (9, 50257), (2100, 1003), (3, 270001)):
+        z, index, teacher, desc = ops.distill_case(rows, vocab, 6, "bf16", "fp32")
+        z[0, 40:60] = NINF
+        index[0, 0] = 45
+        teacher[0, 0] = 12.0
+        want = ref.distill(z, index, teacher, 1.0)
+        loss, lse, loss2, lse2, both, back = run(ctx, z, index, teacher, desc, None)
+        fine = torch.isfinite(want["loss"])
+        assert not fine[0]
+        for got in (loss, loss2):
+            assert torch.equal(torch.isfinite(got).cpu(), fine)
+            assert torch.equal(got.double().cpu()[~fine], want["loss"][~fine])
+            ops.close(got[fine.cuda()], want["loss"][fine], want["s_loss"][fine], "fp32", 96, "loss")
+        assert torch.isfinite(both.float()).all() and torch.isfinite(back.float()).all()
+
+
 @pytest.mark.parametrize("vocab", [1, 2, 3, 5, 7, 9])
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("rows,pad,shift", [(3000, 0, 0), (3000, 0, 5), (3000, 2, 3), (3, 0, 1)])
