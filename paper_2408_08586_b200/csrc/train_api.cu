@@ -110,7 +110,7 @@ int rubick_block_norm_forward(rubick_ctx *ctx, const rubick_block_norm_desc *h_d
     a.d = *h_desc;
     a.x = d_x; a.y = d_y; a.w_after = d_w_after; a.gate = d_gate; a.w_before = d_w_before;
     a.x_out = d_x_out; a.h = d_h; a.rstd = d_rstd; a.status = ctx->d_status;
-    if (!d_gate) a.d.group_rows = a.d.rows;
+    if (!d_gate || a.d.group_rows > a.d.rows) a.d.group_rows = a.d.rows;
     CUDA_TRY(ctx, launch_norm_forward(a, ctx->num_sms, ctx->stream), "launch block_norm_forward");
     return RUBICK_OK;
 }
@@ -140,7 +140,7 @@ int rubick_block_norm_backward(rubick_ctx *ctx, const rubick_block_norm_desc *h_
     if ((rc = set_device(ctx))) return rc;
     NormArgs a = {};
     a.d = *h_desc;
-    if (!d_gate) a.d.group_rows = a.d.rows;
+    if (!d_gate || a.d.group_rows > a.d.rows) a.d.group_rows = a.d.rows;
     a.x = before ? d_x_out : nullptr; a.y = d_y; a.w_after = d_w_after; a.gate = d_gate; a.w_before = d_w_before;
     a.status = ctx->d_status;
     a.rstd_in = d_rstd; a.dx_out = d_dx_out; a.dh = d_dh;

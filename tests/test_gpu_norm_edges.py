@@ -85,3 +85,21 @@ def test_block_norm_of_rows_shorter_than_a_copy(ctx, rows, pad, shift, cols, dty
     ops.guarded(h)
     got, want = gradients(ctx, s, opt, desc, rows, cols)
     check(got, want, dtype)
+
+
+@pytest.mark.parametrize("group", [2 ** 63 - 1, 2 ** 62 + 5, 2 ** 33, 3001])
+@pytest.mark.parametrize("cols", [768, 515, 16384])
+def test_block_norm_groups_longer_than_the_rows(ctx, group, cols):
+    """A gate row for any number of rows serves all that there are."""
+    import torch
+    rows = 3000 if cols < 16384 else 200
+    s, opt, desc = ops.norm_case(rows, cols, "bf16", "bf16", "one")
+    long = rb.block_norm(rows, cols, torch.bfloat16, eps=1e-5, alpha=0.7, group_rows=group)
+    outs = []
+    for d in (desc, long):
+        x_out, h, rstd = torch.empty_like(s["x"]), torch.empty_like(s["x"]), torch.empty(rows, 2, device="cuda")
+        ctx.block_norm_forward(d, s["x"], s["y"], s["w_after"], s["gate"], s["w_before"], x_out, h, rstd)
+        got, want = gradients(ctx, s, opt, d, rows, cols)
+        check(got, want, "bf16")
+        outs.append([x_out, h, rstd, *got.values()])
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
