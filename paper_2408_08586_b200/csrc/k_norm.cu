@@ -686,7 +686,8 @@ __global__ void __launch_bounds__(512) norm_backward_ring_kernel(const __grid_co
                     d[e] = fma2(f1, x[e], fma2(rb2, mul2(h[e], wb[i][e]), d[e]));           // G
                     const f2 rg = mul2(ra2, d[e]);
                     t[i][e] = fma2(rg, y[e], t[i][e]);
-                    y[e] = fma2(f2y, y[e], mul2(k[i][e], rg));
+                    const f2 du = mul2(k[i][e], rg);
+                    y[e] = after ? fma2(f2y, y[e], du) : du;      // (zero times an infinite y is not zero)
                 }
                 C::store(dx, c, tpr, cols, d);
                 if (block) C::store(dy, c, tpr, cols, y);

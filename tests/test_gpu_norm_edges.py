@@ -103,3 +103,26 @@ def test_block_norm_groups_longer_than_the_rows(ctx, group, cols):
         check(got, want, "bf16")
         outs.append([x_out, h, rstd, *got.values()])
     assert all(torch.equal(a, b) for a, b in zip(*outs))
+
+
+@pytest.mark.parametrize("cols", [512, 771, 16384])
+@pytest.mark.parametrize("before", [False, True])
+def test_block_norm_gradient_beside_an_infinite_activation(ctx, cols, before):
+    """Without a norm after the block, du = alpha g G does not look at y: an infinite y makes its gate's gradient infinite,
+    not its own NaN."""
+    import torch
+    rows = 6
+    s, opt, desc = ops.norm_case(rows, cols, "bf16", "bf16", "token", after=False, before=before)
+    y = s["y"].clone()
+    y[2, 5], y[3, 7] = float("inf"), float("-inf")
+    x_out, rstd = s["x"].clone(), torch.full((rows, 2), 0.5, device="cuda")
+    outs = []
+    for block in (s["y"], y):
+        dx, dy, dg = torch.empty_like(x_out), torch.empty_like(x_out), torch.empty_like(s["gate"])
+        dwb = torch.empty(cols, device="cuda") if before else None
+        ctx.block_norm_backward(desc, x_out if before else None, block, None, s["gate"], s["w_before"], rstd, s["dx_out"], s["dh"], dx, dy, None, dg, dwb)
+        ctx.sync()
+        outs.append((dx, dy, dg))
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    off = ~torch.isfinite(outs[1][2].float())
+    assert off.sum() == 2 and off[2, 5] and off[3, 7]
