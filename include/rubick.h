@@ -446,6 +446,9 @@ int rubick_greedy_round_spread(rubick_ctx *ctx, const rubick_job *d_jobs, int J,
  * held in single precision and every output is rounded to its type once.  Distances between rows (ld_*) are in
  * elements; rows of any alignment are taken, rows on 16-byte boundaries are the fast case.  An output may be the
  * input that a call names as its equal (same address and distance) and must not overlap any other input.
+ * Calls may be captured into a CUDA graph once a call of the same sizes has run outside of the capture; scratch that would
+ * have to grow in one is refused (ESTATE).  Scratch that a graph names stays until rubick_destroy; it is the context's, so
+ * a graph must not run beside other work of the context.
  * rows = 0 is allowed: reductions over no rows are written as zeros.  Results do not depend on the order in which
  * blocks run: there are no floating-point atomics. */
 

@@ -79,7 +79,7 @@ int rubick_create(rubick_ctx **out, const rubick_env *h_env, int device, void *c
     ctx->inc_J = 0; ctx->inc_N = 0; ctx->inc_cur = 0;
     for (int i = 0; i < 2; ++i) { ctx->d_inc_state[i] = nullptr; ctx->d_inc_nodes[i] = nullptr; ctx->cap_inc_state[i] = 0; ctx->cap_inc_nodes[i] = 0; }
     ctx->d_inc_reconf = nullptr; ctx->cap_inc_reconf = 0; ctx->d_inc_jobs = nullptr; ctx->cap_inc_jobs = 0;
-    ctx->d_train = nullptr; ctx->cap_train = 0; ctx->d_tickets = nullptr; ctx->cap_tickets = 0;
+    ctx->d_train = nullptr; ctx->cap_train = 0; ctx->d_tickets = nullptr; ctx->cap_tickets = 0; ctx->n_retired = 0;
     ctx->tile_jobs = 2048;            // 0.5 GB table tile at 2,640 plans x 24 core levels
     cudaDeviceProp prop;
     if (cudaGetDeviceProperties(&prop, device) != cudaSuccess) { delete ctx; return RUBICK_ECUDA; }
@@ -102,6 +102,7 @@ void rubick_destroy(rubick_ctx *ctx)
     cudaFree(ctx->d_top);
     cudaFree(ctx->d_jobs_stage); cudaFree(ctx->d_out_stage); cudaFree(ctx->d_node_stage);
     cudaFree(ctx->d_best_todo); cudaFree(ctx->d_train); cudaFree(ctx->d_tickets);
+    for (int i = 0; i < ctx->n_retired; ++i) cudaFree(ctx->retired[i]);
     for (int i = 0; i < 2; ++i) { cudaFree(ctx->d_inc_state[i]); cudaFree(ctx->d_inc_nodes[i]); }
     cudaFree(ctx->d_inc_reconf); cudaFree(ctx->d_inc_jobs);
     delete ctx;

@@ -109,6 +109,7 @@ struct rubick_ctx {
     size_t cap_inc_state[2], cap_inc_nodes[2], cap_inc_reconf, cap_inc_jobs;
     void *d_train; size_t cap_train;                // scratch of the training-step operators, in bytes
     uint32_t *d_tickets; size_t cap_tickets;        // their arrival counters, zero between calls
+    void *retired[128]; int n_retired;              // what these two were before they grew: captured graphs may name it
     int tile_jobs;                      // job tile of rubick_schedule_round
     int num_sms;
     std::string err;

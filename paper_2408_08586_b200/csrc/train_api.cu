@@ -21,25 +21,48 @@ int set_device(rubick_ctx *ctx)
     return RUBICK_OK;
 }
 
-// scratch of at least `bytes` bytes; earlier work of the stream may still use the old one
+// A new buffer for one that has become too small, twice as large at least, so that there are few of them: the old one is kept
+// until the context goes, since earlier work of the stream and captured graphs may still use it.  In a capture nothing
+// grows (an allocation would end it, and the clearing of counters would become part of the graph).
+int grow(rubick_ctx *ctx, void **ptr, size_t *cap, size_t need, const char *what)
+{
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    CUDA_TRY(ctx, cudaStreamIsCapturing(ctx->stream, &capture), "cudaStreamIsCapturing");
+    if (capture != cudaStreamCaptureStatusNone) return fail(ctx, RUBICK_ESTATE, "training-step operators: scratch would have to grow during a stream capture; make the call once before it");
+    if (*ptr && ctx->n_retired == int(sizeof(ctx->retired) / sizeof(ctx->retired[0]))) return fail(ctx, RUBICK_ENOMEM, "training-step operators: scratch has grown too often");
+    const size_t least = 1 << 16;
+    size_t bytes = need > 2 * *cap ? need : 2 * *cap;
+    if (bytes < least) bytes = least;
+    void *fresh = nullptr;
+    if (cudaMalloc(&fresh, bytes) != cudaSuccess) {
+        (void)cudaGetLastError();
+        bytes = need;
+        CUDA_TRY(ctx, cudaMalloc(&fresh, bytes), what);
+    }
+    if (*ptr) ctx->retired[ctx->n_retired++] = *ptr;
+    *ptr = fresh;
+    *cap = bytes;
+    return RUBICK_OK;
+}
+
+// scratch of at least `bytes` bytes
 int scratch(rubick_ctx *ctx, size_t bytes)
 {
-    if (bytes <= ctx->cap_train) return RUBICK_OK;
-    if (ctx->d_train) { cudaStreamSynchronize(ctx->stream); cudaFree(ctx->d_train); ctx->d_train = nullptr; ctx->cap_train = 0; }
-    CUDA_TRY(ctx, cudaMalloc(&ctx->d_train, bytes), "cudaMalloc (training scratch)");
-    ctx->cap_train = bytes;
-    return RUBICK_OK;
+    return bytes <= ctx->cap_train ? RUBICK_OK : grow(ctx, &ctx->d_train, &ctx->cap_train, bytes, "cudaMalloc (training scratch)");
 }
 
 // arrival counters: zero when they are made, and every launch leaves them zero
 int tickets(rubick_ctx *ctx, size_t n)
 {
     if (n <= ctx->cap_tickets) return RUBICK_OK;
-    if (ctx->d_tickets) { cudaStreamSynchronize(ctx->stream); cudaFree(ctx->d_tickets); ctx->d_tickets = nullptr; ctx->cap_tickets = 0; }
-    CUDA_TRY(ctx, cudaMalloc(reinterpret_cast<void **>(&ctx->d_tickets), n * sizeof(uint32_t)), "cudaMalloc (arrival counters)");
-    const cudaError_t e = cudaMemsetAsync(ctx->d_tickets, 0, n * sizeof(uint32_t), ctx->stream);
-    if (e != cudaSuccess) { cudaFree(ctx->d_tickets); ctx->d_tickets = nullptr; return cuda_fail(ctx, e, "cudaMemsetAsync (arrival counters)"); }
-    ctx->cap_tickets = n;
+    void *fresh = ctx->d_tickets;
+    size_t bytes = ctx->cap_tickets * sizeof(uint32_t);
+    const int rc = grow(ctx, &fresh, &bytes, n * sizeof(uint32_t), "cudaMalloc (arrival counters)");
+    if (rc) return rc;
+    ctx->d_tickets = static_cast<uint32_t *>(fresh);
+    ctx->cap_tickets = 0;                         // (none of them until they are cleared)
+    CUDA_TRY(ctx, cudaMemsetAsync(fresh, 0, bytes, ctx->stream), "cudaMemsetAsync (arrival counters)");
+    ctx->cap_tickets = bytes / sizeof(uint32_t);
     return RUBICK_OK;
 }
 
