@@ -809,14 +809,15 @@ template <typename T, int NV, bool STEP> cudaError_t launch_rows(const DistillAr
     return e;
 }
 
-// How many clusters of `ranks` blocks the GPU holds at once, asked once per kernel and shape.
+// How many clusters of `ranks` blocks the current GPU holds at once, asked once per GPU, kernel and shape.
 template <typename K> int resident_clusters(K kernel, int threads, int smem, int ranks, int num_sms)
 {
-    struct Known { const void *kernel; int smem, ranks, n; };
+    struct Known { const void *kernel; int device, smem, ranks, n; };
     static thread_local Known known[16];
     static thread_local unsigned turn = 0;
-    for (const Known &e : known) if (e.kernel == reinterpret_cast<const void *>(kernel) && e.smem == smem && e.ranks == ranks) return e.n;
-    int n = 0;
+    int device = 0, n = 0;
+    if (cudaGetDevice(&device) != cudaSuccess) { (void)cudaGetLastError(); return 0; }
+    for (const Known &e : known) if (e.kernel == reinterpret_cast<const void *>(kernel) && e.device == device && e.smem == smem && e.ranks == ranks) return e.n;
     if (ranks > 1) {
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(unsigned(num_sms / ranks * ranks));
@@ -832,7 +833,7 @@ template <typename K> int resident_clusters(K kernel, int threads, int smem, int
         if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess) { (void)cudaGetLastError(); n = 0; }
         n *= num_sms;
     }
-    known[turn++ % 16] = Known{reinterpret_cast<const void *>(kernel), smem, ranks, n};
+    known[turn++ % 16] = Known{reinterpret_cast<const void *>(kernel), device, smem, ranks, n};
     return n;
 }
 
