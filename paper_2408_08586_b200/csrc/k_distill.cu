@@ -213,11 +213,11 @@ __device__ __forceinline__ float give_back(float m, float c, float off) { return
 // From FAR on |m c| has a remainder that moves exponents out of their range (and is infinite for the lowest values, masks of a
 // whole stretch of the vocabulary): a warp then moves its part of the row to its maximum first, in the row's own type.
 // That is exact for what lies within a factor of two of the maximum; what lies farther has no probability either way.  (The
-// difference before the product for every row cost 1.5 % of the step, and out of line 9 %; this costs 0.3 to 1 %.)  Beyond
-// FARTHEST a remainder is no factor that single precision has.
+// step over 2,048 rows of 128,000 bf16 takes 243.0 us with this and 241.3 without; 263 with the far sums out of line.)
+// Beyond FARTHEST a remainder is no factor that single precision has.
 constexpr float FAR = 1048576.f, FARTHEST = 1073741824.f;
 // the same answer for the whole warp
-__device__ __forceinline__ bool far_away(float m, float c, float limit = FAR) { return __any_sync(0xffffffffu, !(fabsf(m) * c < limit)); }
+__device__ __forceinline__ bool far_away(float m, float c) { return __any_sync(0xffffffffu, !(fabsf(m) * c < FAR)); }
 template <typename T> __device__ __forceinline__ uint4 less(const uint4 &r, float m)
 {
     float v[Lanes<T>::N];
@@ -226,14 +226,14 @@ template <typename T> __device__ __forceinline__ uint4 less(const uint4 &r, floa
     for (int e = 0; e < Lanes<T>::N; ++e) v[e] -= m;
     return pack16<T>(v);
 }
-// A part's exponents towards the row's maximum, z c + sub: of a part that was moved to its own maximum (`far`), and of others,
-// which have no probability, nor a remainder, where the row is far (all -inf, or the row far above them).
+// A part's exponents towards the row's maximum, z c + sub, and the factor for what sub's rounding took; `moved`: what the part
+// was moved by.  Where the row is far and the part is not, the part has no probability (or is all -inf): sub stays a number then,
+// and the factor one too.
 struct Toward { float sub, back; };
-__device__ __forceinline__ Toward toward(float shift, float c, bool far, float own)
+__device__ __forceinline__ Toward toward(float shift, float c, float moved)
 {
-    const float sub = fminf(-shift * c, FARTHEST);
-    const Toward t{sub, far_away(shift, c, FARTHEST) ? 1.f : give_back(shift, c, sub)};
-    return far ? Toward{(own - shift) * c, 1.f} : t;
+    const float d = shift - moved, sub = fminf(-d * c, FARTHEST);
+    return Toward{sub, ex2(fminf(fmaxf(-fmaf(d, c, sub), -64.f), 64.f))};
 }
 
 // Of a log-sum given in two parts: the factor that 2^(z c + sub), sub = -lse log2(e), lacks by the rounding of lse, of c and
@@ -273,8 +273,10 @@ __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
 
 // Loss and log-sum of a row, by one warp.  log p is a difference of numbers of ten and more that may nearly meet log q: that
-// difference alone is taken in double precision, the logarithm of the sum as exponent and logarithm of the mantissa.
-__device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, const Teacher &t, float shift, float total, bool live)
+// difference alone is taken in double precision, the logarithm of the sum as exponent and logarithm of the mantissa.  LOW: where
+// asked for, the log-sum in two parts (for a forward pass before another; compiled into the step, which has no use for it,
+// it cost 14 of 254 us over 2,048 rows of 128,000).
+template <bool LOW> __device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, const Teacher &t, float shift, float total, bool live)
 {
     const int lane = threadIdx.x & 31;
     float log_whole = 0.f, log_rest = log2f(total);
@@ -294,8 +296,8 @@ __device__ __forceinline__ void write_loss(const DistillArgs &a, int64_t row, co
     loss = warp_sum(loss);
     if (lane == 0) {
         a.loss[row] = live ? a.d.temperature * loss : 0.f;
-        if (a.lse_low) {
-            const double lse = live ? double(shift) / double(a.d.temperature) + LN2_D * (double(log_whole) + double(log_rest)) : 0.0;
+        if (LOW && a.lse_low) {
+            const double lse = live ? (double(shift) + unit * log_total) / double(a.d.temperature) : 0.0;
             a.lse[row] = float(lse);
             a.lse_low[row] = isfinite(float(lse)) ? float(lse - double(float(lse))) : 0.f;
         } else if (a.lse) {
@@ -331,17 +333,17 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
     // takes the loss and so every entry's logit, the others those that they will write
     if (warp == ROW_WARPS - 1) read_teacher<T>(a, row, z, rank ? z.first(v0) : 0, rank ? z.first(v1) : z.vocab, teacher);
     Pair p{-INFINITY, 0.f};
-    bool far = false;             // this warp's part has been moved to its maximum
+    float moved = 0.f;            // what this warp's part has been moved by
     {
         Top<T> top;
 #pragma unroll
         for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) top.take(r[i]);
         p.m = warp_max(top.get());
         float base = p.m == -INFINITY ? 0.f : p.m;
-        far = far_away(base, c);
-        if (far) {
+        if (far_away(base, c)) {
 #pragma unroll
             for (int i = 0; i < NV; ++i) if (mine + i * ROW_THREADS < v1) r[i] = less<T>(r[i], base);
+            moved = base;
             base = 0.f;
         }
         f2 s = 0ull;
@@ -395,13 +397,13 @@ __global__ void __launch_bounds__(ROW_THREADS, 2) distill_row_kernel(const __gri
     total = warp_sum(total);
     const bool live = *teacher.live;
     if (rank == 0 && warp == ROW_WARPS - 1) {
-        write_loss(a, row, teacher, shift, total, live);
+        write_loss<!STEP>(a, row, teacher, shift, total, live);
     }
     if constexpr (STEP) {
         const float up = (a.dloss ? a.dloss[row] : 1.f) * a.d.temperature, inv = total > 0.f || total != total ? 1.f / total : 0.f;
         T *dz = static_cast<T *>(a.dz) + row * a.d.ld;
         const bool same = (reinterpret_cast<uintptr_t>(dz) & 15) == (reinterpret_cast<uintptr_t>(z.row) & 15);
-        const Toward t = toward(shift, c, far, p.m);
+        const Toward t = toward(shift, c, moved);
         const f2 off = both(t.sub), scale = both(up * inv * t.back);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -637,7 +639,7 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
             const int b = n & 1;
             wait(sync.t_empty + b, (n >> 1) & 1);
             if (MODE != RING_BACKWARD && rank == 0)
-                write_loss(a, first_row + int64_t(n) * clusters, teacher_at(b), sum_of[b].m, sum_of[b].s, live_of[b]);
+                write_loss<MODE == RING_FORWARD>(a, first_row + int64_t(n) * clusters, teacher_at(b), sum_of[b].m, sum_of[b].s, live_of[b]);
             __syncwarp();
         };
         for (int n = 0; n < RING_STAGES; ++n) issue(n);
@@ -686,8 +688,7 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
             }
             __syncwarp();
             if (lane == 0) bar_arrive(sync.empty + st);
-            float shift = 0.f, total = 0.f;
-            bool far = false;                                // this warp's part has been moved to its maximum
+            float shift = 0.f, total = 0.f, moved = 0.f;     // moved: what this warp's part of the row has been moved by
             if constexpr (MODE != RING_BACKWARD) {
                 Top<T> top;
 #pragma unroll
@@ -695,10 +696,10 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
                 Pair p;
                 p.m = warp_max(top.get());
                 float base = p.m == -INFINITY ? 0.f : p.m;
-                far = far_away(base, c);
-                if (far) {
+                if (far_away(base, c)) {
 #pragma unroll
                     for (int i = 0; i < NV; ++i) if (i < iters) r[i] = less<T>(r[i], base);
+                    moved = base;
                     base = 0.f;
                 }
                 const f2 off = both(-base * c);
@@ -734,7 +735,7 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
                 bool none = false;
                 if (MODE == RING_STEP) {
                     inv = total > 0.f || total != total ? __fdividef(1.f, total) : 0.f;
-                    const Toward t = toward(shift, c, far, far ? pairs[b][rank * WARPS + warp].m : 0.f);
+                    const Toward t = toward(shift, c, moved);
                     sub = t.sub;
                     back = t.back;
                 } else {
