@@ -65,18 +65,22 @@ ROUTER_RENORM = 1
 MAX_NORM_COLS, MAX_EXPERTS, MAX_CHOSEN, MAX_TEACHER_LOGITS = 16384, 1024, 32, 1024
 
 
-class BlockNormDesc(C.Structure):
+class _OperatorDesc(C.Structure):
+    looked_over = ()        # names of the methods that have seen this descriptor's tensors
+
+
+class BlockNormDesc(_OperatorDesc):
     _fields_ = [("rows", C.c_int64), ("group_rows", C.c_int64), ("ld_x", C.c_int64), ("ld_y", C.c_int64), ("ld_h", C.c_int64),
                 ("ld_gate", C.c_int64), ("cols", C.c_int32), ("dtype", C.c_int32), ("wtype", C.c_int32), ("flags", C.c_uint32),
                 ("eps", C.c_float), ("alpha", C.c_float)]
 
 
-class RouterDesc(C.Structure):
+class RouterDesc(_OperatorDesc):
     _fields_ = [("rows", C.c_int64), ("group_rows", C.c_int64), ("ld", C.c_int64), ("experts", C.c_int32), ("k", C.c_int32),
                 ("dtype", C.c_int32), ("flags", C.c_uint32), ("coef", C.c_float), ("reserved", C.c_int32)]
 
 
-class DistillDesc(C.Structure):
+class DistillDesc(_OperatorDesc):
     _fields_ = [("rows", C.c_int64), ("ld", C.c_int64), ("vocab", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32),
                 ("ttype", C.c_int32), ("temperature", C.c_float), ("reserved", C.c_int32)]
 
@@ -450,40 +454,78 @@ class Context:
 
     # ---- operators of a training step.  Descriptors: block_norm(), router(), distill().  Tensors are the caller's, on
     # ---- this context's device; None where the header allows NULL.  The work goes to the context's stream.
+    # The first call of a method with a descriptor looks its tensors over: their types and device against the descriptor and
+    # the context, and that neighbours in a row are neighbours in memory.  (On every call it is 1 us of 5 for a few tokens;
+    # what such a look finds is in the program, not in the data.)  Sizes and row distances are the descriptor's to state.
+
+    def _look_over(self, desc, method, rows=(), weights=(), teacher=(), floats=(), ints=(), masks=()):
+        import torch
+        types = {BF16: (torch.bfloat16,), F16: (torch.float16,), F32: (torch.float32,)}
+        wtype = getattr(desc, "wtype", desc.dtype)
+        known = desc.dtype in types and wtype in (desc.dtype, F32) and getattr(desc, "ttype", desc.dtype) in types
+        if not known:
+            return                       # the entry point refuses the descriptor
+        for tensors, allowed in ((rows, types[desc.dtype]), (weights, types[wtype]), (teacher, types[getattr(desc, "ttype", desc.dtype)]),
+                                 (floats, (torch.float32,)), (ints, (torch.int32,)), (masks, (torch.uint8, torch.bool))):
+            for x in tensors:
+                if x is None:
+                    continue
+                if x.dtype not in allowed:
+                    raise RubickError(EINVAL, f"{method}: a tensor of type {x.dtype} where the descriptor says {allowed[0]}")
+                if x.get_device() != self.device:
+                    raise RubickError(EINVAL, f"{method}: a tensor on {x.device}, the context is on cuda:{self.device}")
+                if x.dim() and x.shape[-1] > 1 and x.stride(-1) != 1:
+                    raise RubickError(EINVAL, f"{method}: a tensor of strides {tuple(x.stride())}: neighbours in a row have to be neighbours in memory")
+        desc.looked_over += (method,)
 
     def block_norm_forward(self, desc, d_x, d_y, d_w_after, d_gate, d_w_before, d_x_out, d_h, d_rstd=None):
         """rubick_block_norm_forward"""
+        if "block_norm_forward" not in desc.looked_over:
+            self._look_over(desc, "block_norm_forward", rows=(d_x, d_y, d_gate, d_x_out, d_h), weights=(d_w_after, d_w_before), floats=(d_rstd,))
         return self._check(lib().rubick_block_norm_forward(self._h, desc, _addr(d_x), _addr(d_y), _addr(d_w_after), _addr(d_gate),
                                                            _addr(d_w_before), _addr(d_x_out), _addr(d_h), _addr(d_rstd)))
 
     def block_norm_backward(self, desc, d_x_out, d_y, d_w_after, d_gate, d_w_before, d_rstd, d_dx_out, d_dh, d_dx, d_dy,
                             d_dw_after=None, d_dgate=None, d_dw_before=None):
         """rubick_block_norm_backward"""
+        if "block_norm_backward" not in desc.looked_over:
+            self._look_over(desc, "block_norm_backward", rows=(d_x_out, d_y, d_gate, d_dx_out, d_dh, d_dx, d_dy, d_dgate), weights=(d_w_after, d_w_before),
+                            floats=(d_rstd, d_dw_after, d_dw_before))
         return self._check(lib().rubick_block_norm_backward(
             self._h, desc, _addr(d_x_out), _addr(d_y), _addr(d_w_after), _addr(d_gate), _addr(d_w_before), _addr(d_rstd),
             _addr(d_dx_out), _addr(d_dh), _addr(d_dx), _addr(d_dy), _addr(d_dw_after), _addr(d_dgate), _addr(d_dw_before)))
 
     def router_forward(self, desc, d_logits, d_mask, d_index, d_weight, d_counts, d_prob_sum, d_valid, d_loss):
         """rubick_router_forward"""
+        if "router_forward" not in desc.looked_over:
+            self._look_over(desc, "router_forward", rows=(d_logits,), masks=(d_mask,), ints=(d_index, d_counts, d_valid), floats=(d_weight, d_prob_sum, d_loss))
         return self._check(lib().rubick_router_forward(self._h, desc, _addr(d_logits), _addr(d_mask), _addr(d_index), _addr(d_weight),
                                                        _addr(d_counts), _addr(d_prob_sum), _addr(d_valid), _addr(d_loss)))
 
     def router_backward(self, desc, d_logits, d_index, d_weight, d_counts, d_valid, d_dloss, d_dweight, d_dlogits):
         """rubick_router_backward"""
+        if "router_backward" not in desc.looked_over:
+            self._look_over(desc, "router_backward", rows=(d_logits, d_dlogits), ints=(d_index, d_counts, d_valid), floats=(d_weight, d_dloss, d_dweight))
         return self._check(lib().rubick_router_backward(self._h, desc, _addr(d_logits), _addr(d_index), _addr(d_weight), _addr(d_counts),
                                                         _addr(d_valid), _addr(d_dloss), _addr(d_dweight), _addr(d_dlogits)))
 
     def distill_forward(self, desc, d_z, d_index, d_teacher, d_loss, d_lse=None):
         """rubick_distill_forward"""
+        if "distill_forward" not in desc.looked_over:
+            self._look_over(desc, "distill_forward", rows=(d_z,), ints=(d_index,), teacher=(d_teacher,), floats=(d_loss, d_lse))
         return self._check(lib().rubick_distill_forward(self._h, desc, _addr(d_z), _addr(d_index), _addr(d_teacher), _addr(d_loss),
                                                         _addr(d_lse)))
 
     def distill_backward(self, desc, d_z, d_index, d_teacher, d_lse, d_dloss, d_dz):
         """rubick_distill_backward"""
+        if "distill_backward" not in desc.looked_over:
+            self._look_over(desc, "distill_backward", rows=(d_z, d_dz), ints=(d_index,), teacher=(d_teacher,), floats=(d_lse, d_dloss))
         return self._check(lib().rubick_distill_backward(self._h, desc, _addr(d_z), _addr(d_index), _addr(d_teacher), _addr(d_lse),
                                                          _addr(d_dloss), _addr(d_dz)))
 
     def distill_step(self, desc, d_z, d_index, d_teacher, d_dloss, d_loss, d_lse, d_dz):
         """rubick_distill_step"""
+        if "distill_step" not in desc.looked_over:
+            self._look_over(desc, "distill_step", rows=(d_z, d_dz), ints=(d_index,), teacher=(d_teacher,), floats=(d_dloss, d_loss, d_lse))
         return self._check(lib().rubick_distill_step(self._h, desc, _addr(d_z), _addr(d_index), _addr(d_teacher), _addr(d_dloss),
                                                      _addr(d_loss), _addr(d_lse), _addr(d_dz)))
