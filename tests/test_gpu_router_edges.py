@@ -147,3 +147,22 @@ def test_router_gradient_of_many_groups_repeats_itself(ctx):
     dz, size = ref.router_backward(want, 4, 1.0, dweight, **opt)
     ops.close(outs[0], dz, size, "fp32", 64, "dlogits")
     assert all(torch.equal(out, outs[0]) for out in outs)
+
+
+@pytest.mark.parametrize("rows,group", [(40000, 1), (70001, 2)])
+def test_router_gradient_of_groups_that_are_counted_beforehand(ctx, rows, group):
+    import torch
+    z, mask, opt, desc = ops.router_case(rows, 8, 2, "bf16", group=group, masked=rows // 3)
+    groups = -(-rows // group)
+    o = ops.router_outputs(rows, 8, 2, groups)
+    ctx.router_forward(desc, z, mask, o["index"], o["weight"], o["counts"], o["prob_sum"], o["valid"], o["loss"])
+    out, dw = ops.like(z), torch.randn(rows, 2, generator=ops.gen(6)).cuda()
+    ctx.router_backward(desc, z, o["index"], o["weight"], o["counts"], o["valid"], None, dw, out[0])
+    ctx.sync()
+    want = ref.router_forward(z, mask, 2, **opt)
+    assert torch.equal(o["valid"].cpu().long(), want["valid"])
+    loss = torch.tensor([want["loss"]], dtype=torch.float64)
+    ops.close(o["loss"], loss, loss.abs(), "fp32", 64, "loss")
+    dz, size = ref.router_backward(want, 2, 1.0, dw, **opt)
+    ops.close(out[0], dz, size, "bf16", 64, "dlogits")
+    ops.guarded(out)
