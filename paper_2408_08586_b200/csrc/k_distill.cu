@@ -838,8 +838,11 @@ template <typename K> int resident_clusters(K kernel, int threads, int smem, int
     return n;
 }
 
-// The ring, where a row fits the registers of up to eight blocks and every resident cluster gets three rows or more;
-// otherwise *done stays false and nothing is launched.
+// The ring, where a row fits the registers of up to eight blocks and there is a row for every other resident cluster (step over
+// 40 x 128,000 bf16, 48 clusters: 12.8 us against 23.0 by a cluster a row; 120 x 32,000: 11.8 against 20.0; 900 x 5,000:
+// 19.0 against 28.1).  The gradient alone of rows that one block holds, whose parts need nothing of each other, wants three
+// rows a block (1,300 x 5,000: 22.0 against 16.9; 2 blocks, 250 x 32,000: 14.9 against 18.9).  Otherwise *done stays
+// false and nothing is launched.
 template <typename T, int M, int MODE, bool RAGGED> cudaError_t launch_ring(const DistillArgs &a, int vectors, int num_sms, cudaStream_t st, bool *done)
 {
     const int ranks = (vectors + M * RING_NV - 1) / (M * RING_NV), per = (vectors + ranks - 1) / ranks;
@@ -850,7 +853,7 @@ template <typename T, int M, int MODE, bool RAGGED> cudaError_t launch_ring(cons
     // the separate gradient needs no cluster: its parts are blocks that know nothing of each other
     int n = resident_clusters(kernel, M + 32, smem, MODE == RING_BACKWARD ? 1 : ranks, num_sms);
     if (MODE == RING_BACKWARD) n /= ranks;
-    if (n < 1 || a.d.rows < 3 * int64_t(n)) return cudaSuccess;
+    if (n < 1 || (MODE == RING_BACKWARD && ranks == 1 ? a.d.rows < 3 * int64_t(n) : a.d.rows * 2 < n)) return cudaSuccess;
     // the gradient's vectors are stored as z's are read: its rows have to lie in their 16 bytes as z's do
     if (MODE != RING_FORWARD && ((reinterpret_cast<uintptr_t>(a.dz) ^ reinterpret_cast<uintptr_t>(a.z)) & 15)) return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
