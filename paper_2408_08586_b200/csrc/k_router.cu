@@ -758,8 +758,15 @@ RouterShape router_shape(const RouterArgs &a)
     return s;
 }
 
-// groups so many that a warp each fills the SMs
-bool by_warp(const RouterArgs &a, int num_sms) { return a.groups >= int64_t(num_sms) * ROUTER_WARPS * 2; }
+// Groups so many that a warp each does: four to sixteen an SM, more the longer a warp would be at one (a warp against a
+// block each, bf16: 600 groups of 4 x 64 9.7 against 15.4 us, 2,300 of them 11.3 against 37.9; 600 of 40 x 128 23.6
+// against 21.5, 900 28.2 against 27.6, 1,800 29.7 against 44; 600 of 200 x 128 82 against 44, 2,300 104 against 124).
+bool by_warp(const RouterArgs &a, int num_sms)
+{
+    const RouterShape s = router_shape(a);
+    const int64_t passes = (a.d.group_rows * s.lanes + 31) / 32, an_sm = passes / 2;
+    return a.groups >= int64_t(num_sms) * (an_sm < 4 ? 4 : an_sm > 16 ? 16 : an_sm);
+}
 
 template <typename T, bool BACK, int EPL, bool VEC, int LANES> cudaError_t launch_shape(const RouterArgs &a, int num_sms, cudaStream_t st)
 {
