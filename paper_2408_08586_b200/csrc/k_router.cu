@@ -221,10 +221,9 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
     const float off = -shift * 1.4426950408889634f;
     const bool far = __any_sync(0xffffffffu, fabsf(shift) >= FAR);
     f2 e[EPL / 2], sums = 0ull;
-    if (!far) {
 #pragma unroll
-        for (int i = 0; i < EPL / 2; ++i) e[i] = fma2(z[i], both(1.4426950408889634f), both(off));
-    } else {
+    for (int i = 0; i < EPL / 2; ++i) e[i] = fma2(z[i], both(1.4426950408889634f), both(off));
+    if (far) {
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < EPL / 2; ++i) top = fmaxf(top, fmaxf(lo(z[i]), hi(z[i])));
