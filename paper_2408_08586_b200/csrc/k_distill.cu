@@ -11,9 +11,10 @@
 // Bound by memory: 2 bytes a logit forward, 4 for the step in 16-bit types, against one exponential (two for the
 // step) from a pipe that gives 16 a clock and SM.
 //
-// Measured on a B200: step over 2,048 x 128,000 bf16 240 us = 4.3 TB/s (383 with a row a cluster and no ring), the
-// pipe of the exponentials 53 % busy; gradient alone 1,000 x 32,000 fp16 33 us = 3.8 TB/s; forward 32 x 50,257 bf16 10 us,
-// the time of the teacher's two dependent reads and a barrier.
+// Measured on a B200: step over 2,048 x 128,000 bf16, 48 rows padding, 242 us = 4.3 TB/s (383 with a row a cluster and no
+// ring), the pipe of the exponentials 53 % and the issue slots 51 % busy; gradient alone 1,000 x 32,000 fp16 33 us = 3.8
+// TB/s, its warps waiting for copies (38 % of the warps an SM can hold, two stages a block); forward 2,048 x 128,000 bf16
+// 153 us = 3.4 TB/s; 32 x 50,257 bf16 10 us, the time of the teacher's two dependent reads and a barrier.
 
 #include <cooperative_groups.h>
 

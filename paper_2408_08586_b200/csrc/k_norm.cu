@@ -12,12 +12,14 @@
 //   D m2 = sum q (dx' + b e) - b m1 sum q xh,
 // and the three sums (e xh, q (dx' + b e), q xh) come from one reduction: one barrier a row instead of two.
 //
-// All of it is bound by memory: 4 row elements move per column forward, 6 backward, for a dozen operations.  A row
-// stays in the registers of one warp or one block between its loads and its stores.
+// 4 row elements move per column forward, 6 backward, for a dozen operations: the floor is memory's.  Many rows travel
+// through a ring of shared-memory stages; few rows forward stay in the registers of a warp or a block between their loads and
+// their stores; rows too wide for the ring backward are read twice.
 //
 // Measured on a B200 (6.54 TB/s copy): forward 8,192 x 5,120 bf16 71 us = 4.7 TB/s, backward 16,384 x 4,096 bf16
-// 151 us = 5.3 TB/s with its join, 2,048 x 1,280 fp16 24 us (13 the rows, 8 the join: few rows are few bytes, and what is
-// left is the time of one row's trip); 1,000 x 1,537 fp32 forward 8.2 us; four rows 5 us.
+// 151 us = 5.3 TB/s with its join, 2,048 x 1,280 fp16 24 us (13 the rows, 8 the join, which reads again what 683 runs of
+// three rows have left: 10 MB beside 31 MB of rows); 1,000 x 1,537 fp32 forward 8.2 us; four rows 5 us; over 8,192 columns
+// 2,048 x 16,384 bf16 forward 129 us = 2.1 TB/s, backward 520 us = 0.8 TB/s (one block of 512 threads an SM, every row twice).
 
 #include "train_common.cuh"
 

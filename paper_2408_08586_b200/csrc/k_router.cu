@@ -20,10 +20,11 @@
 // 65,536 of them.)  Sixteen elements a lane: fewer leave the steps that a warp's rows share to fewer rows, more make the
 // sort dear.
 //
-// Bound by instruction issue, not by memory: four rows of 128 experts are 2 KB, and some 790 instructions of a warp, half
-// of them for keys, sort and choice.  65,536 x 128 fp32, 8 chosen: 33 us = 1.1 TB/s; three blocks an SM instead of two
-// spill and take as long.  Backward, 131,072 x 256 bf16: 39 us = 3.8 TB/s.  512 x 8 bf16: 6 us, most of it the joins'
-// waiting for one another.
+// Bound by the latency of one chain, not by memory: four rows of 128 experts are 2 KB and some 800 instructions of a warp, half
+// of them for keys, sort and choice, and the choice is k steps of shuffles, a comparison and a load from shared memory that
+// wait for one another.  3.7 warps a scheduler, as their registers allow, fill 47 % of the issue slots.  65,536 x 128 fp32, 8
+// chosen: 33 us = 1.1 TB/s; three blocks an SM instead of two spill and take as long.  Backward, 131,072 x 256 bf16: 39 us =
+// 3.8 TB/s, 65 % of the issue slots.  512 x 8 bf16: 6 us, most of it the joins' waiting for one another.
 //
 // Probability sums stay in the lane that owns the column until its chunk of rows ends, then go chunk by chunk, in order,
 // into the group's sum: the last block of a group to arrive adds them up, the last of all the loss.  Where groups are
@@ -214,7 +215,7 @@ __device__ __forceinline__ void route_rows(const RouterArgs &a, int64_t row, boo
     // The exponents are taken against what the keys leave of the largest logit, times log2(e) and rounded: both are off by a
     // share of the logit, the same for the whole row, which divides out again.  From FAR on that share could move an exponent
     // out of its range (of a few million, and infinite for the lowest values): then against the largest logit itself, the
-    // differences before the product.  (Always so: 2 to 4 % more for 65,536 x 128 fp32, 33 us.)
+    // differences before the product.  (Always so: 2 to 4 % more for 65,536 x 128 fp32, 33 us; this costs nothing.)
     constexpr float FAR = 1024.f;
     const uint32_t cut = first & ~low;
     float shift = some ? __uint_as_float(cut & 0x80000000u ? cut & 0x7fffffffu : ~(cut | low)) : 0.f;

@@ -6,6 +6,10 @@ at hand: a block, a mixture of experts and a distillation head, with the block n
 and the distillation loss of ``include/rubick.h`` between them, forward and backward.  The blocks themselves are plain
 matrix products by torch (a job's own framework would run its own); everything between them is the library's.
 
+It is a sample of how the operators are used together, not a model: a block here is one product, without attention, and
+measure() scales such layers up.  A job's own tau and k_bwd come from a profile of the job itself, and its coefficients
+from rubick_fit_models.
+
     x0 -> norm -> block -> [norm, gate, + alpha, norm] -> router -> experts -> [norm, gate, + alpha, norm] -> head -> loss
 """
 import torch
