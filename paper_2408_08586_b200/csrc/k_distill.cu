@@ -746,12 +746,10 @@ __global__ void __launch_bounds__(M + 32, M == 256 ? 3 : 1) distill_ring_kernel(
                 // single-precision gradients from a saved log-sum: what the factors lose by rounding is added back
                 constexpr bool FINE = MODE == RING_BACKWARD && sizeof(T) == 4;
                 const float c_low = FINE ? float(LOG2E_D / double(a.d.temperature) - double(c)) : 0.f;
-                const float given_low = MODE == RING_BACKWARD && a.lse_low ? a.lse_low[row] : 0.f;
-                const float sub_low = FINE ? float(-(double(lse_of[b]) + double(given_low)) * LOG2E_D - double(sub)) : 0.f;
-                if (MODE == RING_BACKWARD && !FINE && a.lse_low) back = give_back_lse(lse_of[b], given_low, a.d.temperature, c, sub);
+                const float sub_low = FINE ? float(-double(lse_of[b]) * LOG2E_D - double(sub)) : 0.f;
                 const auto prob = [&](float x) {
                     if (MODE == RING_STEP) return inv * ex2((x - shift) * c);
-                    return x == -INFINITY || none ? 0.f : FINE ? ex2(fmaf(x, c, sub) + fmaf(x, c_low, sub_low)) : back * ex2(fmaf(x, c, sub));
+                    return x == -INFINITY || none ? 0.f : ex2(FINE ? fmaf(x, c, sub) + fmaf(x, c_low, sub_low) : fmaf(x, c, sub));
                 };
                 T *dz = static_cast<T *>(a.dz) + row * a.d.ld, *to = dz + z.first(mine);
                 const bool some = live && !none;
