@@ -880,7 +880,10 @@ template <typename T, int MODE> cudaError_t try_ring(const DistillArgs &a, int n
     return cudaSuccess;
 }
 
-// blocks of a row: a power of two up to 8
+// Blocks of a row: a power of two up to 8, more while they leave half of the SMs without one (step over 60 x 32,000 bf16: 10.8 us,
+// 22.0 with two blocks an SM for the limit; 32 x 50,257 11.8 and 13.8; 8 x 128,000 11.8 both).
+constexpr int cluster_limit(int num_sms) { return num_sms / 2; }
+
 template <typename T> cudaError_t forward_of(const DistillArgs &a, int num_sms, cudaStream_t st)
 {
     bool done;
@@ -888,7 +891,7 @@ template <typename T> cudaError_t forward_of(const DistillArgs &a, int num_sms, 
     if (done || e != cudaSuccess) return e;
     const int vectors = a.d.vocab / Lanes<T>::N + 2;
     int ranks = 1;
-    while (ranks < MAX_RANKS && a.d.rows * ranks < 2 * int64_t(num_sms) && vectors > ranks * ROW_THREADS) ranks *= 2;
+    while (ranks < MAX_RANKS && a.d.rows * ranks < cluster_limit(num_sms) && vectors > ranks * ROW_THREADS) ranks *= 2;
     return launch_rows<T, 4, false>(a, ranks, st);
 }
 
@@ -898,9 +901,10 @@ template <typename T> cudaError_t backward_of(const DistillArgs &a, int num_sms,
     const cudaError_t e = try_ring<T, RING_BACKWARD>(a, num_sms, st, &done);
     if (done || e != cudaSuccess) return e;
     const int64_t vectors = a.d.vocab / Lanes<T>::N + 2;
-    // up to 32 KB of z a block; less where that does not fill the SMs twice over
+    // up to 32 KB of z a block; less where that leaves SMs without a block (20 x 128,000 bf16: 9.7 us, 12.8 with eight blocks an SM
+    // for the limit, each of which reads the teacher; 60 x 32,000 7.7 and 10.8)
     int64_t parts = (vectors + 8 * BACK_THREADS - 1) / (8 * BACK_THREADS);
-    while (parts * a.d.rows < 8 * int64_t(num_sms) && parts * BACK_THREADS < vectors) parts *= 2;
+    while (parts * a.d.rows < int64_t(num_sms) && parts * BACK_THREADS < vectors) parts *= 2;
     if (parts * a.d.rows > 0x7fffffff) parts = 0x7fffffff / a.d.rows;
     distill_backward_kernel<T><<<unsigned(a.d.rows * parts), BACK_THREADS, 0, st>>>(a, int(parts));
     count_launch();
@@ -916,7 +920,7 @@ template <typename T> cudaError_t step_of(const DistillArgs &a, int num_sms, cud
     const int vectors = (a.d.vocab + 2 * Lanes<T>::N - 2) / Lanes<T>::N;       // of a row at the worst shift
     int ranks = 1;
     while (ranks < MAX_RANKS && ranks * NV * ROW_THREADS < vectors) ranks *= 2;
-    while (ranks < MAX_RANKS && a.d.rows * ranks < 2 * int64_t(num_sms) && vectors > ranks * ROW_THREADS) ranks *= 2;
+    while (ranks < MAX_RANKS && a.d.rows * ranks < cluster_limit(num_sms) && vectors > ranks * ROW_THREADS) ranks *= 2;
     if (ranks * NV * ROW_THREADS >= vectors) return launch_rows<T, NV, true>(a, ranks, st);
     // longer than a cluster's registers: two passes, with the log-sum between them in two parts (one float has ulps of 2^-9
     // about 30,000, and every probability would be off by as much)
