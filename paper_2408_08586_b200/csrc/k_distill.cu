@@ -14,7 +14,7 @@
 // Measured on a B200: step over 2,048 x 128,000 bf16, 48 rows padding, 242 us = 4.3 TB/s (383 with a row a cluster and no
 // ring), the pipe of the exponentials 53 % and the issue slots 51 % busy; gradient alone 1,000 x 32,000 fp16 33 us = 3.8
 // TB/s, its warps waiting for copies (38 % of the warps an SM can hold, two stages a block); forward 2,048 x 128,000 bf16
-// 153 us = 3.4 TB/s; 32 x 50,257 bf16 10 us, the time of the teacher's two dependent reads and a barrier.
+// 153 us = 3.4 TB/s; 32 x 50,257 bf16 8.2 us, the time of the teacher's two dependent reads and a barrier.
 
 #include <cooperative_groups.h>
 
@@ -838,10 +838,10 @@ template <typename K> int resident_clusters(K kernel, int threads, int smem, int
 }
 
 // The ring, where a row fits the registers of up to eight blocks and there is a row for every other resident cluster (step over
-// 40 x 128,000 bf16, 48 clusters: 12.8 us against 23.0 by a cluster a row; 120 x 32,000: 11.8 against 20.0; 900 x 5,000:
-// 19.0 against 28.1).  The gradient alone of rows that one block holds, whose parts need nothing of each other, wants three
-// rows a block (1,300 x 5,000: 22.0 against 16.9; 2 blocks, 250 x 32,000: 14.9 against 18.9).  Otherwise *done stays
-// false and nothing is launched.
+// 40 x 128,000 bf16, 48 clusters: 12.8 us against 15.8 by a cluster a row; 100 x 128,000: 20 against 25; 900 x 5,000: 19
+// against 27; 24 x 128,000 and 120 x 32,000: 11.8 both).  The gradient alone of rows that one block holds, whose parts need
+// nothing of each other, wants three rows a block (900 x 5,000: 17.5 against 12.8; longer rows, 100 x 128,000: 14.9 against
+// 17.9, 250 x 32,000: 14.9 against 13.2).  Otherwise *done stays false and nothing is launched.
 template <typename T, int M, int MODE, bool RAGGED> cudaError_t launch_ring(const DistillArgs &a, int vectors, int num_sms, cudaStream_t st, bool *done)
 {
     const int ranks = (vectors + M * RING_NV - 1) / (M * RING_NV), per = (vectors + ranks - 1) / ranks;

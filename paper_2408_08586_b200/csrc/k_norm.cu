@@ -851,8 +851,8 @@ Shape forward_shape(const NormArgs &a, int num_sms)
     Shape s;
     const int es = esize_of(a.d.dtype);
     s.ve = vectors_fit(a, es) ? 16 / es : 1;
-    // a ring has to be filled before it runs: two rows a resident block (with a block each, 600 x 4,096 bf16: 12.3 us against 20.5
-    // in registers, 2,400 x 1,280 12.3 against 17.4; with one, 300 x 4,096: 10.2 against 9.2)
+    // a ring has to be filled before it runs: two rows a resident block (2,400 x 1,280 bf16: 12.8 us against 18.9 in registers, 600 x
+    // 4,096 12.8 against 13.8, 2,000 x 1,537 23 against 60; with one row a block, 3,000 x 256: 8.7 against 7.7)
     s.ring = ring_shape(a, false, num_sms, s) && a.d.rows >= int64_t(num_sms) * s.blocks * 2;
     if (s.ring) return s;
     const int most = 32 / s.ve, nvec = (a.d.cols + s.ve - 1) / s.ve;
