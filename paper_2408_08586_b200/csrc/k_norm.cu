@@ -846,14 +846,23 @@ void keep_groups(const NormArgs &a, int64_t *chunk_rows, int *n_chunks)
     *n_chunks = int((a.d.rows + *chunk_rows - 1) / *chunk_rows);
 }
 
+// Forward rows that a resident block of the ring has to have, in halves: a ring has to be filled before it runs, and narrow rows do
+// well in registers.  Ring against registers, bf16: 9,500 x 256 12.8 us and 11.7, 12,000 x 256 12.8 and 13.8; 4,800 x 512 12.8
+// and 11.8, 6,000 x 512 12.8 and 13.8; 1,480 x 1,280 10.8 and 12.8; 2,400 x 4,096 22 and 46.  Rows at odd addresses:
+// 20,000 x 125 28 and 17; 3,000 x 300 17 and 12, 4,800 x 300 21 and 42; 2,000 x 615 18 and 15, 3,000 x 615 22 and 50;
+// 740 x 1,030 15 and 13, 1,480 x 1,030 19 and 45.
+int64_t ring_halves(const NormArgs &a, const Shape &s)
+{
+    if (s.ring_vec) return s.tpr > 64 ? 2 : s.tpr == 32 && s.nv == 1 ? 8 : 4;
+    return a.d.cols <= 128 ? int64_t(1) << 31 : s.tpr > 32 ? 3 : 4;
+}
+
 Shape forward_shape(const NormArgs &a, int num_sms)
 {
     Shape s;
     const int es = esize_of(a.d.dtype);
     s.ve = vectors_fit(a, es) ? 16 / es : 1;
-    // a ring has to be filled before it runs: two rows a resident block (2,400 x 1,280 bf16: 12.8 us against 18.9 in registers, 600 x
-    // 4,096 12.8 against 13.8, 2,000 x 1,537 23 against 60; with one row a block, 3,000 x 256: 8.7 against 7.7)
-    s.ring = ring_shape(a, false, num_sms, s) && a.d.rows >= int64_t(num_sms) * s.blocks * 2;
+    s.ring = ring_shape(a, false, num_sms, s) && 2 * a.d.rows >= int64_t(num_sms) * s.blocks * ring_halves(a, s);
     if (s.ring) return s;
     const int most = 32 / s.ve, nvec = (a.d.cols + s.ve - 1) / s.ve;
     int warps = (nvec + most * 32 - 1) / (most * 32);
