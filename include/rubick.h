@@ -571,6 +571,110 @@ int rubick_distill_backward(rubick_ctx *ctx, const rubick_distill_desc *h_desc, 
 int rubick_distill_step(rubick_ctx *ctx, const rubick_distill_desc *h_desc, const void *d_z, const int32_t *d_index,
                         const void *d_teacher, const float *d_dloss, float *d_loss, float *d_lse, void *d_dz);
 
+/* ---- products, dropout and cross entropy of a training step ------------------------------------
+ * What surrounds the operators above in a step: the matrix products with what hangs on them, dropout, and the training
+ * loss at the head.  The conventions of the operators above hold.
+ *
+ * Dropout's mask is never stored: forward and backward make it from {seed, offset}, two 64-bit numbers in device memory
+ * (d_seed, 8-byte aligned), so that a captured graph draws anew once they have been changed.  Element (row, col) is kept when
+ * word col % 4 of Philox4x32-10 (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011) at the counter
+ * (col / 4, row, offset's lower half, its upper half) under the key (seed's lower half, its upper half) is at least p 2^32;
+ * what is kept is divided by 1 - p.  drop(v) below is v / (1 - p) or, whatever v is, 0.  Calls of equal sizes that are to
+ * differ need another offset. */
+
+/* flag of rubick_linear_desc and rubick_head_loss_desc */
+#define RUBICK_WEIGHT_BY_OUTPUT  1u   /* the weight has a row per output, [outputs][inputs], not [inputs][outputs] */
+
+/* activations of rubick_linear_desc */
+#define RUBICK_ACT_NONE       0
+#define RUBICK_ACT_RELU       1
+#define RUBICK_ACT_GELU       2       /* v Phi(v)                                                     */
+#define RUBICK_ACT_GELU_TANH  3       /* v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2             */
+#define RUBICK_ACT_SILU       4       /* v / (1 + exp(-v))                                             */
+
+#define RUBICK_MAX_FEATURES   (1 << 24)   /* inputs, outputs, hidden                                   */
+
+typedef struct {
+    int64_t rows;                /* tokens, below 2^31                                                       */
+    int64_t ld_x, ld_w;          /* distance between rows of x, dx / of w, dw                                 */
+    int64_t ld_out, ld_res, ld_pre;   /* ... of out, dout / residual / pre                                    */
+    int32_t inputs, outputs;     /* 1 .. RUBICK_MAX_FEATURES                                                  */
+    int32_t dtype;               /* RUBICK_BF16 or RUBICK_F16 (the tensor cores' operands): every tensor but the biases */
+    int32_t btype;               /* type of the bias: dtype or RUBICK_F32                                     */
+    uint32_t flags;
+    int32_t activation;          /* RUBICK_ACT_*                                                              */
+    float   p;                   /* probability that dropout takes an element, 0 <= p < 1                      */
+    int32_t reserved;            /* 0                                                                         */
+} rubick_linear_desc;
+
+/* Matrix product with bias, activation, dropout and residual:
+ *     z = x W + bias          out = residual + drop(act(z))
+ * d_bias and d_residual may be NULL; d_pre (optional) receives z for the backward pass (act is taken from z before it is
+ * rounded).  d_seed is read where p > 0 and may be NULL otherwise.  d_out may equal d_residual.  Products are summed in
+ * single precision.  Rows of x and w on 16-byte boundaries are read as they lie; others are laid out anew in the context's
+ * scratch first.  Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
+int rubick_linear_forward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, const void *d_x, const void *d_w,
+                          const void *d_bias, const void *d_residual, const uint64_t *d_seed, void *d_pre, void *d_out);
+
+/* Gradients of the same product:  dz = act'(pre) drop(dout),  dx = dz W^T,  dw = x^T dz (laid out as w),  dbias = sum of dz
+ * over the rows (float [outputs], from dz before it is rounded).  d_pre (what forward wrote) may be NULL without an
+ * activation.  Each of d_dx, d_dw, d_dbias may be NULL: it is not computed (d_w and d_x may be NULL with d_dx and d_dw).
+ * The residual's gradient is dout itself.  dz is rounded to dtype for the two products; the context keeps it in scratch
+ * (rows x outputs).  rows = 0 writes zeros to dw and dbias.  Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
+int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, const void *d_x, const void *d_w,
+                           const void *d_pre, const uint64_t *d_seed, const void *d_dout, void *d_dx, void *d_dw,
+                           float *d_dbias);
+
+typedef struct {
+    int64_t rows;                /* tokens, below 2^31                                                       */
+    int64_t ld_x, ld_res, ld_out;    /* distance between rows of x, dx / residual / out, dout                  */
+    int32_t cols;                /* 1 .. RUBICK_MAX_FEATURES                                                  */
+    int32_t dtype;               /* type of every tensor                                                      */
+    float   p;                   /* 0 <= p < 1                                                                */
+    int32_t reserved;            /* 0                                                                         */
+} rubick_dropout_desc;
+
+/* out = residual + drop(x); d_residual may be NULL.  d_out may equal d_x or d_residual.  d_seed may be NULL where p = 0.
+ * Errors: EINVAL, ECUDA. */
+int rubick_dropout_forward(rubick_ctx *ctx, const rubick_dropout_desc *h_desc, const uint64_t *d_seed, const void *d_x,
+                           const void *d_residual, void *d_out);
+
+/* dx = drop(dout), under the {seed, offset} of forward (the residual's gradient is dout itself).  d_dx may equal d_dout.
+ * Errors: EINVAL, ECUDA. */
+int rubick_dropout_backward(rubick_ctx *ctx, const rubick_dropout_desc *h_desc, const uint64_t *d_seed, const void *d_dout,
+                            void *d_dx);
+
+typedef struct {
+    int64_t rows;                /* tokens, below 2^31                                                       */
+    int64_t ld_h, ld_w;          /* distance between rows of h, dh / of w, dw                                 */
+    int32_t hidden;              /* 1 .. RUBICK_MAX_FEATURES                                                  */
+    int32_t vocab;               /* 1 .. 2^30                                                                 */
+    int32_t dtype;               /* RUBICK_BF16 or RUBICK_F16: h, w and their gradients                        */
+    uint32_t flags;
+} rubick_head_loss_desc;
+
+/* Softmax cross entropy of a head's logits z = h W against one label per row, in pieces of the vocabulary: the logits are
+ * never in memory.
+ *     d_lse[n] = log sum_v exp(z_nv)          d_loss[n] = lse - z_{n, label n}
+ * Both are 0 for a row whose label (int32) is outside 0 .. vocab - 1 (padding), whatever its h holds.  d_lse is optional.
+ * A row with a NaN or +inf logit gets NaN.  The context keeps 8 bytes per row and 128 tokens of the vocabulary.
+ * Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
+int rubick_head_loss_forward(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,
+                             const int32_t *d_label, float *d_loss, float *d_lse);
+
+/* dz = d_dloss[n] (exp(z - lse) - onehot(label)),  dh = dz W^T,  dw = h^T dz (laid out as w), with forward's d_lse; rows
+ * without a label add nothing and get zeros.  d_dloss NULL = 1.  d_dh or d_dw may be NULL: it is not computed.  The logits
+ * are computed again, a piece of the vocabulary at a time; dz of a piece is rounded to dtype under a common power of two.
+ * The context keeps the piece (up to 256 MB, or 128 tokens), a copy of h and, with several pieces, dh in single precision.
+ * d_lse is one float: rows whose logits are all far from zero want the step below.  rows = 0 writes zeros to dw.
+ * Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
+int rubick_head_loss_backward(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,
+                              const int32_t *d_label, const float *d_lse, const float *d_dloss, void *d_dh, void *d_dw);
+
+/* Both at once, for a loss whose weight per row is known beforehand.  Outputs as theirs; d_lse is optional here too. */
+int rubick_head_loss_step(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,
+                          const int32_t *d_label, const float *d_dloss, float *d_loss, float *d_lse, void *d_dh, void *d_dw);
+
 /* ---- measurement aids (the paper has no counterpart) ------------------------------------------- */
 
 #define RUBICK_PROBE_WRITE 0   /* float4 streaming stores over d_buf:            work = bytes written        */

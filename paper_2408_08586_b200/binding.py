@@ -62,6 +62,9 @@ MAX_PIECES = 32
 BF16, F16, F32 = 0, 1, 2
 NORM_AFTER, NORM_BEFORE, NORM_UNIT_OFFSET, NORM_TANH_GATE = 1, 2, 4, 8
 ROUTER_RENORM = 1
+WEIGHT_BY_OUTPUT = 1
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+MAX_FEATURES = 1 << 24
 MAX_NORM_COLS, MAX_EXPERTS, MAX_CHOSEN, MAX_TEACHER_LOGITS = 16384, 1024, 32, 1024
 
 
@@ -83,6 +86,22 @@ class RouterDesc(_OperatorDesc):
 class DistillDesc(_OperatorDesc):
     _fields_ = [("rows", C.c_int64), ("ld", C.c_int64), ("vocab", C.c_int32), ("k", C.c_int32), ("dtype", C.c_int32),
                 ("ttype", C.c_int32), ("temperature", C.c_float), ("reserved", C.c_int32)]
+
+
+class LinearDesc(_OperatorDesc):
+    _fields_ = [("rows", C.c_int64), ("ld_x", C.c_int64), ("ld_w", C.c_int64), ("ld_out", C.c_int64), ("ld_res", C.c_int64),
+                ("ld_pre", C.c_int64), ("inputs", C.c_int32), ("outputs", C.c_int32), ("dtype", C.c_int32), ("btype", C.c_int32),
+                ("flags", C.c_uint32), ("activation", C.c_int32), ("p", C.c_float), ("reserved", C.c_int32)]
+
+
+class DropoutDesc(_OperatorDesc):
+    _fields_ = [("rows", C.c_int64), ("ld_x", C.c_int64), ("ld_res", C.c_int64), ("ld_out", C.c_int64), ("cols", C.c_int32),
+                ("dtype", C.c_int32), ("p", C.c_float), ("reserved", C.c_int32)]
+
+
+class HeadLossDesc(_OperatorDesc):
+    _fields_ = [("rows", C.c_int64), ("ld_h", C.c_int64), ("ld_w", C.c_int64), ("hidden", C.c_int32), ("vocab", C.c_int32),
+                ("dtype", C.c_int32), ("flags", C.c_uint32)]
 
 
 def _type_code(dtype):
@@ -120,6 +139,32 @@ def distill(rows, vocab, k, dtype, ttype=None, *, temperature=1.0, ld=None):
                        _type_code(dtype if ttype is None else ttype), float(temperature), 0)
 
 
+def linear(rows, inputs, outputs, dtype, btype=None, *, activation="none", p=0.0, by_output=False, ld_x=None, ld_w=None,
+           ld_out=None, ld_res=None, ld_pre=None):
+    """rubick_linear_desc.  btype: type of the bias (None: as dtype); p: dropout; by_output: the weight is [outputs, inputs].
+    ld_*: distances between rows (None: without gaps; ld_res and ld_pre as ld_out)."""
+    ld_out = int(outputs) if ld_out is None else int(ld_out)
+    wide = int(inputs if by_output else outputs)
+    return LinearDesc(int(rows), int(inputs) if ld_x is None else int(ld_x), wide if ld_w is None else int(ld_w), ld_out,
+                      ld_out if ld_res is None else int(ld_res), ld_out if ld_pre is None else int(ld_pre), int(inputs), int(outputs),
+                      _type_code(dtype), _type_code(dtype if btype is None else btype), WEIGHT_BY_OUTPUT * bool(by_output),
+                      ACTIVATIONS[activation] if isinstance(activation, str) else int(activation), float(p), 0)
+
+
+def dropout(rows, cols, dtype, *, p, ld=None, ld_x=None, ld_res=None, ld_out=None):
+    """rubick_dropout_desc.  ld: distance between rows of every tensor (None: cols), ld_x / ld_res / ld_out where they differ."""
+    ld = int(cols) if ld is None else int(ld)
+    return DropoutDesc(int(rows), ld if ld_x is None else int(ld_x), ld if ld_res is None else int(ld_res), ld if ld_out is None else int(ld_out),
+                       int(cols), _type_code(dtype), float(p), 0)
+
+
+def head_loss(rows, hidden, vocab, dtype, *, by_output=False, ld_h=None, ld_w=None):
+    """rubick_head_loss_desc.  by_output: the weight is [vocab, hidden], as an embedding is."""
+    wide = int(hidden if by_output else vocab)
+    return HeadLossDesc(int(rows), int(hidden) if ld_h is None else int(ld_h), wide if ld_w is None else int(ld_w), int(hidden), int(vocab),
+                        _type_code(dtype), WEIGHT_BY_OUTPUT * bool(by_output))
+
+
 class Cluster(C.Structure):
     _fields_ = [("n_nodes", C.c_int32), ("n_tenants", C.c_int32), ("quota_gpus", C.POINTER(C.c_int32)),
                 ("quota_cpus", C.POINTER(C.c_int32))]
@@ -142,7 +187,9 @@ EXPORTS = ["rubick_create", "rubick_destroy", "rubick_sync", "rubick_last_error"
            "rubick_schedule_round_host", "rubick_incremental_event_host", "rubick_probe", "rubick_kernel_launches",
            "rubick_set_placement", "rubick_greedy_round_spread",
            "rubick_block_norm_forward", "rubick_block_norm_backward", "rubick_router_forward", "rubick_router_backward",
-           "rubick_distill_forward", "rubick_distill_backward", "rubick_distill_step"]
+           "rubick_distill_forward", "rubick_distill_backward", "rubick_distill_step",
+           "rubick_linear_forward", "rubick_linear_backward", "rubick_dropout_forward", "rubick_dropout_backward",
+           "rubick_head_loss_forward", "rubick_head_loss_backward", "rubick_head_loss_step"]
 
 _lib = None
 
@@ -197,6 +244,13 @@ def lib():
         L.rubick_distill_forward.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 5
         L.rubick_distill_backward.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 6
         L.rubick_distill_step.argtypes = [vp, C.POINTER(DistillDesc)] + [vp] * 7
+        L.rubick_linear_forward.argtypes = [vp, C.POINTER(LinearDesc)] + [vp] * 7
+        L.rubick_linear_backward.argtypes = [vp, C.POINTER(LinearDesc)] + [vp] * 8
+        L.rubick_dropout_forward.argtypes = [vp, C.POINTER(DropoutDesc)] + [vp] * 4
+        L.rubick_dropout_backward.argtypes = [vp, C.POINTER(DropoutDesc)] + [vp] * 3
+        L.rubick_head_loss_forward.argtypes = [vp, C.POINTER(HeadLossDesc)] + [vp] * 5
+        L.rubick_head_loss_backward.argtypes = [vp, C.POINTER(HeadLossDesc)] + [vp] * 7
+        L.rubick_head_loss_step.argtypes = [vp, C.POINTER(HeadLossDesc)] + [vp] * 8
         L.rubick_kernel_launches.argtypes = []
         L.rubick_kernel_launches.restype = C.c_ulonglong
         for name in EXPORTS:
@@ -452,21 +506,21 @@ class Context:
                                                              C.byref(steps)), allow=(ESTEPS,))
         return steps.value, rc == ESTEPS
 
-    # ---- operators of a training step.  Descriptors: block_norm(), router(), distill().  Tensors are the caller's, on
+    # ---- operators of a training step.  Descriptors: block_norm(), router(), distill(), linear(), dropout(), head_loss().  Tensors are the caller's, on
     # ---- this context's device; None where the header allows NULL.  The work goes to the context's stream.
     # The first call of a method with a descriptor looks its tensors over: their types and device against the descriptor and
     # the context, and that neighbours in a row are neighbours in memory.  (On every call it is 1 us of 5 for a few tokens;
     # what such a look finds is in the program, not in the data.)  Sizes and row distances are the descriptor's to state.
 
-    def _look_over(self, desc, method, rows=(), weights=(), teacher=(), floats=(), ints=(), masks=()):
+    def _look_over(self, desc, method, rows=(), weights=(), teacher=(), floats=(), ints=(), masks=(), seeds=()):
         import torch
         types = {BF16: (torch.bfloat16,), F16: (torch.float16,), F32: (torch.float32,)}
-        wtype = getattr(desc, "wtype", desc.dtype)
+        wtype = getattr(desc, "wtype", getattr(desc, "btype", desc.dtype))
         known = desc.dtype in types and wtype in (desc.dtype, F32) and getattr(desc, "ttype", desc.dtype) in types
         if not known:
             return                       # the entry point refuses the descriptor
         for tensors, allowed in ((rows, types[desc.dtype]), (weights, types[wtype]), (teacher, types[getattr(desc, "ttype", desc.dtype)]),
-                                 (floats, (torch.float32,)), (ints, (torch.int32,)), (masks, (torch.uint8, torch.bool))):
+                                 (floats, (torch.float32,)), (ints, (torch.int32,)), (masks, (torch.uint8, torch.bool)), (seeds, (torch.int64, torch.uint64))):
             for x in tensors:
                 if x is None:
                     continue
@@ -529,3 +583,49 @@ class Context:
             self._look_over(desc, "distill_step", rows=(d_z, d_dz), ints=(d_index,), teacher=(d_teacher,), floats=(d_dloss, d_loss, d_lse))
         return self._check(lib().rubick_distill_step(self._h, desc, _addr(d_z), _addr(d_index), _addr(d_teacher), _addr(d_dloss),
                                                      _addr(d_loss), _addr(d_lse), _addr(d_dz)))
+
+    def linear_forward(self, desc, d_x, d_w, d_bias, d_residual, d_seed, d_pre, d_out):
+        """rubick_linear_forward.  d_seed: two 64-bit integers {seed, offset}."""
+        if "linear_forward" not in desc.looked_over:
+            self._look_over(desc, "linear_forward", rows=(d_x, d_w, d_residual, d_pre, d_out), weights=(d_bias,), seeds=(d_seed,))
+        return self._check(lib().rubick_linear_forward(self._h, desc, _addr(d_x), _addr(d_w), _addr(d_bias), _addr(d_residual), _addr(d_seed),
+                                                       _addr(d_pre), _addr(d_out)))
+
+    def linear_backward(self, desc, d_x, d_w, d_pre, d_seed, d_dout, d_dx, d_dw, d_dbias=None):
+        """rubick_linear_backward"""
+        if "linear_backward" not in desc.looked_over:
+            self._look_over(desc, "linear_backward", rows=(d_x, d_w, d_pre, d_dout, d_dx, d_dw), floats=(d_dbias,), seeds=(d_seed,))
+        return self._check(lib().rubick_linear_backward(self._h, desc, _addr(d_x), _addr(d_w), _addr(d_pre), _addr(d_seed), _addr(d_dout),
+                                                        _addr(d_dx), _addr(d_dw), _addr(d_dbias)))
+
+    def dropout_forward(self, desc, d_seed, d_x, d_residual, d_out):
+        """rubick_dropout_forward.  d_seed: two 64-bit integers {seed, offset}."""
+        if "dropout_forward" not in desc.looked_over:
+            self._look_over(desc, "dropout_forward", rows=(d_x, d_residual, d_out), seeds=(d_seed,))
+        return self._check(lib().rubick_dropout_forward(self._h, desc, _addr(d_seed), _addr(d_x), _addr(d_residual), _addr(d_out)))
+
+    def dropout_backward(self, desc, d_seed, d_dout, d_dx):
+        """rubick_dropout_backward"""
+        if "dropout_backward" not in desc.looked_over:
+            self._look_over(desc, "dropout_backward", rows=(d_dout, d_dx), seeds=(d_seed,))
+        return self._check(lib().rubick_dropout_backward(self._h, desc, _addr(d_seed), _addr(d_dout), _addr(d_dx)))
+
+    def head_loss_forward(self, desc, d_h, d_w, d_label, d_loss, d_lse=None):
+        """rubick_head_loss_forward"""
+        if "head_loss_forward" not in desc.looked_over:
+            self._look_over(desc, "head_loss_forward", rows=(d_h, d_w), ints=(d_label,), floats=(d_loss, d_lse))
+        return self._check(lib().rubick_head_loss_forward(self._h, desc, _addr(d_h), _addr(d_w), _addr(d_label), _addr(d_loss), _addr(d_lse)))
+
+    def head_loss_backward(self, desc, d_h, d_w, d_label, d_lse, d_dloss, d_dh, d_dw):
+        """rubick_head_loss_backward"""
+        if "head_loss_backward" not in desc.looked_over:
+            self._look_over(desc, "head_loss_backward", rows=(d_h, d_w, d_dh, d_dw), ints=(d_label,), floats=(d_lse, d_dloss))
+        return self._check(lib().rubick_head_loss_backward(self._h, desc, _addr(d_h), _addr(d_w), _addr(d_label), _addr(d_lse), _addr(d_dloss),
+                                                           _addr(d_dh), _addr(d_dw)))
+
+    def head_loss_step(self, desc, d_h, d_w, d_label, d_dloss, d_loss, d_lse, d_dh, d_dw):
+        """rubick_head_loss_step"""
+        if "head_loss_step" not in desc.looked_over:
+            self._look_over(desc, "head_loss_step", rows=(d_h, d_w, d_dh, d_dw), ints=(d_label,), floats=(d_dloss, d_loss, d_lse))
+        return self._check(lib().rubick_head_loss_step(self._h, desc, _addr(d_h), _addr(d_w), _addr(d_label), _addr(d_dloss), _addr(d_loss),
+                                                       _addr(d_lse), _addr(d_dh), _addr(d_dw)))

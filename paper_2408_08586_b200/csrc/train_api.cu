@@ -3,7 +3,7 @@
 
 #include <cmath>
 
-#include "train_common.cuh"
+#include "product.cuh"
 
 using namespace rubick;
 
@@ -109,6 +109,197 @@ int check_distill(rubick_ctx *ctx, const rubick_distill_desc *d)
     if (d->ld < d->vocab) return fail(ctx, RUBICK_EINVAL, "distill: ld smaller than vocab");
     if (!(d->temperature > 0.f) || std::isinf(d->temperature)) return fail(ctx, RUBICK_EINVAL, "distill: the temperature must be positive and finite");
     if (d->reserved) return fail(ctx, RUBICK_EINVAL, "distill: reserved must be 0");
+    return RUBICK_OK;
+}
+
+bool is16(int32_t dtype) { return dtype == RUBICK_BF16 || dtype == RUBICK_F16; }
+bool features(int32_t n) { return n >= 1 && n <= RUBICK_MAX_FEATURES; }
+bool probability(float p) { return p >= 0.f && p < 1.f; }
+
+DropArgs drop_args(float p, const uint64_t *seed)
+{
+    if (p == 0.f) return DropArgs{nullptr, 0, 1.f};
+    return DropArgs{seed, uint32_t(double(p) * 4294967296.0), float(1.0 / (1.0 - double(p)))};
+}
+
+int check_linear(rubick_ctx *ctx, const rubick_linear_desc *d, const void *seed)
+{
+    if (!d) return fail(ctx, RUBICK_EINVAL, "linear: null descriptor");
+    if (d->rows < 0 || d->rows > 0x7fffffff) return fail(ctx, RUBICK_EINVAL, "linear: rows must be 0 .. 2^31 - 1");
+    if (!features(d->inputs) || !features(d->outputs)) return fail(ctx, RUBICK_EINVAL, "linear: inputs or outputs out of range");
+    if (!is16(d->dtype) || (d->btype != d->dtype && d->btype != RUBICK_F32)) return fail(ctx, RUBICK_EINVAL, "linear: the operands are RUBICK_BF16 or RUBICK_F16, the bias of their type or RUBICK_F32");
+    if (d->flags & ~RUBICK_WEIGHT_BY_OUTPUT) return fail(ctx, RUBICK_EINVAL, "linear: unknown flag");
+    if (d->activation < RUBICK_ACT_NONE || d->activation > RUBICK_ACT_SILU) return fail(ctx, RUBICK_EINVAL, "linear: unknown activation");
+    if (!probability(d->p)) return fail(ctx, RUBICK_EINVAL, "linear: p must be in [0, 1)");
+    if (d->reserved) return fail(ctx, RUBICK_EINVAL, "linear: reserved must be 0");
+    if (d->p > 0.f && (!seed || !on(seed, 8))) return fail(ctx, RUBICK_EINVAL, "linear: the seed is null or not aligned");
+    return RUBICK_OK;
+}
+// distance between the rows of a weight against its width
+bool weight_distance(int64_t ld, bool by_output, int32_t inputs, int32_t outputs) { return ld >= (by_output ? inputs : outputs); }
+
+int check_dropout(rubick_ctx *ctx, const rubick_dropout_desc *d, const void *seed)
+{
+    if (!d) return fail(ctx, RUBICK_EINVAL, "dropout: null descriptor");
+    if (d->rows < 0 || d->rows > 0x7fffffff) return fail(ctx, RUBICK_EINVAL, "dropout: rows must be 0 .. 2^31 - 1");
+    if (!features(d->cols)) return fail(ctx, RUBICK_EINVAL, "dropout: cols out of range");
+    if (!known(d->dtype)) return fail(ctx, RUBICK_EINVAL, "dropout: unknown type");
+    if (!probability(d->p)) return fail(ctx, RUBICK_EINVAL, "dropout: p must be in [0, 1)");
+    if (d->ld_x < d->cols || d->ld_out < d->cols) return fail(ctx, RUBICK_EINVAL, "dropout: a row distance is smaller than cols");
+    if (d->reserved) return fail(ctx, RUBICK_EINVAL, "dropout: reserved must be 0");
+    if (d->p > 0.f && (!seed || !on(seed, 8))) return fail(ctx, RUBICK_EINVAL, "dropout: the seed is null or not aligned");
+    return RUBICK_OK;
+}
+
+int check_head(rubick_ctx *ctx, const rubick_head_loss_desc *d)
+{
+    if (!d) return fail(ctx, RUBICK_EINVAL, "head loss: null descriptor");
+    if (d->rows < 0 || d->rows > 0x7fffffff) return fail(ctx, RUBICK_EINVAL, "head loss: rows must be 0 .. 2^31 - 1");
+    if (!features(d->hidden)) return fail(ctx, RUBICK_EINVAL, "head loss: hidden out of range");
+    if (d->vocab < 1 || d->vocab > (1 << 30)) return fail(ctx, RUBICK_EINVAL, "head loss: vocab out of range");
+    if (!is16(d->dtype)) return fail(ctx, RUBICK_EINVAL, "head loss: the type is RUBICK_BF16 or RUBICK_F16");
+    if (d->flags & ~RUBICK_WEIGHT_BY_OUTPUT) return fail(ctx, RUBICK_EINVAL, "head loss: unknown flag");
+    if (d->ld_h < d->hidden || !weight_distance(d->ld_w, d->flags & RUBICK_WEIGHT_BY_OUTPUT, d->hidden, d->vocab)) return fail(ctx, RUBICK_EINVAL, "head loss: a row distance is too small");
+    return RUBICK_OK;
+}
+
+// Parts of the scratch buffer: taken first, which adds them up, and addressed once the buffer is there.
+struct Parts {
+    size_t used = 0;
+    size_t take(size_t bytes) { const size_t at = used; used += (bytes + 255) & ~size_t(255); return at; }
+};
+template <typename T> T *part(rubick_ctx *ctx, size_t at) { return reinterpret_cast<T *>(static_cast<char *>(ctx->d_train) + at); }
+int64_t up8(int64_t n) { return (n + 7) & ~int64_t(7); }
+bool wide16(const void *p, int64_t ld) { return train::aligned16(p) && (ld & 7) == 0; }
+
+// One product and what it keeps in scratch.
+struct Planned { ProductKind kind; size_t part; };
+Planned plan_product(Parts &parts, ProductArgs &a, int num_sms)
+{
+    a.splits = product_splits(a, num_sms);
+    if (a.splits == 1) return Planned{PRODUCT_OUT, 0};
+    if (!a.ld_acc) a.ld_acc = up8(a.n);
+    return Planned{PRODUCT_PART, parts.take(size_t(a.splits) * a.m * a.ld_acc * sizeof(float))};
+}
+cudaError_t run_product(rubick_ctx *ctx, const Planned &p, ProductArgs &a)
+{
+    if (p.kind == PRODUCT_PART) a.part = part<float>(ctx, p.part);
+    return launch_product(p.kind, a, ctx->num_sms, ctx->stream);
+}
+
+// The head's loss, its gradient, or both.
+int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w, const int32_t *d_label,
+              const float *d_lse_in, const float *d_dloss, float *d_loss, float *d_lse, void *d_dh, void *d_dw, bool forward, bool backward)
+{
+    const rubick_head_loss_desc &d = *h_desc;
+    const bool by_output = d.flags & RUBICK_WEIGHT_BY_OUTPUT;
+    int rc;
+    if ((rc = set_device(ctx))) return rc;
+    if (d.rows == 0) {
+        if (d_dw) CUDA_TRY(ctx, cudaMemset2DAsync(d_dw, size_t(d.ld_w) * 2, 0, size_t(by_output ? d.hidden : d.vocab) * 2, by_output ? d.vocab : d.hidden, ctx->stream), "clear dw");
+        return RUBICK_OK;
+    }
+    const int64_t ld_copy = up8(d.hidden), tiles = (int64_t(d.vocab) + STATS_COLS - 1) / STATS_COLS;
+    Parts parts;
+    const size_t at_copy = parts.take(size_t(d.rows) * ld_copy * 2);
+    const size_t at_stats = forward ? parts.take(size_t(tiles) * d.rows * sizeof(float2)) : 0, at_label = forward ? parts.take(size_t(d.rows) * 4) : 0;
+    const size_t at_base = forward && backward ? parts.take(size_t(d.rows) * 4) : 0, at_rest = forward && backward ? parts.take(size_t(d.rows) * 4) : 0;
+    const size_t at_weight = backward ? parts.take(size_t(d.rows) * 4) : 0, at_scale = backward ? parts.take(8) : 0;
+    // the vocabulary of a piece: as much as 256 MB of dz take, in whole tiles
+    int64_t piece = (int64_t(256) << 20) / (2 * d.rows) / 256 * 256;
+    if (piece < 256) piece = 256;
+    if (piece > d.vocab) piece = d.vocab;
+    const int64_t ld_dz = up8(piece);
+    const bool several = piece < d.vocab;
+    const size_t at_dz = backward ? parts.take(size_t(d.rows) * ld_dz * 2) : 0;
+    const size_t at_acc = backward && several && d_dh ? parts.take(size_t(d.rows) * ld_copy * 4) : 0;
+    // the two products of a gradient, one after the other: their splits' sums share a place
+    const size_t joined = parts.used;
+    size_t most = joined;
+    auto gradient_products = [&](int64_t first, int64_t n, ProductArgs &h, ProductArgs &w) {
+        h = ProductArgs{}; w = ProductArgs{};
+        h.dtype = w.dtype = d.dtype;
+        h.status = w.status = ctx->d_status;
+        h.m = d.rows; h.n = d.hidden; h.k = n;
+        h.ld_out = d.ld_h; h.ld_acc = ld_copy;
+        h.b = Operand{static_cast<const char *>(d_w) + (by_output ? first * d.ld_w : first) * 2, d.ld_w, !by_output};
+        h.out = d_dh;
+        h.wide = wide16(d_dh, d.ld_h) ? WIDE_OUT : 0;
+        w.k = d.rows;
+        w.ld_out = d.ld_w;
+        w.wide = wide16(d_dw, d.ld_w) ? WIDE_OUT : 0;
+        if (by_output) { w.m = n; w.n = d.hidden; w.out = static_cast<char *>(d_dw) + first * d.ld_w * 2; }
+        else { w.m = d.hidden; w.n = n; w.out = static_cast<char *>(d_dw) + first * 2; }
+    };
+    if (backward) {
+        for (const int64_t n : {piece, (d.vocab - 1) % piece + 1}) {
+            ProductArgs h, w;
+            gradient_products(0, n, h, w);
+            for (ProductArgs *x : {&h, &w}) {
+                parts.used = joined;
+                plan_product(parts, *x, ctx->num_sms);
+                if (parts.used > most) most = parts.used;
+            }
+        }
+    }
+    if ((rc = scratch(ctx, most))) return rc;
+
+    HeadPrepArgs pre = {};
+    pre.rows = d.rows; pre.ld_h = d.ld_h; pre.ld_copy = ld_copy; pre.hidden = d.hidden; pre.vocab = d.vocab; pre.dtype = d.dtype;
+    pre.h = d_h; pre.label = d_label; pre.dloss = d_dloss; pre.copy = part<void>(ctx, at_copy);
+    if (backward) { pre.weight = part<float>(ctx, at_weight); pre.scale = part<float>(ctx, at_scale); pre.largest = part<uint32_t>(ctx, at_scale) + 1; }
+    CUDA_TRY(ctx, launch_head_prep(pre, ctx->num_sms, ctx->stream), "launch head_prep");
+
+    ProductArgs z = {};
+    z.m = d.rows; z.k = d.hidden; z.dtype = d.dtype; z.status = ctx->d_status;
+    z.a = Operand{pre.copy, ld_copy, 1};
+    z.label = d_label; z.vocab = d.vocab;
+    if (forward) {
+        z.n = d.vocab;
+        z.b = Operand{d_w, d.ld_w, by_output};
+        z.stats = part<float2>(ctx, at_stats); z.at_label = part<float>(ctx, at_label);
+        CUDA_TRY(ctx, launch_product(PRODUCT_STATS, z, ctx->num_sms, ctx->stream), "launch product (logits)");
+        HeadFinishArgs f = {};
+        f.rows = d.rows; f.vocab = d.vocab; f.tiles = int(tiles);
+        f.label = d_label; f.stats = z.stats; f.at_label = z.at_label; f.loss = d_loss; f.lse = d_lse;
+        if (backward) { f.base = part<float>(ctx, at_base); f.rest = part<float>(ctx, at_rest); }
+        CUDA_TRY(ctx, launch_head_finish(f, ctx->num_sms, ctx->stream), "launch head_finish");
+    }
+    if (!backward) return RUBICK_OK;
+    z.base = forward ? part<float>(ctx, at_base) : d_lse_in;
+    z.rest = forward ? part<float>(ctx, at_rest) : nullptr;
+    z.weight = pre.weight;
+    for (int64_t first = 0; first < d.vocab; first += piece) {
+        const int64_t n = first + piece < d.vocab ? piece : d.vocab - first;
+        ProductArgs h, w;
+        gradient_products(first, n, h, w);
+        z.n = n; z.first = int32_t(first);
+        z.b = Operand{h.b.p, d.ld_w, by_output};
+        z.out = part<void>(ctx, at_dz); z.ld_out = ld_dz;
+        CUDA_TRY(ctx, launch_product(PRODUCT_GRAD, z, ctx->num_sms, ctx->stream), "launch product (logits' gradient)");
+        h.scale = w.scale = pre.scale;
+        h.a = Operand{z.out, ld_dz, 1};
+        const Operand dz = {z.out, ld_dz, 0}, copy = {pre.copy, ld_copy, 0};
+        w.a = by_output ? dz : copy;
+        w.b = by_output ? copy : dz;
+        if (several && d_dh) {
+            if (first) h.acc_in = part<float>(ctx, at_acc);
+            if (first + n < d.vocab) h.acc_out = part<float>(ctx, at_acc);
+        }
+        for (ProductArgs *x : {&h, &w}) {
+            if (!(x == &h ? d_dh : d_dw)) continue;
+            parts.used = joined;
+            const Planned p = plan_product(parts, *x, ctx->num_sms);
+            CUDA_TRY(ctx, run_product(ctx, p, *x), "launch product (gradient)");
+        }
+    }
+    return RUBICK_OK;
+}
+
+int check_head_call(rubick_ctx *ctx, const void *h, const void *w, const int32_t *label)
+{
+    if (!h || !w || !label) return fail(ctx, RUBICK_EINVAL, "head loss: null pointer");
+    if (!on(h, 2) || !on(w, 2) || !on(label, 4)) return fail(ctx, RUBICK_EINVAL, "head loss: a tensor is not aligned to its type");
     return RUBICK_OK;
 }
 
@@ -300,6 +491,176 @@ int rubick_distill_step(rubick_ctx *ctx, const rubick_distill_desc *h_desc, cons
     }
     CUDA_TRY(ctx, launch_distill_step(a, ctx->num_sms, ctx->stream), "launch distill_step");
     return RUBICK_OK;
+}
+
+int rubick_linear_forward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, const void *d_x, const void *d_w,
+                          const void *d_bias, const void *d_residual, const uint64_t *d_seed, void *d_pre, void *d_out)
+{
+    if (!ctx) return RUBICK_EINVAL;
+    int rc = check_linear(ctx, h_desc, d_seed);
+    if (rc) return rc;
+    const rubick_linear_desc &d = *h_desc;
+    const bool by_output = d.flags & RUBICK_WEIGHT_BY_OUTPUT;
+    if (d.ld_x < d.inputs || !weight_distance(d.ld_w, by_output, d.inputs, d.outputs) || d.ld_out < d.outputs || (d_residual && d.ld_res < d.outputs) || (d_pre && d.ld_pre < d.outputs))
+        return fail(ctx, RUBICK_EINVAL, "linear: a row distance is too small");
+    if (d.rows == 0) return RUBICK_OK;
+    if (!d_x || !d_w || !d_out) return fail(ctx, RUBICK_EINVAL, "linear: null pointer");
+    if (!on(d_x, 2) || !on(d_w, 2) || !on(d_bias, esize(d.btype)) || !on(d_residual, 2) || !on(d_pre, 2) || !on(d_out, 2))
+        return fail(ctx, RUBICK_EINVAL, "linear: a tensor is not aligned to its type");
+    if ((rc = set_device(ctx))) return rc;
+    ProductArgs a = {};
+    a.m = d.rows; a.n = d.outputs; a.k = d.inputs; a.dtype = d.dtype; a.status = ctx->d_status;
+    a.a = Operand{d_x, d.ld_x, 1};
+    a.b = Operand{d_w, d.ld_w, by_output};
+    a.out = d_out; a.ld_out = d.ld_out; a.pre = d_pre; a.ld_pre = d.ld_pre; a.residual = d_residual; a.ld_res = d.ld_res;
+    a.bias = d_bias; a.bias_f32 = d.btype == RUBICK_F32; a.act = d.activation;
+    a.wide = (wide16(d_out, d.ld_out) ? WIDE_OUT : 0) | (wide16(d_pre, d.ld_pre) ? WIDE_PRE : 0) | (wide16(d_residual, d.ld_res) ? WIDE_RES : 0) |
+             (train::aligned16(d_bias) ? WIDE_BIAS : 0);
+    a.drop = drop_args(d.p, d_seed);
+    Parts parts;
+    const Planned p = plan_product(parts, a, ctx->num_sms);
+    if ((rc = scratch(ctx, parts.used))) return rc;
+    CUDA_TRY(ctx, run_product(ctx, p, a), "launch linear_forward");
+    return RUBICK_OK;
+}
+
+int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, const void *d_x, const void *d_w,
+                           const void *d_pre, const uint64_t *d_seed, const void *d_dout, void *d_dx, void *d_dw,
+                           float *d_dbias)
+{
+    if (!ctx) return RUBICK_EINVAL;
+    int rc = check_linear(ctx, h_desc, d_seed);
+    if (rc) return rc;
+    const rubick_linear_desc &d = *h_desc;
+    const bool by_output = d.flags & RUBICK_WEIGHT_BY_OUTPUT, act = d.activation != RUBICK_ACT_NONE;
+    if (((d_dx || d_dw) && (d.ld_x < d.inputs || !weight_distance(d.ld_w, by_output, d.inputs, d.outputs))) || d.ld_out < d.outputs || (act && d.ld_pre < d.outputs))
+        return fail(ctx, RUBICK_EINVAL, "linear: a row distance is too small");
+    if (!on(d_dw, 2) || !on(d_dbias, 4)) return fail(ctx, RUBICK_EINVAL, "linear: a tensor is not aligned to its type");
+    if (d.rows == 0) {
+        if ((rc = set_device(ctx))) return rc;
+        const int32_t wide = by_output ? d.inputs : d.outputs, high = by_output ? d.outputs : d.inputs;
+        if (d_dw) CUDA_TRY(ctx, cudaMemset2DAsync(d_dw, size_t(d.ld_w) * 2, 0, size_t(wide) * 2, high, ctx->stream), "clear dw");
+        if (d_dbias) CUDA_TRY(ctx, cudaMemsetAsync(d_dbias, 0, size_t(d.outputs) * 4, ctx->stream), "clear dbias");
+        return RUBICK_OK;
+    }
+    if (!d_dout || (act && !d_pre) || (d_dx && !d_w) || (d_dw && !d_x)) return fail(ctx, RUBICK_EINVAL, "linear: null pointer");
+    if (!on(d_x, 2) || !on(d_w, 2) || !on(d_pre, 2) || !on(d_dout, 2) || !on(d_dx, 2)) return fail(ctx, RUBICK_EINVAL, "linear: a tensor is not aligned to its type");
+    if (!d_dx && !d_dw && !d_dbias) return RUBICK_OK;
+    if ((rc = set_device(ctx))) return rc;
+    // dz is dout itself where nothing lies between them and the products can read it as it lies
+    const bool products = d_dx || d_dw, plain = !act && d.p == 0.f && wide16(d_dout, d.ld_out);
+    LinearGradArgs g = {};
+    g.rows = d.rows; g.ld_dout = d.ld_out; g.ld_pre = d.ld_pre; g.ld_dz = up8(d.outputs); g.cols = d.outputs; g.dtype = d.dtype; g.act = d.activation;
+    g.dout = d_dout; g.pre = d_pre; g.drop = drop_args(d.p, d_seed); g.dbias = d_dbias;
+    g.chunks = linear_grad_chunks(d.rows, d.outputs, ctx->num_sms);
+    Parts parts;
+    const bool keep = products && !plain;
+    const size_t at_dz = keep ? parts.take(size_t(d.rows) * g.ld_dz * 2) : 0;
+    const size_t at_sums = d_dbias ? parts.take(size_t(g.chunks) * d.outputs * 4) : 0;
+    ProductArgs dx = {}, dw = {};
+    dx.dtype = dw.dtype = d.dtype;
+    dx.status = dw.status = ctx->d_status;
+    dx.m = d.rows; dx.n = d.inputs; dx.k = d.outputs;
+    dx.out = d_dx; dx.ld_out = d.ld_x; dx.wide = wide16(d_dx, d.ld_x) ? WIDE_OUT : 0;
+    dx.b = Operand{d_w, d.ld_w, !by_output};
+    dw.m = by_output ? d.outputs : d.inputs; dw.n = by_output ? d.inputs : d.outputs; dw.k = d.rows;
+    dw.out = d_dw; dw.ld_out = d.ld_w; dw.wide = wide16(d_dw, d.ld_w) ? WIDE_OUT : 0;
+    const size_t joined = parts.used;
+    const Planned px = d_dx ? plan_product(parts, dx, ctx->num_sms) : Planned{};
+    const size_t most = parts.used;
+    parts.used = joined;                       // (one after the other: their splits' sums share a place)
+    const Planned pw = d_dw ? plan_product(parts, dw, ctx->num_sms) : Planned{};
+    if ((rc = scratch(ctx, parts.used > most ? parts.used : most))) return rc;
+    if (keep) g.dz = part<void>(ctx, at_dz);
+    if (d_dbias) g.part = part<float>(ctx, at_sums);
+    if (keep || d_dbias) CUDA_TRY(ctx, launch_linear_grad(g, ctx->num_sms, ctx->stream), "launch linear_grad");
+    const void *dz = keep ? g.dz : d_dout;
+    const int64_t ld_dz = keep ? g.ld_dz : d.ld_out;
+    if (d_dx) {
+        dx.a = Operand{dz, ld_dz, 1};
+        CUDA_TRY(ctx, run_product(ctx, px, dx), "launch product (dx)");
+    }
+    if (d_dw) {
+        const Operand x = {d_x, d.ld_x, 0}, z = {dz, ld_dz, 0};
+        dw.a = by_output ? z : x;
+        dw.b = by_output ? x : z;
+        CUDA_TRY(ctx, run_product(ctx, pw, dw), "launch product (dw)");
+    }
+    return RUBICK_OK;
+}
+
+static int dropout(rubick_ctx *ctx, const rubick_dropout_desc *h_desc, const uint64_t *d_seed, const void *d_x, const void *d_residual, void *d_out, bool back)
+{
+    if (!ctx) return RUBICK_EINVAL;
+    int rc = check_dropout(ctx, h_desc, d_seed);
+    if (rc) return rc;
+    if (d_residual && h_desc->ld_res < h_desc->cols) return fail(ctx, RUBICK_EINVAL, "dropout: a row distance is smaller than cols");
+    if (h_desc->rows == 0) return RUBICK_OK;
+    if (!d_x || !d_out) return fail(ctx, RUBICK_EINVAL, "dropout: null pointer");
+    const int es = esize(h_desc->dtype);
+    if (!on(d_x, es) || !on(d_residual, es) || !on(d_out, es)) return fail(ctx, RUBICK_EINVAL, "dropout: a tensor is not aligned to its type");
+    if ((rc = set_device(ctx))) return rc;
+    DropoutArgs a = {};
+    a.d = *h_desc;
+    if (back) { a.d.ld_x = h_desc->ld_out; a.d.ld_out = h_desc->ld_x; }      // dout lies as out, dx as x
+    a.x = d_x; a.residual = d_residual; a.out = d_out;
+    a.drop = drop_args(h_desc->p, d_seed);
+    CUDA_TRY(ctx, launch_dropout(a, ctx->num_sms, ctx->stream), "launch dropout");
+    return RUBICK_OK;
+}
+
+int rubick_dropout_forward(rubick_ctx *ctx, const rubick_dropout_desc *h_desc, const uint64_t *d_seed, const void *d_x,
+                           const void *d_residual, void *d_out)
+{
+    return dropout(ctx, h_desc, d_seed, d_x, d_residual, d_out, false);
+}
+
+int rubick_dropout_backward(rubick_ctx *ctx, const rubick_dropout_desc *h_desc, const uint64_t *d_seed, const void *d_dout,
+                            void *d_dx)
+{
+    return dropout(ctx, h_desc, d_seed, d_dout, nullptr, d_dx, true);
+}
+
+int rubick_head_loss_forward(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,
+                             const int32_t *d_label, float *d_loss, float *d_lse)
+{
+    if (!ctx) return RUBICK_EINVAL;
+    int rc = check_head(ctx, h_desc);
+    if (rc) return rc;
+    if (h_desc->rows == 0) return RUBICK_OK;
+    if ((rc = check_head_call(ctx, d_h, d_w, d_label))) return rc;
+    if (!d_loss) return fail(ctx, RUBICK_EINVAL, "head loss: null pointer");
+    if (!on(d_loss, 4) || !on(d_lse, 4)) return fail(ctx, RUBICK_EINVAL, "head loss: a tensor is not aligned to its type");
+    return head_loss(ctx, h_desc, d_h, d_w, d_label, nullptr, nullptr, d_loss, d_lse, nullptr, nullptr, true, false);
+}
+
+int rubick_head_loss_backward(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,
+                              const int32_t *d_label, const float *d_lse, const float *d_dloss, void *d_dh, void *d_dw)
+{
+    if (!ctx) return RUBICK_EINVAL;
+    int rc = check_head(ctx, h_desc);
+    if (rc) return rc;
+    if (!on(d_dh, 2) || !on(d_dw, 2) || !on(d_lse, 4) || !on(d_dloss, 4)) return fail(ctx, RUBICK_EINVAL, "head loss: a tensor is not aligned to its type");
+    if (h_desc->rows) {
+        if ((rc = check_head_call(ctx, d_h, d_w, d_label))) return rc;
+        if (!d_lse) return fail(ctx, RUBICK_EINVAL, "head loss: null pointer");
+    }
+    if (!d_dh && !d_dw) return RUBICK_OK;
+    return head_loss(ctx, h_desc, d_h, d_w, d_label, d_lse, d_dloss, nullptr, nullptr, d_dh, d_dw, false, true);
+}
+
+int rubick_head_loss_step(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,
+                          const int32_t *d_label, const float *d_dloss, float *d_loss, float *d_lse, void *d_dh, void *d_dw)
+{
+    if (!ctx) return RUBICK_EINVAL;
+    int rc = check_head(ctx, h_desc);
+    if (rc) return rc;
+    if (!on(d_dh, 2) || !on(d_dw, 2) || !on(d_loss, 4) || !on(d_lse, 4) || !on(d_dloss, 4)) return fail(ctx, RUBICK_EINVAL, "head loss: a tensor is not aligned to its type");
+    if (h_desc->rows) {
+        if ((rc = check_head_call(ctx, d_h, d_w, d_label))) return rc;
+        if (!d_loss) return fail(ctx, RUBICK_EINVAL, "head loss: null pointer");
+    }
+    return head_loss(ctx, h_desc, d_h, d_w, d_label, nullptr, d_dloss, d_loss, d_lse, d_dh, d_dw, true, d_dh || d_dw);
 }
 
 }  // extern "C"
