@@ -1,81 +1,258 @@
-// Matrix products of a training step with their epilogues.
+// Matrix products of a training step with their epilogues, on the tensor cores.
+//
+// D[m][n] = sum_k A[m][k] B[n][k], operands of 16 bits, sums in single precision.  A persistent block (or a pair of blocks on
+// neighbouring multiprocessors, which share the tile's columns of B) takes tile after tile.  One thread has the tensor-copy
+// engine fetch 64 k of both operands into a ring of stages, one thread multiplies them into tensor memory, and eight warps
+// take a finished tile out of it while the next one is multiplied into its other half.
+#include <type_traits>
+
 #include "product.cuh"
+#include "tcgen.cuh"
 
 namespace rubick {
 namespace {
 
 using namespace train;
 
-constexpr int BM = 64, BN = STATS_COLS, BK = 16;
+constexpr int BM = 128, BK = 64;                     // rows a block, k a stage
+constexpr int THREADS = 384;                         // fetch, multiply, allocate, -, and eight warps that read
+constexpr int READERS = 8, FIRST_READER = 4;
+constexpr int STAGING = READERS * 4096;              // 32 rows x 128 bytes a warp
+constexpr int SHARED_LIMIT = 232448;
 
-// 64 x 128 sums a block, 4 x 8 a thread, through shared memory in single precision.
-template <typename T, ProductKind KIND> __global__ void __launch_bounds__(256) product_kernel(const __grid_constant__ ProductArgs a)
+template <int BN, bool PAIR> struct Shape {
+    static constexpr int CTAS = PAIR ? 2 : 1;
+    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN / CTAS * BK * 2, STAGE = A_BYTES + B_BYTES;
+    static constexpr int STAGES = (SHARED_LIMIT - STAGING - 2048) / STAGE > 8 ? 8 : (SHARED_LIMIT - STAGING - 2048) / STAGE;
+    static constexpr int SHARED = STAGES * STAGE + STAGING + 1024 + 256;      // 1,024 to begin on such a boundary
+    static constexpr uint32_t COLUMNS = 2 * BN;                               // of tensor memory: two tiles
+};
+struct Tiling { int tiles_m, tiles_n, steps, splits; int64_t all; };
+
+// Tile number -> tile row, tile column, split: eight tile rows at a time, so that what runs at once shares operands in L2.
+__device__ __forceinline__ void place(const Tiling &t, int64_t i, int &m, int &n, int &split)
 {
-    __shared__ float sa[BK][BM + 1], sb[BK][BN + 1];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4;
-    const int64_t m0 = int64_t(blockIdx.y) * BM, n0 = int64_t(blockIdx.x) * BN;
-    const int split = blockIdx.z;
-    const int64_t steps = (a.k + BK - 1) / BK;
-    const int64_t k0 = KIND == PRODUCT_PART ? steps * split / a.splits * BK : 0, k1 = KIND == PRODUCT_PART ? steps * (split + 1) / a.splits * BK : a.k;
-    const T *pa = static_cast<const T *>(a.a.p), *pb = static_cast<const T *>(a.b.p);
-    float v[4][8] = {};
-    for (int64_t k = k0; k < k1; k += BK) {
-        for (int i = threadIdx.x; i < BM * BK; i += 256) {
-            const int r = a.a.along_k ? i / BK : i % BM, q = a.a.along_k ? i % BK : i / BM;
-            const int64_t m = m0 + r, kk = k + q;
-            sa[q][r] = m < a.m && kk < a.k ? to_f(a.a.along_k ? pa[m * a.a.ld + kk] : pa[kk * a.a.ld + m]) : 0.f;
-        }
-        for (int i = threadIdx.x; i < BN * BK; i += 256) {
-            const int r = a.b.along_k ? i / BK : i % BN, q = a.b.along_k ? i % BK : i / BN;
-            const int64_t n = n0 + r, kk = k + q;
-            sb[q][r] = n < a.n && kk < a.k ? to_f(a.b.along_k ? pb[n * a.b.ld + kk] : pb[kk * a.b.ld + n]) : 0.f;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < BK; ++q)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = fmaf(sa[q][ty * 4 + i], sb[q][tx * 8 + j], v[i][j]);
-        __syncthreads();
+    const int64_t each = int64_t(t.tiles_m) * t.tiles_n;
+    split = int(i / each);
+    const int r = int(i - split * each), band = 8 * t.tiles_n, b = r / band, high = t.tiles_m - b * 8 < 8 ? t.tiles_m - b * 8 : 8, q = r - b * band;
+    m = b * 8 + q % high;
+    n = q / high;
+}
+
+__device__ __forceinline__ float ninf() { return __uint_as_float(0xff800000u); }
+
+template <typename T, ProductKind KIND, int BN, bool PAIR>
+__global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                                                             const __grid_constant__ ProductArgs a, const __grid_constant__ Tiling t)
+{
+    using S = Shape<BN, PAIR>;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+    uint8_t *const shared = raw + (base - smem_addr(raw));
+    const uint32_t stages = base, bars = base + S::STAGES * S::STAGE + STAGING;
+    const uint32_t full = bars, empty = full + 8 * S::STAGES, done = empty + 8 * S::STAGES, taken = done + 16;
+    volatile uint32_t *const words = reinterpret_cast<volatile uint32_t *>(shared + S::STAGES * S::STAGE + STAGING + 16 * S::STAGES + 32);
+    volatile uint32_t *const given_up = words;       // [0] someone waited in vain; [1] where the tensor memory begins
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = PAIR ? cluster_rank() : 0;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S::STAGES; ++s) { barrier_init(full + 8 * s, 1); barrier_init(empty + 8 * s, 1); }
+        for (int i = 0; i < 2; ++i) { barrier_init(done + 8 * i, 1); barrier_init(taken + 8 * i, READERS * S::CTAS); }
+        barrier_init_done();
+        *given_up = 0;
     }
-    const Drop drop(a.drop);
-    const float scale = a.scale ? *a.scale : 1.f;
-    const int64_t c = n0 + tx * 8;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t row = m0 + ty * 4 + i;
-        const bool in = row < a.m;
-        if constexpr (KIND == PRODUCT_OUT) {
-            if (in && c < a.n) finish8<T>(a, drop, scale, row, c, v[i]);
-        } else if constexpr (KIND == PRODUCT_PART) {
-            if (in && c < a.n) store8<float>(a.part + (int64_t(split) * a.m + row) * a.ld_acc, c, a.ld_acc, true, v[i]);
-        } else if constexpr (KIND == PRODUCT_STATS) {
-            float top = __uint_as_float(0xff800000u), sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) if (c + e < a.n) top = fmaxf(top, v[i][e]);
-#pragma unroll
-            for (int o = 8; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-            const float at = top == __uint_as_float(0xff800000u) ? 0.f : top;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) if (c + e < a.n) sum += ex2((v[i][e] - at) * LOG2E);
-#pragma unroll
-            for (int o = 8; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            if (in) {
-                if (tx == 0) a.stats[int64_t(blockIdx.x) * a.m + row] = make_float2(top, sum);
-                const int64_t l = int64_t(a.label[row]) - a.first - c;
-                if (l >= 0 && l < 8 && c + l < a.n) a.at_label[row] = v[i][l];
+    if (warp == 2) {
+        tmem_alloc<PAIR>(smem_addr(const_cast<uint32_t *>(words + 1)), S::COLUMNS);
+        tmem_alloc_done<PAIR>();
+    }
+    tcgen_before_sync();
+    __syncthreads();
+    if constexpr (PAIR) cluster_sync();
+    tcgen_after_sync();
+    const uint32_t tmem = words[1];
+    const int64_t first = blockIdx.x / S::CTAS, step = gridDim.x / S::CTAS;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t round = 0;                      // stages filled so far
+            bool fine = true;
+            for (int64_t i = first; fine && i < t.all; i += step) {
+                int tm, tn, split;
+                place(t, i, tm, tn, split);
+                const int m0 = (tm * S::CTAS + int(rank)) * BM, n0 = tn * BN + int(rank) * (BN / S::CTAS);
+                const int k1 = int(int64_t(t.steps) * (split + 1) / t.splits);
+                for (int k = int(int64_t(t.steps) * split / t.splits); k < k1; ++k, ++round) {
+                    const uint32_t s = round % S::STAGES, into = stages + s * S::STAGE;
+                    if (!(fine = barrier_wait(empty + 8 * s, (round / S::STAGES & 1) ^ 1, given_up))) break;
+                    if (rank == 0) barrier_expect(full + 8 * s, S::STAGE * S::CTAS);
+                    const uint32_t bar = PAIR ? at_rank(full + 8 * s, 0) : full + 8 * s;
+                    if (a.a.along_k) tensor_load<PAIR>(into, &map_a, k * BK, m0, bar);
+                    else
+                        for (int j = 0; j < BM / 64; ++j) tensor_load<PAIR>(into + j * BLOCK_BYTES, &map_a, m0 + 64 * j, k * BK, bar);
+                    if (a.b.along_k) tensor_load<PAIR>(into + S::A_BYTES, &map_b, k * BK, n0, bar);
+                    else
+                        for (int j = 0; j < BN / S::CTAS / 64; ++j) tensor_load<PAIR>(into + S::A_BYTES + j * BLOCK_BYTES, &map_b, n0 + 64 * j, k * BK, bar);
+                }
             }
-        } else {
-            if (in && c < a.ld_out) {
-                const float base = a.base[row], rest = a.rest ? a.rest[row] : 0.f, w = a.weight[row];
-                const int64_t l = int64_t(a.label[row]) - a.first - c;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[i][e] = w == 0.f ? 0.f : w * (ex2(((v[i][e] - base) - rest) * LOG2E) - (e == l ? 1.f : 0.f));
-                store8<T>(static_cast<T *>(a.out) + row * a.ld_out, c, a.ld_out, true, v[i]);
+            // given up: the copies in flight write into this block's memory, so they are waited for before it goes
+            if (!fine && rank == 0) {
+                volatile uint32_t never = 0;
+                for (uint32_t r = round > S::STAGES ? round - S::STAGES : 0; r < round; ++r) barrier_wait(full + 8 * (r % S::STAGES), r / S::STAGES & 1, &never);
             }
         }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            const bool ak = a.a.along_k, bk = a.b.along_k;
+            const uint32_t desc = instruction_desc(std::is_same<T, bf16>::value, ak, bk, BM * S::CTAS, BN);
+            const uint64_t da = operand_desc(stages, ak), db = operand_desc(stages + S::A_BYTES, bk);
+            const uint32_t sa = operand_step(ak), sb = operand_step(bk);
+            uint32_t round = 0, tile = 0;
+            bool fine = true;
+            for (int64_t i = first; fine && i < t.all; i += step, ++tile) {
+                const int split = int(i / (int64_t(t.tiles_m) * t.tiles_n));
+                const int k0 = int(int64_t(t.steps) * split / t.splits), k1 = int(int64_t(t.steps) * (split + 1) / t.splits);
+                const uint32_t half = tile & 1, d = tmem + half * BN;
+                if (!(fine = barrier_wait(taken + 8 * half, (tile / 2 & 1) ^ 1, given_up))) break;
+                tcgen_after_sync();
+                for (int k = k0; k < k1; ++k, ++round) {
+                    const uint32_t s = round % S::STAGES, at = s * (S::STAGE >> 4);
+                    if (!(fine = barrier_wait(full + 8 * s, round / S::STAGES & 1, given_up))) break;
+                    tcgen_after_sync();
+#pragma unroll
+                    for (int q = 0; q < BK / 16; ++q) multiply<PAIR>(d, da + at + q * sa, db + at + q * sb, desc, k > k0 || q > 0);
+                    multiplied<PAIR>(empty + 8 * s);
+                }
+                if (fine) multiplied<PAIR>(done + 8 * half);
+            }
+            if (!fine) {                             // what was multiplied is waited for before the tensor memory goes
+                volatile uint32_t never = 0;
+                for (uint32_t r = round > S::STAGES ? round - S::STAGES : 0; r < round; ++r) barrier_wait(empty + 8 * (r % S::STAGES), r / S::STAGES & 1, &never);
+            }
+        }
+        __syncwarp();
+    } else if (warp >= FIRST_READER) {
+        const int quarter = warp & 3, side = (warp - FIRST_READER) >> 2;       // 32 rows, half of the columns
+        uint8_t *const mine = shared + S::STAGES * S::STAGE + (warp - FIRST_READER) * 4096;
+        const Drop drop(a.drop);
+        const float scale = a.scale ? *a.scale : 1.f;
+        uint32_t tile = 0;
+        for (int64_t i = first; i < t.all; i += step, ++tile) {
+            int tm, tn, split;
+            place(t, i, tm, tn, split);
+            const uint32_t half = tile & 1;
+            const int64_t m0 = (int64_t(tm) * S::CTAS + rank) * BM + quarter * 32;
+            const int64_t n0 = int64_t(tn) * BN + side * (BN / 2);
+            if (!barrier_wait(done + 8 * half, tile / 2 & 1, given_up)) break;
+            __syncwarp();
+            tcgen_after_sync();
+            const uint32_t at = tmem + half * BN + side * (BN / 2) + (uint32_t(quarter * 32) << 16);
+            if constexpr (KIND == PRODUCT_OUT || KIND == PRODUCT_PART) {
+                // 32 rows x 32 sums through shared memory, pieces of 16 bytes exchanged by the row, so that a warp then holds
+                // eight neighbouring sums a lane and its accesses cover whole sectors of eight rows
+                for (int c = 0; c < BN / 2; c += 32) {
+                    float v[32];
+                    tmem_load32(at + c, v);
+                    if (n0 + c >= a.n) continue;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        *reinterpret_cast<float4 *>(mine + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                    __syncwarp();
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int line = r * 8 + (lane >> 2), q = (lane & 3) * 2;
+                        const float4 x = *reinterpret_cast<const float4 *>(mine + line * 128 + ((q ^ (line & 7)) << 4));
+                        const float4 y = *reinterpret_cast<const float4 *>(mine + line * 128 + (((q + 1) ^ (line & 7)) << 4));
+                        float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                        const int64_t row = m0 + line, col = n0 + c + q * 4;
+                        if (row < a.m && col < a.n) {
+                            if constexpr (KIND == PRODUCT_OUT) finish8<T>(a, drop, scale, row, col, w);
+                            else store8<float>(a.part + (int64_t(split) * a.m + row) * a.ld_acc, col, a.ld_acc, true, w);
+                        }
+                    }
+                    __syncwarp();
+                }
+            } else if constexpr (KIND == PRODUCT_STATS) {
+                // a thread has a row: running maximum and sum of exponentials over its columns
+                const int64_t row = m0 + lane;
+                const int64_t label = row < a.m ? int64_t(a.label[row]) - a.first - n0 : -1;
+                float top = ninf(), sum = 0.f;
+                for (int c = 0; c < BN / 2; c += 32) {
+                    float v[32];
+                    tmem_load32(at + c, v);
+                    const int64_t left = a.n - (n0 + c);
+                    if (left <= 0) continue;
+                    if (left < 32) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) if (e >= left) v[e] = ninf();
+                    }
+                    if (__any_sync(0xffffffffu, label >= c && label < c + 32 && label < c + left)) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) if (label == c + e && e < left) a.at_label[row] = v[e];
+                    }
+                    float m = v[0];
+#pragma unroll
+                    for (int e = 1; e < 32; ++e) m = fmaxf(m, v[e]);
+                    m = fmaxf(m, top);
+                    const float from = m == ninf() ? 0.f : m;
+                    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) { s0 += ex2((v[e] - from) * LOG2E); s1 += ex2((v[e + 1] - from) * LOG2E); }
+                    sum = sum * ex2((top - from) * LOG2E) + (s0 + s1);
+                    top = m;
+                }
+                if (row < a.m && n0 < a.n) a.stats[(int64_t(tn) * 2 + side) * a.m + row] = make_float2(top, sum);
+            } else {
+                // a thread has a row; 64 columns become 128 bytes of it, written line by line
+                const int64_t row = m0 + lane;
+                const bool in = row < a.m;
+                const float from = in ? a.base[row] : 0.f, rest = in && a.rest ? a.rest[row] : 0.f, w = in ? a.weight[row] : 0.f;
+                const uint32_t mask = w == 0.f ? 0u : 0xffffffffu;            // (rows that take no part, whatever their logits are)
+                const int64_t label = in ? int64_t(a.label[row]) - a.first - n0 : -1;
+                for (int c = 0; c < BN / 2; c += 64) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float v[32];
+                        tmem_load32(at + c + 32 * h, v);
+                        const int here = c + 32 * h;
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = w * ex2(((v[e] - from) - rest) * LOG2E);
+                        if (__any_sync(0xffffffffu, label >= here && label < here + 32)) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) if (label == here + e) v[e] -= w;
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            uint4 p;
+                            p.x = pack_pair(v[8 * q], v[8 * q + 1], T()) & mask; p.y = pack_pair(v[8 * q + 2], v[8 * q + 3], T()) & mask;
+                            p.z = pack_pair(v[8 * q + 4], v[8 * q + 5], T()) & mask; p.w = pack_pair(v[8 * q + 6], v[8 * q + 7], T()) & mask;
+                            *reinterpret_cast<uint4 *>(mine + lane * 128 + (((h * 4 + q) ^ (lane & 7)) << 4)) = p;
+                        }
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const int line = r * 4 + (lane >> 3), q = lane & 7;
+                        const uint4 p = *reinterpret_cast<const uint4 *>(mine + line * 128 + ((q ^ (line & 7)) << 4));
+                        const int64_t to = m0 + line, col = n0 + c + q * 8;
+                        if (to < a.m && col < a.ld_out) *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + to * a.ld_out + col) = p;
+                    }
+                    __syncwarp();
+                }
+            }
+            tcgen_before_sync();
+            __syncwarp();
+            if (lane == 0) barrier_arrive_at(PAIR ? at_rank(taken + 8 * half, 0) : taken + 8 * half);
+        }
     }
+    __syncthreads();
+    if constexpr (PAIR) cluster_sync();              // the other block's copies, products and arrivals end here as well
+    if (warp == 2) {
+        tcgen_after_sync();
+        tmem_free<PAIR>(tmem, S::COLUMNS);
+    }
+    if (threadIdx.x == 0 && *given_up && a.status) atomicOr(a.status, DS_COPY_LOST);
 }
 
 // The sums of the splits joined, and PRODUCT_OUT's epilogue.
@@ -97,37 +274,113 @@ template <typename T> __global__ void __launch_bounds__(256) join_kernel(const _
     }
 }
 
-template <typename T> cudaError_t product(ProductKind kind, const ProductArgs &a, int num_sms, cudaStream_t st)
+// Rows laid out anew, on 16-byte boundaries (the copy engine takes no others).
+__global__ void __launch_bounds__(256) lay_out_kernel(const uint16_t *from, int64_t ld_from, uint16_t *to, int64_t ld_to, int64_t rows, int64_t cols)
 {
-    const dim3 grid(unsigned((a.n + BN - 1) / BN), unsigned((a.m + BM - 1) / BM), kind == PRODUCT_PART ? a.splits : 1);
+    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y)
+        for (int64_t c = int64_t(blockIdx.x) * 256 + threadIdx.x; c < cols; c += int64_t(gridDim.x) * 256) to[row * ld_to + c] = from[row * ld_from + c];
+}
+
+using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                 const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiled encode_tiled()
+{
+    static const EncodeTiled found = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult r = cudaDriverEntryPointSymbolNotFound;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &r) != cudaSuccess || r != cudaDriverEntryPointSuccess) f = nullptr;
+        return reinterpret_cast<EncodeTiled>(f);
+    }();
+    return found;
+}
+
+// The copy engine's view of an operand with `dim` rows and k columns: boxes of 64 k x `high` rows, or 64 rows x 64 k.
+bool operand_map(CUtensorMap *map, const Operand &o, int dtype, int64_t dim, int64_t k, int high)
+{
+    const EncodeTiled encode = encode_tiled();
+    if (!encode) return false;
+    const cuuint64_t dims[2] = {cuuint64_t(o.along_k ? k : dim), cuuint64_t(o.along_k ? dim : k)}, strides[1] = {cuuint64_t(o.ld) * 2};
+    const cuuint32_t box[2] = {64, cuuint32_t(o.along_k ? high : 64)}, one[2] = {1, 1};
+    return encode(map, dtype == RUBICK_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(o.p), dims, strides, box, one,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename T, ProductKind KIND, int BN, bool PAIR> cudaError_t launch(const ProductArgs &a, int num_sms, cudaStream_t st)
+{
+    using S = Shape<BN, PAIR>;
+    CUtensorMap map_a, map_b;
+    if (!operand_map(&map_a, a.a, a.dtype, a.m, a.k, BM) || !operand_map(&map_b, a.b, a.dtype, a.n, a.k, BN / S::CTAS)) return cudaErrorInvalidValue;
+    Tiling t;
+    t.tiles_m = int((a.m + BM * S::CTAS - 1) / (BM * S::CTAS));
+    t.tiles_n = int((a.n + BN - 1) / BN);
+    t.steps = int((a.k + BK - 1) / BK);
+    t.splits = KIND == PRODUCT_PART ? a.splits : 1;
+    t.all = int64_t(t.tiles_m) * t.tiles_n * t.splits;
+    const auto kernel = product_kernel<T, KIND, BN, PAIR>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SHARED);
+    if (e != cudaSuccess) return e;
+    const int64_t most = num_sms / S::CTAS;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(unsigned((t.all < most ? t.all : most) * S::CTAS));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = S::SHARED;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = S::CTAS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, a, t);
+    count_launch();
+    return e;
+}
+
+template <typename T, int BN, bool PAIR> cudaError_t product(ProductKind kind, const ProductArgs &a, int num_sms, cudaStream_t st)
+{
     switch (kind) {
-    case PRODUCT_OUT: product_kernel<T, PRODUCT_OUT><<<grid, 256, 0, st>>>(a); break;
-    case PRODUCT_STATS: product_kernel<T, PRODUCT_STATS><<<grid, 256, 0, st>>>(a); break;
-    case PRODUCT_GRAD: product_kernel<T, PRODUCT_GRAD><<<grid, 256, 0, st>>>(a); break;
-    case PRODUCT_PART: {
-        product_kernel<T, PRODUCT_PART><<<grid, 256, 0, st>>>(a);
-        const int64_t blocks = (a.m * ((a.n + 7) / 8) + 255) / 256, most = int64_t(num_sms) * 8;
-        join_kernel<T><<<int(blocks < most ? blocks : most), 256, 0, st>>>(a);
-        count_launch();
-        break;
+    case PRODUCT_OUT: return launch<T, PRODUCT_OUT, BN, PAIR>(a, num_sms, st);
+    case PRODUCT_STATS: return launch<T, PRODUCT_STATS, BN, PAIR>(a, num_sms, st);
+    case PRODUCT_GRAD: return launch<T, PRODUCT_GRAD, BN, PAIR>(a, num_sms, st);
+    case PRODUCT_PART: break;
     }
-    }
+    cudaError_t e = launch<T, PRODUCT_PART, BN, PAIR>(a, num_sms, st);
+    if (e != cudaSuccess) return e;
+    const int64_t blocks = (a.m * ((a.n + 7) / 8) + 255) / 256, most = int64_t(num_sms) * 8;
+    join_kernel<T><<<int(blocks < most ? blocks : most), 256, 0, st>>>(a);
     count_launch();
     return cudaGetLastError();
 }
+
+// Pairs of blocks (tiles of 256 x 256) where there are enough such tiles for half of the card's pairs; else single blocks
+// (128 x 128), with the k dealt out to several where there are fewer tiles than multiprocessors.
+bool in_pairs(const ProductArgs &a, int num_sms) { return ((a.m + 255) / 256) * ((a.n + 255) / 256) >= num_sms / 4; }
 
 }  // namespace
 
 int product_splits(const ProductArgs &a, int num_sms)
 {
-    const int64_t tiles = ((a.m + BM - 1) / BM) * ((a.n + BN - 1) / BN), most = (a.k + 255) / 256;
+    if (in_pairs(a, num_sms)) return 1;
+    const int64_t tiles = ((a.m + BM - 1) / BM) * ((a.n + 127) / 128), most = (a.k + 511) / 512;
     const int64_t s = num_sms / (tiles < 1 ? 1 : tiles);
     return int(s < 2 || most < 2 ? 1 : s < most ? s : most);
 }
 
+int product_stats_cols(const ProductArgs &a, int num_sms) { return in_pairs(a, num_sms) ? 128 : 64; }
+
+bool product_takes(const Operand &o) { return aligned16(o.p) && (o.ld & 7) == 0; }
+
+cudaError_t launch_lay_out(const void *from, int64_t ld_from, void *to, int64_t ld_to, int64_t rows, int64_t cols, cudaStream_t st)
+{
+    const int64_t across = (cols + 255) / 256;
+    lay_out_kernel<<<dim3(unsigned(across < 64 ? across : 64), unsigned(rows < 16384 ? rows : 16384)), 256, 0, st>>>(static_cast<const uint16_t *>(from), ld_from, static_cast<uint16_t *>(to), ld_to, rows, cols);
+    count_launch();
+    return cudaGetLastError();
+}
+
 cudaError_t launch_product(ProductKind kind, const ProductArgs &a, int num_sms, cudaStream_t st)
 {
-    return a.dtype == RUBICK_BF16 ? product<train::bf16>(kind, a, num_sms, st) : product<train::f16>(kind, a, num_sms, st);
+    if (in_pairs(a, num_sms)) return a.dtype == RUBICK_BF16 ? product<bf16, 256, true>(kind, a, num_sms, st) : product<f16, 256, true>(kind, a, num_sms, st);
+    return a.dtype == RUBICK_BF16 ? product<bf16, 128, false>(kind, a, num_sms, st) : product<f16, 128, false>(kind, a, num_sms, st);
 }
 
 }  // namespace rubick

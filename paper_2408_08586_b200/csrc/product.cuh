@@ -13,8 +13,6 @@ struct DropArgs { const uint64_t *seed; uint32_t below; float scale; };     // k
 
 enum ProductKind { PRODUCT_OUT, PRODUCT_PART, PRODUCT_STATS, PRODUCT_GRAD };
 
-constexpr int STATS_COLS = 128;          // columns of the logits that one pair (maximum, sum) covers
-
 struct ProductArgs {
     int64_t m, n, k;
     Operand a, b;
@@ -34,7 +32,7 @@ struct ProductArgs {
     // PRODUCT_STATS, PRODUCT_GRAD: the logits of vocabulary first .. first + n - 1
     const int32_t *label;
     int32_t first, vocab;
-    float2 *stats;                       // [ceil(n / STATS_COLS)][m]
+    float2 *stats;                       // [ceil(n / product_stats_cols)][m]
     float *at_label;                     // [m] logit of the label
     const float *base, *rest;            // log of the row's sum of exponentials, in two parts (rest may be NULL)
     const float *weight;                 // [m] weight of a row times the common power of two
@@ -81,7 +79,10 @@ struct HeadFinishArgs {
     float *base, *rest;                  // the row's maximum and the log of its sum behind it, or NULL
 };
 
-int product_splits(const ProductArgs &a, int num_sms);
+int product_splits(const ProductArgs &a, int num_sms);           // into how many parts the k are dealt out
+int product_stats_cols(const ProductArgs &a, int num_sms);       // columns of the logits that one pair (maximum, sum) covers
+bool product_takes(const Operand &o);                            // as it lies, that is
+cudaError_t launch_lay_out(const void *from, int64_t ld_from, void *to, int64_t ld_to, int64_t rows, int64_t cols, cudaStream_t st);
 cudaError_t launch_product(ProductKind kind, const ProductArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_dropout(const DropoutArgs &a, int num_sms, cudaStream_t st);
 int linear_grad_chunks(int64_t rows, int cols, int num_sms);

@@ -1,0 +1,131 @@
+// The fifth-generation tensor cores: tiles fetched by the tensor-copy engine, products of 16-bit operands summed in tensor
+// memory, and the barriers between those who fetch, multiply and read.
+#pragma once
+
+#include <cuda.h>
+
+#include "train_common.cuh"
+
+namespace rubick {
+namespace train {
+
+__device__ __forceinline__ uint32_t cluster_rank() { uint32_t r; asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r)); return r; }
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the address of the same place in the shared memory of the cluster's block `rank`
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void barrier_init_done() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// bar: an address in the cluster's shared memory
+__device__ __forceinline__ void barrier_arrive_at(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// Waits for a phase to end, a bounded number of times, and not at all once someone of the block has given up.
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t *given_up)
+{
+    for (int i = 0; i < (1 << 18); ++i) {
+        uint32_t done;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+        if (done) return true;
+        if (*given_up) return false;
+    }
+    *given_up = 1;
+    return false;
+}
+
+// A box of a matrix into shared memory; bar counts its bytes (with PAIR: a barrier of the pair's first block).
+template <bool PAIR> __device__ __forceinline__ void tensor_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    if constexpr (PAIR)
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                     ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+// ---- tensor memory ---------------------------------------------------------------------------------------------
+template <bool PAIR> __device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t columns)       // by a whole warp
+{
+    if constexpr (PAIR) asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(columns) : "memory");
+    else asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst), "r"(columns) : "memory");
+}
+template <bool PAIR> __device__ __forceinline__ void tmem_alloc_done()
+{
+    if constexpr (PAIR) asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    else asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+}
+template <bool PAIR> __device__ __forceinline__ void tmem_free(uint32_t at, uint32_t columns)
+{
+    if constexpr (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void tcgen_before_sync() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tcgen_after_sync() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// 32 columns of the warp's 32 lanes: lane i gets row i
+__device__ __forceinline__ void tmem_load32(uint32_t at, float (&v)[32])
+{
+    uint32_t r[32];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+                 "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];\n"
+                 "tcgen05.wait::ld.sync.aligned;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+                   "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(at));
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// ---- products --------------------------------------------------------------------------------------------------
+// An operand in shared memory, written by the copy engine with its 128-byte pattern (eight 16-byte pieces of a 128-byte line
+// exchanged by the number of the line modulo eight).  k next to each other: a line is 64 k of one row, eight rows make 1,024
+// bytes.  Rows next to each other: a line is 64 rows of one k, eight k make 1,024 bytes, 64 k a block of 64 rows.
+constexpr uint32_t BLOCK_BYTES = 64 * 128;
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, bool along_k)
+{
+    const uint64_t leading = along_k ? 1 : BLOCK_BYTES >> 4;          // between blocks of 64 rows
+    const uint64_t stride = 1024 >> 4;                                // between eight lines and the next
+    return uint64_t((addr & 0x3ffff) >> 4) | leading << 16 | stride << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+// ... 16 k further on, in 16-byte units
+__device__ __forceinline__ uint32_t operand_step(bool along_k) { return along_k ? 32 >> 4 : 16 * 128 >> 4; }
+
+// 16-bit operands, single-precision sums; m x n sums
+__host__ __device__ constexpr uint32_t instruction_desc(bool is_bf16, bool a_along_k, bool b_along_k, int m, int n)
+{
+    return 1u << 4 | uint32_t(is_bf16) << 7 | uint32_t(is_bf16) << 10 | uint32_t(!a_along_k) << 15 | uint32_t(!b_along_k) << 16 |
+           uint32_t(n >> 3) << 17 | uint32_t(m >> 4) << 24;
+}
+template <bool PAIR> __device__ __forceinline__ void multiply(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add)
+{
+    if constexpr (PAIR)
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(uint32_t(add)) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(desc), "r"(uint32_t(add)) : "memory");
+}
+// one arrival at bar (with PAIR: at the same place of both blocks) once everything this thread has multiplied is done
+template <bool PAIR> __device__ __forceinline__ void multiplied(uint32_t bar)
+{
+    if constexpr (PAIR)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(uint16_t(3)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+}  // namespace train
+}  // namespace rubick

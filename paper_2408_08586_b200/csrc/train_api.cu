@@ -187,6 +187,22 @@ cudaError_t run_product(rubick_ctx *ctx, const Planned &p, ProductArgs &a)
     return launch_product(p.kind, a, ctx->num_sms, ctx->stream);
 }
 
+// An operand that the products cannot read as it lies gets a place in scratch and is laid out anew there.
+struct Laid { bool copy; size_t at; int64_t rows, cols; };
+Laid plan_operand(Parts &parts, const Operand &o, int64_t rows, int64_t cols)
+{
+    if (product_takes(o)) return Laid{false, 0, rows, cols};
+    return Laid{true, parts.take(size_t(rows) * up8(cols) * 2), rows, cols};
+}
+cudaError_t lay_out(rubick_ctx *ctx, const Laid &l, Operand &o)
+{
+    if (!l.copy) return cudaSuccess;
+    const Operand to = {part<void>(ctx, l.at), up8(l.cols), o.along_k};
+    const cudaError_t e = launch_lay_out(o.p, o.ld, const_cast<void *>(to.p), to.ld, l.rows, l.cols, ctx->stream);
+    o = to;
+    return e;
+}
+
 // The head's loss, its gradient, or both.
 int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w, const int32_t *d_label,
               const float *d_lse_in, const float *d_dloss, float *d_loss, float *d_lse, void *d_dh, void *d_dw, bool forward, bool backward)
@@ -199,8 +215,15 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
         if (d_dw) CUDA_TRY(ctx, cudaMemset2DAsync(d_dw, size_t(d.ld_w) * 2, 0, size_t(by_output ? d.hidden : d.vocab) * 2, by_output ? d.vocab : d.hidden, ctx->stream), "clear dw");
         return RUBICK_OK;
     }
-    const int64_t ld_copy = up8(d.hidden), tiles = (int64_t(d.vocab) + STATS_COLS - 1) / STATS_COLS;
+    const int64_t ld_copy = up8(d.hidden);
     Parts parts;
+    ProductArgs z = {};
+    z.m = d.rows; z.n = d.vocab; z.k = d.hidden; z.dtype = d.dtype; z.status = ctx->d_status;
+    z.label = d_label; z.vocab = d.vocab;
+    const int unit = product_stats_cols(z, ctx->num_sms);
+    const int64_t tiles = (int64_t(d.vocab) + unit - 1) / unit;
+    Operand weight = {d_w, d.ld_w, by_output};
+    const Laid laid = plan_operand(parts, weight, by_output ? d.vocab : d.hidden, by_output ? d.hidden : d.vocab);
     const size_t at_copy = parts.take(size_t(d.rows) * ld_copy * 2);
     const size_t at_stats = forward ? parts.take(size_t(tiles) * d.rows * sizeof(float2)) : 0, at_label = forward ? parts.take(size_t(d.rows) * 4) : 0;
     const size_t at_base = forward && backward ? parts.take(size_t(d.rows) * 4) : 0, at_rest = forward && backward ? parts.take(size_t(d.rows) * 4) : 0;
@@ -222,7 +245,7 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
         h.status = w.status = ctx->d_status;
         h.m = d.rows; h.n = d.hidden; h.k = n;
         h.ld_out = d.ld_h; h.ld_acc = ld_copy;
-        h.b = Operand{static_cast<const char *>(d_w) + (by_output ? first * d.ld_w : first) * 2, d.ld_w, !by_output};
+        h.b = Operand{static_cast<const char *>(weight.p) + (by_output ? first * weight.ld : first) * 2, weight.ld, !by_output};
         h.out = d_dh;
         h.wide = wide16(d_dh, d.ld_h) ? WIDE_OUT : 0;
         w.k = d.rows;
@@ -250,13 +273,10 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     if (backward) { pre.weight = part<float>(ctx, at_weight); pre.scale = part<float>(ctx, at_scale); pre.largest = part<uint32_t>(ctx, at_scale) + 1; }
     CUDA_TRY(ctx, launch_head_prep(pre, ctx->num_sms, ctx->stream), "launch head_prep");
 
-    ProductArgs z = {};
-    z.m = d.rows; z.k = d.hidden; z.dtype = d.dtype; z.status = ctx->d_status;
+    CUDA_TRY(ctx, lay_out(ctx, laid, weight), "launch lay_out");
     z.a = Operand{pre.copy, ld_copy, 1};
-    z.label = d_label; z.vocab = d.vocab;
     if (forward) {
-        z.n = d.vocab;
-        z.b = Operand{d_w, d.ld_w, by_output};
+        z.b = weight;
         z.stats = part<float2>(ctx, at_stats); z.at_label = part<float>(ctx, at_label);
         CUDA_TRY(ctx, launch_product(PRODUCT_STATS, z, ctx->num_sms, ctx->stream), "launch product (logits)");
         HeadFinishArgs f = {};
@@ -274,7 +294,7 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
         ProductArgs h, w;
         gradient_products(first, n, h, w);
         z.n = n; z.first = int32_t(first);
-        z.b = Operand{h.b.p, d.ld_w, by_output};
+        z.b = Operand{h.b.p, weight.ld, by_output};
         z.out = part<void>(ctx, at_dz); z.ld_out = ld_dz;
         CUDA_TRY(ctx, launch_product(PRODUCT_GRAD, z, ctx->num_sms, ctx->stream), "launch product (logits' gradient)");
         h.scale = w.scale = pre.scale;
@@ -518,8 +538,11 @@ int rubick_linear_forward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, con
              (train::aligned16(d_bias) ? WIDE_BIAS : 0);
     a.drop = drop_args(d.p, d_seed);
     Parts parts;
+    const Laid x = plan_operand(parts, a.a, d.rows, d.inputs), w = plan_operand(parts, a.b, by_output ? d.outputs : d.inputs, by_output ? d.inputs : d.outputs);
     const Planned p = plan_product(parts, a, ctx->num_sms);
     if ((rc = scratch(ctx, parts.used))) return rc;
+    CUDA_TRY(ctx, lay_out(ctx, x, a.a), "launch lay_out (x)");
+    CUDA_TRY(ctx, lay_out(ctx, w, a.b), "launch lay_out (w)");
     CUDA_TRY(ctx, run_product(ctx, p, a), "launch linear_forward");
     return RUBICK_OK;
 }
@@ -565,6 +588,8 @@ int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, co
     dx.b = Operand{d_w, d.ld_w, !by_output};
     dw.m = by_output ? d.outputs : d.inputs; dw.n = by_output ? d.inputs : d.outputs; dw.k = d.rows;
     dw.out = d_dw; dw.ld_out = d.ld_w; dw.wide = wide16(d_dw, d.ld_w) ? WIDE_OUT : 0;
+    Operand x = {d_x, d.ld_x, 0};
+    const Laid laid_x = d_dw ? plan_operand(parts, x, d.rows, d.inputs) : Laid{}, laid_w = d_dx ? plan_operand(parts, dx.b, by_output ? d.outputs : d.inputs, by_output ? d.inputs : d.outputs) : Laid{};
     const size_t joined = parts.used;
     const Planned px = d_dx ? plan_product(parts, dx, ctx->num_sms) : Planned{};
     const size_t most = parts.used;
@@ -578,10 +603,12 @@ int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, co
     const int64_t ld_dz = keep ? g.ld_dz : d.ld_out;
     if (d_dx) {
         dx.a = Operand{dz, ld_dz, 1};
+        CUDA_TRY(ctx, lay_out(ctx, laid_w, dx.b), "launch lay_out (w)");
         CUDA_TRY(ctx, run_product(ctx, px, dx), "launch product (dx)");
     }
     if (d_dw) {
-        const Operand x = {d_x, d.ld_x, 0}, z = {dz, ld_dz, 0};
+        CUDA_TRY(ctx, lay_out(ctx, laid_x, x), "launch lay_out (x)");
+        const Operand z = {dz, ld_dz, 0};
         dw.a = by_output ? z : x;
         dw.b = by_output ? x : z;
         CUDA_TRY(ctx, run_product(ctx, pw, dw), "launch product (dw)");
