@@ -27,21 +27,21 @@ template <int BN, bool PAIR> struct Shape {
     static constexpr int SHARED = STAGES * STAGE + STAGING + 1024 + 256;      // 1,024 to begin on such a boundary
     static constexpr uint32_t COLUMNS = 2 * BN;                               // of tensor memory: two tiles
 };
-struct Tiling { int tiles_m, tiles_n, steps, splits; int64_t all; };
+struct Tiling { uint32_t tiles_m, tiles_n, each, all; int steps, per; };      // per: k stages of a split
 
 // Tile number -> tile row, tile column, split: eight tile rows at a time, so that what runs at once shares operands in L2.
-__device__ __forceinline__ void place(const Tiling &t, int64_t i, int &m, int &n, int &split)
+__device__ __forceinline__ void place(const Tiling &t, uint32_t i, int &m, int &n, int &split)
 {
-    const int64_t each = int64_t(t.tiles_m) * t.tiles_n;
-    split = int(i / each);
-    const int r = int(i - split * each), band = 8 * t.tiles_n, b = r / band, high = t.tiles_m - b * 8 < 8 ? t.tiles_m - b * 8 : 8, q = r - b * band;
-    m = b * 8 + q % high;
-    n = q / high;
+    const uint32_t s = t.all == t.each ? 0 : i / t.each, r = i - s * t.each, band = 8 * t.tiles_n, b = r / band, q = r - b * band;
+    const uint32_t high = t.tiles_m - b * 8 < 8 ? t.tiles_m - b * 8 : 8;
+    split = int(s);
+    n = int(q / high);
+    m = int(b * 8 + (q - n * high));
 }
 
 __device__ __forceinline__ float ninf() { return __uint_as_float(0xff800000u); }
 
-template <typename T, ProductKind KIND, int BN, bool PAIR>
+template <typename T, ProductKind KIND, int ACT, int BN, bool PAIR>
 __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                              const __grid_constant__ ProductArgs a, const __grid_constant__ Tiling t)
 {
@@ -71,18 +71,18 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
     if constexpr (PAIR) cluster_sync();
     tcgen_after_sync();
     const uint32_t tmem = words[1];
-    const int64_t first = blockIdx.x / S::CTAS, step = gridDim.x / S::CTAS;
+    const uint32_t first = blockIdx.x / S::CTAS, step = gridDim.x / S::CTAS;
 
     if (warp == 0) {
         if (lane == 0) {
             uint32_t round = 0;                      // stages filled so far
             bool fine = true;
-            for (int64_t i = first; fine && i < t.all; i += step) {
+            for (uint32_t i = first; fine && i < t.all; i += step) {
                 int tm, tn, split;
                 place(t, i, tm, tn, split);
                 const int m0 = (tm * S::CTAS + int(rank)) * BM, n0 = tn * BN + int(rank) * (BN / S::CTAS);
-                const int k1 = int(int64_t(t.steps) * (split + 1) / t.splits);
-                for (int k = int(int64_t(t.steps) * split / t.splits); k < k1; ++k, ++round) {
+                const int k0 = split * t.per, k1 = k0 + t.per < t.steps ? k0 + t.per : t.steps;
+                for (int k = k0; k < k1; ++k, ++round) {
                     const uint32_t s = round % S::STAGES, into = stages + s * S::STAGE;
                     if (!(fine = barrier_wait(empty + 8 * s, (round / S::STAGES & 1) ^ 1, given_up))) break;
                     if (rank == 0) barrier_expect(full + 8 * s, S::STAGE * S::CTAS);
@@ -110,9 +110,8 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             const uint32_t sa = operand_step(ak), sb = operand_step(bk);
             uint32_t round = 0, tile = 0;
             bool fine = true;
-            for (int64_t i = first; fine && i < t.all; i += step, ++tile) {
-                const int split = int(i / (int64_t(t.tiles_m) * t.tiles_n));
-                const int k0 = int(int64_t(t.steps) * split / t.splits), k1 = int(int64_t(t.steps) * (split + 1) / t.splits);
+            for (uint32_t i = first; fine && i < t.all; i += step, ++tile) {
+                const int k0 = t.all == t.each ? 0 : int(i / t.each) * t.per, k1 = k0 + t.per < t.steps ? k0 + t.per : t.steps;
                 const uint32_t half = tile & 1, d = tmem + half * BN;
                 if (!(fine = barrier_wait(taken + 8 * half, (tile / 2 & 1) ^ 1, given_up))) break;
                 tcgen_after_sync();
@@ -135,10 +134,10 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
     } else if (warp >= FIRST_READER) {
         const int quarter = warp & 3, side = (warp - FIRST_READER) >> 2;       // 32 rows, half of the columns
         uint8_t *const mine = shared + S::STAGES * S::STAGE + (warp - FIRST_READER) * 4096;
-        const Drop drop(a.drop);
-        const float scale = a.scale ? *a.scale : 1.f;
+        const Finish<T, ACT> finish(a);
+        const int64_t rows = a.m, cols = a.n;
         uint32_t tile = 0;
-        for (int64_t i = first; i < t.all; i += step, ++tile) {
+        for (uint32_t i = first; i < t.all; i += step, ++tile) {
             int tm, tn, split;
             place(t, i, tm, tn, split);
             const uint32_t half = tile & 1;
@@ -151,24 +150,44 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             if constexpr (KIND == PRODUCT_OUT || KIND == PRODUCT_PART) {
                 // 32 rows x 32 sums through shared memory, pieces of 16 bytes exchanged by the row, so that a warp then holds
                 // eight neighbouring sums a lane and its accesses cover whole sectors of eight rows
-                for (int c = 0; c < BN / 2; c += 32) {
-                    float v[32];
+                const int q = (lane & 3) * 2, above = lane >> 2;
+                const bool quick = KIND == PRODUCT_OUT && m0 + 32 <= rows && finish.takes_four();
+#pragma unroll 1
+                for (int c = 0; c < BN / 2 && n0 + c < cols; c += 32) {
+                    const int64_t col = n0 + c + q * 4;
+                    float v[32], bias[8];
+                    if constexpr (KIND == PRODUCT_OUT) finish.load_bias(col, bias);
                     tmem_load32(at + c, v);
-                    if (n0 + c >= a.n) continue;
 #pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        *reinterpret_cast<float4 *>(mine + lane * 128 + ((q ^ (lane & 7)) << 4)) = make_float4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                    for (int p = 0; p < 8; ++p)
+                        *reinterpret_cast<float4 *>(mine + lane * 128 + ((p ^ (lane & 7)) << 4)) = make_float4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
                     __syncwarp();
+                    float w[4][8];
 #pragma unroll
                     for (int r = 0; r < 4; ++r) {
-                        const int line = r * 8 + (lane >> 2), q = (lane & 3) * 2;
-                        const float4 x = *reinterpret_cast<const float4 *>(mine + line * 128 + ((q ^ (line & 7)) << 4));
-                        const float4 y = *reinterpret_cast<const float4 *>(mine + line * 128 + (((q + 1) ^ (line & 7)) << 4));
-                        float w[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                        const int64_t row = m0 + line, col = n0 + c + q * 4;
-                        if (row < a.m && col < a.n) {
-                            if constexpr (KIND == PRODUCT_OUT) finish8<T>(a, drop, scale, row, col, w);
-                            else store8<float>(a.part + (int64_t(split) * a.m + row) * a.ld_acc, col, a.ld_acc, true, w);
+                        const uint8_t *const line = mine + (r * 8 + above) * 128;
+                        const float4 x = *reinterpret_cast<const float4 *>(line + ((q ^ above) << 4)), y = *reinterpret_cast<const float4 *>(line + (((q + 1) ^ above) << 4));
+                        w[r][0] = x.x; w[r][1] = x.y; w[r][2] = x.z; w[r][3] = x.w; w[r][4] = y.x; w[r][5] = y.y; w[r][6] = y.z; w[r][7] = y.w;
+                    }
+                    if constexpr (KIND == PRODUCT_PART) {
+                        float *const to = a.part + (int64_t(split) * rows + m0 + above) * finish.ld_acc + col;
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            if (m0 + above + 8 * r < rows && col < cols) {
+                                *reinterpret_cast<float4 *>(to + 8 * r * finish.ld_acc) = make_float4(w[r][0], w[r][1], w[r][2], w[r][3]);
+                                *reinterpret_cast<float4 *>(to + 8 * r * finish.ld_acc + 4) = make_float4(w[r][4], w[r][5], w[r][6], w[r][7]);
+                            }
+                        }
+                    } else if (quick && n0 + c + 32 <= cols) {
+                        finish.four(m0 + above, col, w, bias);
+                    } else {
+                        // edges and rows at odd addresses: back through shared memory, so that this is one loop and not four copies
+#pragma unroll 1
+                        for (int r = 0; r < 4; ++r) {
+                            const uint8_t *const line = mine + (r * 8 + above) * 128;
+                            const float4 x = *reinterpret_cast<const float4 *>(line + ((q ^ above) << 4)), y = *reinterpret_cast<const float4 *>(line + (((q + 1) ^ above) << 4));
+                            float u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                            if (m0 + above + 8 * r < rows && col < cols) finish(m0 + above + 8 * r, col, u, bias);
                         }
                     }
                     __syncwarp();
@@ -176,12 +195,12 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             } else if constexpr (KIND == PRODUCT_STATS) {
                 // a thread has a row: running maximum and sum of exponentials over its columns
                 const int64_t row = m0 + lane;
-                const int64_t label = row < a.m ? int64_t(a.label[row]) - a.first - n0 : -1;
+                const int64_t label = row < rows ? int64_t(a.label[row]) - a.first - n0 : -1;
                 float top = ninf(), sum = 0.f;
                 for (int c = 0; c < BN / 2; c += 32) {
                     float v[32];
                     tmem_load32(at + c, v);
-                    const int64_t left = a.n - (n0 + c);
+                    const int64_t left = cols - (n0 + c);
                     if (left <= 0) continue;
                     if (left < 32) {
 #pragma unroll
@@ -202,11 +221,11 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                     sum = sum * ex2((top - from) * LOG2E) + (s0 + s1);
                     top = m;
                 }
-                if (row < a.m && n0 < a.n) a.stats[(int64_t(tn) * 2 + side) * a.m + row] = make_float2(top, sum);
+                if (row < rows && n0 < cols) a.stats[(int64_t(tn) * 2 + side) * rows + row] = make_float2(top, sum);
             } else {
                 // a thread has a row; 64 columns become 128 bytes of it, written line by line
                 const int64_t row = m0 + lane;
-                const bool in = row < a.m;
+                const bool in = row < rows;
                 const float from = in ? a.base[row] : 0.f, rest = in && a.rest ? a.rest[row] : 0.f, w = in ? a.weight[row] : 0.f;
                 const uint32_t mask = w == 0.f ? 0u : 0xffffffffu;            // (rows that take no part, whatever their logits are)
                 const int64_t label = in ? int64_t(a.label[row]) - a.first - n0 : -1;
@@ -236,7 +255,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                         const int line = r * 4 + (lane >> 3), q = lane & 7;
                         const uint4 p = *reinterpret_cast<const uint4 *>(mine + line * 128 + ((q ^ (line & 7)) << 4));
                         const int64_t to = m0 + line, col = n0 + c + q * 8;
-                        if (to < a.m && col < a.ld_out) *reinterpret_cast<uint4 *>(static_cast<T *>(a.out) + to * a.ld_out + col) = p;
+                        if (to < rows && col < finish.ld_out) *reinterpret_cast<uint4 *>(finish.out + to * finish.ld_out + col) = p;
                     }
                     __syncwarp();
                 }
@@ -256,21 +275,22 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
 }
 
 // The sums of the splits joined, and PRODUCT_OUT's epilogue.
-template <typename T> __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductArgs a)
+template <typename T, int ACT> __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductArgs a)
 {
-    const Drop drop(a.drop);
-    const float scale = a.scale ? *a.scale : 1.f;
+    const Finish<T, ACT> finish(a);
     const int64_t units = (a.n + 7) / 8, all = a.m * units;
     for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += int64_t(gridDim.x) * blockDim.x) {
         const int64_t row = i / units, c = (i - row * units) * 8;
-        float v[8] = {};
+        float v[8] = {}, bias[8];
+        finish.load_bias(c, bias);
+#pragma unroll 4
         for (int s = 0; s < a.splits; ++s) {
             float p[8];
             load8<float>(a.part + (int64_t(s) * a.m + row) * a.ld_acc, c, a.ld_acc, true, p);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += p[e];
         }
-        finish8<T>(a, drop, scale, row, c, v);
+        finish(row, c, v, bias);
     }
 }
 
@@ -305,23 +325,21 @@ bool operand_map(CUtensorMap *map, const Operand &o, int dtype, int64_t dim, int
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, ProductKind KIND, int BN, bool PAIR> cudaError_t launch(const ProductArgs &a, int num_sms, cudaStream_t st)
+template <typename T, ProductKind KIND, int ACT, int BN, bool PAIR> cudaError_t launch(const ProductArgs &a, int num_sms, cudaStream_t st)
 {
     using S = Shape<BN, PAIR>;
     CUtensorMap map_a, map_b;
     if (!operand_map(&map_a, a.a, a.dtype, a.m, a.k, BM) || !operand_map(&map_b, a.b, a.dtype, a.n, a.k, BN / S::CTAS)) return cudaErrorInvalidValue;
-    Tiling t;
-    t.tiles_m = int((a.m + BM * S::CTAS - 1) / (BM * S::CTAS));
-    t.tiles_n = int((a.n + BN - 1) / BN);
-    t.steps = int((a.k + BK - 1) / BK);
-    t.splits = KIND == PRODUCT_PART ? a.splits : 1;
-    t.all = int64_t(t.tiles_m) * t.tiles_n * t.splits;
-    const auto kernel = product_kernel<T, KIND, BN, PAIR>;
+    const int64_t tiles_m = (a.m + BM * S::CTAS - 1) / (BM * S::CTAS), tiles_n = (a.n + BN - 1) / BN, steps = (a.k + BK - 1) / BK;
+    const int64_t splits = KIND == PRODUCT_PART ? a.splits : 1, all = tiles_m * tiles_n * splits;
+    if (all > 0x7fffffff || steps > 0x7fffffff / BK) return cudaErrorInvalidValue;
+    const Tiling t = {uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(tiles_m * tiles_n), uint32_t(all), int(steps), int((steps + splits - 1) / splits)};
+    const auto kernel = product_kernel<T, KIND, ACT, BN, PAIR>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SHARED);
     if (e != cudaSuccess) return e;
     const int64_t most = num_sms / S::CTAS;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned((t.all < most ? t.all : most) * S::CTAS));
+    cfg.gridDim = dim3(unsigned((all < most ? all : most) * S::CTAS));
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = S::SHARED;
     cfg.stream = st;
@@ -335,20 +353,38 @@ template <typename T, ProductKind KIND, int BN, bool PAIR> cudaError_t launch(co
     return e;
 }
 
+template <typename T, int ACT> cudaError_t join(const ProductArgs &a, int num_sms, cudaStream_t st)
+{
+    const int64_t blocks = (a.m * ((a.n + 7) / 8) + 255) / 256, most = int64_t(num_sms) * 8;
+    join_kernel<T, ACT><<<int(blocks < most ? blocks : most), 256, 0, st>>>(a);
+    count_launch();
+    return cudaGetLastError();
+}
+
 template <typename T, int BN, bool PAIR> cudaError_t product(ProductKind kind, const ProductArgs &a, int num_sms, cudaStream_t st)
 {
     switch (kind) {
-    case PRODUCT_OUT: return launch<T, PRODUCT_OUT, BN, PAIR>(a, num_sms, st);
-    case PRODUCT_STATS: return launch<T, PRODUCT_STATS, BN, PAIR>(a, num_sms, st);
-    case PRODUCT_GRAD: return launch<T, PRODUCT_GRAD, BN, PAIR>(a, num_sms, st);
+    case PRODUCT_STATS: return launch<T, PRODUCT_STATS, RUBICK_ACT_NONE, BN, PAIR>(a, num_sms, st);
+    case PRODUCT_GRAD: return launch<T, PRODUCT_GRAD, RUBICK_ACT_NONE, BN, PAIR>(a, num_sms, st);
+    case PRODUCT_OUT:
+        switch (a.act) {
+        case RUBICK_ACT_RELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_RELU, BN, PAIR>(a, num_sms, st);
+        case RUBICK_ACT_GELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU, BN, PAIR>(a, num_sms, st);
+        case RUBICK_ACT_GELU_TANH: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU_TANH, BN, PAIR>(a, num_sms, st);
+        case RUBICK_ACT_SILU: return launch<T, PRODUCT_OUT, RUBICK_ACT_SILU, BN, PAIR>(a, num_sms, st);
+        }
+        return launch<T, PRODUCT_OUT, RUBICK_ACT_NONE, BN, PAIR>(a, num_sms, st);
     case PRODUCT_PART: break;
     }
-    cudaError_t e = launch<T, PRODUCT_PART, BN, PAIR>(a, num_sms, st);
+    const cudaError_t e = launch<T, PRODUCT_PART, RUBICK_ACT_NONE, BN, PAIR>(a, num_sms, st);
     if (e != cudaSuccess) return e;
-    const int64_t blocks = (a.m * ((a.n + 7) / 8) + 255) / 256, most = int64_t(num_sms) * 8;
-    join_kernel<T><<<int(blocks < most ? blocks : most), 256, 0, st>>>(a);
-    count_launch();
-    return cudaGetLastError();
+    switch (a.act) {
+    case RUBICK_ACT_RELU: return join<T, RUBICK_ACT_RELU>(a, num_sms, st);
+    case RUBICK_ACT_GELU: return join<T, RUBICK_ACT_GELU>(a, num_sms, st);
+    case RUBICK_ACT_GELU_TANH: return join<T, RUBICK_ACT_GELU_TANH>(a, num_sms, st);
+    case RUBICK_ACT_SILU: return join<T, RUBICK_ACT_SILU>(a, num_sms, st);
+    }
+    return join<T, RUBICK_ACT_NONE>(a, num_sms, st);
 }
 
 // Pairs of blocks (tiles of 256 x 256) where there are enough such tiles for half of the card's pairs; else single blocks
@@ -360,9 +396,11 @@ bool in_pairs(const ProductArgs &a, int num_sms) { return ((a.m + 255) / 256) * 
 int product_splits(const ProductArgs &a, int num_sms)
 {
     if (in_pairs(a, num_sms)) return 1;
-    const int64_t tiles = ((a.m + BM - 1) / BM) * ((a.n + 127) / 128), most = (a.k + 511) / 512;
-    const int64_t s = num_sms / (tiles < 1 ? 1 : tiles);
-    return int(s < 2 || most < 2 ? 1 : s < most ? s : most);
+    const int64_t tiles = ((a.m + BM - 1) / BM) * ((a.n + 127) / 128), steps = (a.k + BK - 1) / BK, most = (steps + 7) / 8;
+    int64_t s = num_sms / (tiles < 1 ? 1 : tiles);
+    s = s < 2 || most < 2 ? 1 : s < most ? s : most;
+    const int64_t per = (steps + s - 1) / s;
+    return int((steps + per - 1) / per);              // (no split is left without work)
 }
 
 int product_stats_cols(const ProductArgs &a, int num_sms) { return in_pairs(a, num_sms) ? 128 : 64; }

@@ -27,8 +27,9 @@ __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// bar: an address in the cluster's shared memory
-__device__ __forceinline__ void barrier_arrive_at(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// bar: an address in the cluster's shared memory.  What it reports is that tensor memory has been read (ordered by the fences
+// of tcgen05); it does not wait for this thread's stores, which a releasing arrival would (1,000 cycles a tile).
+__device__ __forceinline__ void barrier_arrive_at(uint32_t bar) { asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // Waits for a phase to end, a bounded number of times, and not at all once someone of the block has given up.
 __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile uint32_t *given_up)
 {
