@@ -181,13 +181,45 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                     } else if (quick && n0 + c + 32 <= cols) {
                         finish.four(m0 + above, col, w, bias);
                     } else {
-                        // edges and rows at odd addresses: back through shared memory, so that this is one loop and not four copies
+                        // Edges, and rows at any address: what is eight sums a lane goes back to where it was, and tensors are read and
+                        // written a row at a time, a column a lane (eight 2-byte stores a lane would touch every sector 16 times).
+                        const int64_t column = n0 + c + lane;
+                        const int high = rows - m0 < 32 ? int(rows - m0) : 32;
+                        auto cell = [&](int r) { return reinterpret_cast<float *>(mine + r * 128 + (((lane >> 2) ^ (r & 7)) << 4)) + (lane & 3); };
+                        bool over = false;
+                        for (int pass = 0; pass < 2 && !over; ++pass) {
+                            if (pass == 1 && finish.pre) {
+                                __syncwarp();
+                                if (column < cols)
+                                    for (int r = 0; r < high; ++r) finish.pre[(m0 + r) * finish.ld_pre + column] = from_f<T>(*cell(r));
+                                __syncwarp();
+                            }
 #pragma unroll 1
-                        for (int r = 0; r < 4; ++r) {
-                            const uint8_t *const line = mine + (r * 8 + above) * 128;
-                            const float4 x = *reinterpret_cast<const float4 *>(line + ((q ^ above) << 4)), y = *reinterpret_cast<const float4 *>(line + (((q + 1) ^ above) << 4));
-                            float u[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-                            if (m0 + above + 8 * r < rows && col < cols) finish(m0 + above + 8 * r, col, u, bias);
+                            for (int r = 0; r < 4; ++r) {
+                                uint8_t *const line = mine + (r * 8 + above) * 128;
+                                float4 *const fx = reinterpret_cast<float4 *>(line + ((q ^ above) << 4)), *const fy = reinterpret_cast<float4 *>(line + (((q + 1) ^ above) << 4));
+                                float u[8] = {fx->x, fx->y, fx->z, fx->w, fy->x, fy->y, fy->z, fy->w};
+                                const int64_t row = m0 + above + 8 * r;
+                                if (pass == 0) {
+                                    if (row < rows && col < cols) finish.accumulate(row, col, u);
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) u[e] += bias[e];
+                                } else {
+                                    finish.activate(row, col, u);
+                                }
+                                *fx = make_float4(u[0], u[1], u[2], u[3]);
+                                *fy = make_float4(u[4], u[5], u[6], u[7]);
+                            }
+                            over = finish.acc_out != nullptr;
+                        }
+                        __syncwarp();
+                        if (!over && column < cols) {
+#pragma unroll 4
+                            for (int r = 0; r < high; ++r) {
+                                float u = *cell(r);
+                                if (finish.residual) u += to_f(finish.residual[(m0 + r) * finish.ld_res + column]);
+                                finish.out[(m0 + r) * finish.ld_out + column] = from_f<T>(u);
+                            }
                         }
                     }
                     __syncwarp();
@@ -294,11 +326,17 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256) join_kerne
     }
 }
 
-// Rows laid out anew, on 16-byte boundaries (the copy engine takes no others).
-__global__ void __launch_bounds__(256) lay_out_kernel(const uint16_t *from, int64_t ld_from, uint16_t *to, int64_t ld_to, int64_t rows, int64_t cols)
+// Rows laid out anew, on 16-byte boundaries (the copy engine takes no others); up to two matrices at once.
+__global__ void __launch_bounds__(256) lay_out_kernel(const __grid_constant__ LayOutArgs a)
 {
-    for (int64_t row = blockIdx.y; row < rows; row += gridDim.y)
-        for (int64_t c = int64_t(blockIdx.x) * 256 + threadIdx.x; c < cols; c += int64_t(gridDim.x) * 256) to[row * ld_to + c] = from[row * ld_from + c];
+    const LayOutArgs::One &o = a.one[blockIdx.z];
+    const uint16_t *const from = static_cast<const uint16_t *>(o.from);
+    uint16_t *const to = static_cast<uint16_t *>(o.to);
+    const int64_t units = (o.cols + 7) / 8;
+    for (int64_t row = blockIdx.y * 4 + (threadIdx.x >> 6); row < o.rows; row += gridDim.y * 4)
+#pragma unroll 2
+        for (int64_t u = blockIdx.x * 64 + (threadIdx.x & 63); u < units; u += gridDim.x * 64)
+            *reinterpret_cast<uint4 *>(to + row * o.ld_to + u * 8) = load_any(reinterpret_cast<const bf16 *>(from) + row * o.ld_from, u * 8, o.cols);
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -407,10 +445,20 @@ int product_stats_cols(const ProductArgs &a, int num_sms) { return in_pairs(a, n
 
 bool product_takes(const Operand &o) { return aligned16(o.p) && (o.ld & 7) == 0; }
 
-cudaError_t launch_lay_out(const void *from, int64_t ld_from, void *to, int64_t ld_to, int64_t rows, int64_t cols, cudaStream_t st)
+cudaError_t launch_lay_out(const LayOutArgs &a, int num_sms, cudaStream_t st)
 {
-    const int64_t across = (cols + 255) / 256;
-    lay_out_kernel<<<dim3(unsigned(across < 64 ? across : 64), unsigned(rows < 16384 ? rows : 16384)), 256, 0, st>>>(static_cast<const uint16_t *>(from), ld_from, static_cast<uint16_t *>(to), ld_to, rows, cols);
+    if (a.n == 0) return cudaSuccess;
+    int64_t across = 1, high = 1;
+    for (int i = 0; i < a.n; ++i) {
+        const int64_t x = (a.one[i].cols + 511) / 512, y = (a.one[i].rows + 3) / 4;
+        across = x > across ? x : across;
+        high = y > high ? y : high;
+    }
+    const int64_t places = int64_t(num_sms) * 8;
+    across = across < places ? across : places;
+    const int64_t most = (places + across - 1) / across;
+    high = high < most ? high : most;
+    lay_out_kernel<<<dim3(unsigned(across), unsigned(high), a.n), 256, 0, st>>>(a);
     count_launch();
     return cudaGetLastError();
 }

@@ -45,6 +45,8 @@ struct DropoutArgs {
     const void *x, *residual;
     void *out;
     DropArgs drop;
+    bool wide;                           // every row begins on a 16-byte boundary
+    int lanes, strips, chunks;           // threads that share a row (a power of two), strips of columns, runs of rows
 };
 // dz = act'(pre) drop(dout) with its column sums
 struct LinearGradArgs {
@@ -55,7 +57,10 @@ struct LinearGradArgs {
     void *dz;                            // NULL: only the column sums are wanted
     float *dbias;                        // or NULL
     float *part;                         // [chunks][cols] sums of row chunks
-    int chunks;
+    uint32_t *tickets;                   // [strips] arrivals, zero between calls
+    int chunks, strips;                  // of rows, of columns
+    bool wide;                           // every row of dout and pre begins on a 16-byte boundary
+    int lanes;                           // lanes of a warp that share a row (a power of two); the others take further rows
 };
 // rows of h whose label takes part (zeros for the others), next to each other; the largest weight of a row
 struct HeadPrepArgs {
@@ -79,33 +84,28 @@ struct HeadFinishArgs {
     float *base, *rest;                  // the row's maximum and the log of its sum behind it, or NULL
 };
 
+struct LayOutArgs {
+    struct One { const void *from; int64_t ld_from; void *to; int64_t ld_to, rows, cols; } one[2];
+    int n;
+};
+
 int product_splits(const ProductArgs &a, int num_sms);           // into how many parts the k are dealt out
 int product_stats_cols(const ProductArgs &a, int num_sms);       // columns of the logits that one pair (maximum, sum) covers
 bool product_takes(const Operand &o);                            // as it lies, that is
-cudaError_t launch_lay_out(const void *from, int64_t ld_from, void *to, int64_t ld_to, int64_t rows, int64_t cols, cudaStream_t st);
+cudaError_t launch_lay_out(const LayOutArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_product(ProductKind kind, const ProductArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_dropout(const DropoutArgs &a, int num_sms, cudaStream_t st);
-int linear_grad_chunks(int64_t rows, int cols, int num_sms);
+void plan_linear_grad(LinearGradArgs &a, int num_sms);
 cudaError_t launch_linear_grad(const LinearGradArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_head_prep(const HeadPrepArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_head_finish(const HeadFinishArgs &a, int num_sms, cudaStream_t st);
 
 namespace train {
 
-// ---- Philox4x32-10 (Salmon et al., SC 2011): four words of a counter under a key -------------------------------------
-__device__ __forceinline__ uint4 philox(uint32_t quad, uint32_t row, uint64_t seed, uint64_t offset)
-{
-    uint32_t c0 = quad, c1 = row, c2 = uint32_t(offset), c3 = uint32_t(offset >> 32);
-    uint32_t k0 = uint32_t(seed), k1 = uint32_t(seed >> 32);
-#pragma unroll
-    for (int i = 0; i < 10; ++i) {
-        const uint64_t a = uint64_t(0xD2511F53u) * c0, b = uint64_t(0xCD9E8D57u) * c2;
-        c0 = uint32_t(b >> 32) ^ c1 ^ k0; c1 = uint32_t(b);
-        c2 = uint32_t(a >> 32) ^ c3 ^ k1; c3 = uint32_t(a);
-        k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
-    }
-    return make_uint4(c0, c1, c2, c3);
-}
+// ---- dropout: Philox4x32-10 (Salmon et al., SC 2011), the four words of a counter under a key -------------------------
+// A round takes (c0, c1, c2, c3) to (hi(M1 c2) ^ c1 ^ k0, lo(M1 c2), hi(M0 c0) ^ c3 ^ k1, lo(M0 c0)).  The counter is (column / 4,
+// row, offset), so what of its first three rounds does not depend on the row is worked out once for a thread's columns:
+// of the 20 products of a counter 15 are left to each row, and one for all of a row's counters.
 struct Drop {
     uint64_t seed, offset;
     uint32_t below;
@@ -115,15 +115,48 @@ struct Drop {
     {
         if (on) { seed = a.seed[0]; offset = a.seed[1]; }
     }
-    // VE elements of a row from column c (a multiple of four)
-    template <int VE> __device__ __forceinline__ void apply(int64_t row, int c, float (&v)[VE]) const
+};
+template <int VE> struct DropColumns {
+    static_assert(VE % 4 == 0, "a counter serves four columns");
+    static constexpr uint32_t M0 = 0xD2511F53u, M1 = 0xCD9E8D57u, W0 = 0x9E3779B9u, W1 = 0xBB67AE85u;
+    uint32_t k0, k1, row_key, below;
+    uint32_t second[VE / 4], third[VE / 4], fourth[VE / 4], fifth[VE / 4];
+    __device__ __forceinline__ static uint32_t hi(uint64_t v) { return uint32_t(v >> 32); }
+    __device__ __forceinline__ static uint32_t lo(uint64_t v) { return uint32_t(v); }
+    // from column c on (a multiple of four)
+    __device__ __forceinline__ DropColumns(const Drop &d, int c) : k0(uint32_t(d.seed)), k1(uint32_t(d.seed >> 32)), below(d.below)
     {
-        static_assert(VE % 4 == 0, "a counter serves four columns");
+        const uint64_t b1 = uint64_t(M1) * uint32_t(d.offset);
+        row_key = hi(b1) ^ k0;                                         // round 1: c0 = row ^ row_key
 #pragma unroll
-        for (int q = 0; q < VE; q += 4) {
-            const uint4 w = philox(uint32_t(c + q) >> 2, uint32_t(row), seed, offset);
-            v[q] = w.x >= below ? v[q] * scale : 0.f; v[q + 1] = w.y >= below ? v[q + 1] * scale : 0.f;
-            v[q + 2] = w.z >= below ? v[q + 2] * scale : 0.f; v[q + 3] = w.w >= below ? v[q + 3] * scale : 0.f;
+        for (int q = 0; q < VE / 4; ++q) {
+            const uint64_t a1 = uint64_t(M0) * (uint32_t(c) / 4 + q);
+            const uint32_t c2 = hi(a1) ^ uint32_t(d.offset >> 32) ^ k1, c3 = lo(a1);
+            second[q] = c3 ^ (k1 + W1);                                // round 2: c2 = hi(M0 c0) ^ second, c3 = lo(M0 c0)
+            const uint64_t b2 = uint64_t(M1) * c2;
+            const uint32_t c0 = hi(b2) ^ lo(b1) ^ (k0 + W0);
+            third[q] = lo(b2) ^ (k0 + 2 * W0);                         // round 3: c0 = hi(M1 c2) ^ third, c1 = lo(M1 c2)
+            const uint64_t a3 = uint64_t(M0) * c0;
+            fourth[q] = hi(a3) ^ (k1 + 2 * W1);                        //          c2 = c3 ^ fourth
+            fifth[q] = lo(a3);                                         //          c3
+        }
+    }
+    // 0 where an element of the row is dropped; the others still lack their factor
+    __device__ __forceinline__ void choose(uint32_t row, float (&v)[VE]) const
+    {
+        const uint64_t a2 = uint64_t(M0) * (row ^ row_key);
+#pragma unroll
+        for (int q = 0; q < VE / 4; ++q) {
+            const uint64_t b3 = uint64_t(M1) * (hi(a2) ^ second[q]);
+            uint32_t c0 = hi(b3) ^ third[q], c1 = lo(b3), c2 = lo(a2) ^ fourth[q], c3 = fifth[q];
+#pragma unroll
+            for (uint32_t i = 3; i < 10; ++i) {
+                const uint64_t a = uint64_t(M0) * c0, b = uint64_t(M1) * c2;
+                c0 = hi(b) ^ c1 ^ (k0 + i * W0); c1 = lo(b);
+                c2 = hi(a) ^ c3 ^ (k1 + i * W1); c3 = lo(a);
+            }
+            v[4 * q] = c0 >= below ? v[4 * q] : 0.f; v[4 * q + 1] = c1 >= below ? v[4 * q + 1] : 0.f;
+            v[4 * q + 2] = c2 >= below ? v[4 * q + 2] : 0.f; v[4 * q + 3] = c3 >= below ? v[4 * q + 3] : 0.f;
         }
     }
 };
@@ -132,11 +165,23 @@ struct Drop {
 // v / (1 + exp(-u)): where the exponential overflows the quick division gives the right 0
 __device__ __forceinline__ float over_one_plus_exp(float v, float u) { return __fdividef(v, 1.f + __expf(-u)); }
 __device__ __forceinline__ float tanh_arg2(float v) { return 1.5957691216057308f * (v + 0.044715f * v * v * v); }   // 2 sqrt(2 / pi) ..
+// Phi(v), the normal distribution's integral, and exp(-v^2 / 2): erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x),
+// x = |v| / sqrt(2) (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: off by 1.5e-7 at most).  The
+// exponential is the one that the slope needs as well, and on the far left nothing cancels, as in 1 + erf.
+__device__ __forceinline__ float normal_integral(float v, float &bell)
+{
+    const float x = fabsf(v) * 0.70710678118654752f, t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
+    bell = __expf(-0.5f * v * v);
+    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float tail = 0.5f * p * bell;
+    return v > 0.f ? 1.f - tail : tail;
+}
 __device__ __forceinline__ float act_value(int act, float v)
 {
+    float bell;
     switch (act) {
     case RUBICK_ACT_RELU: return v > 0.f ? v : (v != v ? v : 0.f);
-    case RUBICK_ACT_GELU: return 0.5f * v * erfcf(-0.70710678118654752f * v);     // (1 + erf would cancel on the far left)
+    case RUBICK_ACT_GELU: return v * normal_integral(v, bell);
     case RUBICK_ACT_GELU_TANH: return over_one_plus_exp(v, tanh_arg2(v));          // (1 + tanh u) / 2 = 1 / (1 + exp(-2 u))
     case RUBICK_ACT_SILU: return over_one_plus_exp(v, v);
     }
@@ -144,21 +189,65 @@ __device__ __forceinline__ float act_value(int act, float v)
 }
 __device__ __forceinline__ float act_slope(int act, float v)
 {
+    float bell;
     switch (act) {
     case RUBICK_ACT_RELU: return v > 0.f ? 1.f : (v != v ? v : 0.f);
-    case RUBICK_ACT_GELU: return 0.5f * erfcf(-0.70710678118654752f * v) + v * 0.3989422804014327f * __expf(-0.5f * v * v);
+    case RUBICK_ACT_GELU: {
+        const float phi = normal_integral(v, bell);
+        return fmaf(v * 0.3989422804014327f, bell, phi);
+    }
+    // with s = 1 / (1 + exp(-u)), 1 - s (off by half a step of one, in products with what stays below one)
     case RUBICK_ACT_GELU_TANH: {
-        const float s = over_one_plus_exp(1.f, tanh_arg2(v)), r = over_one_plus_exp(1.f, -tanh_arg2(v));   // r = 1 - s
-        return s + s * r * v * 1.5957691216057308f * (1.f + 0.134145f * v * v);
+        const float s = over_one_plus_exp(1.f, tanh_arg2(v));
+        return s + s * (1.f - s) * v * 1.5957691216057308f * (1.f + 0.134145f * v * v);
     }
     case RUBICK_ACT_SILU: {
-        const float s = over_one_plus_exp(1.f, v), r = over_one_plus_exp(1.f, -v);
-        return s * (1.f + v * r);
+        const float s = over_one_plus_exp(1.f, v);
+        return s * (1.f + v * (1.f - s));
     }
     }
     return 1.f;
 }
 
+// 16 bytes of a row from column c on, whatever its alignment: the two aligned pieces that hold them, shifted, where both lie
+// within the row, else element by element (0 past the end).
+template <typename T> __device__ __forceinline__ uint4 load_any(const T *row, int64_t c, int64_t n)
+{
+    constexpr int N = Lanes<T>::N;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(row + c), from = at & ~uintptr_t(15);
+    const uint32_t off = uint32_t(at) & 15;
+    if (c + N <= n && from >= reinterpret_cast<uintptr_t>(row) && from + 32 <= reinterpret_cast<uintptr_t>(row + n)) {
+        const uint4 a = ld_cached(reinterpret_cast<const void *>(from)), b = ld_cached(reinterpret_cast<const void *>(from + 16));
+        uint32_t w[7] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z};
+        uint32_t last = b.w;
+        if (off & 4) {
+#pragma unroll
+            for (int i = 0; i < 6; ++i) w[i] = w[i + 1];
+            w[6] = last; last = 0;
+        }
+        if (off & 8) {
+#pragma unroll
+            for (int i = 0; i < 5; ++i) w[i] = w[i + 2];
+            w[5] = last;
+        }
+        const uint32_t bits = (off & 3) * 8;
+        return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+    }
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        if (c + e < n) {
+            if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(row[c + e]);
+            else w[e >> 1] |= uint32_t(reinterpret_cast<const uint16_t *>(row)[c + e]) << (16 * (e & 1));
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// ... with the word that says whether every row begins on a 16-byte boundary
+template <typename T> __device__ __forceinline__ uint4 load_raw(const T *row, int64_t c, int64_t n, bool wide)
+{
+    return wide && c + Lanes<T>::N <= n ? ld_stream(row + c) : load_any(row, c, n);
+}
 // Eight elements of a row from column c on (a multiple of eight), 16 bytes at a time where the tensor allows it; columns
 // from n on are not touched.
 template <typename T> __device__ __forceinline__ void load8(const T *row, int64_t c, int64_t n, bool wide, float (&v)[8])
@@ -218,7 +307,8 @@ template <typename T, int ACT> struct Finish {
         if (bias_f32) load8<float>(static_cast<const float *>(bias), c, n, wide & WIDE_BIAS, b);
         else load8<T>(static_cast<const T *>(bias), c, n, wide & WIDE_BIAS, b);
     }
-    __device__ __forceinline__ void operator()(int64_t row, int64_t c, float (&v)[8], const float (&b)[8]) const
+    // the sum so far; true: that is all there is to do
+    __device__ __forceinline__ bool accumulate(int64_t row, int64_t c, float (&v)[8]) const
     {
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= scale;
@@ -228,15 +318,28 @@ template <typename T, int ACT> struct Finish {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += s[e];
         }
-        if (acc_out) { store8<float>(acc_out + row * ld_acc, c, ld_acc, true, v); return; }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] += b[e];
-        if (pre) store8<T>(pre + row * ld_pre, c, n, wide & WIDE_PRE, v);
+        if (acc_out) store8<float>(acc_out + row * ld_acc, c, ld_acc, true, v);
+        return acc_out != nullptr;
+    }
+    __device__ __forceinline__ void activate(int64_t row, int64_t c, float (&v)[8]) const
+    {
         if constexpr (ACT != RUBICK_ACT_NONE) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = act_value(ACT, v[e]);
         }
-        if (drop.on) drop.apply<8>(row, int(c), v);
+        if (drop.on) {
+            DropColumns<8>(drop, int(c)).choose(uint32_t(row), v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= drop.scale;
+        }
+    }
+    __device__ __forceinline__ void operator()(int64_t row, int64_t c, float (&v)[8], const float (&b)[8]) const
+    {
+        if (accumulate(row, c, v)) return;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += b[e];
+        if (pre) store8<T>(pre + row * ld_pre, c, n, wide & WIDE_PRE, v);
+        activate(row, c, v);
         if (residual) {
             float r[8];
             load8<T>(residual + row * ld_res, c, n, wide & WIDE_RES, r);
@@ -270,8 +373,13 @@ template <typename T, int ACT> struct Finish {
                 for (int e = 0; e < 8; ++e) v[r][e] = act_value(ACT, v[r][e]);
         }
         if (drop.on) {
+            const DropColumns<8> columns(drop, int(c));
 #pragma unroll
-            for (int r = 0; r < 4; ++r) drop.apply<8>(row + 8 * r, int(c), v[r]);
+            for (int r = 0; r < 4; ++r) {
+                columns.choose(uint32_t(row + 8 * r), v[r]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[r][e] *= drop.scale;
+            }
         }
         if (residual) {
 #pragma unroll

@@ -194,13 +194,12 @@ Laid plan_operand(Parts &parts, const Operand &o, int64_t rows, int64_t cols)
     if (product_takes(o)) return Laid{false, 0, rows, cols};
     return Laid{true, parts.take(size_t(rows) * up8(cols) * 2), rows, cols};
 }
-cudaError_t lay_out(rubick_ctx *ctx, const Laid &l, Operand &o)
+void lay_out(rubick_ctx *ctx, LayOutArgs &all, const Laid &l, Operand &o)
 {
-    if (!l.copy) return cudaSuccess;
+    if (!l.copy) return;
     const Operand to = {part<void>(ctx, l.at), up8(l.cols), o.along_k};
-    const cudaError_t e = launch_lay_out(o.p, o.ld, const_cast<void *>(to.p), to.ld, l.rows, l.cols, ctx->stream);
+    all.one[all.n++] = LayOutArgs::One{o.p, o.ld, const_cast<void *>(to.p), to.ld, l.rows, l.cols};
     o = to;
-    return e;
 }
 
 // The head's loss, its gradient, or both.
@@ -273,7 +272,9 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     if (backward) { pre.weight = part<float>(ctx, at_weight); pre.scale = part<float>(ctx, at_scale); pre.largest = part<uint32_t>(ctx, at_scale) + 1; }
     CUDA_TRY(ctx, launch_head_prep(pre, ctx->num_sms, ctx->stream), "launch head_prep");
 
-    CUDA_TRY(ctx, lay_out(ctx, laid, weight), "launch lay_out");
+    LayOutArgs lay = {};
+    lay_out(ctx, lay, laid, weight);
+    CUDA_TRY(ctx, launch_lay_out(lay, ctx->num_sms, ctx->stream), "launch lay_out");
     z.a = Operand{pre.copy, ld_copy, 1};
     if (forward) {
         z.b = weight;
@@ -541,8 +542,10 @@ int rubick_linear_forward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, con
     const Laid x = plan_operand(parts, a.a, d.rows, d.inputs), w = plan_operand(parts, a.b, by_output ? d.outputs : d.inputs, by_output ? d.inputs : d.outputs);
     const Planned p = plan_product(parts, a, ctx->num_sms);
     if ((rc = scratch(ctx, parts.used))) return rc;
-    CUDA_TRY(ctx, lay_out(ctx, x, a.a), "launch lay_out (x)");
-    CUDA_TRY(ctx, lay_out(ctx, w, a.b), "launch lay_out (w)");
+    LayOutArgs lay = {};
+    lay_out(ctx, lay, x, a.a);
+    lay_out(ctx, lay, w, a.b);
+    CUDA_TRY(ctx, launch_lay_out(lay, ctx->num_sms, ctx->stream), "launch lay_out");
     CUDA_TRY(ctx, run_product(ctx, p, a), "launch linear_forward");
     return RUBICK_OK;
 }
@@ -575,7 +578,7 @@ int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, co
     LinearGradArgs g = {};
     g.rows = d.rows; g.ld_dout = d.ld_out; g.ld_pre = d.ld_pre; g.ld_dz = up8(d.outputs); g.cols = d.outputs; g.dtype = d.dtype; g.act = d.activation;
     g.dout = d_dout; g.pre = d_pre; g.drop = drop_args(d.p, d_seed); g.dbias = d_dbias;
-    g.chunks = linear_grad_chunks(d.rows, d.outputs, ctx->num_sms);
+    plan_linear_grad(g, ctx->num_sms);
     Parts parts;
     const bool keep = products && !plain;
     const size_t at_dz = keep ? parts.take(size_t(d.rows) * g.ld_dz * 2) : 0;
@@ -598,16 +601,22 @@ int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, co
     if ((rc = scratch(ctx, parts.used > most ? parts.used : most))) return rc;
     if (keep) g.dz = part<void>(ctx, at_dz);
     if (d_dbias) g.part = part<float>(ctx, at_sums);
+    if (d_dbias && g.chunks > 1) {
+        if ((rc = tickets(ctx, size_t(g.strips)))) return rc;
+        g.tickets = ctx->d_tickets;
+    }
     if (keep || d_dbias) CUDA_TRY(ctx, launch_linear_grad(g, ctx->num_sms, ctx->stream), "launch linear_grad");
+    LayOutArgs lay = {};
+    if (d_dw) lay_out(ctx, lay, laid_x, x);
+    if (d_dx) lay_out(ctx, lay, laid_w, dx.b);
+    CUDA_TRY(ctx, launch_lay_out(lay, ctx->num_sms, ctx->stream), "launch lay_out");
     const void *dz = keep ? g.dz : d_dout;
     const int64_t ld_dz = keep ? g.ld_dz : d.ld_out;
     if (d_dx) {
         dx.a = Operand{dz, ld_dz, 1};
-        CUDA_TRY(ctx, lay_out(ctx, laid_w, dx.b), "launch lay_out (w)");
         CUDA_TRY(ctx, run_product(ctx, px, dx), "launch product (dx)");
     }
     if (d_dw) {
-        CUDA_TRY(ctx, lay_out(ctx, laid_x, x), "launch lay_out (x)");
         const Operand z = {dz, ld_dz, 0};
         dw.a = by_output ? z : x;
         dw.b = by_output ? x : z;
