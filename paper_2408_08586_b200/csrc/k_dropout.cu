@@ -8,48 +8,54 @@ using namespace train;
 
 // out = residual + drop(x), 16 bytes of columns a thread: a block takes a strip of columns of a run of rows, so that a thread
 // keeps to its columns and to what the generator needs of them.
-template <typename T> __global__ void __launch_bounds__(256, 3) dropout_kernel(const __grid_constant__ DropoutArgs a)
+template <typename T, int LANES, bool RESIDUAL, bool WIDE> __global__ void __launch_bounds__(256, 3) dropout_kernel(const __grid_constant__ DropoutArgs a)
 {
-    constexpr int VE = Lanes<T>::N, ROWS = 2;
-    __shared__ uint4 staged[256];
-    const Drop drop(a.drop);
-    const int cols = a.d.cols, lanes = a.lanes, lane = threadIdx.x & 31, first = blockIdx.x * lanes * VE, step = 256 / lanes;
-    const int c = first + (threadIdx.x & (lanes - 1)) * VE;
-    const DropColumns<VE> columns(drop, c);
-    const int64_t per = (a.d.rows + a.chunks - 1) / a.chunks, from = per * blockIdx.y, to = from + per < a.d.rows ? from + per : a.d.rows;
+    constexpr int VE = Lanes<T>::N, ROWS = 2, STEP = 256 / LANES, ACROSS = LANES * VE;
+    __shared__ uint4 staged[WIDE ? 1 : 256];
+    const int cols = a.d.cols, lane = threadIdx.x & 31, first = blockIdx.x * ACROSS;
+    const int c = first + (threadIdx.x & (LANES - 1)) * VE;
+    const int per = int((a.d.rows + a.chunks - 1) / a.chunks);
+    const int64_t from = int64_t(per) * blockIdx.y;
+    const int high = int(a.d.rows - from < per ? a.d.rows - from : per);              // rows of this block
     const int64_t ld_x = a.d.ld_x, ld_res = a.d.ld_res, ld_out = a.d.ld_out;
-    const T *const x = static_cast<const T *>(a.x), *const residual = static_cast<const T *>(a.residual);
-    T *const out = static_cast<T *>(a.out);
-    const bool wide = a.wide;
-    const float scale = drop.scale;
+    const T *const x = static_cast<const T *>(a.x) + from * ld_x, *const residual = RESIDUAL ? static_cast<const T *>(a.residual) + from * ld_res : nullptr;
+    T *const out = static_cast<T *>(a.out) + from * ld_out;
+    const bool inside = c < cols;
     uint4 p[ROWS], q[ROWS];
-    auto fetch = [&](int64_t row) {
+    auto fetch = [&](int row) {
 #pragma unroll
         for (int i = 0; i < ROWS; ++i)
-            if (row + i * step < to && c < cols) {
-                p[i] = load_raw(x + (row + i * step) * ld_x, c, cols, wide);
-                if (residual) q[i] = load_raw(residual + (row + i * step) * ld_res, c, cols, wide);
+            if (row + i * STEP < high && inside) {
+                p[i] = load_raw(x + (row + i * STEP) * ld_x, c, cols, WIDE);
+                if constexpr (RESIDUAL) q[i] = load_raw(residual + (row + i * STEP) * ld_res, c, cols, WIDE);
             }
     };
-    int64_t row = from + threadIdx.x / lanes;
-    const int64_t ahead = lane / lanes;                // rows from the warp's first one to this thread's
+    int row = threadIdx.x / LANES;
+    const int ahead = lane / LANES;                    // rows from the warp's first one to this thread's
     fetch(row);
-    while (row - ahead < to) {
+    const Drop drop(a.drop);                           // (behind the first loads: its seed is in memory too)
+    const DropColumns<VE> columns(drop, c);
+    const float scale = drop.scale;
+    while (row - ahead < high) {
         // the next rows are asked for before these are worked on
         uint4 mine[ROWS], other[ROWS];
 #pragma unroll
-        for (int i = 0; i < ROWS; ++i) { mine[i] = p[i]; other[i] = q[i]; }
-        fetch(row + ROWS * step);
+        for (int i = 0; i < ROWS; ++i) {
+            mine[i] = p[i];
+            if constexpr (RESIDUAL) other[i] = q[i];
+        }
+        fetch(row + ROWS * STEP);
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
-            const int64_t here = row + i * step;
-            const bool in = here < to && c < cols;
+            const int here = row + i * STEP;
+            const bool in = here < high && inside;
             uint4 result = {};
             if (in) {
-                float v[VE], r[VE];
+                float v[VE];
                 unpack16<T>(mine[i], v);
-                if (drop.on) columns.choose(uint32_t(here), v);
-                if (residual) {
+                if (drop.on) columns.choose(uint32_t(from + here), v);
+                if constexpr (RESIDUAL) {
+                    float r[VE];
                     unpack16<T>(other[i], r);
 #pragma unroll
                     for (int e = 0; e < VE; ++e) v[e] = fmaf(v[e], scale, r[e]);
@@ -58,31 +64,32 @@ template <typename T> __global__ void __launch_bounds__(256, 3) dropout_kernel(c
                     for (int e = 0; e < VE; ++e) v[e] *= scale;
                 }
                 result = pack16<T>(v);
-            }
-            if (wide) {
-                if (in && c + VE <= cols) { st_stream(out + here * ld_out + c, result); continue; }
-                if (in) {
-                    const T *const part = reinterpret_cast<const T *>(&result);
+                if constexpr (WIDE) {
+                    T *const to = out + here * ld_out;
+                    if (c + VE <= cols) st_stream(to + c, result);
+                    else {
+                        const T *const part = reinterpret_cast<const T *>(&result);
 #pragma unroll
-                    for (int e = 0; e < VE; ++e) if (c + e < cols) out[here * ld_out + c + e] = part[e];
+                        for (int e = 0; e < VE; ++e) if (c + e < cols) to[c + e] = part[e];
+                    }
                 }
-                continue;
             }
-            // rows at any address: through shared memory, so that neighbouring lanes write neighbouring elements (16 bytes of
-            // a lane one by one would touch every sector 16 times)
-            staged[threadIdx.x] = result;
-            __syncwarp();
-            const T *const flat = reinterpret_cast<const T *>(staged + (threadIdx.x & ~31));
-            const int across = lanes * VE;
+            if constexpr (!WIDE) {
+                // rows at any address: through shared memory, so that neighbouring lanes write neighbouring elements (16 bytes of
+                // a lane one by one would touch every sector 16 times)
+                staged[threadIdx.x] = result;
+                __syncwarp();
+                const T *const flat = reinterpret_cast<const T *>(staged + (threadIdx.x & ~31));
+                T *const to = out + (here - ahead) * ld_out + first;
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const int at = e * 32 + lane, col = first + (at & (across - 1));
-                const int64_t line = here - ahead + at / across;
-                if (line < to && col < cols) out[line * ld_out + col] = flat[at];
+                for (int e = 0; e < VE; ++e) {
+                    const int at = e * 32 + lane, col = at % ACROSS, line = at / ACROSS;
+                    if (here - ahead + line < high && first + col < cols) to[line * ld_out + col] = flat[at];
+                }
+                __syncwarp();
             }
-            __syncwarp();
         }
-        row += ROWS * step;
+        row += ROWS * STEP;
     }
 }
 
@@ -95,7 +102,6 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256, 3) linear_
 {
     __shared__ float sums[GRAD_WARPS][32][9];
     __shared__ bool last;
-    const Drop drop(a.drop);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cols = a.cols;
     const int lanes = a.lanes, c = (blockIdx.x * lanes + (lane & (lanes - 1))) * 8, sub = lane / lanes, abreast = 32 / lanes;
     const int64_t per = (a.rows + a.chunks - 1) / a.chunks, from = per * blockIdx.y, to = from + per < a.rows ? from + per : a.rows;
@@ -105,7 +111,6 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256, 3) linear_
     const int64_t ld_dout = a.ld_dout, ld_pre = a.ld_pre, ld_dz = a.ld_dz, step = int64_t(GRAD_WARPS) * abreast;
     float total[8] = {};
     if (c < cols) {
-        const DropColumns<8> columns(drop, c);
         uint4 p[GRAD_ROWS], q[GRAD_ROWS];
         auto fetch = [&](int64_t row) {
 #pragma unroll
@@ -117,6 +122,8 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256, 3) linear_
         };
         int64_t row = from + warp * abreast + sub;
         fetch(row);
+        const Drop drop(a.drop);                       // (behind the first loads: its seed is in memory too)
+        const DropColumns<8> columns(drop, c);
         while (row < to) {
             // the next rows are asked for before these are worked on
             uint4 mine[GRAD_ROWS], other[GRAD_ROWS];
@@ -206,19 +213,29 @@ int runs(int64_t rows, int64_t strips, int64_t least, int64_t places)
     return int(best > 65535 ? 65535 : best);
 }
 
-template <typename T> cudaError_t dropout(DropoutArgs a, int num_sms, cudaStream_t st)
+template <typename T, int LANES> cudaError_t dropout(DropoutArgs a, bool wide, int num_sms, cudaStream_t st)
 {
-    const int es = int(sizeof(T)), ve = Lanes<T>::N;
-    a.wide = aligned16(a.x) && aligned16(a.out) && aligned16(a.residual) && (a.d.ld_x * es) % 16 == 0 && (a.d.ld_out * es) % 16 == 0 &&
-             (!a.residual || (a.d.ld_res * es) % 16 == 0);
-    const int units = (a.d.cols + ve - 1) / ve;
-    a.lanes = 8;                                      // 128 bytes of a row
-    while (a.lanes > 1 && a.lanes / 2 >= units) a.lanes /= 2;
-    a.strips = (units + a.lanes - 1) / a.lanes;
-    a.chunks = runs(a.d.rows, a.strips, 256 / a.lanes, int64_t(num_sms) * 3);
-    dropout_kernel<T><<<dim3(a.strips, a.chunks), 256, 0, st>>>(a);
+    constexpr int across = LANES * Lanes<T>::N;
+    const int strips = (a.d.cols + across - 1) / across;
+    a.chunks = runs(a.d.rows, strips, 256 / LANES, int64_t(num_sms) * 3);
+    const dim3 grid(strips, a.chunks);
+    if (a.residual) {
+        if (wide) dropout_kernel<T, LANES, true, true><<<grid, 256, 0, st>>>(a);
+        else dropout_kernel<T, LANES, true, false><<<grid, 256, 0, st>>>(a);
+    } else {
+        if (wide) dropout_kernel<T, LANES, false, true><<<grid, 256, 0, st>>>(a);
+        else dropout_kernel<T, LANES, false, false><<<grid, 256, 0, st>>>(a);
+    }
     count_launch();
     return cudaGetLastError();
+}
+// Eight threads a row, 128 bytes of it; one for rows of up to 16 bytes.
+template <typename T> cudaError_t dropout(const DropoutArgs &a, int num_sms, cudaStream_t st)
+{
+    const int es = int(sizeof(T));
+    const bool wide = aligned16(a.x) && aligned16(a.out) && aligned16(a.residual) && (a.d.ld_x * es) % 16 == 0 && (a.d.ld_out * es) % 16 == 0 &&
+                      (!a.residual || (a.d.ld_res * es) % 16 == 0);
+    return a.d.cols <= Lanes<T>::N ? dropout<T, 1>(a, wide, num_sms, st) : dropout<T, 8>(a, wide, num_sms, st);
 }
 
 template <typename T, int ACT> cudaError_t linear_grad(LinearGradArgs a, cudaStream_t st)

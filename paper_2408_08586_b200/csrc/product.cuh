@@ -45,8 +45,7 @@ struct DropoutArgs {
     const void *x, *residual;
     void *out;
     DropArgs drop;
-    bool wide;                           // every row begins on a 16-byte boundary
-    int lanes, strips, chunks;           // threads that share a row (a power of two), strips of columns, runs of rows
+    int chunks;                          // runs of rows
 };
 // dz = act'(pre) drop(dout) with its column sums
 struct LinearGradArgs {
@@ -211,40 +210,35 @@ __device__ __forceinline__ float act_slope(int act, float v)
 
 // 16 bytes of a row from column c on, whatever its alignment: the two aligned pieces that hold them, shifted, where both lie
 // within the row, else element by element (0 past the end).
-template <typename T> __device__ __forceinline__ uint4 load_any(const T *row, int64_t c, int64_t n)
+template <typename T, typename I> __device__ __forceinline__ uint4 load_any(const T *row, I c, I n)
 {
     constexpr int N = Lanes<T>::N;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(row + c), from = at & ~uintptr_t(15);
-    const uint32_t off = uint32_t(at) & 15;
-    if (c + N <= n && from >= reinterpret_cast<uintptr_t>(row) && from + 32 <= reinterpret_cast<uintptr_t>(row + n)) {
-        const uint4 a = ld_cached(reinterpret_cast<const void *>(from)), b = ld_cached(reinterpret_cast<const void *>(from + 16));
-        uint32_t w[7] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z};
-        uint32_t last = b.w;
-        if (off & 4) {
-#pragma unroll
-            for (int i = 0; i < 6; ++i) w[i] = w[i + 1];
-            w[6] = last; last = 0;
-        }
-        if (off & 8) {
-#pragma unroll
-            for (int i = 0; i < 5; ++i) w[i] = w[i + 2];
-            w[5] = last;
-        }
-        const uint32_t bits = (off & 3) * 8;
-        return make_uint4(__funnelshift_r(w[0], w[1], bits), __funnelshift_r(w[1], w[2], bits), __funnelshift_r(w[2], w[3], bits), __funnelshift_r(w[3], w[4], bits));
+    const T *const at = row + c;
+    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(at)) & 15;
+    const I before = I(off / uint32_t(sizeof(T)));
+    if (c >= before && c - before + 2 * N <= n) {
+        const uint8_t *const from = reinterpret_cast<const uint8_t *>(at) - off;
+        const uint4 a = ld_cached(from), b = ld_cached(from + 16);
+        const bool four = off & 4, eight = off & 8;
+        // 32 bytes moved down by eight, then four, then what is left below four
+        const uint32_t u0 = eight ? a.z : a.x, u1 = eight ? a.w : a.y, u2 = eight ? b.x : a.z, u3 = eight ? b.y : a.w, u4 = eight ? b.z : b.x, u5 = eight ? b.w : b.y;
+        const uint32_t w0 = four ? u1 : u0, w1 = four ? u2 : u1, w2 = four ? u3 : u2, w3 = four ? u4 : u3, w4 = four ? u5 : u4;
+        if constexpr (sizeof(T) == 4) return make_uint4(w0, w1, w2, w3);
+        const uint32_t bits = (off & 2) * 8;
+        return make_uint4(__funnelshift_r(w0, w1, bits), __funnelshift_r(w1, w2, bits), __funnelshift_r(w2, w3, bits), __funnelshift_r(w3, w4, bits));
     }
     uint32_t w[4] = {};
 #pragma unroll
     for (int e = 0; e < N; ++e) {
         if (c + e < n) {
-            if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(row[c + e]);
-            else w[e >> 1] |= uint32_t(reinterpret_cast<const uint16_t *>(row)[c + e]) << (16 * (e & 1));
+            if constexpr (sizeof(T) == 4) w[e] = __float_as_uint(at[e]);
+            else w[e >> 1] |= uint32_t(reinterpret_cast<const uint16_t *>(at)[e]) << (16 * (e & 1));
         }
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // ... with the word that says whether every row begins on a 16-byte boundary
-template <typename T> __device__ __forceinline__ uint4 load_raw(const T *row, int64_t c, int64_t n, bool wide)
+template <typename T> __device__ __forceinline__ uint4 load_raw(const T *row, int c, int n, bool wide)
 {
     return wide && c + Lanes<T>::N <= n ? ld_stream(row + c) : load_any(row, c, n);
 }
