@@ -11,6 +11,8 @@ using namespace train;
 template <typename T, int LANES, bool RESIDUAL, bool WIDE> __global__ void __launch_bounds__(256, 3) dropout_kernel(const __grid_constant__ DropoutArgs a)
 {
     constexpr int VE = Lanes<T>::N, ROWS = 2, STEP = 256 / LANES, ACROSS = LANES * VE;
+    chain_go();
+    chain_wait();
     __shared__ uint4 staged[WIDE ? 1 : 256];
     const int cols = a.d.cols, lane = threadIdx.x & 31, first = blockIdx.x * ACROSS;
     const int c = first + (threadIdx.x & (LANES - 1)) * VE;
@@ -102,6 +104,8 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256, 3) linear_
 {
     __shared__ float sums[GRAD_WARPS][32][9];
     __shared__ bool last;
+    chain_go();
+    chain_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cols = a.cols;
     const int lanes = a.lanes, c = (blockIdx.x * lanes + (lane & (lanes - 1))) * 8, sub = lane / lanes, abreast = 32 / lanes;
     const int64_t per = (a.rows + a.chunks - 1) / a.chunks, from = per * blockIdx.y, to = from + per < a.rows ? from + per : a.rows;
@@ -219,15 +223,9 @@ template <typename T, int LANES> cudaError_t dropout(DropoutArgs a, bool wide, i
     const int strips = (a.d.cols + across - 1) / across;
     a.chunks = runs(a.d.rows, strips, 256 / LANES, int64_t(num_sms) * 3);
     const dim3 grid(strips, a.chunks);
-    if (a.residual) {
-        if (wide) dropout_kernel<T, LANES, true, true><<<grid, 256, 0, st>>>(a);
-        else dropout_kernel<T, LANES, true, false><<<grid, 256, 0, st>>>(a);
-    } else {
-        if (wide) dropout_kernel<T, LANES, false, true><<<grid, 256, 0, st>>>(a);
-        else dropout_kernel<T, LANES, false, false><<<grid, 256, 0, st>>>(a);
-    }
-    count_launch();
-    return cudaGetLastError();
+    const auto kernel = a.residual ? (wide ? dropout_kernel<T, LANES, true, true> : dropout_kernel<T, LANES, true, false>)
+                                   : (wide ? dropout_kernel<T, LANES, false, true> : dropout_kernel<T, LANES, false, false>);
+    return launch_chained(kernel, grid, dim3(256), 0, 1, st, a);
 }
 // Eight threads a row, 128 bytes of it; one for rows of up to 16 bytes.
 template <typename T> cudaError_t dropout(const DropoutArgs &a, int num_sms, cudaStream_t st)
@@ -242,9 +240,7 @@ template <typename T, int ACT> cudaError_t linear_grad(LinearGradArgs a, cudaStr
 {
     const dim3 grid(a.strips, a.chunks);
     a.wide = aligned16(a.dout) && (a.ld_dout & 7) == 0 && (ACT == RUBICK_ACT_NONE || (aligned16(a.pre) && (a.ld_pre & 7) == 0));
-    linear_grad_kernel<T, ACT><<<grid, 256, 0, st>>>(a);
-    count_launch();
-    return cudaGetLastError();
+    return launch_chained(linear_grad_kernel<T, ACT>, grid, dim3(256), 0, 1, st, a);
 }
 template <typename T> cudaError_t linear_grad(const LinearGradArgs &a, cudaStream_t st)
 {

@@ -4,6 +4,7 @@
 // neighbouring multiprocessors, which share the tile's columns of B) takes tile after tile.  One thread has the tensor-copy
 // engine fetch 64 k of both operands into a ring of stages, one thread multiplies them into tensor memory, and eight warps
 // take a finished tile out of it while the next one is multiplied into its other half.
+#include <atomic>
 #include <type_traits>
 
 #include "product.cuh"
@@ -17,17 +18,24 @@ using namespace train;
 constexpr int BM = 128, BK = 64;                     // rows a block, k a stage
 constexpr int THREADS = 384;                         // fetch, multiply, allocate, -, and eight warps that read
 constexpr int READERS = 8, FIRST_READER = 4;
+constexpr int STAGES = 6, A_BYTES = BM * BK * 2, STAGE = 2 * A_BYTES;          // 128 rows of A, up to 128 of B
 constexpr int STAGING = READERS * 4096;              // 32 rows x 128 bytes a warp
-constexpr int SHARED_LIMIT = 232448;
+constexpr int SHARED = STAGES * STAGE + STAGING + 1024 + 256;                  // 1,024 to begin on such a boundary
+constexpr int SINGLE_COLS = 128, PAIR_COLS = 256;    // most columns of a tile
+constexpr int SHARE_LINE = SINGLE_COLS * 4 + 16;     // bytes of a row of sums that blocks share (16 apart in the banks)
+static_assert(SHARED <= 232448 && BM * SHARE_LINE <= STAGES * STAGE, "what a block may have");
 
-template <int BN, bool PAIR> struct Shape {
-    static constexpr int CTAS = PAIR ? 2 : 1;
-    static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN / CTAS * BK * 2, STAGE = A_BYTES + B_BYTES;
-    static constexpr int STAGES = (SHARED_LIMIT - STAGING - 2048) / STAGE > 8 ? 8 : (SHARED_LIMIT - STAGING - 2048) / STAGE;
-    static constexpr int SHARED = STAGES * STAGE + STAGING + 1024 + 256;      // 1,024 to begin on such a boundary
-    static constexpr uint32_t COLUMNS = 2 * BN;                               // of tensor memory: two tiles
+// A product cut into tiles of 128 (256 with a pair) rows and `cols` columns; `per` of the k stages go to each split.
+struct Tiling {
+    uint32_t tiles_m, tiles_n, each, all;
+    int steps, per, cols;
+    uint32_t bytes;                                  // of a stage, per block
+    uint32_t share, first;                           // blocks of a cluster that share a tile's k, and the first of them all
 };
-struct Tiling { uint32_t tiles_m, tiles_n, each, all; int steps, per; };      // per: k stages of a split
+// Up to two products of one launch: the second one's tiles follow the first one's.  With a cluster of single blocks every
+// block has one tile, or a share of the k of one.
+struct Work { ProductArgs a[2]; Tiling t[2]; uint32_t all, cluster; };
+struct Maps { CUtensorMap a[2], b[2]; };
 
 // Tile number -> tile row, tile column, split: eight tile rows at a time, so that what runs at once shares operands in L2.
 __device__ __forceinline__ void place(const Tiling &t, uint32_t i, int &m, int &n, int &split)
@@ -41,29 +49,34 @@ __device__ __forceinline__ void place(const Tiling &t, uint32_t i, int &m, int &
 
 __device__ __forceinline__ float ninf() { return __uint_as_float(0xff800000u); }
 
-template <typename T, ProductKind KIND, int ACT, int BN, bool PAIR>
-__global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                             const __grid_constant__ ProductArgs a, const __grid_constant__ Tiling t)
+template <typename T, ProductKind KIND, int ACT, bool PAIR>
+__global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Work work)
 {
-    using S = Shape<BN, PAIR>;
+    constexpr int CTAS = PAIR ? 2 : 1;
+    constexpr uint32_t HALF = PAIR ? PAIR_COLS : SINGLE_COLS, COLUMNS = 2 * HALF;      // of tensor memory: two tiles
+    chain_go();
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
     uint8_t *const shared = raw + (base - smem_addr(raw));
-    const uint32_t stages = base, bars = base + S::STAGES * S::STAGE + STAGING;
-    const uint32_t full = bars, empty = full + 8 * S::STAGES, done = empty + 8 * S::STAGES, taken = done + 16;
-    volatile uint32_t *const words = reinterpret_cast<volatile uint32_t *>(shared + S::STAGES * S::STAGE + STAGING + 16 * S::STAGES + 32);
+    const uint32_t stages = base, bars = base + STAGES * STAGE + STAGING;
+    const uint32_t full = bars, empty = full + 8 * STAGES, done = empty + 8 * STAGES, taken = done + 16;
+    volatile uint32_t *const words = reinterpret_cast<volatile uint32_t *>(shared + STAGES * STAGE + STAGING + 16 * STAGES + 32);
     volatile uint32_t *const given_up = words;       // [0] someone waited in vain; [1] where the tensor memory begins
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = PAIR ? cluster_rank() : 0;
+    // a pair's rank in its cluster; a single block's among those that share its tile
+    const bool shared_tiles = !PAIR && KIND == PRODUCT_OUT && work.cluster > 1;
+    const int mine_is = shared_tiles && blockIdx.x >= work.t[1].first;
+    const uint32_t ranks = PAIR ? 2 : shared_tiles ? work.t[mine_is].share : 1;
+    const uint32_t rank = PAIR ? cluster_rank() : shared_tiles ? (blockIdx.x - work.t[mine_is].first) % ranks : 0;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::STAGES; ++s) { barrier_init(full + 8 * s, 1); barrier_init(empty + 8 * s, 1); }
-        for (int i = 0; i < 2; ++i) { barrier_init(done + 8 * i, 1); barrier_init(taken + 8 * i, READERS * S::CTAS); }
+        for (int s = 0; s < STAGES; ++s) { barrier_init(full + 8 * s, 1); barrier_init(empty + 8 * s, 1); }
+        for (int i = 0; i < 2; ++i) { barrier_init(done + 8 * i, 1); barrier_init(taken + 8 * i, READERS * CTAS); }
         barrier_init_done();
         *given_up = 0;
     }
     if (warp == 2) {
-        tmem_alloc<PAIR>(smem_addr(const_cast<uint32_t *>(words + 1)), S::COLUMNS);
+        tmem_alloc<PAIR>(smem_addr(const_cast<uint32_t *>(words + 1)), COLUMNS);
         tmem_alloc_done<PAIR>();
     }
     tcgen_before_sync();
@@ -71,92 +84,138 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
     if constexpr (PAIR) cluster_sync();
     tcgen_after_sync();
     const uint32_t tmem = words[1];
-    const uint32_t first = blockIdx.x / S::CTAS, step = gridDim.x / S::CTAS;
+    const uint32_t first = !shared_tiles ? blockIdx.x / ranks : (mine_is ? work.t[0].all : 0) + (blockIdx.x - work.t[mine_is].first) / ranks;
+    const uint32_t step = shared_tiles ? 0x80000000u : gridDim.x / ranks;
+    const uint32_t end = shared_tiles && !mine_is ? work.t[0].all : work.all;     // (blocks that fill a cluster up have no tile)
+    chain_wait();
 
     if (warp == 0) {
         if (lane == 0) {
-            uint32_t round = 0;                      // stages filled so far
+            uint32_t round = 0, i = first;           // stages filled so far, tile
             bool fine = true;
-            for (uint32_t i = first; fine && i < t.all; i += step) {
-                int tm, tn, split;
-                place(t, i, tm, tn, split);
-                const int m0 = (tm * S::CTAS + int(rank)) * BM, n0 = tn * BN + int(rank) * (BN / S::CTAS);
-                const int k0 = split * t.per, k1 = k0 + t.per < t.steps ? k0 + t.per : t.steps;
-                for (int k = k0; k < k1; ++k, ++round) {
-                    const uint32_t s = round % S::STAGES, into = stages + s * S::STAGE;
-                    if (!(fine = barrier_wait(empty + 8 * s, (round / S::STAGES & 1) ^ 1, given_up))) break;
-                    if (rank == 0) barrier_expect(full + 8 * s, S::STAGE * S::CTAS);
-                    const uint32_t bar = PAIR ? at_rank(full + 8 * s, 0) : full + 8 * s;
-                    if (a.a.along_k) tensor_load<PAIR>(into, &map_a, k * BK, m0, bar);
-                    else
-                        for (int j = 0; j < BM / 64; ++j) tensor_load<PAIR>(into + j * BLOCK_BYTES, &map_a, m0 + 64 * j, k * BK, bar);
-                    if (a.b.along_k) tensor_load<PAIR>(into + S::A_BYTES, &map_b, k * BK, n0, bar);
-                    else
-                        for (int j = 0; j < BN / S::CTAS / 64; ++j) tensor_load<PAIR>(into + S::A_BYTES + j * BLOCK_BYTES, &map_b, n0 + 64 * j, k * BK, bar);
+            const uint32_t bar0 = PAIR ? at_rank(full, 0) : full;
+            // (one loop for each product, so that its maps and sizes are at fixed places: chosen by a variable they cost a fifth of
+            // the kernel's rate)
+            auto fetch = [&](auto number) {
+                constexpr int which = decltype(number)::value;
+                const Tiling &t = work.t[which];
+                const ProductArgs &a = work.a[which];
+                const uint32_t to = which ? end : end < work.t[0].all ? end : work.t[0].all;
+                for (; fine && i < to; i += step) {
+                    int tm, tn, split;
+                    place(t, which ? i - work.t[0].all : i, tm, tn, split);
+                    if (!PAIR) split += rank;        // (a tile's blocks; there are no splits beside them)
+                    const int m0 = (tm * CTAS + (PAIR ? int(rank) : 0)) * BM, n0 = tn * t.cols + (PAIR ? int(rank) * (t.cols / 2) : 0);
+                    const int k0 = split * t.per, k1 = k0 + t.per < t.steps ? k0 + t.per : t.steps;
+                    const bool ak = a.a.along_k, bk = a.b.along_k;
+                    const int blocks = (t.cols / CTAS + 63) / 64;
+                    const uint32_t bytes = t.bytes * CTAS;
+                    for (int k = k0; k < k1; ++k, ++round) {
+                        const uint32_t s = round % STAGES, into = stages + s * STAGE, bar = bar0 + 8 * s;
+                        if (!(fine = barrier_wait(empty + 8 * s, (round / STAGES & 1) ^ 1, given_up))) break;
+                        if (!PAIR || rank == 0) barrier_expect(full + 8 * s, bytes);
+                        if (ak) tensor_load<PAIR>(into, &maps.a[which], k * BK, m0, bar);
+                        else
+                            for (int j = 0; j < BM / 64; ++j) tensor_load<PAIR>(into + j * BLOCK_BYTES, &maps.a[which], m0 + 64 * j, k * BK, bar);
+                        if (bk) tensor_load<PAIR>(into + A_BYTES, &maps.b[which], k * BK, n0, bar);
+                        else
+                            for (int j = 0; j < blocks; ++j) tensor_load<PAIR>(into + A_BYTES + j * BLOCK_BYTES, &maps.b[which], n0 + 64 * j, k * BK, bar);
+                    }
                 }
-            }
+            };
+            fetch(std::integral_constant<int, 0>());
+            if constexpr (KIND == PRODUCT_OUT && ACT == RUBICK_ACT_NONE) fetch(std::integral_constant<int, 1>());
             // given up: the copies in flight write into this block's memory, so they are waited for before it goes
-            if (!fine && rank == 0) {
+            if (!fine && (!PAIR || rank == 0)) {
                 volatile uint32_t never = 0;
-                for (uint32_t r = round > S::STAGES ? round - S::STAGES : 0; r < round; ++r) barrier_wait(full + 8 * (r % S::STAGES), r / S::STAGES & 1, &never);
+                for (uint32_t r = round > STAGES ? round - STAGES : 0; r < round; ++r) barrier_wait(full + 8 * (r % STAGES), r / STAGES & 1, &never);
             }
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
-            const bool ak = a.a.along_k, bk = a.b.along_k;
-            const uint32_t desc = instruction_desc(std::is_same<T, bf16>::value, ak, bk, BM * S::CTAS, BN);
-            const uint64_t da = operand_desc(stages, ak), db = operand_desc(stages + S::A_BYTES, bk);
-            const uint32_t sa = operand_step(ak), sb = operand_step(bk);
-            uint32_t round = 0, tile = 0;
+        if (lane == 0 && (!PAIR || rank == 0)) {
+            uint32_t round = 0, tile = 0, i = first;
             bool fine = true;
-            for (uint32_t i = first; fine && i < t.all; i += step, ++tile) {
-                const int k0 = t.all == t.each ? 0 : int(i / t.each) * t.per, k1 = k0 + t.per < t.steps ? k0 + t.per : t.steps;
-                const uint32_t half = tile & 1, d = tmem + half * BN;
-                if (!(fine = barrier_wait(taken + 8 * half, (tile / 2 & 1) ^ 1, given_up))) break;
-                tcgen_after_sync();
-                for (int k = k0; k < k1; ++k, ++round) {
-                    const uint32_t s = round % S::STAGES, at = s * (S::STAGE >> 4);
-                    if (!(fine = barrier_wait(full + 8 * s, round / S::STAGES & 1, given_up))) break;
+            auto sum = [&](auto number) {
+                constexpr int which = decltype(number)::value;
+                const Tiling &t = work.t[which];
+                const bool ak = work.a[which].a.along_k, bk = work.a[which].b.along_k;
+                const uint32_t desc = instruction_desc(std::is_same<T, bf16>::value, ak, bk, BM * CTAS, t.cols);
+                const uint64_t da = operand_desc(stages, ak), db = operand_desc(stages + A_BYTES, bk);
+                const uint32_t sa = operand_step(ak), sb = operand_step(bk);
+                const uint32_t to = which ? end : end < work.t[0].all ? end : work.t[0].all;
+                for (; fine && i < to; i += step, ++tile) {
+                    const int split = !PAIR ? int(rank) : t.all == t.each ? 0 : int((which ? i - work.t[0].all : i) / t.each);
+                    const int k0 = split * t.per, k1 = k0 + t.per < t.steps ? k0 + t.per : t.steps;
+                    const uint32_t half = tile & 1, d = tmem + half * HALF;
+                    if (!(fine = barrier_wait(taken + 8 * half, (tile / 2 & 1) ^ 1, given_up))) break;
                     tcgen_after_sync();
+                    for (int k = k0; k < k1; ++k, ++round) {
+                        const uint32_t s = round % STAGES, at = s * (STAGE >> 4);
+                        if (!(fine = barrier_wait(full + 8 * s, round / STAGES & 1, given_up))) break;
+                        tcgen_after_sync();
 #pragma unroll
-                    for (int q = 0; q < BK / 16; ++q) multiply<PAIR>(d, da + at + q * sa, db + at + q * sb, desc, k > k0 || q > 0);
-                    multiplied<PAIR>(empty + 8 * s);
+                        for (int q = 0; q < BK / 16; ++q) multiply<PAIR>(d, da + at + q * sa, db + at + q * sb, desc, k > k0 || q > 0);
+                        multiplied<PAIR>(empty + 8 * s);
+                    }
+                    if (fine) multiplied<PAIR>(done + 8 * half);
                 }
-                if (fine) multiplied<PAIR>(done + 8 * half);
-            }
+            };
+            sum(std::integral_constant<int, 0>());
+            if constexpr (KIND == PRODUCT_OUT && ACT == RUBICK_ACT_NONE) sum(std::integral_constant<int, 1>());
             if (!fine) {                             // what was multiplied is waited for before the tensor memory goes
                 volatile uint32_t never = 0;
-                for (uint32_t r = round > S::STAGES ? round - S::STAGES : 0; r < round; ++r) barrier_wait(empty + 8 * (r % S::STAGES), r / S::STAGES & 1, &never);
+                for (uint32_t r = round > STAGES ? round - STAGES : 0; r < round; ++r) barrier_wait(empty + 8 * (r % STAGES), r / STAGES & 1, &never);
             }
         }
         __syncwarp();
     } else if (warp >= FIRST_READER) {
         const int quarter = warp & 3, side = (warp - FIRST_READER) >> 2;       // 32 rows, half of the columns
-        uint8_t *const mine = shared + S::STAGES * S::STAGE + (warp - FIRST_READER) * 4096;
-        const Finish<T, ACT> finish(a);
-        const int64_t rows = a.m, cols = a.n;
+        uint8_t *const mine = shared + STAGES * STAGE + (warp - FIRST_READER) * 4096;
+        constexpr bool TWO = KIND == PRODUCT_OUT && ACT == RUBICK_ACT_NONE;      // products there may be
+        int which = TWO && first >= work.t[0].all;
+        Finish<T, ACT> finish(work.a[which]);
         uint32_t tile = 0;
-        for (uint32_t i = first; i < t.all; i += step, ++tile) {
+        for (uint32_t i = first; i < end; i += step, ++tile) {
+            if (TWO && !which && i >= work.t[0].all) {
+                which = 1;
+                finish = Finish<T, ACT>(work.a[1]);
+            }
+            const ProductArgs &a = work.a[TWO ? which : 0];
+            const Tiling &t = work.t[TWO ? which : 0];
+            const int64_t rows = a.m, cols = a.n;
             int tm, tn, split;
-            place(t, i, tm, tn, split);
+            place(t, which ? i - work.t[0].all : i, tm, tn, split);
             const uint32_t half = tile & 1;
-            const int64_t m0 = (int64_t(tm) * S::CTAS + rank) * BM + quarter * 32;
-            const int64_t n0 = int64_t(tn) * BN + side * (BN / 2);
+            const int width = KIND == PRODUCT_OUT ? t.cols / 2 : int(HALF) / 2;      // (only sums may be cut otherwise)
+            const int64_t m0 = (int64_t(tm) * CTAS + (PAIR ? rank : 0)) * BM + quarter * 32;
+            const int64_t n0 = int64_t(tn) * t.cols + side * width;
             if (!barrier_wait(done + 8 * half, tile / 2 & 1, given_up)) break;
             __syncwarp();
             tcgen_after_sync();
-            const uint32_t at = tmem + half * BN + side * (BN / 2) + (uint32_t(quarter * 32) << 16);
-            if constexpr (KIND == PRODUCT_OUT || KIND == PRODUCT_PART) {
+            const uint32_t at = tmem + half * HALF + side * width + (uint32_t(quarter * 32) << 16);
+            if (ranks > 1 && shared_tiles) {
+                // this block's share of the sums, for all of the cluster to read (nothing is copied or multiplied any more)
+                if (m0 < rows)
+#pragma unroll 1
+                    for (int c = 0; c < SINGLE_COLS / 2; c += 32) {
+                        float v[32];
+                        tmem_load32(at + c, v);
+                        float4 *const to = reinterpret_cast<float4 *>(shared + (quarter * 32 + lane) * SHARE_LINE + (side * (SINGLE_COLS / 2) + c) * 4);
+#pragma unroll
+                        for (int p = 0; p < 8; ++p) to[p] = make_float4(v[4 * p], v[4 * p + 1], v[4 * p + 2], v[4 * p + 3]);
+                    }
+            } else if constexpr (KIND == PRODUCT_OUT) {
                 // 32 rows x 32 sums through shared memory, pieces of 16 bytes exchanged by the row, so that a warp then holds
                 // eight neighbouring sums a lane and its accesses cover whole sectors of eight rows
                 const int q = (lane & 3) * 2, above = lane >> 2;
-                const bool quick = KIND == PRODUCT_OUT && m0 + 32 <= rows && finish.takes_four();
+                const bool quick = m0 + 32 <= rows && finish.takes_four();
+                float *const part = t.all == t.each ? nullptr : a.part + (int64_t(split) * rows + m0 + above) * finish.ld_acc;
 #pragma unroll 1
-                for (int c = 0; c < BN / 2 && n0 + c < cols; c += 32) {
+                for (int c = 0; c < width && n0 + c < cols; c += 32) {
                     const int64_t col = n0 + c + q * 4;
                     float v[32], bias[8];
-                    if constexpr (KIND == PRODUCT_OUT) finish.load_bias(col, bias);
+                    finish.load_bias(col, bias);
                     tmem_load32(at + c, v);
 #pragma unroll
                     for (int p = 0; p < 8; ++p)
@@ -169,8 +228,8 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                         const float4 x = *reinterpret_cast<const float4 *>(line + ((q ^ above) << 4)), y = *reinterpret_cast<const float4 *>(line + (((q + 1) ^ above) << 4));
                         w[r][0] = x.x; w[r][1] = x.y; w[r][2] = x.z; w[r][3] = x.w; w[r][4] = y.x; w[r][5] = y.y; w[r][6] = y.z; w[r][7] = y.w;
                     }
-                    if constexpr (KIND == PRODUCT_PART) {
-                        float *const to = a.part + (int64_t(split) * rows + m0 + above) * finish.ld_acc + col;
+                    if (part) {
+                        float *const to = part + col;
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             if (m0 + above + 8 * r < rows && col < cols) {
@@ -229,7 +288,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 const int64_t row = m0 + lane;
                 const int64_t label = row < rows ? int64_t(a.label[row]) - a.first - n0 : -1;
                 float top = ninf(), sum = 0.f;
-                for (int c = 0; c < BN / 2; c += 32) {
+                for (int c = 0; c < width; c += 32) {
                     float v[32];
                     tmem_load32(at + c, v);
                     const int64_t left = cols - (n0 + c);
@@ -258,10 +317,12 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 // a thread has a row; 64 columns become 128 bytes of it, written line by line
                 const int64_t row = m0 + lane;
                 const bool in = row < rows;
-                const float from = in ? a.base[row] : 0.f, rest = in && a.rest ? a.rest[row] : 0.f, w = in ? a.weight[row] : 0.f;
-                const uint32_t mask = w == 0.f ? 0u : 0xffffffffu;            // (rows that take no part, whatever their logits are)
-                const int64_t label = in ? int64_t(a.label[row]) - a.first - n0 : -1;
-                for (int c = 0; c < BN / 2; c += 64) {
+                const int is = in ? a.label[row] : -1;
+                const bool live = is >= 0 && is < a.vocab;
+                const float from = live ? a.base[row] : 0.f, rest = live && a.rest ? a.rest[row] : 0.f, w = live ? (a.dloss ? a.dloss[row] : 1.f) * *a.up : 0.f;
+                const uint32_t mask = live ? 0xffffffffu : 0u;                // (rows that take no part, whatever their logits are)
+                const int64_t label = live ? int64_t(is) - a.first - n0 : -1;
+                for (int c = 0; c < width; c += 64) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         float v[32];
@@ -298,17 +359,49 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
         }
     }
     __syncthreads();
-    if constexpr (PAIR) cluster_sync();              // the other block's copies, products and arrivals end here as well
+    if (PAIR || shared_tiles) cluster_sync();        // (a pair: the other block's copies, products and arrivals end here as well)
+    if (shared_tiles) {
+        // the blocks' shares added up in their order, every `ranks`-th row here: eight sums a lane, two rows a warp
+        if (ranks > 1 && first < end && warp >= FIRST_READER && !*given_up) {
+            const int which = mine_is;
+            const uint32_t from_rank = cluster_rank() - rank;
+            const ProductArgs &a = work.a[which];
+            const Finish<T, ACT> finish(a);
+            int tm, tn, split;
+            place(work.t[which], which ? first - work.t[0].all : first, tm, tn, split);
+            const int64_t m0 = int64_t(tm) * BM, c = int64_t(tn) * SINGLE_COLS + (lane & 15) * 8;
+            const int high = a.m - m0 < BM ? int(a.m - m0) : BM;
+            float bias[8];
+            finish.load_bias(c, bias);
+            for (int r = ((warp - FIRST_READER) * 2 + (lane >> 4)) * int(ranks) + int(rank); r < high; r += READERS * 2 * int(ranks)) {
+                const uint32_t at = stages + r * SHARE_LINE + (lane & 15) * 32;
+                float v[8] = {};
+                for (uint32_t s = 0; s < ranks; ++s) {
+                    const uint32_t from = at_rank(at, from_rank + s);
+                    float4 x, y;
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(from));
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y.x), "=f"(y.y), "=f"(y.z), "=f"(y.w) : "r"(from + 16));
+                    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
+                }
+                if (c < a.n) finish(m0 + r, c, v, bias);
+            }
+        }
+        cluster_sync();                              // nobody's share goes while it is read
+    }
     if (warp == 2) {
         tcgen_after_sync();
-        tmem_free<PAIR>(tmem, S::COLUMNS);
+        tmem_free<PAIR>(tmem, COLUMNS);
     }
-    if (threadIdx.x == 0 && *given_up && a.status) atomicOr(a.status, DS_COPY_LOST);
+    if (threadIdx.x == 0 && *given_up && work.a[0].status) atomicOr(work.a[0].status, DS_COPY_LOST);
 }
 
-// The sums of the splits joined, and PRODUCT_OUT's epilogue.
-template <typename T, int ACT> __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ ProductArgs a)
+// The sums of the splits joined, and PRODUCT_OUT's epilogue; of up to two products.
+template <typename T, int ACT> __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Work work)
 {
+    chain_go();
+    chain_wait();
+    const ProductArgs &a = work.a[blockIdx.y];
+    if (a.splits == 1) return;
     const Finish<T, ACT> finish(a);
     const int64_t units = (a.n + 7) / 8, all = a.m * units;
     for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += int64_t(gridDim.x) * blockDim.x) {
@@ -329,6 +422,8 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256) join_kerne
 // Rows laid out anew, on 16-byte boundaries (the copy engine takes no others); up to two matrices at once.
 __global__ void __launch_bounds__(256) lay_out_kernel(const __grid_constant__ LayOutArgs a)
 {
+    chain_go();
+    chain_wait();
     const LayOutArgs::One &o = a.one[blockIdx.z];
     const uint16_t *const from = static_cast<const uint16_t *>(o.from);
     uint16_t *const to = static_cast<uint16_t *>(o.to);
@@ -363,85 +458,150 @@ bool operand_map(CUtensorMap *map, const Operand &o, int dtype, int64_t dim, int
                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, ProductKind KIND, int ACT, int BN, bool PAIR> cudaError_t launch(const ProductArgs &a, int num_sms, cudaStream_t st)
+// Clusters of single blocks that are resident at once on this GPU, one block a multiprocessor: 74 of two, 33 of four, 15 of
+// eight (a cluster lies within a group of multiprocessors, and those are not whole multiples).
+int resident_clusters(int size)
 {
-    using S = Shape<BN, PAIR>;
-    CUtensorMap map_a, map_b;
-    if (!operand_map(&map_a, a.a, a.dtype, a.m, a.k, BM) || !operand_map(&map_b, a.b, a.dtype, a.n, a.k, BN / S::CTAS)) return cudaErrorInvalidValue;
-    const int64_t tiles_m = (a.m + BM * S::CTAS - 1) / (BM * S::CTAS), tiles_n = (a.n + BN - 1) / BN, steps = (a.k + BK - 1) / BK;
-    const int64_t splits = KIND == PRODUCT_PART ? a.splits : 1, all = tiles_m * tiles_n * splits;
-    if (all > 0x7fffffff || steps > 0x7fffffff / BK) return cudaErrorInvalidValue;
-    const Tiling t = {uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(tiles_m * tiles_n), uint32_t(all), int(steps), int((steps + splits - 1) / splits)};
-    const auto kernel = product_kernel<T, KIND, ACT, BN, PAIR>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SHARED);
-    if (e != cudaSuccess) return e;
-    const int64_t most = num_sms / S::CTAS;
+    static std::atomic<int> known[64][4];
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return 0;
+    std::atomic<int> &slot = known[device][size == 2 ? 1 : size == 4 ? 2 : 3];
+    int n = slot.load(std::memory_order_relaxed);
+    if (n) return n - 1;
+    const auto kernel = product_kernel<bf16, PRODUCT_OUT, RUBICK_ACT_NONE, false>;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(unsigned((all < most ? all : most) * S::CTAS));
-    cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = S::SHARED;
-    cfg.stream = st;
+    cfg.gridDim = dim3(64 * size); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = SHARED;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = S::CTAS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = size; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, kernel, map_a, map_b, a, t);
-    count_launch();
-    return e;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        (void)cudaGetLastError();
+        n = 0;
+    }
+    slot.store(n + 1, std::memory_order_relaxed);
+    return n;
 }
 
-template <typename T, int ACT> cudaError_t join(const ProductArgs &a, int num_sms, cudaStream_t st)
+// How a product is cut.  What a way takes is estimated in microseconds from measured times: a stage of 64 k takes a pair of
+// blocks 0.33 for 256 x 256 sums (0.25 for 192 columns, 0.2 for 128), a single block PLAN_SINGLE for 128 x 128.
+struct Way { bool pair; int cols, share, splits; float cost; int64_t blocks; };
+Way way_of(ProductKind kind, const ProductArgs &a, int num_sms, bool pair)
 {
-    const int64_t blocks = (a.m * ((a.n + 7) / 8) + 255) / 256, most = int64_t(num_sms) * 8;
-    join_kernel<T, ACT><<<int(blocks < most ? blocks : most), 256, 0, st>>>(a);
-    count_launch();
-    return cudaGetLastError();
+    const int64_t steps = (a.k + BK - 1) / BK;
+    Way best = {pair, pair ? PAIR_COLS : SINGLE_COLS, 1, 1, 3e38f, 0};
+    if (pair) {
+        for (const int cols : {256, 192, 128}) {
+            if (kind != PRODUCT_OUT && cols != PAIR_COLS) continue;
+            const int64_t tiles = ((a.m + 255) / 256) * ((a.n + cols - 1) / cols), places = num_sms / 2;
+            for (int s = 1; s <= 8; ++s) {
+                if (s > 1 && (kind != PRODUCT_OUT || steps < 8 * s)) break;
+                const int64_t per = (steps + s - 1) / s, splits = (steps + per - 1) / per, waves = (tiles * splits + places - 1) / places;
+                const float each = cols == 256 ? 0.33f : cols == 192 ? 0.25f : 0.2f;
+                const float cost = float(waves) * float(per) * each + 8.f + (splits > 1 ? 4.f + float(splits) * float(a.m) * float(a.n) * 2e-6f : 0.f);
+                if (cost < best.cost) best = Way{true, cols, 1, int(splits), cost, 2 * tiles * splits};
+            }
+        }
+    } else {
+        const int64_t tiles = ((a.m + 127) / 128) * ((a.n + 127) / 128);
+        for (int s = 1; s <= 8; s *= 2) {
+            if (s > 1 && (kind != PRODUCT_OUT || steps < 2 * s || tiles > resident_clusters(s))) break;
+            const int64_t per = (steps + s - 1) / s, waves = (tiles + num_sms - 1) / num_sms;
+            if ((steps + per - 1) / per != s) continue;          // (no block is left without work)
+            const float cost = float(waves) * float(per) * 0.33f + 6.f + (s > 1 ? 1.f : 0.f);
+            if (cost < best.cost) best = Way{false, SINGLE_COLS, s, 1, cost, tiles * s};
+        }
+    }
+    return best;
+}
+Way way_of(ProductKind kind, const ProductArgs &a, int num_sms)
+{
+    const Way p = way_of(kind, a, num_sms, true), s = way_of(kind, a, num_sms, false);
+    return p.cost < s.cost ? p : s;
 }
 
-template <typename T, int BN, bool PAIR> cudaError_t product(ProductKind kind, const ProductArgs &a, int num_sms, cudaStream_t st)
+template <typename T, ProductKind KIND, int ACT, bool PAIR> cudaError_t launch(ProductArgs *a, const Way *ways, int n, int num_sms, cudaStream_t st)
+{
+    constexpr int CTAS = PAIR ? 2 : 1;
+    Maps maps;
+    Work work = {};
+    work.cluster = CTAS;
+    for (int i = 0; i < n; ++i) if (uint32_t(ways[i].share) > work.cluster) work.cluster = ways[i].share;
+    uint32_t blocks_of_shares = 0;
+    bool joined = false;
+    for (int i = 0; i < n; ++i) {
+        const int cols = ways[i].cols;
+        if (!operand_map(&maps.a[i], a[i].a, a[i].dtype, a[i].m, a[i].k, BM) || !operand_map(&maps.b[i], a[i].b, a[i].dtype, a[i].n, a[i].k, cols / CTAS)) return cudaErrorInvalidValue;
+        a[i].splits = ways[i].splits;
+        const int64_t tiles_m = (a[i].m + BM * CTAS - 1) / (BM * CTAS), tiles_n = (a[i].n + cols - 1) / cols, steps = (a[i].k + BK - 1) / BK;
+        const int64_t parts = PAIR ? ways[i].splits : ways[i].share, all = tiles_m * tiles_n * (PAIR ? parts : 1);
+        if (work.all + all > 0x7fffffff || steps > 0x7fffffff / BK) return cudaErrorInvalidValue;
+        const uint32_t bytes = A_BYTES + (a[i].b.along_k ? cols / CTAS * 128 : (cols / CTAS + 63) / 64 * BLOCK_BYTES);
+        work.a[i] = a[i];
+        work.t[i] = Tiling{uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(tiles_m * tiles_n), uint32_t(all), int(steps), int((steps + parts - 1) / parts), cols, bytes, uint32_t(ways[i].share), blocks_of_shares};
+        if (!PAIR && work.cluster > 1) {
+            if (all * ways[i].share > 1 << 20) return cudaErrorInvalidValue;
+            blocks_of_shares += (uint32_t(all) * ways[i].share + work.cluster - 1) / work.cluster * work.cluster;
+        }
+        work.all += uint32_t(all);
+        joined = joined || ways[i].splits > 1;
+    }
+    for (int i = n; i < 2; ++i) { maps.a[i] = maps.a[0]; maps.b[i] = maps.b[0]; work.a[i].splits = 1; work.t[i].first = 0xffffffffu; }
+    const auto kernel = product_kernel<T, KIND, ACT, PAIR>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED);
+    if (e != cudaSuccess) return e;
+    const int64_t most = num_sms / CTAS;
+    const unsigned grid = blocks_of_shares ? blocks_of_shares : unsigned((work.all < most ? work.all : most) * CTAS);
+    e = launch_chained(kernel, dim3(grid), dim3(THREADS), SHARED, int(work.cluster), st, maps, work);
+    if (e != cudaSuccess || !joined) return e;
+    int64_t blocks = 1;
+    for (int i = 0; i < n; ++i) {
+        const int64_t b = (a[i].m * ((a[i].n + 7) / 8) + 255) / 256;
+        if (a[i].splits > 1 && b > blocks) blocks = b;
+    }
+    const int64_t places = int64_t(num_sms) * 8;
+    return launch_chained(join_kernel<T, ACT>, dim3(unsigned(blocks < places ? blocks : places), n), dim3(256), 0, 1, st, work);
+}
+
+template <typename T, ProductKind KIND, int ACT> cudaError_t launch(ProductArgs *a, const Way *ways, int n, int num_sms, cudaStream_t st)
+{
+    return ways[0].pair ? launch<T, KIND, ACT, true>(a, ways, n, num_sms, st) : launch<T, KIND, ACT, false>(a, ways, n, num_sms, st);
+}
+
+template <typename T> cudaError_t product(ProductKind kind, ProductArgs *a, const Way *ways, int n, int num_sms, cudaStream_t st)
 {
     switch (kind) {
-    case PRODUCT_STATS: return launch<T, PRODUCT_STATS, RUBICK_ACT_NONE, BN, PAIR>(a, num_sms, st);
-    case PRODUCT_GRAD: return launch<T, PRODUCT_GRAD, RUBICK_ACT_NONE, BN, PAIR>(a, num_sms, st);
-    case PRODUCT_OUT:
-        switch (a.act) {
-        case RUBICK_ACT_RELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_RELU, BN, PAIR>(a, num_sms, st);
-        case RUBICK_ACT_GELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU, BN, PAIR>(a, num_sms, st);
-        case RUBICK_ACT_GELU_TANH: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU_TANH, BN, PAIR>(a, num_sms, st);
-        case RUBICK_ACT_SILU: return launch<T, PRODUCT_OUT, RUBICK_ACT_SILU, BN, PAIR>(a, num_sms, st);
-        }
-        return launch<T, PRODUCT_OUT, RUBICK_ACT_NONE, BN, PAIR>(a, num_sms, st);
-    case PRODUCT_PART: break;
+    case PRODUCT_STATS: return launch<T, PRODUCT_STATS, RUBICK_ACT_NONE>(a, ways, n, num_sms, st);
+    case PRODUCT_GRAD: return launch<T, PRODUCT_GRAD, RUBICK_ACT_NONE>(a, ways, n, num_sms, st);
+    case PRODUCT_OUT: break;
     }
-    const cudaError_t e = launch<T, PRODUCT_PART, RUBICK_ACT_NONE, BN, PAIR>(a, num_sms, st);
-    if (e != cudaSuccess) return e;
-    switch (a.act) {
-    case RUBICK_ACT_RELU: return join<T, RUBICK_ACT_RELU>(a, num_sms, st);
-    case RUBICK_ACT_GELU: return join<T, RUBICK_ACT_GELU>(a, num_sms, st);
-    case RUBICK_ACT_GELU_TANH: return join<T, RUBICK_ACT_GELU_TANH>(a, num_sms, st);
-    case RUBICK_ACT_SILU: return join<T, RUBICK_ACT_SILU>(a, num_sms, st);
+    switch (a[0].act) {
+    case RUBICK_ACT_RELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_RELU>(a, ways, n, num_sms, st);
+    case RUBICK_ACT_GELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU>(a, ways, n, num_sms, st);
+    case RUBICK_ACT_GELU_TANH: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU_TANH>(a, ways, n, num_sms, st);
+    case RUBICK_ACT_SILU: return launch<T, PRODUCT_OUT, RUBICK_ACT_SILU>(a, ways, n, num_sms, st);
     }
-    return join<T, RUBICK_ACT_NONE>(a, num_sms, st);
+    return launch<T, PRODUCT_OUT, RUBICK_ACT_NONE>(a, ways, n, num_sms, st);
 }
-
-// Pairs of blocks (tiles of 256 x 256) where there are enough such tiles for half of the card's pairs; else single blocks
-// (128 x 128), with the k dealt out to several where there are fewer tiles than multiprocessors.
-bool in_pairs(const ProductArgs &a, int num_sms) { return ((a.m + 255) / 256) * ((a.n + 255) / 256) >= num_sms / 4; }
 
 }  // namespace
 
-int product_splits(const ProductArgs &a, int num_sms)
+size_t plan_products(ProductKind kind, ProductArgs *a, int n, int num_sms)
 {
-    if (in_pairs(a, num_sms)) return 1;
-    const int64_t tiles = ((a.m + BM - 1) / BM) * ((a.n + 127) / 128), steps = (a.k + BK - 1) / BK, most = (steps + 7) / 8;
-    int64_t s = num_sms / (tiles < 1 ? 1 : tiles);
-    s = s < 2 || most < 2 ? 1 : s < most ? s : most;
-    const int64_t per = (steps + s - 1) / s;
-    return int((steps + per - 1) / per);              // (no split is left without work)
+    size_t floats = 0;
+    for (int i = 0; i < n; ++i) {
+        a[i].splits = way_of(kind, a[i], num_sms).splits;
+        if (a[i].splits > 1) {
+            if (!a[i].ld_acc) a[i].ld_acc = (a[i].n + 7) & ~int64_t(7);
+            a[i].part_at = floats;
+            floats += size_t(a[i].splits) * a[i].m * a[i].ld_acc;
+        }
+    }
+    return floats;
 }
 
-int product_stats_cols(const ProductArgs &a, int num_sms) { return in_pairs(a, num_sms) ? 128 : 64; }
+int product_stats_cols(const ProductArgs &a, int num_sms) { return way_of(PRODUCT_STATS, a, num_sms).cols / 2; }
 
 bool product_takes(const Operand &o) { return aligned16(o.p) && (o.ld & 7) == 0; }
 
@@ -458,15 +618,27 @@ cudaError_t launch_lay_out(const LayOutArgs &a, int num_sms, cudaStream_t st)
     across = across < places ? across : places;
     const int64_t most = (places + across - 1) / across;
     high = high < most ? high : most;
-    lay_out_kernel<<<dim3(unsigned(across), unsigned(high), a.n), 256, 0, st>>>(a);
-    count_launch();
-    return cudaGetLastError();
+    return launch_chained(lay_out_kernel, dim3(unsigned(across), unsigned(high), a.n), dim3(256), 0, 1, st, a);
 }
 
-cudaError_t launch_product(ProductKind kind, const ProductArgs &a, int num_sms, cudaStream_t st)
+cudaError_t launch_products(ProductKind kind, ProductArgs *a, int n, float *part, int num_sms, cudaStream_t st)
 {
-    if (in_pairs(a, num_sms)) return a.dtype == RUBICK_BF16 ? product<bf16, 256, true>(kind, a, num_sms, st) : product<f16, 256, true>(kind, a, num_sms, st);
-    return a.dtype == RUBICK_BF16 ? product<bf16, 128, false>(kind, a, num_sms, st) : product<f16, 128, false>(kind, a, num_sms, st);
+    // A product is cut by its own sizes, so that it is the same bits alone or with another.  Two share a launch where both are cut
+    // into the same kind of tiles and every block of theirs has a place at once; larger ones keep each other's operands out of
+    // L2 (4,096 x 2,048 -> 8,192, both gradients: 242 us together, 214 one after the other).
+    Way ways[2];
+    for (int i = 0; i < n; ++i) { ways[i] = way_of(kind, a[i], num_sms); a[i].part = part + a[i].part_at; }
+    bool together = n == 1;
+    if (n == 2 && ways[0].pair == ways[1].pair) {
+        const int share = ways[0].share > ways[1].share ? ways[0].share : ways[1].share;
+        const int64_t blocks = (ways[0].blocks + share - 1) / share + (ways[1].blocks + share - 1) / share;
+        together = blocks <= (share > 1 ? resident_clusters(share) : num_sms);
+    }
+    for (int i = 0; i < n; i += together ? n : 1) {
+        const cudaError_t e = a[0].dtype == RUBICK_BF16 ? product<bf16>(kind, a + i, ways + i, together ? n : 1, num_sms, st) : product<f16>(kind, a + i, ways + i, together ? n : 1, num_sms, st);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 }  // namespace rubick

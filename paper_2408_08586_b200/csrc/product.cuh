@@ -11,7 +11,7 @@ struct Operand { const void *p; int64_t ld; int along_k; };
 
 struct DropArgs { const uint64_t *seed; uint32_t below; float scale; };     // kept: word >= below, times scale; seed NULL: no dropout
 
-enum ProductKind { PRODUCT_OUT, PRODUCT_PART, PRODUCT_STATS, PRODUCT_GRAD };
+enum ProductKind { PRODUCT_OUT, PRODUCT_STATS, PRODUCT_GRAD };
 
 struct ProductArgs {
     int64_t m, n, k;
@@ -26,8 +26,9 @@ struct ProductArgs {
     DropArgs drop;
     const float *scale;                  // one float in device memory, or NULL
     const float *acc_in; float *acc_out; // single-precision sums of earlier pieces, and of this and the earlier ones
-    // PRODUCT_PART: the k are dealt out to `splits`, which write their sums to part[split][m][ld_acc]
+    // with splits > 1 the k are dealt out, and the sums of each lie in part[split][m][ld_acc] until they are joined
     float *part;
+    size_t part_at;                      // where they begin in the launch's scratch, in floats
     int splits;
     // PRODUCT_STATS, PRODUCT_GRAD: the logits of vocabulary first .. first + n - 1
     const int32_t *label;
@@ -35,7 +36,7 @@ struct ProductArgs {
     float2 *stats;                       // [ceil(n / product_stats_cols)][m]
     float *at_label;                     // [m] logit of the label
     const float *base, *rest;            // log of the row's sum of exponentials, in two parts (rest may be NULL)
-    const float *weight;                 // [m] weight of a row times the common power of two
+    const float *dloss, *up;             // [m] weight of a row (NULL: 1), and the common power of two
     uint32_t *status;
 };
 enum { WIDE_OUT = 1, WIDE_PRE = 2, WIDE_RES = 4, WIDE_BIAS = 8 };
@@ -61,7 +62,7 @@ struct LinearGradArgs {
     bool wide;                           // every row of dout and pre begins on a 16-byte boundary
     int lanes;                           // lanes of a warp that share a row (a power of two); the others take further rows
 };
-// rows of h whose label takes part (zeros for the others), next to each other; the largest weight of a row
+// rows of h whose label takes part (zeros for the others), next to each other; the weights' common power of two
 struct HeadPrepArgs {
     int64_t rows, ld_h, ld_copy;
     int hidden, vocab, dtype;
@@ -69,9 +70,7 @@ struct HeadPrepArgs {
     const int32_t *label;
     const float *dloss;
     void *copy;
-    float *weight;                       // [rows] weight times 2^s
-    float *scale;                        // 2^-s
-    uint32_t *largest;                   // bits of the largest finite |weight|
+    float *scale;                        // 2^-s, 2^s
 };
 struct HeadFinishArgs {
     int64_t rows;
@@ -88,18 +87,41 @@ struct LayOutArgs {
     int n;
 };
 
-int product_splits(const ProductArgs &a, int num_sms);           // into how many parts the k are dealt out
+// Up to two products of one launch (two only for PRODUCT_OUT without activations): how they are cut, and the floats of
+// scratch that this takes.
+size_t plan_products(ProductKind kind, ProductArgs *a, int n, int num_sms);
+cudaError_t launch_products(ProductKind kind, ProductArgs *a, int n, float *part, int num_sms, cudaStream_t st);
 int product_stats_cols(const ProductArgs &a, int num_sms);       // columns of the logits that one pair (maximum, sum) covers
 bool product_takes(const Operand &o);                            // as it lies, that is
 cudaError_t launch_lay_out(const LayOutArgs &a, int num_sms, cudaStream_t st);
-cudaError_t launch_product(ProductKind kind, const ProductArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_dropout(const DropoutArgs &a, int num_sms, cudaStream_t st);
 void plan_linear_grad(LinearGradArgs &a, int num_sms);
 cudaError_t launch_linear_grad(const LinearGradArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_head_prep(const HeadPrepArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_head_finish(const HeadFinishArgs &a, int num_sms, cudaStream_t st);
 
+// A launch that may begin while the one before it in the stream ends: its kernel waits (chain_wait) before it touches memory.
+template <typename... P, typename... A> cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, const A &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, args...);
+    count_launch();
+    return e;
+}
+
 namespace train {
+
+// The next launch may begin; everything before this one is over.
+__device__ __forceinline__ void chain_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 // ---- dropout: Philox4x32-10 (Salmon et al., SC 2011), the four words of a counter under a key -------------------------
 // A round takes (c0, c1, c2, c3) to (hi(M1 c2) ^ c1 ^ k0, lo(M1 c2), hi(M0 c0) ^ c3 ^ k1, lo(M0 c0)).  The counter is (column / 4,

@@ -172,21 +172,6 @@ template <typename T> T *part(rubick_ctx *ctx, size_t at) { return reinterpret_c
 int64_t up8(int64_t n) { return (n + 7) & ~int64_t(7); }
 bool wide16(const void *p, int64_t ld) { return train::aligned16(p) && (ld & 7) == 0; }
 
-// One product and what it keeps in scratch.
-struct Planned { ProductKind kind; size_t part; };
-Planned plan_product(Parts &parts, ProductArgs &a, int num_sms)
-{
-    a.splits = product_splits(a, num_sms);
-    if (a.splits == 1) return Planned{PRODUCT_OUT, 0};
-    if (!a.ld_acc) a.ld_acc = up8(a.n);
-    return Planned{PRODUCT_PART, parts.take(size_t(a.splits) * a.m * a.ld_acc * sizeof(float))};
-}
-cudaError_t run_product(rubick_ctx *ctx, const Planned &p, ProductArgs &a)
-{
-    if (p.kind == PRODUCT_PART) a.part = part<float>(ctx, p.part);
-    return launch_product(p.kind, a, ctx->num_sms, ctx->stream);
-}
-
 // An operand that the products cannot read as it lies gets a place in scratch and is laid out anew there.
 struct Laid { bool copy; size_t at; int64_t rows, cols; };
 Laid plan_operand(Parts &parts, const Operand &o, int64_t rows, int64_t cols)
@@ -223,10 +208,14 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     const int64_t tiles = (int64_t(d.vocab) + unit - 1) / unit;
     Operand weight = {d_w, d.ld_w, by_output};
     const Laid laid = plan_operand(parts, weight, by_output ? d.vocab : d.hidden, by_output ? d.hidden : d.vocab);
-    const size_t at_copy = parts.take(size_t(d.rows) * ld_copy * 2);
+    // the gradient of w sums over the rows, so that those without a label have to be zeros; elsewhere h is read as it lies
+    const bool copied = backward && d_dw;
+    Operand hidden = {d_h, d.ld_h, 1};
+    const Laid laid_h = copied ? Laid{} : plan_operand(parts, hidden, d.rows, d.hidden);
+    const size_t at_copy = copied ? parts.take(size_t(d.rows) * ld_copy * 2) : 0;
     const size_t at_stats = forward ? parts.take(size_t(tiles) * d.rows * sizeof(float2)) : 0, at_label = forward ? parts.take(size_t(d.rows) * 4) : 0;
     const size_t at_base = forward && backward ? parts.take(size_t(d.rows) * 4) : 0, at_rest = forward && backward ? parts.take(size_t(d.rows) * 4) : 0;
-    const size_t at_weight = backward ? parts.take(size_t(d.rows) * 4) : 0, at_scale = backward ? parts.take(8) : 0;
+    const size_t at_scale = backward ? parts.take(8) : 0;
     // the vocabulary of a piece: as much as 256 MB of dz take, in whole tiles
     int64_t piece = (int64_t(256) << 20) / (2 * d.rows) / 256 * 256;
     if (piece < 256) piece = 256;
@@ -235,9 +224,7 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     const bool several = piece < d.vocab;
     const size_t at_dz = backward ? parts.take(size_t(d.rows) * ld_dz * 2) : 0;
     const size_t at_acc = backward && several && d_dh ? parts.take(size_t(d.rows) * ld_copy * 4) : 0;
-    // the two products of a gradient, one after the other: their splits' sums share a place
-    const size_t joined = parts.used;
-    size_t most = joined;
+    size_t sums = 0;
     auto gradient_products = [&](int64_t first, int64_t n, ProductArgs &h, ProductArgs &w) {
         h = ProductArgs{}; w = ProductArgs{};
         h.dtype = w.dtype = d.dtype;
@@ -255,31 +242,32 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     };
     if (backward) {
         for (const int64_t n : {piece, (d.vocab - 1) % piece + 1}) {
-            ProductArgs h, w;
-            gradient_products(0, n, h, w);
-            for (ProductArgs *x : {&h, &w}) {
-                parts.used = joined;
-                plan_product(parts, *x, ctx->num_sms);
-                if (parts.used > most) most = parts.used;
-            }
+            ProductArgs g[2];
+            gradient_products(0, n, g[0], g[1]);
+            const size_t need = d_dh && d_dw ? plan_products(PRODUCT_OUT, g, 2, ctx->num_sms) : plan_products(PRODUCT_OUT, d_dh ? g : g + 1, 1, ctx->num_sms);
+            sums = need > sums ? need : sums;
         }
     }
-    if ((rc = scratch(ctx, most))) return rc;
+    const size_t at_sums = parts.take(sums * sizeof(float));
+    if ((rc = scratch(ctx, parts.used))) return rc;
 
     HeadPrepArgs pre = {};
     pre.rows = d.rows; pre.ld_h = d.ld_h; pre.ld_copy = ld_copy; pre.hidden = d.hidden; pre.vocab = d.vocab; pre.dtype = d.dtype;
-    pre.h = d_h; pre.label = d_label; pre.dloss = d_dloss; pre.copy = part<void>(ctx, at_copy);
-    if (backward) { pre.weight = part<float>(ctx, at_weight); pre.scale = part<float>(ctx, at_scale); pre.largest = part<uint32_t>(ctx, at_scale) + 1; }
-    CUDA_TRY(ctx, launch_head_prep(pre, ctx->num_sms, ctx->stream), "launch head_prep");
-
+    pre.h = d_h; pre.label = d_label; pre.dloss = d_dloss;
+    if (copied) { pre.copy = part<void>(ctx, at_copy); hidden = Operand{pre.copy, ld_copy, 1}; }
+    if (backward) {
+        pre.scale = part<float>(ctx, at_scale);
+        CUDA_TRY(ctx, launch_head_prep(pre, ctx->num_sms, ctx->stream), "launch head_prep");
+    }
     LayOutArgs lay = {};
     lay_out(ctx, lay, laid, weight);
+    if (!copied) lay_out(ctx, lay, laid_h, hidden);
     CUDA_TRY(ctx, launch_lay_out(lay, ctx->num_sms, ctx->stream), "launch lay_out");
-    z.a = Operand{pre.copy, ld_copy, 1};
+    z.a = hidden;
     if (forward) {
         z.b = weight;
         z.stats = part<float2>(ctx, at_stats); z.at_label = part<float>(ctx, at_label);
-        CUDA_TRY(ctx, launch_product(PRODUCT_STATS, z, ctx->num_sms, ctx->stream), "launch product (logits)");
+        CUDA_TRY(ctx, launch_products(PRODUCT_STATS, &z, 1, nullptr, ctx->num_sms, ctx->stream), "launch product (logits)");
         HeadFinishArgs f = {};
         f.rows = d.rows; f.vocab = d.vocab; f.tiles = int(tiles);
         f.label = d_label; f.stats = z.stats; f.at_label = z.at_label; f.loss = d_loss; f.lse = d_lse;
@@ -289,15 +277,15 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     if (!backward) return RUBICK_OK;
     z.base = forward ? part<float>(ctx, at_base) : d_lse_in;
     z.rest = forward ? part<float>(ctx, at_rest) : nullptr;
-    z.weight = pre.weight;
+    z.dloss = d_dloss; z.up = pre.scale + 1;
     for (int64_t first = 0; first < d.vocab; first += piece) {
         const int64_t n = first + piece < d.vocab ? piece : d.vocab - first;
-        ProductArgs h, w;
+        ProductArgs g[2], &h = g[0], &w = g[1];
         gradient_products(first, n, h, w);
         z.n = n; z.first = int32_t(first);
         z.b = Operand{h.b.p, weight.ld, by_output};
         z.out = part<void>(ctx, at_dz); z.ld_out = ld_dz;
-        CUDA_TRY(ctx, launch_product(PRODUCT_GRAD, z, ctx->num_sms, ctx->stream), "launch product (logits' gradient)");
+        CUDA_TRY(ctx, launch_products(PRODUCT_GRAD, &z, 1, nullptr, ctx->num_sms, ctx->stream), "launch product (logits' gradient)");
         h.scale = w.scale = pre.scale;
         h.a = Operand{z.out, ld_dz, 1};
         const Operand dz = {z.out, ld_dz, 0}, copy = {pre.copy, ld_copy, 0};
@@ -307,12 +295,10 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
             if (first) h.acc_in = part<float>(ctx, at_acc);
             if (first + n < d.vocab) h.acc_out = part<float>(ctx, at_acc);
         }
-        for (ProductArgs *x : {&h, &w}) {
-            if (!(x == &h ? d_dh : d_dw)) continue;
-            parts.used = joined;
-            const Planned p = plan_product(parts, *x, ctx->num_sms);
-            CUDA_TRY(ctx, run_product(ctx, p, *x), "launch product (gradient)");
-        }
+        ProductArgs *const which = d_dh ? g : g + 1;
+        const int products = d_dh && d_dw ? 2 : 1;
+        plan_products(PRODUCT_OUT, which, products, ctx->num_sms);
+        CUDA_TRY(ctx, launch_products(PRODUCT_OUT, which, products, part<float>(ctx, at_sums), ctx->num_sms, ctx->stream), "launch products (gradients)");
     }
     return RUBICK_OK;
 }
@@ -540,13 +526,13 @@ int rubick_linear_forward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, con
     a.drop = drop_args(d.p, d_seed);
     Parts parts;
     const Laid x = plan_operand(parts, a.a, d.rows, d.inputs), w = plan_operand(parts, a.b, by_output ? d.outputs : d.inputs, by_output ? d.inputs : d.outputs);
-    const Planned p = plan_product(parts, a, ctx->num_sms);
+    const size_t at_sums = parts.take(plan_products(PRODUCT_OUT, &a, 1, ctx->num_sms) * sizeof(float));
     if ((rc = scratch(ctx, parts.used))) return rc;
     LayOutArgs lay = {};
     lay_out(ctx, lay, x, a.a);
     lay_out(ctx, lay, w, a.b);
     CUDA_TRY(ctx, launch_lay_out(lay, ctx->num_sms, ctx->stream), "launch lay_out");
-    CUDA_TRY(ctx, run_product(ctx, p, a), "launch linear_forward");
+    CUDA_TRY(ctx, launch_products(PRODUCT_OUT, &a, 1, part<float>(ctx, at_sums), ctx->num_sms, ctx->stream), "launch linear_forward");
     return RUBICK_OK;
 }
 
@@ -582,8 +568,8 @@ int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, co
     Parts parts;
     const bool keep = products && !plain;
     const size_t at_dz = keep ? parts.take(size_t(d.rows) * g.ld_dz * 2) : 0;
-    const size_t at_sums = d_dbias ? parts.take(size_t(g.chunks) * d.outputs * 4) : 0;
-    ProductArgs dx = {}, dw = {};
+    const size_t at_columns = d_dbias ? parts.take(size_t(g.chunks) * d.outputs * 4) : 0;
+    ProductArgs both[2] = {}, &dx = both[0], &dw = both[1];
     dx.dtype = dw.dtype = d.dtype;
     dx.status = dw.status = ctx->d_status;
     dx.m = d.rows; dx.n = d.inputs; dx.k = d.outputs;
@@ -593,14 +579,12 @@ int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, co
     dw.out = d_dw; dw.ld_out = d.ld_w; dw.wide = wide16(d_dw, d.ld_w) ? WIDE_OUT : 0;
     Operand x = {d_x, d.ld_x, 0};
     const Laid laid_x = d_dw ? plan_operand(parts, x, d.rows, d.inputs) : Laid{}, laid_w = d_dx ? plan_operand(parts, dx.b, by_output ? d.outputs : d.inputs, by_output ? d.inputs : d.outputs) : Laid{};
-    const size_t joined = parts.used;
-    const Planned px = d_dx ? plan_product(parts, dx, ctx->num_sms) : Planned{};
-    const size_t most = parts.used;
-    parts.used = joined;                       // (one after the other: their splits' sums share a place)
-    const Planned pw = d_dw ? plan_product(parts, dw, ctx->num_sms) : Planned{};
-    if ((rc = scratch(ctx, parts.used > most ? parts.used : most))) return rc;
+    ProductArgs *const which = d_dx ? both : both + 1;
+    const int n_products = d_dx && d_dw ? 2 : 1;
+    const size_t at_sums = products ? parts.take(plan_products(PRODUCT_OUT, which, n_products, ctx->num_sms) * sizeof(float)) : 0;
+    if ((rc = scratch(ctx, parts.used))) return rc;
     if (keep) g.dz = part<void>(ctx, at_dz);
-    if (d_dbias) g.part = part<float>(ctx, at_sums);
+    if (d_dbias) g.part = part<float>(ctx, at_columns);
     if (d_dbias && g.chunks > 1) {
         if ((rc = tickets(ctx, size_t(g.strips)))) return rc;
         g.tickets = ctx->d_tickets;
@@ -612,16 +596,11 @@ int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, co
     CUDA_TRY(ctx, launch_lay_out(lay, ctx->num_sms, ctx->stream), "launch lay_out");
     const void *dz = keep ? g.dz : d_dout;
     const int64_t ld_dz = keep ? g.ld_dz : d.ld_out;
-    if (d_dx) {
-        dx.a = Operand{dz, ld_dz, 1};
-        CUDA_TRY(ctx, run_product(ctx, px, dx), "launch product (dx)");
-    }
-    if (d_dw) {
-        const Operand z = {dz, ld_dz, 0};
-        dw.a = by_output ? z : x;
-        dw.b = by_output ? x : z;
-        CUDA_TRY(ctx, run_product(ctx, pw, dw), "launch product (dw)");
-    }
+    dx.a = Operand{dz, ld_dz, 1};
+    const Operand z = {dz, ld_dz, 0};
+    dw.a = by_output ? z : x;
+    dw.b = by_output ? x : z;
+    if (products) CUDA_TRY(ctx, launch_products(PRODUCT_OUT, which, n_products, part<float>(ctx, at_sums), ctx->num_sms, ctx->stream), "launch products (gradients)");
     return RUBICK_OK;
 }
 
