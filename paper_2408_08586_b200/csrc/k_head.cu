@@ -68,26 +68,38 @@ __global__ void __launch_bounds__(32 * FINISH_WARPS) head_finish_kernel(const __
     const int64_t row = int64_t(blockIdx.x) * 32 + lane;
     const bool live = row < a.rows && takes_part(a.label[row], a.vocab);
     float top = ninf, sum = 0.f;
-    auto join = [&](float2 p) {
-        const float m = fmaxf(top, p.x), at = m == ninf ? 0.f : m;
-        sum = sum * ex2((top - at) * LOG2E) + p.y * ex2((p.x - at) * LOG2E);
+    // eight at a time: their maximum first, then terms that do not wait for one another
+    constexpr int AHEAD = 8;
+    auto join = [&](const float2 (&p)[AHEAD]) {
+        float m = top;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) m = fmaxf(m, p[j].x);
+        const float at = m == ninf ? 0.f : m;
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) s += p[j].y * ex2((p[j].x - at) * LOG2E);
+        sum = fmaf(sum, ex2((top - at) * LOG2E), s);
         top = m;
     };
     if (live) {
-        constexpr int AHEAD = 8;
         for (int i = warp; i < a.tiles; i += FINISH_WARPS * AHEAD) {
             float2 p[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) p[j] = i + j * FINISH_WARPS < a.tiles ? a.stats[int64_t(i + j * FINISH_WARPS) * a.rows + row] : make_float2(ninf, 0.f);
-#pragma unroll
-            for (int j = 0; j < AHEAD; ++j) join(p[j]);
+            join(p);
         }
     }
     joined[warp][lane] = make_float2(top, sum);
     __syncthreads();
     if (warp || row >= a.rows) return;
-#pragma unroll 8
-    for (int w = 1; w < FINISH_WARPS; ++w) join(joined[w][lane]);
+    top = ninf; sum = 0.f;
+#pragma unroll 1
+    for (int w = 0; w < FINISH_WARPS; w += AHEAD) {
+        float2 p[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) p[j] = joined[w + j][lane];
+        join(p);
+    }
     const float rest = logf(sum), lse = top + rest;
     a.loss[row] = live ? (top - a.at_label[row]) + rest : 0.f;
     if (a.lse) a.lse[row] = live ? lse : 0.f;

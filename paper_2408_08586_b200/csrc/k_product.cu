@@ -245,8 +245,10 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                         const int64_t column = n0 + c + lane;
                         const int high = rows - m0 < 32 ? int(rows - m0) : 32;
                         auto cell = [&](int r) { return reinterpret_cast<float *>(mine + r * 128 + (((lane >> 2) ^ (r & 7)) << 4)) + (lane & 3); };
+                        // (a gradient's sums have nothing but their factor to get)
+                        const bool bare = ACT == RUBICK_ACT_NONE && !finish.acc_in && !finish.acc_out && !finish.bias && !finish.pre && !finish.drop.on;
                         bool over = false;
-                        for (int pass = 0; pass < 2 && !over; ++pass) {
+                        for (int pass = 0; pass < 2 && !over && !bare; ++pass) {
                             if (pass == 1 && finish.pre) {
                                 __syncwarp();
                                 if (column < cols)
@@ -273,11 +275,15 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                         }
                         __syncwarp();
                         if (!over && column < cols) {
+                            const float factor = bare ? finish.scale : 1.f;
+                            T *to = finish.out + m0 * finish.ld_out + column;
+                            if (finish.residual) {
+                                const T *res = finish.residual + m0 * finish.ld_res + column;
 #pragma unroll 4
-                            for (int r = 0; r < high; ++r) {
-                                float u = *cell(r);
-                                if (finish.residual) u += to_f(finish.residual[(m0 + r) * finish.ld_res + column]);
-                                finish.out[(m0 + r) * finish.ld_out + column] = from_f<T>(u);
+                                for (int r = 0; r < high; ++r, to += finish.ld_out, res += finish.ld_res) *to = from_f<T>(fmaf(*cell(r), factor, to_f(*res)));
+                            } else {
+#pragma unroll 8
+                                for (int r = 0; r < high; ++r, to += finish.ld_out) *to = from_f<T>(*cell(r) * factor);
                             }
                         }
                     }
@@ -484,8 +490,9 @@ int resident_clusters(int size)
     return n;
 }
 
-// How a product is cut.  What a way takes is estimated in microseconds from measured times: a stage of 64 k takes a pair of
-// blocks 0.33 for 256 x 256 sums (0.25 for 192 columns, 0.2 for 128), a single block PLAN_SINGLE for 128 x 128.
+// How a product is cut.  What a way takes is estimated in microseconds from measured times: a stage of 32 KB a block takes
+// 0.33 (256 x 256 sums of a pair as well as 128 x 128 of a single block: it is the fetching that lasts, 97 GB/s a
+// multiprocessor), smaller stages as much less; what does not depend on the tiles is 8 for a pair and 6 for a single block.
 struct Way { bool pair; int cols, share, splits; float cost; int64_t blocks; };
 Way way_of(ProductKind kind, const ProductArgs &a, int num_sms, bool pair)
 {
@@ -498,7 +505,7 @@ Way way_of(ProductKind kind, const ProductArgs &a, int num_sms, bool pair)
             for (int s = 1; s <= 8; ++s) {
                 if (s > 1 && (kind != PRODUCT_OUT || steps < 8 * s)) break;
                 const int64_t per = (steps + s - 1) / s, splits = (steps + per - 1) / per, waves = (tiles * splits + places - 1) / places;
-                const float each = cols == 256 ? 0.33f : cols == 192 ? 0.25f : 0.2f;
+                const float each = (A_BYTES + (a.b.along_k ? cols / 2 * 128 : (cols / 2 + 63) / 64 * int(BLOCK_BYTES))) * (0.33f / STAGE);
                 const float cost = float(waves) * float(per) * each + 8.f + (splits > 1 ? 4.f + float(splits) * float(a.m) * float(a.n) * 2e-6f : 0.f);
                 if (cost < best.cost) best = Way{true, cols, 1, int(splits), cost, 2 * tiles * splits};
             }
