@@ -37,6 +37,11 @@ struct Tiling {
 struct Work { ProductArgs a[2]; Tiling t[2]; uint32_t all, cluster; };
 struct Maps { CUtensorMap a[2], b[2]; };
 
+// Pairs of blocks, single blocks, or single blocks for products of up to FEW_ROWS rows, which exchange the operands: a tile is
+// 128 columns by all rows (16, 32, 48 or 64 of them), so that a stage is little more than the weights it is there for.
+enum Shape : int { SHAPE_PAIR, SHAPE_SINGLE, SHAPE_FEW };
+constexpr int FEW_ROWS = 64;
+
 // Tile number -> tile row, tile column, split: eight tile rows at a time, so that what runs at once shares operands in L2.
 __device__ __forceinline__ void place(const Tiling &t, uint32_t i, int &m, int &n, int &split)
 {
@@ -49,9 +54,10 @@ __device__ __forceinline__ void place(const Tiling &t, uint32_t i, int &m, int &
 
 __device__ __forceinline__ float ninf() { return __uint_as_float(0xff800000u); }
 
-template <typename T, ProductKind KIND, int ACT, bool PAIR>
+template <typename T, ProductKind KIND, int ACT, Shape SHAPE>
 __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Work work)
 {
+    constexpr bool PAIR = SHAPE == SHAPE_PAIR, FEW = SHAPE == SHAPE_FEW;
     constexpr int CTAS = PAIR ? 2 : 1;
     constexpr uint32_t HALF = PAIR ? PAIR_COLS : SINGLE_COLS, COLUMNS = 2 * HALF;      // of tensor memory: two tiles
     chain_go();
@@ -64,7 +70,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
     volatile uint32_t *const given_up = words;       // [0] someone waited in vain; [1] where the tensor memory begins
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // a pair's rank in its cluster; a single block's among those that share its tile
-    const bool shared_tiles = !PAIR && KIND == PRODUCT_OUT && work.cluster > 1;
+    const bool shared_tiles = !PAIR && KIND == PRODUCT_OUT && (FEW || work.cluster > 1);
     const int mine_is = shared_tiles && blockIdx.x >= work.t[1].first;
     const uint32_t ranks = PAIR ? 2 : shared_tiles ? work.t[mine_is].share : 1;
     const uint32_t rank = PAIR ? cluster_rank() : shared_tiles ? (blockIdx.x - work.t[mine_is].first) % ranks : 0;
@@ -105,9 +111,9 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                     int tm, tn, split;
                     place(t, which ? i - work.t[0].all : i, tm, tn, split);
                     if (!PAIR) split += rank;        // (a tile's blocks; there are no splits beside them)
-                    const int m0 = (tm * CTAS + (PAIR ? int(rank) : 0)) * BM, n0 = tn * t.cols + (PAIR ? int(rank) * (t.cols / 2) : 0);
+                    const int m0 = FEW ? tn * BM : (tm * CTAS + (PAIR ? int(rank) : 0)) * BM, n0 = FEW ? 0 : tn * t.cols + (PAIR ? int(rank) * (t.cols / 2) : 0);
                     const int k0 = split * t.per, k1 = k0 + t.per < t.steps ? k0 + t.per : t.steps;
-                    const bool ak = a.a.along_k, bk = a.b.along_k;
+                    const bool ak = FEW ? a.b.along_k : a.a.along_k, bk = FEW || a.b.along_k;
                     const int blocks = (t.cols / CTAS + 63) / 64;
                     const uint32_t bytes = t.bytes * CTAS;
                     for (int k = k0; k < k1; ++k, ++round) {
@@ -139,7 +145,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             auto sum = [&](auto number) {
                 constexpr int which = decltype(number)::value;
                 const Tiling &t = work.t[which];
-                const bool ak = work.a[which].a.along_k, bk = work.a[which].b.along_k;
+                const bool ak = FEW ? work.a[which].b.along_k : work.a[which].a.along_k, bk = FEW || work.a[which].b.along_k;
                 const uint32_t desc = instruction_desc(std::is_same<T, bf16>::value, ak, bk, BM * CTAS, t.cols);
                 const uint64_t da = operand_desc(stages, ak), db = operand_desc(stages + A_BYTES, bk);
                 const uint32_t sa = operand_step(ak), sb = operand_step(bk);
@@ -176,6 +182,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
         int which = TWO && first >= work.t[0].all;
         Finish<T, ACT> finish(work.a[which]);
         uint32_t tile = 0;
+        float running_top = ninf(), running_sum = 0.f;             // few rows: of all of the block's tiles
         for (uint32_t i = first; i < end; i += step, ++tile) {
             if (TWO && !which && i >= work.t[0].all) {
                 which = 1;
@@ -188,13 +195,36 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             place(t, which ? i - work.t[0].all : i, tm, tn, split);
             const uint32_t half = tile & 1;
             const int width = KIND == PRODUCT_OUT ? t.cols / 2 : int(HALF) / 2;      // (only sums may be cut otherwise)
-            const int64_t m0 = (int64_t(tm) * CTAS + (PAIR ? rank : 0)) * BM + quarter * 32;
-            const int64_t n0 = int64_t(tn) * t.cols + side * width;
+            const int64_t m0 = FEW ? side * 32 : (int64_t(tm) * CTAS + (PAIR ? rank : 0)) * BM + quarter * 32;
+            const int64_t n0 = FEW ? int64_t(tn) * BM + quarter * 32 : int64_t(tn) * t.cols + side * width;
             if (!barrier_wait(done + 8 * half, tile / 2 & 1, given_up)) break;
             __syncwarp();
             tcgen_after_sync();
-            const uint32_t at = tmem + half * HALF + side * width + (uint32_t(quarter * 32) << 16);
-            if (ranks > 1 && shared_tiles) {
+            const uint32_t at = tmem + half * HALF + side * (FEW ? 32 : width) + (uint32_t(quarter * 32) << 16);
+            // 32 columns of the warp's rows, a lane a row (few rows: a lane has a column, and they are exchanged)
+            auto load32 = [&](int c, float (&v)[32]) {
+                tmem_load32(at + c, v);
+                if constexpr (FEW) {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) *reinterpret_cast<float *>(mine + e * 128 + (((lane >> 2) ^ (e & 7)) << 4) + (lane & 3) * 4) = v[e];
+                    __syncwarp();
+#pragma unroll
+                    for (int p = 0; p < 8; ++p) {
+                        const float4 x = *reinterpret_cast<const float4 *>(mine + lane * 128 + ((p ^ (lane & 7)) << 4));
+                        v[4 * p] = x.x; v[4 * p + 1] = x.y; v[4 * p + 2] = x.z; v[4 * p + 3] = x.w;
+                    }
+                    __syncwarp();
+                }
+            };
+            if (FEW && m0 >= rows) {
+                // (no rows for this half of the warps)
+            } else if (KIND == PRODUCT_OUT && FEW) {
+                float v[32];
+                tmem_load32(at, v);
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (m0 + e < rows) *reinterpret_cast<float *>(shared + (m0 + e) * SHARE_LINE + (quarter * 32 + lane) * 4) = v[e];
+            } else if (ranks > 1 && shared_tiles) {
                 // this block's share of the sums, for all of the cluster to read (nothing is copied or multiplied any more)
                 if (m0 < rows)
 #pragma unroll 1
@@ -293,10 +323,10 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 // a thread has a row: running maximum and sum of exponentials over its columns
                 const int64_t row = m0 + lane;
                 const int64_t label = row < rows ? int64_t(a.label[row]) - a.first - n0 : -1;
-                float top = ninf(), sum = 0.f;
-                for (int c = 0; c < width; c += 32) {
+                float top = FEW ? running_top : ninf(), sum = FEW ? running_sum : 0.f;
+                for (int c = 0; c < (FEW ? 32 : width); c += 32) {
                     float v[32];
-                    tmem_load32(at + c, v);
+                    load32(c, v);
                     const int64_t left = cols - (n0 + c);
                     if (left <= 0) continue;
                     if (left < 32) {
@@ -318,7 +348,8 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                     sum = sum * ex2((top - from) * LOG2E) + (s0 + s1);
                     top = m;
                 }
-                if (row < rows && n0 < cols) a.stats[(int64_t(tn) * 2 + side) * rows + row] = make_float2(top, sum);
+                if constexpr (FEW) { running_top = top; running_sum = sum; }
+                else if (row < rows && n0 < cols) a.stats[(int64_t(tn) * 2 + side) * rows + row] = make_float2(top, sum);
             } else {
                 // a thread has a row; 64 columns become 128 bytes of it, written line by line
                 const int64_t row = m0 + lane;
@@ -328,11 +359,11 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 const float from = live ? a.base[row] : 0.f, rest = live && a.rest ? a.rest[row] : 0.f, w = live ? (a.dloss ? a.dloss[row] : 1.f) * *a.up : 0.f;
                 const uint32_t mask = live ? 0xffffffffu : 0u;                // (rows that take no part, whatever their logits are)
                 const int64_t label = live ? int64_t(is) - a.first - n0 : -1;
-                for (int c = 0; c < width; c += 64) {
+                for (int c = 0; c < (FEW ? 32 : width); c += 64) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
+                    for (int h = 0; h < (FEW ? 1 : 2); ++h) {
                         float v[32];
-                        tmem_load32(at + c + 32 * h, v);
+                        load32(c + 32 * h, v);
                         const int here = c + 32 * h;
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = w * ex2(((v[e] - from) - rest) * LOG2E);
@@ -345,9 +376,11 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                             uint4 p;
                             p.x = pack_pair(v[8 * q], v[8 * q + 1], T()) & mask; p.y = pack_pair(v[8 * q + 2], v[8 * q + 3], T()) & mask;
                             p.z = pack_pair(v[8 * q + 4], v[8 * q + 5], T()) & mask; p.w = pack_pair(v[8 * q + 6], v[8 * q + 7], T()) & mask;
-                            *reinterpret_cast<uint4 *>(mine + lane * 128 + (((h * 4 + q) ^ (lane & 7)) << 4)) = p;
+                            if constexpr (!FEW) *reinterpret_cast<uint4 *>(mine + lane * 128 + (((h * 4 + q) ^ (lane & 7)) << 4)) = p;
+                            else if (in && n0 + q * 8 < finish.ld_out) *reinterpret_cast<uint4 *>(finish.out + row * finish.ld_out + n0 + q * 8) = p;
                         }
                     }
+                    if constexpr (FEW) break;
                     __syncwarp();
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
@@ -363,12 +396,26 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             __syncwarp();
             if (lane == 0) barrier_arrive_at(PAIR ? at_rank(taken + 8 * half, 0) : taken + 8 * half);
         }
+        if constexpr (KIND == PRODUCT_STATS && FEW) *reinterpret_cast<float2 *>(mine + lane * 8) = make_float2(running_top, running_sum);
     }
     __syncthreads();
+    if constexpr (KIND == PRODUCT_STATS && FEW) {
+        // a block's pair of a row: its warps' quarters joined
+        const ProductArgs &a = work.a[0];
+        if (threadIdx.x < a.m) {
+            const uint8_t *const theirs = shared + STAGES * STAGE + (threadIdx.x >> 5) * 4 * 4096 + (threadIdx.x & 31) * 8;
+            float2 p[4];
+            float top = ninf(), sum = 0.f;
+            for (int w = 0; w < 4; ++w) { p[w] = *reinterpret_cast<const float2 *>(theirs + w * 4096); top = fmaxf(top, p[w].x); }
+            const float from = top == ninf() ? 0.f : top;
+            for (int w = 0; w < 4; ++w) sum += p[w].y * ex2((p[w].x - from) * LOG2E);
+            a.stats[int64_t(blockIdx.x) * a.m + threadIdx.x] = make_float2(top, sum);
+        }
+    }
     if (PAIR || shared_tiles) cluster_sync();        // (a pair: the other block's copies, products and arrivals end here as well)
     if (shared_tiles) {
         // the blocks' shares added up in their order, every `ranks`-th row here: eight sums a lane, two rows a warp
-        if (ranks > 1 && first < end && warp >= FIRST_READER && !*given_up) {
+        if ((FEW || ranks > 1) && first < end && warp >= FIRST_READER && !*given_up) {
             const int which = mine_is;
             const uint32_t from_rank = cluster_rank() - rank;
             const ProductArgs &a = work.a[which];
@@ -407,7 +454,8 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256) join_kerne
     chain_go();
     chain_wait();
     const ProductArgs &a = work.a[blockIdx.y];
-    if (a.splits == 1) return;
+    const int splits = a.way.splits;
+    if (splits == 1) return;
     const Finish<T, ACT> finish(a);
     const int64_t units = (a.n + 7) / 8, all = a.m * units;
     for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += int64_t(gridDim.x) * blockDim.x) {
@@ -415,7 +463,7 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256) join_kerne
         float v[8] = {}, bias[8];
         finish.load_bias(c, bias);
 #pragma unroll 4
-        for (int s = 0; s < a.splits; ++s) {
+        for (int s = 0; s < splits; ++s) {
             float p[8];
             load8<float>(a.part + (int64_t(s) * a.m + row) * a.ld_acc, c, a.ld_acc, true, p);
 #pragma unroll
@@ -474,7 +522,7 @@ int resident_clusters(int size)
     std::atomic<int> &slot = known[device][size == 2 ? 1 : size == 4 ? 2 : 3];
     int n = slot.load(std::memory_order_relaxed);
     if (n) return n - 1;
-    const auto kernel = product_kernel<bf16, PRODUCT_OUT, RUBICK_ACT_NONE, false>;
+    const auto kernel = product_kernel<bf16, PRODUCT_OUT, RUBICK_ACT_NONE, SHAPE_SINGLE>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(64 * size); cfg.blockDim = dim3(THREADS); cfg.dynamicSmemBytes = SHARED;
     cudaLaunchAttribute attr[1];
@@ -493,69 +541,69 @@ int resident_clusters(int size)
 // How a product is cut.  What a way takes is estimated in microseconds from measured times: a stage of 32 KB a block takes
 // 0.33 (256 x 256 sums of a pair as well as 128 x 128 of a single block: it is the fetching that lasts, 97 GB/s a
 // multiprocessor), smaller stages as much less; what does not depend on the tiles is 8 for a pair and 6 for a single block.
-struct Way { bool pair; int cols, share, splits; float cost; int64_t blocks; };
-Way way_of(ProductKind kind, const ProductArgs &a, int num_sms, bool pair)
+ProductWay way_of(ProductKind kind, const ProductArgs &a, int num_sms)
 {
     const int64_t steps = (a.k + BK - 1) / BK;
-    Way best = {pair, pair ? PAIR_COLS : SINGLE_COLS, 1, 1, 3e38f, 0};
-    if (pair) {
-        for (const int cols : {256, 192, 128}) {
-            if (kind != PRODUCT_OUT && cols != PAIR_COLS) continue;
-            const int64_t tiles = ((a.m + 255) / 256) * ((a.n + cols - 1) / cols), places = num_sms / 2;
-            for (int s = 1; s <= 8; ++s) {
-                if (s > 1 && (kind != PRODUCT_OUT || steps < 8 * s)) break;
-                const int64_t per = (steps + s - 1) / s, splits = (steps + per - 1) / per, waves = (tiles * splits + places - 1) / places;
-                const float each = (A_BYTES + (a.b.along_k ? cols / 2 * 128 : (cols / 2 + 63) / 64 * int(BLOCK_BYTES))) * (0.33f / STAGE);
-                const float cost = float(waves) * float(per) * each + 8.f + (splits > 1 ? 4.f + float(splits) * float(a.m) * float(a.n) * 2e-6f : 0.f);
-                if (cost < best.cost) best = Way{true, cols, 1, int(splits), cost, 2 * tiles * splits};
-            }
+    ProductWay best = {SHAPE_SINGLE, SINGLE_COLS, 1, 1, 3e38f, 0};
+    for (const int cols : {256, 192, 128}) {
+        if (kind != PRODUCT_OUT && cols != PAIR_COLS) continue;
+        const int64_t tiles = ((a.m + 255) / 256) * ((a.n + cols - 1) / cols), places = num_sms / 2;
+        for (int s = 1; s <= 8; ++s) {
+            if (s > 1 && (kind != PRODUCT_OUT || steps < 8 * s)) break;
+            const int64_t per = (steps + s - 1) / s, splits = (steps + per - 1) / per, waves = (tiles * splits + places - 1) / places;
+            const float each = (A_BYTES + (a.b.along_k ? cols / 2 * 128 : (cols / 2 + 63) / 64 * int(BLOCK_BYTES))) * (0.33f / STAGE);
+            const float cost = float(waves) * float(per) * each + 8.f + (splits > 1 ? 4.f + float(splits) * float(a.m) * float(a.n) * 2e-6f : 0.f);
+            if (cost < best.cost) best = ProductWay{SHAPE_PAIR, cols, 1, int(splits), cost, 2 * tiles * splits};
         }
-    } else {
-        const int64_t tiles = ((a.m + 127) / 128) * ((a.n + 127) / 128);
+    }
+    // single blocks: 128 x 128 sums, or few rows
+    for (const Shape shape : {SHAPE_SINGLE, SHAPE_FEW}) {
+        if (shape == SHAPE_FEW && (a.m > FEW_ROWS || !a.a.along_k)) continue;
+        const int cols = shape == SHAPE_FEW ? int(a.m + 15) / 16 * 16 : SINGLE_COLS;
+        const int64_t tiles = (shape == SHAPE_FEW ? 1 : (a.m + 127) / 128) * ((a.n + 127) / 128);
+        const float each = (A_BYTES + cols * 128) * (0.33f / STAGE);
         for (int s = 1; s <= 8; s *= 2) {
             if (s > 1 && (kind != PRODUCT_OUT || steps < 2 * s || tiles > resident_clusters(s))) break;
             const int64_t per = (steps + s - 1) / s, waves = (tiles + num_sms - 1) / num_sms;
             if ((steps + per - 1) / per != s) continue;          // (no block is left without work)
-            const float cost = float(waves) * float(per) * 0.33f + 6.f + (s > 1 ? 1.f : 0.f);
-            if (cost < best.cost) best = Way{false, SINGLE_COLS, s, 1, cost, tiles * s};
+            // (a gradient has another one beside it, which has no few rows: two launches instead of one)
+            const float cost = float(waves) * float(per) * each + 6.f + (s > 1 ? 1.f : 0.f) + (shape == SHAPE_FEW && a.beside ? 3.f : 0.f);
+            if (cost < best.cost) best = ProductWay{shape, cols, s, 1, cost, tiles * s};
         }
     }
     return best;
 }
-Way way_of(ProductKind kind, const ProductArgs &a, int num_sms)
-{
-    const Way p = way_of(kind, a, num_sms, true), s = way_of(kind, a, num_sms, false);
-    return p.cost < s.cost ? p : s;
-}
 
-template <typename T, ProductKind KIND, int ACT, bool PAIR> cudaError_t launch(ProductArgs *a, const Way *ways, int n, int num_sms, cudaStream_t st)
+template <typename T, ProductKind KIND, int ACT, Shape SHAPE> cudaError_t launch(ProductArgs *a, int n, int num_sms, cudaStream_t st)
 {
+    constexpr bool PAIR = SHAPE == SHAPE_PAIR, FEW = SHAPE == SHAPE_FEW;
     constexpr int CTAS = PAIR ? 2 : 1;
     Maps maps;
     Work work = {};
     work.cluster = CTAS;
-    for (int i = 0; i < n; ++i) if (uint32_t(ways[i].share) > work.cluster) work.cluster = ways[i].share;
+    for (int i = 0; i < n; ++i) if (uint32_t(a[i].way.share) > work.cluster) work.cluster = a[i].way.share;
     uint32_t blocks_of_shares = 0;
     bool joined = false;
     for (int i = 0; i < n; ++i) {
-        const int cols = ways[i].cols;
-        if (!operand_map(&maps.a[i], a[i].a, a[i].dtype, a[i].m, a[i].k, BM) || !operand_map(&maps.b[i], a[i].b, a[i].dtype, a[i].n, a[i].k, cols / CTAS)) return cudaErrorInvalidValue;
-        a[i].splits = ways[i].splits;
-        const int64_t tiles_m = (a[i].m + BM * CTAS - 1) / (BM * CTAS), tiles_n = (a[i].n + cols - 1) / cols, steps = (a[i].k + BK - 1) / BK;
-        const int64_t parts = PAIR ? ways[i].splits : ways[i].share, all = tiles_m * tiles_n * (PAIR ? parts : 1);
+        const int cols = a[i].way.cols;
+        if (!operand_map(&maps.a[i], FEW ? a[i].b : a[i].a, a[i].dtype, FEW ? a[i].n : a[i].m, a[i].k, BM) ||
+            !operand_map(&maps.b[i], FEW ? a[i].a : a[i].b, a[i].dtype, FEW ? a[i].m : a[i].n, a[i].k, cols / CTAS)) return cudaErrorInvalidValue;
+        if (FEW && !a[i].a.along_k) return cudaErrorInvalidValue;
+        const int64_t tiles_m = FEW ? 1 : (a[i].m + BM * CTAS - 1) / (BM * CTAS), tiles_n = (a[i].n + (FEW ? BM : cols) - 1) / (FEW ? BM : cols), steps = (a[i].k + BK - 1) / BK;
+        const int64_t parts = PAIR ? a[i].way.splits : a[i].way.share, all = tiles_m * tiles_n * (PAIR ? parts : 1);
         if (work.all + all > 0x7fffffff || steps > 0x7fffffff / BK) return cudaErrorInvalidValue;
-        const uint32_t bytes = A_BYTES + (a[i].b.along_k ? cols / CTAS * 128 : (cols / CTAS + 63) / 64 * BLOCK_BYTES);
+        const uint32_t bytes = A_BYTES + (FEW || a[i].b.along_k ? cols / CTAS * 128 : (cols / CTAS + 63) / 64 * BLOCK_BYTES);
         work.a[i] = a[i];
-        work.t[i] = Tiling{uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(tiles_m * tiles_n), uint32_t(all), int(steps), int((steps + parts - 1) / parts), cols, bytes, uint32_t(ways[i].share), blocks_of_shares};
-        if (!PAIR && work.cluster > 1) {
-            if (all * ways[i].share > 1 << 20) return cudaErrorInvalidValue;
-            blocks_of_shares += (uint32_t(all) * ways[i].share + work.cluster - 1) / work.cluster * work.cluster;
+        work.t[i] = Tiling{uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(tiles_m * tiles_n), uint32_t(all), int(steps), int((steps + parts - 1) / parts), cols, bytes, uint32_t(a[i].way.share), blocks_of_shares};
+        if (!PAIR && KIND == PRODUCT_OUT && (FEW || work.cluster > 1)) {
+            if (all * a[i].way.share > 1 << 20) return cudaErrorInvalidValue;
+            blocks_of_shares += (uint32_t(all) * a[i].way.share + work.cluster - 1) / work.cluster * work.cluster;
         }
         work.all += uint32_t(all);
-        joined = joined || ways[i].splits > 1;
+        joined = joined || a[i].way.splits > 1;
     }
-    for (int i = n; i < 2; ++i) { maps.a[i] = maps.a[0]; maps.b[i] = maps.b[0]; work.a[i].splits = 1; work.t[i].first = 0xffffffffu; }
-    const auto kernel = product_kernel<T, KIND, ACT, PAIR>;
+    for (int i = n; i < 2; ++i) { maps.a[i] = maps.a[0]; maps.b[i] = maps.b[0]; work.a[i].way.splits = 1; work.t[i].first = 0xffffffffu; }
+    const auto kernel = product_kernel<T, KIND, ACT, SHAPE>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED);
     if (e != cudaSuccess) return e;
     const int64_t most = num_sms / CTAS;
@@ -565,31 +613,36 @@ template <typename T, ProductKind KIND, int ACT, bool PAIR> cudaError_t launch(P
     int64_t blocks = 1;
     for (int i = 0; i < n; ++i) {
         const int64_t b = (a[i].m * ((a[i].n + 7) / 8) + 255) / 256;
-        if (a[i].splits > 1 && b > blocks) blocks = b;
+        if (a[i].way.splits > 1 && b > blocks) blocks = b;
     }
     const int64_t places = int64_t(num_sms) * 8;
     return launch_chained(join_kernel<T, ACT>, dim3(unsigned(blocks < places ? blocks : places), n), dim3(256), 0, 1, st, work);
 }
 
-template <typename T, ProductKind KIND, int ACT> cudaError_t launch(ProductArgs *a, const Way *ways, int n, int num_sms, cudaStream_t st)
+template <typename T, ProductKind KIND, int ACT> cudaError_t launch(ProductArgs *a, int n, int num_sms, cudaStream_t st)
 {
-    return ways[0].pair ? launch<T, KIND, ACT, true>(a, ways, n, num_sms, st) : launch<T, KIND, ACT, false>(a, ways, n, num_sms, st);
+    switch (a[0].way.shape) {
+    case SHAPE_PAIR: return launch<T, KIND, ACT, SHAPE_PAIR>(a, n, num_sms, st);
+    case SHAPE_FEW: return launch<T, KIND, ACT, SHAPE_FEW>(a, n, num_sms, st);
+    case SHAPE_SINGLE: break;
+    }
+    return launch<T, KIND, ACT, SHAPE_SINGLE>(a, n, num_sms, st);
 }
 
-template <typename T> cudaError_t product(ProductKind kind, ProductArgs *a, const Way *ways, int n, int num_sms, cudaStream_t st)
+template <typename T> cudaError_t product(ProductKind kind, ProductArgs *a, int n, int num_sms, cudaStream_t st)
 {
     switch (kind) {
-    case PRODUCT_STATS: return launch<T, PRODUCT_STATS, RUBICK_ACT_NONE>(a, ways, n, num_sms, st);
-    case PRODUCT_GRAD: return launch<T, PRODUCT_GRAD, RUBICK_ACT_NONE>(a, ways, n, num_sms, st);
+    case PRODUCT_STATS: return launch<T, PRODUCT_STATS, RUBICK_ACT_NONE>(a, n, num_sms, st);
+    case PRODUCT_GRAD: return launch<T, PRODUCT_GRAD, RUBICK_ACT_NONE>(a, n, num_sms, st);
     case PRODUCT_OUT: break;
     }
     switch (a[0].act) {
-    case RUBICK_ACT_RELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_RELU>(a, ways, n, num_sms, st);
-    case RUBICK_ACT_GELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU>(a, ways, n, num_sms, st);
-    case RUBICK_ACT_GELU_TANH: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU_TANH>(a, ways, n, num_sms, st);
-    case RUBICK_ACT_SILU: return launch<T, PRODUCT_OUT, RUBICK_ACT_SILU>(a, ways, n, num_sms, st);
+    case RUBICK_ACT_RELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_RELU>(a, n, num_sms, st);
+    case RUBICK_ACT_GELU: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU>(a, n, num_sms, st);
+    case RUBICK_ACT_GELU_TANH: return launch<T, PRODUCT_OUT, RUBICK_ACT_GELU_TANH>(a, n, num_sms, st);
+    case RUBICK_ACT_SILU: return launch<T, PRODUCT_OUT, RUBICK_ACT_SILU>(a, n, num_sms, st);
     }
-    return launch<T, PRODUCT_OUT, RUBICK_ACT_NONE>(a, ways, n, num_sms, st);
+    return launch<T, PRODUCT_OUT, RUBICK_ACT_NONE>(a, n, num_sms, st);
 }
 
 }  // namespace
@@ -598,17 +651,22 @@ size_t plan_products(ProductKind kind, ProductArgs *a, int n, int num_sms)
 {
     size_t floats = 0;
     for (int i = 0; i < n; ++i) {
-        a[i].splits = way_of(kind, a[i], num_sms).splits;
-        if (a[i].splits > 1) {
+        a[i].way = way_of(kind, a[i], num_sms);
+        if (a[i].way.splits > 1) {
             if (!a[i].ld_acc) a[i].ld_acc = (a[i].n + 7) & ~int64_t(7);
             a[i].part_at = floats;
-            floats += size_t(a[i].splits) * a[i].m * a[i].ld_acc;
+            floats += size_t(a[i].way.splits) * a[i].m * a[i].ld_acc;
         }
     }
     return floats;
 }
 
-int product_stats_cols(const ProductArgs &a, int num_sms) { return way_of(PRODUCT_STATS, a, num_sms).cols / 2; }
+int64_t product_stats_pairs(const ProductArgs &a, int num_sms)
+{
+    const ProductWay w = way_of(PRODUCT_STATS, a, num_sms);
+    if (w.shape == SHAPE_FEW) return w.blocks < num_sms ? w.blocks : num_sms;
+    return (a.n + w.cols / 2 - 1) / (w.cols / 2);
+}
 
 bool product_takes(const Operand &o) { return aligned16(o.p) && (o.ld & 7) == 0; }
 
@@ -633,16 +691,16 @@ cudaError_t launch_products(ProductKind kind, ProductArgs *a, int n, float *part
     // A product is cut by its own sizes, so that it is the same bits alone or with another.  Two share a launch where both are cut
     // into the same kind of tiles and every block of theirs has a place at once; larger ones keep each other's operands out of
     // L2 (4,096 x 2,048 -> 8,192, both gradients: 242 us together, 214 one after the other).
-    Way ways[2];
-    for (int i = 0; i < n; ++i) { ways[i] = way_of(kind, a[i], num_sms); a[i].part = part + a[i].part_at; }
+    for (int i = 0; i < n; ++i) a[i].part = part + a[i].part_at;
     bool together = n == 1;
-    if (n == 2 && ways[0].pair == ways[1].pair) {
-        const int share = ways[0].share > ways[1].share ? ways[0].share : ways[1].share;
-        const int64_t blocks = (ways[0].blocks + share - 1) / share + (ways[1].blocks + share - 1) / share;
+    if (n == 2 && a[0].way.shape == a[1].way.shape) {
+        const ProductWay &x = a[0].way, &y = a[1].way;
+        const int share = x.share > y.share ? x.share : y.share;
+        const int64_t blocks = (x.blocks + share - 1) / share + (y.blocks + share - 1) / share;
         together = blocks <= (share > 1 ? resident_clusters(share) : num_sms);
     }
     for (int i = 0; i < n; i += together ? n : 1) {
-        const cudaError_t e = a[0].dtype == RUBICK_BF16 ? product<bf16>(kind, a + i, ways + i, together ? n : 1, num_sms, st) : product<f16>(kind, a + i, ways + i, together ? n : 1, num_sms, st);
+        const cudaError_t e = a[0].dtype == RUBICK_BF16 ? product<bf16>(kind, a + i, together ? n : 1, num_sms, st) : product<f16>(kind, a + i, together ? n : 1, num_sms, st);
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;

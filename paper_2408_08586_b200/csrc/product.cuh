@@ -13,6 +13,10 @@ struct DropArgs { const uint64_t *seed; uint32_t below; float scale; };     // k
 
 enum ProductKind { PRODUCT_OUT, PRODUCT_STATS, PRODUCT_GRAD };
 
+// How a product is cut: into which tiles, how many blocks of a cluster share one's k, into how many parts the k are dealt out
+// besides.
+struct ProductWay { int shape, cols, share, splits; float cost; int64_t blocks; };
+
 struct ProductArgs {
     int64_t m, n, k;
     Operand a, b;
@@ -26,14 +30,15 @@ struct ProductArgs {
     DropArgs drop;
     const float *scale;                  // one float in device memory, or NULL
     const float *acc_in; float *acc_out; // single-precision sums of earlier pieces, and of this and the earlier ones
-    // with splits > 1 the k are dealt out, and the sums of each lie in part[split][m][ld_acc] until they are joined
+    // with way.splits > 1 the sums of each part of the k lie in part[split][m][ld_acc] until they are joined
     float *part;
     size_t part_at;                      // where they begin in the launch's scratch, in floats
-    int splits;
+    ProductWay way;
+    bool beside;                         // one of the two gradients of a product
     // PRODUCT_STATS, PRODUCT_GRAD: the logits of vocabulary first .. first + n - 1
     const int32_t *label;
     int32_t first, vocab;
-    float2 *stats;                       // [ceil(n / product_stats_cols)][m]
+    float2 *stats;                       // [product_stats_pairs][m]: maximum, sum of exponentials
     float *at_label;                     // [m] logit of the label
     const float *base, *rest;            // log of the row's sum of exponentials, in two parts (rest may be NULL)
     const float *dloss, *up;             // [m] weight of a row (NULL: 1), and the common power of two
@@ -87,11 +92,11 @@ struct LayOutArgs {
     int n;
 };
 
-// Up to two products of one launch (two only for PRODUCT_OUT without activations): how they are cut, and the floats of
-// scratch that this takes.
+// Up to two products of one launch (two only for PRODUCT_OUT without activations): how they are cut, which goes by their sizes
+// and by how their operands lie (along_k has to be there already), and the floats of scratch that this takes.
 size_t plan_products(ProductKind kind, ProductArgs *a, int n, int num_sms);
 cudaError_t launch_products(ProductKind kind, ProductArgs *a, int n, float *part, int num_sms, cudaStream_t st);
-int product_stats_cols(const ProductArgs &a, int num_sms);       // columns of the logits that one pair (maximum, sum) covers
+int64_t product_stats_pairs(const ProductArgs &a, int num_sms);      // pairs (maximum, sum) of a row that the logits come in
 bool product_takes(const Operand &o);                            // as it lies, that is
 cudaError_t launch_lay_out(const LayOutArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_dropout(const DropoutArgs &a, int num_sms, cudaStream_t st);

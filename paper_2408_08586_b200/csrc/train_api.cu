@@ -204,10 +204,10 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     ProductArgs z = {};
     z.m = d.rows; z.n = d.vocab; z.k = d.hidden; z.dtype = d.dtype; z.status = ctx->d_status;
     z.label = d_label; z.vocab = d.vocab;
-    const int unit = product_stats_cols(z, ctx->num_sms);
-    const int64_t tiles = (int64_t(d.vocab) + unit - 1) / unit;
     Operand weight = {d_w, d.ld_w, by_output};
     const Laid laid = plan_operand(parts, weight, by_output ? d.vocab : d.hidden, by_output ? d.hidden : d.vocab);
+    z.a.along_k = 1; z.b.along_k = by_output;
+    const int64_t tiles = forward ? product_stats_pairs(z, ctx->num_sms) : 0;
     // the gradient of w sums over the rows, so that those without a label have to be zeros; elsewhere h is read as it lies
     const bool copied = backward && d_dw;
     Operand hidden = {d_h, d.ld_h, 1};
@@ -230,6 +230,8 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
         h.dtype = w.dtype = d.dtype;
         h.status = w.status = ctx->d_status;
         h.m = d.rows; h.n = d.hidden; h.k = n;
+        h.a.along_k = 1;
+        h.beside = w.beside = true;
         h.ld_out = d.ld_h; h.ld_acc = ld_copy;
         h.b = Operand{static_cast<const char *>(weight.p) + (by_output ? first * weight.ld : first) * 2, weight.ld, !by_output};
         h.out = d_dh;
@@ -267,6 +269,7 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     if (forward) {
         z.b = weight;
         z.stats = part<float2>(ctx, at_stats); z.at_label = part<float>(ctx, at_label);
+        plan_products(PRODUCT_STATS, &z, 1, ctx->num_sms);
         CUDA_TRY(ctx, launch_products(PRODUCT_STATS, &z, 1, nullptr, ctx->num_sms, ctx->stream), "launch product (logits)");
         HeadFinishArgs f = {};
         f.rows = d.rows; f.vocab = d.vocab; f.tiles = int(tiles);
@@ -285,6 +288,7 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
         z.n = n; z.first = int32_t(first);
         z.b = Operand{h.b.p, weight.ld, by_output};
         z.out = part<void>(ctx, at_dz); z.ld_out = ld_dz;
+        plan_products(PRODUCT_GRAD, &z, 1, ctx->num_sms);
         CUDA_TRY(ctx, launch_products(PRODUCT_GRAD, &z, 1, nullptr, ctx->num_sms, ctx->stream), "launch product (logits' gradient)");
         h.scale = w.scale = pre.scale;
         h.a = Operand{z.out, ld_dz, 1};
@@ -573,6 +577,8 @@ int rubick_linear_backward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, co
     dx.dtype = dw.dtype = d.dtype;
     dx.status = dw.status = ctx->d_status;
     dx.m = d.rows; dx.n = d.inputs; dx.k = d.outputs;
+    dx.a.along_k = 1;
+    dx.beside = dw.beside = true;
     dx.out = d_dx; dx.ld_out = d.ld_x; dx.wide = wide16(d_dx, d.ld_x) ? WIDE_OUT : 0;
     dx.b = Operand{d_w, d.ld_w, !by_output};
     dw.m = by_output ? d.outputs : d.inputs; dw.n = by_output ? d.inputs : d.outputs; dw.k = d.rows;
