@@ -106,7 +106,62 @@ __global__ void __launch_bounds__(32 * FINISH_WARPS) head_finish_kernel(const __
     if (a.base) { a.base[row] = live ? top : 0.f; a.rest[row] = live ? rest : 0.f; }
 }
 
+// dz = w (exp(z - lse) - onehot) from exp(z - top) of the row's pieces, 16 bytes a lane and four at a time: every piece has one
+// factor.  The label's entry is taken from its logit instead, which leaves 1 - p as exact as the logit is.
+template <typename T> __global__ void __launch_bounds__(256) head_scale_kernel(const __grid_constant__ HeadScaleArgs a)
+{
+    chain_go();
+    chain_wait();
+    constexpr int AHEAD = 4, SEGMENT = 32 * 8 * AHEAD;
+    const int lane = threadIdx.x & 31;
+    const int64_t segments = (a.ld + SEGMENT - 1) / SEGMENT, all = a.rows * segments, step = int64_t(gridDim.x) * 8;
+    const float up = *a.up;
+    for (int64_t i = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); i < all; i += step) {
+        const int64_t row = i / segments, c = (i - row * segments) * SEGMENT + lane * 8;
+        const int label = a.label[row];
+        const bool live = takes_part(label, a.vocab);
+        T *const at = static_cast<T *>(a.dz) + row * a.ld + c;
+        uint4 p[AHEAD];
+        float2 pair[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (live && c + j * 256 < a.ld) {
+                p[j] = *reinterpret_cast<const uint4 *>(at + j * 256);
+                const int64_t unit = (c + j * 256) / a.unit;
+                pair[j] = c + j * 256 < a.vocab ? a.stats[unit * a.rows + row] : make_float2(0.f, 0.f);
+            }
+        const float base = live ? a.base[row] : 0.f, rest = live ? a.rest[row] : 0.f, w = live ? (a.dloss ? a.dloss[row] : 1.f) * up : 0.f;
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            if (c + j * 256 >= a.ld) continue;
+            uint4 out = {};
+            if (live) {
+                float v[8];
+                unpack16<T>(p[j], v);
+                // (a pair without logits above -inf has kept zeros)
+                const float f = pair[j].x == __uint_as_float(0xff800000u) ? 0.f : w * ex2(((pair[j].x - base) - rest) * LOG2E) * (1.f / KEPT);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= f;
+                const int64_t l = label - (c + j * 256);
+                if (l >= 0 && l < 8) {
+                    const float y = w * ex2(((a.at_label[row] - base) - rest) * LOG2E) - w;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) if (e == l) v[e] = y;
+                }
+                out = pack16<T>(v);
+            }
+            *reinterpret_cast<uint4 *>(at + j * 256) = out;
+        }
+    }
+}
+
 }  // namespace
+
+cudaError_t launch_head_scale(const HeadScaleArgs &a, int num_sms, cudaStream_t st)
+{
+    const int64_t warps = a.rows * ((a.ld + 1023) / 1024), blocks = (warps + 7) / 8, most = int64_t(num_sms) * 8;
+    return launch_chained(a.dtype == RUBICK_BF16 ? head_scale_kernel<train::bf16> : head_scale_kernel<train::f16>, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), 0, 1, st, a);
+}
 
 cudaError_t launch_head_prep(const HeadPrepArgs &a, int num_sms, cudaStream_t st)
 {

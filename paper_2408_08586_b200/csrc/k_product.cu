@@ -54,6 +54,39 @@ __device__ __forceinline__ void place(const Tiling &t, uint32_t i, int &m, int &
 
 __device__ __forceinline__ float ninf() { return __uint_as_float(0xff800000u); }
 
+// 32 x 32 numbers of a warp, a lane a column, become a lane a row.
+__device__ __forceinline__ void exchange(uint8_t *mine, int lane, float (&v)[32])
+{
+#pragma unroll
+    for (int e = 0; e < 32; ++e) *reinterpret_cast<float *>(mine + e * 128 + (((lane >> 2) ^ (e & 7)) << 4) + (lane & 3) * 4) = v[e];
+    __syncwarp();
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        const float4 x = *reinterpret_cast<const float4 *>(mine + lane * 128 + ((p ^ (lane & 7)) << 4));
+        v[4 * p] = x.x; v[4 * p + 1] = x.y; v[4 * p + 2] = x.z; v[4 * p + 3] = x.w;
+    }
+    __syncwarp();
+}
+// 32 rows of 128 bytes, 16-byte pieces exchanged by the row, to rows of 16-byte boundaries: whole lines at a time.
+template <typename T> __device__ __forceinline__ void write_lines(const uint8_t *mine, int lane, T *to, int64_t m0, int64_t rows, int64_t ld, int64_t left)
+{
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const int line = r * 4 + (lane >> 3), q = lane & 7;
+        const uint4 p = *reinterpret_cast<const uint4 *>(mine + line * 128 + ((q ^ (line & 7)) << 4));
+        if (m0 + line < rows && q * 8 < left) *reinterpret_cast<uint4 *>(to + (m0 + line) * ld + q * 8) = p;
+    }
+}
+
+// Sums in tensor memory are cut off, not rounded, whenever 16 products join them, always towards zero: over 4,096 k that
+// takes 2e-6 of a logit.  The loss is a difference of logits in single precision, so its logits are summed up in parts of
+// SUM_STEPS x 64 k, which the reading warps add in registers (log-sums off by 1.3e-6 become SUM_ERROR); gradients and layers,
+// which are rounded to 16 bits, take their sums as they are.
+constexpr int SUM_STEPS = 8;
+// The reading warps of a pair need 128 registers for that, so they take some of the others': 64 x 128 + 216 x 256 threads' are
+// less than the 168 x 384 the block has (checked before a launch).
+constexpr int OTHERS_REGISTERS = 64, READERS_REGISTERS = 216;
+
 template <typename T, ProductKind KIND, int ACT, Shape SHAPE>
 __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_constant__ Maps maps, const __grid_constant__ Work work)
 {
@@ -95,8 +128,9 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
     const uint32_t end = shared_tiles && !mine_is ? work.t[0].all : work.all;     // (blocks that fill a cluster up have no tile)
     chain_wait();
 
-    if (warp == 0) {
-        if (lane == 0) {
+    if (warp < FIRST_READER) {
+        if constexpr (KIND == PRODUCT_STATS && PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHERS_REGISTERS));
+        if (warp == 0 && lane == 0) {
             uint32_t round = 0, i = first;           // stages filled so far, tile
             bool fine = true;
             const uint32_t bar0 = PAIR ? at_rank(full, 0) : full;
@@ -137,9 +171,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 for (uint32_t r = round > STAGES ? round - STAGES : 0; r < round; ++r) barrier_wait(full + 8 * (r % STAGES), r / STAGES & 1, &never);
             }
         }
-        __syncwarp();
-    } else if (warp == 1) {
-        if (lane == 0 && (!PAIR || rank == 0)) {
+        if (warp == 1 && lane == 0 && (!PAIR || rank == 0)) {
             uint32_t round = 0, tile = 0, i = first;
             bool fine = true;
             auto sum = [&](auto number) {
@@ -150,21 +182,24 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 const uint64_t da = operand_desc(stages, ak), db = operand_desc(stages + A_BYTES, bk);
                 const uint32_t sa = operand_step(ak), sb = operand_step(bk);
                 const uint32_t to = which ? end : end < work.t[0].all ? end : work.t[0].all;
-                for (; fine && i < to; i += step, ++tile) {
+                for (; fine && i < to; i += step) {
                     const int split = !PAIR ? int(rank) : t.all == t.each ? 0 : int((which ? i - work.t[0].all : i) / t.each);
                     const int k0 = split * t.per, k1 = k0 + t.per < t.steps ? k0 + t.per : t.steps;
-                    const uint32_t half = tile & 1, d = tmem + half * HALF;
-                    if (!(fine = barrier_wait(taken + 8 * half, (tile / 2 & 1) ^ 1, given_up))) break;
-                    tcgen_after_sync();
-                    for (int k = k0; k < k1; ++k, ++round) {
-                        const uint32_t s = round % STAGES, at = s * (STAGE >> 4);
-                        if (!(fine = barrier_wait(full + 8 * s, round / STAGES & 1, given_up))) break;
+                    for (int k = k0; fine && k < k1; ++tile) {
+                        const int stop = KIND == PRODUCT_STATS && k + SUM_STEPS < k1 ? k + SUM_STEPS : k1;
+                        const uint32_t half = tile & 1, d = tmem + half * HALF;
+                        if (!(fine = barrier_wait(taken + 8 * half, (tile / 2 & 1) ^ 1, given_up))) break;
                         tcgen_after_sync();
+                        for (bool add = false; k < stop; ++k, ++round) {
+                            const uint32_t s = round % STAGES, at = s * (STAGE >> 4);
+                            if (!(fine = barrier_wait(full + 8 * s, round / STAGES & 1, given_up))) break;
+                            tcgen_after_sync();
 #pragma unroll
-                        for (int q = 0; q < BK / 16; ++q) multiply<PAIR>(d, da + at + q * sa, db + at + q * sb, desc, k > k0 || q > 0);
-                        multiplied<PAIR>(empty + 8 * s);
+                            for (int q = 0; q < BK / 16; ++q, add = true) multiply<PAIR>(d, da + at + q * sa, db + at + q * sb, desc, add);
+                            multiplied<PAIR>(empty + 8 * s);
+                        }
+                        if (fine) multiplied<PAIR>(done + 8 * half);
                     }
-                    if (fine) multiplied<PAIR>(done + 8 * half);
                 }
             };
             sum(std::integral_constant<int, 0>());
@@ -175,7 +210,8 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             }
         }
         __syncwarp();
-    } else if (warp >= FIRST_READER) {
+    } else {
+        if constexpr (KIND == PRODUCT_STATS && PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(READERS_REGISTERS));
         const int quarter = warp & 3, side = (warp - FIRST_READER) >> 2;       // 32 rows, half of the columns
         uint8_t *const mine = shared + STAGES * STAGE + (warp - FIRST_READER) * 4096;
         constexpr bool TWO = KIND == PRODUCT_OUT && ACT == RUBICK_ACT_NONE;      // products there may be
@@ -183,7 +219,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
         Finish<T, ACT> finish(work.a[which]);
         uint32_t tile = 0;
         float running_top = ninf(), running_sum = 0.f;             // few rows: of all of the block's tiles
-        for (uint32_t i = first; i < end; i += step, ++tile) {
+        for (uint32_t i = first; i < end; i += step) {
             if (TWO && !which && i >= work.t[0].all) {
                 which = 1;
                 finish = Finish<T, ACT>(work.a[1]);
@@ -197,25 +233,93 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             const int width = KIND == PRODUCT_OUT ? t.cols / 2 : int(HALF) / 2;      // (only sums may be cut otherwise)
             const int64_t m0 = FEW ? side * 32 : (int64_t(tm) * CTAS + (PAIR ? rank : 0)) * BM + quarter * 32;
             const int64_t n0 = FEW ? int64_t(tn) * BM + quarter * 32 : int64_t(tn) * t.cols + side * width;
+            if constexpr (KIND == PRODUCT_STATS) {
+                // A thread has a row: its columns' logits, summed up a part of the k at a time, then their maximum and the sum of
+                // their exponentials.
+                constexpr int W = FEW ? 32 : int(HALF) / 2;
+                float v[W];
+#pragma unroll
+                for (int e = 0; e < W; ++e) v[e] = 0.f;
+                bool gone = false;
+#pragma unroll 1
+                for (int k = 0; k < t.steps && !gone; k += SUM_STEPS, ++tile) {
+                    const uint32_t now = tile & 1;
+                    if (!barrier_wait(done + 8 * now, tile / 2 & 1, given_up)) { gone = true; break; }
+                    __syncwarp();
+                    tcgen_after_sync();
+                    if (!FEW || m0 < rows) {
+                        const uint32_t at = tmem + now * HALF + side * W + (uint32_t(quarter * 32) << 16);
+#pragma unroll
+                        for (int c = 0; c < W; c += 32) {
+                            float x[32];
+                            tmem_load32(at + c, x);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) v[c + e] += x[e];
+                        }
+                    }
+                    tcgen_before_sync();
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive_at(PAIR ? at_rank(taken + 8 * now, 0) : taken + 8 * now);
+                }
+                if (gone) break;
+                if (FEW && m0 >= rows) continue;                   // (no rows for this half of the warps)
+                if constexpr (FEW) exchange(mine, lane, v);
+                const int64_t row = m0 + lane, left = cols - n0;
+                const int64_t label = row < rows ? int64_t(a.label[row]) - a.first - n0 : -1;
+                if (left < W) {
+#pragma unroll
+                    for (int e = 0; e < W; ++e) if (e >= left) v[e] = ninf();
+                }
+#pragma unroll
+                for (int c = 0; c < W; c += 32)
+                    if (__any_sync(0xffffffffu, label >= c && label < c + 32 && label < left)) {
+#pragma unroll
+                        for (int e = c; e < c + 32; ++e) if (label == e && e < left) a.at_label[row] = v[e];
+                    }
+                float top = FEW ? running_top : ninf(), s[4] = {};
+#pragma unroll
+                for (int e = 0; e < W; ++e) top = fmaxf(top, v[e]);
+                const float from = top == ninf() ? 0.f : top;
+#pragma unroll
+                for (int c = 0; c < W; c += 64) {
+#pragma unroll
+                    for (int h = 0; h < (W < 64 ? 1 : 2); ++h) {
+#pragma unroll
+                        for (int e = c + 32 * h; e < c + 32 * h + 32; ++e) { v[e] = ex2((v[e] - from) * LOG2E); s[e & 3] += v[e]; }
+                        if constexpr (!FEW) {
+                            if (finish.out) {
+#pragma unroll
+                                for (int q = 0; q < 4; ++q) {
+                                    const float *const x = v + c + 32 * h + 8 * q;
+                                    uint4 p;
+                                    p.x = pack_pair(KEPT * x[0], KEPT * x[1], T()); p.y = pack_pair(KEPT * x[2], KEPT * x[3], T());
+                                    p.z = pack_pair(KEPT * x[4], KEPT * x[5], T()); p.w = pack_pair(KEPT * x[6], KEPT * x[7], T());
+                                    *reinterpret_cast<uint4 *>(mine + lane * 128 + (((h * 4 + q) ^ (lane & 7)) << 4)) = p;
+                                }
+                            }
+                        }
+                    }
+                    if constexpr (!FEW) {
+                        if (finish.out) {
+                            __syncwarp();
+                            write_lines(mine, lane, finish.out + n0 + c, m0, rows, finish.ld_out, finish.ld_out - n0 - c);
+                            __syncwarp();
+                        }
+                    }
+                }
+                const float sum = (s[0] + s[1]) + (s[2] + s[3]);
+                if constexpr (FEW) {
+                    running_sum = fmaf(running_sum, ex2((running_top - from) * LOG2E), sum);
+                    running_top = top;
+                } else if (row < rows && n0 < cols) {
+                    a.stats[(int64_t(tn) * 2 + side) * rows + row] = make_float2(top, sum);
+                }
+                continue;
+            }
             if (!barrier_wait(done + 8 * half, tile / 2 & 1, given_up)) break;
             __syncwarp();
             tcgen_after_sync();
             const uint32_t at = tmem + half * HALF + side * (FEW ? 32 : width) + (uint32_t(quarter * 32) << 16);
-            // 32 columns of the warp's rows, a lane a row (few rows: a lane has a column, and they are exchanged)
-            auto load32 = [&](int c, float (&v)[32]) {
-                tmem_load32(at + c, v);
-                if constexpr (FEW) {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) *reinterpret_cast<float *>(mine + e * 128 + (((lane >> 2) ^ (e & 7)) << 4) + (lane & 3) * 4) = v[e];
-                    __syncwarp();
-#pragma unroll
-                    for (int p = 0; p < 8; ++p) {
-                        const float4 x = *reinterpret_cast<const float4 *>(mine + lane * 128 + ((p ^ (lane & 7)) << 4));
-                        v[4 * p] = x.x; v[4 * p + 1] = x.y; v[4 * p + 2] = x.z; v[4 * p + 3] = x.w;
-                    }
-                    __syncwarp();
-                }
-            };
             if (FEW && m0 >= rows) {
                 // (no rows for this half of the warps)
             } else if (KIND == PRODUCT_OUT && FEW) {
@@ -319,37 +423,6 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                     }
                     __syncwarp();
                 }
-            } else if constexpr (KIND == PRODUCT_STATS) {
-                // a thread has a row: running maximum and sum of exponentials over its columns
-                const int64_t row = m0 + lane;
-                const int64_t label = row < rows ? int64_t(a.label[row]) - a.first - n0 : -1;
-                float top = FEW ? running_top : ninf(), sum = FEW ? running_sum : 0.f;
-                for (int c = 0; c < (FEW ? 32 : width); c += 32) {
-                    float v[32];
-                    load32(c, v);
-                    const int64_t left = cols - (n0 + c);
-                    if (left <= 0) continue;
-                    if (left < 32) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) if (e >= left) v[e] = ninf();
-                    }
-                    if (__any_sync(0xffffffffu, label >= c && label < c + 32 && label < c + left)) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) if (label == c + e && e < left) a.at_label[row] = v[e];
-                    }
-                    float m = v[0];
-#pragma unroll
-                    for (int e = 1; e < 32; ++e) m = fmaxf(m, v[e]);
-                    m = fmaxf(m, top);
-                    const float from = m == ninf() ? 0.f : m;
-                    float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) { s0 += ex2((v[e] - from) * LOG2E); s1 += ex2((v[e + 1] - from) * LOG2E); }
-                    sum = sum * ex2((top - from) * LOG2E) + (s0 + s1);
-                    top = m;
-                }
-                if constexpr (FEW) { running_top = top; running_sum = sum; }
-                else if (row < rows && n0 < cols) a.stats[(int64_t(tn) * 2 + side) * rows + row] = make_float2(top, sum);
             } else {
                 // a thread has a row; 64 columns become 128 bytes of it, written line by line
                 const int64_t row = m0 + lane;
@@ -363,7 +436,8 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
 #pragma unroll
                     for (int h = 0; h < (FEW ? 1 : 2); ++h) {
                         float v[32];
-                        load32(c + 32 * h, v);
+                        tmem_load32(at + c + 32 * h, v);
+                        if constexpr (FEW) exchange(mine, lane, v);
                         const int here = c + 32 * h;
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = w * ex2(((v[e] - from) - rest) * LOG2E);
@@ -382,19 +456,14 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                     }
                     if constexpr (FEW) break;
                     __syncwarp();
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) {
-                        const int line = r * 4 + (lane >> 3), q = lane & 7;
-                        const uint4 p = *reinterpret_cast<const uint4 *>(mine + line * 128 + ((q ^ (line & 7)) << 4));
-                        const int64_t to = m0 + line, col = n0 + c + q * 8;
-                        if (to < rows && col < finish.ld_out) *reinterpret_cast<uint4 *>(finish.out + to * finish.ld_out + col) = p;
-                    }
+                    write_lines(mine, lane, finish.out + n0 + c, m0, rows, finish.ld_out, finish.ld_out - n0 - c);
                     __syncwarp();
                 }
             }
             tcgen_before_sync();
             __syncwarp();
             if (lane == 0) barrier_arrive_at(PAIR ? at_rank(taken + 8 * half, 0) : taken + 8 * half);
+            ++tile;
         }
         if constexpr (KIND == PRODUCT_STATS && FEW) *reinterpret_cast<float2 *>(mine + lane * 8) = make_float2(running_top, running_sum);
     }
@@ -606,6 +675,12 @@ template <typename T, ProductKind KIND, int ACT, Shape SHAPE> cudaError_t launch
     const auto kernel = product_kernel<T, KIND, ACT, SHAPE>;
     cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED);
     if (e != cudaSuccess) return e;
+    if constexpr (KIND == PRODUCT_STATS && PAIR) {
+        // a block that lacks the registers its warps ask for would wait for them for ever
+        cudaFuncAttributes has;
+        if ((e = cudaFuncGetAttributes(&has, kernel)) != cudaSuccess) return e;
+        if (has.numRegs * THREADS < OTHERS_REGISTERS * 128 + READERS_REGISTERS * 256) return cudaErrorInvalidConfiguration;
+    }
     const int64_t most = num_sms / CTAS;
     const unsigned grid = blocks_of_shares ? blocks_of_shares : unsigned((work.all < most ? work.all : most) * CTAS);
     e = launch_chained(kernel, dim3(grid), dim3(THREADS), SHARED, int(work.cluster), st, maps, work);
@@ -660,6 +735,8 @@ size_t plan_products(ProductKind kind, ProductArgs *a, int n, int num_sms)
     }
     return floats;
 }
+
+bool product_keeps(const ProductArgs &a, int num_sms) { return way_of(PRODUCT_STATS, a, num_sms).shape != SHAPE_FEW; }
 
 int64_t product_stats_pairs(const ProductArgs &a, int num_sms)
 {

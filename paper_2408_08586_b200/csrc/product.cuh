@@ -35,7 +35,8 @@ struct ProductArgs {
     size_t part_at;                      // where they begin in the launch's scratch, in floats
     ProductWay way;
     bool beside;                         // one of the two gradients of a product
-    // PRODUCT_STATS, PRODUCT_GRAD: the logits of vocabulary first .. first + n - 1
+    // PRODUCT_STATS, PRODUCT_GRAD: the logits of vocabulary first .. first + n - 1; with `out`, PRODUCT_STATS keeps there the
+    // exponentials of their distances to their pair's maximum, times KEPT
     const int32_t *label;
     int32_t first, vocab;
     float2 *stats;                       // [product_stats_pairs][m]: maximum, sum of exponentials
@@ -45,6 +46,8 @@ struct ProductArgs {
     uint32_t *status;
 };
 enum { WIDE_OUT = 1, WIDE_PRE = 2, WIDE_RES = 4, WIDE_BIAS = 8 };
+
+constexpr float KEPT = 16384.f;          // (so that half precision holds those of 2^-28 and more to 11 bits)
 
 struct DropoutArgs {
     rubick_dropout_desc d;
@@ -96,6 +99,7 @@ struct LayOutArgs {
 // and by how their operands lie (along_k has to be there already), and the floats of scratch that this takes.
 size_t plan_products(ProductKind kind, ProductArgs *a, int n, int num_sms);
 cudaError_t launch_products(ProductKind kind, ProductArgs *a, int n, float *part, int num_sms, cudaStream_t st);
+bool product_keeps(const ProductArgs &a, int num_sms);               // whether PRODUCT_STATS can keep the exponentials
 int64_t product_stats_pairs(const ProductArgs &a, int num_sms);      // pairs (maximum, sum) of a row that the logits come in
 bool product_takes(const Operand &o);                            // as it lies, that is
 cudaError_t launch_lay_out(const LayOutArgs &a, int num_sms, cudaStream_t st);
@@ -104,6 +108,16 @@ void plan_linear_grad(LinearGradArgs &a, int num_sms);
 cudaError_t launch_linear_grad(const LinearGradArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_head_prep(const HeadPrepArgs &a, int num_sms, cudaStream_t st);
 cudaError_t launch_head_finish(const HeadFinishArgs &a, int num_sms, cudaStream_t st);
+// kept exponentials become dz where they lie
+struct HeadScaleArgs {
+    int64_t rows, ld;
+    int vocab, dtype, unit;              // columns of a pair
+    const int32_t *label;
+    const float2 *stats;
+    const float *at_label, *base, *rest, *dloss, *up;
+    void *dz;
+};
+cudaError_t launch_head_scale(const HeadScaleArgs &a, int num_sms, cudaStream_t st);
 
 // A launch that may begin while the one before it in the stream ends: its kernel waits (chain_wait) before it touches memory.
 template <typename... P, typename... A> cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, const A &...args)

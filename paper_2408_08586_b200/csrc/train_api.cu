@@ -216,12 +216,15 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     const size_t at_stats = forward ? parts.take(size_t(tiles) * d.rows * sizeof(float2)) : 0, at_label = forward ? parts.take(size_t(d.rows) * 4) : 0;
     const size_t at_base = forward && backward ? parts.take(size_t(d.rows) * 4) : 0, at_rest = forward && backward ? parts.take(size_t(d.rows) * 4) : 0;
     const size_t at_scale = backward ? parts.take(8) : 0;
-    // the vocabulary of a piece: as much as 256 MB of dz take, in whole tiles
-    int64_t piece = (int64_t(256) << 20) / (2 * d.rows) / 256 * 256;
+    // the vocabulary of a piece: as much as 512 MB of dz take, in whole tiles
+    int64_t piece = (int64_t(512) << 20) / (2 * d.rows) / 256 * 256;
     if (piece < 256) piece = 256;
     if (piece > d.vocab) piece = d.vocab;
     const int64_t ld_dz = up8(piece);
     const bool several = piece < d.vocab;
+    // Where dz is one piece, a step writes the exponentials that it sums up to dz's place and makes dz of them there, instead of
+    // working the logits out again: three products, not four (2,048 x 4,096 x 128,000 bf16 KEPT_BOTH_SIDES).
+    const bool kept = forward && backward && !several && product_keeps(z, ctx->num_sms);
     const size_t at_dz = backward ? parts.take(size_t(d.rows) * ld_dz * 2) : 0;
     const size_t at_acc = backward && several && d_dh ? parts.take(size_t(d.rows) * ld_copy * 4) : 0;
     size_t sums = 0;
@@ -269,6 +272,7 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     if (forward) {
         z.b = weight;
         z.stats = part<float2>(ctx, at_stats); z.at_label = part<float>(ctx, at_label);
+        if (kept) { z.out = part<void>(ctx, at_dz); z.ld_out = ld_dz; }
         plan_products(PRODUCT_STATS, &z, 1, ctx->num_sms);
         CUDA_TRY(ctx, launch_products(PRODUCT_STATS, &z, 1, nullptr, ctx->num_sms, ctx->stream), "launch product (logits)");
         HeadFinishArgs f = {};
@@ -288,8 +292,15 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
         z.n = n; z.first = int32_t(first);
         z.b = Operand{h.b.p, weight.ld, by_output};
         z.out = part<void>(ctx, at_dz); z.ld_out = ld_dz;
-        plan_products(PRODUCT_GRAD, &z, 1, ctx->num_sms);
-        CUDA_TRY(ctx, launch_products(PRODUCT_GRAD, &z, 1, nullptr, ctx->num_sms, ctx->stream), "launch product (logits' gradient)");
+        if (kept) {
+            HeadScaleArgs k = {};
+            k.rows = d.rows; k.ld = ld_dz; k.vocab = d.vocab; k.dtype = d.dtype; k.unit = z.way.cols / 2;
+            k.label = d_label; k.stats = z.stats; k.at_label = z.at_label; k.base = z.base; k.rest = z.rest; k.dloss = d_dloss; k.up = z.up; k.dz = z.out;
+            CUDA_TRY(ctx, launch_head_scale(k, ctx->num_sms, ctx->stream), "launch head_scale");
+        } else {
+            plan_products(PRODUCT_GRAD, &z, 1, ctx->num_sms);
+            CUDA_TRY(ctx, launch_products(PRODUCT_GRAD, &z, 1, nullptr, ctx->num_sms, ctx->stream), "launch product (logits' gradient)");
+        }
         h.scale = w.scale = pre.scale;
         h.a = Operand{z.out, ld_dz, 1};
         const Operand dz = {z.out, ld_dz, 0}, copy = {pre.copy, ld_copy, 0};
