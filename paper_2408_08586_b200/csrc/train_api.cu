@@ -223,8 +223,10 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     const int64_t ld_dz = up8(piece);
     const bool several = piece < d.vocab;
     // Where dz is one piece, a step writes the exponentials that it sums up to dz's place and makes dz of them there, instead of
-    // working the logits out again: three products, not four (2,048 x 4,096 x 128,000 bf16 KEPT_BOTH_SIDES).
-    const bool kept = forward && backward && !several && product_keeps(z, ctx->num_sms);
+    // working the logits out again: three products, not four (2,048 x 4,096 x 128,000 bf16 5.3 ms, 7.0 with four).  It pays
+    // where a product costs more than reading and writing dz once: from 640 features on (4,096 x 32,000: 768 features 642 us,
+    // 664 with four; 512: 490 and 471), or where dz stays in L2 (1,024 x 256 x 16,000 89 us, 98; 512 x 256 x 50,000 151, 147).
+    const bool kept = forward && backward && !several && (d.hidden >= 640 || d.rows * ld_dz * 2 <= 40 << 20) && product_keeps(z, ctx->num_sms);
     const size_t at_dz = backward ? parts.take(size_t(d.rows) * ld_dz * 2) : 0;
     const size_t at_acc = backward && several && d_dh ? parts.take(size_t(d.rows) * ld_copy * 4) : 0;
     size_t sums = 0;

@@ -11,6 +11,11 @@ measure() scales such layers up.  A job's own tau and k_bwd come from a profile 
 from rubick_fit_models.
 
     x0 -> norm -> block -> [norm, gate, + alpha, norm] -> router -> experts -> [norm, gate, + alpha, norm] -> head -> loss
+
+DenseStep is the step of a model without experts that learns from labels, with its products, its dropout and its head's
+cross entropy by the library too:
+
+    x0 -> dropout -> [norm -> up, gelu -> down, dropout, +] -> norm -> head, cross entropy
 """
 import torch
 
@@ -136,6 +141,84 @@ class TrainingStep:
         return {**{name: g[name] for name in PARAMETERS}, "x": b["dx"]}
 
 
+DENSE_PARAMETERS = ("w_in", "w_up", "b_up", "w_down", "b_down", "w_out", "w_head")
+
+
+class DenseStep:
+    """Holds the parameters, the descriptors and the buffers of a step of `tokens` tokens in a 16-bit type.
+
+    inner: features between the block's products; drop: probability of both dropouts; tied: the head's weight has a row per
+    token of the vocabulary, as an embedding has.  The masks of a step come from self.seed, on the device: advance() draws new
+    ones for the next step, also inside of a captured graph."""
+
+    def __init__(self, ctx, tokens, hidden, vocab, *, inner=None, drop=0.1, tied=True, dtype=torch.bfloat16, seed=0, device="cuda:0"):
+        self.ctx, self.tokens, self.hidden, self.vocab, self.dtype = ctx, int(tokens), int(hidden), int(vocab), dtype
+        self.inner = 4 * self.hidden if inner is None else int(inner)
+        n, d, m, v = self.tokens, self.hidden, self.inner, self.vocab
+        g = torch.Generator(device=device).manual_seed(seed)
+        draw = lambda *shape, scale=1.0, shift=0.0: torch.randn(*shape, generator=g, device=device).mul_(scale).add_(shift).to(dtype)  # noqa: E731
+        self.p = dict(w_in=draw(d, scale=0.1, shift=1.0), w_up=draw(d, m, scale=d ** -0.5), b_up=draw(m, scale=0.1), w_down=draw(m, d, scale=m ** -0.5),
+                      b_down=draw(d, scale=0.1), w_out=draw(d, scale=0.1, shift=1.0),
+                      w_head=draw(v, d, scale=d ** -0.5) if tied else draw(d, v, scale=d ** -0.5))
+        self.enter = rb.dropout(n, d, dtype, p=drop)
+        self.norm = rb.block_norm(n, d, dtype, norm_after=False)
+        self.up = rb.linear(n, d, m, dtype, activation="gelu")
+        self.down = rb.linear(n, m, d, dtype, p=drop)
+        self.loss = rb.head_loss(n, d, v, dtype, by_output=tied)
+        self.seed = torch.tensor([[seed, 0], [seed, 1]], dtype=torch.int64, device=device)
+        rows = lambda *shape: torch.empty(*shape, dtype=dtype, device=device)  # noqa: E731
+        f32 = lambda *shape: torch.empty(*shape, dtype=torch.float32, device=device)  # noqa: E731
+        self.b = dict(x=rows(n, d), h0=rows(n, d), r0=f32(n, 2), pre=rows(n, m), a=rows(n, m), x1=rows(n, d), h1=rows(n, d), r1=f32(n, 2), nll=f32(n), lse=f32(n),
+                      dh=rows(n, d), dx=rows(n, d), da=rows(n, m))
+        self.g = {name: f32(d) if name in ("w_in", "w_out", "b_down") else f32(m) if name == "b_up" else torch.empty_like(self.p[name]) for name in DENSE_PARAMETERS}
+
+    def advance(self):
+        """Other masks from here on."""
+        self.seed[:, 1] += 2
+
+    def hidden_states(self, x):
+        """Everything before the head."""
+        c, p, b = self.ctx, self.p, self.b
+        c.dropout_forward(self.enter, self.seed[0], x, None, b["x"])
+        c.block_norm_forward(self.norm, b["x"], None, None, None, p["w_in"], None, b["h0"], b["r0"])
+        c.linear_forward(self.up, b["h0"], p["w_up"], p["b_up"], None, None, b["pre"], b["a"])
+        c.linear_forward(self.down, b["a"], p["w_down"], p["b_down"], b["x"], self.seed[1], None, b["x1"])
+        c.block_norm_forward(self.norm, b["x1"], None, None, None, p["w_out"], None, b["h1"], b["r1"])
+        return b["h1"]
+
+    def forward(self, x, label):
+        """-> cross entropy of every token; label: int32 [tokens], tokens with a negative label are left out."""
+        self.label = label
+        self.ctx.head_loss_forward(self.loss, self.hidden_states(x), self.p["w_head"], label, self.b["nll"], self.b["lse"])
+        return self.b["nll"]
+
+    def backward(self, token_weight=None):
+        """Gradients of sum(token_weight * cross entropy) -> {parameter: gradient}, and of x under "x"."""
+        self.ctx.head_loss_backward(self.loss, self.b["h1"], self.p["w_head"], self.label, self.b["lse"], token_weight, self.b["dh"], self.g["w_head"])
+        return self._backward_from_head()
+
+    def step(self, x, label, token_weight=None):
+        """Forward and backward pass with the head's loss and gradients in one call -> (losses, gradients)."""
+        self.ctx.head_loss_step(self.loss, self.hidden_states(x), self.p["w_head"], label, token_weight, self.b["nll"], None, self.b["dh"], self.g["w_head"])
+        return self.b["nll"], self._backward_from_head()
+
+    def _backward_from_head(self):
+        c, p, b, g = self.ctx, self.p, self.b, self.g
+        c.block_norm_backward(self.norm, b["x1"], None, None, None, p["w_out"], b["r1"], None, b["dh"], b["dx"], None, None, None, g["w_out"])
+        c.linear_backward(self.down, b["a"], p["w_down"], None, self.seed[1], b["dx"], b["da"], g["w_down"], g["b_down"])
+        c.linear_backward(self.up, b["h0"], p["w_up"], b["pre"], None, b["da"], b["dh"], g["w_up"], g["b_up"])
+        c.block_norm_backward(self.norm, b["x"], None, None, None, p["w_in"], b["r0"], b["dx"], b["dh"], b["dx"], None, None, None, g["w_in"])
+        c.dropout_backward(self.enter, self.seed[0], b["dx"], b["dx"])
+        return {**g, "x": b["dx"]}
+
+
+def draw_labels(step, seed=0):
+    """(x, labels) for a DenseStep: a random stream and random tokens."""
+    g = torch.Generator(device=step.p["w_in"].device).manual_seed(seed)
+    x = torch.randn(step.tokens, step.hidden, generator=g, device=step.p["w_in"].device).to(step.dtype)
+    return x, torch.randint(0, step.vocab, (step.tokens,), generator=g, device=x.device).to(torch.int32)
+
+
 def draw_batch(step, seed=0):
     """(x, teacher indices, teacher logits) for a step: a random residual stream, distinct entries, largest first."""
     g = torch.Generator(device=step.p["w_in"].device).manual_seed(seed)
@@ -148,9 +231,10 @@ def draw_batch(step, seed=0):
 
 
 def measure(step, layers, seq, repeats=10):
-    """Times a step on the GPU and scales it to a model of `layers` such layers and one head.
+    """Times a step (either kind) on the GPU and scales it to a model of `layers` such layers and one head.
     -> dict(tau, k_bwd): forward seconds per sample of `seq` tokens, backward / forward, as rubick_job takes them."""
-    x, index, teacher = draw_batch(step)
+    batch = draw_labels(step) if isinstance(step, DenseStep) else draw_batch(step)
+    x = batch[0]
     samples = step.tokens / seq
 
     def seconds(f):
@@ -166,8 +250,8 @@ def measure(step, layers, seq, repeats=10):
         return begin.elapsed_time(end) / 1e3 / repeats
 
     body = seconds(lambda: step.hidden_states(x))
-    forward = seconds(lambda: step.forward(x, index, teacher))
-    both = seconds(lambda: (step.forward(x, index, teacher), step.backward()))
+    forward = seconds(lambda: step.forward(*batch))
+    both = seconds(lambda: (step.forward(*batch), step.backward()))
     back = max(both - forward, 0.0)
     head_share = max(forward - body, 0.0) / forward
     whole = body * layers + max(forward - body, 0.0)
@@ -194,6 +278,8 @@ def main():
         jobs["w"][j] = np.float32(3.0 * got["tau"])
         print(f"hidden {hidden}, {layers} layers, {seq} tokens a sample: tau {got['tau'] * 1e3:.2f} ms, k_bwd {got['k_bwd']:.2f}")
         del step
+    dense = measure(DenseStep(ctx, 4 * 1024, 1280, 32000), 24, 1024)
+    print(f"without experts, from labels: hidden 1280, 24 layers, 1024 tokens a sample: tau {dense['tau'] * 1e3:.2f} ms, k_bwd {dense['k_bwd']:.2f}")
     n_nodes = 4
     d_out = torch.empty(3 * rb.ASSIGN_DTYPE.itemsize, dtype=torch.uint8, device="cuda:0")
     steps, _ = ctx.schedule_round(rb.to_device(rb.pack_jobs(jobs)), 3, n_nodes, 1 << 20, d_out)
