@@ -612,7 +612,8 @@ typedef struct {
  * d_bias and d_residual may be NULL; d_pre (optional) receives z for the backward pass (act is taken from z before it is
  * rounded).  d_seed is read where p > 0 and may be NULL otherwise.  d_out may equal d_residual.  Products are summed in
  * single precision.  Rows of x and w on 16-byte boundaries are read as they lie; others are laid out anew in the context's
- * scratch first.  Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
+ * scratch first, which also holds single-precision sums where the inputs are dealt out (up to 8 times rows x outputs).
+ * Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
 int rubick_linear_forward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, const void *d_x, const void *d_w,
                           const void *d_bias, const void *d_residual, const uint64_t *d_seed, void *d_pre, void *d_out);
 
@@ -657,7 +658,8 @@ typedef struct {
  * never in memory.
  *     d_lse[n] = log sum_v exp(z_nv)          d_loss[n] = lse - z_{n, label n}
  * Both are 0 for a row whose label (int32) is outside 0 .. vocab - 1 (padding), whatever its h holds.  d_lse is optional.
- * A row with a NaN or +inf logit gets NaN.  The context keeps 8 bytes per row and 128 tokens of the vocabulary.
+ * A row with a NaN or +inf logit gets NaN.  The context keeps 8 bytes per row and 64 tokens of the vocabulary, and copies of
+ * h and w where their rows are not on 16-byte boundaries.
  * Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
 int rubick_head_loss_forward(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,
                              const int32_t *d_label, float *d_loss, float *d_lse);
@@ -665,13 +667,15 @@ int rubick_head_loss_forward(rubick_ctx *ctx, const rubick_head_loss_desc *h_des
 /* dz = d_dloss[n] (exp(z - lse) - onehot(label)),  dh = dz W^T,  dw = h^T dz (laid out as w), with forward's d_lse; rows
  * without a label add nothing and get zeros.  d_dloss NULL = 1.  d_dh or d_dw may be NULL: it is not computed.  The logits
  * are computed again, a piece of the vocabulary at a time; dz of a piece is rounded to dtype under a common power of two.
- * The context keeps the piece (up to 256 MB, or 128 tokens), a copy of h and, with several pieces, dh in single precision.
+ * The context keeps the piece (up to 512 MB, or 256 tokens), a copy of h and, with several pieces, dh in single precision.
  * d_lse is one float: rows whose logits are all far from zero want the step below.  rows = 0 writes zeros to dw.
  * Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
 int rubick_head_loss_backward(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,
                               const int32_t *d_label, const float *d_lse, const float *d_dloss, void *d_dh, void *d_dw);
 
-/* Both at once, for a loss whose weight per row is known beforehand.  Outputs as theirs; d_lse is optional here too. */
+/* Both at once, for a loss whose weight per row is known beforehand.  Outputs as theirs; d_lse is optional here too.  Where the
+ * whole vocabulary is one piece, dz is made of the exponentials that the loss sums up (rounded to dtype once more) instead of
+ * the logits again, if that is quicker.  Errors: as theirs. */
 int rubick_head_loss_step(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,
                           const int32_t *d_label, const float *d_dloss, float *d_loss, float *d_lse, void *d_dh, void *d_dw);
 

@@ -10,7 +10,7 @@ using namespace train;
 // keeps to its columns and to what the generator needs of them.
 template <typename T, int LANES, bool RESIDUAL, bool WIDE> __global__ void __launch_bounds__(256, 3) dropout_kernel(const __grid_constant__ DropoutArgs a)
 {
-    constexpr int VE = Lanes<T>::N, ROWS = 2, STEP = 256 / LANES, ACROSS = LANES * VE;
+    constexpr int VE = Lanes<T>::N, ROWS = WIDE ? 2 : 1, STEP = 256 / LANES, ACROSS = LANES * VE;
     chain_go();
     chain_wait();
     __shared__ uint4 staged[WIDE ? 1 : 256];
@@ -23,13 +23,13 @@ template <typename T, int LANES, bool RESIDUAL, bool WIDE> __global__ void __lau
     const T *const x = static_cast<const T *>(a.x) + from * ld_x, *const residual = RESIDUAL ? static_cast<const T *>(a.residual) + from * ld_res : nullptr;
     T *const out = static_cast<T *>(a.out) + from * ld_out;
     const bool inside = c < cols;
-    uint4 p[ROWS], q[ROWS];
+    Pieces<WIDE> p[ROWS], q[ROWS];
     auto fetch = [&](int row) {
 #pragma unroll
         for (int i = 0; i < ROWS; ++i)
             if (row + i * STEP < high && inside) {
-                p[i] = load_raw(x + (row + i * STEP) * ld_x, c, cols, WIDE);
-                if constexpr (RESIDUAL) q[i] = load_raw(residual + (row + i * STEP) * ld_res, c, cols, WIDE);
+                p[i] = ask<WIDE>(x + (row + i * STEP) * ld_x, c, cols);
+                if constexpr (RESIDUAL) q[i] = ask<WIDE>(residual + (row + i * STEP) * ld_res, c, cols);
             }
     };
     int row = threadIdx.x / LANES;
@@ -40,7 +40,7 @@ template <typename T, int LANES, bool RESIDUAL, bool WIDE> __global__ void __lau
     const float scale = drop.scale;
     while (row - ahead < high) {
         // the next rows are asked for before these are worked on
-        uint4 mine[ROWS], other[ROWS];
+        Pieces<WIDE> mine[ROWS], other[ROWS];
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {
             mine[i] = p[i];
@@ -54,11 +54,11 @@ template <typename T, int LANES, bool RESIDUAL, bool WIDE> __global__ void __lau
             uint4 result = {};
             if (in) {
                 float v[VE];
-                unpack16<T>(mine[i], v);
+                unpack16<T>(take<WIDE>(x + here * ld_x, c, cols, mine[i]), v);
                 if (drop.on) columns.choose(uint32_t(from + here), v);
                 if constexpr (RESIDUAL) {
                     float r[VE];
-                    unpack16<T>(other[i], r);
+                    unpack16<T>(take<WIDE>(residual + here * ld_res, c, cols, other[i]), r);
 #pragma unroll
                     for (int e = 0; e < VE; ++e) v[e] = fmaf(v[e], scale, r[e]);
                 } else {
@@ -96,12 +96,12 @@ template <typename T, int LANES, bool RESIDUAL, bool WIDE> __global__ void __lau
 }
 
 constexpr int GRAD_WARPS = 8;
-constexpr int GRAD_ROWS = 2;             // rows that a thread has under way
 
 // dz = act'(pre) drop(dout), eight columns a thread, and the sums of its columns: a block takes a strip of columns of a run of
 // rows and leaves its sums; the strip's last block adds the runs' sums in their order.
-template <typename T, int ACT> __global__ void __launch_bounds__(256, 3) linear_grad_kernel(const __grid_constant__ LinearGradArgs a)
+template <typename T, int ACT, bool WIDE> __global__ void __launch_bounds__(256, 3) linear_grad_kernel(const __grid_constant__ LinearGradArgs a)
 {
+    constexpr int ROWS = WIDE ? 2 : 1;                 // rows that a thread has under way, and as many asked for
     __shared__ float sums[GRAD_WARPS][32][9];
     __shared__ bool last;
     chain_go();
@@ -111,17 +111,16 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256, 3) linear_
     const int64_t per = (a.rows + a.chunks - 1) / a.chunks, from = per * blockIdx.y, to = from + per < a.rows ? from + per : a.rows;
     const T *const dout = static_cast<const T *>(a.dout), *const pre = static_cast<const T *>(a.pre);
     T *const dz = static_cast<T *>(a.dz);
-    const bool wide = a.wide;
     const int64_t ld_dout = a.ld_dout, ld_pre = a.ld_pre, ld_dz = a.ld_dz, step = int64_t(GRAD_WARPS) * abreast;
     float total[8] = {};
     if (c < cols) {
-        uint4 p[GRAD_ROWS], q[GRAD_ROWS];
+        Pieces<WIDE> p[ROWS], q[ROWS];
         auto fetch = [&](int64_t row) {
 #pragma unroll
-            for (int i = 0; i < GRAD_ROWS; ++i)
+            for (int i = 0; i < ROWS; ++i)
                 if (row + i * step < to) {
-                    p[i] = load_raw(dout + (row + i * step) * ld_dout, c, cols, wide);
-                    if constexpr (ACT != RUBICK_ACT_NONE) q[i] = load_raw(pre + (row + i * step) * ld_pre, c, cols, wide);
+                    p[i] = ask<WIDE>(dout + (row + i * step) * ld_dout, c, cols);
+                    if constexpr (ACT != RUBICK_ACT_NONE) q[i] = ask<WIDE>(pre + (row + i * step) * ld_pre, c, cols);
                 }
         };
         int64_t row = from + warp * abreast + sub;
@@ -130,22 +129,22 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256, 3) linear_
         const DropColumns<8> columns(drop, c);
         while (row < to) {
             // the next rows are asked for before these are worked on
-            uint4 mine[GRAD_ROWS], other[GRAD_ROWS];
+            Pieces<WIDE> mine[ROWS], other[ROWS];
 #pragma unroll
-            for (int i = 0; i < GRAD_ROWS; ++i) { mine[i] = p[i]; other[i] = q[i]; }
-            fetch(row + GRAD_ROWS * step);
+            for (int i = 0; i < ROWS; ++i) { mine[i] = p[i]; other[i] = q[i]; }
+            fetch(row + ROWS * step);
 #pragma unroll
-            for (int i = 0; i < GRAD_ROWS; ++i)
+            for (int i = 0; i < ROWS; ++i)
                 if (row + i * step < to) {
                     float v[8], z[8];
-                    unpack16<T>(mine[i], v);
+                    unpack16<T>(take<WIDE>(dout + (row + i * step) * ld_dout, c, cols, mine[i]), v);
                     if (drop.on) {
                         columns.choose(uint32_t(row + i * step), v);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[e] *= drop.scale;
                     }
                     if constexpr (ACT != RUBICK_ACT_NONE) {
-                        unpack16<T>(other[i], z);
+                        unpack16<T>(take<WIDE>(pre + (row + i * step) * ld_pre, c, cols, other[i]), z);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[e] *= act_slope(ACT, z[e]);
                     }
@@ -153,7 +152,7 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256, 3) linear_
 #pragma unroll
                     for (int e = 0; e < 8; ++e) total[e] += v[e];
                 }
-            row += GRAD_ROWS * step;
+            row += ROWS * step;
         }
     }
     if (!a.dbias) return;
@@ -236,11 +235,10 @@ template <typename T> cudaError_t dropout(const DropoutArgs &a, int num_sms, cud
     return a.d.cols <= Lanes<T>::N ? dropout<T, 1>(a, wide, num_sms, st) : dropout<T, 8>(a, wide, num_sms, st);
 }
 
-template <typename T, int ACT> cudaError_t linear_grad(LinearGradArgs a, cudaStream_t st)
+template <typename T, int ACT> cudaError_t linear_grad(const LinearGradArgs &a, cudaStream_t st)
 {
-    const dim3 grid(a.strips, a.chunks);
-    a.wide = aligned16(a.dout) && (a.ld_dout & 7) == 0 && (ACT == RUBICK_ACT_NONE || (aligned16(a.pre) && (a.ld_pre & 7) == 0));
-    return launch_chained(linear_grad_kernel<T, ACT>, grid, dim3(256), 0, 1, st, a);
+    const bool wide = aligned16(a.dout) && (a.ld_dout & 7) == 0 && (ACT == RUBICK_ACT_NONE || (aligned16(a.pre) && (a.ld_pre & 7) == 0));
+    return launch_chained(wide ? linear_grad_kernel<T, ACT, true> : linear_grad_kernel<T, ACT, false>, dim3(a.strips, a.chunks), dim3(256), 0, 1, st, a);
 }
 template <typename T> cudaError_t linear_grad(const LinearGradArgs &a, cudaStream_t st)
 {

@@ -80,7 +80,7 @@ template <typename T> __device__ __forceinline__ void write_lines(const uint8_t 
 
 // Sums in tensor memory are cut off, not rounded, whenever 16 products join them, always towards zero: over 4,096 k that
 // takes 2e-6 of a logit.  The loss is a difference of logits in single precision, so its logits are summed up in parts of
-// SUM_STEPS x 64 k, which the reading warps add in registers (log-sums off by 1.3e-6 become SUM_ERROR); gradients and layers,
+// SUM_STEPS x 64 k, which the reading warps add in registers (log-sums off by 1.3e-6 become 1.3e-7); gradients and layers,
 // which are rounded to 16 bits, take their sums as they are.
 constexpr int SUM_STEPS = 8;
 // The reading warps of a pair need 128 registers for that, so they take some of the others': 64 x 128 + 216 x 256 threads' are

@@ -67,7 +67,6 @@ struct LinearGradArgs {
     float *part;                         // [chunks][cols] sums of row chunks
     uint32_t *tickets;                   // [strips] arrivals, zero between calls
     int chunks, strips;                  // of rows, of columns
-    bool wide;                           // every row of dout and pre begins on a 16-byte boundary
     int lanes;                           // lanes of a warp that share a row (a power of two); the others take further rows
 };
 // rows of h whose label takes part (zeros for the others), next to each other; the weights' common power of two
@@ -202,16 +201,21 @@ template <int VE> struct DropColumns {
 };
 
 // ---- activations -------------------------------------------------------------------------------------------------
-// v / (1 + exp(-u)): where the exponential overflows the quick division gives the right 0
-__device__ __forceinline__ float over_one_plus_exp(float v, float u) { return __fdividef(v, 1.f + __expf(-u)); }
+// The hardware's exponential and reciprocal, subnormal numbers taken as zero (with them kept, each costs three instructions
+// more, for results that are rounded to 16 bits or summed with larger ones).
+constexpr float LOG2E = 1.4426950408889634f;
+__device__ __forceinline__ float ex2(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+__device__ __forceinline__ float rcp(float v) { float r; asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
+// v / (1 + exp(-u)): where the exponential overflows the reciprocal is the right 0
+__device__ __forceinline__ float over_one_plus_exp(float v, float u) { return v * rcp(1.f + ex2(-LOG2E * u)); }
 __device__ __forceinline__ float tanh_arg2(float v) { return 1.5957691216057308f * (v + 0.044715f * v * v * v); }   // 2 sqrt(2 / pi) ..
 // Phi(v), the normal distribution's integral, and exp(-v^2 / 2): erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x),
 // x = |v| / sqrt(2) (Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26: off by 1.5e-7 at most).  The
 // exponential is the one that the slope needs as well, and on the far left nothing cancels, as in 1 + erf.
 __device__ __forceinline__ float normal_integral(float v, float &bell)
 {
-    const float x = fabsf(v) * 0.70710678118654752f, t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
-    bell = __expf(-0.5f * v * v);
+    const float x = fabsf(v) * 0.70710678118654752f, t = rcp(fmaf(0.3275911f, x, 1.f));
+    bell = ex2(-0.5f * LOG2E * v * v);
     const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
     const float tail = 0.5f * p * bell;
     return v > 0.f ? 1.f - tail : tail;
@@ -249,24 +253,33 @@ __device__ __forceinline__ float act_slope(int act, float v)
     return 1.f;
 }
 
-// 16 bytes of a row from column c on, whatever its alignment: the two aligned pieces that hold them, shifted, where both lie
-// within the row, else element by element (0 past the end).
-template <typename T, typename I> __device__ __forceinline__ uint4 load_any(const T *row, I c, I n)
+// 16 bytes of a row from column c on, whatever its alignment: the two aligned pieces that hold them, asked for in one step and
+// shifted in another, where both lie within the row; else element by element (0 past the end).  WIDE: every row begins on a
+// 16-byte boundary, and one piece is all.
+template <bool WIDE> struct Pieces { uint4 a, b; };
+template <> struct Pieces<true> { uint4 a; };
+template <typename T, typename I> __device__ __forceinline__ bool two_pieces(const T *at, I c, I n, uint32_t &off)
+{
+    off = uint32_t(reinterpret_cast<uintptr_t>(at)) & 15;
+    const I before = I(off / uint32_t(sizeof(T)));
+    return c >= before && c - before + 2 * Lanes<T>::N <= n;
+}
+template <bool WIDE, typename T, typename I> __device__ __forceinline__ Pieces<WIDE> ask(const T *row, I c, I n)
 {
     constexpr int N = Lanes<T>::N;
     const T *const at = row + c;
-    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(at)) & 15;
-    const I before = I(off / uint32_t(sizeof(T)));
-    if (c >= before && c - before + 2 * N <= n) {
-        const uint8_t *const from = reinterpret_cast<const uint8_t *>(at) - off;
-        const uint4 a = ld_cached(from), b = ld_cached(from + 16);
-        const bool four = off & 4, eight = off & 8;
-        // 32 bytes moved down by eight, then four, then what is left below four
-        const uint32_t u0 = eight ? a.z : a.x, u1 = eight ? a.w : a.y, u2 = eight ? b.x : a.z, u3 = eight ? b.y : a.w, u4 = eight ? b.z : b.x, u5 = eight ? b.w : b.y;
-        const uint32_t w0 = four ? u1 : u0, w1 = four ? u2 : u1, w2 = four ? u3 : u2, w3 = four ? u4 : u3, w4 = four ? u5 : u4;
-        if constexpr (sizeof(T) == 4) return make_uint4(w0, w1, w2, w3);
-        const uint32_t bits = (off & 2) * 8;
-        return make_uint4(__funnelshift_r(w0, w1, bits), __funnelshift_r(w1, w2, bits), __funnelshift_r(w2, w3, bits), __funnelshift_r(w3, w4, bits));
+    Pieces<WIDE> p;
+    if constexpr (WIDE) {
+        if (c + N <= n) { p.a = ld_stream(at); return p; }
+    } else {
+        uint32_t off;
+        if (two_pieces(at, c, n, off)) {
+            const uint8_t *const from = reinterpret_cast<const uint8_t *>(at) - off;
+            p.a = ld_cached(from);
+            p.b = ld_cached(from + 16);
+            return p;
+        }
+        p.b = uint4{};
     }
     uint32_t w[4] = {};
 #pragma unroll
@@ -276,13 +289,27 @@ template <typename T, typename I> __device__ __forceinline__ uint4 load_any(cons
             else w[e >> 1] |= uint32_t(reinterpret_cast<const uint16_t *>(at)[e]) << (16 * (e & 1));
         }
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    p.a = make_uint4(w[0], w[1], w[2], w[3]);
+    return p;
 }
-// ... with the word that says whether every row begins on a 16-byte boundary
-template <typename T> __device__ __forceinline__ uint4 load_raw(const T *row, int c, int n, bool wide)
+template <bool WIDE, typename T, typename I> __device__ __forceinline__ uint4 take(const T *row, I c, I n, const Pieces<WIDE> &p)
 {
-    return wide && c + Lanes<T>::N <= n ? ld_stream(row + c) : load_any(row, c, n);
+    if constexpr (WIDE) return p.a;
+    else {
+        uint32_t off;
+        if (!two_pieces(row + c, c, n, off)) return p.a;
+        const uint4 &a = p.a, &b = p.b;
+        const bool four = off & 4, eight = off & 8;
+        // 32 bytes moved down by eight, then four, then what is left below four
+        const uint32_t u0 = eight ? a.z : a.x, u1 = eight ? a.w : a.y, u2 = eight ? b.x : a.z, u3 = eight ? b.y : a.w, u4 = eight ? b.z : b.x, u5 = eight ? b.w : b.y;
+        const uint32_t w0 = four ? u1 : u0, w1 = four ? u2 : u1, w2 = four ? u3 : u2, w3 = four ? u4 : u3, w4 = four ? u5 : u4;
+        if constexpr (sizeof(T) == 4) return make_uint4(w0, w1, w2, w3);
+        const uint32_t bits = (off & 2) * 8;
+        return make_uint4(__funnelshift_r(w0, w1, bits), __funnelshift_r(w1, w2, bits), __funnelshift_r(w2, w3, bits), __funnelshift_r(w3, w4, bits));
+    }
 }
+template <typename T, typename I> __device__ __forceinline__ uint4 load_any(const T *row, I c, I n) { return take<false>(row, c, n, ask<false>(row, c, n)); }
+
 // Eight elements of a row from column c on (a multiple of eight), 16 bytes at a time where the tensor allows it; columns
 // from n on are not touched.
 template <typename T> __device__ __forceinline__ void load8(const T *row, int64_t c, int64_t n, bool wide, float (&v)[8])
@@ -435,8 +462,6 @@ template <typename T, int ACT> struct Finish {
     }
 };
 
-constexpr float LOG2E = 1.4426950408889634f;
-__device__ __forceinline__ float ex2(float v) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v)); return r; }
 
 }  // namespace train
 }  // namespace rubick
