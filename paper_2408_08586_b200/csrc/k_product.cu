@@ -45,9 +45,15 @@ constexpr int FEW_ROWS = 64;
 // Tile number -> tile row, tile column, split: eight tile rows at a time, so that what runs at once shares operands in L2.
 __device__ __forceinline__ void place(const Tiling &t, uint32_t i, int &m, int &n, int &split)
 {
-    const uint32_t s = t.all == t.each ? 0 : i / t.each, r = i - s * t.each, band = 8 * t.tiles_n, b = r / band, q = r - b * band;
-    const uint32_t high = t.tiles_m - b * 8 < 8 ? t.tiles_m - b * 8 : 8;
+    const uint32_t s = t.all == t.each ? 0 : i / t.each, r = i - s * t.each;
     split = int(s);
+    if (t.tiles_m <= 8) {
+        n = t.tiles_m == 1 ? int(r) : int(r / t.tiles_m);
+        m = int(r - n * t.tiles_m);
+        return;
+    }
+    const uint32_t band = 8 * t.tiles_n, b = r / band, q = r - b * band;
+    const uint32_t high = t.tiles_m - b * 8 < 8 ? t.tiles_m - b * 8 : 8;
     n = int(q / high);
     m = int(b * 8 + (q - n * high));
 }
@@ -117,12 +123,23 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
     if (warp == 2) {
         tmem_alloc<PAIR>(smem_addr(const_cast<uint32_t *>(words + 1)), COLUMNS);
         tmem_alloc_done<PAIR>();
+    } else if (threadIdx.x == 96) {
+        tensor_prefetch(&maps.a[0]);
+        tensor_prefetch(&maps.b[0]);
     }
     tcgen_before_sync();
-    __syncthreads();
-    if constexpr (PAIR) cluster_sync();
+    if constexpr (PAIR) {
+        __syncthreads();
+        cluster_sync();
+    } else if (warp == 0) {
+        // (the first warp fetches: it knows the barriers and does not wait for the tensor memory)
+        __syncwarp();
+        asm volatile("bar.arrive 1, %0;" ::"n"(THREADS) : "memory");
+    } else {
+        asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
+    }
     tcgen_after_sync();
-    const uint32_t tmem = words[1];
+    const uint32_t tmem = !PAIR && warp == 0 ? 0 : words[1];
     const uint32_t first = !shared_tiles ? blockIdx.x / ranks : (mine_is ? work.t[0].all : 0) + (blockIdx.x - work.t[mine_is].first) / ranks;
     const uint32_t step = shared_tiles ? 0x80000000u : gridDim.x / ranks;
     const uint32_t end = shared_tiles && !mine_is ? work.t[0].all : work.all;     // (blocks that fill a cluster up have no tile)
@@ -210,6 +227,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             }
         }
         __syncwarp();
+        if (shared_tiles) cluster_sync();
     } else {
         if constexpr (KIND == PRODUCT_STATS && PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(READERS_REGISTERS));
         const int quarter = warp & 3, side = (warp - FIRST_READER) >> 2;       // 32 rows, half of the columns
@@ -219,6 +237,10 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
         Finish<T, ACT> finish(work.a[which]);
         uint32_t tile = 0;
         float running_top = ninf(), running_sum = 0.f;             // few rows: of all of the block's tiles
+        // a cluster's tile: eight columns a lane, two rows a warp, every `ranks`-th row of them here
+        const int share_row = ((warp - FIRST_READER) * 2 + (lane >> 4)) * int(ranks) + int(rank);
+        int64_t share_m0 = 0, share_col = 0;
+        float share_bias[8], share_residual[8];
         for (uint32_t i = first; i < end; i += step) {
             if (TWO && !which && i >= work.t[0].all) {
                 which = 1;
@@ -315,6 +337,14 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                     a.stats[(int64_t(tn) * 2 + side) * rows + row] = make_float2(top, sum);
                 }
                 continue;
+            }
+            if (shared_tiles) {
+                share_m0 = int64_t(tm) * BM;
+                share_col = int64_t(tn) * SINGLE_COLS + (lane & 15) * 8;
+                if (share_col < cols && share_m0 + share_row < rows) {         // (asked for while the sums are still made)
+                    finish.load_bias(share_col, share_bias);
+                    finish.load_residual(share_m0 + share_row, share_col, share_residual);
+                }
             }
             if (!barrier_wait(done + 8 * half, tile / 2 & 1, given_up)) break;
             __syncwarp();
@@ -466,6 +496,34 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             ++tile;
         }
         if constexpr (KIND == PRODUCT_STATS && FEW) *reinterpret_cast<float2 *>(mine + lane * 8) = make_float2(running_top, running_sum);
+        if (shared_tiles) {
+            // the blocks' shares added up in their order
+            cluster_sync();
+            if ((FEW || ranks > 1) && first < end && !*given_up) {
+                const int64_t rows = work.a[which].m, cols = work.a[which].n;
+                const uint32_t from_rank = cluster_rank() - rank;
+                for (int r = share_row; r < BM && share_m0 + r < rows; r += READERS * 2 * int(ranks)) {
+                    const uint32_t from = stages + r * SHARE_LINE + (lane & 15) * 32;
+                    float4 x[8], y[8];
+#pragma unroll
+                    for (int s = 0; s < 8; ++s)
+                        if (s < int(ranks)) {
+                            const uint32_t there = at_rank(from, from_rank + s);
+                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[s].x), "=f"(x[s].y), "=f"(x[s].z), "=f"(x[s].w) : "r"(there));
+                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y[s].x), "=f"(y[s].y), "=f"(y[s].z), "=f"(y[s].w) : "r"(there + 16));
+                        }
+                    if (share_col >= cols) continue;
+                    if (r != share_row) finish.load_residual(share_m0 + r, share_col, share_residual);
+                    float v[8] = {};
+#pragma unroll
+                    for (int s = 0; s < 8; ++s)
+                        if (s < int(ranks)) {
+                            v[0] += x[s].x; v[1] += x[s].y; v[2] += x[s].z; v[3] += x[s].w; v[4] += y[s].x; v[5] += y[s].y; v[6] += y[s].z; v[7] += y[s].w;
+                        }
+                    finish(share_m0 + r, share_col, v, share_bias, share_residual);
+                }
+            }
+        }
     }
     __syncthreads();
     if constexpr (KIND == PRODUCT_STATS && FEW) {
@@ -481,35 +539,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             a.stats[int64_t(blockIdx.x) * a.m + threadIdx.x] = make_float2(top, sum);
         }
     }
-    if (PAIR || shared_tiles) cluster_sync();        // (a pair: the other block's copies, products and arrivals end here as well)
-    if (shared_tiles) {
-        // the blocks' shares added up in their order, every `ranks`-th row here: eight sums a lane, two rows a warp
-        if ((FEW || ranks > 1) && first < end && warp >= FIRST_READER && !*given_up) {
-            const int which = mine_is;
-            const uint32_t from_rank = cluster_rank() - rank;
-            const ProductArgs &a = work.a[which];
-            const Finish<T, ACT> finish(a);
-            int tm, tn, split;
-            place(work.t[which], which ? first - work.t[0].all : first, tm, tn, split);
-            const int64_t m0 = int64_t(tm) * BM, c = int64_t(tn) * SINGLE_COLS + (lane & 15) * 8;
-            const int high = a.m - m0 < BM ? int(a.m - m0) : BM;
-            float bias[8];
-            finish.load_bias(c, bias);
-            for (int r = ((warp - FIRST_READER) * 2 + (lane >> 4)) * int(ranks) + int(rank); r < high; r += READERS * 2 * int(ranks)) {
-                const uint32_t at = stages + r * SHARE_LINE + (lane & 15) * 32;
-                float v[8] = {};
-                for (uint32_t s = 0; s < ranks; ++s) {
-                    const uint32_t from = at_rank(at, from_rank + s);
-                    float4 x, y;
-                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(from));
-                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y.x), "=f"(y.y), "=f"(y.z), "=f"(y.w) : "r"(from + 16));
-                    v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w; v[4] += y.x; v[5] += y.y; v[6] += y.z; v[7] += y.w;
-                }
-                if (c < a.n) finish(m0 + r, c, v, bias);
-            }
-        }
-        cluster_sync();                              // nobody's share goes while it is read
-    }
+    if (PAIR || shared_tiles) cluster_meet();        // (the other blocks' copies, products, arrivals and reads end here as well)
     if (warp == 2) {
         tcgen_after_sync();
         tmem_free<PAIR>(tmem, COLUMNS);
@@ -529,8 +559,9 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256) join_kerne
     const int64_t units = (a.n + 7) / 8, all = a.m * units;
     for (int64_t i = int64_t(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += int64_t(gridDim.x) * blockDim.x) {
         const int64_t row = i / units, c = (i - row * units) * 8;
-        float v[8] = {}, bias[8];
+        float v[8] = {}, bias[8], residual[8];
         finish.load_bias(c, bias);
+        finish.load_residual(row, c, residual);
 #pragma unroll 4
         for (int s = 0; s < splits; ++s) {
             float p[8];
@@ -538,7 +569,7 @@ template <typename T, int ACT> __global__ void __launch_bounds__(256) join_kerne
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += p[e];
         }
-        finish(row, c, v, bias);
+        finish(row, c, v, bias, residual);
     }
 }
 

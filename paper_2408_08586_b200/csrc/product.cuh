@@ -395,19 +395,22 @@ template <typename T, int ACT> struct Finish {
             for (int e = 0; e < 8; ++e) v[e] *= drop.scale;
         }
     }
-    __device__ __forceinline__ void operator()(int64_t row, int64_t c, float (&v)[8], const float (&b)[8]) const
+    // the residual of eight columns, 0 without one
+    __device__ __forceinline__ void load_residual(int64_t row, int64_t c, float (&r)[8]) const
+    {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = 0.f;
+        if (residual && !acc_out) load8<T>(residual + row * ld_res, c, n, wide & WIDE_RES, r);
+    }
+    __device__ __forceinline__ void operator()(int64_t row, int64_t c, float (&v)[8], const float (&b)[8], const float (&r)[8]) const
     {
         if (accumulate(row, c, v)) return;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] += b[e];
         if (pre) store8<T>(pre + row * ld_pre, c, n, wide & WIDE_PRE, v);
         activate(row, c, v);
-        if (residual) {
-            float r[8];
-            load8<T>(residual + row * ld_res, c, n, wide & WIDE_RES, r);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += r[e];
-        }
+        for (int e = 0; e < 8; ++e) v[e] += r[e];
         store8<T>(out + row * ld_out, c, n, wide & WIDE_OUT, v);
     }
     // The same for eight sums of four rows each, 8 rows apart, all of them within the matrix and every tensor read and written

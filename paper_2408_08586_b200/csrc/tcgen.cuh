@@ -14,6 +14,11 @@ __device__ __forceinline__ void cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// ... where nothing but the arrival itself matters: it does not wait for this thread's stores
+__device__ __forceinline__ void cluster_meet()
+{
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;\nbarrier.cluster.wait.aligned;" ::: "memory");
+}
 // the address of the same place in the shared memory of the cluster's block `rank`
 __device__ __forceinline__ uint32_t at_rank(uint32_t addr, uint32_t rank)
 {
@@ -44,6 +49,7 @@ __device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, vola
     return false;
 }
 
+__device__ __forceinline__ void tensor_prefetch(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // A box of a matrix into shared memory; bar counts its bytes (with PAIR: a barrier of the pair's first block).
 template <bool PAIR> __device__ __forceinline__ void tensor_load(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t bar)
 {
