@@ -649,7 +649,7 @@ ProductWay way_of(ProductKind kind, const ProductArgs &a, int num_sms)
         if (kind != PRODUCT_OUT && cols != PAIR_COLS) continue;
         const int64_t tiles = ((a.m + 255) / 256) * ((a.n + cols - 1) / cols), places = num_sms / 2;
         for (int s = 1; s <= 8; ++s) {
-            if (s > 1 && (kind != PRODUCT_OUT || steps < 8 * s)) break;
+            if (s > 1 && (kind != PRODUCT_OUT || steps < 8 * s || tiles > 64 * places)) break;       // (what many tiles would gain is too little)
             const int64_t per = (steps + s - 1) / s, splits = (steps + per - 1) / per, waves = (tiles * splits + places - 1) / places;
             const float each = (A_BYTES + (a.b.along_k ? cols / 2 * 128 : (cols / 2 + 63) / 64 * int(BLOCK_BYTES))) * (0.33f / STAGE);
             const float cost = float(waves) * float(per) * each + 8.f + (splits > 1 ? 4.f + float(splits) * float(a.m) * float(a.n) * 2e-6f : 0.f);
@@ -704,13 +704,19 @@ template <typename T, ProductKind KIND, int ACT, Shape SHAPE> cudaError_t launch
     }
     for (int i = n; i < 2; ++i) { maps.a[i] = maps.a[0]; maps.b[i] = maps.b[0]; work.a[i].way.splits = 1; work.t[i].first = 0xffffffffu; }
     const auto kernel = product_kernel<T, KIND, ACT, SHAPE>;
-    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED);
+    static std::atomic<uint64_t> ready{0};            // devices, by bits, on which the kernel has its shared memory
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
-    if constexpr (KIND == PRODUCT_STATS && PAIR) {
-        // a block that lacks the registers its warps ask for would wait for them for ever
-        cudaFuncAttributes has;
-        if ((e = cudaFuncGetAttributes(&has, kernel)) != cudaSuccess) return e;
-        if (has.numRegs * THREADS < OTHERS_REGISTERS * 128 + READERS_REGISTERS * 256) return cudaErrorInvalidConfiguration;
+    if (device > 63 || !(ready.load(std::memory_order_relaxed) >> device & 1)) {
+        if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SHARED)) != cudaSuccess) return e;
+        if constexpr (KIND == PRODUCT_STATS && PAIR) {
+            // a block that lacks the registers its warps ask for would wait for them for ever
+            cudaFuncAttributes has;
+            if ((e = cudaFuncGetAttributes(&has, kernel)) != cudaSuccess) return e;
+            if (has.numRegs * THREADS < OTHERS_REGISTERS * 128 + READERS_REGISTERS * 256) return cudaErrorInvalidConfiguration;
+        }
+        if (device <= 63) ready.fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
     }
     const int64_t most = num_sms / CTAS;
     const unsigned grid = blocks_of_shares ? blocks_of_shares : unsigned((work.all < most ? work.all : most) * CTAS);
