@@ -30,6 +30,7 @@ struct Tiling {
     uint32_t tiles_m, tiles_n, each, all;
     int steps, per, cols;
     uint32_t bytes;                                  // of a stage, per block
+    uint32_t band_part;                              // 2^32 / (8 tiles_n), rounded up
     uint32_t share, first;                           // blocks of a cluster that share a tile's k, and the first of them all
 };
 // Up to two products of one launch: the second one's tiles follow the first one's.  With a cluster of single blocks every
@@ -52,10 +53,13 @@ __device__ __forceinline__ void place(const Tiling &t, uint32_t i, int &m, int &
         m = int(r - n * t.tiles_m);
         return;
     }
-    const uint32_t band = 8 * t.tiles_n, b = r / band, q = r - b * band;
-    const uint32_t high = t.tiles_m - b * 8 < 8 ? t.tiles_m - b * 8 : 8;
-    n = int(q / high);
-    m = int(b * 8 + (q - n * high));
+    // r / band by a multiplication: the quotient by the rounded-up reciprocal is never too small, and one too large at most
+    const uint32_t band = 8 * t.tiles_n;
+    uint32_t b = __umulhi(r, t.band_part);
+    if (b * band > r) --b;
+    const uint32_t q = r - b * band, high = t.tiles_m - b * 8;
+    n = high >= 8 ? int(q >> 3) : int(q / high);
+    m = int(b * 8 + (high >= 8 ? q & 7 : q - n * high));
 }
 
 __device__ __forceinline__ float ninf() { return __uint_as_float(0xff800000u); }
@@ -76,11 +80,20 @@ __device__ __forceinline__ void exchange(uint8_t *mine, int lane, float (&v)[32]
 // 32 rows of 128 bytes, 16-byte pieces exchanged by the row, to rows of 16-byte boundaries: whole lines at a time.
 template <typename T> __device__ __forceinline__ void write_lines(const uint8_t *mine, int lane, T *to, int64_t m0, int64_t rows, int64_t ld, int64_t left)
 {
+    // (all read before any is written: the compiler cannot know that the two do not meet, and would wait for each in turn)
+    const int line = lane >> 3, q = lane & 7;
+    uint4 p[8];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const int line = r * 4 + (lane >> 3), q = lane & 7;
-        const uint4 p = *reinterpret_cast<const uint4 *>(mine + line * 128 + ((q ^ (line & 7)) << 4));
-        if (m0 + line < rows && q * 8 < left) *reinterpret_cast<uint4 *>(to + (m0 + line) * ld + q * 8) = p;
+    for (int r = 0; r < 8; ++r) p[r] = *reinterpret_cast<const uint4 *>(mine + (r * 4 + line) * 128 + ((q ^ ((r * 4 + line) & 7)) << 4));
+    if (q * 8 >= left) return;
+    T *const first = to + (m0 + line) * ld + q * 8;
+    const int64_t step = 4 * ld;
+    if (m0 + 32 <= rows) {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) *reinterpret_cast<uint4 *>(first + r * step) = p[r];
+    } else {
+#pragma unroll
+        for (int r = 0; r < 8; ++r) if (m0 + r * 4 + line < rows) *reinterpret_cast<uint4 *>(first + r * step) = p[r];
     }
 }
 
@@ -375,8 +388,39 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 const int q = (lane & 3) * 2, above = lane >> 2;
                 const bool quick = m0 + 32 <= rows && finish.takes_four();
                 float *const part = t.all == t.each ? nullptr : a.part + (int64_t(split) * rows + m0 + above) * finish.ld_acc;
+                int done_cols = 0;
+                if (!part && finish.takes_rows()) {
+                    // a thread has a row of 64 sums, which become 128 bytes of it, written line by line
 #pragma unroll 1
-                for (int c = 0; c < width && n0 + c < cols; c += 32) {
+                    for (; done_cols + 64 <= width && n0 + done_cols + 64 <= cols; done_cols += 64) {
+                        float v[64];
+                        tmem_load64(at + done_cols, v);
+                        if (finish.bias) {
+#pragma unroll
+                            for (int p = 0; p < 8; ++p) {
+                                float bias[8];
+                                finish.load_bias(n0 + done_cols + 8 * p, bias);
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) v[8 * p + e] = fmaf(v[8 * p + e], finish.scale, bias[e]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 64; ++e) v[e] *= finish.scale;
+                        }
+#pragma unroll
+                        for (int p = 0; p < 8; ++p) {
+                            float x[8];
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) x[e] = act_value(ACT, v[8 * p + e]);
+                            *reinterpret_cast<uint4 *>(mine + lane * 128 + ((p ^ (lane & 7)) << 4)) = pack16<T>(x);
+                        }
+                        __syncwarp();
+                        write_lines(mine, lane, finish.out + n0 + done_cols, m0, rows, finish.ld_out, 64);
+                        __syncwarp();
+                    }
+                }
+#pragma unroll 1
+                for (int c = done_cols; c < width && n0 + c < cols; c += 32) {
                     const int64_t col = n0 + c + q * 4;
                     float v[32], bias[8];
                     finish.load_bias(col, bias);
@@ -463,11 +507,18 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 const uint32_t mask = live ? 0xffffffffu : 0u;                // (rows that take no part, whatever their logits are)
                 const int64_t label = live ? int64_t(is) - a.first - n0 : -1;
                 for (int c = 0; c < (FEW ? 32 : width); c += 64) {
+                    float all[FEW ? 32 : 64];
+                    if constexpr (FEW) {
+                        tmem_load32(at, all);
+                        exchange(mine, lane, all);
+                    } else {
+                        tmem_load64(at + c, all);
+                    }
 #pragma unroll
                     for (int h = 0; h < (FEW ? 1 : 2); ++h) {
                         float v[32];
-                        tmem_load32(at + c + 32 * h, v);
-                        if constexpr (FEW) exchange(mine, lane, v);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) v[e] = all[32 * h + e];
                         const int here = c + 32 * h;
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] = w * ex2(((v[e] - from) - rest) * LOG2E);
@@ -694,7 +745,8 @@ template <typename T, ProductKind KIND, int ACT, Shape SHAPE> cudaError_t launch
         if (work.all + all > 0x7fffffff || steps > 0x7fffffff / BK) return cudaErrorInvalidValue;
         const uint32_t bytes = A_BYTES + (FEW || a[i].b.along_k ? cols / CTAS * 128 : (cols / CTAS + 63) / 64 * BLOCK_BYTES);
         work.a[i] = a[i];
-        work.t[i] = Tiling{uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(tiles_m * tiles_n), uint32_t(all), int(steps), int((steps + parts - 1) / parts), cols, bytes, uint32_t(a[i].way.share), blocks_of_shares};
+        work.t[i] = Tiling{uint32_t(tiles_m), uint32_t(tiles_n), uint32_t(tiles_m * tiles_n), uint32_t(all), int(steps), int((steps + parts - 1) / parts), cols, bytes,
+                           uint32_t(((uint64_t(1) << 32) + 8 * tiles_n - 1) / (8 * tiles_n)), uint32_t(a[i].way.share), blocks_of_shares};
         if (!PAIR && KIND == PRODUCT_OUT && (FEW || work.cluster > 1)) {
             if (all * a[i].way.share > 1 << 20) return cudaErrorInvalidValue;
             blocks_of_shares += (uint32_t(all) * a[i].way.share + work.cluster - 1) / work.cluster * work.cluster;

@@ -458,6 +458,8 @@ template <typename T, int ACT> struct Finish {
 #pragma unroll
         for (int r = 0; r < 4; ++r) *reinterpret_cast<uint4 *>(out + (row + 8 * r) * ld_out + c) = pack16<T>(v[r]);
     }
+    // whether there is nothing to fetch or keep for a row's sums: a thread may then finish a whole row of 64
+    __device__ __forceinline__ bool takes_rows() const { return !acc_in && !acc_out && !pre && !residual && !drop.on && (wide & WIDE_OUT); }
     // whether a whole block of 32 rows x 32 columns may go that way
     __device__ __forceinline__ bool takes_four() const
     {
