@@ -111,6 +111,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
 {
     constexpr bool PAIR = SHAPE == SHAPE_PAIR, FEW = SHAPE == SHAPE_FEW;
     constexpr int CTAS = PAIR ? 2 : 1;
+    constexpr bool TWO = KIND == PRODUCT_OUT && ACT == RUBICK_ACT_NONE && !PAIR;      // products there may be
     constexpr uint32_t HALF = PAIR ? PAIR_COLS : SINGLE_COLS, COLUMNS = 2 * HALF;      // of tensor memory: two tiles
     chain_go();
     extern __shared__ uint8_t raw[];
@@ -194,7 +195,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 }
             };
             fetch(std::integral_constant<int, 0>());
-            if constexpr (KIND == PRODUCT_OUT && ACT == RUBICK_ACT_NONE) fetch(std::integral_constant<int, 1>());
+            if constexpr (TWO) fetch(std::integral_constant<int, 1>());
             // given up: the copies in flight write into this block's memory, so they are waited for before it goes
             if (!fine && (!PAIR || rank == 0)) {
                 volatile uint32_t never = 0;
@@ -233,7 +234,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 }
             };
             sum(std::integral_constant<int, 0>());
-            if constexpr (KIND == PRODUCT_OUT && ACT == RUBICK_ACT_NONE) sum(std::integral_constant<int, 1>());
+            if constexpr (TWO) sum(std::integral_constant<int, 1>());
             if (!fine) {                             // what was multiplied is waited for before the tensor memory goes
                 volatile uint32_t never = 0;
                 for (uint32_t r = round > STAGES ? round - STAGES : 0; r < round; ++r) barrier_wait(empty + 8 * (r % STAGES), r / STAGES & 1, &never);
@@ -245,9 +246,8 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
         if constexpr (KIND == PRODUCT_STATS && PAIR) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(READERS_REGISTERS));
         const int quarter = warp & 3, side = (warp - FIRST_READER) >> 2;       // 32 rows, half of the columns
         uint8_t *const mine = shared + STAGES * STAGE + (warp - FIRST_READER) * 4096;
-        constexpr bool TWO = KIND == PRODUCT_OUT && ACT == RUBICK_ACT_NONE;      // products there may be
-        int which = TWO && first >= work.t[0].all;
-        Finish<T, ACT> finish(work.a[which]);
+        const int which = TWO && first >= work.t[0].all;           // (of two products every block has one tile)
+        const Finish<T, ACT> finish(work.a[which]);
         uint32_t tile = 0;
         float running_top = ninf(), running_sum = 0.f;             // few rows: of all of the block's tiles
         // a cluster's tile: eight columns a lane, two rows a warp, every `ranks`-th row of them here
@@ -255,15 +255,11 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
         int64_t share_m0 = 0, share_col = 0;
         float share_bias[8], share_residual[8];
         for (uint32_t i = first; i < end; i += step) {
-            if (TWO && !which && i >= work.t[0].all) {
-                which = 1;
-                finish = Finish<T, ACT>(work.a[1]);
-            }
             const ProductArgs &a = work.a[TWO ? which : 0];
             const Tiling &t = work.t[TWO ? which : 0];
             const int64_t rows = a.m, cols = a.n;
             int tm, tn, split;
-            place(t, which ? i - work.t[0].all : i, tm, tn, split);
+            place(t, TWO && which ? i - work.t[0].all : i, tm, tn, split);
             const uint32_t half = tile & 1;
             const int width = KIND == PRODUCT_OUT ? t.cols / 2 : int(HALF) / 2;      // (only sums may be cut otherwise)
             const int64_t m0 = FEW ? side * 32 : (int64_t(tm) * CTAS + (PAIR ? rank : 0)) * BM + quarter * 32;
@@ -485,13 +481,30 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                         if (!over && column < cols) {
                             const float factor = bare ? finish.scale : 1.f;
                             T *to = finish.out + m0 * finish.ld_out + column;
-                            if (finish.residual) {
-                                const T *res = finish.residual + m0 * finish.ld_res + column;
-#pragma unroll 4
-                                for (int r = 0; r < high; ++r, to += finish.ld_out, res += finish.ld_res) *to = from_f<T>(fmaf(*cell(r), factor, to_f(*res)));
-                            } else {
-#pragma unroll 8
-                                for (int r = 0; r < high; ++r, to += finish.ld_out) *to = from_f<T>(*cell(r) * factor);
+                            const T *res = finish.residual ? finish.residual + m0 * finish.ld_res + column : nullptr;
+                            // (eight read before they are written, as above)
+#pragma unroll 1
+                            for (int r = 0; r < high; r += 8) {
+                                float u[8];
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) u[e] = *cell(r + e) * factor;
+                                if (r + 8 <= high && !res) {
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) { *to = from_f<T>(u[e]); to += finish.ld_out; }
+                                    continue;
+                                }
+                                if (res) {
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) {
+                                        if (r + e < high) u[e] += to_f(*res);
+                                        res += finish.ld_res;
+                                    }
+                                }
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) {
+                                    if (r + e < high) *to = from_f<T>(u[e]);
+                                    to += finish.ld_out;
+                                }
                             }
                         }
                     }
@@ -555,22 +568,25 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 const uint32_t from_rank = cluster_rank() - rank;
                 for (int r = share_row; r < BM && share_m0 + r < rows; r += READERS * 2 * int(ranks)) {
                     const uint32_t from = stages + r * SHARE_LINE + (lane & 15) * 32;
-                    float4 x[8], y[8];
-#pragma unroll
-                    for (int s = 0; s < 8; ++s)
-                        if (s < int(ranks)) {
-                            const uint32_t there = at_rank(from, from_rank + s);
-                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[s].x), "=f"(x[s].y), "=f"(x[s].z), "=f"(x[s].w) : "r"(there));
-                            asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y[s].x), "=f"(y[s].y), "=f"(y[s].z), "=f"(y[s].w) : "r"(there + 16));
-                        }
-                    if (share_col >= cols) continue;
-                    if (r != share_row) finish.load_residual(share_m0 + r, share_col, share_residual);
                     float v[8] = {};
 #pragma unroll
-                    for (int s = 0; s < 8; ++s)
-                        if (s < int(ranks)) {
-                            v[0] += x[s].x; v[1] += x[s].y; v[2] += x[s].z; v[3] += x[s].w; v[4] += y[s].x; v[5] += y[s].y; v[6] += y[s].z; v[7] += y[s].w;
-                        }
+                    for (int g = 0; g < 8; g += 4) {               // four at a time
+                        float4 x[4], y[4];
+#pragma unroll
+                        for (int s = 0; s < 4; ++s)
+                            if (g + s < int(ranks)) {
+                                const uint32_t there = at_rank(from, from_rank + g + s);
+                                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[s].x), "=f"(x[s].y), "=f"(x[s].z), "=f"(x[s].w) : "r"(there));
+                                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y[s].x), "=f"(y[s].y), "=f"(y[s].z), "=f"(y[s].w) : "r"(there + 16));
+                            }
+#pragma unroll
+                        for (int s = 0; s < 4; ++s)
+                            if (g + s < int(ranks)) {
+                                v[0] += x[s].x; v[1] += x[s].y; v[2] += x[s].z; v[3] += x[s].w; v[4] += y[s].x; v[5] += y[s].y; v[6] += y[s].z; v[7] += y[s].w;
+                            }
+                    }
+                    if (share_col >= cols) continue;
+                    if (r != share_row) finish.load_residual(share_m0 + r, share_col, share_residual);
                     finish(share_m0 + r, share_col, v, share_bias, share_residual);
                 }
             }
@@ -771,6 +787,7 @@ template <typename T, ProductKind KIND, int ACT, Shape SHAPE> cudaError_t launch
         if (device <= 63) ready.fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
     }
     const int64_t most = num_sms / CTAS;
+    if (n == 2 && !blocks_of_shares && work.all > most) return cudaErrorInvalidValue;
     const unsigned grid = blocks_of_shares ? blocks_of_shares : unsigned((work.all < most ? work.all : most) * CTAS);
     e = launch_chained(kernel, dim3(grid), dim3(THREADS), SHARED, int(work.cluster), st, maps, work);
     if (e != cudaSuccess || !joined) return e;
@@ -855,11 +872,12 @@ cudaError_t launch_lay_out(const LayOutArgs &a, int num_sms, cudaStream_t st)
 cudaError_t launch_products(ProductKind kind, ProductArgs *a, int n, float *part, int num_sms, cudaStream_t st)
 {
     // A product is cut by its own sizes, so that it is the same bits alone or with another.  Two share a launch where both are cut
-    // into the same kind of tiles and every block of theirs has a place at once; larger ones keep each other's operands out of
-    // L2 (4,096 x 2,048 -> 8,192, both gradients: 242 us together, 214 one after the other).
+    // into the same kind of tiles of single blocks and every block of theirs has a place at once (83 x 64 -> 704, both gradients:
+    // 13.4 us, 23.9 in two launches with their joins); larger ones keep each other's operands out of L2 (4,096 x 2,048 -> 8,192:
+    // 242 us together, 214 one after the other).
     for (int i = 0; i < n; ++i) a[i].part = part + a[i].part_at;
     bool together = n == 1;
-    if (n == 2 && a[0].way.shape == a[1].way.shape) {
+    if (n == 2 && a[0].way.shape == a[1].way.shape && a[0].way.shape != SHAPE_PAIR) {
         const ProductWay &x = a[0].way, &y = a[1].way;
         const int share = x.share > y.share ? x.share : y.share;
         const int64_t blocks = (x.blocks + share - 1) / share + (y.blocks + share - 1) / share;
