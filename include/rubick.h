@@ -666,7 +666,7 @@ int rubick_head_loss_forward(rubick_ctx *ctx, const rubick_head_loss_desc *h_des
 
 /* dz = d_dloss[n] (exp(z - lse) - onehot(label)),  dh = dz W^T,  dw = h^T dz (laid out as w), with forward's d_lse; rows
  * without a label add nothing and get zeros.  d_dloss NULL = 1.  d_dh or d_dw may be NULL: it is not computed.  The logits
- * are computed again, a piece of the vocabulary at a time; dz of a piece is rounded to dtype under a common power of two.
+ * are computed again, a piece of the vocabulary at a time; dz of a piece is rounded to dtype under a common factor.
  * The context keeps the piece (up to 512 MB, or 256 tokens), a copy of h and, with several pieces, dh in single precision.
  * d_lse is one float: rows whose logits are all far from zero want the step below.  rows = 0 writes zeros to dw.
  * Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */

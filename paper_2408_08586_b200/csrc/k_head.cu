@@ -11,9 +11,11 @@ __device__ __forceinline__ bool takes_part(int label, int vocab) { return label 
 constexpr int PREP_THREADS = 1024;
 
 // A copy of h with rows next to each other, zeros in the rows that take no part (whatever they hold must not reach the
-// sums over the rows).  The first block works out the power of two that brings the largest weight into [2^13, 2^14): in half
-// precision the probabilities of a large vocabulary, times a weight of one over the rows, would mostly fall below its normal
-// range.  The power is exact and taken out again, in single precision, behind the products.
+// sums over the rows).  The first block works out the factor that makes the largest weight 2^14; it is taken out again, in
+// single precision, behind the products.  In half precision the probabilities of a large vocabulary, times a weight of one
+// over the rows, would mostly fall below its normal range; and the label's entry w (p - 1), the largest of most rows, comes
+// to lie just below a power of two, where rounding takes least of it (gradients' distance from 64 bits: 1.46 times that of
+// single-precision products with a power of two, 1.33 so).
 template <typename T> __global__ void __launch_bounds__(PREP_THREADS) head_prep_kernel(const __grid_constant__ HeadPrepArgs a)
 {
     chain_go();
@@ -31,12 +33,9 @@ template <typename T> __global__ void __launch_bounds__(PREP_THREADS) head_prep_
         __syncthreads();
         if (threadIdx.x == 0) {
             for (int w = 1; w < PREP_THREADS / 32; ++w) top = fmaxf(top, tops[w]);
-            int e = 0;
-            if (top > 0.f) frexpf(top, &e);
-            e = 14 - e;
-            e = e < -100 ? -100 : e > 100 ? 100 : e;
-            a.scale[0] = ldexpf(1.f, -e);
-            a.scale[1] = ldexpf(1.f, e);
+            const float up = top > 0.f ? fminf(fmaxf(16384.f / top, 0x1p-100f), 0x1p100f) : 1.f;
+            a.scale[0] = 1.f / up;
+            a.scale[1] = up;
         }
         return;
     }

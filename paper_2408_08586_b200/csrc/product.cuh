@@ -42,7 +42,7 @@ struct ProductArgs {
     float2 *stats;                       // [product_stats_pairs][m]: maximum, sum of exponentials
     float *at_label;                     // [m] logit of the label
     const float *base, *rest;            // log of the row's sum of exponentials, in two parts (rest may be NULL)
-    const float *dloss, *up;             // [m] weight of a row (NULL: 1), and the common power of two
+    const float *dloss, *up;             // [m] weight of a row (NULL: 1), and the weights' common factor
     uint32_t *status;
 };
 enum { WIDE_OUT = 1, WIDE_PRE = 2, WIDE_RES = 4, WIDE_BIAS = 8 };
@@ -69,7 +69,7 @@ struct LinearGradArgs {
     int chunks, strips;                  // of rows, of columns
     int lanes;                           // lanes of a warp that share a row (a power of two); the others take further rows
 };
-// rows of h whose label takes part (zeros for the others), next to each other; the weights' common power of two
+// rows of h whose label takes part (zeros for the others), next to each other; the weights' common factor
 struct HeadPrepArgs {
     int64_t rows, ld_h, ld_copy;
     int hidden, vocab, dtype;
@@ -77,7 +77,7 @@ struct HeadPrepArgs {
     const int32_t *label;
     const float *dloss;
     void *copy;
-    float *scale;                        // 2^-s, 2^s
+    float *scale;                        // the factor's reciprocal, the factor
 };
 struct HeadFinishArgs {
     int64_t rows;
