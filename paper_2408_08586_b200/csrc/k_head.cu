@@ -49,6 +49,7 @@ template <typename T> __global__ void __launch_bounds__(PREP_THREADS) head_prep_
     for (int64_t i = first; i < all; i += step) {
         const uint4 v = takes_part(a.label[row], a.vocab) ? load_any(static_cast<const T *>(a.h) + row * a.ld_h, int64_t(u) * 8, int64_t(a.hidden)) : uint4{};
         *reinterpret_cast<uint4 *>(static_cast<T *>(a.copy) + row * a.ld_copy + u * 8) = v;
+        if (a.twice) *reinterpret_cast<uint4 *>(static_cast<T *>(a.copy) + (a.rows + row) * a.ld_copy + u * 8) = v;
         row += down; u += along;
         if (u >= units) { u -= units; ++row; }
     }

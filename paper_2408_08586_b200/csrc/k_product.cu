@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             if (shared_tiles) {
                 share_m0 = int64_t(tm) * BM;
                 share_col = int64_t(tn) * SINGLE_COLS + (lane & 15) * 8;
-                if (share_col < cols && share_m0 + share_row < rows) {         // (asked for while the sums are still made)
+                if (share_col < cols && share_m0 + share_row < (FEW && a.fold ? a.fold : rows)) {      // (asked for while the sums are still made)
                     finish.load_bias(share_col, share_bias);
                     finish.load_residual(share_m0 + share_row, share_col, share_residual);
                 }
@@ -545,7 +545,18 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                             p.x = pack_pair(v[8 * q], v[8 * q + 1], T()) & mask; p.y = pack_pair(v[8 * q + 2], v[8 * q + 3], T()) & mask;
                             p.z = pack_pair(v[8 * q + 4], v[8 * q + 5], T()) & mask; p.w = pack_pair(v[8 * q + 6], v[8 * q + 7], T()) & mask;
                             if constexpr (!FEW) *reinterpret_cast<uint4 *>(mine + lane * 128 + (((h * 4 + q) ^ (lane & 7)) << 4)) = p;
-                            else if (in && n0 + q * 8 < finish.ld_out) *reinterpret_cast<uint4 *>(finish.out + row * finish.ld_out + n0 + q * 8) = p;
+                            else if (in && n0 + q * 8 < finish.ld_out) {
+                                *reinterpret_cast<uint4 *>(finish.out + row * finish.ld_out + n0 + q * 8) = p;
+                                if (a.in_two) {
+                                    float high[8];
+                                    unpack16<T>(p, high);
+#pragma unroll
+                                    for (int e = 0; e < 8; ++e) high[e] = v[8 * q + e] - high[e];
+                                    uint4 low = pack16<T>(high);
+                                    low.x &= mask; low.y &= mask; low.z &= mask; low.w &= mask;
+                                    *reinterpret_cast<uint4 *>(finish.out + (rows + row) * finish.ld_out + n0 + q * 8) = low;
+                                }
+                            }
                         }
                     }
                     if constexpr (FEW) break;
@@ -564,18 +575,20 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
             // the blocks' shares added up in their order
             cluster_sync();
             if ((FEW || ranks > 1) && first < end && !*given_up) {
-                const int64_t rows = work.a[which].m, cols = work.a[which].n;
+                const int fold = FEW ? work.a[which].fold : 0;
+                const int64_t rows = fold ? fold : work.a[which].m, cols = work.a[which].n;
                 const uint32_t from_rank = cluster_rank() - rank;
                 for (int r = share_row; r < BM && share_m0 + r < rows; r += READERS * 2 * int(ranks)) {
                     const uint32_t from = stages + r * SHARE_LINE + (lane & 15) * 32;
                     float v[8] = {};
+                    for (uint32_t below = 0; below <= uint32_t(fold); below += fold ? fold : 1)
 #pragma unroll
                     for (int g = 0; g < 8; g += 4) {               // four at a time
                         float4 x[4], y[4];
 #pragma unroll
                         for (int s = 0; s < 4; ++s)
                             if (g + s < int(ranks)) {
-                                const uint32_t there = at_rank(from, from_rank + g + s);
+                                const uint32_t there = at_rank(from + below * SHARE_LINE, from_rank + g + s);
                                 asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[s].x), "=f"(x[s].y), "=f"(x[s].z), "=f"(x[s].w) : "r"(there));
                                 asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(y[s].x), "=f"(y[s].y), "=f"(y[s].z), "=f"(y[s].w) : "r"(there + 16));
                             }
@@ -713,6 +726,7 @@ ProductWay way_of(ProductKind kind, const ProductArgs &a, int num_sms)
     const int64_t steps = (a.k + BK - 1) / BK;
     ProductWay best = {SHAPE_SINGLE, SINGLE_COLS, 1, 1, 3e38f, 0};
     for (const int cols : {256, 192, 128}) {
+        if (a.fold || a.in_two) break;
         if (kind != PRODUCT_OUT && cols != PAIR_COLS) continue;
         const int64_t tiles = ((a.m + 255) / 256) * ((a.n + cols - 1) / cols), places = num_sms / 2;
         for (int s = 1; s <= 8; ++s) {
@@ -725,7 +739,7 @@ ProductWay way_of(ProductKind kind, const ProductArgs &a, int num_sms)
     }
     // single blocks: 128 x 128 sums, or few rows
     for (const Shape shape : {SHAPE_SINGLE, SHAPE_FEW}) {
-        if (shape == SHAPE_FEW && (a.m > FEW_ROWS || !a.a.along_k)) continue;
+        if (shape == SHAPE_FEW ? a.m > FEW_ROWS || !a.a.along_k : a.fold || a.in_two) continue;
         const int cols = shape == SHAPE_FEW ? int(a.m + 15) / 16 * 16 : SINGLE_COLS;
         const int64_t tiles = (shape == SHAPE_FEW ? 1 : (a.m + 127) / 128) * ((a.n + 127) / 128);
         const float each = (A_BYTES + cols * 128) * (0.33f / STAGE);
@@ -841,6 +855,8 @@ size_t plan_products(ProductKind kind, ProductArgs *a, int n, int num_sms)
     }
     return floats;
 }
+
+bool product_few(int64_t rows) { return 2 * rows <= FEW_ROWS; }
 
 bool product_keeps(const ProductArgs &a, int num_sms) { return way_of(PRODUCT_STATS, a, num_sms).shape != SHAPE_FEW; }
 

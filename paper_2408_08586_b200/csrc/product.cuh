@@ -35,6 +35,7 @@ struct ProductArgs {
     size_t part_at;                      // where they begin in the launch's scratch, in floats
     ProductWay way;
     bool beside;                         // one of the two gradients of a product
+    int fold;                            // rows fold .. 2 fold - 1 are added to the first ones (0: they are rows like others)
     // PRODUCT_STATS, PRODUCT_GRAD: the logits of vocabulary first .. first + n - 1; with `out`, PRODUCT_STATS keeps there the
     // exponentials of their distances to their pair's maximum, times KEPT
     const int32_t *label;
@@ -43,6 +44,7 @@ struct ProductArgs {
     float *at_label;                     // [m] logit of the label
     const float *base, *rest;            // log of the row's sum of exponentials, in two parts (rest may be NULL)
     const float *dloss, *up;             // [m] weight of a row (NULL: 1), and the weights' common factor
+    bool in_two;                         // PRODUCT_GRAD writes m more rows: what the first ones lack by their rounding
     uint32_t *status;
 };
 enum { WIDE_OUT = 1, WIDE_PRE = 2, WIDE_RES = 4, WIDE_BIAS = 8 };
@@ -77,6 +79,7 @@ struct HeadPrepArgs {
     const int32_t *label;
     const float *dloss;
     void *copy;
+    bool twice;                          // the copy's rows once more behind them
     float *scale;                        // the factor's reciprocal, the factor
 };
 struct HeadFinishArgs {
@@ -98,6 +101,7 @@ struct LayOutArgs {
 // and by how their operands lie (along_k has to be there already), and the floats of scratch that this takes.
 size_t plan_products(ProductKind kind, ProductArgs *a, int n, int num_sms);
 cudaError_t launch_products(ProductKind kind, ProductArgs *a, int n, float *part, int num_sms, cudaStream_t st);
+bool product_few(int64_t rows);                                      // whether PRODUCT_GRAD can write that many rows in two
 bool product_keeps(const ProductArgs &a, int num_sms);               // whether PRODUCT_STATS can keep the exponentials
 int64_t product_stats_pairs(const ProductArgs &a, int num_sms);      // pairs (maximum, sum) of a row that the logits come in
 bool product_takes(const Operand &o);                            // as it lies, that is

@@ -212,12 +212,16 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     const bool copied = backward && d_dw;
     Operand hidden = {d_h, d.ld_h, 1};
     const Laid laid_h = copied ? Laid{} : plan_operand(parts, hidden, d.rows, d.hidden);
-    const size_t at_copy = copied ? parts.take(size_t(d.rows) * ld_copy * 2) : 0;
+    // Few rows: dz is kept in two numbers of 16 bits, the second one in rows of its own, which cost the products next to nothing.
+    // (A row's gradient is mostly its label's entry, so with a handful of rows one rounding decides how far it is off.)
+    const bool in_two = backward && product_few(d.rows);
+    const int64_t dz_rows = in_two ? 2 * d.rows : d.rows;
+    const size_t at_copy = copied ? parts.take(size_t(dz_rows) * ld_copy * 2) : 0;
     const size_t at_stats = forward ? parts.take(size_t(tiles) * d.rows * sizeof(float2)) : 0, at_label = forward ? parts.take(size_t(d.rows) * 4) : 0;
     const size_t at_base = forward && backward ? parts.take(size_t(d.rows) * 4) : 0, at_rest = forward && backward ? parts.take(size_t(d.rows) * 4) : 0;
     const size_t at_scale = backward ? parts.take(8) : 0;
     // the vocabulary of a piece: as much as 512 MB of dz take, in whole tiles
-    int64_t piece = (int64_t(512) << 20) / (2 * d.rows) / 256 * 256;
+    int64_t piece = (int64_t(512) << 20) / (2 * dz_rows) / 256 * 256;
     if (piece < 256) piece = 256;
     if (piece > d.vocab) piece = d.vocab;
     const int64_t ld_dz = up8(piece);
@@ -226,22 +230,23 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     // working the logits out again: three products, not four (2,048 x 4,096 x 128,000 bf16 5.3 ms, 7.0 with four).  It pays
     // where a product costs more than reading and writing dz once: from 640 features on (4,096 x 32,000: 768 features 642 us,
     // 664 with four; 512: 490 and 471), or where dz stays in L2 (1,024 x 256 x 16,000 89 us, 98; 512 x 256 x 50,000 151, 147).
-    const bool kept = forward && backward && !several && (d.hidden >= 640 || d.rows * ld_dz * 2 <= 40 << 20) && product_keeps(z, ctx->num_sms);
-    const size_t at_dz = backward ? parts.take(size_t(d.rows) * ld_dz * 2) : 0;
+    const bool kept = forward && backward && !several && !in_two && (d.hidden >= 640 || d.rows * ld_dz * 2 <= 40 << 20) && product_keeps(z, ctx->num_sms);
+    const size_t at_dz = backward ? parts.take(size_t(dz_rows) * ld_dz * 2) : 0;
     const size_t at_acc = backward && several && d_dh ? parts.take(size_t(d.rows) * ld_copy * 4) : 0;
     size_t sums = 0;
     auto gradient_products = [&](int64_t first, int64_t n, ProductArgs &h, ProductArgs &w) {
         h = ProductArgs{}; w = ProductArgs{};
         h.dtype = w.dtype = d.dtype;
         h.status = w.status = ctx->d_status;
-        h.m = d.rows; h.n = d.hidden; h.k = n;
+        h.m = dz_rows; h.n = d.hidden; h.k = n;
+        h.fold = in_two ? int(d.rows) : 0;
         h.a.along_k = 1;
         h.beside = w.beside = true;
         h.ld_out = d.ld_h; h.ld_acc = ld_copy;
         h.b = Operand{static_cast<const char *>(weight.p) + (by_output ? first * weight.ld : first) * 2, weight.ld, !by_output};
         h.out = d_dh;
         h.wide = wide16(d_dh, d.ld_h) ? WIDE_OUT : 0;
-        w.k = d.rows;
+        w.k = dz_rows;
         w.ld_out = d.ld_w;
         w.wide = wide16(d_dw, d.ld_w) ? WIDE_OUT : 0;
         if (by_output) { w.m = n; w.n = d.hidden; w.out = static_cast<char *>(d_dw) + first * d.ld_w * 2; }
@@ -260,7 +265,7 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
 
     HeadPrepArgs pre = {};
     pre.rows = d.rows; pre.ld_h = d.ld_h; pre.ld_copy = ld_copy; pre.hidden = d.hidden; pre.vocab = d.vocab; pre.dtype = d.dtype;
-    pre.h = d_h; pre.label = d_label; pre.dloss = d_dloss;
+    pre.h = d_h; pre.label = d_label; pre.dloss = d_dloss; pre.twice = in_two;
     if (copied) { pre.copy = part<void>(ctx, at_copy); hidden = Operand{pre.copy, ld_copy, 1}; }
     if (backward) {
         pre.scale = part<float>(ctx, at_scale);
@@ -286,7 +291,7 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     if (!backward) return RUBICK_OK;
     z.base = forward ? part<float>(ctx, at_base) : d_lse_in;
     z.rest = forward ? part<float>(ctx, at_rest) : nullptr;
-    z.dloss = d_dloss; z.up = pre.scale + 1;
+    z.dloss = d_dloss; z.up = pre.scale + 1; z.in_two = in_two;
     for (int64_t first = 0; first < d.vocab; first += piece) {
         const int64_t n = first + piece < d.vocab ? piece : d.vocab - first;
         ProductArgs g[2], &h = g[0], &w = g[1];
