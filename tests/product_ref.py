@@ -44,8 +44,11 @@ def act(z, name):
             "gelu_tanh": lambda: f.gelu(z, approximate="tanh"), "silu": lambda: f.silu(z)}[name]()
 
 
+DEVICE = "cpu"           # large products are worked out on the GPU, by torch in double precision
+
+
 def d64(t):
-    return None if t is None else t.detach().double().cpu()
+    return None if t is None else t.detach().double().to(DEVICE)
 
 
 def linear_forward(x, w, bias=None, residual=None, *, activation="none", by_output=False, seed=None, p=0.0):
@@ -55,7 +58,7 @@ def linear_forward(x, w, bias=None, residual=None, *, activation="none", by_outp
     z, size = x @ w, x.abs() @ w.abs()
     if bias is not None:
         z, size = z + bias, size + bias.abs()
-    factor = keep(seed, *z.shape, p)
+    factor = keep(seed, *z.shape, p).to(z.device)
     out = act(z, activation) * factor
     out = torch.where(factor == 0, 0.0, out)
     size_out = 1.2 * size * factor                     # (no activation's slope exceeds 1.2)
@@ -67,7 +70,7 @@ def linear_forward(x, w, bias=None, residual=None, *, activation="none", by_outp
 def linear_backward(x, w, pre, dout, *, activation="none", by_output=False, seed=None, p=0.0):
     """-> {name: (gradient, term size)}"""
     x, w, pre, dout = map(d64, (x, w, pre, dout))
-    factor = keep(seed, *dout.shape, p)
+    factor = keep(seed, *dout.shape, p).to(dout.device)
     dz = torch.where(factor == 0, 0.0, dout * factor)
     if activation != "none":
         z = pre.clone().requires_grad_()
@@ -86,7 +89,7 @@ def head(h, w, label, dloss=None, *, by_output=False, lse=None):
     """-> {name: (value, term size)}; rows without a label are left out whatever they hold"""
     h, w, dloss, lse = map(d64, (h, w, dloss, lse))
     w = w.t() if by_output else w                      # [hidden, vocab]
-    label = label.long().cpu()
+    label = label.long().to(h.device)
     live = (label >= 0) & (label < w.shape[1])
     h = torch.where(live[:, None], h, 0.0)
     z, size = h @ w, h.abs() @ w.abs()
@@ -94,7 +97,7 @@ def head(h, w, label, dloss=None, *, by_output=False, lse=None):
     total = torch.logsumexp(z, 1)
     worst = size.max(1)[0]
     got = {"loss": (torch.where(live, total - z.gather(1, at)[:, 0], 0.0), worst), "lse": (torch.where(live, total, 0.0), worst)}
-    g = torch.ones(len(h), dtype=torch.float64) if dloss is None else dloss
+    g = torch.ones(len(h), dtype=torch.float64, device=h.device) if dloss is None else dloss
     g = torch.where(live, g, 0.0)
     p = torch.exp(z - (total if lse is None else lse)[:, None])
     hit = torch.zeros_like(z).scatter_(1, at, 1.0)
