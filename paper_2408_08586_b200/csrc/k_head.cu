@@ -33,7 +33,7 @@ template <typename T> __global__ void __launch_bounds__(PREP_THREADS) head_prep_
         __syncthreads();
         if (threadIdx.x == 0) {
             for (int w = 1; w < PREP_THREADS / 32; ++w) top = fmaxf(top, tops[w]);
-            const float up = top > 0.f ? fminf(fmaxf(16384.f / top, 0x1p-100f), 0x1p100f) : 1.f;
+            const float up = top > 0.f ? fminf(16384.f / top, 0x1p126f) : 1.f;
             a.scale[0] = 1.f / up;
             a.scale[1] = up;
         }
