@@ -612,7 +612,9 @@ typedef struct {
  * d_bias and d_residual may be NULL; d_pre (optional) receives z for the backward pass (act is taken from z before it is
  * rounded).  d_seed is read where p > 0 and may be NULL otherwise.  d_out may equal d_residual.  Products are summed in
  * single precision.  Rows of x and w on 16-byte boundaries are read as they lie; others are laid out anew in the context's
- * scratch first, which also holds single-precision sums where the inputs are dealt out (up to 8 times rows x outputs).
+ * scratch first, which also holds single-precision sums where the inputs are dealt out (up to 8 times rows x outputs, or
+ * 5,000,000; where sums have more than 131,072 products, rows x outputs for every 131,072 of them).  The same goes for the
+ * sums of the gradients.
  * Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
 int rubick_linear_forward(rubick_ctx *ctx, const rubick_linear_desc *h_desc, const void *d_x, const void *d_w,
                           const void *d_bias, const void *d_residual, const uint64_t *d_seed, void *d_pre, void *d_out);
@@ -667,7 +669,8 @@ int rubick_head_loss_forward(rubick_ctx *ctx, const rubick_head_loss_desc *h_des
 /* dz = d_dloss[n] (exp(z - lse) - onehot(label)),  dh = dz W^T,  dw = h^T dz (laid out as w), with forward's d_lse; rows
  * without a label add nothing and get zeros.  d_dloss NULL = 1.  d_dh or d_dw may be NULL: it is not computed.  The logits
  * are computed again, a piece of the vocabulary at a time; dz of a piece is rounded to dtype under a common factor.
- * The context keeps the piece (up to 512 MB, or 256 tokens), a copy of h and, with several pieces, dh in single precision.
+ * The context keeps the piece (up to 512 MB and 524,288 tokens, or 256 tokens), a copy of h and, with several pieces, dh in
+ * single precision, besides what the products keep (as above).
  * d_lse is one float: rows whose logits are all far from zero want the step below.  rows = 0 writes zeros to dw.
  * Errors: EINVAL, ENOMEM, ESTATE, ECUDA. */
 int rubick_head_loss_backward(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *d_h, const void *d_w,

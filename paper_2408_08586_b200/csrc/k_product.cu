@@ -718,6 +718,10 @@ int resident_clusters(int size)
     return n;
 }
 
+// Stages that are summed up in tensor memory at most.  What is cut off there grows with their number (sums of 2,000,000 positive
+// products in one go are 0.5 % short, of 131,072 less than half a step of bfloat16), so longer sums are dealt out.
+constexpr int64_t LONGEST = 2048;
+
 // How a product is cut.  What a way takes is estimated in microseconds from measured times: a stage of 32 KB a block takes
 // 0.33 (256 x 256 sums of a pair as well as 128 x 128 of a single block: it is the fetching that lasts, 97 GB/s a
 // multiprocessor), smaller stages as much less; what does not depend on the tiles is 8 for a pair and 6 for a single block.
@@ -729,11 +733,16 @@ ProductWay way_of(ProductKind kind, const ProductArgs &a, int num_sms)
         if (a.fold || a.in_two) break;
         if (kind != PRODUCT_OUT && cols != PAIR_COLS) continue;
         const int64_t tiles = ((a.m + 255) / 256) * ((a.n + cols - 1) / cols), places = num_sms / 2;
-        for (int s = 1; s <= 8; ++s) {
-            if (s > 1 && (kind != PRODUCT_OUT || steps < 8 * s || tiles > 64 * places)) break;       // (what many tiles would gain is too little)
+        // up to eight splits, or as many as make few tiles one for every pair (two 64-column operands of 262,144 rows: 198 us with
+        // eight blocks of a cluster, 72 so)
+        const int64_t whole = tiles < places ? places / tiles : 0;
+        for (int64_t i = 1; i <= 9; ++i) {
+            int64_t s = i <= 8 ? i : whole;
+            if (s * LONGEST < steps && kind == PRODUCT_OUT) s = (steps + LONGEST - 1) / LONGEST;
+            else if (s < 1 || (s > 1 && (kind != PRODUCT_OUT || steps < 8 * s || tiles > 64 * places))) continue;       // (what many tiles would gain is too little)
             const int64_t per = (steps + s - 1) / s, splits = (steps + per - 1) / per, waves = (tiles * splits + places - 1) / places;
             const float each = (A_BYTES + (a.b.along_k ? cols / 2 * 128 : (cols / 2 + 63) / 64 * int(BLOCK_BYTES))) * (0.33f / STAGE);
-            const float cost = float(waves) * float(per) * each + 8.f + (splits > 1 ? 4.f + float(splits) * float(a.m) * float(a.n) * 2e-6f : 0.f);
+            const float cost = float(waves) * float(per) * each + 8.f + (splits > 1 ? 4.f + float(splits) * (0.1f + float(a.m) * float(a.n) * 2e-6f) : 0.f);
             if (cost < best.cost) best = ProductWay{SHAPE_PAIR, cols, 1, int(splits), cost, 2 * tiles * splits};
         }
     }
@@ -745,6 +754,7 @@ ProductWay way_of(ProductKind kind, const ProductArgs &a, int num_sms)
         const float each = (A_BYTES + cols * 128) * (0.33f / STAGE);
         for (int s = 1; s <= 8; s *= 2) {
             if (s > 1 && (kind != PRODUCT_OUT || steps < 2 * s || tiles > resident_clusters(s))) break;
+            if (kind == PRODUCT_OUT && s * LONGEST < steps && !a.fold) continue;
             const int64_t per = (steps + s - 1) / s, waves = (tiles + num_sms - 1) / num_sms;
             if ((steps + per - 1) / per != s) continue;          // (no block is left without work)
             // (a gradient has another one beside it, which has no few rows: two launches instead of one)

@@ -220,9 +220,10 @@ int head_loss(rubick_ctx *ctx, const rubick_head_loss_desc *h_desc, const void *
     const size_t at_stats = forward ? parts.take(size_t(tiles) * d.rows * sizeof(float2)) : 0, at_label = forward ? parts.take(size_t(d.rows) * 4) : 0;
     const size_t at_base = forward && backward ? parts.take(size_t(d.rows) * 4) : 0, at_rest = forward && backward ? parts.take(size_t(d.rows) * 4) : 0;
     const size_t at_scale = backward ? parts.take(8) : 0;
-    // the vocabulary of a piece: as much as 512 MB of dz take, in whole tiles
+    // the vocabulary of a piece: as much as 512 MB of dz take, in whole tiles, and no longer than sums in tensor memory should be
     int64_t piece = (int64_t(512) << 20) / (2 * dz_rows) / 256 * 256;
     if (piece < 256) piece = 256;
+    if (piece > 1 << 19) piece = 1 << 19;
     if (piece > d.vocab) piece = d.vocab;
     const int64_t ld_dz = up8(piece);
     const bool several = piece < d.vocab;

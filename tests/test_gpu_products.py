@@ -509,6 +509,41 @@ def test_head_loss_with_closed_tokens_and_small_weights(ctx):
     assert (off <= 1e-9 * 2.0 ** -10 * size + 2.0 ** -24).all()
 
 
+def test_head_loss_with_the_largest_weights(ctx):
+    """Loss weights near single precision's largest: half precision's gradients overflow to infinities of the right sign, never
+    to NaN, and bfloat16's are as exact as others."""
+    import torch
+    for rows in (20, 40):
+        for dtype, weight in (("fp16", 1e38), ("bf16", 1e34)):
+            desc, h, w, label, _, _ = head_case(rows, 32, 500, dtype, {})
+            dloss = torch.full((rows,), weight, device="cuda")
+            loss, lse = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+            dw = torch.empty_like(w)
+            ctx.head_loss_step(desc, h, w, label, dloss, loss, lse, None, dw)
+            want, size, _ = ref.head(h, w, label, dloss)["dw"]
+            got = dw.double().cpu()
+            assert not torch.isnan(got).any()
+            sure = want.abs() > 2.0 ** -6 * size
+            if dtype == "fp16":
+                assert (got[sure] == torch.copysign(torch.tensor(float("inf"), dtype=torch.float64), want[sure])).all()
+            else:
+                assert ((got - want).abs() <= 2.0 ** -7 * (want.abs() + size)).all()
+
+
+def test_sums_over_millions_of_rows(ctx):
+    """2^21 positive products a sum, which tensor memory must not sum in one go: half precision's rounding (2^-11) and what sums of
+    131,072 are cut off by at most (8,192 joins of 2^-23 each: 2^-10)."""
+    import torch
+    rows = 1 << 21
+    g = torch.Generator(device="cuda").manual_seed(11)
+    x, dout = (torch.rand(rows, n, generator=g, device="cuda").mul_(0.125).half() for n in (24, 72))
+    dw = torch.empty(24, 72, dtype=torch.float16, device="cuda")
+    ctx.linear_backward(rb.linear(rows, 24, 72, torch.float16), x, dw, None, None, dout, None, dw)
+    ctx.sync()
+    want = x.double().t() @ dout.double()
+    assert float(((dw.double() - want).abs() / want).max()) <= 2.0 ** -11 + 2.0 ** -10
+
+
 def test_results_do_not_depend_on_what_ran_before(ctx):
     """Twice the same call gives the same bits, with other calls of the context in between."""
     import torch
