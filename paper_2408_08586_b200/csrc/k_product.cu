@@ -161,7 +161,8 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
 
     if (warp < FIRST_READER) {
         if constexpr (KIND == PRODUCT_STATS && PAIR) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHERS_REGISTERS));
-        if (warp == 0 && lane == 0) {
+        if (warp == 0 || warp == 3) {                // one fetches A, one B: a thread's copies go out one after the other
+            const bool one = elected(), fetches_a = warp == 0;
             uint32_t round = 0, i = first;           // stages filled so far, tile
             bool fine = true;
             const uint32_t bar0 = PAIR ? at_rank(full, 0) : full;
@@ -183,14 +184,22 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                     const uint32_t bytes = t.bytes * CTAS;
                     for (int k = k0; k < k1; ++k, ++round) {
                         const uint32_t s = round % STAGES, into = stages + s * STAGE, bar = bar0 + 8 * s;
-                        if (!(fine = barrier_wait(empty + 8 * s, (round / STAGES & 1) ^ 1, given_up))) break;
-                        if (!PAIR || rank == 0) barrier_expect(full + 8 * s, bytes);
-                        if (ak) tensor_load<PAIR>(into, &maps.a[which], k * BK, m0, bar);
-                        else
-                            for (int j = 0; j < BM / 64; ++j) tensor_load<PAIR>(into + j * BLOCK_BYTES, &maps.a[which], m0 + 64 * j, k * BK, bar);
-                        if (bk) tensor_load<PAIR>(into + A_BYTES, &maps.b[which], k * BK, n0, bar);
-                        else
-                            for (int j = 0; j < blocks; ++j) tensor_load<PAIR>(into + A_BYTES + j * BLOCK_BYTES, &maps.b[which], n0 + 64 * j, k * BK, bar);
+                        if (!(fine = __all_sync(0xffffffffu, barrier_wait(empty + 8 * s, (round / STAGES & 1) ^ 1, given_up)))) break;
+                        if (one && fetches_a) {
+                            if (!PAIR || rank == 0) barrier_expect(full + 8 * s, bytes);
+                            if (ak) tensor_load<PAIR>(into, &maps.a[which], k * BK, m0, bar);
+                            else {
+#pragma unroll
+                                for (int j = 0; j < BM / 64; ++j) tensor_load<PAIR>(into + j * BLOCK_BYTES, &maps.a[which], m0 + 64 * j, k * BK, bar);
+                            }
+                        } else if (one) {
+                            if (bk) tensor_load<PAIR>(into + A_BYTES, &maps.b[which], k * BK, n0, bar);
+                            else {
+                                tensor_load<PAIR>(into + A_BYTES, &maps.b[which], n0, k * BK, bar);
+                                if (blocks > 1) tensor_load<PAIR>(into + A_BYTES + BLOCK_BYTES, &maps.b[which], n0 + 64, k * BK, bar);
+                            }
+                        }
+                        __syncwarp();
                     }
                 }
             };
@@ -202,7 +211,8 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                 for (uint32_t r = round > STAGES ? round - STAGES : 0; r < round; ++r) barrier_wait(full + 8 * (r % STAGES), r / STAGES & 1, &never);
             }
         }
-        if (warp == 1 && lane == 0 && (!PAIR || rank == 0)) {
+        if (warp == 1 && (!PAIR || rank == 0)) {
+            const bool one = elected();
             uint32_t round = 0, tile = 0, i = first;
             bool fine = true;
             auto sum = [&](auto number) {
@@ -219,17 +229,22 @@ __global__ void __launch_bounds__(THREADS, 1) product_kernel(const __grid_consta
                     for (int k = k0; fine && k < k1; ++tile) {
                         const int stop = KIND == PRODUCT_STATS && k + SUM_STEPS < k1 ? k + SUM_STEPS : k1;
                         const uint32_t half = tile & 1, d = tmem + half * HALF;
-                        if (!(fine = barrier_wait(taken + 8 * half, (tile / 2 & 1) ^ 1, given_up))) break;
+                        if (!(fine = __all_sync(0xffffffffu, barrier_wait(taken + 8 * half, (tile / 2 & 1) ^ 1, given_up)))) break;
                         tcgen_after_sync();
                         for (bool add = false; k < stop; ++k, ++round) {
                             const uint32_t s = round % STAGES, at = s * (STAGE >> 4);
-                            if (!(fine = barrier_wait(full + 8 * s, round / STAGES & 1, given_up))) break;
+                            if (!(fine = __all_sync(0xffffffffu, barrier_wait(full + 8 * s, round / STAGES & 1, given_up)))) break;
                             tcgen_after_sync();
+                            if (one) {
 #pragma unroll
-                            for (int q = 0; q < BK / 16; ++q, add = true) multiply<PAIR>(d, da + at + q * sa, db + at + q * sb, desc, add);
-                            multiplied<PAIR>(empty + 8 * s);
+                                for (int q = 0; q < BK / 16; ++q) multiply<PAIR>(d, da + at + q * sa, db + at + q * sb, desc, add || q);
+                                multiplied<PAIR>(empty + 8 * s);
+                            }
+                            add = true;
+                            __syncwarp();
                         }
-                        if (fine) multiplied<PAIR>(done + 8 * half);
+                        if (fine && one) multiplied<PAIR>(done + 8 * half);
+                        __syncwarp();
                     }
                 }
             };
@@ -722,9 +737,9 @@ int resident_clusters(int size)
 // products in one go are 0.5 % short, of 131,072 less than half a step of bfloat16), so longer sums are dealt out.
 constexpr int64_t LONGEST = 2048;
 
-// How a product is cut.  What a way takes is estimated in microseconds from measured times: a stage of 32 KB a block takes
-// 0.33 (256 x 256 sums of a pair as well as 128 x 128 of a single block: it is the fetching that lasts, 97 GB/s a
-// multiprocessor), smaller stages as much less; what does not depend on the tiles is 8 for a pair and 6 for a single block.
+// How a product is cut.  What a way takes is estimated in microseconds from measured times: a stage takes a pair 0.32 with 256
+// columns, 0.25 with 192, 0.21 with 128, a single block of 128 x 128 sums 0.26, smaller ones as much less as they fetch, however
+// the operands lie; what does not depend on the tiles is 6 for a pair and 4 for a single block.
 ProductWay way_of(ProductKind kind, const ProductArgs &a, int num_sms)
 {
     const int64_t steps = (a.k + BK - 1) / BK;
@@ -741,8 +756,7 @@ ProductWay way_of(ProductKind kind, const ProductArgs &a, int num_sms)
             if (s * LONGEST < steps && kind == PRODUCT_OUT) s = (steps + LONGEST - 1) / LONGEST;
             else if (s < 1 || (s > 1 && (kind != PRODUCT_OUT || steps < 8 * s || tiles > 64 * places))) continue;       // (what many tiles would gain is too little)
             const int64_t per = (steps + s - 1) / s, splits = (steps + per - 1) / per, waves = (tiles * splits + places - 1) / places;
-            const float each = (A_BYTES + (a.b.along_k ? cols / 2 * 128 : (cols / 2 + 63) / 64 * int(BLOCK_BYTES))) * (0.33f / STAGE);
-            const float cost = float(waves) * float(per) * each + 8.f + (splits > 1 ? 4.f + float(splits) * (0.1f + float(a.m) * float(a.n) * 2e-6f) : 0.f);
+            const float cost = float(waves) * float(per) * (0.1f + float(cols) * 0.00086f) + 6.f + (splits > 1 ? 4.f + float(splits) * (0.1f + float(a.m) * float(a.n) * 2e-6f) : 0.f);
             if (cost < best.cost) best = ProductWay{SHAPE_PAIR, cols, 1, int(splits), cost, 2 * tiles * splits};
         }
     }
@@ -751,14 +765,14 @@ ProductWay way_of(ProductKind kind, const ProductArgs &a, int num_sms)
         if (shape == SHAPE_FEW ? a.m > FEW_ROWS || !a.a.along_k : a.fold || a.in_two) continue;
         const int cols = shape == SHAPE_FEW ? int(a.m + 15) / 16 * 16 : SINGLE_COLS;
         const int64_t tiles = (shape == SHAPE_FEW ? 1 : (a.m + 127) / 128) * ((a.n + 127) / 128);
-        const float each = (A_BYTES + cols * 128) * (0.33f / STAGE);
+        const float each = (A_BYTES + cols * 128) * (0.26f / STAGE);
         for (int s = 1; s <= 8; s *= 2) {
             if (s > 1 && (kind != PRODUCT_OUT || steps < 2 * s || tiles > resident_clusters(s))) break;
             if (kind == PRODUCT_OUT && s * LONGEST < steps && !a.fold) continue;
             const int64_t per = (steps + s - 1) / s, waves = (tiles + num_sms - 1) / num_sms;
             if ((steps + per - 1) / per != s) continue;          // (no block is left without work)
             // (a gradient has another one beside it, which has no few rows: two launches instead of one)
-            const float cost = float(waves) * float(per) * each + 6.f + (s > 1 ? 1.f : 0.f) + (shape == SHAPE_FEW && a.beside ? 3.f : 0.f);
+            const float cost = float(waves) * float(per) * each + 4.f + (s > 1 ? 1.f : 0.f) + (shape == SHAPE_FEW && a.beside ? 3.f : 0.f);
             if (cost < best.cost) best = ProductWay{shape, cols, s, 1, cost, tiles * s};
         }
     }
