@@ -1,9 +1,20 @@
 // Matrix products of a training step with their epilogues, on the tensor cores.
 //
 // D[m][n] = sum_k A[m][k] B[n][k], operands of 16 bits, sums in single precision.  A persistent block (or a pair of blocks on
-// neighbouring multiprocessors, which share the tile's columns of B) takes tile after tile.  One thread has the tensor-copy
-// engine fetch 64 k of both operands into a ring of stages, one thread multiplies them into tensor memory, and eight warps
+// neighbouring multiprocessors, which share the tile's columns of B) takes tile after tile.  Two warps have the tensor-copy
+// engine fetch 64 k of an operand each into a ring of stages, one warp multiplies them into tensor memory, and eight warps
 // take a finished tile out of it while the next one is multiplied into its other half.
+//
+// These warps go through their loops whole, and one elected thread issues: in a branch of a single lane the compiler moves
+// every operand of a copy or product to a uniform register as if lanes could differ, which cost 0.35 us a stage of a pair
+// whatever its width; now it is 0.32 with 256 columns, 0.25 with 192, 0.21 with 128.
+//
+// What bounds it: large products the tensor cores at the clock that the card's power allows (8,192 x 4,096 -> 16,384 bf16 with
+// gelu and pre kept 724 us alone, 1.52 PFLOP/s, 843 between other work; 4,096 x 2,048 -> 8,192 90 us); products of fewer tiles
+// than pairs the length of one tile and 5 us before and behind it (2,048 x 5,120 -> 1,280 fp16 56 tiles of 192 columns on 74
+// pairs, 25 to 29 us); a few rows the weights' way from memory (32 x 768 -> 50,257 18.6 us, 4.1 TB/s with all that comes after
+// it; 4 x 4,096 -> 4,096 9.1 us, of which 5 are a launch's); little depth the sums' way out (16,384 x 64 -> 16,384 136 us,
+// 4 TB/s).  Half of the ring's stages do as well for a single tile; a large product lost 10 % with three.
 #include <atomic>
 #include <type_traits>
 
