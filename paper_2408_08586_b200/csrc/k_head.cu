@@ -1,7 +1,7 @@
 // The head's cross entropy: what runs before and after the products of its logits.
 //
-// All of it is bound by memory or by one trip to it: head_prep copies h (730 x 805 4 us), head_finish reads 8 bytes per row
-// and 64 or 128 tokens (4 to 6 us), head_scale reads and writes dz once (2,048 x 128,000 bf16 177 us, 5.9 TB/s).
+// All of it is bound by memory or by one trip to it: head_prep copies h (2,048 x 4,096 9 us), head_finish reads 8 bytes per
+// row and 64 or 128 tokens (5 to 9 us), head_scale reads and writes dz once (2,048 x 128,000 bf16 177 us, 5.9 TB/s).
 #include "product.cuh"
 
 namespace rubick {
